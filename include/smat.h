@@ -420,6 +420,112 @@ smat_status smat_merge_ties_thresholds(const smat_merge_tensor* tensors, int32_t
                                        const smat_merge_config* cfg, const void* d_workspace,
                                        uint32_t* d_out, smat_stream_t stream);
 
+/* ----------------------------------------------------------- linear layers ---
+ * The products of a linear layer (the tensors of the mask set S, Sec. 4.1: attention and MLP weights) with
+ * what surrounds them, and activations saved in 8 bits for the backward pass. The model's forward and backward
+ * pass on theta~ or theta is made of them; the paper fixes none of it.
+ *
+ *   smat_linear        h = x W^T + b,  y = act(h) + residual, and on request h saved in 8 bits
+ *   smat_grad_input    dx = (dy W) * act'(h^),                h^ read from its 8 bits
+ *   smat_grad_weight   dW = dy^T x^, db = sum over rows of dy; x^ = act(8-bit values), or x as it is
+ *   smat_pack8, smat_unpack8, smat_act_grad8                  a matrix saved, read back through an
+ *                                                             activation, and dy * act'(h^)
+ *
+ * Matrices are row-major with a row stride ("ld", in elements, at least the number of columns); x is [rows, k],
+ * W [n, k], y, dy and residual [rows, n], dx [rows, k], dW [n, k], bias and db [n]. One dtype per call. Sums
+ * are held in fp32 and rounded once, when a result is written; a bf16 call multiplies bf16 values on the tensor
+ * cores (x^ is rounded to bf16 first, as the layer's input was in the forward pass). Results do not depend on
+ * timing: no sum is joined by atomics.
+ *
+ * 8 bits: a row is cut into groups of SMAT_PACK8_GROUP columns (the last may be shorter). Group g of a row has
+ * one byte e and stands for q * 2^(e - 127), q its int8 values: 2^(e - 127) is the smallest power of two, from
+ * 2^-126 on, with which every |q| is at most 127, q = round(x / 2^(e - 127)), ties to even. bf16 holds every such
+ * value exactly. A group with an infinity or NaN has e = 255: its infinities read back as they were and
+ * everything else in it as NaN, so that an overflow stays visible. q is [rows, columns] with row stride ldq, e is
+ * [rows, ceil(columns / 32)] with row stride lde.
+ *
+ * rows, k and n may be 0 (sums over nothing are 0). Outputs must not overlap inputs or one another, except that
+ * y may be the residual itself (same pointer and stride). */
+typedef enum {
+  SMAT_ACT_NONE = 0,
+  SMAT_ACT_RELU = 1,
+  SMAT_ACT_GELU = 2,       /* h Phi(h) */
+  SMAT_ACT_GELU_TANH = 3,  /* h (1 + tanh(sqrt(2 / pi) (h + 0.044715 h^3))) / 2 */
+  SMAT_ACT_QUICK_GELU = 4, /* h sigmoid(1.702 h) */
+  SMAT_ACT_SILU = 5        /* h sigmoid(h) */
+} smat_act;
+
+#define SMAT_PACK8_GROUP 32
+
+typedef struct {
+  const void* x;
+  const void* w;
+  const void* bias;     /* or NULL */
+  const void* residual; /* or NULL */
+  void* y;
+  int8_t* q;  /* h in 8 bits: q and e, or both NULL */
+  uint8_t* e;
+  int64_t rows, k, n;
+  int64_t ldx, ldw, ldr, ldy, ldq, lde;
+  int32_t dtype; /* smat_dtype of x, w, bias, residual and y */
+  int32_t act;   /* smat_act */
+} smat_linear_args;
+
+typedef struct {
+  const void* dy;
+  const void* w;
+  const int8_t* q; /* h^ [rows, k] in 8 bits; both NULL with SMAT_ACT_NONE */
+  const uint8_t* e;
+  void* dx;
+  int64_t rows, k, n;
+  int64_t lddy, ldw, ldq, lde, lddx;
+  int32_t dtype;
+  int32_t act;
+} smat_grad_input_args;
+
+/* smat_grad_weight_args.accumulate: add to what dw / db hold. */
+#define SMAT_ACCUMULATE_DW 1
+#define SMAT_ACCUMULATE_DB 2
+
+typedef struct {
+  const void* dy;
+  const void* x;   /* x [rows, k] (act must be SMAT_ACT_NONE), or NULL and */
+  const int8_t* q; /* its 8 bits, read through act */
+  const uint8_t* e;
+  void* dw;
+  void* db; /* or NULL */
+  int64_t rows, k, n;
+  int64_t lddy, ldx, ldq, lde, lddw;
+  int32_t dtype;
+  int32_t act;
+  int32_t accumulate;
+  int32_t reserved; /* 0 */
+} smat_grad_weight_args;
+
+/* Bytes of device workspace a call needs (0 where it needs none, and on invalid arguments, which the call itself
+ * reports). */
+size_t smat_linear_workspace_bytes(const smat_linear_args* args);
+size_t smat_grad_input_workspace_bytes(const smat_grad_input_args* args);
+size_t smat_grad_weight_workspace_bytes(const smat_grad_weight_args* args);
+
+/* Enqueue one operator on `stream`. d_workspace: device memory of at least the bytes above, 256-byte aligned, not
+ * in use by another call until this one's work has finished (NULL where 0 bytes are needed). */
+smat_status smat_linear(const smat_linear_args* args, void* d_workspace, size_t workspace_bytes,
+                        smat_stream_t stream);
+smat_status smat_grad_input(const smat_grad_input_args* args, void* d_workspace, size_t workspace_bytes,
+                            smat_stream_t stream);
+smat_status smat_grad_weight(const smat_grad_weight_args* args, void* d_workspace, size_t workspace_bytes,
+                             smat_stream_t stream);
+
+/* x [rows, cols] of dtype saved in 8 bits; act applied to saved values (out of dtype); and dy * act'(saved). */
+smat_status smat_pack8(const void* x, int64_t ldx, int8_t* q, int64_t ldq, uint8_t* e, int64_t lde, int64_t rows,
+                       int64_t cols, int32_t dtype, smat_stream_t stream);
+smat_status smat_unpack8(const int8_t* q, int64_t ldq, const uint8_t* e, int64_t lde, void* out, int64_t ldout,
+                         int64_t rows, int64_t cols, int32_t dtype, int32_t act, smat_stream_t stream);
+smat_status smat_act_grad8(const void* dy, int64_t lddy, const int8_t* q, int64_t ldq, const uint8_t* e,
+                           int64_t lde, void* out, int64_t ldout, int64_t rows, int64_t cols, int32_t dtype,
+                           int32_t act, smat_stream_t stream);
+
 /* SMAT_ABI_VERSION of the loaded library. */
 int32_t smat_abi_version(void);
 

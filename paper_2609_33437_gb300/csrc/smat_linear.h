@@ -1,0 +1,54 @@
+// What the host side of the linear layers (smat_linear_host.cpp) and their kernels share.
+#pragma once
+
+#include <cstdint>
+
+#include <cuda_runtime.h>
+
+#include "smat.h"
+
+namespace smat {
+namespace lin {
+
+// What happens to a product's sums on their way out.
+enum Mode : int { kForward = 0, kGradInput = 1, kGradWeight = 2 };
+
+// One product: out(i, j) from sum over l of A(i, l) B(j, l), i < I, j < J, l < L. An operand with the sum running
+// along its rows ("K-major") has A(i, l) at a[i * lda + l]; one with the sum running down its columns ("MN-major")
+// at a[l * lda + i]:
+//   forward      A = x [rows, k]   B = W [n, k]   both K-major
+//   grad_input   A = dy [rows, n]  K-major, B = W [n, k] MN-major, j runs over k
+//   grad_weight  A = dy [rows, n]  B = x [rows, k] both MN-major, i over n and j over k
+struct Product {
+  int mode;  // Mode
+  int dtype;
+  const void* a;
+  const void* b;
+  int64_t lda, ldb;
+  int64_t I, J, L;
+  // the epilogue
+  const void* bias;      // [J]
+  const void* residual;  // [I, J]
+  void* out;             // [I, J]
+  int8_t* q;             // [I, J]: written by the forward, read by grad_input
+  uint8_t* e;
+  int64_t ldr, ldo, ldq, lde;
+  int act;
+  int accumulate;  // grad_weight: add to what out holds
+};
+
+// SIMT kernels (smat_linear_simt.cu): any type, size, stride and alignment.
+cudaError_t launch_simt(const Product& p, int sms, cudaStream_t s);
+
+// smat_pack8.cu; `dy` NULL: out = act(h^), else dy * act'(h^)
+cudaError_t launch_pack8(const void* x, int64_t ldx, int8_t* q, int64_t ldq, uint8_t* e, int64_t lde, int64_t rows,
+                         int64_t cols, int dtype, int sms, cudaStream_t s);
+cudaError_t launch_unpack8(const int8_t* q, int64_t ldq, const uint8_t* e, int64_t lde, const void* dy, int64_t lddy,
+                           void* out, int64_t ldout, int64_t rows, int64_t cols, int dtype, int act, int sms,
+                           cudaStream_t s);
+// db[n] = sum over rows of dy[rows, n], or added to db
+cudaError_t launch_row_sums(const void* dy, int64_t lddy, void* db, int64_t rows, int64_t cols, int dtype, bool add,
+                            int sms, cudaStream_t s);
+
+}  // namespace lin
+}  // namespace smat

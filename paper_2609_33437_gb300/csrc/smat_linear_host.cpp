@@ -1,0 +1,299 @@
+// Host side of the linear layers (include/smat.h): argument checks, workspace, launches.
+
+#include <cstdarg>
+#include <cstdio>
+
+#include <cuda_runtime.h>
+
+#include "smat.h"
+#include "smat_internal.h"
+#include "smat_linear.h"
+
+using namespace smat;
+using namespace smat::lin;
+
+namespace {
+
+smat_status lfail(smat_status st, const char* fmt, ...) {
+  char buf[512];
+  va_list ap;
+  va_start(ap, fmt);
+  std::vsnprintf(buf, sizeof(buf), fmt, ap);
+  va_end(ap);
+  return (smat_status)record_error_code(st, buf);
+}
+
+smat_status cuda_status(cudaError_t e, const char* what) {
+  if (e == cudaSuccess) return SMAT_OK;
+  return lfail(SMAT_ERR_CUDA, "%s: %s (%s)", what, cudaGetErrorName(e), cudaGetErrorString(e));
+}
+
+// Sizes are below 2^31 - 2^16, so that kernels can round them up and count in 32 bits (offsets are 64 bits wide).
+// The second size of a result (n of linear and grad_weight, k of grad_input) is cut into at most 65535 tiles.
+constexpr int64_t kMaxSize = (int64_t(1) << 31) - (1 << 16);
+constexpr int64_t kMaxCols = int64_t(65535) * 64;
+
+size_t elem_of(int32_t dtype) { return dtype == SMAT_BF16 ? 2 : 4; }
+
+// One matrix argument; `cols` 0 or `rows` 0: nothing is read.
+struct Mat {
+  const char* name;
+  const void* p;
+  int64_t rows, cols, ld;
+  size_t elem;
+  bool written;
+  bool empty() const { return rows == 0 || cols == 0; }
+  uintptr_t begin() const { return (uintptr_t)p; }
+  uintptr_t end() const { return begin() + ((size_t)(rows - 1) * (size_t)ld + (size_t)cols) * elem; }
+};
+
+// Whether two matrices share an element. Views of one buffer with one row stride whose columns lie apart (the
+// slices of a joint projection) do not.
+bool overlap(const Mat& a, const Mat& b) {
+  if (a.empty() || b.empty() || a.end() <= b.begin() || b.end() <= a.begin()) return false;
+  const uintptr_t stride = (uintptr_t)a.ld * a.elem;
+  if (stride != (uintptr_t)b.ld * b.elem || stride == 0) return true;
+  const Mat &lo = a.begin() <= b.begin() ? a : b, &hi = a.begin() <= b.begin() ? b : a;
+  const uintptr_t off = (hi.begin() - lo.begin()) % stride;
+  return off < (uintptr_t)lo.cols * lo.elem || off + (uintptr_t)hi.cols * hi.elem > stride;
+}
+
+smat_status check_sizes(int64_t rows, int64_t k, int64_t n, int32_t dtype, int32_t act) {
+  const int64_t sizes[3] = {rows, k, n};
+  const char* names[3] = {"rows", "k", "n"};
+  for (int i = 0; i < 3; ++i)
+    if (sizes[i] < 0 || sizes[i] > (i == 0 ? kMaxSize : kMaxCols))
+      return lfail(SMAT_ERR_INVALID_ARG, "%s %lld out of range", names[i], (long long)sizes[i]);
+  if (dtype != SMAT_F32 && dtype != SMAT_BF16) return lfail(SMAT_ERR_UNSUPPORTED, "dtype %d not supported", dtype);
+  if (act < SMAT_ACT_NONE || act > SMAT_ACT_SILU) return lfail(SMAT_ERR_UNSUPPORTED, "activation %d not supported", act);
+  return SMAT_OK;
+}
+
+// `same`: two matrices that may be one and the same (or -1)
+smat_status check_mats(const Mat* m, int count, int same_a, int same_b) {
+  for (int i = 0; i < count; ++i) {
+    if (m[i].empty()) continue;
+    if (!m[i].p) return lfail(SMAT_ERR_INVALID_ARG, "%s is NULL", m[i].name);
+    if (m[i].ld < m[i].cols || m[i].ld > (int64_t(1) << 40))
+      return lfail(SMAT_ERR_INVALID_ARG, "%s: row stride %lld for %lld columns", m[i].name, (long long)m[i].ld,
+                   (long long)m[i].cols);
+    if ((uintptr_t)m[i].p % m[i].elem)
+      return lfail(SMAT_ERR_ALIGNMENT, "%s: not aligned to %zu bytes", m[i].name, m[i].elem);
+  }
+  for (int i = 0; i < count; ++i) {
+    if (!m[i].written) continue;
+    for (int j = 0; j < count; ++j) {
+      if (i == j || (m[j].written && j < i)) continue;
+      if ((i == same_a && j == same_b) && m[i].p == m[j].p && m[i].ld == m[j].ld) continue;
+      if (overlap(m[i], m[j]))
+        return lfail(SMAT_ERR_INVALID_ARG, "%s overlaps %s", m[i].name, m[j].name);
+    }
+  }
+  GpuAccess access;
+  for (int i = 0; i < count; ++i) {
+    if (m[i].empty()) continue;
+    const int ok = access.check(m[i].p);
+    if (ok < 0) return lfail(SMAT_ERR_CUDA, "no current CUDA device or pointer attributes unavailable");
+    if (!ok) return lfail(SMAT_ERR_INVALID_ARG, "%s is not accessible from the GPU", m[i].name);
+  }
+  return SMAT_OK;
+}
+
+smat_status device_sms(int* sms) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev);
+  return cuda_status(e, "device query");
+}
+
+int64_t groups_of(int64_t cols) { return (cols + SMAT_PACK8_GROUP - 1) / SMAT_PACK8_GROUP; }
+
+constexpr size_t kWsAlign = 256;
+size_t up(size_t x) { return (x + kWsAlign - 1) / kWsAlign * kWsAlign; }
+
+smat_status check_workspace(const void* d_workspace, size_t bytes, size_t needed) {
+  if (needed == 0) return SMAT_OK;
+  if (!d_workspace) return lfail(SMAT_ERR_WORKSPACE, "workspace is NULL");
+  if ((uintptr_t)d_workspace % kWsAlign) return lfail(SMAT_ERR_WORKSPACE, "workspace not 256-byte aligned");
+  if (bytes < needed) return lfail(SMAT_ERR_WORKSPACE, "workspace %zu bytes < %zu needed", bytes, needed);
+  return SMAT_OK;
+}
+
+// grad_weight with x^ in 8 bits: x^ as values, rows padded to 64 bytes
+int64_t values_ld(const smat_grad_weight_args* a) { return (a->k + 31) / 32 * 32; }
+size_t values_bytes(const smat_grad_weight_args* a) {
+  return a->q && a->rows > 0 && a->n > 0 ? up((size_t)a->rows * (size_t)values_ld(a) * elem_of(a->dtype)) : 0;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t smat_linear_workspace_bytes(const smat_linear_args*) { return 0; }
+size_t smat_grad_input_workspace_bytes(const smat_grad_input_args*) { return 0; }
+size_t smat_grad_weight_workspace_bytes(const smat_grad_weight_args* a) {
+  if (!a || a->rows < 0 || a->rows > kMaxSize || a->k < 0 || a->k > kMaxCols) return 0;
+  return values_bytes(a);
+}
+
+smat_status smat_linear(const smat_linear_args* a, void*, size_t, smat_stream_t stream) {
+  if (!a) return lfail(SMAT_ERR_INVALID_ARG, "args is NULL");
+  smat_status st = check_sizes(a->rows, a->k, a->n, a->dtype, a->act);
+  if (st != SMAT_OK) return st;
+  if (!a->q != !a->e) return lfail(SMAT_ERR_INVALID_ARG, "q and e: give both or neither");
+  const size_t es = elem_of(a->dtype);
+  const int64_t m = a->rows, k = a->k, n = a->n;
+  const Mat mats[] = {
+      {"y", a->y, m, n, a->ldy, es, true},
+      {"q", a->q, a->q ? m : 0, n, a->ldq, 1, true},
+      {"e", a->e, a->e ? m : 0, groups_of(n), a->lde, 1, true},
+      {"x", a->x, n ? m : 0, k, a->ldx, es, false},
+      {"w", a->w, m ? n : 0, k, a->ldw, es, false},
+      {"bias", a->bias, m && a->bias ? 1 : 0, n, n, es, false},
+      {"residual", a->residual, a->residual ? m : 0, n, a->ldr, es, false},
+  };
+  st = check_mats(mats, 7, 0, 6);
+  if (st != SMAT_OK || m == 0 || n == 0) return st;
+  int sms = 1;
+  st = device_sms(&sms);
+  if (st != SMAT_OK) return st;
+  Product p = {};
+  p.mode = kForward;
+  p.dtype = a->dtype;
+  p.a = a->x, p.b = a->w, p.lda = a->ldx, p.ldb = a->ldw;
+  p.I = m, p.J = n, p.L = k;
+  p.bias = a->bias, p.residual = a->residual, p.out = a->y, p.q = a->q, p.e = a->e;
+  p.ldr = a->ldr, p.ldo = a->ldy, p.ldq = a->ldq, p.lde = a->lde;
+  p.act = a->act;
+  return cuda_status(launch_simt(p, sms, stream), "linear launch");
+}
+
+smat_status smat_grad_input(const smat_grad_input_args* a, void*, size_t, smat_stream_t stream) {
+  if (!a) return lfail(SMAT_ERR_INVALID_ARG, "args is NULL");
+  smat_status st = check_sizes(a->rows, a->k, a->n, a->dtype, a->act);
+  if (st != SMAT_OK) return st;
+  const bool act = a->act != SMAT_ACT_NONE;
+  if (act != (a->q != nullptr) || act != (a->e != nullptr))
+    return lfail(SMAT_ERR_INVALID_ARG, "q and e: give both with an activation, neither without");
+  const size_t es = elem_of(a->dtype);
+  const int64_t m = a->rows, k = a->k, n = a->n;
+  const Mat mats[] = {
+      {"dx", a->dx, m, k, a->lddx, es, true},
+      {"dy", a->dy, k ? m : 0, n, a->lddy, es, false},
+      {"w", a->w, m ? n : 0, k, a->ldw, es, false},
+      {"q", a->q, act ? m : 0, k, a->ldq, 1, false},
+      {"e", a->e, act ? m : 0, groups_of(k), a->lde, 1, false},
+  };
+  st = check_mats(mats, 5, -1, -1);
+  if (st != SMAT_OK || m == 0 || k == 0) return st;
+  int sms = 1;
+  st = device_sms(&sms);
+  if (st != SMAT_OK) return st;
+  Product p = {};
+  p.mode = kGradInput;
+  p.dtype = a->dtype;
+  p.a = a->dy, p.b = a->w, p.lda = a->lddy, p.ldb = a->ldw;
+  p.I = m, p.J = k, p.L = n;
+  p.out = a->dx, p.q = const_cast<int8_t*>(a->q), p.e = const_cast<uint8_t*>(a->e);
+  p.ldo = a->lddx, p.ldq = a->ldq, p.lde = a->lde;
+  p.act = a->act;
+  return cuda_status(launch_simt(p, sms, stream), "grad_input launch");
+}
+
+smat_status smat_grad_weight(const smat_grad_weight_args* a, void* d_workspace, size_t workspace_bytes,
+                             smat_stream_t stream) {
+  if (!a) return lfail(SMAT_ERR_INVALID_ARG, "args is NULL");
+  smat_status st = check_sizes(a->rows, a->k, a->n, a->dtype, a->act);
+  if (st != SMAT_OK) return st;
+  if (!a->q != !a->e) return lfail(SMAT_ERR_INVALID_ARG, "q and e: give both or neither");
+  const int64_t m = a->rows, k = a->k, n = a->n;
+  const bool some = m > 0 && k > 0 && n > 0;
+  if (some && !a->x == !a->q) return lfail(SMAT_ERR_INVALID_ARG, "give x, or q and e, not both");
+  if (!a->q && a->act != SMAT_ACT_NONE)
+    return lfail(SMAT_ERR_INVALID_ARG, "an activation is applied to x in 8 bits only");
+  if ((a->accumulate & ~(SMAT_ACCUMULATE_DW | SMAT_ACCUMULATE_DB)) || a->reserved)
+    return lfail(SMAT_ERR_UNSUPPORTED, "unknown accumulate flags 0x%x", a->accumulate);
+  const size_t es = elem_of(a->dtype);
+  const Mat mats[] = {
+      {"dw", a->dw, n, k, a->lddw, es, true},
+      {"db", a->db, a->db ? 1 : 0, n, n, es, true},
+      {"dy", a->dy, m, n, a->lddy, es, false},
+      {"x", a->x, n && a->x ? m : 0, k, a->ldx, es, false},
+      {"q", a->q, n && a->q ? m : 0, k, a->ldq, 1, false},
+      {"e", a->e, n && a->e ? m : 0, groups_of(k), a->lde, 1, false},
+  };
+  st = check_mats(mats, 6, -1, -1);
+  if (st != SMAT_OK || n == 0) return st;
+  st = check_workspace(d_workspace, workspace_bytes, values_bytes(a));
+  if (st != SMAT_OK) return st;
+  int sms = 1;
+  st = device_sms(&sms);
+  if (st != SMAT_OK) return st;
+  if (a->db) {
+    st = cuda_status(launch_row_sums(a->dy, a->lddy, a->db, m, n, a->dtype, a->accumulate & SMAT_ACCUMULATE_DB, sms,
+                                     stream), "row sums launch");
+    if (st != SMAT_OK) return st;
+  }
+  if (k == 0) return SMAT_OK;
+  const void* x = a->x;
+  int64_t ldx = a->ldx;
+  if (a->q && m > 0) {
+    x = d_workspace;
+    ldx = values_ld(a);
+    st = cuda_status(launch_unpack8(a->q, a->ldq, a->e, a->lde, nullptr, 0, d_workspace, ldx, m, k, a->dtype, a->act,
+                                    sms, stream), "unpack launch");
+    if (st != SMAT_OK) return st;
+  }
+  Product p = {};
+  p.mode = kGradWeight;
+  p.dtype = a->dtype;
+  p.a = a->dy, p.b = x, p.lda = a->lddy, p.ldb = ldx;
+  p.I = n, p.J = k, p.L = m;
+  p.out = a->dw, p.ldo = a->lddw;
+  p.accumulate = a->accumulate & SMAT_ACCUMULATE_DW;
+  return cuda_status(launch_simt(p, sms, stream), "grad_weight launch");
+}
+
+static smat_status elementwise(const char* what, const void* dy, int64_t lddy, const int8_t* q, int64_t ldq,
+                               const uint8_t* e, int64_t lde, void* out, int64_t ldout, int64_t rows, int64_t cols,
+                               int32_t dtype, int32_t act, bool pack, bool slope, smat_stream_t stream) {
+  smat_status st = check_sizes(rows, cols, 0, dtype, act);
+  if (st != SMAT_OK) return st;
+  const size_t es = elem_of(dtype);
+  const Mat mats[] = {
+      {pack ? "x" : "out", out, rows, cols, ldout, es, !pack},
+      {"q", q, rows, cols, ldq, 1, pack},
+      {"e", e, rows, groups_of(cols), lde, 1, pack},
+      {"dy", dy, slope ? rows : 0, cols, lddy, es, false},
+  };
+  st = check_mats(mats, 4, -1, -1);
+  if (st != SMAT_OK || rows == 0 || cols == 0) return st;
+  int sms = 1;
+  st = device_sms(&sms);
+  if (st != SMAT_OK) return st;
+  return cuda_status(pack ? launch_pack8(out, ldout, const_cast<int8_t*>(q), ldq, const_cast<uint8_t*>(e), lde, rows,
+                                         cols, dtype, sms, stream)
+                          : launch_unpack8(q, ldq, e, lde, dy, lddy, out, ldout, rows, cols, dtype, act, sms, stream),
+                     what);
+}
+
+smat_status smat_pack8(const void* x, int64_t ldx, int8_t* q, int64_t ldq, uint8_t* e, int64_t lde, int64_t rows,
+                       int64_t cols, int32_t dtype, smat_stream_t stream) {
+  return elementwise("pack8 launch", nullptr, 0, q, ldq, e, lde, const_cast<void*>(x), ldx, rows, cols, dtype,
+                     SMAT_ACT_NONE, true, false, stream);
+}
+
+smat_status smat_unpack8(const int8_t* q, int64_t ldq, const uint8_t* e, int64_t lde, void* out, int64_t ldout,
+                         int64_t rows, int64_t cols, int32_t dtype, int32_t act, smat_stream_t stream) {
+  return elementwise("unpack8 launch", nullptr, 0, q, ldq, e, lde, out, ldout, rows, cols, dtype, act, false, false,
+                     stream);
+}
+
+smat_status smat_act_grad8(const void* dy, int64_t lddy, const int8_t* q, int64_t ldq, const uint8_t* e, int64_t lde,
+                           void* out, int64_t ldout, int64_t rows, int64_t cols, int32_t dtype, int32_t act,
+                           smat_stream_t stream) {
+  return elementwise("act_grad8 launch", dy, lddy, q, ldq, e, lde, out, ldout, rows, cols, dtype, act, false, true,
+                     stream);
+}
+
+}  // extern "C"

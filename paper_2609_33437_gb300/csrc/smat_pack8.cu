@@ -1,0 +1,286 @@
+// Activations in 8 bits (include/smat.h, "linear layers"): a matrix saved, read back through an activation, a
+// gradient times the activation's slope at saved values, and a gradient's sums over its rows.
+//
+// All four are one pass over memory. A thread takes 16 columns of a row at a time: 32 bytes of bf16 (one 256-bit
+// access, a whole sector) and 16 bytes of q; the two threads of a group of 32 exchange their largest magnitude by
+// one shuffle. Rows whose pointers or strides do not allow that are taken element by element.
+
+#include "smat_linear.cuh"
+#include "smat_linear.h"
+
+namespace smat {
+namespace lin {
+namespace {
+
+constexpr int kUnit = 16;      // columns per thread and step
+constexpr int kThreads = 256;  // of the elementwise kernels
+
+template <class T>
+__device__ __forceinline__ void load_unit(const T* p, int count, bool vec, float (&v)[kUnit]) {
+  if (vec && count == kUnit) {
+    if constexpr (sizeof(T) == 2) {
+      uint32_t w[8];
+      asm volatile("ld.global.nc.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                   : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
+                   : "l"(p));
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        v[2 * i] = __uint_as_float(w[i] << 16);
+        v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+      }
+    } else {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        asm volatile("ld.global.nc.v8.f32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                     : "=f"(v[8 * h]), "=f"(v[8 * h + 1]), "=f"(v[8 * h + 2]), "=f"(v[8 * h + 3]), "=f"(v[8 * h + 4]),
+                       "=f"(v[8 * h + 5]), "=f"(v[8 * h + 6]), "=f"(v[8 * h + 7])
+                     : "l"(p + 8 * h));
+    }
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < kUnit; ++i) v[i] = i < count ? to_float(p[i]) : 0.0f;
+}
+
+template <class T>
+__device__ __forceinline__ void store_unit(T* p, int count, bool vec, const float (&v)[kUnit]) {
+  if (vec && count == kUnit) {
+    if constexpr (sizeof(T) == 2) {
+      uint32_t w[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+        w[i] = *reinterpret_cast<const uint32_t*>(&b);
+      }
+      asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]),
+                   "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+                   : "memory");
+    } else {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        asm volatile("st.global.v8.f32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p + 8 * h), "f"(v[8 * h]),
+                     "f"(v[8 * h + 1]), "f"(v[8 * h + 2]), "f"(v[8 * h + 3]), "f"(v[8 * h + 4]), "f"(v[8 * h + 5]),
+                     "f"(v[8 * h + 6]), "f"(v[8 * h + 7])
+                     : "memory");
+    }
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < kUnit; ++i)
+    if (i < count) p[i] = from_float<T>(v[i]);
+}
+
+__device__ __forceinline__ void load_q(const int8_t* p, int count, bool vec, uint32_t (&w)[4]) {
+  if (vec && count == kUnit) {
+    const uint4 u = __ldg(reinterpret_cast<const uint4*>(p));
+    w[0] = u.x, w[1] = u.y, w[2] = u.z, w[3] = u.w;
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = 0;
+#pragma unroll
+  for (int i = 0; i < kUnit; ++i)
+    if (i < count) w[i / 4] |= (uint32_t)(uint8_t)p[i] << (8 * (i % 4));
+}
+
+// The threads' walk over a matrix: blockDim.x threads side by side along a row, blockDim.y rows, steps of the grid.
+// Units come in pairs (a group of 32), so both threads of a pair run every step.
+#define SMAT_EACH_UNIT(cols, rows)                                                                     \
+  const int pairs = (int)(((cols) + kGroup - 1) / kGroup) * 2;                                         \
+  for (int64_t r = (int64_t)blockIdx.y * blockDim.y + threadIdx.y; r < (rows);                         \
+       r += (int64_t)gridDim.y * blockDim.y)                                                           \
+    for (int u = (int)(blockIdx.x * blockDim.x + threadIdx.x); u < pairs; u += (int)(gridDim.x * blockDim.x))
+
+template <class T>
+__global__ void __launch_bounds__(kThreads) pack8_kernel(const T* x, int64_t ldx, int8_t* q, int64_t ldq, uint8_t* e,
+                                                         int64_t lde, int64_t rows, int64_t cols, bool vx, bool vq) {
+  SMAT_EACH_UNIT(cols, rows) {
+    const int64_t c = (int64_t)u * kUnit;
+    const int count = (int)(cols - c < 0 ? 0 : (cols - c < kUnit ? cols - c : kUnit));
+    float v[kUnit];
+    load_unit(x + r * ldx + c, count, vx, v);
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < kUnit; ++i) top = max(top, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+    // the other half of the group: the neighbouring thread (blockDim.x is even, so both are in this warp and run
+    // the same steps)
+    const unsigned pair = 3u << ((threadIdx.x + threadIdx.y * blockDim.x) & 30);
+    top = max(top, __shfl_xor_sync(pair, top, 1));
+    const uint32_t ex = pack_exponent(top);
+    const float f = pack_factor(ex);
+    if ((u & 1) == 0) e[r * lde + u / 2] = (uint8_t)ex;
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      w[i] = pack_value(v[4 * i], f) | pack_value(v[4 * i + 1], f) << 8 | pack_value(v[4 * i + 2], f) << 16 |
+             pack_value(v[4 * i + 3], f) << 24;
+    int8_t* o = q + r * ldq + c;
+    if (vq && count == kUnit) {
+      *reinterpret_cast<uint4*>(o) = make_uint4(w[0], w[1], w[2], w[3]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kUnit; ++i)
+        if (i < count) o[i] = (int8_t)(w[i / 4] >> (8 * (i % 4)));
+    }
+  }
+}
+
+// out = act(h^), or dy * act'(h^) where DY
+template <class T, int ACT, bool DY>
+__global__ void __launch_bounds__(kThreads)
+    unpack8_kernel(const int8_t* q, int64_t ldq, const uint8_t* e, int64_t lde, const T* dy, int64_t lddy, T* out,
+                   int64_t ldout, int64_t rows, int64_t cols, bool vq, bool vdy, bool vout) {
+  SMAT_EACH_UNIT(cols, rows) {
+    const int64_t c = (int64_t)u * kUnit;
+    const int count = (int)(cols - c < 0 ? 0 : (cols - c < kUnit ? cols - c : kUnit));
+    if (count == 0) continue;
+    uint32_t w[4];
+    load_q(q + r * ldq + c, count, vq, w);
+    const float scale = unpack_scale(e[r * lde + u / 2]);
+    float v[kUnit];
+    if (DY) load_unit(dy + r * lddy + c, count, vdy, v);
+#pragma unroll
+    for (int i = 0; i < kUnit; ++i) {
+      const float h = unpack_value(w[i / 4], i % 4, scale);
+      v[i] = DY ? v[i] * act_slope<ACT>(h) : act_value<ACT>(h);
+    }
+    store_unit(out + r * ldout + c, count, vout, v);
+  }
+}
+
+// db[n] = sum over rows of dy (added to db where `add`). A CTA takes 64 columns and, with the other CTAs of its
+// cluster, every row: a thread adds 8 columns of every 32nd row of the CTA's share in fp32, shared memory joins the
+// threads, the first CTA of the cluster adds the shares in order. One launch, no atomics.
+constexpr int kSumCols = 64, kSumLanes = 8, kSumRows = kThreads / kSumLanes;
+
+template <class T>
+__global__ void __launch_bounds__(kThreads)
+    row_sums_kernel(const T* dy, int64_t lddy, T* db, int64_t rows, int64_t cols, bool vec, bool add) {
+  __shared__ float part[kSumRows][kSumCols + 1];
+  __shared__ float total[kSumCols];
+  const int lane = threadIdx.x % kSumLanes, row = threadIdx.x / kSumLanes;
+  const int64_t c = (int64_t)blockIdx.x * kSumCols + lane * 8;
+  const int count = (int)(cols - c < 0 ? 0 : (cols - c < 8 ? cols - c : 8));
+  float s[8] = {};
+  const int64_t step = (int64_t)kSumRows * gridDim.y;
+#pragma unroll 4
+  for (int64_t r = (int64_t)blockIdx.y * kSumRows + row; r < rows; r += step) {
+    const T* p = dy + r * lddy + c;
+    if (vec && count == 8) {
+      if constexpr (sizeof(T) == 2) {
+        const uint4 u = __ldg(reinterpret_cast<const uint4*>(p));
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          s[2 * i] += __uint_as_float(w[i] << 16);
+          s[2 * i + 1] += __uint_as_float(w[i] & 0xFFFF0000u);
+        }
+      } else {
+        const float4 a = __ldg(reinterpret_cast<const float4*>(p)), b = __ldg(reinterpret_cast<const float4*>(p) + 1);
+        s[0] += a.x, s[1] += a.y, s[2] += a.z, s[3] += a.w, s[4] += b.x, s[5] += b.y, s[6] += b.z, s[7] += b.w;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (i < count) s[i] += to_float(p[i]);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) part[row][lane * 8 + i] = s[i];
+  __syncthreads();
+  if (threadIdx.x < kSumCols) {
+    float t = 0.0f;
+    for (int i = 0; i < kSumRows; ++i) t += part[i][threadIdx.x];
+    total[threadIdx.x] = t;
+  }
+  cluster_sync();
+  const int64_t n = (int64_t)blockIdx.x * kSumCols + threadIdx.x;
+  if (blockIdx.y == 0 && threadIdx.x < kSumCols && n < cols) {
+    float t = 0.0f;
+    for (unsigned i = 0; i < gridDim.y; ++i) t += cluster_load(&total[threadIdx.x], i);
+    db[n] = from_float<T>(add ? to_float(db[n]) + t : t);
+  }
+  cluster_sync();  // the shares stay until they have been read
+}
+
+bool can(const void* p, int64_t ld, size_t elem, size_t bytes) {
+  return (uintptr_t)p % bytes == 0 && (uint64_t)ld * elem % bytes == 0;
+}
+
+struct Shape {
+  dim3 grid, block;
+};
+
+// A block is as wide as a row has units, at most 256 threads; the grid has enough blocks for eight per SM.
+Shape shape_of(int64_t rows, int64_t cols, int sms) {
+  const int64_t units = (cols + kGroup - 1) / kGroup * 2;
+  unsigned x = 2;
+  while (x < kThreads && x < units) x *= 2;
+  const unsigned y = kThreads / x;
+  const int64_t bx = (units + x - 1) / x, by = (rows + y - 1) / y;
+  const int64_t most = (int64_t)sms * 16;
+  const int64_t gx = bx < most ? bx : most;
+  int64_t gy = (most + gx - 1) / gx;
+  gy = gy < by ? gy : by;
+  return {dim3((unsigned)gx, (unsigned)(gy < 65535 ? gy : 65535)), dim3(x, y)};
+}
+
+template <class T, bool DY>
+cudaError_t unpack_as(const int8_t* q, int64_t ldq, const uint8_t* e, int64_t lde, const void* dy, int64_t lddy,
+                      void* out, int64_t ldout, int64_t rows, int64_t cols, int act, int sms, cudaStream_t s) {
+  const Shape h = shape_of(rows, cols, sms);
+  const bool vq = can(q, ldq, 1, 16), vdy = DY && can(dy, lddy, sizeof(T), 32), vout = can(out, ldout, sizeof(T), 32);
+  SMAT_WITH_ACT(act, (unpack8_kernel<T, ACT, DY><<<h.grid, h.block, 0, s>>>(
+                         q, ldq, e, lde, (const T*)dy, lddy, (T*)out, ldout, rows, cols, vq, vdy, vout)))
+  return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t launch_pack8(const void* x, int64_t ldx, int8_t* q, int64_t ldq, uint8_t* e, int64_t lde, int64_t rows,
+                         int64_t cols, int dtype, int sms, cudaStream_t s) {
+  const Shape h = shape_of(rows, cols, sms);
+  const bool vq = can(q, ldq, 1, 16);
+  if (dtype == SMAT_BF16)
+    pack8_kernel<__nv_bfloat16><<<h.grid, h.block, 0, s>>>((const __nv_bfloat16*)x, ldx, q, ldq, e, lde, rows, cols,
+                                                           can(x, ldx, 2, 32), vq);
+  else
+    pack8_kernel<float><<<h.grid, h.block, 0, s>>>((const float*)x, ldx, q, ldq, e, lde, rows, cols,
+                                                   can(x, ldx, 4, 32), vq);
+  return cudaGetLastError();
+}
+
+cudaError_t launch_unpack8(const int8_t* q, int64_t ldq, const uint8_t* e, int64_t lde, const void* dy, int64_t lddy,
+                           void* out, int64_t ldout, int64_t rows, int64_t cols, int dtype, int act, int sms,
+                           cudaStream_t s) {
+  if (dtype == SMAT_BF16)
+    return dy ? unpack_as<__nv_bfloat16, true>(q, ldq, e, lde, dy, lddy, out, ldout, rows, cols, act, sms, s)
+              : unpack_as<__nv_bfloat16, false>(q, ldq, e, lde, dy, lddy, out, ldout, rows, cols, act, sms, s);
+  return dy ? unpack_as<float, true>(q, ldq, e, lde, dy, lddy, out, ldout, rows, cols, act, sms, s)
+            : unpack_as<float, false>(q, ldq, e, lde, dy, lddy, out, ldout, rows, cols, act, sms, s);
+}
+
+cudaError_t launch_row_sums(const void* dy, int64_t lddy, void* db, int64_t rows, int64_t cols, int dtype, bool add,
+                            int sms, cudaStream_t s) {
+  const unsigned gx = (unsigned)((cols + kSumCols - 1) / kSumCols);
+  // as many CTAs per cluster as fill the chip with two each, at least 64 rows for each
+  unsigned split = 1;
+  while (split < 8 && gx * split < 2u * (unsigned)sms && (int64_t)split * 2 * 64 <= rows) split *= 2;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(gx, split);
+  cfg.blockDim = dim3(kThreads);
+  cfg.stream = s;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim = {1, split, 1};
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  if (dtype == SMAT_BF16)
+    return cudaLaunchKernelEx(&cfg, row_sums_kernel<__nv_bfloat16>, (const __nv_bfloat16*)dy, lddy, (__nv_bfloat16*)db,
+                              rows, cols, can(dy, lddy, 2, 16), add);
+  return cudaLaunchKernelEx(&cfg, row_sums_kernel<float>, (const float*)dy, lddy, (float*)db, rows, cols,
+                            can(dy, lddy, 4, 16), add);
+}
+
+}  // namespace lin
+}  // namespace smat

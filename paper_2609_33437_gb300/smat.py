@@ -31,7 +31,9 @@ EXPORTED = ("smat_workspace_bytes", "smat_init", "smat_simulate_multi", "smat_gr
             "smat_delta_sigma_noalloc", "smat_timing_enable", "smat_timing_read", "smat_status_string",
             "smat_last_error", "smat_abi_version", "smat_refill_theta0", "smat_mark_theta0_resident",
             "smat_merge_workspace_bytes", "smat_merge", "smat_merge_ties_thresholds",
-            "smat_grad_map_adamw_multi")
+            "smat_grad_map_adamw_multi", "smat_linear_workspace_bytes", "smat_grad_input_workspace_bytes",
+            "smat_grad_weight_workspace_bytes", "smat_linear", "smat_grad_input", "smat_grad_weight",
+            "smat_pack8", "smat_unpack8", "smat_act_grad8")
 
 
 class AdamW(ctypes.Structure):
@@ -110,6 +112,16 @@ def load_library(build_if_missing: bool = True) -> ctypes.CDLL:
     L.smat_debug_fused.argtypes = [P, U32, P, I32, U32, P]
     L.smat_delta_sigma_noalloc.argtypes = [P, P, I64, I32, ctypes.c_float, P, P]
     L.smat_delta_sigma_noalloc.restype = I32
+    for name in ("smat_linear", "smat_grad_input", "smat_grad_weight"):
+        getattr(L, name + "_workspace_bytes").argtypes = [P]
+        getattr(L, name + "_workspace_bytes").restype = ctypes.c_size_t
+        getattr(L, name).argtypes = [P, P, ctypes.c_size_t, P]
+        getattr(L, name).restype = I32
+    L.smat_pack8.argtypes = [P, I64, P, I64, P, I64, I64, I64, I32, P]
+    L.smat_unpack8.argtypes = [P, I64, P, I64, P, I64, I64, I64, I32, I32, P]
+    L.smat_act_grad8.argtypes = [P, I64, P, I64, P, I64, P, I64, I64, I64, I32, I32, P]
+    for name in ("smat_pack8", "smat_unpack8", "smat_act_grad8"):
+        getattr(L, name).restype = I32
     L.smat_timing_enable.argtypes = [P, I32]
     L.smat_timing_read.argtypes = [P, P, P]
     L.smat_status_string.argtypes = [I32]
