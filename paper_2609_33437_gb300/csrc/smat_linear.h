@@ -37,8 +37,13 @@ struct Product {
   int accumulate;  // grad_weight: add to what out holds
 };
 
-// SIMT kernels (smat_linear_simt.cu): any type, size, stride and alignment.
+// fp32 (smat_linear_simt.cu): any size, stride and alignment.
 cudaError_t launch_simt(const Product& p, int sms, cudaStream_t s);
+
+// bf16 on the tensor cores (smat_linear_tc.cu): a and b on 16-byte boundaries, lda and ldb multiples of 8.
+cudaError_t launch_tc(const Product& p, int sms, cudaStream_t s);
+// Reads and clears the tensor-core products' error bits; waits for the stream.
+cudaError_t read_errors(int* out, cudaStream_t s);
 
 // smat_pack8.cu; `dy` NULL: out = act(h^), else dy * act'(h^)
 cudaError_t launch_pack8(const void* x, int64_t ldx, int8_t* q, int64_t ldq, uint8_t* e, int64_t lde, int64_t rows,
@@ -49,6 +54,10 @@ cudaError_t launch_unpack8(const int8_t* q, int64_t ldq, const uint8_t* e, int64
 // db[n] = sum over rows of dy[rows, n], or added to db
 cudaError_t launch_row_sums(const void* dy, int64_t lddy, void* db, int64_t rows, int64_t cols, int dtype, bool add,
                             int sms, cudaStream_t s);
+
+// A bf16 matrix [rows, cols] copied to rows of stride ldto
+cudaError_t launch_copy_rows(const void* from, int64_t ld, void* to, int64_t ldto, int64_t rows, int64_t cols, int sms,
+                             cudaStream_t s);
 
 }  // namespace lin
 }  // namespace smat

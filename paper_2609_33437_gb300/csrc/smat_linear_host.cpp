@@ -119,24 +119,100 @@ smat_status check_workspace(const void* d_workspace, size_t bytes, size_t needed
   return SMAT_OK;
 }
 
-// grad_weight with x^ in 8 bits: x^ as values, rows padded to 64 bytes
-int64_t values_ld(const smat_grad_weight_args* a) { return (a->k + 31) / 32 * 32; }
-size_t values_bytes(const smat_grad_weight_args* a) {
-  return a->q && a->rows > 0 && a->n > 0 ? up((size_t)a->rows * (size_t)values_ld(a) * elem_of(a->dtype)) : 0;
+// The tensor-core products read bf16 operands whose rows start on 16 bytes. One that does not is copied to the
+// workspace first: rows of ld_of(cols) elements.
+int64_t ld_of(int64_t cols) { return (cols + 31) / 32 * 32; }
+size_t copy_bytes(int64_t rows, int64_t cols, size_t elem) { return up((size_t)rows * (size_t)ld_of(cols) * elem); }
+
+struct Operand {
+  const void* p;
+  int64_t rows, cols, ld;
+  bool copied;
+};
+Operand operand(const void* p, int64_t rows, int64_t cols, int64_t ld, int32_t dtype) {
+  Operand o = {p, rows, cols, ld, false};
+  if (dtype != SMAT_BF16 || rows == 0 || cols == 0) return o;
+  if (rows == 1) o.ld = ld_of(cols);  // any stride will do
+  o.copied = (uintptr_t)p % 16 || o.ld % 8;
+  return o;
+}
+size_t operand_bytes(const Operand& o) { return o.copied ? copy_bytes(o.rows, o.cols, 2) : 0; }
+
+// The operands of the three products, rows and columns as they lie in memory; of grad_weight's x^ in 8 bits, the
+// values it is read back to.
+struct Operands {
+  Operand a, b;
+  size_t values;  // bytes of grad_weight's x^
+  size_t bytes() const { return values + operand_bytes(a) + operand_bytes(b); }
+};
+Operands operands(const smat_linear_args* g) {
+  if (g->n == 0 || g->rows == 0) return {};
+  return {operand(g->x, g->rows, g->k, g->ldx, g->dtype), operand(g->w, g->n, g->k, g->ldw, g->dtype), 0};
+}
+Operands operands(const smat_grad_input_args* g) {
+  if (g->k == 0 || g->rows == 0) return {};
+  return {operand(g->dy, g->rows, g->n, g->lddy, g->dtype), operand(g->w, g->n, g->k, g->ldw, g->dtype), 0};
+}
+Operands operands(const smat_grad_weight_args* g) {
+  if (g->k == 0 || g->n == 0 || g->rows == 0) return {};
+  Operands o = {operand(g->dy, g->rows, g->n, g->lddy, g->dtype), {}, 0};
+  if (g->q)
+    o.values = copy_bytes(g->rows, g->k, elem_of(g->dtype));
+  else
+    o.b = operand(g->x, g->rows, g->k, g->ldx, g->dtype);
+  return o;
+}
+
+// Copies what has to be copied, then the product.
+smat_status run_product(Product& p, const Operands& o, char* d_workspace, int sms, cudaStream_t s, const char* what) {
+  const Operand* in[2] = {&o.a, &o.b};
+  const void** to[2] = {&p.a, &p.b};
+  int64_t* ld[2] = {&p.lda, &p.ldb};
+  for (int i = 0; i < 2; ++i) {
+    if (!in[i]->p) continue;
+    *to[i] = in[i]->p;
+    *ld[i] = in[i]->ld;
+    if (!in[i]->copied) continue;
+    *to[i] = d_workspace;
+    *ld[i] = ld_of(in[i]->cols);
+    const smat_status st = cuda_status(
+        launch_copy_rows(in[i]->p, in[i]->ld, d_workspace, *ld[i], in[i]->rows, in[i]->cols, sms, s), "copy launch");
+    if (st != SMAT_OK) return st;
+    d_workspace += operand_bytes(*in[i]);
+  }
+  return cuda_status(p.dtype == SMAT_BF16 ? launch_tc(p, sms, s) : launch_simt(p, sms, s), what);
+}
+
+// A call's size check without its message: what the size queries return 0 for.
+bool sizes_fit(int64_t rows, int64_t k, int64_t n) {
+  return rows >= 0 && rows <= kMaxSize && k >= 0 && k <= kMaxCols && n >= 0 && n <= kMaxCols;
+}
+
+// An exception (the host's memory running out) is a status like any other failure.
+template <class F>
+smat_status guarded(F&& f) {
+  try {
+    return f();
+  } catch (...) {
+    return SMAT_ERR_CUDA;
+  }
+}
+
+template <class A>
+size_t workspace_of(const A* a) {
+  return a && sizes_fit(a->rows, a->k, a->n) ? operands(a).bytes() : 0;
 }
 
 }  // namespace
 
 extern "C" {
 
-size_t smat_linear_workspace_bytes(const smat_linear_args*) { return 0; }
-size_t smat_grad_input_workspace_bytes(const smat_grad_input_args*) { return 0; }
-size_t smat_grad_weight_workspace_bytes(const smat_grad_weight_args* a) {
-  if (!a || a->rows < 0 || a->rows > kMaxSize || a->k < 0 || a->k > kMaxCols) return 0;
-  return values_bytes(a);
-}
+size_t smat_linear_workspace_bytes(const smat_linear_args* a) { return workspace_of(a); }
+size_t smat_grad_input_workspace_bytes(const smat_grad_input_args* a) { return workspace_of(a); }
+size_t smat_grad_weight_workspace_bytes(const smat_grad_weight_args* a) { return workspace_of(a); }
 
-smat_status smat_linear(const smat_linear_args* a, void*, size_t, smat_stream_t stream) {
+static smat_status linear(const smat_linear_args* a, void* d_workspace, size_t workspace_bytes,
+                          smat_stream_t stream) {
   if (!a) return lfail(SMAT_ERR_INVALID_ARG, "args is NULL");
   smat_status st = check_sizes(a->rows, a->k, a->n, a->dtype, a->act);
   if (st != SMAT_OK) return st;
@@ -154,21 +230,24 @@ smat_status smat_linear(const smat_linear_args* a, void*, size_t, smat_stream_t 
   };
   st = check_mats(mats, 7, 0, 6);
   if (st != SMAT_OK || m == 0 || n == 0) return st;
+  const Operands ops = operands(a);
+  st = check_workspace(d_workspace, workspace_bytes, ops.bytes());
+  if (st != SMAT_OK) return st;
   int sms = 1;
   st = device_sms(&sms);
   if (st != SMAT_OK) return st;
   Product p = {};
   p.mode = kForward;
   p.dtype = a->dtype;
-  p.a = a->x, p.b = a->w, p.lda = a->ldx, p.ldb = a->ldw;
   p.I = m, p.J = n, p.L = k;
   p.bias = a->bias, p.residual = a->residual, p.out = a->y, p.q = a->q, p.e = a->e;
   p.ldr = a->ldr, p.ldo = a->ldy, p.ldq = a->ldq, p.lde = a->lde;
   p.act = a->act;
-  return cuda_status(launch_simt(p, sms, stream), "linear launch");
+  return run_product(p, ops, (char*)d_workspace, sms, stream, "linear launch");
 }
 
-smat_status smat_grad_input(const smat_grad_input_args* a, void*, size_t, smat_stream_t stream) {
+static smat_status grad_input(const smat_grad_input_args* a, void* d_workspace, size_t workspace_bytes,
+                              smat_stream_t stream) {
   if (!a) return lfail(SMAT_ERR_INVALID_ARG, "args is NULL");
   smat_status st = check_sizes(a->rows, a->k, a->n, a->dtype, a->act);
   if (st != SMAT_OK) return st;
@@ -186,22 +265,24 @@ smat_status smat_grad_input(const smat_grad_input_args* a, void*, size_t, smat_s
   };
   st = check_mats(mats, 5, -1, -1);
   if (st != SMAT_OK || m == 0 || k == 0) return st;
+  const Operands ops = operands(a);
+  st = check_workspace(d_workspace, workspace_bytes, ops.bytes());
+  if (st != SMAT_OK) return st;
   int sms = 1;
   st = device_sms(&sms);
   if (st != SMAT_OK) return st;
   Product p = {};
   p.mode = kGradInput;
   p.dtype = a->dtype;
-  p.a = a->dy, p.b = a->w, p.lda = a->lddy, p.ldb = a->ldw;
   p.I = m, p.J = k, p.L = n;
   p.out = a->dx, p.q = const_cast<int8_t*>(a->q), p.e = const_cast<uint8_t*>(a->e);
   p.ldo = a->lddx, p.ldq = a->ldq, p.lde = a->lde;
   p.act = a->act;
-  return cuda_status(launch_simt(p, sms, stream), "grad_input launch");
+  return run_product(p, ops, (char*)d_workspace, sms, stream, "grad_input launch");
 }
 
-smat_status smat_grad_weight(const smat_grad_weight_args* a, void* d_workspace, size_t workspace_bytes,
-                             smat_stream_t stream) {
+static smat_status grad_weight(const smat_grad_weight_args* a, void* d_workspace, size_t workspace_bytes,
+                               smat_stream_t stream) {
   if (!a) return lfail(SMAT_ERR_INVALID_ARG, "args is NULL");
   smat_status st = check_sizes(a->rows, a->k, a->n, a->dtype, a->act);
   if (st != SMAT_OK) return st;
@@ -224,7 +305,8 @@ smat_status smat_grad_weight(const smat_grad_weight_args* a, void* d_workspace, 
   };
   st = check_mats(mats, 6, -1, -1);
   if (st != SMAT_OK || n == 0) return st;
-  st = check_workspace(d_workspace, workspace_bytes, values_bytes(a));
+  const Operands ops = operands(a);
+  st = check_workspace(d_workspace, workspace_bytes, ops.bytes());
   if (st != SMAT_OK) return st;
   int sms = 1;
   st = device_sms(&sms);
@@ -235,23 +317,39 @@ smat_status smat_grad_weight(const smat_grad_weight_args* a, void* d_workspace, 
     if (st != SMAT_OK) return st;
   }
   if (k == 0) return SMAT_OK;
-  const void* x = a->x;
-  int64_t ldx = a->ldx;
-  if (a->q && m > 0) {
-    x = d_workspace;
-    ldx = values_ld(a);
-    st = cuda_status(launch_unpack8(a->q, a->ldq, a->e, a->lde, nullptr, 0, d_workspace, ldx, m, k, a->dtype, a->act,
-                                    sms, stream), "unpack launch");
+  if (ops.values) {
+    st = cuda_status(launch_unpack8(a->q, a->ldq, a->e, a->lde, nullptr, 0, d_workspace, ld_of(k), m, k, a->dtype,
+                                    a->act, sms, stream), "unpack launch");
     if (st != SMAT_OK) return st;
   }
   Product p = {};
   p.mode = kGradWeight;
   p.dtype = a->dtype;
-  p.a = a->dy, p.b = x, p.lda = a->lddy, p.ldb = ldx;
+  p.b = d_workspace, p.ldb = ld_of(k);  // x^ in 8 bits: its values
   p.I = n, p.J = k, p.L = m;
   p.out = a->dw, p.ldo = a->lddw;
   p.accumulate = a->accumulate & SMAT_ACCUMULATE_DW;
-  return cuda_status(launch_simt(p, sms, stream), "grad_weight launch");
+  return run_product(p, ops, (char*)d_workspace + ops.values, sms, stream, "grad_weight launch");
+}
+
+smat_status smat_linear(const smat_linear_args* a, void* d_workspace, size_t workspace_bytes, smat_stream_t stream) {
+  return guarded([&] { return linear(a, d_workspace, workspace_bytes, stream); });
+}
+smat_status smat_grad_input(const smat_grad_input_args* a, void* d_workspace, size_t workspace_bytes,
+                            smat_stream_t stream) {
+  return guarded([&] { return grad_input(a, d_workspace, workspace_bytes, stream); });
+}
+smat_status smat_grad_weight(const smat_grad_weight_args* a, void* d_workspace, size_t workspace_bytes,
+                             smat_stream_t stream) {
+  return guarded([&] { return grad_weight(a, d_workspace, workspace_bytes, stream); });
+}
+
+smat_status smat_linear_poll_errors(smat_stream_t stream, int32_t* errors_out) {
+  if (!errors_out) return lfail(SMAT_ERR_INVALID_ARG, "errors_out is NULL");
+  int v = 0;
+  const smat_status st = cuda_status(read_errors(&v, stream), "error flag read");
+  if (st == SMAT_OK) *errors_out = v;
+  return st;
 }
 
 static smat_status elementwise(const char* what, const void* dy, int64_t lddy, const int8_t* q, int64_t ldq,
@@ -279,21 +377,21 @@ static smat_status elementwise(const char* what, const void* dy, int64_t lddy, c
 
 smat_status smat_pack8(const void* x, int64_t ldx, int8_t* q, int64_t ldq, uint8_t* e, int64_t lde, int64_t rows,
                        int64_t cols, int32_t dtype, smat_stream_t stream) {
-  return elementwise("pack8 launch", nullptr, 0, q, ldq, e, lde, const_cast<void*>(x), ldx, rows, cols, dtype,
-                     SMAT_ACT_NONE, true, false, stream);
+  return guarded([&] { return elementwise("pack8 launch", nullptr, 0, q, ldq, e, lde, const_cast<void*>(x), ldx, rows, cols, dtype,
+                     SMAT_ACT_NONE, true, false, stream); });
 }
 
 smat_status smat_unpack8(const int8_t* q, int64_t ldq, const uint8_t* e, int64_t lde, void* out, int64_t ldout,
                          int64_t rows, int64_t cols, int32_t dtype, int32_t act, smat_stream_t stream) {
-  return elementwise("unpack8 launch", nullptr, 0, q, ldq, e, lde, out, ldout, rows, cols, dtype, act, false, false,
-                     stream);
+  return guarded([&] { return elementwise("unpack8 launch", nullptr, 0, q, ldq, e, lde, out, ldout, rows, cols, dtype, act, false, false,
+                     stream); });
 }
 
 smat_status smat_act_grad8(const void* dy, int64_t lddy, const int8_t* q, int64_t ldq, const uint8_t* e, int64_t lde,
                            void* out, int64_t ldout, int64_t rows, int64_t cols, int32_t dtype, int32_t act,
                            smat_stream_t stream) {
-  return elementwise("act_grad8 launch", dy, lddy, q, ldq, e, lde, out, ldout, rows, cols, dtype, act, false, true,
-                     stream);
+  return guarded([&] { return elementwise("act_grad8 launch", dy, lddy, q, ldq, e, lde, out, ldout, rows, cols, dtype, act, false, true,
+                     stream); });
 }
 
 }  // extern "C"

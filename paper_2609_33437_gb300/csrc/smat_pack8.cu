@@ -203,6 +203,20 @@ __global__ void __launch_bounds__(kThreads)
   cluster_sync();  // the shares stay until they have been read
 }
 
+// Rows of 2-byte values to rows that start on 16 bytes: a thread moves 8 neighbouring values, read one by one.
+__global__ void __launch_bounds__(kThreads)
+    copy_rows_kernel(const uint16_t* from, int64_t ld, uint16_t* to, int64_t ldto, int64_t rows, int64_t cols) {
+  for (int64_t r = (int64_t)blockIdx.y * blockDim.y + threadIdx.y; r < rows; r += (int64_t)gridDim.y * blockDim.y)
+    for (int64_t c = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) * 8; c < cols;
+         c += (int64_t)gridDim.x * blockDim.x * 8) {
+      uint32_t w[4] = {};
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (c + i < cols) w[i / 2] |= (uint32_t)from[r * ld + c + i] << (16 * (i % 2));
+      *reinterpret_cast<uint4*>(to + r * ldto + c) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+}
+
 bool can(const void* p, int64_t ld, size_t elem, size_t bytes) {
   return (uintptr_t)p % bytes == 0 && (uint64_t)ld * elem % bytes == 0;
 }
@@ -212,8 +226,7 @@ struct Shape {
 };
 
 // A block is as wide as a row has units, at most 256 threads; the grid has enough blocks for eight per SM.
-Shape shape_of(int64_t rows, int64_t cols, int sms) {
-  const int64_t units = (cols + kGroup - 1) / kGroup * 2;
+Shape shape_for(int64_t rows, int64_t units, int sms) {
   unsigned x = 2;
   while (x < kThreads && x < units) x *= 2;
   const unsigned y = kThreads / x;
@@ -224,6 +237,8 @@ Shape shape_of(int64_t rows, int64_t cols, int sms) {
   gy = gy < by ? gy : by;
   return {dim3((unsigned)gx, (unsigned)(gy < 65535 ? gy : 65535)), dim3(x, y)};
 }
+
+Shape shape_of(int64_t rows, int64_t cols, int sms) { return shape_for(rows, (cols + kGroup - 1) / kGroup * 2, sms); }
 
 template <class T, bool DY>
 cudaError_t unpack_as(const int8_t* q, int64_t ldq, const uint8_t* e, int64_t lde, const void* dy, int64_t lddy,
@@ -258,6 +273,13 @@ cudaError_t launch_unpack8(const int8_t* q, int64_t ldq, const uint8_t* e, int64
               : unpack_as<__nv_bfloat16, false>(q, ldq, e, lde, dy, lddy, out, ldout, rows, cols, act, sms, s);
   return dy ? unpack_as<float, true>(q, ldq, e, lde, dy, lddy, out, ldout, rows, cols, act, sms, s)
             : unpack_as<float, false>(q, ldq, e, lde, dy, lddy, out, ldout, rows, cols, act, sms, s);
+}
+
+cudaError_t launch_copy_rows(const void* from, int64_t ld, void* to, int64_t ldto, int64_t rows, int64_t cols, int sms,
+                             cudaStream_t s) {
+  const Shape h = shape_for(rows, (cols + 7) / 8, sms);
+  copy_rows_kernel<<<h.grid, h.block, 0, s>>>((const uint16_t*)from, ld, (uint16_t*)to, ldto, rows, cols);
+  return cudaGetLastError();
 }
 
 cudaError_t launch_row_sums(const void* dy, int64_t lddy, void* db, int64_t rows, int64_t cols, int dtype, bool add,

@@ -15,6 +15,7 @@ dimensions and a row stride (the last dimension is contiguous). Argument marshal
 the library's kernels, on the current stream or the one given.
 """
 
+import ctypes
 import functools
 import struct
 from typing import Optional, Tuple, Union
@@ -295,6 +296,14 @@ def act_grad8(dy: torch.Tensor, saved: Packed8, act: str, out: Optional[torch.Te
     _call("smat_act_grad8", dy.device, dy.data_ptr(), lddy, pq, ldq, pe,
           lde, ph, ldh, rows, cols, code, a)
     return dh
+
+
+def poll_errors(stream: Optional[torch.cuda.Stream] = None) -> int:
+    """Read and clear the products' device error flags (0 = none; 1 = a bounded wait ran out and a result is
+    unfinished); synchronises the stream."""
+    v = ctypes.c_int32()
+    S.check("smat_linear_poll_errors", S.load_library().smat_linear_poll_errors(S._stream_handle(stream), ctypes.byref(v)))
+    return v.value
 
 
 # ------------------------------------------------------------------- layers ---

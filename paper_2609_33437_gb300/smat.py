@@ -33,7 +33,7 @@ EXPORTED = ("smat_workspace_bytes", "smat_init", "smat_simulate_multi", "smat_gr
             "smat_merge_workspace_bytes", "smat_merge", "smat_merge_ties_thresholds",
             "smat_grad_map_adamw_multi", "smat_linear_workspace_bytes", "smat_grad_input_workspace_bytes",
             "smat_grad_weight_workspace_bytes", "smat_linear", "smat_grad_input", "smat_grad_weight",
-            "smat_pack8", "smat_unpack8", "smat_act_grad8")
+            "smat_pack8", "smat_unpack8", "smat_act_grad8", "smat_linear_poll_errors")
 
 
 class AdamW(ctypes.Structure):
@@ -120,7 +120,8 @@ def load_library(build_if_missing: bool = True) -> ctypes.CDLL:
     L.smat_pack8.argtypes = [P, I64, P, I64, P, I64, I64, I64, I32, P]
     L.smat_unpack8.argtypes = [P, I64, P, I64, P, I64, I64, I64, I32, I32, P]
     L.smat_act_grad8.argtypes = [P, I64, P, I64, P, I64, P, I64, I64, I64, I32, I32, P]
-    for name in ("smat_pack8", "smat_unpack8", "smat_act_grad8"):
+    L.smat_linear_poll_errors.argtypes = [P, ctypes.POINTER(I32)]
+    for name in ("smat_pack8", "smat_unpack8", "smat_act_grad8", "smat_linear_poll_errors"):
         getattr(L, name).restype = I32
     L.smat_timing_enable.argtypes = [P, I32]
     L.smat_timing_read.argtypes = [P, P, P]
