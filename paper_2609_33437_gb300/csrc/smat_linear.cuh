@@ -14,10 +14,40 @@ namespace lin {
 
 constexpr int kGroup = SMAT_PACK8_GROUP;
 
-// sigmoid by the hardware's exponential (2 ulp) and reciprocal: 1e-6 relative over the whole range, and its
-// limits at infinities. Every activation below that has a sigmoid form uses it, the tanh form of GELU too
-// (1 + tanh u = 2 sigmoid(2u)), so that small values far out on the negative side keep their digits.
-__device__ __forceinline__ float sigmoid(float x) { return __fdividef(1.0f, 1.0f + __expf(-x)); }
+// The hardware's 2^x and 1 / x, 2 ulp and 1 ulp, results below 2^-126 flushed to 0: one instruction each, where
+// expf and a division are 6 to 10. An epilogue makes a value per sum, and its instructions bound it.
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float rcp_fast(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+// sigmoid(c h), 1e-6 relative where it is above 2^-120, with its limits at infinities. The activations with a
+// sigmoid form use it, the tanh form of GELU too (1 + tanh u = 2 sigmoid(2u)), so that small values far out on the
+// negative side keep their digits.
+__device__ __forceinline__ float sigmoid(float x, float c = 1.0f) {
+  return rcp_fast(1.0f + exp2_fast(-c * kLog2e * x));
+}
+
+// Phi(h) by Abramowitz and Stegun 7.1.26 (erfc(z) = t (a1 + t (a2 + ...)) exp(-z^2), t = 1 / (1 + p z), z = |h| /
+// sqrt2; off by 1.5e-7 at most, so Phi by 0.75e-7), taken from the side where it is small; `g` = exp(-h^2 / 2).
+__device__ __forceinline__ float normal_cdf(float h, float& g) {
+  const float t = rcp_fast(fmaf(0.3275911f * 0.70710678f, fabsf(h), 1.0f));
+  g = exp2_fast(h * h * (-0.5f * kLog2e));
+  float s = fmaf(t, 0.5f * 1.061405429f, 0.5f * -1.453152027f);
+  s = fmaf(s, t, 0.5f * 1.421413741f);
+  s = fmaf(s, t, 0.5f * -0.284496736f);
+  s = fmaf(s, t, 0.5f * 0.254829592f);
+  s = s * t * g;
+  return h > 0.0f ? 1.0f - s : s;
+}
 
 constexpr float kTanhGain = 1.5957691216057308f;  // 2 sqrt(2 / pi)
 constexpr float kTanhCube = 0.044715f;
@@ -25,9 +55,12 @@ constexpr float kTanhCube = 0.044715f;
 template <int ACT>
 __device__ __forceinline__ float act_value(float h) {
   if (ACT == SMAT_ACT_RELU) return h > 0.0f || h != h ? h : 0.0f;
-  if (ACT == SMAT_ACT_GELU) return 0.5f * h * erfcf(-0.70710678118654752f * h);
-  if (ACT == SMAT_ACT_GELU_TANH) return h * sigmoid(kTanhGain * h * fmaf(kTanhCube, h * h, 1.0f));
-  if (ACT == SMAT_ACT_QUICK_GELU) return h * sigmoid(1.702f * h);
+  if (ACT == SMAT_ACT_GELU) {
+    float g;
+    return h * normal_cdf(h, g);
+  }
+  if (ACT == SMAT_ACT_GELU_TANH) return h * sigmoid(h * fmaf(kTanhCube, h * h, 1.0f), kTanhGain);
+  if (ACT == SMAT_ACT_QUICK_GELU) return h * sigmoid(h, 1.702f);
   if (ACT == SMAT_ACT_SILU) return h * sigmoid(h);
   return h;
 }
@@ -38,16 +71,20 @@ template <int ACT>
 __device__ __forceinline__ float act_slope(float h) {
   if (ACT == SMAT_ACT_RELU) return h > 0.0f ? 1.0f : (h != h ? h : 0.0f);
   if (ACT == SMAT_ACT_NONE) return 1.0f;
-  h = h > 100.0f ? 100.0f : (h < -100.0f ? -100.0f : h);
-  if (ACT == SMAT_ACT_GELU)
-    return fmaf(h * 0.39894228040143268f, __expf(-0.5f * h * h), 0.5f * erfcf(-0.70710678118654752f * h));
+  asm("min.NaN.f32 %0, %0, 0f42C80000;\nmax.NaN.f32 %0, %0, 0fC2C80000;" : "+f"(h));
+  if (ACT == SMAT_ACT_GELU) {
+    float g;
+    const float c = normal_cdf(h, g);
+    return fmaf(h * 0.39894228040143268f, g, c);
+  }
   if (ACT == SMAT_ACT_GELU_TANH) {
-    const float s = sigmoid(kTanhGain * h * fmaf(kTanhCube, h * h, 1.0f));
-    return fmaf(h * kTanhGain * fmaf(3.0f * kTanhCube, h * h, 1.0f), s * (1.0f - s), s);
+    const float u = h * h;
+    const float s = sigmoid(h * fmaf(kTanhCube, u, 1.0f), kTanhGain);
+    return fmaf(h * fmaf(3.0f * kTanhCube * kTanhGain, u, kTanhGain), fmaf(-s, s, s), s);
   }
   const float c = ACT == SMAT_ACT_QUICK_GELU ? 1.702f : 1.0f;
-  const float s = sigmoid(c * h);
-  return fmaf(c * h, s * (1.0f - s), s);
+  const float s = sigmoid(h, c);
+  return fmaf(c * h, fmaf(-s, s, s), s);
 }
 
 // Runs the statement with ACT one of the six activations: the branch is taken once per block of elements.
@@ -69,23 +106,66 @@ __device__ __forceinline__ uint32_t pack_exponent(uint32_t top) {
   return top >= 0x7F800000u ? 255u : (uint32_t)(e < 1 ? 1 : e);
 }
 
-// 2^(127 - e), by which a value is multiplied before it is rounded. The products are exact (or far below 1/2).
-// For e = 255 the factor is 0: 0 for finite values, NaN for infinities and NaN, which pack_value sorts out.
-__device__ __forceinline__ float pack_factor(uint32_t e) {
-  return e == 255u ? 0.0f : __uint_as_float((254u - e) << 23);
+// q of a value in the low byte (the others hold something else), the factor being 2^(127 - e): the product is exact,
+// or far below 1/2, and its rounding to a whole number, ties to even, is
+// that of an addition to 1.5 * 2^23, whose last place is 1. In a group of e = 255 it is not q: see pack_poisoned.
+__device__ __forceinline__ uint32_t pack_value(float x, float factor) {
+  return __float_as_uint(fmaf(x, factor, 12582912.0f));
 }
 
-// q of one value, in the low byte.
-__device__ __forceinline__ uint32_t pack_value(float x, float factor) {
-  if (factor == 0.0f) return fabsf(x) == __int_as_float(0x7F800000) ? (x > 0.0f ? 127u : 129u) : 0u;
-  return (uint32_t)__float2int_rn(x * factor) & 0xFFu;
+// q in a group that holds an infinity or NaN: +-127 for infinities, 0 for the rest
+__device__ __forceinline__ uint32_t pack_poisoned(float x) {
+  return fabsf(x) == __int_as_float(0x7F800000) ? (x > 0.0f ? 127u : 129u) : 0u;
+}
+
+// the low bytes of four words
+__device__ __forceinline__ uint32_t low_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  return __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(c, d, 0x0040), 0x5410);
+}
+
+// 4 * WORDS values' q
+template <int WORDS>
+__device__ __forceinline__ void pack_words(const float* v, uint32_t e, uint32_t* w) {
+  if (e == 255u) {
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i, v += 4)
+      w[i] = low_bytes(pack_poisoned(v[0]), pack_poisoned(v[1]), pack_poisoned(v[2]), pack_poisoned(v[3]));
+    return;
+  }
+  const float f = __uint_as_float((254u - e) << 23);
+#pragma unroll
+  for (int i = 0; i < WORDS; ++i, v += 4)
+    w[i] = low_bytes(pack_value(v[0], f), pack_value(v[1], f), pack_value(v[2], f), pack_value(v[3], f));
+}
+__device__ __forceinline__ uint32_t pack_one(float x, uint32_t e) {
+  return e == 255u ? pack_poisoned(x) : pack_value(x, __uint_as_float((254u - e) << 23));
+}
+
+// The larger magnitude; NaN if one is (as bits: larger than infinity's).
+__device__ __forceinline__ float larger(float a, float b) {
+  float y;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(fabsf(a)), "f"(fabsf(b)));
+  return y;
 }
 
 // 2^(e - 127); infinity for e = 255 (q = 0 then reads as NaN, +-127 as +-infinity).
 __device__ __forceinline__ float unpack_scale(uint32_t e) { return __uint_as_float(e << 23); }
 
-__device__ __forceinline__ float unpack_value(uint32_t word, int byte, float scale) {
-  return (float)(int8_t)(word >> (8 * byte)) * scale;
+// The values of 4 * WORDS q. 2^23 + 128 + q is a float whose last place is 1: a byte of q + 128 put into 2^23's bits;
+// what is left is one multiply-add, exact like the product (a conversion from an integer runs at an eighth of its
+// rate). Where 2^23 times the scale could overflow, from e = 230 on, and for e = 255, the product it is.
+template <int WORDS>
+__device__ __forceinline__ void unpack_words8(const uint32_t* w, uint32_t e, float* v) {
+  const float by = unpack_scale(e);
+  if (e >= 230u) {
+#pragma unroll
+    for (int i = 0; i < 4 * WORDS; ++i) v[i] = (float)(int8_t)(w[i / 4] >> (8 * (i % 4))) * by;
+    return;
+  }
+  const float less = -8388736.0f * by;
+#pragma unroll
+  for (int i = 0; i < 4 * WORDS; ++i)
+    v[i] = fmaf(__uint_as_float(__byte_perm(w[i / 4] ^ 0x80808080u, 0x4B000000u, 0x7540 | (i % 4))), by, less);
 }
 
 // Thread-block cluster: a barrier of all its threads (with release and acquire of shared memory), and a float of

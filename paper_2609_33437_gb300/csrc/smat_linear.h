@@ -1,6 +1,7 @@
 // What the host side of the linear layers (smat_linear_host.cpp) and their kernels share.
 #pragma once
 
+#include <atomic>
 #include <cstdint>
 
 #include <cuda_runtime.h>
@@ -9,6 +10,18 @@
 
 namespace smat {
 namespace lin {
+
+// Allows a kernel its dynamic shared memory, once per kernel and device.
+template <class F>
+cudaError_t allow_shared(F* f, int bytes, std::atomic<uint64_t>& done) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  const uint64_t bit = dev < 64 ? uint64_t(1) << dev : 0;
+  if (e != cudaSuccess || (done.load(std::memory_order_relaxed) & bit)) return e;
+  e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+  return e;
+}
 
 // What happens to a product's sums on their way out.
 enum Mode : int { kForward = 0, kGradInput = 1, kGradWeight = 2 };

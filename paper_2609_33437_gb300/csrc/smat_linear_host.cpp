@@ -1,5 +1,6 @@
 // Host side of the linear layers (include/smat.h): argument checks, workspace, launches.
 
+#include <atomic>
 #include <cstdarg>
 #include <cstdio>
 
@@ -99,10 +100,14 @@ smat_status check_mats(const Mat* m, int count, int same_a, int same_b) {
   return SMAT_OK;
 }
 
+// The current device's SM count, asked for once per device.
 smat_status device_sms(int* sms) {
+  static std::atomic<int> known[64];
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess && dev < 64 && (*sms = known[dev].load(std::memory_order_relaxed)) > 0) return SMAT_OK;
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev);
+  if (e == cudaSuccess && dev < 64) known[dev].store(*sms, std::memory_order_relaxed);
   return cuda_status(e, "device query");
 }
 

@@ -120,16 +120,18 @@ __device__ __forceinline__ void finish4(const Args& a, int64_t i, int64_t j, flo
         if (t < count) v[t] += to_float(((const T*)p.bias)[j + t]);
     }
     if (p.q) {
-      uint32_t top = 0;
+      float big = 0.0f;
 #pragma unroll
-      for (int t = 0; t < 4; ++t) top = max(top, t < count ? __float_as_uint(v[t]) & 0x7FFFFFFFu : 0u);
+      for (int t = 0; t < 4; ++t) big = t < count ? larger(big, v[t]) : big;
+      uint32_t top = __float_as_uint(big);
 #pragma unroll
       for (int d = 1; d < 8; d *= 2) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
       const uint32_t ex = pack_exponent(top);
-      const float f = pack_factor(ex);
+      uint32_t w;
+      pack_words<1>(v, ex, &w);
 #pragma unroll
       for (int t = 0; t < 4; ++t)
-        if (t < count) p.q[i * p.ldq + j + t] = (int8_t)pack_value(v[t], f);
+        if (t < count) p.q[i * p.ldq + j + t] = (int8_t)(w >> (8 * t));
       if (count > 0 && j % kGroup == 0) p.e[i * p.lde + j / kGroup] = (uint8_t)ex;
     }
     if (count <= 0) return;
@@ -255,7 +257,8 @@ cudaError_t launch_tile(const Args& a, int shares, cudaStream_t s) {
   constexpr int kSlices = 2 * kBK * (BM + kPad + kBN + kPad) * 4, kSums = BM * kBN * 4;
   constexpr int kBytes = kSlices > kSums ? kSlices : kSums;
   auto* f = simt_kernel<T, BM, A_MN, B_MN>;
-  cudaError_t e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes);
+  static std::atomic<uint64_t> allowed;
+  const cudaError_t e = allow_shared(f, kBytes, allowed);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)((a.p.I + BM - 1) / BM), (unsigned)((a.p.J + kBN - 1) / kBN), (unsigned)shares);

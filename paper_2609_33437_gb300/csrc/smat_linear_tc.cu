@@ -131,7 +131,8 @@ __device__ __forceinline__ void mma_commit(uint32_t bar) {
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 
-// 32 columns of the warp's 32 rows of tensor memory: thread's row, columns in order
+// 32 columns of the warp's 32 rows of tensor memory: thread's row, columns in order. The load and its wait are one
+// statement, so that nothing can read the registers in between.
 __device__ __forceinline__ void take32(uint32_t at, float (&v)[32]) {
   uint32_t u[32];
   asm volatile(
@@ -167,12 +168,38 @@ __device__ __forceinline__ void store_words8(void* p, const uint32_t (&w)[8]) {
                : "memory");
 }
 
-// 32 columns j .. j + 31 of row i, one thread: whole sectors in and out.
+// What finishing 32 columns of a row reads, asked for before the sums are there: the residual, the older gradient or
+// q, and e.
+struct Beside {
+  uint32_t w[16];
+  uint32_t e;
+};
+
 template <int MODE>
-__device__ __forceinline__ void finish_row(const Args& a, int64_t i, int64_t j, float (&v)[32]) {
+__device__ __forceinline__ void ask_row(const Args& a, int64_t i, int64_t j, Beside& in) {
+  const Product& p = a.p;
+  if (i >= p.I) return;
+  if (MODE == kGradInput) {
+    if (p.act == SMAT_ACT_NONE) return;
+    load_words8(p.q + i * p.ldq + j, *reinterpret_cast<uint32_t (*)[8]>(&in.w[0]));
+    in.e = p.e[i * p.lde + j / kGroup];
+    return;
+  }
+  const bf16* from = MODE == kForward ? (const bf16*)p.residual + i * p.ldr + j
+                                      : (const bf16*)p.out + i * p.ldo + j;
+  if (MODE == kForward ? p.residual != nullptr : p.accumulate != 0) {
+    load_words8(from, *reinterpret_cast<uint32_t (*)[8]>(&in.w[0]));
+    load_words8(from + 16, *reinterpret_cast<uint32_t (*)[8]>(&in.w[8]));
+  }
+}
+
+// 32 columns j .. j + 31 of row i, one thread: whole sectors in and out. Returns the saved group's e.
+template <int MODE>
+__device__ __forceinline__ uint32_t finish_row(const Args& a, int64_t i, int64_t j, float (&v)[32], const Beside& in) {
   const Product& p = a.p;
   bf16* out = (bf16*)p.out + i * p.ldo + j;
   const bool there = i < p.I;
+  uint32_t ex = 0;
   if (MODE == kForward) {
     if (p.bias) {
       const bf16* b = (const bf16*)p.bias + j;
@@ -192,63 +219,41 @@ __device__ __forceinline__ void finish_row(const Args& a, int64_t i, int64_t j, 
       }
     }
     if (p.q) {
-      uint32_t top = 0;
+      float big = 0.0f;
 #pragma unroll
-      for (int t = 0; t < 32; ++t) top = max(top, __float_as_uint(v[t]) & 0x7FFFFFFFu);
-      const uint32_t ex = pack_exponent(top);
-      const float f = pack_factor(ex);
+      for (int t = 0; t < 32; ++t) big = larger(big, v[t]);
+      ex = pack_exponent(__float_as_uint(big));
       uint32_t w[8];
-#pragma unroll
-      for (int t = 0; t < 8; ++t)
-        w[t] = pack_value(v[4 * t], f) | pack_value(v[4 * t + 1], f) << 8 | pack_value(v[4 * t + 2], f) << 16 |
-               pack_value(v[4 * t + 3], f) << 24;
-      if (there) {
-        store_words8(p.q + i * p.ldq + j, w);
-        p.e[i * p.lde + j / kGroup] = (uint8_t)ex;
-      }
+      pack_words<8>(v, ex, w);
+      if (there) store_words8(p.q + i * p.ldq + j, w);
     }
     SMAT_WITH_ACT(p.act, _Pragma("unroll") for (int t = 0; t < 32; ++t) v[t] = act_value<ACT>(v[t]))
-    if (p.residual && there) {
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        uint32_t w[8];
-        float f[16];
-        load_words8((const bf16*)p.residual + i * p.ldr + j + 16 * h, w);
-        unpack_words(w, 8, f);
-#pragma unroll
-        for (int t = 0; t < 16; ++t) v[16 * h + t] += f[t];
-      }
+  }
+  if (MODE == kGradInput) {
+    if (p.act != SMAT_ACT_NONE) {
+      float h[32];
+      unpack_words8<8>(in.w, in.e, h);
+      SMAT_WITH_ACT(p.act, _Pragma("unroll") for (int t = 0; t < 32; ++t) v[t] *= act_slope<ACT>(h[t]))
     }
+  } else if (MODE == kForward ? p.residual != nullptr : p.accumulate != 0) {
+    float f[32];
+    unpack_words(in.w, 16, f);
+#pragma unroll
+    for (int t = 0; t < 32; ++t) v[t] += f[t];
   }
-  if (MODE == kGradInput && p.act != SMAT_ACT_NONE && there) {
-    uint32_t w[8];
-    load_words8(p.q + i * p.ldq + j, w);
-    const float scale = unpack_scale(p.e[i * p.lde + j / kGroup]);
-    SMAT_WITH_ACT(p.act, _Pragma("unroll") for (int t = 0; t < 32; ++t) v[t] *=
-                  act_slope<ACT>(unpack_value(w[t / 4], t % 4, scale)))
-  }
-  if (!there) return;
-  if (MODE == kGradWeight && p.accumulate) {
+  if (there) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       uint32_t w[8];
-      float f[16];
-      load_words8(out + 16 * h, w);
-      unpack_words(w, 8, f);
 #pragma unroll
-      for (int t = 0; t < 16; ++t) v[16 * h + t] += f[t];
+      for (int t = 0; t < 8; ++t) {
+        const __nv_bfloat162 b = __floats2bfloat162_rn(v[16 * h + 2 * t], v[16 * h + 2 * t + 1]);
+        w[t] = *reinterpret_cast<const uint32_t*>(&b);
+      }
+      store_words8(out + 16 * h, w);
     }
   }
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    uint32_t w[8];
-#pragma unroll
-    for (int t = 0; t < 8; ++t) {
-      const __nv_bfloat162 b = __floats2bfloat162_rn(v[16 * h + 2 * t], v[16 * h + 2 * t + 1]);
-      w[t] = *reinterpret_cast<const uint32_t*>(&b);
-    }
-    store_words8(out + 16 * h, w);
-  }
+  return ex;
 }
 
 // Column j of rows i .. i + 31, one thread; the warp holds 32 neighbouring columns from a multiple of 32 on. Rows are
@@ -277,10 +282,10 @@ __device__ __forceinline__ void finish_column(const Args& a, int64_t i, int64_t 
 #pragma unroll
         for (int t = 0; t < 8; ++t) {
           const uint32_t top =
-              __reduce_max_sync(0xFFFFFFFFu, there ? __float_as_uint(v[s + t]) & 0x7FFFFFFFu : 0u);
+              __reduce_max_sync(0xFFFFFFFFu, there ? __float_as_uint(fabsf(v[s + t])) : 0u);
           const uint32_t ex = pack_exponent(top);
           if (there && t < rows) {
-            p.q[(i + s + t) * p.ldq + j] = (int8_t)pack_value(v[s + t], pack_factor(ex));
+            p.q[(i + s + t) * p.ldq + j] = (int8_t)pack_one(v[s + t], ex);
             if (lane == 0) p.e[(i + s + t) * p.lde + j / kGroup] = (uint8_t)ex;
           }
         }
@@ -307,26 +312,41 @@ __device__ __forceinline__ void finish_column(const Args& a, int64_t i, int64_t 
   }
 }
 
-// 32 columns (of the tile) of the warp's 32 rows (of the tile): what they are of the result, and out with them.
-template <int MODE, bool SWAP>
-__device__ __forceinline__ void finish(const Args& a, int64_t row0, int64_t col0, float (&v)[32], float* turn) {
+// `count` blocks of 32 columns of the tile, from column col0 of the result on, of the warp's 32 rows (row0 on; rows
+// and columns of the tile, that is): `sums(c, v)` gives block c's sums.
+template <int MODE, bool SWAP, class Sums>
+__device__ __forceinline__ void finish(const Args& a, int64_t row0, int64_t col0, int first, int end, int step,
+                                       float* turn, Sums&& sums) {
   const int lane = threadIdx.x % 32;
-  if (SWAP) {
-    if (col0 < a.p.I && row0 < a.p.J) finish_column<MODE>(a, col0, row0 + lane, v);
-    return;
-  }
-  if (row0 >= a.p.I || col0 >= a.p.J) return;
-  if (a.wide && col0 + 32 <= a.p.J) {
-    finish_row<MODE>(a, row0 + lane, col0, v);
-    return;
-  }
-  __syncwarp();
+  if (first >= end) return;
+  const bool rows = !SWAP && a.wide;
+  Beside in;
+  if (rows && col0 + 32 * first + 32 <= a.p.J) ask_row<MODE>(a, row0 + lane, col0 + 32 * first, in);
+  for (int c = first; c < end; c += step) {
+    const int64_t col = col0 + 32 * c;
+    float v[32];
+    sums(c, v);
+    if (SWAP) {
+      if (col < a.p.I && row0 < a.p.J) finish_column<MODE>(a, col, row0 + lane, v);
+      continue;
+    }
+    if (rows && col + 32 <= a.p.J) {
+      const Beside now = in;
+      if (c + step < end && col + 32 * step + 32 <= a.p.J) ask_row<MODE>(a, row0 + lane, col + 32 * step, in);
+      const uint32_t ex = finish_row<MODE>(a, row0 + lane, col, v, now);
+      if (MODE == kForward && a.p.q && row0 + lane < a.p.I)
+        a.p.e[(row0 + lane) * a.p.lde + col / kGroup] = (uint8_t)ex;
+      continue;
+    }
+    if (row0 >= a.p.I || col >= a.p.J) continue;
+    __syncwarp();
 #pragma unroll
-  for (int t = 0; t < 32; ++t) turn[lane * 33 + t] = v[t];
-  __syncwarp();
+    for (int t = 0; t < 32; ++t) turn[lane * 33 + t] = v[t];
+    __syncwarp();
 #pragma unroll
-  for (int t = 0; t < 32; ++t) v[t] = turn[t * 33 + lane];
-  finish_column<MODE>(a, row0, col0 + lane, v);
+    for (int t = 0; t < 32; ++t) v[t] = turn[t * 33 + lane];
+    finish_column<MODE>(a, row0, col + lane, v);
+  }
 }
 
 // The tiles' order: strips of 16 tiles of rows, down a strip's rows first, so that the tiles in work at one time
@@ -463,34 +483,33 @@ __global__ void __launch_bounds__(kThreads, 1)
       const uint32_t half = made & 1, sums = tmem + half * BN + ((uint32_t)(32 * quarter) << 16);
       if (!bar_wait(sums_full + 8 * half, made / 2 & 1, dead)) break;
       fence_after();
-      if (shares == 1) {
-        if (warp / 4 >= BN / 32 && lane == 0) bar_arrive(sums_empty + 8 * half);  // none of a narrow tile's columns
-        for (int c = warp / 4; c < BN / 32; c += kEpiWarps / 4) {
-          float v[32];
-          if (slices > 0) {
-            take32(sums + 32 * c, v);
-          } else {
+      // this warp's blocks of 32 columns: the first or the second half of the tile's
+      constexpr int kBlocks = BN / 32, kMine = (kBlocks + 1) / 2;
+      const int first = warp / 4 * kMine, end = min(kBlocks, first + kMine);
+      auto take = [&](int c, float(&v)[32]) {
+        if (slices > 0) {
+          take32(sums + 32 * c, v);
+        } else {
 #pragma unroll
-            for (int t = 0; t < 32; ++t) v[t] = 0.0f;
-          }
-          if (c + kEpiWarps / 4 >= BN / 32) {  // the last of this warp's columns are out
+          for (int t = 0; t < 32; ++t) v[t] = 0.0f;
+        }
+      };
+      if (shares == 1) {
+        if (first >= end && lane == 0) bar_arrive(sums_empty + 8 * half);  // none of a narrow tile's columns
+        finish<MODE, SWAP>(a, r0, c0, first, end, 1, turn, [&](int c, float(&v)[32]) {
+          take(c, v);
+          if (c + 1 == end) {  // the last of this warp's columns are out
             fence_before();
             __syncwarp();
             if (lane == 0) bar_arrive(sums_empty + 8 * half);
           }
-          finish<MODE, SWAP>(a, r0, c0 + 32 * c, v, turn);
-        }
+        });
       } else {
         // the ring is free: every product that read it is done. [column][128 rows]
         float* part = reinterpret_cast<float*>(ring) + 32 * quarter + lane;
-        for (int c = warp / 4; c < BN / 32; c += kEpiWarps / 4) {
+        for (int c = first; c < end; ++c) {
           float v[32];
-          if (slices > 0) {
-            take32(sums + 32 * c, v);
-          } else {
-#pragma unroll
-            for (int t = 0; t < 32; ++t) v[t] = 0.0f;
-          }
+          take(c, v);
 #pragma unroll
           for (int t = 0; t < 32; ++t) part[(32 * c + t) * kBM] = v[t];
         }
@@ -508,15 +527,15 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int quarter = warp % 4;
       const float* part = reinterpret_cast<const float*>(ring) + 32 * quarter + lane;
       float* turn = reinterpret_cast<float*>(ring + kStages * kStage + warp * kTurn);
-      for (int c = (int)rank + (int)shares * (warp / 4); c < BN / 32; c += (int)shares * (kEpiWarps / 4)) {
-        float v[32];
+      finish<MODE, SWAP>(
+          a, tr * kBM + 32 * quarter, tc * BN, (int)rank + (int)shares * (warp / 4), BN / 32,
+          (int)shares * (kEpiWarps / 4), turn, [&](int c, float(&v)[32]) {
 #pragma unroll
-        for (int t = 0; t < 32; ++t) v[t] = 0.0f;
-        for (uint32_t s = 0; s < shares; ++s)
+            for (int t = 0; t < 32; ++t) v[t] = 0.0f;
+            for (uint32_t s = 0; s < shares; ++s)
 #pragma unroll
-          for (int t = 0; t < 32; ++t) v[t] += cluster_load(part + (32 * c + t) * kBM, s);
-        finish<MODE, SWAP>(a, tr * kBM + 32 * quarter, tc * BN + 32 * c, v, turn);
-      }
+              for (int t = 0; t < 32; ++t) v[t] += cluster_load(part + (32 * c + t) * kBM, s);
+          });
     }
     cluster_sync();
   }
@@ -586,7 +605,8 @@ cudaError_t launch_tile(const Product& p, int sms, cudaStream_t s) {
     if (!ok) return cudaErrorNotSupported;
   }
   auto* f = tc_kernel<MODE, SWAP, BN>;
-  cudaError_t e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, Ring<BN>::kBytes);
+  static std::atomic<uint64_t> allowed;
+  const cudaError_t e = allow_shared(f, Ring<BN>::kBytes, allowed);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   const int64_t ctas = shares > 1 ? a.tiles * shares : (a.tiles < sms ? a.tiles : sms);

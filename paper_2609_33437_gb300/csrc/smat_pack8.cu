@@ -99,21 +99,18 @@ __global__ void __launch_bounds__(kThreads) pack8_kernel(const T* x, int64_t ldx
     const int count = (int)(cols - c < 0 ? 0 : (cols - c < kUnit ? cols - c : kUnit));
     float v[kUnit];
     load_unit(x + r * ldx + c, count, vx, v);
-    uint32_t top = 0;
+    float big = 0.0f;
 #pragma unroll
-    for (int i = 0; i < kUnit; ++i) top = max(top, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+    for (int i = 0; i < kUnit; ++i) big = larger(big, v[i]);
+    uint32_t top = __float_as_uint(big);
     // the other half of the group: the neighbouring thread (blockDim.x is even, so both are in this warp and run
     // the same steps)
     const unsigned pair = 3u << ((threadIdx.x + threadIdx.y * blockDim.x) & 30);
     top = max(top, __shfl_xor_sync(pair, top, 1));
     const uint32_t ex = pack_exponent(top);
-    const float f = pack_factor(ex);
     if ((u & 1) == 0) e[r * lde + u / 2] = (uint8_t)ex;
     uint32_t w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      w[i] = pack_value(v[4 * i], f) | pack_value(v[4 * i + 1], f) << 8 | pack_value(v[4 * i + 2], f) << 16 |
-             pack_value(v[4 * i + 3], f) << 24;
+    pack_words<4>(v, ex, w);
     int8_t* o = q + r * ldq + c;
     if (vq && count == kUnit) {
       *reinterpret_cast<uint4*>(o) = make_uint4(w[0], w[1], w[2], w[3]);
@@ -136,22 +133,36 @@ __global__ void __launch_bounds__(kThreads)
     if (count == 0) continue;
     uint32_t w[4];
     load_q(q + r * ldq + c, count, vq, w);
-    const float scale = unpack_scale(e[r * lde + u / 2]);
-    float v[kUnit];
+    float h[kUnit], v[kUnit];
+    unpack_words8<4>(w, e[r * lde + u / 2], h);
     if (DY) load_unit(dy + r * lddy + c, count, vdy, v);
 #pragma unroll
-    for (int i = 0; i < kUnit; ++i) {
-      const float h = unpack_value(w[i / 4], i % 4, scale);
-      v[i] = DY ? v[i] * act_slope<ACT>(h) : act_value<ACT>(h);
-    }
+    for (int i = 0; i < kUnit; ++i) v[i] = DY ? v[i] * act_slope<ACT>(h[i]) : act_value<ACT>(h[i]);
     store_unit(out + r * ldout + c, count, vout, v);
   }
 }
 
 // db[n] = sum over rows of dy (added to db where `add`). A CTA takes 64 columns and, with the other CTAs of its
-// cluster, every row: a thread adds 8 columns of every 32nd row of the CTA's share in fp32, shared memory joins the
+// cluster, every row: a thread adds 8 columns of every 32nd row of the CTA's share in fp32, eight rows' loads at a time, shared memory joins the
 // threads, the first CTA of the cluster adds the shares in order. One launch, no atomics.
 constexpr int kSumCols = 64, kSumLanes = 8, kSumRows = kThreads / kSumLanes;
+
+template <class T>
+__device__ __forceinline__ void add8(const uint4* u, float (&s)[8]) {
+#pragma unroll
+  for (int h = 0; h < (int)sizeof(T) / 2; ++h) {
+    const uint32_t w[4] = {u[h].x, u[h].y, u[h].z, u[h].w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (sizeof(T) == 2) {
+        s[2 * i] += __uint_as_float(w[i] << 16);
+        s[2 * i + 1] += __uint_as_float(w[i] & 0xFFFF0000u);
+      } else {
+        s[4 * h + i] += __uint_as_float(w[i]);
+      }
+    }
+  }
+}
 
 template <class T>
 __global__ void __launch_bounds__(kThreads)
@@ -163,27 +174,32 @@ __global__ void __launch_bounds__(kThreads)
   const int count = (int)(cols - c < 0 ? 0 : (cols - c < 8 ? cols - c : 8));
   float s[8] = {};
   const int64_t step = (int64_t)kSumRows * gridDim.y;
-#pragma unroll 4
-  for (int64_t r = (int64_t)blockIdx.y * kSumRows + row; r < rows; r += step) {
-    const T* p = dy + r * lddy + c;
-    if (vec && count == 8) {
-      if constexpr (sizeof(T) == 2) {
-        const uint4 u = __ldg(reinterpret_cast<const uint4*>(p));
-        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+  int64_t r = (int64_t)blockIdx.y * kSumRows + row;
+  if (vec && count == 8) {
+    // eight rows' loads in flight per thread: with one at a time the pass waits for memory (23 us instead of 6 at
+    // 8224 x 1024 bf16)
+    constexpr int kAhead = 8, kLoads = sizeof(T) / 2;
+    for (; r + (kAhead - 1) * step < rows; r += kAhead * step) {
+      uint4 u[kAhead][kLoads];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          s[2 * i] += __uint_as_float(w[i] << 16);
-          s[2 * i + 1] += __uint_as_float(w[i] & 0xFFFF0000u);
-        }
-      } else {
-        const float4 a = __ldg(reinterpret_cast<const float4*>(p)), b = __ldg(reinterpret_cast<const float4*>(p) + 1);
-        s[0] += a.x, s[1] += a.y, s[2] += a.z, s[3] += a.w, s[4] += b.x, s[5] += b.y, s[6] += b.z, s[7] += b.w;
-      }
-    } else {
+      for (int t = 0; t < kAhead; ++t)
+#pragma unroll
+        for (int h = 0; h < kLoads; ++h) u[t][h] = __ldg(reinterpret_cast<const uint4*>(dy + (r + t * step) * lddy + c) + h);
+#pragma unroll
+      for (int t = 0; t < kAhead; ++t) add8<T>(u[t], s);
+    }
+    for (; r < rows; r += step) {
+      uint4 u[kLoads];
+#pragma unroll
+      for (int h = 0; h < kLoads; ++h) u[h] = __ldg(reinterpret_cast<const uint4*>(dy + r * lddy + c) + h);
+      add8<T>(u, s);
+    }
+  } else {
+#pragma unroll 4
+    for (; r < rows; r += step)
 #pragma unroll
       for (int i = 0; i < 8; ++i)
-        if (i < count) s[i] += to_float(p[i]);
-    }
+        if (i < count) s[i] += to_float(dy[r * lddy + c + i]);
   }
 #pragma unroll
   for (int i = 0; i < 8; ++i) part[row][lane * 8 + i] = s[i];

@@ -16,7 +16,6 @@ the library's kernels, on the current stream or the one given.
 """
 
 import ctypes
-import functools
 import struct
 from typing import Optional, Tuple, Union
 
@@ -48,7 +47,9 @@ class Packed8:
     def empty(cls, shape, device) -> "Packed8":
         q = torch.empty(shape, dtype=torch.int8, device=device)
         e = torch.empty((*shape[:-1], -(-shape[-1] // GROUP)), dtype=torch.uint8, device=device)
-        return cls(q, e)
+        p = object.__new__(cls)  # made to fit: nothing to check
+        p.q, p.e = q, e
+        return p
 
     @property
     def shape(self):
@@ -123,47 +124,62 @@ def _packed(name: str, p: Packed8, device, rows: int, cols: int):
     return q, ldq, e, lde
 
 
-def _run(func: str, args: bytes, device):
+# The current stream's handle without a Stream object around it (2.8 us of a small call otherwise).
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+    (lambda index: torch.cuda.current_stream(index).cuda_stream)
+_functions = {}  # name -> (size query or None, function), as they are first called
+
+
+def _function(name: str):
+    f = _functions.get(name)
+    if f is None:
+        lib = S.load_library()
+        f = _functions[name] = (getattr(lib, name + "_workspace_bytes", None), getattr(lib, name))
+    return f
+
+
+def _run(name: str, args: bytes, device):
     """Workspace, then the call, on the tensors' device and the current stream."""
-    L = S.load_library()
-    if device.index != torch.cuda.current_device():
+    index = device.index
+    if index != torch.cuda.current_device():
         with torch.cuda.device(device):
-            return _run(func, args, device)
-    nbytes = getattr(L, func + "_workspace_bytes")(args)
-    ws = torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
-    st = getattr(L, func)(args, ws.data_ptr() if nbytes else None, nbytes, torch.cuda.current_stream().cuda_stream)
+            return _run(name, args, device)
+    size, f = _function(name)
+    nbytes = size(args)
+    if nbytes:
+        ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        st = f(args, ws.data_ptr(), nbytes, _raw_stream(index))
+    else:
+        st = f(args, None, 0, _raw_stream(index))
     if st:
-        S.check(func, st)
+        S.check(name, st)
 
 
-def _call(func: str, device, *args):
-    L = S.load_library()
-    if device.index != torch.cuda.current_device():
+def _call(name: str, device, *args):
+    index = device.index
+    if index != torch.cuda.current_device():
         with torch.cuda.device(device):
-            return _call(func, device, *args)
-    st = getattr(L, func)(*args, torch.cuda.current_stream().cuda_stream)
+            return _call(name, device, *args)
+    st = _function(name)[1](*args, _raw_stream(index))
     if st:
-        S.check(func, st)
+        S.check(name, st)
 
 
-def _on_given_stream(f):
-    """stream=...: the call as if that stream were current, so that what it allocates belongs to that stream (and is
-    not memory that the current stream's earlier work may still use)."""
-    @functools.wraps(f)
-    def g(*args, stream: Optional[torch.cuda.Stream] = None, **kw):
-        if stream is None:
-            return f(*args, **kw)
-        with torch.cuda.stream(stream):
-            return f(*args, **kw)
-    return g
+def _on(stream: torch.cuda.Stream, f, *args):
+    """A call on a given stream: as if that stream were current, so that what it allocates belongs to that stream
+    (and is not memory that the current stream's earlier work may still use)."""
+    with torch.cuda.stream(stream):
+        return f(*args)
 
 
-@_on_given_stream
 def linear(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor] = None, act: str = "none",
-           residual: Optional[torch.Tensor] = None, save: bool = False, out: Optional[torch.Tensor] = None):
+           residual: Optional[torch.Tensor] = None, save: bool = False, out: Optional[torch.Tensor] = None,
+           stream: Optional[torch.cuda.Stream] = None):
     """y = act(x W^T + b) + residual; with save, (y, Packed8 of x W^T + b).
 
     x [..., k], w [n, k], bias [n], residual and out [..., n]; out may be the residual."""
+    if stream is not None:
+        return _on(stream, linear, x, w, bias, act, residual, save, out)
     a = _act(act)
     rows, k, ldx = _rows("x", x)
     code = S.dtype_code(x.dtype)
@@ -182,17 +198,19 @@ def linear(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor] = None
     else:
         py, ldy = _like("out", y, dtype, device, rows, n)
     saved = Packed8.empty(shape, device) if save else None
-    pq, ldq, pe, lde = _packed("saved", saved, device, rows, n) if save else (0, n, 0, 1)
+    pq, pe, lde = (saved.q.data_ptr(), saved.e.data_ptr(), saved.e.shape[-1]) if save else (0, 0, 1)
+    ldq = n
     args = _LINEAR.pack(x.data_ptr(), pw, pb, pr, py, pq, pe, rows, k, n, ldx, ldw, ldr, ldy, ldq, lde, code, a)
     _run("smat_linear", args, device)
     return (y, saved) if save else y
 
 
-@_on_given_stream
 def linear_grad_input(dy: torch.Tensor, w: torch.Tensor, act: str = "none", saved: Optional[Packed8] = None,
-                      out: Optional[torch.Tensor] = None) -> torch.Tensor:
+                      out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """dx = (dy W) * act'(h^): back through a layer, and through the activation `act` that made the layer's input
     from the pre-activation `saved` ([..., k]; none with act "none"). dy [..., n], w [n, k]."""
+    if stream is not None:
+        return _on(stream, linear_grad_input, dy, w, act, saved, out)
     a = _act(act)
     if (a != 0) != (saved is not None):
         raise ValueError("saved: needed with an activation, and only then")
@@ -215,14 +233,15 @@ def linear_grad_input(dy: torch.Tensor, w: torch.Tensor, act: str = "none", save
     return dx
 
 
-@_on_given_stream
 def linear_grad_weight(dy: torch.Tensor, x: Union[torch.Tensor, Packed8], act: str = "none", bias: bool = False,
                        out: Optional[torch.Tensor] = None, bias_out: Optional[torch.Tensor] = None,
-                       accumulate: bool = False):
+                       accumulate: bool = False, stream: Optional[torch.cuda.Stream] = None):
     """(dW, db): dW = dy^T x^ [n, k] and, with bias, db [n] = dy's sums over its rows (else None).
 
     x is the layer's input [..., k], or its 8 bits; with `act`, the 8 bits of the pre-activation that `act` made
     the input from. With accumulate, dW is added to `out`, and db to `bias_out` where that is given."""
+    if stream is not None:
+        return _on(stream, linear_grad_weight, dy, x, act, bias, out, bias_out, accumulate)
     a = _act(act)
     packed = isinstance(x, Packed8)
     if a and not packed:
@@ -259,9 +278,10 @@ def linear_grad_weight(dy: torch.Tensor, x: Union[torch.Tensor, Packed8], act: s
     return dw, db
 
 
-@_on_given_stream
-def pack8(x: torch.Tensor) -> Packed8:
+def pack8(x: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> Packed8:
     """x in 8 bits."""
+    if stream is not None:
+        return _on(stream, pack8, x)
     rows, cols, ldx = _rows("x", x)
     code = S.dtype_code(x.dtype)
     p = Packed8.empty(x.shape, x.device)
@@ -270,29 +290,41 @@ def pack8(x: torch.Tensor) -> Packed8:
     return p
 
 
-@_on_given_stream
-def unpack8(p: Packed8, act: str = "none", dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+def unpack8(p: Packed8, act: str = "none", dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None,
+            stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """act of the values that p stands for."""
+    if stream is not None:
+        return _on(stream, unpack8, p, act, dtype, out)
     a = _act(act)
     code = S.dtype_code(dtype)
     rows, cols, ldq = _rows("p.q", p.q)
     pe, lde = _like("p.e", p.e, torch.uint8, p.device, rows, p.e.shape[-1])
-    y = out if out is not None else torch.empty(p.shape, dtype=dtype, device=p.device)
-    py, ldy = _like("out", y, dtype, p.device, rows, cols)
+    y = out
+    if y is None:
+        y = torch.empty(p.q.shape, dtype=dtype, device=p.q.device)
+        py, ldy = y.data_ptr(), cols
+    else:
+        py, ldy = _like("out", y, dtype, p.device, rows, cols)
     _call("smat_unpack8", p.device, p.q.data_ptr(), ldq, pe, lde, py, ldy,
           rows, cols, code, a)
     return y
 
 
-@_on_given_stream
-def act_grad8(dy: torch.Tensor, saved: Packed8, act: str, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+def act_grad8(dy: torch.Tensor, saved: Packed8, act: str, out: Optional[torch.Tensor] = None,
+              stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """dy * act'(h^): a gradient back through an activation, from the pre-activation's 8 bits."""
+    if stream is not None:
+        return _on(stream, act_grad8, dy, saved, act, out)
     a = _act(act)
     rows, cols, lddy = _rows("dy", dy)
     code = S.dtype_code(dy.dtype)
     pq, ldq, pe, lde = _packed("saved", saved, dy.device, rows, cols)
-    dh = out if out is not None else torch.empty(dy.shape, dtype=dy.dtype, device=dy.device)
-    ph, ldh = _like("out", dh, dy.dtype, dy.device, rows, cols)
+    dh = out
+    if dh is None:
+        dh = torch.empty(dy.shape, dtype=dy.dtype, device=dy.device)
+        ph, ldh = dh.data_ptr(), cols
+    else:
+        ph, ldh = _like("out", dh, dy.dtype, dy.device, rows, cols)
     _call("smat_act_grad8", dy.device, dy.data_ptr(), lddy, pq, ldq, pe,
           lde, ph, ldh, rows, cols, code, a)
     return dh
