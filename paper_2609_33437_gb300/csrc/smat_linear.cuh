@@ -183,11 +183,11 @@ __device__ __forceinline__ float cluster_load(const float* p, uint32_t rank) {
   asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(cluster_address(p, rank)) : "memory");
   return v;
 }
-__device__ __forceinline__ float4 cluster_load4(const float* p, uint32_t rank) {
+__device__ __forceinline__ float4 cluster_load4(uint32_t address) {
   float4 v;
   asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];"
                : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
-               : "r"(cluster_address(p, rank))
+               : "r"(address)
                : "memory");
   return v;
 }

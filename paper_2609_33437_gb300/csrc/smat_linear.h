@@ -54,7 +54,9 @@ struct Product {
 cudaError_t launch_simt(const Product& p, int sms, cudaStream_t s);
 
 // bf16 on the tensor cores (smat_linear_tc.cu): a and b on 16-byte boundaries, lda and ldb multiples of 8.
-cudaError_t launch_tc(const Product& p, int sms, cudaStream_t s);
+// `workspace`: tc_workspace() bytes, which go by mode, I, J and L alone.
+cudaError_t tc_workspace(const Product& p, int sms, size_t* bytes);
+cudaError_t launch_tc(const Product& p, int sms, void* workspace, cudaStream_t s);
 // Reads and clears the tensor-core products' error bits; waits for the stream.
 cudaError_t read_errors(int* out, cudaStream_t s);
 

@@ -148,19 +148,33 @@ size_t operand_bytes(const Operand& o) { return o.copied ? copy_bytes(o.rows, o.
 struct Operands {
   Operand a, b;
   size_t values;  // bytes of grad_weight's x^
-  size_t bytes() const { return values + operand_bytes(a) + operand_bytes(b); }
+  size_t parts;   // bytes of a tensor-core product's own
+  size_t bytes() const { return values + operand_bytes(a) + operand_bytes(b) + parts; }
 };
+
+size_t parts_of(int mode, int32_t dtype, int64_t I, int64_t J, int64_t L) {
+  int sms = 0;
+  size_t bytes = 0;
+  if (dtype != SMAT_BF16 || device_sms(&sms) != SMAT_OK) return 0;
+  Product p = {};
+  p.mode = mode, p.I = I, p.J = J, p.L = L;
+  return tc_workspace(p, sms, &bytes) == cudaSuccess ? up(bytes) : 0;
+}
+
 Operands operands(const smat_linear_args* g) {
   if (g->n == 0 || g->rows == 0) return {};
-  return {operand(g->x, g->rows, g->k, g->ldx, g->dtype), operand(g->w, g->n, g->k, g->ldw, g->dtype), 0};
+  return {operand(g->x, g->rows, g->k, g->ldx, g->dtype), operand(g->w, g->n, g->k, g->ldw, g->dtype), 0,
+          parts_of(kForward, g->dtype, g->rows, g->n, g->k)};
 }
 Operands operands(const smat_grad_input_args* g) {
   if (g->k == 0 || g->rows == 0) return {};
-  return {operand(g->dy, g->rows, g->n, g->lddy, g->dtype), operand(g->w, g->n, g->k, g->ldw, g->dtype), 0};
+  return {operand(g->dy, g->rows, g->n, g->lddy, g->dtype), operand(g->w, g->n, g->k, g->ldw, g->dtype), 0,
+          parts_of(kGradInput, g->dtype, g->rows, g->k, g->n)};
 }
 Operands operands(const smat_grad_weight_args* g) {
   if (g->k == 0 || g->n == 0 || g->rows == 0) return {};
-  Operands o = {operand(g->dy, g->rows, g->n, g->lddy, g->dtype), {}, 0};
+  Operands o = {operand(g->dy, g->rows, g->n, g->lddy, g->dtype), {}, 0,
+                parts_of(kGradWeight, g->dtype, g->n, g->k, g->rows)};
   if (g->q)
     o.values = copy_bytes(g->rows, g->k, elem_of(g->dtype));
   else
@@ -185,7 +199,7 @@ smat_status run_product(Product& p, const Operands& o, char* d_workspace, int sm
     if (st != SMAT_OK) return st;
     d_workspace += operand_bytes(*in[i]);
   }
-  return cuda_status(p.dtype == SMAT_BF16 ? launch_tc(p, sms, s) : launch_simt(p, sms, s), what);
+  return cuda_status(p.dtype == SMAT_BF16 ? launch_tc(p, sms, d_workspace, s) : launch_simt(p, sms, s), what);
 }
 
 // A call's size check without its message: what the size queries return 0 for.

@@ -241,7 +241,7 @@ __global__ void __launch_bounds__(kThreads, BM == 128 ? 2 : 3) simt_kernel(const
       v[0] = t.x, v[1] = t.y, v[2] = t.z, v[3] = t.w;
     } else {
       for (int s = 0; s < shares; ++s) {
-        const float4 t = cluster_load4(&sums[row][lane * 4], (uint32_t)s);
+        const float4 t = cluster_load4(cluster_address(&sums[row][lane * 4], (uint32_t)s));
         v[0] += t.x, v[1] += t.y, v[2] += t.z, v[3] += t.w;
       }
     }

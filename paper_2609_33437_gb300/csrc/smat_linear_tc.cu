@@ -35,12 +35,15 @@ constexpr int kBytesA = kBM * kBK * 2;
 constexpr int kTurn = 32 * 33 * 4;  // a warp's 32 x 32 sums, turned
 constexpr unsigned long long kWaitNs = 2000000000ull;
 
-template <int BN>
+// Swapped tiles are narrow and bound by the weight's bytes: two CTAs per SM, so that one's start and end lie beside
+// the other's copies.
+template <int BN, bool SWAP>
 struct Ring {
   static constexpr int kBytesB = BN * kBK * 2;
-  static constexpr int kStages = BN == 256 ? 4 : (BN == 128 ? 6 : 8);
+  static constexpr int kStages = SWAP ? (BN == 32 ? 5 : BN == 64 ? 4 : 3) : 4;
   static constexpr int kStage = kBytesA + kBytesB;
-  static constexpr int kBytes = kStages * kStage + kEpiWarps * kTurn + 1024;
+  static constexpr int kBytes = kStages * kStage + (SWAP ? 0 : kEpiWarps * kTurn) + 1024;
+  static constexpr int kCtas = SWAP ? 2 : 1;  // per SM
 };
 
 struct Args {
@@ -48,7 +51,9 @@ struct Args {
   int64_t tiles, tiles_r, tiles_c;  // of the tile's rows and columns (of 128 and BN)
   int slices;                       // of 64 along the sum
   int share;                        // slices per CTA of a cluster
-  bool wide;                        // rows of out, residual and q start on 32 bytes: 32 columns of a row at a time
+  float* parts;                     // the shares' sums, or NULL
+  bool by_rows;                     // rows of out and residual start on 16 bytes, those of q on 8
+  bool full_sectors;                // rows of out, residual and q start on 32 bytes
   bool wide_bias;                   // bias on 16 bytes
 };
 
@@ -148,6 +153,17 @@ __device__ __forceinline__ void take32(uint32_t at, float (&v)[32]) {
   for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(u[i]);
 }
 
+__device__ __forceinline__ void take8(uint32_t at, float (&v)[8]) {
+  uint32_t u[8];
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];\ntcgen05.wait::ld.sync.aligned;"
+      : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7])
+      : "r"(at)
+      : "memory");
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(u[i]);
+}
+
 using bf16 = __nv_bfloat16;
 
 __device__ __forceinline__ void unpack_words(const uint32_t* w, int words, float* v) {
@@ -157,15 +173,45 @@ __device__ __forceinline__ void unpack_words(const uint32_t* w, int words, float
     v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
   }
 }
-__device__ __forceinline__ void load_words8(const void* p, uint32_t (&w)[8]) {
-  asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
-               : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
-               : "l"(p));
+// 32 bytes of a row: one access to a whole sector, or two of 16 bytes, or (q) four of 8
+template <int LEAST>
+__device__ __forceinline__ void load_words8(const void* p, bool sectors, uint32_t* w) {
+  if (sectors) {
+    asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
+                 : "l"(p));
+  } else if (LEAST == 16) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      asm volatile("ld.global.v4.b32 {%0,%1,%2,%3}, [%4];"
+                   : "=r"(w[4 * h]), "=r"(w[4 * h + 1]), "=r"(w[4 * h + 2]), "=r"(w[4 * h + 3])
+                   : "l"((const char*)p + 16 * h));
+  } else {
+#pragma unroll
+    for (int h = 0; h < 4; ++h)
+      asm volatile("ld.global.v2.b32 {%0,%1}, [%2];"
+                   : "=r"(w[2 * h]), "=r"(w[2 * h + 1])
+                   : "l"((const char*)p + 8 * h));
+  }
 }
-__device__ __forceinline__ void store_words8(void* p, const uint32_t (&w)[8]) {
-  asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]),
-               "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
-               : "memory");
+template <int LEAST>
+__device__ __forceinline__ void store_words8(void* p, bool sectors, const uint32_t* w) {
+  if (sectors) {
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]),
+                 "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+                 : "memory");
+  } else if (LEAST == 16) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      asm volatile("st.global.v4.b32 [%0], {%1,%2,%3,%4};" ::"l"((char*)p + 16 * h), "r"(w[4 * h]), "r"(w[4 * h + 1]),
+                   "r"(w[4 * h + 2]), "r"(w[4 * h + 3])
+                   : "memory");
+  } else {
+#pragma unroll
+    for (int h = 0; h < 4; ++h)
+      asm volatile("st.global.v2.b32 [%0], {%1,%2};" ::"l"((char*)p + 8 * h), "r"(w[2 * h]), "r"(w[2 * h + 1])
+                   : "memory");
+  }
 }
 
 // What finishing 32 columns of a row reads, asked for before the sums are there: the residual, the older gradient or
@@ -181,15 +227,15 @@ __device__ __forceinline__ void ask_row(const Args& a, int64_t i, int64_t j, Bes
   if (i >= p.I) return;
   if (MODE == kGradInput) {
     if (p.act == SMAT_ACT_NONE) return;
-    load_words8(p.q + i * p.ldq + j, *reinterpret_cast<uint32_t (*)[8]>(&in.w[0]));
+    load_words8<8>(p.q + i * p.ldq + j, a.full_sectors, in.w);
     in.e = p.e[i * p.lde + j / kGroup];
     return;
   }
   const bf16* from = MODE == kForward ? (const bf16*)p.residual + i * p.ldr + j
                                       : (const bf16*)p.out + i * p.ldo + j;
   if (MODE == kForward ? p.residual != nullptr : p.accumulate != 0) {
-    load_words8(from, *reinterpret_cast<uint32_t (*)[8]>(&in.w[0]));
-    load_words8(from + 16, *reinterpret_cast<uint32_t (*)[8]>(&in.w[8]));
+    load_words8<16>(from, a.full_sectors, in.w);
+    load_words8<16>(from + 16, a.full_sectors, in.w + 8);
   }
 }
 
@@ -225,7 +271,7 @@ __device__ __forceinline__ uint32_t finish_row(const Args& a, int64_t i, int64_t
       ex = pack_exponent(__float_as_uint(big));
       uint32_t w[8];
       pack_words<8>(v, ex, w);
-      if (there) store_words8(p.q + i * p.ldq + j, w);
+      if (there) store_words8<8>(p.q + i * p.ldq + j, a.full_sectors, w);
     }
     SMAT_WITH_ACT(p.act, _Pragma("unroll") for (int t = 0; t < 32; ++t) v[t] = act_value<ACT>(v[t]))
   }
@@ -250,87 +296,90 @@ __device__ __forceinline__ uint32_t finish_row(const Args& a, int64_t i, int64_t
         const __nv_bfloat162 b = __floats2bfloat162_rn(v[16 * h + 2 * t], v[16 * h + 2 * t + 1]);
         w[t] = *reinterpret_cast<const uint32_t*>(&b);
       }
-      store_words8(out + 16 * h, w);
+      store_words8<16>(out + 16 * h, a.full_sectors, w);
     }
   }
   return ex;
 }
 
-// Column j of rows i .. i + 31, one thread; the warp holds 32 neighbouring columns from a multiple of 32 on. Rows are
-// taken 8 at a time, what they read first.
-template <int MODE>
-__device__ __forceinline__ void finish_column(const Args& a, int64_t i, int64_t j, float (&v)[32]) {
+// Column j of rows i .. i + N - 1, one thread; the warp holds 32 neighbouring columns from a multiple of 32 on. What
+// the rows read is asked for first, all of it.
+template <int MODE, int N>
+__device__ __forceinline__ void finish_column(const Args& a, int64_t i, int64_t j, float (&v)[N]) {
   const Product& p = a.p;
+  if (i >= p.I) return;
+  const int rows = (int)(p.I - i < N ? p.I - i : N);
   const bool there = j < p.J;
+  const int mine = there ? rows : 0;
   const int lane = threadIdx.x % 32;
   bf16* out = (bf16*)p.out + i * p.ldo + j;
-  const float bias = MODE == kForward && p.bias && there ? to_float(((const bf16*)p.bias)[j]) : 0.0f;
+  if (MODE == kForward) {
+    float x[N];
+    const float bias = p.bias && there ? to_float(((const bf16*)p.bias)[j]) : 0.0f;
+    if (p.residual) {
+      const bf16* r = (const bf16*)p.residual + i * p.ldr + j;
 #pragma unroll
-  for (int s = 0; s < 32; s += 8) {
-    const int rows = (int)(p.I - i - s < 8 ? p.I - i - s : 8);
-    if (rows <= 0) return;
-    float x[8];
-    if (MODE == kForward) {
+      for (int t = 0; t < N; ++t) x[t] = t < mine ? to_float(r[t * p.ldr]) : 0.0f;
+    }
 #pragma unroll
-      for (int t = 0; t < 8; ++t)
-        x[t] = p.residual && there && t < rows
-                   ? to_float(((const bf16*)p.residual)[(i + s + t) * p.ldr + j])
-                   : 0.0f;
+    for (int t = 0; t < N; ++t) v[t] += bias;
+    if (p.q) {
 #pragma unroll
-      for (int t = 0; t < 8; ++t) v[s + t] += bias;
-      if (p.q) {
-#pragma unroll
-        for (int t = 0; t < 8; ++t) {
-          const uint32_t top =
-              __reduce_max_sync(0xFFFFFFFFu, there ? __float_as_uint(fabsf(v[s + t])) : 0u);
-          const uint32_t ex = pack_exponent(top);
-          if (there && t < rows) {
-            p.q[(i + s + t) * p.ldq + j] = (int8_t)pack_one(v[s + t], ex);
-            if (lane == 0) p.e[(i + s + t) * p.lde + j / kGroup] = (uint8_t)ex;
-          }
+      for (int t = 0; t < N; ++t) {
+        const uint32_t top = __reduce_max_sync(0xFFFFFFFFu, there ? __float_as_uint(fabsf(v[t])) : 0u);
+        const uint32_t ex = pack_exponent(top);
+        if (t < mine) {
+          p.q[(i + t) * p.ldq + j] = (int8_t)pack_one(v[t], ex);
+          if (lane == 0) p.e[(i + t) * p.lde + j / kGroup] = (uint8_t)ex;
         }
       }
-      SMAT_WITH_ACT(p.act, _Pragma("unroll") for (int t = 0; t < 8; ++t) v[s + t] = act_value<ACT>(v[s + t]) + x[t])
     }
-    if (MODE == kGradInput && p.act != SMAT_ACT_NONE) {
+    SMAT_WITH_ACT(p.act, _Pragma("unroll") for (int t = 0; t < N; ++t) v[t] = act_value<ACT>(v[t]))
+    if (p.residual) {
 #pragma unroll
-      for (int t = 0; t < 8; ++t)
-        x[t] = there && t < rows ? (float)p.q[(i + s + t) * p.ldq + j] *
-                                       unpack_scale(p.e[(i + s + t) * p.lde + j / kGroup])
-                                 : 0.0f;
-      SMAT_WITH_ACT(p.act, _Pragma("unroll") for (int t = 0; t < 8; ++t) v[s + t] *= act_slope<ACT>(x[t]))
+      for (int t = 0; t < N; ++t) v[t] += x[t];
     }
-    if (MODE == kGradWeight && p.accumulate) {
+  } else if (MODE == kGradInput ? p.act != SMAT_ACT_NONE : p.accumulate != 0) {
+    float x[N];
+    if (MODE == kGradInput) {
+      const int8_t* q = p.q + i * p.ldq + j;
+      const uint8_t* e = p.e + i * p.lde + j / kGroup;
+      int qs[N];
+      uint32_t es[N];
 #pragma unroll
-      for (int t = 0; t < 8; ++t) x[t] = there && t < rows ? to_float(out[(s + t) * p.ldo]) : 0.0f;
+      for (int t = 0; t < N; ++t) {
+        qs[t] = t < mine ? q[t * p.ldq] : 0;
+        es[t] = t < mine ? e[t * p.lde] : 0;
+      }
 #pragma unroll
-      for (int t = 0; t < 8; ++t) v[s + t] += x[t];
+      for (int t = 0; t < N; ++t) x[t] = (float)qs[t] * unpack_scale(es[t]);
+      SMAT_WITH_ACT(p.act, _Pragma("unroll") for (int t = 0; t < N; ++t) v[t] *= act_slope<ACT>(x[t]))
+    } else {
+#pragma unroll
+      for (int t = 0; t < N; ++t) x[t] = t < mine ? to_float(out[t * p.ldo]) : 0.0f;
+#pragma unroll
+      for (int t = 0; t < N; ++t) v[t] += x[t];
     }
-#pragma unroll
-    for (int t = 0; t < 8; ++t)
-      if (there && t < rows) out[(s + t) * p.ldo] = from_float<bf16>(v[s + t]);
   }
+#pragma unroll
+  for (int t = 0; t < N; ++t)
+    if (t < mine) out[t * p.ldo] = from_float<bf16>(v[t]);
 }
 
-// `count` blocks of 32 columns of the tile, from column col0 of the result on, of the warp's 32 rows (row0 on; rows
-// and columns of the tile, that is): `sums(c, v)` gives block c's sums.
-template <int MODE, bool SWAP, class Sums>
-__device__ __forceinline__ void finish(const Args& a, int64_t row0, int64_t col0, int first, int end, int step,
-                                       float* turn, Sums&& sums) {
+// Blocks `first`, `first + step`, ... below `end` of 32 columns of a tile that begins at row row0 (this warp's 32) and
+// column col0 of the result: `sums(c, v)` gives block c's sums.
+template <int MODE, class Sums>
+__device__ __forceinline__ void finish_rows(const Args& a, int64_t row0, int64_t col0, int first, int end, int step,
+                                            float* turn, Sums&& sums) {
   const int lane = threadIdx.x % 32;
   if (first >= end) return;
-  const bool rows = !SWAP && a.wide;
   Beside in;
-  if (rows && col0 + 32 * first + 32 <= a.p.J) ask_row<MODE>(a, row0 + lane, col0 + 32 * first, in);
+  if (a.by_rows && col0 + 32 * first + 32 <= a.p.J) ask_row<MODE>(a, row0 + lane, col0 + 32 * first, in);
   for (int c = first; c < end; c += step) {
     const int64_t col = col0 + 32 * c;
     float v[32];
     sums(c, v);
-    if (SWAP) {
-      if (col < a.p.I && row0 < a.p.J) finish_column<MODE>(a, col, row0 + lane, v);
-      continue;
-    }
-    if (rows && col + 32 <= a.p.J) {
+    if (a.by_rows && col + 32 <= a.p.J) {
       const Beside now = in;
       if (c + step < end && col + 32 * step + 32 <= a.p.J) ask_row<MODE>(a, row0 + lane, col + 32 * step, in);
       const uint32_t ex = finish_row<MODE>(a, row0 + lane, col, v, now);
@@ -345,7 +394,34 @@ __device__ __forceinline__ void finish(const Args& a, int64_t row0, int64_t col0
     __syncwarp();
 #pragma unroll
     for (int t = 0; t < 32; ++t) v[t] = turn[t * 33 + lane];
-    finish_column<MODE>(a, row0, col + lane, v);
+    finish_column<MODE, 32>(a, row0, col + lane, v);
+  }
+}
+
+// A CTA's share of a tile's sums lies as [column][128 rows], so that a warp's 32 rows of a column are 128 bytes in a
+// row: in the workspace (a.parts), or, where the tile has no more than 8 columns, in its own shared memory, which the
+// others read across the cluster. (Reading larger tiles there is slow: 128 x 256 sums of 8 shares took 15 us, through
+// the workspace, which stays in L2, 3.) The shares are added in the cluster's order, several CTAs' loads in flight.
+template <int N>
+__device__ __forceinline__ void put_part(float* p, const float (&v)[N]) {
+#pragma unroll
+  for (int t = 0; t < N; ++t) p[t * kBM] = v[t];
+}
+template <int N, class Load>
+__device__ __forceinline__ void add_parts(uint32_t shares, float (&v)[N], Load&& load) {
+  constexpr int kAhead = N == 32 ? 2 : 4;
+#pragma unroll
+  for (int t = 0; t < N; ++t) v[t] = 0.0f;
+  for (uint32_t s = 0; s < shares; s += kAhead) {
+    float x[kAhead][N];
+#pragma unroll
+    for (int h = 0; h < kAhead; ++h)
+#pragma unroll
+      for (int t = 0; t < N; ++t) x[h][t] = s + h < shares ? load(s + h, t) : 0.0f;
+#pragma unroll
+    for (int h = 0; h < kAhead; ++h)
+#pragma unroll
+      for (int t = 0; t < N; ++t) v[t] += x[h][t];
   }
 }
 
@@ -360,14 +436,14 @@ __device__ __forceinline__ void tile_place(const Args& a, int64_t tile, int64_t&
 }
 
 template <int MODE, bool SWAP, int BN>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(kThreads, Ring<BN, SWAP>::kCtas)
     tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
               const __grid_constant__ Args a) {
   // the tile's rows come from W where swapped, from the other operand else
   constexpr bool A_MN = SWAP ? MODE == kGradInput : MODE == kGradWeight;
   constexpr bool B_MN = SWAP ? false : MODE != kForward;
   static_assert(!(SWAP && MODE == kGradWeight), "a weight gradient's rows and columns are both a layer's");
-  constexpr int kStages = Ring<BN>::kStages, kStage = Ring<BN>::kStage;
+  constexpr int kStages = Ring<BN, SWAP>::kStages, kStage = Ring<BN, SWAP>::kStage;
 
   extern __shared__ uint8_t raw[];
   __shared__ __align__(8) uint64_t bars[2 * kStages + 5];
@@ -379,7 +455,36 @@ __global__ void __launch_bounds__(kThreads, 1)
   const uint32_t full = smem_address(bars), empty = full + 8 * kStages, sums_full = empty + 8 * kStages,
                  sums_empty = sums_full + 16, drained = sums_empty + 16;
 
-  if (threadIdx.x == 0) {
+  uint32_t shares, rank;
+  asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(shares));
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+  const int slice0 = (int)rank * a.share;
+  const int slices = max(0, min(a.share, a.slices - slice0));
+  const int64_t first_tile = blockIdx.x / shares, step = gridDim.x / shares;
+
+  auto turn_of = [&](int w) { return reinterpret_cast<float*>(ring + kStages * kStage + w * kTurn); };
+  auto fetch = [&](uint32_t s, int64_t tile, int k) {
+    int64_t tr, tc;
+    tile_place(a, tile, tr, tc);
+    const int r0 = (int)(tr * kBM), c0 = (int)(tc * BN), l = (slice0 + k) * kBK;
+    const uint32_t bar = full + 8 * s, to_a = smem_address(ring) + s * kStage, to_b = to_a + kBytesA;
+    bar_expect(bar, kStage);
+    if (A_MN) {
+#pragma unroll
+      for (int b = 0; b < kBM / 64; ++b) tma_load(to_a + b * 8192, &map_a, r0 + 64 * b, l, bar);
+    } else {
+      tma_load(to_a, &map_a, l, r0, bar);
+    }
+    if (B_MN) {
+#pragma unroll
+      for (int b = 0; b < BN / 64; ++b) tma_load(to_b + b * 8192, &map_b, c0 + 64 * b, l, bar);
+    } else {
+      tma_load(to_b, &map_b, l, c0, bar);
+    }
+  };
+  const int ahead = first_tile < a.tiles ? min(slices, kStages) : 0;  // slices fetched before the CTA meets
+
+  if (warp == kTmaWarp && lane == 0) {
     dead_flag = 0;
     for (int s = 0; s < kStages; ++s) {
       bar_init(full + 8 * s, 1);
@@ -391,7 +496,9 @@ __global__ void __launch_bounds__(kThreads, 1)
       bar_init(sums_empty + 8 * b, kEpiWarps);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    for (int k = 0; k < ahead; ++k) fetch(k, first_tile, k);
   }
+  __syncwarp();
   if (warp == kMmaWarp) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_address(&tmem_at)),
                  "r"(2 * BN)
@@ -403,41 +510,16 @@ __global__ void __launch_bounds__(kThreads, 1)
   fence_after();
   const uint32_t tmem = tmem_at;
 
-  uint32_t shares, rank;
-  asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(shares));
-  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
-  const int slice0 = (int)rank * a.share;
-  const int slices = max(0, min(a.share, a.slices - slice0));
-  const int64_t step = gridDim.x / shares;
-
   if (warp == kTmaWarp && lane == 0) {
-    uint32_t n = 0;  // slices fetched so far
+    uint32_t n = (uint32_t)ahead;  // slices fetched so far
     bool ok = true;
-    for (int64_t tile = blockIdx.x / shares; ok && tile < a.tiles; tile += step) {
-      int64_t tr, tc;
-      tile_place(a, tile, tr, tc);
-      const int r0 = (int)(tr * kBM), c0 = (int)(tc * BN);
-      for (int k = 0; k < slices; ++k, ++n) {
+    for (int64_t tile = first_tile; ok && tile < a.tiles; tile += step)
+      for (int k = tile == first_tile ? ahead : 0; k < slices; ++k, ++n) {
         const uint32_t s = n % kStages;
         ok = bar_wait(empty + 8 * s, (n / kStages + 1) & 1, dead);
         if (!ok) break;
-        const uint32_t bar = full + 8 * s, to_a = smem_address(ring) + s * kStage, to_b = to_a + kBytesA;
-        const int l = (slice0 + k) * kBK;
-        bar_expect(bar, kStage);
-        if (A_MN) {
-#pragma unroll
-          for (int b = 0; b < kBM / 64; ++b) tma_load(to_a + b * 8192, &map_a, r0 + 64 * b, l, bar);
-        } else {
-          tma_load(to_a, &map_a, l, r0, bar);
-        }
-        if (B_MN) {
-#pragma unroll
-          for (int b = 0; b < BN / 64; ++b) tma_load(to_b + b * 8192, &map_b, c0 + 64 * b, l, bar);
-        } else {
-          tma_load(to_b, &map_b, l, c0, bar);
-        }
+        fetch(s, tile, k);
       }
-    }
     if (!ok)  // copies in flight land before the CTA ends
       for (uint32_t s = 0; s < kStages && s < n; ++s) {
         const uint32_t last = n - 1 - s;
@@ -448,7 +530,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     constexpr uint32_t kInst = kInstruction<A_MN, B_MN, BN>;
     uint32_t n = 0, made = 0;
     bool ok = true;
-    for (int64_t tile = blockIdx.x / shares; ok && tile < a.tiles; tile += step, ++made) {
+    for (int64_t tile = first_tile; ok && tile < a.tiles; tile += step, ++made) {
       const uint32_t half = made & 1, sums = tmem + half * BN;
       ok = bar_wait(sums_empty + 8 * half, (made / 2 + 1) & 1, dead);
       if (!ok) break;
@@ -474,68 +556,97 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
   } else if (warp < kEpiWarps) {
     const int quarter = warp % 4;  // the 32 rows of tensor memory that this warp may read
-    float* turn = reinterpret_cast<float*>(ring + kStages * kStage + warp * kTurn);
+    // this thread's row of the CTA's share of the sums. The ring is free by then: every product that read it is done
+    float* part = (a.parts ? a.parts + ((size_t)first_tile * shares + rank) * BN * kBM : reinterpret_cast<float*>(ring)) +
+                  32 * quarter + lane;
     uint32_t made = 0;
-    for (int64_t tile = blockIdx.x / shares; tile < a.tiles; tile += step, ++made) {
+    for (int64_t tile = first_tile; tile < a.tiles; tile += step, ++made) {
       int64_t tr, tc;
       tile_place(a, tile, tr, tc);
       const int64_t r0 = tr * kBM + 32 * quarter, c0 = tc * BN;
       const uint32_t half = made & 1, sums = tmem + half * BN + ((uint32_t)(32 * quarter) << 16);
       if (!bar_wait(sums_full + 8 * half, made / 2 & 1, dead)) break;
       fence_after();
-      // this warp's blocks of 32 columns: the first or the second half of the tile's
-      constexpr int kBlocks = BN / 32, kMine = (kBlocks + 1) / 2;
-      const int first = warp / 4 * kMine, end = min(kBlocks, first + kMine);
-      auto take = [&](int c, float(&v)[32]) {
-        if (slices > 0) {
-          take32(sums + 32 * c, v);
-        } else {
-#pragma unroll
-          for (int t = 0; t < 32; ++t) v[t] = 0.0f;
-        }
+      auto release = [&] {  // this warp has what it needs of these sums
+        fence_before();
+        __syncwarp();
+        if (lane == 0) bar_arrive(sums_empty + 8 * half);
       };
-      if (shares == 1) {
-        if (first >= end && lane == 0) bar_arrive(sums_empty + 8 * half);  // none of a narrow tile's columns
-        finish<MODE, SWAP>(a, r0, c0, first, end, 1, turn, [&](int c, float(&v)[32]) {
-          take(c, v);
-          if (c + 1 == end) {  // the last of this warp's columns are out
-            fence_before();
-            __syncwarp();
-            if (lane == 0) bar_arrive(sums_empty + 8 * half);
-          }
-        });
-      } else {
-        // the ring is free: every product that read it is done. [column][128 rows]
-        float* part = reinterpret_cast<float*>(ring) + 32 * quarter + lane;
-        for (int c = first; c < end; ++c) {
-          float v[32];
-          take(c, v);
+      if constexpr (SWAP) {
+        const int blocks = (int)((min((int64_t)BN, a.p.I - c0) + 7) / 8);  // of 8 columns of the tile, rows of the result
+        for (int c = warp / 4; c < blocks; c += kEpiWarps / 4) {
+          float v[8];
+          if (slices > 0) {
+            take8(sums + 8 * c, v);
+          } else {
 #pragma unroll
-          for (int t = 0; t < 32; ++t) part[(32 * c + t) * kBM] = v[t];
+            for (int t = 0; t < 8; ++t) v[t] = 0.0f;
+          }
+          if (shares == 1) {
+            if (r0 < a.p.J) finish_column<MODE, 8>(a, c0 + 8 * c, r0 + lane, v);
+          } else {
+            put_part(part + 8 * c * kBM, v);
+          }
+        }
+        release();
+      } else {
+        // this warp's blocks of 32 columns: the first or the second half of the tile's
+        constexpr int kMine = BN / 64;
+        const int first = warp / 4 * kMine, end = first + kMine;
+        auto take = [&](int c, float(&v)[32]) {
+          if (slices > 0) {
+            take32(sums + 32 * c, v);
+          } else {
+#pragma unroll
+            for (int t = 0; t < 32; ++t) v[t] = 0.0f;
+          }
+        };
+        if (shares == 1) {
+          finish_rows<MODE>(a, r0, c0, first, end, 1, turn_of(warp), [&](int c, float(&v)[32]) {
+            take(c, v);
+            if (c + 1 == end) release();
+          });
+        } else {
+          for (int c = first; c < end && c0 + 32 * c < a.p.J && r0 < a.p.I; ++c) {
+            float v[32];
+            take(c, v);
+            put_part(part + 32 * c * kBM, v);
+          }
         }
       }
     }
   }
   __syncwarp();
   if (shares > 1) {
-    // one tile per cluster: its CTAs add up and finish 32 columns each in turn
+    // one tile per cluster: its CTAs add up and finish blocks of its columns in turn
     __syncthreads();
     cluster_sync();
     if (warp < kEpiWarps && !*dead) {
       int64_t tr, tc;
-      tile_place(a, blockIdx.x / shares, tr, tc);
+      tile_place(a, first_tile, tr, tc);
       const int quarter = warp % 4;
-      const float* part = reinterpret_cast<const float*>(ring) + 32 * quarter + lane;
-      float* turn = reinterpret_cast<float*>(ring + kStages * kStage + warp * kTurn);
-      finish<MODE, SWAP>(
-          a, tr * kBM + 32 * quarter, tc * BN, (int)rank + (int)shares * (warp / 4), BN / 32,
-          (int)shares * (kEpiWarps / 4), turn, [&](int c, float(&v)[32]) {
-#pragma unroll
-            for (int t = 0; t < 32; ++t) v[t] = 0.0f;
-            for (uint32_t s = 0; s < shares; ++s)
-#pragma unroll
-              for (int t = 0; t < 32; ++t) v[t] += cluster_load(part + (32 * c + t) * kBM, s);
-          });
+      const int64_t r0 = tr * kBM + 32 * quarter, c0 = tc * BN;
+      const float* part = (a.parts ? a.parts + (size_t)first_tile * shares * BN * kBM : reinterpret_cast<float*>(ring)) +
+                          32 * quarter + lane;
+      const int first = (int)rank + (int)shares * (warp / 4), turns = (int)shares * (kEpiWarps / 4);
+      if constexpr (SWAP) {
+        const int cols = (int)min((int64_t)BN, a.p.I - c0);
+        for (int c = first; 8 * c < cols && r0 < a.p.J; c += turns) {
+          float v[8];
+          if (a.parts)
+            add_parts(shares, v, [&](uint32_t s, int t) { return __ldcg(part + ((size_t)s * BN + 8 * c + t) * kBM); });
+          else
+            add_parts(shares, v, [&](uint32_t s, int t) {
+              return 8 * c + t < cols ? cluster_load(part + (8 * c + t) * kBM, s) : 0.0f;
+            });
+          finish_column<MODE, 8>(a, c0 + 8 * c, r0 + lane, v);
+        }
+      } else {
+        const int blocks = r0 < a.p.I ? (int)((min((int64_t)BN, a.p.J - c0) + 31) / 32) : 0;
+        finish_rows<MODE>(a, r0, c0, first, blocks, turns, turn_of(warp), [&](int c, float(&v)[32]) {
+          add_parts(shares, v, [&](uint32_t s, int t) { return __ldcg(part + ((size_t)s * BN + 32 * c + t) * kBM); });
+        });
+      }
     }
     cluster_sync();
   }
@@ -576,25 +687,86 @@ bool encode(CUtensorMap* map, const void* p, int64_t inner, int64_t outer, int64
                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-bool can(const void* p, int64_t ld, size_t elem) { return (uintptr_t)p % 32 == 0 && (uint64_t)ld * elem % 32 == 0; }
+// How many clusters of `shares` CTAs of a kernel run at once on the current device, asked for once (a GPU's parts hold
+// different numbers of SMs, so this is less than SMs / shares).
+template <class F>
+int64_t clusters_at_once(F* f, int shares, int bytes, std::atomic<int> (&known)[64][9]) {
+  int dev = 0, n = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev >= 64) return 1;
+  if ((n = known[dev][shares].load(std::memory_order_relaxed)) > 0) return n;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)shares);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = bytes;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim = {(unsigned)shares, 1, 1};
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  if (cudaOccupancyMaxActiveClusters(&n, f, &cfg) != cudaSuccess || n < 1) {
+    cudaGetLastError();
+    n = 1;
+  }
+  known[dev][shares].store(n, std::memory_order_relaxed);
+  return n;
+}
+
+// One product's launch: tiles, shares of the sum, workspace.
+struct Plan {
+  int64_t tiles_r, tiles_c, ctas;
+  int slices, share, shares;
+  size_t bytes;  // of the shares' sums
+};
 
 template <int MODE, bool SWAP, int BN>
-cudaError_t launch_tile(const Product& p, int sms, cudaStream_t s) {
+cudaError_t plan_tile(const Product& p, int sms, Plan* plan) {
+  static std::atomic<uint64_t> allowed;
+  static std::atomic<int> clusters[64][9];
+  auto* f = tc_kernel<MODE, SWAP, BN>;
+  const cudaError_t e = allow_shared(f, Ring<BN, SWAP>::kBytes, allowed);
+  if (e != cudaSuccess) return e;
+  const int64_t R = SWAP ? p.J : p.I, C = SWAP ? p.I : p.J;
+  Plan g = {};
+  g.tiles_r = (R + kBM - 1) / kBM;
+  g.tiles_c = (C + BN - 1) / BN;
+  g.slices = (int)((p.L + kBK - 1) / kBK);
+  const int64_t tiles = g.tiles_r * g.tiles_c, room = (int64_t)Ring<BN, SWAP>::kCtas * sms;
+  // Shares of the sum as long as all CTAs have room at once, three slices in each at least. Where the tensor cores bound
+  // a tile, all clusters have to run at once, or the last ones double the time; swapped tiles wait for memory, and more
+  // bytes in flight outweigh that.
+  int shares = 8;
+  while (shares > 1 && (tiles * shares > room || g.slices < 3 * shares ||
+                        (!SWAP && tiles > clusters_at_once(f, shares, Ring<BN, SWAP>::kBytes, clusters))))
+    --shares;
+  g.share = (g.slices + shares - 1) / shares;
+  g.shares = shares > 1 ? (g.slices + g.share - 1) / g.share : 1;
+  g.ctas = g.shares > 1 ? tiles * g.shares : (tiles < room ? tiles : room);
+  if (g.shares > 1 && !(SWAP && p.I <= 8)) g.bytes = (size_t)tiles * g.shares * BN * kBM * sizeof(float);
+  *plan = g;
+  return cudaSuccess;
+}
+
+template <int MODE, bool SWAP, int BN>
+cudaError_t launch_tile(const Product& p, int sms, void* workspace, cudaStream_t s) {
   constexpr bool A_MN = SWAP ? MODE == kGradInput : MODE == kGradWeight;
   constexpr bool B_MN = SWAP ? false : MODE != kForward;
+  Plan g;
+  cudaError_t e = plan_tile<MODE, SWAP, BN>(p, sms, &g);
+  if (e != cudaSuccess) return e;
   Args a = {};
   a.p = p;
   const int64_t R = SWAP ? p.J : p.I, C = SWAP ? p.I : p.J;
-  a.tiles_r = (R + kBM - 1) / kBM;
-  a.tiles_c = (C + BN - 1) / BN;
-  a.tiles = a.tiles_r * a.tiles_c;
-  a.slices = (int)((p.L + kBK - 1) / kBK);
-  a.wide = can(p.out, p.ldo, 2) && (!p.residual || can(p.residual, p.ldr, 2)) && (!p.q || can(p.q, p.ldq, 1));
+  a.tiles_r = g.tiles_r, a.tiles_c = g.tiles_c, a.tiles = g.tiles_r * g.tiles_c;
+  a.slices = g.slices, a.share = g.share;
+  a.parts = g.bytes ? (float*)workspace : nullptr;
+  auto rows_on = [](const void* q, int64_t ld, int elem, int bytes) {
+    return (uintptr_t)q % bytes == 0 && (uint64_t)ld * elem % bytes == 0;
+  };
+  a.by_rows = rows_on(p.out, p.ldo, 2, 16) && (!p.residual || rows_on(p.residual, p.ldr, 2, 16)) &&
+              (!p.q || rows_on(p.q, p.ldq, 1, 8));
+  a.full_sectors = rows_on(p.out, p.ldo, 2, 32) && (!p.residual || rows_on(p.residual, p.ldr, 2, 32)) &&
+                   (!p.q || rows_on(p.q, p.ldq, 1, 32));
   a.wide_bias = (uintptr_t)p.bias % 16 == 0;
-  // shares of the sum while the CTAs are fewer than the SMs, four slices in each at least
-  int shares = 1;
-  while (shares < 8 && a.tiles * shares * 2 <= sms && a.slices >= shares * 2 * 4) shares *= 2;
-  a.share = (a.slices + shares - 1) / shares;
 
   CUtensorMap ma = {}, mb = {};  // not read where the sum is over nothing
   if (p.L > 0) {
@@ -604,43 +776,66 @@ cudaError_t launch_tile(const Product& p, int sms, cudaStream_t s) {
                     (B_MN ? encode(&mb, pb, C, p.L, ldb, kBK) : encode(&mb, pb, p.L, C, ldb, BN));
     if (!ok) return cudaErrorNotSupported;
   }
-  auto* f = tc_kernel<MODE, SWAP, BN>;
-  static std::atomic<uint64_t> allowed;
-  const cudaError_t e = allow_shared(f, Ring<BN>::kBytes, allowed);
-  if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
-  const int64_t ctas = shares > 1 ? a.tiles * shares : (a.tiles < sms ? a.tiles : sms);
-  cfg.gridDim = dim3((unsigned)ctas);
+  cfg.gridDim = dim3((unsigned)g.ctas);
   cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = Ring<BN>::kBytes;
+  cfg.dynamicSmemBytes = Ring<BN, SWAP>::kBytes;
   cfg.stream = s;
   cudaLaunchAttribute at[1];
   at[0].id = cudaLaunchAttributeClusterDimension;
-  at[0].val.clusterDim = {(unsigned)shares, 1, 1};
+  at[0].val.clusterDim = {(unsigned)g.shares, 1, 1};
   cfg.attrs = at;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, f, ma, mb, a);
+  return cudaLaunchKernelEx(&cfg, tc_kernel<MODE, SWAP, BN>, ma, mb, a);
 }
 
-template <int MODE>
-cudaError_t launch_mode(const Product& p, int sms, cudaStream_t s) {
-  if (MODE != kGradWeight) {
-    constexpr int M = MODE == kGradWeight ? (int)kForward : MODE;
-    if (p.I <= 32) return launch_tile<M, true, 32>(p, sms, s);
-    if (p.I <= 64) return launch_tile<M, true, 64>(p, sms, s);
-    if (p.I <= 128) return launch_tile<M, true, 128>(p, sms, s);
+// The tile for a product: go.run<MODE, SWAP, BN>() of it. Up to 128 rows the weight's columns take the tile's 128 rows.
+template <int MODE, class Go>
+cudaError_t choose_mode(const Product& p, Go&& go) {
+  if constexpr (MODE != kGradWeight) {
+    if (p.I <= 32) return go.template run<MODE, true, 32>();
+    if (p.I <= 64) return go.template run<MODE, true, 64>();
+    if (p.I <= 128) return go.template run<MODE, true, 128>();
   }
-  return launch_tile<MODE, false, 256>(p, sms, s);
+  return go.template run<MODE, false, 256>();
 }
+template <class Go>
+cudaError_t choose(const Product& p, Go&& go) {
+  switch (p.mode) {
+    case kForward: return choose_mode<kForward>(p, go);
+    case kGradInput: return choose_mode<kGradInput>(p, go);
+    default: return choose_mode<kGradWeight>(p, go);
+  }
+}
+
+struct Launch {
+  const Product& p;
+  int sms;
+  void* workspace;
+  cudaStream_t s;
+  template <int MODE, bool SWAP, int BN>
+  cudaError_t run() const {
+    return launch_tile<MODE, SWAP, BN>(p, sms, workspace, s);
+  }
+};
+struct Size {
+  const Product& p;
+  int sms;
+  size_t* bytes;
+  template <int MODE, bool SWAP, int BN>
+  cudaError_t run() const {
+    Plan g;
+    const cudaError_t e = plan_tile<MODE, SWAP, BN>(p, sms, &g);
+    *bytes = e == cudaSuccess ? g.bytes : 0;
+    return e;
+  }
+};
 
 }  // namespace
 
-cudaError_t launch_tc(const Product& p, int sms, cudaStream_t s) {
-  switch (p.mode) {
-    case kForward: return launch_mode<kForward>(p, sms, s);
-    case kGradInput: return launch_mode<kGradInput>(p, sms, s);
-    default: return launch_mode<kGradWeight>(p, sms, s);
-  }
+cudaError_t tc_workspace(const Product& p, int sms, size_t* bytes) { return choose(p, Size{p, sms, bytes}); }
+cudaError_t launch_tc(const Product& p, int sms, void* workspace, cudaStream_t s) {
+  return choose(p, Launch{p, sms, workspace, s});
 }
 
 cudaError_t read_errors(int* out, cudaStream_t s) {
