@@ -50,14 +50,17 @@ struct Product {
   int accumulate;  // grad_weight: add to what out holds
 };
 
-// fp32 (smat_linear_simt.cu): any size, stride and alignment.
-cudaError_t launch_simt(const Product& p, int sms, cudaStream_t s);
+// fp32 (smat_linear_f32.cu): any size, stride and alignment. `workspace`: f32_workspace() bytes, which go by mode, I, J
+// and L alone.
+cudaError_t f32_workspace(const Product& p, int sms, size_t* bytes);
+cudaError_t launch_f32(const Product& p, int sms, void* workspace, cudaStream_t s);
 
 // bf16 on the tensor cores (smat_linear_tc.cu): a and b on 16-byte boundaries, lda and ldb multiples of 8.
 // `workspace`: tc_workspace() bytes, which go by mode, I, J and L alone.
 cudaError_t tc_workspace(const Product& p, int sms, size_t* bytes);
 cudaError_t launch_tc(const Product& p, int sms, void* workspace, cudaStream_t s);
-// Reads and clears the tensor-core products' error bits; waits for the stream.
+// The tensor-core products' error bits of the current device; read and cleared (waits for the stream).
+cudaError_t error_word(int** at);
 cudaError_t read_errors(int* out, cudaStream_t s);
 
 // smat_pack8.cu; `dy` NULL: out = act(h^), else dy * act'(h^)

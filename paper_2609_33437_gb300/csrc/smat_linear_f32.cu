@@ -1,0 +1,711 @@
+// The linear layers' products of fp32 matrices, to fp32 accuracy (smat_linear.h, Product; include/smat.h).
+//
+// Large ones run on the tensor cores. A first kernel cuts every fp32 value into three bf16 values, hi + mid + lo, 8 bits
+// of its significand each: exactly the value. The product then is six products of those parts (the three left out are
+// below 2^-24 of the whole, like one rounding), for a slice of 64 of the sum at a time and the small ones first, so that
+// what an addition in tensor memory cuts off is cut off sums that are small yet; eight warps add the slices' sums in
+// registers, rounding to nearest. Six bf16 products take a quarter of the time that the fp32 units need.
+//
+// An infinity times a part that is 0 would give NaN. So the first kernel says whether it met an infinity or NaN, and
+// where it did, the second one makes its tiles on the fp32 units instead.
+//
+// Small ones, and those of few rows, run on the fp32 units as they are: the cutting would cost more than it gains.
+// A CTA of 256 threads makes a tile of BM x 128 sums, BM / 16 x 8 of them in each thread's registers as packed pairs (one
+// instruction multiplies and adds two). Slices of 16 along l go through shared memory, the next one loaded to registers
+// while one is multiplied. Where the tiles are fewer than the SMs, l is cut among the CTAs of a cluster; each leaves its
+// sums in its own shared memory and then adds up and finishes its share of the rows, in the cluster's order: no atomics,
+// the same result every time.
+
+#include "smat_linear.h"
+#include "smat_linear_tc.cuh"
+
+namespace smat {
+namespace lin {
+namespace {
+
+constexpr int kUnits = 256;  // threads that make a tile on the fp32 units
+constexpr int kBN = 128, kSimtK = 16, kPad = 4;
+
+// A barrier of the first kUnits threads (both kernels' warps 0 to 7).
+__device__ __forceinline__ void units_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
+
+struct Args {
+  Product p;
+  bool va, vb;    // operands whose rows may be read 16 bytes at a time
+  bool vr, vo;    // residual, out likewise
+  int64_t share;  // of the sum, per CTA of a cluster
+};
+
+// four values of a row, `count` of them there
+__device__ __forceinline__ float4 load4(const float* p, int64_t count, bool vec) {
+  if (vec && count >= 4) return *reinterpret_cast<const float4*>(p);
+  return make_float4(count > 0 ? p[0] : 0.0f, count > 1 ? p[1] : 0.0f, count > 2 ? p[2] : 0.0f, count > 3 ? p[3] : 0.0f);
+}
+
+// One operand's slice [R][kSimtK] into registers, then into shared memory as [kSimtK][R + kPad].
+template <int R, bool MN>
+struct Slice {
+  static constexpr int kVecs = R * kSimtK / 4, kSteps = (kVecs + kUnits - 1) / kUnits;
+  float4 v[kSteps];
+
+  __device__ __forceinline__ void load(const float* p, int64_t ld, int64_t first, int64_t end, int64_t l, int64_t l_end,
+                                       bool vec) {
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+      const int at = threadIdx.x + s * kUnits;
+      v[s] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      if (kVecs % kUnits && at >= kVecs) continue;
+      if (MN) {
+        const int64_t k = l + at / (R / 4), i = first + at % (R / 4) * 4;
+        if (k < l_end) v[s] = load4(p + k * ld + i, end - i, vec);
+      } else {
+        const int64_t i = first + at / (kSimtK / 4), k = l + at % (kSimtK / 4) * 4;
+        if (i < end) v[s] = load4(p + i * ld + k, l_end - k, vec);
+      }
+    }
+  }
+
+  __device__ __forceinline__ void store(float (*to)[R + kPad]) const {
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+      const int at = threadIdx.x + s * kUnits;
+      if (kVecs % kUnits && at >= kVecs) continue;
+      if (MN) {
+        *reinterpret_cast<float4*>(&to[at / (R / 4)][at % (R / 4) * 4]) = v[s];
+      } else {
+        const int i = at / (kSimtK / 4), k = at % (kSimtK / 4) * 4;
+        to[k][i] = v[s].x, to[k + 1][i] = v[s].y, to[k + 2][i] = v[s].z, to[k + 3][i] = v[s].w;
+      }
+    }
+  }
+};
+
+__device__ __forceinline__ uint64_t pair_of(float lo, float hi) {
+  uint64_t d;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(lo), "f"(hi));
+  return d;
+}
+__device__ __forceinline__ void fma_pair(uint64_t& acc, uint64_t a, uint64_t b) {
+  asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(acc) : "l"(a), "l"(b));
+}
+
+__device__ __forceinline__ void store4(float* p, int64_t count, bool vec, const float (&v)[4]) {
+  if (vec && count >= 4) {
+    *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (i < count) p[i] = v[i];
+}
+
+// Four sums (i, j .. j + 3) to what the call returns. The 8 lanes that share a group of 32 columns call it together.
+__device__ __forceinline__ void finish4(const Args& a, int64_t i, int64_t j, float (&v)[4]) {
+  const Product& p = a.p;
+  const int64_t count = i < p.I ? p.J - j : 0;
+  float* out = (float*)p.out + i * p.ldo + j;
+  if (p.mode == kForward) {
+    if (p.bias) {
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+        if (t < count) v[t] += ((const float*)p.bias)[j + t];
+    }
+    if (p.q) {
+      float big = 0.0f;
+#pragma unroll
+      for (int t = 0; t < 4; ++t) big = t < count ? larger(big, v[t]) : big;
+      uint32_t top = __float_as_uint(big);
+#pragma unroll
+      for (int d = 1; d < 8; d *= 2) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+      const uint32_t ex = pack_exponent(top);
+      uint32_t w;
+      pack_words<1>(v, ex, &w);
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+        if (t < count) p.q[i * p.ldq + j + t] = (int8_t)(w >> (8 * t));
+      if (count > 0 && j % kGroup == 0) p.e[i * p.lde + j / kGroup] = (uint8_t)ex;
+    }
+    if (count <= 0) return;
+    SMAT_WITH_ACT(p.act, _Pragma("unroll") for (int t = 0; t < 4; ++t) v[t] = act_value<ACT>(v[t]))
+    if (p.residual) {
+      const float4 r = load4((const float*)p.residual + i * p.ldr + j, count, a.vr);
+      v[0] += r.x, v[1] += r.y, v[2] += r.z, v[3] += r.w;
+    }
+  } else {
+    if (count <= 0) return;
+    if (p.mode == kGradInput && p.act != SMAT_ACT_NONE) {
+      const float scale = unpack_scale(p.e[i * p.lde + j / kGroup]);
+      SMAT_WITH_ACT(p.act, _Pragma("unroll") for (int t = 0; t < 4; ++t) if (t < count) v[t] *=
+                    act_slope<ACT>((float)p.q[i * p.ldq + j + t] * scale))
+    }
+    if (p.accumulate) {
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+        if (t < count) v[t] += out[t];
+    }
+  }
+  store4(out, count, a.vo, v);
+}
+
+// ------------------------------------------------------------- fp32 units ---
+
+template <int BM>
+constexpr int kSlicesBytes = 2 * kSimtK * (BM + kPad + kBN + kPad) * 4;
+template <int BM>
+constexpr int kSimtBytes = kSlicesBytes<BM> > BM * kBN * 4 ? kSlicesBytes<BM> : BM * kBN * 4;
+
+// The sums of BM x 128 from (i0, j0) over l0 .. l1, left in `shared` as [BM][128]; threads 0 to 255.
+template <int BM, bool A_MN, bool B_MN>
+__device__ __forceinline__ void simt_sums(const Args& a, float* shared, int64_t i0, int64_t j0, int64_t l0, int64_t l1) {
+  constexpr int TM = BM / 16;  // consecutive rows per thread
+  static_assert(TM == 8 || TM == 2, "");
+  float (*sa)[kSimtK][BM + kPad] = reinterpret_cast<float (*)[kSimtK][BM + kPad]>(shared);
+  float (*sb)[kSimtK][kBN + kPad] = reinterpret_cast<float (*)[kSimtK][kBN + kPad]>(shared + 2 * kSimtK * (BM + kPad));
+  float (*sums)[kBN] = reinterpret_cast<float (*)[kBN]>(shared);  // afterwards
+
+  const Product& p = a.p;
+  const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
+  uint64_t acc[TM][4];
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[i][j] = 0;
+
+  Slice<BM, A_MN> na;
+  Slice<kBN, B_MN> nb;
+  const float *pa = (const float*)p.a, *pb = (const float*)p.b;
+  if (l0 < l1) {
+    na.load(pa, p.lda, i0, p.I, l0, l1, a.va);
+    nb.load(pb, p.ldb, j0, p.J, l0, l1, a.vb);
+    na.store(sa[0]);
+    nb.store(sb[0]);
+  }
+  units_sync();
+  int at = 0;
+  for (int64_t l = l0; l < l1; l += kSimtK, at ^= 1) {
+    const bool more = l + kSimtK < l1;
+    if (more) {
+      na.load(pa, p.lda, i0, p.I, l + kSimtK, l1, a.va);
+      nb.load(pb, p.ldb, j0, p.J, l + kSimtK, l1, a.vb);
+    }
+#pragma unroll
+    for (int k = 0; k < kSimtK; ++k) {
+      const ulonglong2 b01 = *reinterpret_cast<const ulonglong2*>(&sb[at][k][tx * 4]);
+      const ulonglong2 b23 = *reinterpret_cast<const ulonglong2*>(&sb[at][k][64 + tx * 4]);
+      float x[TM];
+      if constexpr (TM == 8) {
+        *reinterpret_cast<float4*>(x) = *reinterpret_cast<const float4*>(&sa[at][k][ty * TM]);
+        *reinterpret_cast<float4*>(x + 4) = *reinterpret_cast<const float4*>(&sa[at][k][ty * TM + 4]);
+      } else {
+        *reinterpret_cast<float2*>(x) = *reinterpret_cast<const float2*>(&sa[at][k][ty * TM]);
+      }
+#pragma unroll
+      for (int i = 0; i < TM; ++i) {
+        const uint64_t xx = pair_of(x[i], x[i]);
+        fma_pair(acc[i][0], xx, b01.x);
+        fma_pair(acc[i][1], xx, b01.y);
+        fma_pair(acc[i][2], xx, b23.x);
+        fma_pair(acc[i][3], xx, b23.y);
+      }
+    }
+    if (more) {
+      na.store(sa[at ^ 1]);
+      nb.store(sb[at ^ 1]);
+    }
+    units_sync();
+  }
+#pragma unroll
+  for (int i = 0; i < TM; ++i) {
+    *reinterpret_cast<ulonglong2*>(&sums[ty * TM + i][tx * 4]) = make_ulonglong2(acc[i][0], acc[i][1]);
+    *reinterpret_cast<ulonglong2*>(&sums[ty * TM + i][64 + tx * 4]) = make_ulonglong2(acc[i][2], acc[i][3]);
+  }
+}
+
+template <int BM, bool A_MN, bool B_MN>
+__global__ void __launch_bounds__(kUnits, BM == 128 ? 2 : 3) simt_kernel(const Args a) {
+  extern __shared__ __align__(16) float shared[];
+  const Product& p = a.p;
+  const int64_t i0 = (int64_t)blockIdx.x * BM, j0 = (int64_t)blockIdx.y * kBN;
+  const int64_t l0 = (int64_t)blockIdx.z * a.share, l1 = l0 + a.share < p.L ? l0 + a.share : p.L;
+  simt_sums<BM, A_MN, B_MN>(a, shared, i0, j0, l0, l1);
+  const int shares = gridDim.z;
+  if (shares > 1)
+    cluster_sync();
+  else
+    __syncthreads();
+  // the rows go around among the CTAs of the cluster and their warps; a warp finishes a row of 128
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  for (int row = (int)blockIdx.z * 8 + warp; row < BM && i0 + row < p.I; row += 8 * shares) {
+    const float* at = shared + row * kBN + lane * 4;
+    float v[4] = {};
+    if (shares == 1) {
+      const float4 t = *reinterpret_cast<const float4*>(at);
+      v[0] = t.x, v[1] = t.y, v[2] = t.z, v[3] = t.w;
+    } else {
+      for (int s = 0; s < shares; ++s) {
+        const float4 t = cluster_load4(cluster_address(at, (uint32_t)s));
+        v[0] += t.x, v[1] += t.y, v[2] += t.z, v[3] += t.w;
+      }
+    }
+    finish4(a, i0 + row, j0 + lane * 4, v);
+  }
+  if (shares > 1) cluster_sync();  // nobody leaves while its sums are read
+}
+
+// ------------------------------------------------------------ tensor cores ---
+
+constexpr int kParts = 3;
+constexpr int kPart = kBM * kBK * 2;                // a slice of one part of one operand
+constexpr int kStage = 2 * kParts * kPart, kStages = 2;
+constexpr int kTcBytes = kStages * kStage + 1024;
+static_assert(kSimtBytes<128> <= kStages * kStage, "a tile on the fp32 units takes the ring's place");
+
+// One operand to cut: fp32 [rows, cols] to parts [3][rows][ldp] of bf16.
+struct Cut {
+  const float* from;
+  uint16_t* to;
+  int64_t rows, cols, ld, ldp;
+  bool vec;  // rows on 16 bytes
+};
+
+// hi and mid are cut off (so that no value rounds up to infinity), lo is what is left: 8 bits at most, exact.
+__device__ __forceinline__ void cut(float x, uint32_t& hi, uint32_t& mid, uint32_t& lo, uint32_t& odd) {
+  hi = __float_as_uint(x) & 0xFFFF0000u;
+  const float r = x - __uint_as_float(hi);
+  mid = __float_as_uint(r) & 0xFFFF0000u;
+  lo = __float_as_uint(r - __uint_as_float(mid));
+  odd |= (__float_as_uint(x) & 0x7F800000u) == 0x7F800000u;
+}
+
+// Both operands of a product; flags[CTA]: whether it met an infinity or NaN. A thread cuts 8 neighbours of a row: 32
+// bytes in, 3 x 16 out.
+__global__ void __launch_bounds__(256) cut_kernel(const Cut a, const Cut b, int ctas_a, uint32_t* flags) {
+  const bool first = (int)blockIdx.x < ctas_a;
+  const Cut& c = first ? a : b;
+  const int64_t ctas = first ? ctas_a : gridDim.x - ctas_a, cta = first ? blockIdx.x : blockIdx.x - ctas_a;
+  const int64_t units = c.ldp / 8, plane = c.rows * c.ldp;
+  uint32_t odd = 0;
+  // a CTA's rows one after another, its threads side by side along a row (a short row's threads share out rows)
+  const int wide = (int)(units < 256 ? units : 256), high = 256 / wide;
+  const int tx = threadIdx.x % wide, ty = threadIdx.x / wide;
+  if (ty < high)
+    for (int64_t r = cta * high + ty; r < c.rows; r += ctas * high)
+      for (int64_t u = tx; u < units; u += wide) {
+        const int64_t at = 8 * u;
+        const float* p = c.from + r * c.ld + at;
+        const float4 x = load4(p, c.cols - at, c.vec), y = load4(p + 4, c.cols - at - 4, c.vec);
+        const float v[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+        uint32_t w[3][4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          uint32_t h0, m0, l0, h1, m1, l1;
+          cut(v[2 * t], h0, m0, l0, odd);
+          cut(v[2 * t + 1], h1, m1, l1, odd);
+          w[0][t] = __byte_perm(h0, h1, 0x7632);
+          w[1][t] = __byte_perm(m0, m1, 0x7632);
+          w[2][t] = __byte_perm(l0, l1, 0x7632);
+        }
+#pragma unroll
+        for (int t = 0; t < 3; ++t)
+          *reinterpret_cast<uint4*>(c.to + t * plane + r * c.ldp + at) = make_uint4(w[t][0], w[t][1], w[t][2], w[t][3]);
+      }
+  const int any = __syncthreads_or((int)odd);
+  if (threadIdx.x == 0) flags[blockIdx.x] = any;
+}
+
+// A warp's 32 x 32 sums from (i, j) on, a row per thread: through shared memory, so that 8 lanes finish 4 columns each of
+// a row. A row's eight quadruples lie in an order of its own, so that neither side's accesses meet in a bank.
+__device__ __forceinline__ void finish_block(const Args& a, int64_t i, int64_t j, const float (&v)[32], float* turn) {
+  if (i >= a.p.I || j >= a.p.J) return;
+  const int lane = threadIdx.x % 32;
+  __syncwarp();
+#pragma unroll
+  for (int t = 0; t < 32; t += 4)
+    *reinterpret_cast<float4*>(turn + lane * 32 + (t ^ (lane % 8 * 4))) = make_float4(v[t], v[t + 1], v[t + 2], v[t + 3]);
+  __syncwarp();
+#pragma unroll 2
+  for (int t = 0; t < 32; t += 4) {
+    const int row = t + lane / 8, col = lane % 8 * 4;
+    const float4 f = *reinterpret_cast<const float4*>(turn + row * 32 + (col ^ (row % 8 * 4)));
+    float x[4] = {f.x, f.y, f.z, f.w};
+    finish4(a, i + row, j + col, x);
+  }
+}
+
+struct TcArgs {
+  Args f;
+  int64_t tiles, tiles_r, tiles_c;
+  int slices, share;  // slices of 64, and those of a CTA of a cluster
+  float* parts;       // shares of sums
+  const uint32_t* flags;
+  int n_flags;
+  int* errors;
+};
+
+// The six products of a slice, small ones first: (part of A, part of B)
+__device__ constexpr int kOrder[6][2] = {{2, 0}, {0, 2}, {1, 1}, {1, 0}, {0, 1}, {0, 0}};
+
+template <bool A_MN, bool B_MN>
+__global__ void __launch_bounds__(kThreads, 1)
+    f32_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+               const __grid_constant__ TcArgs a) {
+  extern __shared__ uint8_t raw[];
+  __shared__ __align__(16) float turns[kEpiWarps][32 * 32];
+  __shared__ __align__(8) uint64_t bars[2 * kStages + 5];
+  __shared__ uint32_t tmem_at;
+  __shared__ int dead_flag;
+  uint8_t* ring = raw + ((1024 - (smem_address(raw) & 1023)) & 1023);
+  volatile int* dead = &dead_flag;
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const uint32_t full = smem_address(bars), empty = full + 8 * kStages, sums_full = empty + 8 * kStages,
+                 sums_empty = sums_full + 16, drained = sums_empty + 16;
+  const Product& p = a.f.p;
+
+  uint32_t shares, rank;
+  asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(shares));
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+  const int slice0 = (int)rank * a.share;
+  const int slices = max(0, min(a.share, a.slices - slice0));
+  const int64_t first_tile = blockIdx.x / shares, step = gridDim.x / shares;
+
+  if (warp == kTmaWarp && lane == 0) {
+    dead_flag = 0;
+    for (int s = 0; s < kStages; ++s) {
+      bar_init(full + 8 * s, 1);
+      bar_init(empty + 8 * s, 1);
+    }
+    bar_init(drained, 1);
+    for (int b = 0; b < 2; ++b) {
+      bar_init(sums_full + 8 * b, 1);
+      bar_init(sums_empty + 8 * b, kEpiWarps);
+    }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncwarp();
+  if (warp == kMmaWarp) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_address(&tmem_at)),
+                 "r"(2 * kBN)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    fence_before();
+  }
+  uint32_t odd = 0;
+  for (int i = threadIdx.x; i < a.n_flags; i += kThreads) odd |= a.flags[i];
+  odd = __syncthreads_or((int)odd);
+  fence_after();
+  const uint32_t tmem = tmem_at;
+
+  if (odd) {
+    // an infinity or NaN in an operand: the cluster's first CTA makes the tile on the fp32 units
+    if (warp < kEpiWarps && rank == 0) {
+      float* sums = reinterpret_cast<float*>(ring);
+      for (int64_t tile = first_tile; tile < a.tiles; tile += step) {
+        int64_t tr, tc;
+        tile_place(a.tiles_r, a.tiles_c, tile, tr, tc);
+        simt_sums<128, A_MN, B_MN>(a.f, sums, tr * kBM, tc * kBN, 0, p.L);
+        units_sync();
+        for (int row = warp; row < kBM && tr * kBM + row < p.I; row += 8) {
+          const float4 t = *reinterpret_cast<const float4*>(sums + row * kBN + lane * 4);
+          float v[4] = {t.x, t.y, t.z, t.w};
+          finish4(a.f, tr * kBM + row, tc * kBN + lane * 4, v);
+        }
+        units_sync();
+      }
+    }
+  } else if (warp == kTmaWarp && lane == 0) {
+    uint32_t n = 0;
+    bool ok = true;
+    for (int64_t tile = first_tile; ok && tile < a.tiles; tile += step) {
+      int64_t tr, tc;
+      tile_place(a.tiles_r, a.tiles_c, tile, tr, tc);
+      const int r0 = (int)(tr * kBM), c0 = (int)(tc * kBN);
+      for (int k = 0; k < slices; ++k, ++n) {
+        const uint32_t s = n % kStages;
+        ok = bar_wait(empty + 8 * s, (n / kStages + 1) & 1, dead, a.errors);
+        if (!ok) break;
+        const int l = (slice0 + k) * kBK;
+        const uint32_t bar = full + 8 * s, to = smem_address(ring) + s * kStage;
+        bar_expect(bar, kStage);
+#pragma unroll
+        for (int q = 0; q < kParts; ++q) {
+          const uint32_t to_a = to + q * kPart, to_b = to + (kParts + q) * kPart;
+          if (A_MN) {
+            tma_load3(to_a, &map_a, r0, l, q, bar);
+            tma_load3(to_a + 8192, &map_a, r0 + 64, l, q, bar);
+          } else {
+            tma_load3(to_a, &map_a, l, r0, q, bar);
+          }
+          if (B_MN) {
+            tma_load3(to_b, &map_b, c0, l, q, bar);
+            tma_load3(to_b + 8192, &map_b, c0 + 64, l, q, bar);
+          } else {
+            tma_load3(to_b, &map_b, l, c0, q, bar);
+          }
+        }
+      }
+    }
+    if (!ok)  // copies in flight land before the CTA ends
+      for (uint32_t s = 0; s < kStages && s < n; ++s) {
+        const uint32_t last = n - 1 - s;
+        for (int i = 0; i < (1 << 20) && !bar_try(full + 8 * (last % kStages), last / kStages & 1); ++i) {
+        }
+      }
+  } else if (warp == kMmaWarp && lane == 0) {
+    constexpr uint32_t kInst = kInstruction<A_MN, B_MN, kBN>;
+    uint32_t n = 0;
+    bool ok = true;
+    for (int64_t tile = first_tile; ok && tile < a.tiles; tile += step)
+      for (int k = 0; k < slices; ++k, ++n) {
+        const uint32_t s = n % kStages, half = n & 1, sums = tmem + half * kBN;
+        ok = bar_wait(sums_empty + 8 * half, (n / 2 + 1) & 1, dead, a.errors) &&
+             bar_wait(full + 8 * s, n / kStages & 1, dead, a.errors);
+        if (!ok) break;
+        fence_after();
+        const uint32_t at = smem_address(ring) + s * kStage;
+#pragma unroll
+        for (int o = 0; o < 6; ++o) {
+          const uint64_t da = descriptor<A_MN>(at + kOrder[o][0] * kPart);
+          const uint64_t db = descriptor<B_MN>(at + (kParts + kOrder[o][1]) * kPart);
+#pragma unroll
+          for (int t = 0; t < kBK / 16; ++t)
+            mma(sums, da + t * kStep16<A_MN>, db + t * kStep16<B_MN>, kInst, o > 0 || t > 0);
+        }
+        mma_commit(empty + 8 * s);
+        mma_commit(sums_full + 8 * half);
+      }
+    if (!ok) {  // products in flight end before the CTA does
+      mma_commit(drained);
+      for (int i = 0; i < (1 << 20) && !bar_try(drained, 0); ++i) {
+      }
+    }
+  } else if (warp < kEpiWarps) {
+    // this warp's sums: 32 rows, 64 columns of the tile
+    const int quarter = warp % 4, first = warp / 4 * 64;
+    float* turn = turns[warp];
+    uint32_t n = 0;
+    bool ok = true;
+    for (int64_t tile = first_tile; ok && tile < a.tiles; tile += step) {
+      int64_t tr, tc;
+      tile_place(a.tiles_r, a.tiles_c, tile, tr, tc);
+      float acc[2][32];
+#pragma unroll
+      for (int t = 0; t < 32; ++t) acc[0][t] = acc[1][t] = 0.0f;
+      for (int k = 0; k < slices; ++k, ++n) {
+        const uint32_t half = n & 1;
+        ok = bar_wait(sums_full + 8 * half, n / 2 & 1, dead, a.errors);
+        if (!ok) break;
+        fence_after();
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          float v[32];
+          take32(tmem + half * kBN + first + 32 * b + ((uint32_t)(32 * quarter) << 16), v);
+#pragma unroll
+          for (int t = 0; t < 32; ++t) acc[b][t] += v[t];
+        }
+        fence_before();
+        __syncwarp();
+        if (lane == 0) bar_arrive(sums_empty + 8 * half);
+      }
+      const int64_t r0 = tr * kBM + 32 * quarter;
+      if (shares > 1) {
+        float* part = a.parts + ((size_t)first_tile * shares + rank) * kBN * kBM + 32 * quarter + lane;
+#pragma unroll
+        for (int b = 0; b < 2; ++b) put_part(part + (first + 32 * b) * kBM, acc[b]);
+      } else if (ok) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b) finish_block(a.f, r0, tc * kBN + first + 32 * b, acc[b], turn);
+      }
+    }
+  }
+  __syncwarp();
+  if (shares > 1) {
+    __syncthreads();
+    cluster_sync();
+    if (!odd && warp < kEpiWarps && !*dead) {
+      int64_t tr, tc;
+      tile_place(a.tiles_r, a.tiles_c, first_tile, tr, tc);
+      const int quarter = warp % 4;
+      const float* part = a.parts + (size_t)first_tile * shares * kBN * kBM + 32 * quarter + lane;
+      for (int c = (int)rank + (int)shares * (warp / 4); c < kBN / 32; c += 2 * (int)shares) {
+        float v[32];
+        add_parts(shares, v, [&](uint32_t s, int t) { return __ldcg(part + ((size_t)s * kBN + 32 * c + t) * kBM); });
+        finish_block(a.f, tr * kBM + 32 * quarter, tc * kBN + 32 * c, v, turns[warp]);
+      }
+    }
+    cluster_sync();
+  }
+  fence_before();
+  __syncthreads();
+  if (warp == kMmaWarp)
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2 * kBN));
+}
+
+// ------------------------------------------------------------- host side ---
+
+bool can(const void* p, int64_t ld) { return (uintptr_t)p % 16 == 0 && ld % 4 == 0; }
+
+Args args_of(const Product& p) {
+  Args a = {};
+  a.p = p;
+  a.va = can(p.a, p.lda);
+  a.vb = can(p.b, p.ldb);
+  a.vr = can(p.residual, p.ldr);
+  a.vo = can(p.out, p.ldo);
+  return a;
+}
+
+cudaLaunchConfig_t config(dim3 grid, int threads, int bytes, dim3 cluster, cudaLaunchAttribute* at, cudaStream_t s) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = bytes;
+  cfg.stream = s;
+  at->id = cudaLaunchAttributeClusterDimension;
+  at->val.clusterDim = {cluster.x, cluster.y, cluster.z};
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  return cfg;
+}
+
+template <int BM, bool A_MN, bool B_MN>
+cudaError_t launch_simt_tile(Args a, int sms, cudaStream_t s) {
+  static std::atomic<uint64_t> allowed;
+  auto* f = simt_kernel<BM, A_MN, B_MN>;
+  const cudaError_t e = allow_shared(f, kSimtBytes<BM>, allowed);
+  if (e != cudaSuccess) return e;
+  const int64_t ti = (a.p.I + BM - 1) / BM, tj = (a.p.J + kBN - 1) / kBN;
+  int shares = 1;
+  // two CTAs fit on an SM; a share is at least 64 long
+  while (shares < 8 && ti * tj * shares * 2 <= 2 * sms && a.p.L >= (int64_t)shares * 2 * 64) shares *= 2;
+  a.share = (a.p.L + shares * kSimtK - 1) / (shares * kSimtK) * kSimtK;
+  cudaLaunchAttribute at;
+  const cudaLaunchConfig_t cfg = config(dim3((unsigned)ti, (unsigned)tj, (unsigned)shares), kUnits, kSimtBytes<BM>,
+                                        dim3(1, 1, (unsigned)shares), &at, s);
+  return cudaLaunchKernelEx(&cfg, f, a);
+}
+
+template <bool A_MN, bool B_MN>
+cudaError_t launch_simt(const Product& p, int sms, cudaStream_t s) {
+  const Args a = args_of(p);
+  return p.I <= 32 ? launch_simt_tile<32, A_MN, B_MN>(a, sms, s) : launch_simt_tile<128, A_MN, B_MN>(a, sms, s);
+}
+
+// What a product on the tensor cores needs: an operand's parts, flags, shares of sums.
+struct Plan {
+  int64_t tiles_r, tiles_c, ctas;
+  int slices, share, shares, cuts_a, cuts_b;
+  int64_t rows_a, cols_a, ldp_a, rows_b, cols_b, ldp_b;
+  size_t bytes_a, bytes_b, bytes_flags, bytes_parts;
+  size_t bytes() const { return bytes_a + bytes_b + bytes_flags + bytes_parts; }
+};
+
+constexpr size_t up(size_t x) { return (x + 255) / 256 * 256; }
+
+// CTAs that cut an operand: two rounds of eight CTAs per SM at most
+int cuts_of(int64_t rows, int64_t ldp, int sms) {
+  const int64_t units = rows * (ldp / 8), ctas = (units + 511) / 512;
+  return (int)(ctas < 8 * sms ? (ctas < 1 ? 1 : ctas) : 8 * sms);
+}
+
+template <bool A_MN, bool B_MN>
+cudaError_t plan_tc(const Product& p, int sms, Plan* plan) {
+  static std::atomic<uint64_t> allowed;
+  static std::atomic<int> clusters[64][9];
+  auto* f = f32_kernel<A_MN, B_MN>;
+  const cudaError_t e = allow_shared(f, kTcBytes, allowed);
+  if (e != cudaSuccess) return e;
+  Plan g = {};
+  g.tiles_r = (p.I + kBM - 1) / kBM;
+  g.tiles_c = (p.J + kBN - 1) / kBN;
+  g.slices = (int)((p.L + kBK - 1) / kBK);
+  const int64_t tiles = g.tiles_r * g.tiles_c;
+  int shares = 8;
+  while (shares > 1 && (tiles * shares > sms || g.slices < 3 * shares ||
+                        tiles > clusters_at_once(f, shares, kTcBytes, clusters)))
+    --shares;
+  g.share = (g.slices + shares - 1) / shares;
+  g.shares = shares > 1 ? (g.slices + g.share - 1) / g.share : 1;
+  g.ctas = g.shares > 1 ? tiles * g.shares : (tiles < sms ? tiles : sms);
+  g.rows_a = A_MN ? p.L : p.I, g.cols_a = A_MN ? p.I : p.L;
+  g.rows_b = B_MN ? p.L : p.J, g.cols_b = B_MN ? p.J : p.L;
+  g.ldp_a = (g.cols_a + 31) / 32 * 32, g.ldp_b = (g.cols_b + 31) / 32 * 32;
+  g.cuts_a = cuts_of(g.rows_a, g.ldp_a, sms), g.cuts_b = cuts_of(g.rows_b, g.ldp_b, sms);
+  g.bytes_a = up((size_t)kParts * g.rows_a * g.ldp_a * 2);
+  g.bytes_b = up((size_t)kParts * g.rows_b * g.ldp_b * 2);
+  g.bytes_flags = up(sizeof(uint32_t) * (g.cuts_a + g.cuts_b));
+  g.bytes_parts = g.shares > 1 ? (size_t)tiles * g.shares * kBN * kBM * sizeof(float) : 0;
+  *plan = g;
+  return cudaSuccess;
+}
+
+// Parts [3][rows][ldp] of `cols` columns in boxes of 64 x `box` of one part; what lies outside reads as 0.
+bool encode_parts(CUtensorMap* map, const void* p, int64_t cols, int64_t rows, int64_t ldp, int box) {
+  const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)kParts};
+  const cuuint64_t strides[2] = {(cuuint64_t)ldp * 2, (cuuint64_t)rows * ldp * 2};
+  const cuuint32_t boxes[3] = {64, (cuuint32_t)box, 1}, ones[3] = {1, 1, 1};
+  const Encode f = encoder();
+  return f && f(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(p), dims, strides, boxes, ones,
+                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <bool A_MN, bool B_MN>
+cudaError_t launch_tc32(const Product& p, int sms, char* workspace, cudaStream_t s) {
+  Plan g;
+  cudaError_t e = plan_tc<A_MN, B_MN>(p, sms, &g);
+  if (e != cudaSuccess) return e;
+  TcArgs a = {};
+  e = error_word(&a.errors);
+  if (e != cudaSuccess) return e;
+  a.f = args_of(p);
+  char *pa = workspace, *pb = pa + g.bytes_a, *pf = pb + g.bytes_b;
+  const Cut ca = {(const float*)p.a, (uint16_t*)pa, g.rows_a, g.cols_a, p.lda, g.ldp_a, a.f.va};
+  const Cut cb = {(const float*)p.b, (uint16_t*)pb, g.rows_b, g.cols_b, p.ldb, g.ldp_b, a.f.vb};
+  a.flags = (const uint32_t*)pf;
+  a.n_flags = g.cuts_a + g.cuts_b;
+  a.parts = (float*)(pf + g.bytes_flags);
+  a.tiles_r = g.tiles_r, a.tiles_c = g.tiles_c, a.tiles = g.tiles_r * g.tiles_c;
+  a.slices = g.slices, a.share = g.share;
+  CUtensorMap ma, mb;
+  if (!encode_parts(&ma, pa, g.cols_a, g.rows_a, g.ldp_a, A_MN ? kBK : kBM) ||
+      !encode_parts(&mb, pb, g.cols_b, g.rows_b, g.ldp_b, B_MN ? kBK : kBN))
+    return cudaErrorNotSupported;
+  cut_kernel<<<g.cuts_a + g.cuts_b, 256, 0, s>>>(ca, cb, g.cuts_a, (uint32_t*)pf);
+  e = cudaGetLastError();
+  if (e != cudaSuccess) return e;
+  cudaLaunchAttribute at;
+  const cudaLaunchConfig_t cfg =
+      config(dim3((unsigned)g.ctas), kThreads, kTcBytes, dim3((unsigned)g.shares, 1, 1), &at, s);
+  return cudaLaunchKernelEx(&cfg, f32_kernel<A_MN, B_MN>, ma, mb, a);
+}
+
+// Whether cutting the operands pays.
+bool on_tensor_cores(const Product& p) {
+  return p.L > 0 && p.I > 32 && (double)p.I * (double)p.J * (double)p.L >= 1 << 25;
+}
+
+}  // namespace
+
+cudaError_t f32_workspace(const Product& p, int sms, size_t* bytes) {
+  *bytes = 0;
+  if (!on_tensor_cores(p)) return cudaSuccess;
+  Plan g;
+  const cudaError_t e = p.mode == kForward     ? plan_tc<false, false>(p, sms, &g)
+                        : p.mode == kGradInput ? plan_tc<false, true>(p, sms, &g)
+                                               : plan_tc<true, true>(p, sms, &g);
+  if (e == cudaSuccess) *bytes = g.bytes();
+  return e;
+}
+
+cudaError_t launch_f32(const Product& p, int sms, void* workspace, cudaStream_t s) {
+  const bool tc = on_tensor_cores(p);
+  char* w = (char*)workspace;
+  switch (p.mode) {
+    case kForward: return tc ? launch_tc32<false, false>(p, sms, w, s) : launch_simt<false, false>(p, sms, s);
+    case kGradInput: return tc ? launch_tc32<false, true>(p, sms, w, s) : launch_simt<false, true>(p, sms, s);
+    default: return tc ? launch_tc32<true, true>(p, sms, w, s) : launch_simt<true, true>(p, sms, s);
+  }
+}
+
+}  // namespace lin
+}  // namespace smat

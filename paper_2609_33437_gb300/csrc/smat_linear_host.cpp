@@ -148,17 +148,18 @@ size_t operand_bytes(const Operand& o) { return o.copied ? copy_bytes(o.rows, o.
 struct Operands {
   Operand a, b;
   size_t values;  // bytes of grad_weight's x^
-  size_t parts;   // bytes of a tensor-core product's own
+  size_t parts;   // bytes of the product's own
   size_t bytes() const { return values + operand_bytes(a) + operand_bytes(b) + parts; }
 };
 
 size_t parts_of(int mode, int32_t dtype, int64_t I, int64_t J, int64_t L) {
   int sms = 0;
   size_t bytes = 0;
-  if (dtype != SMAT_BF16 || device_sms(&sms) != SMAT_OK) return 0;
+  if (device_sms(&sms) != SMAT_OK) return 0;
   Product p = {};
   p.mode = mode, p.I = I, p.J = J, p.L = L;
-  return tc_workspace(p, sms, &bytes) == cudaSuccess ? up(bytes) : 0;
+  const cudaError_t e = dtype == SMAT_BF16 ? tc_workspace(p, sms, &bytes) : f32_workspace(p, sms, &bytes);
+  return e == cudaSuccess ? up(bytes) : 0;
 }
 
 Operands operands(const smat_linear_args* g) {
@@ -199,7 +200,9 @@ smat_status run_product(Product& p, const Operands& o, char* d_workspace, int sm
     if (st != SMAT_OK) return st;
     d_workspace += operand_bytes(*in[i]);
   }
-  return cuda_status(p.dtype == SMAT_BF16 ? launch_tc(p, sms, d_workspace, s) : launch_simt(p, sms, s), what);
+  return cuda_status(p.dtype == SMAT_BF16 ? launch_tc(p, sms, d_workspace, s)
+                                            : launch_f32(p, sms, d_workspace, s),
+                     what);
 }
 
 // A call's size check without its message: what the size queries return 0 for.

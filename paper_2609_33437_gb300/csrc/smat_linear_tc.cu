@@ -15,10 +15,8 @@
 // sums in its shared memory, then every CTA adds up some of the columns in the cluster's order and finishes them. No
 // workspace, no atomics, the same result every time.
 
-#include <cuda.h>
-
-#include "smat_linear.cuh"
 #include "smat_linear.h"
+#include "smat_linear_tc.cuh"
 
 namespace smat {
 namespace lin {
@@ -27,13 +25,8 @@ __device__ int g_errors;  // bit 0: a wait inside a product ran out of time
 
 namespace {
 
-constexpr int kBM = 128, kBK = 64;
-constexpr int kEpiWarps = 8;
-constexpr int kThreads = 32 * (kEpiWarps + 2);
-constexpr int kTmaWarp = kEpiWarps, kMmaWarp = kEpiWarps + 1;
 constexpr int kBytesA = kBM * kBK * 2;
 constexpr int kTurn = 32 * 33 * 4;  // a warp's 32 x 32 sums, turned
-constexpr unsigned long long kWaitNs = 2000000000ull;
 
 // Swapped tiles are narrow and bound by the weight's bytes: two CTAs per SM, so that one's start and end lie beside
 // the other's copies.
@@ -52,117 +45,11 @@ struct Args {
   int slices;                       // of 64 along the sum
   int share;                        // slices per CTA of a cluster
   float* parts;                     // the shares' sums, or NULL
+  int* errors;                      // device error bits
   bool by_rows;                     // rows of out and residual start on 16 bytes, those of q on 8
   bool full_sectors;                // rows of out, residual and q start on 32 bytes
   bool wide_bias;                   // bias on 16 bytes
 };
-
-__device__ __forceinline__ uint32_t smem_address(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-
-__device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count) {
-  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
-}
-__device__ __forceinline__ void bar_arrive(uint32_t bar) {
-  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
-  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
-      : "=r"(ok)
-      : "r"(bar), "r"(parity)
-      : "memory");
-  return ok != 0;
-}
-
-// Waits until the barrier's phase `parity` is over; false after kWaitNs, or once another wait of this CTA has given
-// up: the caller then leaves its loop, the CTA gives back its tensor memory and ends, and g_errors tells the host.
-__device__ __noinline__ bool bar_wait_long(uint32_t bar, uint32_t parity, volatile int* dead) {
-  unsigned long long begin, now;
-  asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(begin));
-  for (;;) {
-    for (int i = 0; i < 256; ++i)
-      if (bar_try(bar, parity)) return true;
-    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(now));
-    if (*dead) return false;
-    if (now - begin > kWaitNs) {
-      *dead = 1;
-      atomicOr(&g_errors, 1);
-      return false;
-    }
-  }
-}
-__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int* dead) {
-  return bar_try(bar, parity) || bar_wait_long(bar, parity, dead);
-}
-
-__device__ __forceinline__ void tma_load(uint32_t to, const CUtensorMap* map, int x, int y, uint32_t bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(to),
-      "l"(map), "r"(bar), "r"(x), "r"(y)
-      : "memory");
-}
-
-// Shared-memory matrix descriptor (128-byte swizzle). K-major: rows of 128 bytes (64 along the sum), 8 rows per
-// 1024-byte block, blocks of rows 1024 bytes apart; 16 along the sum are 32 bytes. MN-major: 128 bytes hold 64 rows
-// of the tile at one place of the sum, 8 places per 1024-byte block; 8 places further on is 1024 bytes, 64 rows
-// further on 64 * 128 bytes; 16 along the sum are 2048 bytes.
-template <bool MN>
-__device__ __forceinline__ uint64_t descriptor(uint32_t address) {
-  const uint64_t lbo = MN ? (kBK * 128) >> 4 : 1;
-  return (uint64_t)((address & 0x3FFFF) >> 4) | lbo << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 |
-         (uint64_t)2 << 61;
-}
-template <bool MN>
-constexpr uint64_t kStep16 = (MN ? 2048 : 32) >> 4;
-
-// kind::f16: fp32 sums of bf16 products, 128 x n
-template <bool A_MN, bool B_MN, int N>
-constexpr uint32_t kInstruction = 1u << 4 | 1u << 7 | 1u << 10 | (uint32_t)A_MN << 15 | (uint32_t)B_MN << 16 |
-                                  (uint32_t)(N >> 3) << 17 | (uint32_t)(kBM >> 4) << 24;
-
-__device__ __forceinline__ void mma(uint32_t sums, uint64_t a, uint64_t b, uint32_t instruction, bool add) {
-  asm volatile(
-      "{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(sums),
-      "l"(a), "l"(b), "r"(instruction), "r"((uint32_t)add)
-      : "memory");
-}
-__device__ __forceinline__ void mma_commit(uint32_t bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-
-// 32 columns of the warp's 32 rows of tensor memory: thread's row, columns in order. The load and its wait are one
-// statement, so that nothing can read the registers in between.
-__device__ __forceinline__ void take32(uint32_t at, float (&v)[32]) {
-  uint32_t u[32];
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,"
-      "%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\ntcgen05.wait::ld.sync.aligned;"
-      : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]), "=r"(u[8]),
-        "=r"(u[9]), "=r"(u[10]), "=r"(u[11]), "=r"(u[12]), "=r"(u[13]), "=r"(u[14]), "=r"(u[15]), "=r"(u[16]),
-        "=r"(u[17]), "=r"(u[18]), "=r"(u[19]), "=r"(u[20]), "=r"(u[21]), "=r"(u[22]), "=r"(u[23]), "=r"(u[24]),
-        "=r"(u[25]), "=r"(u[26]), "=r"(u[27]), "=r"(u[28]), "=r"(u[29]), "=r"(u[30]), "=r"(u[31])
-      : "r"(at)
-      : "memory");
-#pragma unroll
-  for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(u[i]);
-}
-
-__device__ __forceinline__ void take8(uint32_t at, float (&v)[8]) {
-  uint32_t u[8];
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];\ntcgen05.wait::ld.sync.aligned;"
-      : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7])
-      : "r"(at)
-      : "memory");
-#pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(u[i]);
-}
 
 using bf16 = __nv_bfloat16;
 
@@ -401,40 +288,7 @@ __device__ __forceinline__ void finish_rows(const Args& a, int64_t row0, int64_t
 // A CTA's share of a tile's sums lies as [column][128 rows], so that a warp's 32 rows of a column are 128 bytes in a
 // row: in the workspace (a.parts), or, where the tile has no more than 8 columns, in its own shared memory, which the
 // others read across the cluster. (Reading larger tiles there is slow: 128 x 256 sums of 8 shares took 15 us, through
-// the workspace, which stays in L2, 3.) The shares are added in the cluster's order, several CTAs' loads in flight.
-template <int N>
-__device__ __forceinline__ void put_part(float* p, const float (&v)[N]) {
-#pragma unroll
-  for (int t = 0; t < N; ++t) p[t * kBM] = v[t];
-}
-template <int N, class Load>
-__device__ __forceinline__ void add_parts(uint32_t shares, float (&v)[N], Load&& load) {
-  constexpr int kAhead = N == 32 ? 2 : 4;
-#pragma unroll
-  for (int t = 0; t < N; ++t) v[t] = 0.0f;
-  for (uint32_t s = 0; s < shares; s += kAhead) {
-    float x[kAhead][N];
-#pragma unroll
-    for (int h = 0; h < kAhead; ++h)
-#pragma unroll
-      for (int t = 0; t < N; ++t) x[h][t] = s + h < shares ? load(s + h, t) : 0.0f;
-#pragma unroll
-    for (int h = 0; h < kAhead; ++h)
-#pragma unroll
-      for (int t = 0; t < N; ++t) v[t] += x[h][t];
-  }
-}
-
-// The tiles' order: strips of 16 tiles of rows, down a strip's rows first, so that the tiles in work at one time
-// share rows and columns of the operands in L2.
-__device__ __forceinline__ void tile_place(const Args& a, int64_t tile, int64_t& r, int64_t& c) {
-  constexpr int64_t kStrip = 16;
-  const int64_t per = kStrip * a.tiles_c, strip = tile / per, in = tile - strip * per;
-  const int64_t high = a.tiles_r - strip * kStrip < kStrip ? a.tiles_r - strip * kStrip : kStrip;
-  c = in / high;
-  r = strip * kStrip + in - c * high;
-}
-
+// the workspace, which stays in L2, 3.) 
 template <int MODE, bool SWAP, int BN>
 __global__ void __launch_bounds__(kThreads, Ring<BN, SWAP>::kCtas)
     tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
@@ -463,10 +317,8 @@ __global__ void __launch_bounds__(kThreads, Ring<BN, SWAP>::kCtas)
   const int64_t first_tile = blockIdx.x / shares, step = gridDim.x / shares;
 
   auto turn_of = [&](int w) { return reinterpret_cast<float*>(ring + kStages * kStage + w * kTurn); };
-  auto fetch = [&](uint32_t s, int64_t tile, int k) {
-    int64_t tr, tc;
-    tile_place(a, tile, tr, tc);
-    const int r0 = (int)(tr * kBM), c0 = (int)(tc * BN), l = (slice0 + k) * kBK;
+  auto fetch = [&](uint32_t s, int r0, int c0, int k) {
+    const int l = (slice0 + k) * kBK;
     const uint32_t bar = full + 8 * s, to_a = smem_address(ring) + s * kStage, to_b = to_a + kBytesA;
     bar_expect(bar, kStage);
     if (A_MN) {
@@ -496,7 +348,9 @@ __global__ void __launch_bounds__(kThreads, Ring<BN, SWAP>::kCtas)
       bar_init(sums_empty + 8 * b, kEpiWarps);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    for (int k = 0; k < ahead; ++k) fetch(k, first_tile, k);
+    int64_t tr, tc;
+    tile_place(a.tiles_r, a.tiles_c, first_tile, tr, tc);
+    for (int k = 0; k < ahead; ++k) fetch(k, (int)(tr * kBM), (int)(tc * BN), k);
   }
   __syncwarp();
   if (warp == kMmaWarp) {
@@ -513,13 +367,16 @@ __global__ void __launch_bounds__(kThreads, Ring<BN, SWAP>::kCtas)
   if (warp == kTmaWarp && lane == 0) {
     uint32_t n = (uint32_t)ahead;  // slices fetched so far
     bool ok = true;
-    for (int64_t tile = first_tile; ok && tile < a.tiles; tile += step)
+    for (int64_t tile = first_tile; ok && tile < a.tiles; tile += step) {
+      int64_t tr, tc;
+      tile_place(a.tiles_r, a.tiles_c, tile, tr, tc);
       for (int k = tile == first_tile ? ahead : 0; k < slices; ++k, ++n) {
         const uint32_t s = n % kStages;
-        ok = bar_wait(empty + 8 * s, (n / kStages + 1) & 1, dead);
+        ok = bar_wait(empty + 8 * s, (n / kStages + 1) & 1, dead, a.errors);
         if (!ok) break;
-        fetch(s, tile, k);
+        fetch(s, (int)(tr * kBM), (int)(tc * BN), k);
       }
+    }
     if (!ok)  // copies in flight land before the CTA ends
       for (uint32_t s = 0; s < kStages && s < n; ++s) {
         const uint32_t last = n - 1 - s;
@@ -532,12 +389,12 @@ __global__ void __launch_bounds__(kThreads, Ring<BN, SWAP>::kCtas)
     bool ok = true;
     for (int64_t tile = first_tile; ok && tile < a.tiles; tile += step, ++made) {
       const uint32_t half = made & 1, sums = tmem + half * BN;
-      ok = bar_wait(sums_empty + 8 * half, (made / 2 + 1) & 1, dead);
+      ok = bar_wait(sums_empty + 8 * half, (made / 2 + 1) & 1, dead, a.errors);
       if (!ok) break;
       fence_after();
       for (int k = 0; k < slices; ++k, ++n) {
         const uint32_t s = n % kStages;
-        ok = bar_wait(full + 8 * s, n / kStages & 1, dead);
+        ok = bar_wait(full + 8 * s, n / kStages & 1, dead, a.errors);
         if (!ok) break;
         fence_after();
         const uint32_t at_a = smem_address(ring) + s * kStage;
@@ -562,10 +419,10 @@ __global__ void __launch_bounds__(kThreads, Ring<BN, SWAP>::kCtas)
     uint32_t made = 0;
     for (int64_t tile = first_tile; tile < a.tiles; tile += step, ++made) {
       int64_t tr, tc;
-      tile_place(a, tile, tr, tc);
+      tile_place(a.tiles_r, a.tiles_c, tile, tr, tc);
       const int64_t r0 = tr * kBM + 32 * quarter, c0 = tc * BN;
       const uint32_t half = made & 1, sums = tmem + half * BN + ((uint32_t)(32 * quarter) << 16);
-      if (!bar_wait(sums_full + 8 * half, made / 2 & 1, dead)) break;
+      if (!bar_wait(sums_full + 8 * half, made / 2 & 1, dead, a.errors)) break;
       fence_after();
       auto release = [&] {  // this warp has what it needs of these sums
         fence_before();
@@ -623,7 +480,7 @@ __global__ void __launch_bounds__(kThreads, Ring<BN, SWAP>::kCtas)
     cluster_sync();
     if (warp < kEpiWarps && !*dead) {
       int64_t tr, tc;
-      tile_place(a, first_tile, tr, tc);
+      tile_place(a.tiles_r, a.tiles_c, first_tile, tr, tc);
       const int quarter = warp % 4;
       const int64_t r0 = tr * kBM + 32 * quarter, c0 = tc * BN;
       const float* part = (a.parts ? a.parts + (size_t)first_tile * shares * BN * kBM : reinterpret_cast<float*>(ring)) +
@@ -660,22 +517,6 @@ __global__ void __launch_bounds__(kThreads, Ring<BN, SWAP>::kCtas)
 
 namespace {
 
-using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
-                            const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                            CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-Encode encoder() {
-  static const Encode f = [] {
-    void* p = nullptr;
-    cudaDriverEntryPointQueryResult found;
-    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found) != cudaSuccess ||
-        found != cudaDriverEntryPointSuccess)
-      p = nullptr;
-    return reinterpret_cast<Encode>(p);
-  }();
-  return f;
-}
-
 // A row-major bf16 matrix [outer, inner] in boxes of 64 x `box`; what lies outside reads as 0.
 bool encode(CUtensorMap* map, const void* p, int64_t inner, int64_t outer, int64_t ld, int box) {
   const cuuint64_t dims[2] = {(cuuint64_t)inner, (cuuint64_t)outer};
@@ -685,30 +526,6 @@ bool encode(CUtensorMap* map, const void* p, int64_t inner, int64_t outer, int64
   return f && f(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(p), dims, strides, boxes, ones,
                 CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
-// How many clusters of `shares` CTAs of a kernel run at once on the current device, asked for once (a GPU's parts hold
-// different numbers of SMs, so this is less than SMs / shares).
-template <class F>
-int64_t clusters_at_once(F* f, int shares, int bytes, std::atomic<int> (&known)[64][9]) {
-  int dev = 0, n = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || dev >= 64) return 1;
-  if ((n = known[dev][shares].load(std::memory_order_relaxed)) > 0) return n;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)shares);
-  cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = bytes;
-  cudaLaunchAttribute at[1];
-  at[0].id = cudaLaunchAttributeClusterDimension;
-  at[0].val.clusterDim = {(unsigned)shares, 1, 1};
-  cfg.attrs = at;
-  cfg.numAttrs = 1;
-  if (cudaOccupancyMaxActiveClusters(&n, f, &cfg) != cudaSuccess || n < 1) {
-    cudaGetLastError();
-    n = 1;
-  }
-  known[dev][shares].store(n, std::memory_order_relaxed);
-  return n;
 }
 
 // One product's launch: tiles, shares of the sum, workspace.
@@ -758,6 +575,8 @@ cudaError_t launch_tile(const Product& p, int sms, void* workspace, cudaStream_t
   const int64_t R = SWAP ? p.J : p.I, C = SWAP ? p.I : p.J;
   a.tiles_r = g.tiles_r, a.tiles_c = g.tiles_c, a.tiles = g.tiles_r * g.tiles_c;
   a.slices = g.slices, a.share = g.share;
+  e = error_word(&a.errors);
+  if (e != cudaSuccess) return e;
   a.parts = g.bytes ? (float*)workspace : nullptr;
   auto rows_on = [](const void* q, int64_t ld, int elem, int bytes) {
     return (uintptr_t)q % bytes == 0 && (uint64_t)ld * elem % bytes == 0;
@@ -838,9 +657,21 @@ cudaError_t launch_tc(const Product& p, int sms, void* workspace, cudaStream_t s
   return choose(p, Launch{p, sms, workspace, s});
 }
 
+cudaError_t error_word(int** at) {
+  static std::atomic<int*> known[64];
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess && dev < 64 && (*at = known[dev].load(std::memory_order_relaxed))) return e;
+  void* p = nullptr;
+  if (e == cudaSuccess) e = cudaGetSymbolAddress(&p, g_errors);
+  *at = (int*)p;
+  if (e == cudaSuccess && dev < 64) known[dev].store(*at, std::memory_order_relaxed);
+  return e;
+}
+
 cudaError_t read_errors(int* out, cudaStream_t s) {
-  void* at = nullptr;
-  cudaError_t e = cudaGetSymbolAddress(&at, g_errors);
+  int* at = nullptr;
+  cudaError_t e = error_word(&at);
   if (e == cudaSuccess) e = cudaMemcpyAsync(out, at, sizeof(int), cudaMemcpyDeviceToHost, s);
   if (e == cudaSuccess) e = cudaStreamSynchronize(s);
   if (e == cudaSuccess && *out) e = cudaMemsetAsync(at, 0, sizeof(int), s);

@@ -315,6 +315,49 @@ def test_pack_infinities_and_nan(dtype):
     assert torch.equal(cols.cpu(), torch.isfinite(ref).all(0))
 
 
+@pytest.mark.parametrize("rows,k,n", [(40, 200, 300), (300, 520, 392), (1030, 4160, 136)])
+def test_f32_infinities_and_nan_as_in_the_definition(rows, k, n):
+    """Infinities and NaN in fp32 operands, and products that overflow: finite, infinite (of the same sign) and NaN
+    where the definition's sums are, at sizes for the fp32 units and for the tensor cores."""
+    x, w, dy = _rand(1, rows, k, dtype=F32), _rand(2, n, k, dtype=F32), _rand(3, rows, n, dtype=F32)
+    x[5, 7], x[9, 3], x[9, 4], x[11, 0] = float("inf"), float("inf"), -float("inf"), float("nan")
+    w[:, 7] = w[:, 7].abs() + 0.5  # no infinity meets a 0
+    w[:, 3:5] = w[:, 3:5].abs() + 0.5
+    w[20, 9], dy[7, 20], dy[8, 20] = -float("inf"), 3.0, 1.0
+
+    def same(got, ref):
+        got, ref = got.double().cpu(), ref.double()
+        assert torch.equal(got.isnan(), ref.isnan()) and torch.equal(got.isposinf(), ref.isposinf())
+        assert torch.equal(got.isneginf(), ref.isneginf())
+        fine = torch.isfinite(ref)
+        size = ref[fine].abs().max()
+        assert bool(((got - ref)[fine].abs() <= 1e-4 * size).all())
+
+    same(L.linear(x, w), _d(x) @ _d(w).T)
+    same(L.linear_grad_input(dy, w), _d(dy) @ _d(w))
+    same(L.linear_grad_weight(dy, x)[0], _d(dy).T @ _d(x))
+    big = torch.zeros(rows, k, device="cuda")
+    big[:, ::8] = 3e38
+    pos = w.nan_to_num(1.0, 1.0, 1.0).abs() + 1.0
+    y = L.linear(big, pos)
+    assert bool(y.isposinf().all())  # at least 3e38 (1 + ... ) more than twice
+    assert bool(torch.isfinite(L.linear(big * 1e-5, pos)).all())
+    assert L.poll_errors() == 0
+
+
+@pytest.mark.parametrize("rows,k,n", [(600, 896, 1000), (2100, 333, 515), (65, 5000, 2049)])
+def test_f32_small_and_large_values(rows, k, n):
+    """fp32 accuracy whatever the scale: each value in bits that one bf16 does not hold, rows scaled by powers of two."""
+    g = torch.Generator(device="cuda").manual_seed(5)
+    scale = torch.ldexp(torch.ones(rows, 1, device="cuda"), torch.randint(-60, 60, (rows, 1), generator=g, device="cuda"))
+    x = _rand(1, rows, k, dtype=F32) * scale
+    w, dy = _rand(2, n, k, dtype=F32), _rand(3, rows, n, dtype=F32)
+    _check_linear(x, w, None, "none", None, L.linear(x, w))
+    _check_grad_input(dy * scale, w, "none", None, L.linear_grad_input(dy * scale, w))
+    _check_grad_weight(dy, _d(x / scale), L.linear_grad_weight(dy, x / scale)[0], None)
+    assert L.poll_errors() == 0
+
+
 @pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("act", R.ACTS)
 def test_slopes_by_formula_and_by_differences(dtype, act):
