@@ -401,7 +401,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       float* sums = reinterpret_cast<float*>(ring);
       for (int64_t tile = first_tile; tile < a.tiles; tile += step) {
         int64_t tr, tc;
-        tile_place(a.tiles_r, a.tiles_c, tile, tr, tc);
+        tile_place<16>(a.tiles_r, a.tiles_c, tile, tr, tc);
         simt_sums<128, A_MN, B_MN>(a.f, sums, tr * kBM, tc * kBN, 0, p.L);
         units_sync();
         for (int row = warp; row < kBM && tr * kBM + row < p.I; row += 8) {
@@ -417,7 +417,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     bool ok = true;
     for (int64_t tile = first_tile; ok && tile < a.tiles; tile += step) {
       int64_t tr, tc;
-      tile_place(a.tiles_r, a.tiles_c, tile, tr, tc);
+      tile_place<16>(a.tiles_r, a.tiles_c, tile, tr, tc);
       const int r0 = (int)(tr * kBM), c0 = (int)(tc * kBN);
       for (int k = 0; k < slices; ++k, ++n) {
         const uint32_t s = n % kStages;
@@ -486,7 +486,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     bool ok = true;
     for (int64_t tile = first_tile; ok && tile < a.tiles; tile += step) {
       int64_t tr, tc;
-      tile_place(a.tiles_r, a.tiles_c, tile, tr, tc);
+      tile_place<16>(a.tiles_r, a.tiles_c, tile, tr, tc);
       float acc[2][32];
 #pragma unroll
       for (int t = 0; t < 32; ++t) acc[0][t] = acc[1][t] = 0.0f;
@@ -523,7 +523,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     cluster_sync();
     if (!odd && warp < kEpiWarps && !*dead) {
       int64_t tr, tc;
-      tile_place(a.tiles_r, a.tiles_c, first_tile, tr, tc);
+      tile_place<16>(a.tiles_r, a.tiles_c, first_tile, tr, tc);
       const int quarter = warp % 4;
       const float* part = a.parts + (size_t)first_tile * shares * kBN * kBM + 32 * quarter + lane;
       for (int c = (int)rank + (int)shares * (warp / 4); c < kBN / 32; c += 2 * (int)shares) {

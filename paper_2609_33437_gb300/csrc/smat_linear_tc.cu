@@ -1,19 +1,25 @@
 // The linear layers' products of bf16 matrices on the tensor cores (tcgen05; smat_linear.h, Product).
 //
-// A CTA makes tiles of 128 x BN sums: one warp fetches 64-deep slices of both operands by TMA into a ring of
-// 128-byte-swizzled buffers, one thread multiplies them into tensor memory (fp32), eight warps take finished sums
-// out of it, 32 at a time, and finish them (bias, activation, 8-bit form, residual, slope, older gradient) while the
-// next tile's sums are made in the other half of tensor memory.
+// In every CTA one warp fetches 64-deep slices of both operands by TMA into a ring of 128-byte-swizzled buffers, one
+// thread multiplies them into tensor memory (fp32), and eight warps take finished sums out of it, 32 columns at a time,
+// and finish them (bias, activation, 8-bit form, residual, slope, older gradient) while the next tile's sums are made in
+// the other half of tensor memory.
 //
-// SWAP false: the tile's 128 rows are rows i of the result, its columns are j. A thread then holds 32 columns of a
-// row, whole groups of the 8-bit form, and reads and writes 64 bytes of a row at a time (whole sectors).
-// SWAP true, for results of few rows: the 128 rows are columns j and the tile's columns are rows i, so that a wide
-// weight fills the 128 and the few rows cost a narrow tile. A warp then holds 32 neighbouring columns of a row, one
-// per lane. The same form finishes results whose rows do not start on 32 bytes, after a turn through shared memory.
+// Wide products (pair_kernel): two CTAs on neighbouring SMs make a tile of 256 x `width` sums, each 128 of its rows. Each
+// fetches its rows of one operand and half of the other, which the pair's multiplications read from both: 32 KB a slice
+// and CTA for 256 columns, where a CTA by itself needs 48 KB and the copies bound it (8192 x 11008 x 4096: 484 us).
+// `width` and the shares of the sum are chosen by an estimate of the time, see plan_pair. The tile's rows are rows i of
+// the result. A thread holds 32 columns of a row, whole groups of the 8-bit form, and reads and writes 64 bytes of a row
+// at a time; results whose rows do not start on 16 bytes take a turn through shared memory, to 32 neighbouring columns
+// per warp.
 //
-// Where the tiles are fewer than the SMs, the sum is cut among the CTAs of a cluster: each leaves its share of the
-// sums in its shared memory, then every CTA adds up some of the columns in the cluster's order and finishes them. No
-// workspace, no atomics, the same result every time.
+// Products of at most 128 rows (narrow_kernel): the tile's 128 rows are columns j and its 32, 64 or 128 columns are rows
+// i, so that a wide weight fills the 128 and the few rows cost a narrow tile. A warp holds 32 neighbouring columns of a
+// row, one per lane.
+//
+// Where the tiles are fewer than the SMs, the sum is cut among the CTAs (or pairs) of a cluster: each leaves its share of
+// the sums, then every CTA adds up some of the columns in the cluster's order and finishes them. No atomics, the same
+// result every time.
 
 #include "smat_linear.h"
 #include "smat_linear_tc.cuh"
@@ -28,22 +34,27 @@ namespace {
 constexpr int kBytesA = kBM * kBK * 2;
 constexpr int kTurn = 32 * 33 * 4;  // a warp's 32 x 32 sums, turned
 
-// Swapped tiles are narrow and bound by the weight's bytes: two CTAs per SM, so that one's start and end lie beside
-// the other's copies.
-template <int BN, bool SWAP>
+// Narrow tiles are bound by the weight's bytes: two CTAs per SM, so that one's start and end lie beside the other's
+// copies.
+template <int BN>
 struct Ring {
   static constexpr int kBytesB = BN * kBK * 2;
-  static constexpr int kStages = SWAP ? (BN == 32 ? 5 : BN == 64 ? 4 : 3) : 4;
+  static constexpr int kStages = BN == 32 ? 5 : BN == 64 ? 4 : 3;
   static constexpr int kStage = kBytesA + kBytesB;
-  static constexpr int kBytes = kStages * kStage + (SWAP ? 0 : kEpiWarps * kTurn) + 1024;
-  static constexpr int kCtas = SWAP ? 2 : 1;  // per SM
+  static constexpr int kBytes = kStages * kStage + 1024;
+  static constexpr int kCtas = 2;  // per SM
 };
+
+constexpr int kPairRows = 2 * kBM, kPairStages = 6, kPairStage = 2 * kBytesA;
+constexpr int kPairBytes = kPairStages * kPairStage + kEpiWarps * kTurn + 1024;
+constexpr int kSums = 256;  // columns of tensor memory for one tile's sums
 
 struct Args {
   Product p;
-  int64_t tiles, tiles_r, tiles_c;  // of the tile's rows and columns (of 128 and BN)
+  int64_t tiles, tiles_r, tiles_c;  // along the tile's rows and columns
   int slices;                       // of 64 along the sum
-  int share;                        // slices per CTA of a cluster
+  int share;                        // slices per CTA (or pair) of a cluster
+  int width;                        // columns of a pair's tile
   float* parts;                     // the shares' sums, or NULL
   int* errors;                      // device error bits
   bool by_rows;                     // rows of out and residual start on 16 bytes, those of q on 8
@@ -289,15 +300,13 @@ __device__ __forceinline__ void finish_rows(const Args& a, int64_t row0, int64_t
 // row: in the workspace (a.parts), or, where the tile has no more than 8 columns, in its own shared memory, which the
 // others read across the cluster. (Reading larger tiles there is slow: 128 x 256 sums of 8 shares took 15 us, through
 // the workspace, which stays in L2, 3.) 
-template <int MODE, bool SWAP, int BN>
-__global__ void __launch_bounds__(kThreads, Ring<BN, SWAP>::kCtas)
-    tc_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+template <int MODE, int BN>
+__global__ void __launch_bounds__(kThreads, Ring<BN>::kCtas)
+    narrow_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
               const __grid_constant__ Args a) {
-  // the tile's rows come from W where swapped, from the other operand else
-  constexpr bool A_MN = SWAP ? MODE == kGradInput : MODE == kGradWeight;
-  constexpr bool B_MN = SWAP ? false : MODE != kForward;
-  static_assert(!(SWAP && MODE == kGradWeight), "a weight gradient's rows and columns are both a layer's");
-  constexpr int kStages = Ring<BN, SWAP>::kStages, kStage = Ring<BN, SWAP>::kStage;
+  // the tile's rows come from W, its columns from x or dy
+  constexpr bool A_MN = MODE == kGradInput, B_MN = false;
+  constexpr int kStages = Ring<BN>::kStages, kStage = Ring<BN>::kStage;
 
   extern __shared__ uint8_t raw[];
   __shared__ __align__(8) uint64_t bars[2 * kStages + 5];
@@ -316,7 +325,6 @@ __global__ void __launch_bounds__(kThreads, Ring<BN, SWAP>::kCtas)
   const int slices = max(0, min(a.share, a.slices - slice0));
   const int64_t first_tile = blockIdx.x / shares, step = gridDim.x / shares;
 
-  auto turn_of = [&](int w) { return reinterpret_cast<float*>(ring + kStages * kStage + w * kTurn); };
   auto fetch = [&](uint32_t s, int r0, int c0, int k) {
     const int l = (slice0 + k) * kBK;
     const uint32_t bar = full + 8 * s, to_a = smem_address(ring) + s * kStage, to_b = to_a + kBytesA;
@@ -327,12 +335,7 @@ __global__ void __launch_bounds__(kThreads, Ring<BN, SWAP>::kCtas)
     } else {
       tma_load(to_a, &map_a, l, r0, bar);
     }
-    if (B_MN) {
-#pragma unroll
-      for (int b = 0; b < BN / 64; ++b) tma_load(to_b + b * 8192, &map_b, c0 + 64 * b, l, bar);
-    } else {
-      tma_load(to_b, &map_b, l, c0, bar);
-    }
+    tma_load(to_b, &map_b, l, c0, bar);
   };
   const int ahead = first_tile < a.tiles ? min(slices, kStages) : 0;  // slices fetched before the CTA meets
 
@@ -349,7 +352,7 @@ __global__ void __launch_bounds__(kThreads, Ring<BN, SWAP>::kCtas)
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     int64_t tr, tc;
-    tile_place(a.tiles_r, a.tiles_c, first_tile, tr, tc);
+    tile_place<16>(a.tiles_r, a.tiles_c, first_tile, tr, tc);
     for (int k = 0; k < ahead; ++k) fetch(k, (int)(tr * kBM), (int)(tc * BN), k);
   }
   __syncwarp();
@@ -369,7 +372,7 @@ __global__ void __launch_bounds__(kThreads, Ring<BN, SWAP>::kCtas)
     bool ok = true;
     for (int64_t tile = first_tile; ok && tile < a.tiles; tile += step) {
       int64_t tr, tc;
-      tile_place(a.tiles_r, a.tiles_c, tile, tr, tc);
+      tile_place<16>(a.tiles_r, a.tiles_c, tile, tr, tc);
       for (int k = tile == first_tile ? ahead : 0; k < slices; ++k, ++n) {
         const uint32_t s = n % kStages;
         ok = bar_wait(empty + 8 * s, (n / kStages + 1) & 1, dead, a.errors);
@@ -419,7 +422,7 @@ __global__ void __launch_bounds__(kThreads, Ring<BN, SWAP>::kCtas)
     uint32_t made = 0;
     for (int64_t tile = first_tile; tile < a.tiles; tile += step, ++made) {
       int64_t tr, tc;
-      tile_place(a.tiles_r, a.tiles_c, tile, tr, tc);
+      tile_place<16>(a.tiles_r, a.tiles_c, tile, tr, tc);
       const int64_t r0 = tr * kBM + 32 * quarter, c0 = tc * BN;
       const uint32_t half = made & 1, sums = tmem + half * BN + ((uint32_t)(32 * quarter) << 16);
       if (!bar_wait(sums_full + 8 * half, made / 2 & 1, dead, a.errors)) break;
@@ -429,48 +432,22 @@ __global__ void __launch_bounds__(kThreads, Ring<BN, SWAP>::kCtas)
         __syncwarp();
         if (lane == 0) bar_arrive(sums_empty + 8 * half);
       };
-      if constexpr (SWAP) {
-        const int blocks = (int)((min((int64_t)BN, a.p.I - c0) + 7) / 8);  // of 8 columns of the tile, rows of the result
-        for (int c = warp / 4; c < blocks; c += kEpiWarps / 4) {
-          float v[8];
-          if (slices > 0) {
-            take8(sums + 8 * c, v);
-          } else {
-#pragma unroll
-            for (int t = 0; t < 8; ++t) v[t] = 0.0f;
-          }
-          if (shares == 1) {
-            if (r0 < a.p.J) finish_column<MODE, 8>(a, c0 + 8 * c, r0 + lane, v);
-          } else {
-            put_part(part + 8 * c * kBM, v);
-          }
-        }
-        release();
-      } else {
-        // this warp's blocks of 32 columns: the first or the second half of the tile's
-        constexpr int kMine = BN / 64;
-        const int first = warp / 4 * kMine, end = first + kMine;
-        auto take = [&](int c, float(&v)[32]) {
-          if (slices > 0) {
-            take32(sums + 32 * c, v);
-          } else {
-#pragma unroll
-            for (int t = 0; t < 32; ++t) v[t] = 0.0f;
-          }
-        };
-        if (shares == 1) {
-          finish_rows<MODE>(a, r0, c0, first, end, 1, turn_of(warp), [&](int c, float(&v)[32]) {
-            take(c, v);
-            if (c + 1 == end) release();
-          });
+      const int blocks = (int)((min((int64_t)BN, a.p.I - c0) + 7) / 8);  // of 8 columns of the tile, rows of the result
+      for (int c = warp / 4; c < blocks; c += kEpiWarps / 4) {
+        float v[8];
+        if (slices > 0) {
+          take8(sums + 8 * c, v);
         } else {
-          for (int c = first; c < end && c0 + 32 * c < a.p.J && r0 < a.p.I; ++c) {
-            float v[32];
-            take(c, v);
-            put_part(part + 32 * c * kBM, v);
-          }
+#pragma unroll
+          for (int t = 0; t < 8; ++t) v[t] = 0.0f;
+        }
+        if (shares == 1) {
+          if (r0 < a.p.J) finish_column<MODE, 8>(a, c0 + 8 * c, r0 + lane, v);
+        } else {
+          put_part(part + 8 * c * kBM, v);
         }
       }
+      release();
     }
   }
   __syncwarp();
@@ -480,29 +457,22 @@ __global__ void __launch_bounds__(kThreads, Ring<BN, SWAP>::kCtas)
     cluster_sync();
     if (warp < kEpiWarps && !*dead) {
       int64_t tr, tc;
-      tile_place(a.tiles_r, a.tiles_c, first_tile, tr, tc);
+      tile_place<16>(a.tiles_r, a.tiles_c, first_tile, tr, tc);
       const int quarter = warp % 4;
       const int64_t r0 = tr * kBM + 32 * quarter, c0 = tc * BN;
       const float* part = (a.parts ? a.parts + (size_t)first_tile * shares * BN * kBM : reinterpret_cast<float*>(ring)) +
                           32 * quarter + lane;
       const int first = (int)rank + (int)shares * (warp / 4), turns = (int)shares * (kEpiWarps / 4);
-      if constexpr (SWAP) {
-        const int cols = (int)min((int64_t)BN, a.p.I - c0);
-        for (int c = first; 8 * c < cols && r0 < a.p.J; c += turns) {
-          float v[8];
-          if (a.parts)
-            add_parts(shares, v, [&](uint32_t s, int t) { return __ldcg(part + ((size_t)s * BN + 8 * c + t) * kBM); });
-          else
-            add_parts(shares, v, [&](uint32_t s, int t) {
-              return 8 * c + t < cols ? cluster_load(part + (8 * c + t) * kBM, s) : 0.0f;
-            });
-          finish_column<MODE, 8>(a, c0 + 8 * c, r0 + lane, v);
-        }
-      } else {
-        const int blocks = r0 < a.p.I ? (int)((min((int64_t)BN, a.p.J - c0) + 31) / 32) : 0;
-        finish_rows<MODE>(a, r0, c0, first, blocks, turns, turn_of(warp), [&](int c, float(&v)[32]) {
-          add_parts(shares, v, [&](uint32_t s, int t) { return __ldcg(part + ((size_t)s * BN + 32 * c + t) * kBM); });
-        });
+      const int cols = (int)min((int64_t)BN, a.p.I - c0);
+      for (int c = first; 8 * c < cols && r0 < a.p.J; c += turns) {
+        float v[8];
+        if (a.parts)
+          add_parts(shares, v, [&](uint32_t s, int t) { return __ldcg(part + ((size_t)s * BN + 8 * c + t) * kBM); });
+        else
+          add_parts(shares, v, [&](uint32_t s, int t) {
+            return 8 * c + t < cols ? cluster_load(part + (8 * c + t) * kBM, s) : 0.0f;
+          });
+        finish_column<MODE, 8>(a, c0 + 8 * c, r0 + lane, v);
       }
     }
     cluster_sync();
@@ -513,9 +483,188 @@ __global__ void __launch_bounds__(kThreads, Ring<BN, SWAP>::kCtas)
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2 * BN));
 }
 
-}  // namespace
+// A pair's tile: see the head of this file. The pair's first CTA ("leader") multiplies for both.
+template <int MODE>
+__global__ void __launch_bounds__(kThreads, 1)
+    pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+                const __grid_constant__ Args a) {
+  constexpr bool A_MN = MODE == kGradWeight, B_MN = MODE != kForward;
+  constexpr int kStages = kPairStages, kStage = kPairStage;
 
-namespace {
+  extern __shared__ uint8_t raw[];
+  __shared__ __align__(8) uint64_t bars[2 * kStages + 5];
+  __shared__ uint32_t tmem_at;
+  __shared__ int dead_flag;
+  uint8_t* ring = raw + ((1024 - (smem_address(raw) & 1023)) & 1023);
+  volatile int* dead = &dead_flag;
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const uint32_t full = smem_address(bars), empty = full + 8 * kStages, sums_full = empty + 8 * kStages,
+                 sums_empty = sums_full + 16, drained = sums_empty + 16;
+  float* turn = reinterpret_cast<float*>(ring + kStages * kStage + warp * kTurn);
+
+  uint32_t ctas, rank;
+  asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(ctas));
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+  const uint32_t shares = ctas / 2, share = rank / 2, member = rank & 1, leader = rank & ~1u;
+  const int slice0 = (int)share * a.share;
+  const int slices = max(0, min(a.share, a.slices - slice0));
+  const int64_t first_tile = blockIdx.x / ctas, step = gridDim.x / ctas;
+  const int half_width = a.width / 2;
+
+  if (warp == kTmaWarp && lane == 0) {
+    dead_flag = 0;
+    for (int s = 0; s < kStages; ++s) {
+      bar_init(full + 8 * s, 1);
+      bar_init(empty + 8 * s, 1);
+    }
+    bar_init(drained, 1);
+    for (int b = 0; b < 2; ++b) {
+      bar_init(sums_full + 8 * b, 1);
+      bar_init(sums_empty + 8 * b, 2 * kEpiWarps);
+    }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncwarp();
+  if (warp == kMmaWarp) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_address(&tmem_at)),
+                 "r"(2 * kSums)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+    fence_before();
+  }
+  __syncthreads();
+  cluster_sync();  // the partner's barriers are there
+  fence_after();
+  const uint32_t tmem = tmem_at;
+
+  if (warp == kTmaWarp && lane == 0) {
+    const int blocks_b = B_MN ? (half_width + 63) / 64 : 1;  // copies of this CTA's half of the other operand
+    const uint32_t bytes = kBytesA + (B_MN ? blocks_b * 8192 : half_width * kBK * 2);
+    const uint32_t full_there = cluster_address_of(full, leader);
+    uint32_t n = 0;  // slices fetched so far
+    bool ok = true;
+    for (int64_t tile = first_tile; ok && tile < a.tiles; tile += step) {
+      int64_t tr, tc;
+      tile_place<8>(a.tiles_r, a.tiles_c, tile, tr, tc);
+      const int r0 = (int)(tr * kPairRows) + (int)member * kBM, c0 = (int)(tc * a.width) + (int)member * half_width;
+      for (int k = 0; k < slices; ++k, ++n) {
+        const uint32_t s = n % kStages;
+        ok = bar_wait(empty + 8 * s, (n / kStages + 1) & 1, dead, a.errors);
+        if (!ok) break;
+        const int l = (slice0 + k) * kBK;
+        const uint32_t bar = full_there + 8 * s, to_a = smem_address(ring) + s * kStage, to_b = to_a + kBytesA;
+        if (member == 0) bar_expect(full + 8 * s, 2 * bytes);
+        if (A_MN) {
+          tma_load_pair(to_a, &map_a, r0, l, bar);
+          tma_load_pair(to_a + 8192, &map_a, r0 + 64, l, bar);
+        } else {
+          tma_load_pair(to_a, &map_a, l, r0, bar);
+        }
+        if (B_MN) {
+          for (int b = 0; b < blocks_b; ++b) tma_load_pair(to_b + b * 8192, &map_b, c0 + 64 * b, l, bar);
+        } else {
+          tma_load_pair(to_b, &map_b, l, c0, bar);
+        }
+      }
+    }
+    if (!ok && member == 0)  // both CTAs' copies in flight land before either ends (they meet below)
+      for (uint32_t s = 0; s < kStages && s < n; ++s) {
+        const uint32_t last = n - 1 - s;
+        for (int i = 0; i < (1 << 20) && !bar_try(full + 8 * (last % kStages), last / kStages & 1); ++i) {
+        }
+      }
+  } else if (warp == kMmaWarp && lane == 0 && member == 0) {
+    const uint32_t inst = kInstruction<A_MN, B_MN, 0, kPairRows> | (uint32_t)(a.width >> 3) << 17;
+    const uint16_t both = (uint16_t)(3u << rank);
+    uint32_t n = 0, made = 0;
+    bool ok = true;
+    for (int64_t tile = first_tile; ok && tile < a.tiles; tile += step, ++made) {
+      const uint32_t half = made & 1, sums = tmem + half * kSums;
+      ok = bar_wait(sums_empty + 8 * half, (made / 2 + 1) & 1, dead, a.errors);
+      if (!ok) break;
+      fence_after();
+      for (int k = 0; k < slices; ++k, ++n) {
+        const uint32_t s = n % kStages;
+        ok = bar_wait(full + 8 * s, n / kStages & 1, dead, a.errors);
+        if (!ok) break;
+        fence_after();
+        const uint32_t at_a = smem_address(ring) + s * kStage;
+        const uint64_t da = descriptor<A_MN>(at_a), db = descriptor<B_MN>(at_a + kBytesA);
+#pragma unroll
+        for (int t = 0; t < kBK / 16; ++t)
+          mma_pair(sums, da + t * kStep16<A_MN>, db + t * kStep16<B_MN>, inst, k > 0 || t > 0);
+        mma_commit_pair(empty + 8 * s, both);
+      }
+      if (ok) mma_commit_pair(sums_full + 8 * half, both);
+    }
+    if (!ok) {  // products in flight end before the CTAs do
+      mma_commit_pair(drained, (uint16_t)(1u << rank));
+      for (int i = 0; i < (1 << 20) && !bar_try(drained, 0); ++i) {
+      }
+    }
+  } else if (warp < kEpiWarps) {
+    const int quarter = warp % 4;  // the 32 rows of tensor memory that this warp may read
+    const uint32_t sums_empty_there = cluster_address_of(sums_empty, leader);
+    // this warp's blocks of 32 columns: the first or the second half of the tile's
+    const int blocks = a.width / 32, first = warp / 4 ? (blocks + 1) / 2 : 0, end = warp / 4 ? blocks : (blocks + 1) / 2;
+    uint32_t made = 0;
+    for (int64_t tile = first_tile; tile < a.tiles; tile += step, ++made) {
+      int64_t tr, tc;
+      tile_place<8>(a.tiles_r, a.tiles_c, tile, tr, tc);
+      const int64_t r0 = tr * kPairRows + (int)member * kBM + 32 * quarter, c0 = tc * a.width;
+      const uint32_t half = made & 1, sums = tmem + half * kSums + ((uint32_t)(32 * quarter) << 16);
+      if (!bar_wait(sums_full + 8 * half, made / 2 & 1, dead, a.errors)) break;
+      fence_after();
+      auto take = [&](int c, float(&v)[32]) {
+        if (slices > 0) {
+          take32(sums + 32 * c, v);
+        } else {
+#pragma unroll
+          for (int t = 0; t < 32; ++t) v[t] = 0.0f;
+        }
+        if (c + 1 == end) {  // this warp has what it needs of these sums
+          fence_before();
+          __syncwarp();
+          if (lane == 0) bar_arrive_there(sums_empty_there + 8 * half);
+        }
+      };
+      if (shares == 1) {
+        finish_rows<MODE>(a, r0, c0, first, end, 1, turn, take);
+      } else {
+        float* part = a.parts + ((size_t)first_tile * ctas + rank) * a.width * kBM + 32 * quarter + lane;
+        for (int c = first; c < end; ++c) {
+          float v[32];
+          take(c, v);
+          if (c0 + 32 * c < a.p.J && r0 < a.p.I) put_part(part + 32 * c * kBM, v);
+        }
+      }
+    }
+  }
+  __syncwarp();
+  if (shares > 1) {
+    // one tile per cluster: its CTAs add up and finish blocks of their rows' columns in turn
+    __syncthreads();
+    cluster_sync();
+    if (warp < kEpiWarps && !*dead) {
+      int64_t tr, tc;
+      tile_place<8>(a.tiles_r, a.tiles_c, first_tile, tr, tc);
+      const int quarter = warp % 4;
+      const int64_t r0 = tr * kPairRows + (int)member * kBM + 32 * quarter, c0 = tc * a.width;
+      const float* part = a.parts + ((size_t)first_tile * ctas + member) * a.width * kBM + 32 * quarter + lane;
+      const size_t apart = (size_t)2 * a.width * kBM;
+      const int blocks = r0 < a.p.I ? (int)((min((int64_t)a.width, a.p.J - c0) + 31) / 32) : 0;
+      finish_rows<MODE>(a, r0, c0, (int)share + (int)shares * (warp / 4), blocks, (int)shares * (kEpiWarps / 4), turn,
+                        [&](int c, float(&v)[32]) {
+                          add_parts(shares, v, [&](uint32_t s, int t) { return __ldcg(part + s * apart + (32 * c + t) * kBM); });
+                        });
+    }
+  }
+  fence_before();
+  __syncthreads();
+  cluster_sync();  // the partner's multiplications read this CTA's shared memory, and its arrivals write it
+  if (warp == kMmaWarp)
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2 * kSums));
+}
 
 // A row-major bf16 matrix [outer, inner] in boxes of 64 x `box`; what lies outside reads as 0.
 bool encode(CUtensorMap* map, const void* p, int64_t inner, int64_t outer, int64_t ld, int box) {
@@ -531,52 +680,80 @@ bool encode(CUtensorMap* map, const void* p, int64_t inner, int64_t outer, int64
 // One product's launch: tiles, shares of the sum, workspace.
 struct Plan {
   int64_t tiles_r, tiles_c, ctas;
-  int slices, share, shares;
+  int slices, share, shares, width;
   size_t bytes;  // of the shares' sums
 };
 
-template <int MODE, bool SWAP, int BN>
-cudaError_t plan_tile(const Product& p, int sms, Plan* plan) {
+template <int MODE, int BN>
+cudaError_t plan_narrow(const Product& p, int sms, Plan* plan) {
   static std::atomic<uint64_t> allowed;
-  static std::atomic<int> clusters[64][9];
-  auto* f = tc_kernel<MODE, SWAP, BN>;
-  const cudaError_t e = allow_shared(f, Ring<BN, SWAP>::kBytes, allowed);
+  const cudaError_t e = allow_shared(narrow_kernel<MODE, BN>, Ring<BN>::kBytes, allowed);
   if (e != cudaSuccess) return e;
-  const int64_t R = SWAP ? p.J : p.I, C = SWAP ? p.I : p.J;
   Plan g = {};
-  g.tiles_r = (R + kBM - 1) / kBM;
-  g.tiles_c = (C + BN - 1) / BN;
+  g.width = BN;
+  g.tiles_r = (p.J + kBM - 1) / kBM;
+  g.tiles_c = (p.I + BN - 1) / BN;
   g.slices = (int)((p.L + kBK - 1) / kBK);
-  const int64_t tiles = g.tiles_r * g.tiles_c, room = (int64_t)Ring<BN, SWAP>::kCtas * sms;
-  // Shares of the sum as long as all CTAs have room at once, three slices in each at least. Where the tensor cores bound
-  // a tile, all clusters have to run at once, or the last ones double the time; swapped tiles wait for memory, and more
-  // bytes in flight outweigh that.
+  const int64_t tiles = g.tiles_r * g.tiles_c, room = (int64_t)Ring<BN>::kCtas * sms;
+  // Shares of the sum as long as all CTAs have room at once, three slices in each at least.
   int shares = 8;
-  while (shares > 1 && (tiles * shares > room || g.slices < 3 * shares ||
-                        (!SWAP && tiles > clusters_at_once(f, shares, Ring<BN, SWAP>::kBytes, clusters))))
-    --shares;
+  while (shares > 1 && (tiles * shares > room || g.slices < 3 * shares)) --shares;
   g.share = (g.slices + shares - 1) / shares;
   g.shares = shares > 1 ? (g.slices + g.share - 1) / g.share : 1;
   g.ctas = g.shares > 1 ? tiles * g.shares : (tiles < room ? tiles : room);
-  if (g.shares > 1 && !(SWAP && p.I <= 8)) g.bytes = (size_t)tiles * g.shares * BN * kBM * sizeof(float);
+  if (g.shares > 1 && p.I > 8) g.bytes = (size_t)tiles * g.shares * BN * kBM * sizeof(float);
   *plan = g;
   return cudaSuccess;
 }
 
-template <int MODE, bool SWAP, int BN>
-cudaError_t launch_tile(const Product& p, int sms, void* workspace, cudaStream_t s) {
-  constexpr bool A_MN = SWAP ? MODE == kGradInput : MODE == kGradWeight;
-  constexpr bool B_MN = SWAP ? false : MODE != kForward;
-  Plan g;
-  cudaError_t e = plan_tile<MODE, SWAP, BN>(p, sms, &g);
+// Width and shares of a pair's tile: the least estimate of the time in cycles. A slice takes the longer of its
+// multiplications (2 per column) and its copies (16 KB and 64 bytes per column at 64 bytes a cycle, as measured with
+// every SM copying); a tile's columns take about 16 each to finish, beside the next tile's products, and at the end by
+// themselves; shares are written and read through L2. All clusters of a shared sum run at once.
+template <int MODE>
+cudaError_t plan_pair(const Product& p, Plan* plan) {
+  static std::atomic<uint64_t> allowed;
+  static std::atomic<int> clusters[64][9];
+  auto* f = pair_kernel<MODE>;
+  const cudaError_t e = allow_shared(f, kPairBytes, allowed);
   if (e != cudaSuccess) return e;
+  Plan best = {};
+  double least = 0;
+  const int slices = (int)((p.L + kBK - 1) / kBK);
+  const int64_t tiles_r = (p.I + kPairRows - 1) / kPairRows;
+  for (int width = 256; width >= 64; width -= 32) {
+    const int64_t tiles_c = (p.J + width - 1) / width, tiles = tiles_r * tiles_c;
+    for (int shares = 1; shares <= 4; ++shares) {
+      const int64_t at_once = clusters_at_once(f, 2 * shares, kPairBytes, clusters);
+      if (shares > 1 && (tiles > at_once || slices < 3 * shares)) break;
+      const int share = (slices + shares - 1) / shares;
+      const double rounds = (double)((tiles + at_once - 1) / at_once);
+      const double slice = 2.0 * width > 256.0 + width ? 2.0 * width : 256.0 + width;
+      const double products = share * slice, finish = 16.0 * width;
+      const double time = rounds * (products > finish ? products : finish) + finish / shares + 400.0 * rounds +
+                          (shares > 1 ? 3000.0 + 14.0 * width : 0.0);
+      if (best.width == 0 || time < least) {
+        least = time;
+        best.width = width;
+        best.tiles_r = tiles_r, best.tiles_c = tiles_c;
+        best.slices = slices, best.share = share;
+        best.shares = shares > 1 ? (slices + share - 1) / share : 1;
+        best.ctas = 2 * best.shares * (best.shares > 1 ? tiles : (tiles < at_once ? tiles : at_once));
+        best.bytes = best.shares > 1 ? (size_t)tiles * 2 * best.shares * width * kBM * sizeof(float) : 0;
+      }
+    }
+  }
+  *plan = best;
+  return cudaSuccess;
+}
+
+// What both kernels take.
+cudaError_t fill_args(const Product& p, const Plan& g, void* workspace, Args* args) {
   Args a = {};
   a.p = p;
-  const int64_t R = SWAP ? p.J : p.I, C = SWAP ? p.I : p.J;
   a.tiles_r = g.tiles_r, a.tiles_c = g.tiles_c, a.tiles = g.tiles_r * g.tiles_c;
-  a.slices = g.slices, a.share = g.share;
-  e = error_word(&a.errors);
-  if (e != cudaSuccess) return e;
+  a.slices = g.slices, a.share = g.share, a.width = g.width;
+  const cudaError_t e = error_word(&a.errors);
   a.parts = g.bytes ? (float*)workspace : nullptr;
   auto rows_on = [](const void* q, int64_t ld, int elem, int bytes) {
     return (uintptr_t)q % bytes == 0 && (uint64_t)ld * elem % bytes == 0;
@@ -586,37 +763,65 @@ cudaError_t launch_tile(const Product& p, int sms, void* workspace, cudaStream_t
   a.full_sectors = rows_on(p.out, p.ldo, 2, 32) && (!p.residual || rows_on(p.residual, p.ldr, 2, 32)) &&
                    (!p.q || rows_on(p.q, p.ldq, 1, 32));
   a.wide_bias = (uintptr_t)p.bias % 16 == 0;
+  *args = a;
+  return e;
+}
 
-  CUtensorMap ma = {}, mb = {};  // not read where the sum is over nothing
-  if (p.L > 0) {
-    const void *pa = SWAP ? p.b : p.a, *pb = SWAP ? p.a : p.b;
-    const int64_t lda = SWAP ? p.ldb : p.lda, ldb = SWAP ? p.lda : p.ldb;
-    const bool ok = (A_MN ? encode(&ma, pa, R, p.L, lda, kBK) : encode(&ma, pa, p.L, R, lda, kBM)) &&
-                    (B_MN ? encode(&mb, pb, C, p.L, ldb, kBK) : encode(&mb, pb, p.L, C, ldb, BN));
-    if (!ok) return cudaErrorNotSupported;
-  }
+template <class F>
+cudaError_t launch(F* f, int64_t ctas, int cluster, int bytes, const CUtensorMap& ma, const CUtensorMap& mb, const Args& a,
+                   cudaStream_t s) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)g.ctas);
+  cfg.gridDim = dim3((unsigned)ctas);
   cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = Ring<BN, SWAP>::kBytes;
+  cfg.dynamicSmemBytes = bytes;
   cfg.stream = s;
   cudaLaunchAttribute at[1];
   at[0].id = cudaLaunchAttributeClusterDimension;
-  at[0].val.clusterDim = {(unsigned)g.shares, 1, 1};
+  at[0].val.clusterDim = {(unsigned)cluster, 1, 1};
   cfg.attrs = at;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, tc_kernel<MODE, SWAP, BN>, ma, mb, a);
+  return cudaLaunchKernelEx(&cfg, f, ma, mb, a);
 }
 
-// The tile for a product: go.run<MODE, SWAP, BN>() of it. Up to 128 rows the weight's columns take the tile's 128 rows.
+template <int MODE, int BN>
+cudaError_t launch_narrow(const Product& p, int sms, void* workspace, cudaStream_t s) {
+  Plan g;
+  Args a;
+  cudaError_t e = plan_narrow<MODE, BN>(p, sms, &g);
+  if (e == cudaSuccess) e = fill_args(p, g, workspace, &a);
+  if (e != cudaSuccess) return e;
+  CUtensorMap ma = {}, mb = {};  // not read where the sum is over nothing
+  if (p.L > 0 &&
+      !((MODE == kGradInput ? encode(&ma, p.b, p.J, p.L, p.ldb, kBK) : encode(&ma, p.b, p.L, p.J, p.ldb, kBM)) &&
+        encode(&mb, p.a, p.L, p.I, p.lda, BN)))
+    return cudaErrorNotSupported;
+  return launch(narrow_kernel<MODE, BN>, g.ctas, g.shares, Ring<BN>::kBytes, ma, mb, a, s);
+}
+
+template <int MODE>
+cudaError_t launch_pair(const Product& p, void* workspace, cudaStream_t s) {
+  constexpr bool A_MN = MODE == kGradWeight, B_MN = MODE != kForward;
+  Plan g;
+  Args a;
+  cudaError_t e = plan_pair<MODE>(p, &g);
+  if (e == cudaSuccess) e = fill_args(p, g, workspace, &a);
+  if (e != cudaSuccess) return e;
+  CUtensorMap ma = {}, mb = {};
+  if (p.L > 0 && !((A_MN ? encode(&ma, p.a, p.I, p.L, p.lda, kBK) : encode(&ma, p.a, p.L, p.I, p.lda, kBM)) &&
+                   (B_MN ? encode(&mb, p.b, p.J, p.L, p.ldb, kBK) : encode(&mb, p.b, p.L, p.J, p.ldb, g.width / 2))))
+    return cudaErrorNotSupported;
+  return launch(pair_kernel<MODE>, g.ctas, 2 * g.shares, kPairBytes, ma, mb, a, s);
+}
+
+// A product's kernel: go.narrow<MODE, BN>() or go.pair<MODE>(). Up to 128 rows the weight's columns take the tile's rows.
 template <int MODE, class Go>
 cudaError_t choose_mode(const Product& p, Go&& go) {
   if constexpr (MODE != kGradWeight) {
-    if (p.I <= 32) return go.template run<MODE, true, 32>();
-    if (p.I <= 64) return go.template run<MODE, true, 64>();
-    if (p.I <= 128) return go.template run<MODE, true, 128>();
+    if (p.I <= 32) return go.template narrow<MODE, 32>();
+    if (p.I <= 64) return go.template narrow<MODE, 64>();
+    if (p.I <= 128) return go.template narrow<MODE, 128>();
   }
-  return go.template run<MODE, false, 256>();
+  return go.template pair<MODE>();
 }
 template <class Go>
 cudaError_t choose(const Product& p, Go&& go) {
@@ -632,21 +837,32 @@ struct Launch {
   int sms;
   void* workspace;
   cudaStream_t s;
-  template <int MODE, bool SWAP, int BN>
-  cudaError_t run() const {
-    return launch_tile<MODE, SWAP, BN>(p, sms, workspace, s);
+  template <int MODE, int BN>
+  cudaError_t narrow() const {
+    return launch_narrow<MODE, BN>(p, sms, workspace, s);
+  }
+  template <int MODE>
+  cudaError_t pair() const {
+    return launch_pair<MODE>(p, workspace, s);
   }
 };
 struct Size {
   const Product& p;
   int sms;
   size_t* bytes;
-  template <int MODE, bool SWAP, int BN>
-  cudaError_t run() const {
-    Plan g;
-    const cudaError_t e = plan_tile<MODE, SWAP, BN>(p, sms, &g);
+  cudaError_t take(cudaError_t e, const Plan& g) const {
     *bytes = e == cudaSuccess ? g.bytes : 0;
     return e;
+  }
+  template <int MODE, int BN>
+  cudaError_t narrow() const {
+    Plan g = {};
+    return take(plan_narrow<MODE, BN>(p, sms, &g), g);
+  }
+  template <int MODE>
+  cudaError_t pair() const {
+    Plan g = {};
+    return take(plan_pair<MODE>(p, &g), g);
   }
 };
 

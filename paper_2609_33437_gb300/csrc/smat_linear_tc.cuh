@@ -84,10 +84,10 @@ __device__ __forceinline__ uint64_t descriptor(uint32_t address) {
 template <bool MN>
 constexpr uint64_t kStep16 = (MN ? 2048 : 32) >> 4;
 
-// kind::f16: fp32 sums of bf16 products, 128 x n
-template <bool A_MN, bool B_MN, int N>
+// kind::f16: fp32 sums of bf16 products, M x N
+template <bool A_MN, bool B_MN, int N, int M = kBM>
 constexpr uint32_t kInstruction = 1u << 4 | 1u << 7 | 1u << 10 | (uint32_t)A_MN << 15 | (uint32_t)B_MN << 16 |
-                                  (uint32_t)(N >> 3) << 17 | (uint32_t)(kBM >> 4) << 24;
+                                  (uint32_t)(N >> 3) << 17 | (uint32_t)(M >> 4) << 24;
 
 __device__ __forceinline__ void mma(uint32_t sums, uint64_t a, uint64_t b, uint32_t instruction, bool add) {
   asm volatile(
@@ -98,6 +98,38 @@ __device__ __forceinline__ void mma(uint32_t sums, uint64_t a, uint64_t b, uint3
 __device__ __forceinline__ void mma_commit(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
+
+// The same for a pair of CTAs (cta_group::2): copies signal a barrier of either CTA (its address across the cluster), one
+// thread of the first CTA multiplies from both CTAs' shared memory into both's tensor memory, and what it commits to is a
+// barrier of each CTA in `mask`.
+__device__ __forceinline__ uint32_t cluster_address_of(uint32_t shared, uint32_t rank) {
+  uint32_t a;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(shared), "r"(rank));
+  return a;
+}
+__device__ __forceinline__ void bar_arrive_there(uint32_t bar) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void tma_load_pair(uint32_t to, const CUtensorMap* map, int x, int y, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], "
+      "[%2];" ::"r"(to),
+      "l"(map), "r"(bar), "r"(x), "r"(y)
+      : "memory");
+}
+__device__ __forceinline__ void mma_pair(uint32_t sums, uint64_t a, uint64_t b, uint32_t instruction, bool add) {
+  asm volatile(
+      "{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\ntcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(sums),
+      "l"(a), "l"(b), "r"(instruction), "r"((uint32_t)add)
+      : "memory");
+}
+__device__ __forceinline__ void mma_commit_pair(uint32_t bar, uint16_t mask) {
+  asm volatile(
+      "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
+      "h"(mask)
+      : "memory");
+}
+
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 
@@ -154,14 +186,14 @@ __device__ __forceinline__ void add_parts(uint32_t shares, float (&v)[N], Load&&
   }
 }
 
-// The tiles' order: strips of 16 tiles of rows, down a strip's rows first, so that the tiles in work at one time
+// The tiles' order: strips of STRIP tiles of rows, down a strip's rows first, so that the tiles in work at one time
 // share rows and columns of the operands in L2.
+template <int64_t STRIP>
 __device__ __forceinline__ void tile_place(int64_t tiles_r, int64_t tiles_c, int64_t tile, int64_t& r, int64_t& c) {
-  constexpr int64_t kStrip = 16;
-  const int64_t per = kStrip * tiles_c, strip = tile / per, in = tile - strip * per;
-  const int64_t high = tiles_r - strip * kStrip < kStrip ? tiles_r - strip * kStrip : kStrip;
+  const int64_t per = STRIP * tiles_c, strip = tile / per, in = tile - strip * per;
+  const int64_t high = tiles_r - strip * STRIP < STRIP ? tiles_r - strip * STRIP : STRIP;
   c = in / high;
-  r = strip * kStrip + in - c * high;
+  r = strip * STRIP + in - c * high;
 }
 
 // ---- host side ----
