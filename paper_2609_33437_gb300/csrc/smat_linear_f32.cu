@@ -621,7 +621,7 @@ cudaError_t plan_tc(const Product& p, int sms, Plan* plan) {
   const int64_t tiles = g.tiles_r * g.tiles_c;
   int shares = 8;
   while (shares > 1 && (tiles * shares > sms || g.slices < 3 * shares ||
-                        tiles > clusters_at_once(f, shares, kTcBytes, clusters)))
+                        tiles > clusters_at_once(f, shares, kThreads, kTcBytes, clusters)))
     --shares;
   g.share = (g.slices + shares - 1) / shares;
   g.shares = shares > 1 ? (g.slices + g.share - 1) / g.share : 1;

@@ -1,7 +1,7 @@
 // The linear layers' products of bf16 matrices on the tensor cores (tcgen05; smat_linear.h, Product).
 //
 // In every CTA one warp fetches 64-deep slices of both operands by TMA into a ring of 128-byte-swizzled buffers, one
-// thread multiplies them into tensor memory (fp32), and eight warps take finished sums out of it, 32 columns at a time,
+// thread multiplies them into tensor memory (fp32), and further warps take finished sums out of it, 32 columns at a time,
 // and finish them (bias, activation, 8-bit form, residual, slope, older gradient) while the next tile's sums are made in
 // the other half of tensor memory.
 //
@@ -9,9 +9,10 @@
 // fetches its rows of one operand and half of the other, which the pair's multiplications read from both: 32 KB a slice
 // and CTA for 256 columns, where a CTA by itself needs 48 KB and the copies bound it (8192 x 11008 x 4096: 484 us).
 // `width` and the shares of the sum are chosen by an estimate of the time, see plan_pair. The tile's rows are rows i of
-// the result. A thread holds 32 columns of a row, whole groups of the 8-bit form, and reads and writes 64 bytes of a row
-// at a time; results whose rows do not start on 16 bytes take a turn through shared memory, to 32 neighbouring columns
-// per warp.
+// the result. A thread holds 32 columns of a row, whole groups of the 8-bit form; 32 columns of a warp's 32 rows leave
+// through shared memory by TMA, and what is added to them comes in that way (stores of 32 bytes a row and lane bound the
+// kernel by their number: 2056 x 64 x 4096 took 10 us, and more the more warps stored). Results whose rows do not start
+// on 16 bytes take a turn through shared memory, to 32 neighbouring columns per warp.
 //
 // Products of at most 128 rows (narrow_kernel): the tile's 128 rows are columns j and its 32, 64 or 128 columns are rows
 // i, so that a wide weight fills the 128 and the few rows cost a narrow tile. A warp holds 32 neighbouring columns of a
@@ -32,8 +33,6 @@ __device__ int g_errors;  // bit 0: a wait inside a product ran out of time
 namespace {
 
 constexpr int kBytesA = kBM * kBK * 2;
-constexpr int kTurn = 32 * 33 * 4;  // a warp's 32 x 32 sums, turned
-
 // Narrow tiles are bound by the weight's bytes: two CTAs per SM, so that one's start and end lie beside the other's
 // copies.
 template <int BN>
@@ -45,8 +44,14 @@ struct Ring {
   static constexpr int kCtas = 2;  // per SM
 };
 
-constexpr int kPairRows = 2 * kBM, kPairStages = 6, kPairStage = 2 * kBytesA;
-constexpr int kPairBytes = kPairStages * kPairStage + kEpiWarps * kTurn + 1024;
+constexpr int kPairRows = 2 * kBM, kPairStages = 5, kPairStage = 2 * kBytesA;
+constexpr int kPairEpi = 12;  // warps that finish a pair's sums
+constexpr int kPairThreads = 32 * (kPairEpi + 2);
+// A finishing warp's own shared memory: 32 rows of 32 results (64 bytes, swizzled) and of 32 q (32 bytes, swizzled). Rows
+// that are not copied by TMA are turned there, 16 at a time, 33 floats apart.
+constexpr int kDeskRows = 32 * 64, kDeskQ = 32 * 32, kDesk = kDeskRows + kDeskQ;
+static_assert(16 * 33 * 4 <= kDesk, "");
+constexpr int kPairBytes = kPairStages * kPairStage + kPairEpi * kDesk + 1024;
 constexpr int kSums = 256;  // columns of tensor memory for one tile's sums
 
 struct Args {
@@ -57,8 +62,8 @@ struct Args {
   int width;                        // columns of a pair's tile
   float* parts;                     // the shares' sums, or NULL
   int* errors;                      // device error bits
-  bool by_rows;                     // rows of out and residual start on 16 bytes, those of q on 8
-  bool full_sectors;                // rows of out, residual and q start on 32 bytes
+  bool by_rows;                     // rows of out and residual start on 16 bytes, those of q on 8: copied by TMA
+  bool q_by_rows;                   // those of q on 16: by TMA too
   bool wide_bias;                   // bias on 16 bytes
 };
 
@@ -71,83 +76,70 @@ __device__ __forceinline__ void unpack_words(const uint32_t* w, int words, float
     v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
   }
 }
-// 32 bytes of a row: one access to a whole sector, or two of 16 bytes, or (q) four of 8
-template <int LEAST>
-__device__ __forceinline__ void load_words8(const void* p, bool sectors, uint32_t* w) {
-  if (sectors) {
-    asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
-                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
-                 : "l"(p));
-  } else if (LEAST == 16) {
+// 32 q of a row that starts on 8 bytes
+__device__ __forceinline__ void load_q32(const int8_t* p, uint32_t* w) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
-      asm volatile("ld.global.v4.b32 {%0,%1,%2,%3}, [%4];"
-                   : "=r"(w[4 * h]), "=r"(w[4 * h + 1]), "=r"(w[4 * h + 2]), "=r"(w[4 * h + 3])
-                   : "l"((const char*)p + 16 * h));
-  } else {
-#pragma unroll
-    for (int h = 0; h < 4; ++h)
-      asm volatile("ld.global.v2.b32 {%0,%1}, [%2];"
-                   : "=r"(w[2 * h]), "=r"(w[2 * h + 1])
-                   : "l"((const char*)p + 8 * h));
-  }
+  for (int h = 0; h < 4; ++h)
+    asm volatile("ld.global.v2.b32 {%0,%1}, [%2];" : "=r"(w[2 * h]), "=r"(w[2 * h + 1]) : "l"(p + 8 * h));
 }
-template <int LEAST>
-__device__ __forceinline__ void store_words8(void* p, bool sectors, const uint32_t* w) {
-  if (sectors) {
-    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]),
-                 "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
-                 : "memory");
-  } else if (LEAST == 16) {
+__device__ __forceinline__ void store_q32(int8_t* p, const uint32_t* w) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
-      asm volatile("st.global.v4.b32 [%0], {%1,%2,%3,%4};" ::"l"((char*)p + 16 * h), "r"(w[4 * h]), "r"(w[4 * h + 1]),
-                   "r"(w[4 * h + 2]), "r"(w[4 * h + 3])
-                   : "memory");
-  } else {
-#pragma unroll
-    for (int h = 0; h < 4; ++h)
-      asm volatile("st.global.v2.b32 [%0], {%1,%2};" ::"l"((char*)p + 8 * h), "r"(w[2 * h]), "r"(w[2 * h + 1])
-                   : "memory");
-  }
+  for (int h = 0; h < 4; ++h)
+    asm volatile("st.global.v2.b32 [%0], {%1,%2};" ::"l"(p + 8 * h), "r"(w[2 * h]), "r"(w[2 * h + 1]) : "memory");
 }
 
-// What finishing 32 columns of a row reads, asked for before the sums are there: the residual, the older gradient or
-// q, and e.
-struct Beside {
-  uint32_t w[16];
-  uint32_t e;
+// A warp's desk: where its 32 rows of 32 columns wait for TMA, and come from it. 16 bytes of a row lie at a place that
+// changes with the row, as the copies' swizzle has it, so that 8 rows' accesses meet in no bank.
+struct Desk {
+  uint32_t rows, q, bar;  // shared addresses; a barrier for copies in
+  uint32_t phase;
+  __device__ __forceinline__ uint32_t row_at(int lane, int chunk) const {
+    return rows + lane * 64 + ((chunk ^ (lane >> 1 & 3)) << 4);
+  }
+  __device__ __forceinline__ uint32_t q_at(int lane, int chunk) const {
+    return q + lane * 32 + ((chunk ^ (lane >> 2 & 1)) << 4);
+  }
 };
-
-template <int MODE>
-__device__ __forceinline__ void ask_row(const Args& a, int64_t i, int64_t j, Beside& in) {
-  const Product& p = a.p;
-  if (i >= p.I) return;
-  if (MODE == kGradInput) {
-    if (p.act == SMAT_ACT_NONE) return;
-    load_words8<8>(p.q + i * p.ldq + j, a.full_sectors, in.w);
-    in.e = p.e[i * p.lde + j / kGroup];
-    return;
-  }
-  const bf16* from = MODE == kForward ? (const bf16*)p.residual + i * p.ldr + j
-                                      : (const bf16*)p.out + i * p.ldo + j;
-  if (MODE == kForward ? p.residual != nullptr : p.accumulate != 0) {
-    load_words8<16>(from, a.full_sectors, in.w);
-    load_words8<16>(from + 16, a.full_sectors, in.w + 8);
-  }
+__device__ __forceinline__ uint4 desk_load(uint32_t at) {
+  uint4 u;
+  asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w) : "r"(at) : "memory");
+  return u;
+}
+__device__ __forceinline__ void desk_store(uint32_t at, const uint32_t* w) {
+  asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
 }
 
-// 32 columns j .. j + 31 of row i, one thread: whole sectors in and out. Returns the saved group's e.
-template <int MODE>
-__device__ __forceinline__ uint32_t finish_row(const Args& a, int64_t i, int64_t j, float (&v)[32], const Beside& in) {
+// Columns j .. j + 31 of rows i .. i + 31, a row per lane, out by TMA (which leaves out what lies outside the result).
+// sums(v): their sums.
+template <int MODE, class Sums>
+__device__ __forceinline__ void finish_block(const Args& a, const CUtensorMap* map_out, const CUtensorMap* map_in,
+                                            const CUtensorMap* map_q, int64_t i, int64_t j, Desk& desk,
+                                            volatile int* dead, Sums&& sums) {
   const Product& p = a.p;
-  bf16* out = (bf16*)p.out + i * p.ldo + j;
-  const bool there = i < p.I;
-  uint32_t ex = 0;
+  const int lane = threadIdx.x % 32;
+  const bool there = i + lane < p.I;
+  const bool slope = MODE == kGradInput && p.act != SMAT_ACT_NONE;
+  const bool add = MODE == kForward ? p.residual != nullptr : MODE == kGradWeight && p.accumulate;
+  const bool save = MODE == kForward && p.q;
+  if (lane == 0) {
+    asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");  // the last unit has left the desk
+    if (add || (slope && a.q_by_rows)) {
+      bar_expect(desk.bar, add ? kDeskRows : kDeskQ);
+      if (add)
+        tma_load(desk.rows, map_in, (int)j, (int)i, desk.bar);
+      else
+        tma_load(desk.q, map_q, (int)j, (int)i, desk.bar);
+    }
+  }
+  uint32_t e = 1;
+  if (slope && there) e = p.e[(i + lane) * p.lde + j / kGroup];
+  __syncwarp();
+  float v[32];
+  sums(v);
   if (MODE == kForward) {
     if (p.bias) {
       const bf16* b = (const bf16*)p.bias + j;
-      if (a.wide_bias) {
+      if (a.wide_bias && j + 32 <= p.J) {
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
           const uint4 u = __ldg(reinterpret_cast<const uint4*>(b) + t);
@@ -159,45 +151,88 @@ __device__ __forceinline__ uint32_t finish_row(const Args& a, int64_t i, int64_t
         }
       } else {
 #pragma unroll
-        for (int t = 0; t < 32; ++t) v[t] += to_float(b[t]);
+        for (int t = 0; t < 32; ++t)
+          if (j + t < p.J) v[t] += to_float(b[t]);
       }
     }
-    if (p.q) {
-      float big = 0.0f;
+    if (save) {
+      float big[8];  // a tree: one chain of 32 would wait for each step
 #pragma unroll
-      for (int t = 0; t < 32; ++t) big = larger(big, v[t]);
-      ex = pack_exponent(__float_as_uint(big));
+      for (int t = 0; t < 8; ++t) big[t] = larger(larger(v[t], v[t + 8]), larger(v[t + 16], v[t + 24]));
+#pragma unroll
+      for (int t = 4; t > 0; t /= 2)
+#pragma unroll
+        for (int u = 0; u < t; ++u) big[u] = larger(big[u], big[u + t]);
+      const uint32_t ex = pack_exponent(__float_as_uint(big[0]));
       uint32_t w[8];
       pack_words<8>(v, ex, w);
-      if (there) store_words8<8>(p.q + i * p.ldq + j, a.full_sectors, w);
+      if (a.q_by_rows) {
+        desk_store(desk.q_at(lane, 0), w);
+        desk_store(desk.q_at(lane, 1), w + 4);
+      } else if (there && j + 32 <= p.J) {
+        store_q32(p.q + (i + lane) * p.ldq + j, w);
+      } else if (there) {
+#pragma unroll
+        for (int t = 0; t < 32; ++t)
+          if (j + t < p.J) p.q[(i + lane) * p.ldq + j + t] = (int8_t)(w[t / 4] >> (8 * (t % 4)));
+      }
+      if (there && j < p.J) p.e[(i + lane) * p.lde + j / kGroup] = (uint8_t)ex;
     }
     SMAT_WITH_ACT(p.act, _Pragma("unroll") for (int t = 0; t < 32; ++t) v[t] = act_value<ACT>(v[t]))
   }
-  if (MODE == kGradInput) {
-    if (p.act != SMAT_ACT_NONE) {
-      float h[32];
-      unpack_words8<8>(in.w, in.e, h);
-      SMAT_WITH_ACT(p.act, _Pragma("unroll") for (int t = 0; t < 32; ++t) v[t] *= act_slope<ACT>(h[t]))
-    }
-  } else if (MODE == kForward ? p.residual != nullptr : p.accumulate != 0) {
-    float f[32];
-    unpack_words(in.w, 16, f);
-#pragma unroll
-    for (int t = 0; t < 32; ++t) v[t] += f[t];
+  if (add || (slope && a.q_by_rows)) {
+    if (!bar_wait(desk.bar, desk.phase & 1, dead, a.errors)) return;
+    ++desk.phase;
   }
-  if (there) {
+  if (slope) {
+    uint32_t w[8];
+    if (a.q_by_rows) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      uint32_t w[8];
-#pragma unroll
-      for (int t = 0; t < 8; ++t) {
-        const __nv_bfloat162 b = __floats2bfloat162_rn(v[16 * h + 2 * t], v[16 * h + 2 * t + 1]);
-        w[t] = *reinterpret_cast<const uint32_t*>(&b);
+      for (int t = 0; t < 2; ++t) {
+        const uint4 u = desk_load(desk.q_at(lane, t));
+        w[4 * t] = u.x, w[4 * t + 1] = u.y, w[4 * t + 2] = u.z, w[4 * t + 3] = u.w;
       }
-      store_words8<16>(out + 16 * h, a.full_sectors, w);
+    } else if (there && j + 32 <= p.J) {
+      load_q32(p.q + (i + lane) * p.ldq + j, w);
+    } else {
+#pragma unroll
+      for (int t = 0; t < 8; ++t) w[t] = 0;
+      if (there) {
+#pragma unroll
+        for (int t = 0; t < 32; ++t)
+          if (j + t < p.J) w[t / 4] |= (uint32_t)(uint8_t)p.q[(i + lane) * p.ldq + j + t] << (8 * (t % 4));
+      }
     }
+    float x[32];
+    unpack_words8<8>(w, e, x);
+    SMAT_WITH_ACT(p.act, _Pragma("unroll") for (int t = 0; t < 32; ++t) v[t] *= act_slope<ACT>(x[t]))
   }
-  return ex;
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    const uint32_t at = desk.row_at(lane, c);
+    if (add) {
+      const uint4 u = desk_load(at);
+      const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+      float f[8];
+      unpack_words(w, 4, f);
+#pragma unroll
+      for (int t = 0; t < 8; ++t) v[8 * c + t] += f[t];
+    }
+    uint32_t w[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const __nv_bfloat162 b = __floats2bfloat162_rn(v[8 * c + 2 * t], v[8 * c + 2 * t + 1]);
+      w[t] = *reinterpret_cast<const uint32_t*>(&b);
+    }
+    desk_store(at, w);
+  }
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  __syncwarp();
+  if (lane == 0) {
+    tma_store(map_out, desk.rows, (int)j, (int)i);
+    if (save && a.q_by_rows) tma_store(map_q, desk.q, (int)j, (int)i);
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+  }
 }
 
 // Column j of rows i .. i + N - 1, one thread; the warp holds 32 neighbouring columns from a multiple of 32 on. What
@@ -267,39 +302,36 @@ __device__ __forceinline__ void finish_column(const Args& a, int64_t i, int64_t 
 // Blocks `first`, `first + step`, ... below `end` of 32 columns of a tile that begins at row row0 (this warp's 32) and
 // column col0 of the result: `sums(c, v)` gives block c's sums.
 template <int MODE, class Sums>
-__device__ __forceinline__ void finish_rows(const Args& a, int64_t row0, int64_t col0, int first, int end, int step,
-                                            float* turn, Sums&& sums) {
+__device__ __forceinline__ void finish_blocks(const Args& a, const CUtensorMap* map_out, const CUtensorMap* map_in,
+                                              const CUtensorMap* map_q, int64_t row0, int64_t col0, int first, int end,
+                                              int step, Desk& desk, float* turn, volatile int* dead, Sums&& sums) {
   const int lane = threadIdx.x % 32;
-  if (first >= end) return;
-  Beside in;
-  if (a.by_rows && col0 + 32 * first + 32 <= a.p.J) ask_row<MODE>(a, row0 + lane, col0 + 32 * first, in);
+#pragma unroll 1
   for (int c = first; c < end; c += step) {
     const int64_t col = col0 + 32 * c;
-    float v[32];
-    sums(c, v);
-    if (a.by_rows && col + 32 <= a.p.J) {
-      const Beside now = in;
-      if (c + step < end && col + 32 * step + 32 <= a.p.J) ask_row<MODE>(a, row0 + lane, col + 32 * step, in);
-      const uint32_t ex = finish_row<MODE>(a, row0 + lane, col, v, now);
-      if (MODE == kForward && a.p.q && row0 + lane < a.p.I)
-        a.p.e[(row0 + lane) * a.p.lde + col / kGroup] = (uint8_t)ex;
+    if (a.by_rows && row0 < a.p.I && col < a.p.J) {
+      finish_block<MODE>(a, map_out, map_in, map_q, row0, col, desk, dead, [&](float(&v)[32]) { sums(c, v); });
       continue;
     }
+    float v[32];
+    sums(c, v);
     if (row0 >= a.p.I || col >= a.p.J) continue;
-    __syncwarp();
 #pragma unroll
-    for (int t = 0; t < 32; ++t) turn[lane * 33 + t] = v[t];
-    __syncwarp();
+    for (int h = 0; h < 2; ++h) {  // 16 rows at a time
+      __syncwarp();
+      if (lane / 16 == h) {
 #pragma unroll
-    for (int t = 0; t < 32; ++t) v[t] = turn[t * 33 + lane];
-    finish_column<MODE, 32>(a, row0, col + lane, v);
+        for (int t = 0; t < 32; ++t) turn[lane % 16 * 33 + t] = v[t];
+      }
+      __syncwarp();
+      float x[16];
+#pragma unroll
+      for (int t = 0; t < 16; ++t) x[t] = turn[t * 33 + lane];
+      finish_column<MODE, 16>(a, row0 + 16 * h, col + lane, x);
+    }
   }
 }
 
-// A CTA's share of a tile's sums lies as [column][128 rows], so that a warp's 32 rows of a column are 128 bytes in a
-// row: in the workspace (a.parts), or, where the tile has no more than 8 columns, in its own shared memory, which the
-// others read across the cluster. (Reading larger tiles there is slow: 128 x 256 sums of 8 shares took 15 us, through
-// the workspace, which stays in L2, 3.) 
 template <int MODE, int BN>
 __global__ void __launch_bounds__(kThreads, Ring<BN>::kCtas)
     narrow_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
@@ -485,14 +517,15 @@ __global__ void __launch_bounds__(kThreads, Ring<BN>::kCtas)
 
 // A pair's tile: see the head of this file. The pair's first CTA ("leader") multiplies for both.
 template <int MODE>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(kPairThreads, 1)
     pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
-                const __grid_constant__ Args a) {
+                const __grid_constant__ CUtensorMap map_out, const __grid_constant__ CUtensorMap map_in,
+                const __grid_constant__ CUtensorMap map_q, const __grid_constant__ Args a) {
   constexpr bool A_MN = MODE == kGradWeight, B_MN = MODE != kForward;
   constexpr int kStages = kPairStages, kStage = kPairStage;
 
   extern __shared__ uint8_t raw[];
-  __shared__ __align__(8) uint64_t bars[2 * kStages + 5];
+  __shared__ __align__(8) uint64_t bars[2 * kStages + 5 + kPairEpi];
   __shared__ uint32_t tmem_at;
   __shared__ int dead_flag;
   uint8_t* ring = raw + ((1024 - (smem_address(raw) & 1023)) & 1023);
@@ -500,7 +533,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const uint32_t full = smem_address(bars), empty = full + 8 * kStages, sums_full = empty + 8 * kStages,
                  sums_empty = sums_full + 16, drained = sums_empty + 16;
-  float* turn = reinterpret_cast<float*>(ring + kStages * kStage + warp * kTurn);
+  uint8_t* own = ring + kStages * kStage + warp * kDesk;  // a finishing warp's desk
+  Desk desk = {smem_address(own), smem_address(own) + kDeskRows, drained + 8 + 8 * (uint32_t)warp, 0};
 
   uint32_t ctas, rank;
   asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(ctas));
@@ -511,21 +545,22 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int64_t first_tile = blockIdx.x / ctas, step = gridDim.x / ctas;
   const int half_width = a.width / 2;
 
-  if (warp == kTmaWarp && lane == 0) {
+  if (warp == kPairEpi && lane == 0) {
     dead_flag = 0;
     for (int s = 0; s < kStages; ++s) {
       bar_init(full + 8 * s, 1);
       bar_init(empty + 8 * s, 1);
     }
     bar_init(drained, 1);
+    for (int w = 0; w < kPairEpi; ++w) bar_init(drained + 8 + 8 * w, 1);
     for (int b = 0; b < 2; ++b) {
       bar_init(sums_full + 8 * b, 1);
-      bar_init(sums_empty + 8 * b, 2 * kEpiWarps);
+      bar_init(sums_empty + 8 * b, 2 * kPairEpi);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   __syncwarp();
-  if (warp == kMmaWarp) {
+  if (warp == kPairEpi + 1) {
     asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_address(&tmem_at)),
                  "r"(2 * kSums)
                  : "memory");
@@ -537,7 +572,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   fence_after();
   const uint32_t tmem = tmem_at;
 
-  if (warp == kTmaWarp && lane == 0) {
+  if (warp == kPairEpi && lane == 0) {
     const int blocks_b = B_MN ? (half_width + 63) / 64 : 1;  // copies of this CTA's half of the other operand
     const uint32_t bytes = kBytesA + (B_MN ? blocks_b * 8192 : half_width * kBK * 2);
     const uint32_t full_there = cluster_address_of(full, leader);
@@ -573,7 +608,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int i = 0; i < (1 << 20) && !bar_try(full + 8 * (last % kStages), last / kStages & 1); ++i) {
         }
       }
-  } else if (warp == kMmaWarp && lane == 0 && member == 0) {
+  } else if (warp == kPairEpi + 1 && lane == 0 && member == 0) {
     const uint32_t inst = kInstruction<A_MN, B_MN, 0, kPairRows> | (uint32_t)(a.width >> 3) << 17;
     const uint16_t both = (uint16_t)(3u << rank);
     uint32_t n = 0, made = 0;
@@ -602,11 +637,12 @@ __global__ void __launch_bounds__(kThreads, 1)
       for (int i = 0; i < (1 << 20) && !bar_try(drained, 0); ++i) {
       }
     }
-  } else if (warp < kEpiWarps) {
+  } else if (warp < kPairEpi) {
     const int quarter = warp % 4;  // the 32 rows of tensor memory that this warp may read
     const uint32_t sums_empty_there = cluster_address_of(sums_empty, leader);
-    // this warp's blocks of 32 columns: the first or the second half of the tile's
-    const int blocks = a.width / 32, first = warp / 4 ? (blocks + 1) / 2 : 0, end = warp / 4 ? blocks : (blocks + 1) / 2;
+    // this warp's blocks of 32 columns
+    constexpr int kBeside = kPairEpi / 4;  // warps that share 32 rows
+    const int blocks = a.width / 32, first = warp / 4 * blocks / kBeside, end = (warp / 4 + 1) * blocks / kBeside;
     uint32_t made = 0;
     for (int64_t tile = first_tile; tile < a.tiles; tile += step, ++made) {
       int64_t tr, tc;
@@ -615,6 +651,11 @@ __global__ void __launch_bounds__(kThreads, 1)
       const uint32_t half = made & 1, sums = tmem + half * kSums + ((uint32_t)(32 * quarter) << 16);
       if (!bar_wait(sums_full + 8 * half, made / 2 & 1, dead, a.errors)) break;
       fence_after();
+      auto release = [&] {  // this warp has what it needs of these sums
+        fence_before();
+        __syncwarp();
+        if (lane == 0) bar_arrive_there(sums_empty_there + 8 * half);
+      };
       auto take = [&](int c, float(&v)[32]) {
         if (slices > 0) {
           take32(sums + 32 * c, v);
@@ -622,14 +663,11 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
           for (int t = 0; t < 32; ++t) v[t] = 0.0f;
         }
-        if (c + 1 == end) {  // this warp has what it needs of these sums
-          fence_before();
-          __syncwarp();
-          if (lane == 0) bar_arrive_there(sums_empty_there + 8 * half);
-        }
+        if (c + 1 == end) release();
       };
+      if (first == end) release();  // none of a narrow tile's columns
       if (shares == 1) {
-        finish_rows<MODE>(a, r0, c0, first, end, 1, turn, take);
+        finish_blocks<MODE>(a, &map_out, &map_in, &map_q, r0, c0, first, end, 1, desk, (float*)own, dead, take);
       } else {
         float* part = a.parts + ((size_t)first_tile * ctas + rank) * a.width * kBM + 32 * quarter + lane;
         for (int c = first; c < end; ++c) {
@@ -645,7 +683,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     // one tile per cluster: its CTAs add up and finish blocks of their rows' columns in turn
     __syncthreads();
     cluster_sync();
-    if (warp < kEpiWarps && !*dead) {
+    if (warp < kPairEpi && !*dead) {
       int64_t tr, tc;
       tile_place<8>(a.tiles_r, a.tiles_c, first_tile, tr, tc);
       const int quarter = warp % 4;
@@ -653,28 +691,36 @@ __global__ void __launch_bounds__(kThreads, 1)
       const float* part = a.parts + ((size_t)first_tile * ctas + member) * a.width * kBM + 32 * quarter + lane;
       const size_t apart = (size_t)2 * a.width * kBM;
       const int blocks = r0 < a.p.I ? (int)((min((int64_t)a.width, a.p.J - c0) + 31) / 32) : 0;
-      finish_rows<MODE>(a, r0, c0, (int)share + (int)shares * (warp / 4), blocks, (int)shares * (kEpiWarps / 4), turn,
-                        [&](int c, float(&v)[32]) {
-                          add_parts(shares, v, [&](uint32_t s, int t) { return __ldcg(part + s * apart + (32 * c + t) * kBM); });
-                        });
+      finish_blocks<MODE>(a, &map_out, &map_in, &map_q, r0, c0, (int)share + (int)shares * (warp / 4), blocks,
+                          (int)shares * (kPairEpi / 4), desk, (float*)own, dead, [&](int c, float(&v)[32]) {
+                           add_parts(shares, v, [&](uint32_t s, int t) { return __ldcg(part + s * apart + (32 * c + t) * kBM); });
+                         });
     }
   }
+  if (warp < kPairEpi && lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");  // the desk has been read
+  __syncwarp();
   fence_before();
   __syncthreads();
-  cluster_sync();  // the partner's multiplications read this CTA's shared memory, and its arrivals write it
-  if (warp == kMmaWarp)
+  cluster_meet();  // the partner's multiplications read this CTA's shared memory, and its arrivals write it
+  if (warp == kPairEpi + 1)
     asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2 * kSums));
 }
 
-// A row-major bf16 matrix [outer, inner] in boxes of 64 x `box`; what lies outside reads as 0.
-bool encode(CUtensorMap* map, const void* p, int64_t inner, int64_t outer, int64_t ld, int box) {
+// A row-major matrix [outer, inner] of bf16 or bytes in boxes of `wide` x `high`, swizzled over a box's row; what lies
+// outside reads as 0.
+bool encode(CUtensorMap* map, const void* p, int64_t inner, int64_t outer, int64_t ld, int high, int wide = 64,
+            bool bytes = false) {
   const cuuint64_t dims[2] = {(cuuint64_t)inner, (cuuint64_t)outer};
-  const cuuint64_t strides[1] = {(cuuint64_t)ld * 2};
-  const cuuint32_t boxes[2] = {64, (cuuint32_t)box}, ones[2] = {1, 1};
+  const cuuint64_t strides[1] = {(cuuint64_t)ld * (bytes ? 1 : 2)};
+  const cuuint32_t boxes[2] = {(cuuint32_t)wide, (cuuint32_t)high}, ones[2] = {1, 1};
+  const int row = wide * (bytes ? 1 : 2);
   const Encode f = encoder();
-  return f && f(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(p), dims, strides, boxes, ones,
-                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  return f && f(map, bytes ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(p),
+                dims, strides, boxes, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                row == 128  ? CU_TENSOR_MAP_SWIZZLE_128B
+                : row == 64 ? CU_TENSOR_MAP_SWIZZLE_64B
+                            : CU_TENSOR_MAP_SWIZZLE_32B,
+                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 // One product's launch: tiles, shares of the sum, workspace.
@@ -724,7 +770,7 @@ cudaError_t plan_pair(const Product& p, Plan* plan) {
   for (int width = 256; width >= 64; width -= 32) {
     const int64_t tiles_c = (p.J + width - 1) / width, tiles = tiles_r * tiles_c;
     for (int shares = 1; shares <= 4; ++shares) {
-      const int64_t at_once = clusters_at_once(f, 2 * shares, kPairBytes, clusters);
+      const int64_t at_once = clusters_at_once(f, 2 * shares, kPairThreads, kPairBytes, clusters);
       if (shares > 1 && (tiles > at_once || slices < 3 * shares)) break;
       const int share = (slices + shares - 1) / shares;
       const double rounds = (double)((tiles + at_once - 1) / at_once);
@@ -760,19 +806,17 @@ cudaError_t fill_args(const Product& p, const Plan& g, void* workspace, Args* ar
   };
   a.by_rows = rows_on(p.out, p.ldo, 2, 16) && (!p.residual || rows_on(p.residual, p.ldr, 2, 16)) &&
               (!p.q || rows_on(p.q, p.ldq, 1, 8));
-  a.full_sectors = rows_on(p.out, p.ldo, 2, 32) && (!p.residual || rows_on(p.residual, p.ldr, 2, 32)) &&
-                   (!p.q || rows_on(p.q, p.ldq, 1, 32));
+  a.q_by_rows = p.q && rows_on(p.q, p.ldq, 1, 16);
   a.wide_bias = (uintptr_t)p.bias % 16 == 0;
   *args = a;
   return e;
 }
 
-template <class F>
-cudaError_t launch(F* f, int64_t ctas, int cluster, int bytes, const CUtensorMap& ma, const CUtensorMap& mb, const Args& a,
-                   cudaStream_t s) {
+template <class F, class... A>
+cudaError_t launch(F* f, int64_t ctas, int cluster, int threads, int bytes, cudaStream_t s, const A&... args) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)ctas);
-  cfg.blockDim = dim3(kThreads);
+  cfg.blockDim = dim3(threads);
   cfg.dynamicSmemBytes = bytes;
   cfg.stream = s;
   cudaLaunchAttribute at[1];
@@ -780,7 +824,7 @@ cudaError_t launch(F* f, int64_t ctas, int cluster, int bytes, const CUtensorMap
   at[0].val.clusterDim = {(unsigned)cluster, 1, 1};
   cfg.attrs = at;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, f, ma, mb, a);
+  return cudaLaunchKernelEx(&cfg, f, args...);
 }
 
 template <int MODE, int BN>
@@ -795,7 +839,7 @@ cudaError_t launch_narrow(const Product& p, int sms, void* workspace, cudaStream
       !((MODE == kGradInput ? encode(&ma, p.b, p.J, p.L, p.ldb, kBK) : encode(&ma, p.b, p.L, p.J, p.ldb, kBM)) &&
         encode(&mb, p.a, p.L, p.I, p.lda, BN)))
     return cudaErrorNotSupported;
-  return launch(narrow_kernel<MODE, BN>, g.ctas, g.shares, Ring<BN>::kBytes, ma, mb, a, s);
+  return launch(narrow_kernel<MODE, BN>, g.ctas, g.shares, kThreads, Ring<BN>::kBytes, s, ma, mb, a);
 }
 
 template <int MODE>
@@ -810,7 +854,14 @@ cudaError_t launch_pair(const Product& p, void* workspace, cudaStream_t s) {
   if (p.L > 0 && !((A_MN ? encode(&ma, p.a, p.I, p.L, p.lda, kBK) : encode(&ma, p.a, p.L, p.I, p.lda, kBM)) &&
                    (B_MN ? encode(&mb, p.b, p.J, p.L, p.ldb, kBK) : encode(&mb, p.b, p.L, p.J, p.ldb, g.width / 2))))
     return cudaErrorNotSupported;
-  return launch(pair_kernel<MODE>, g.ctas, 2 * g.shares, kPairBytes, ma, mb, a, s);
+  // the results' rows, what is added to them, and q: those that are copied by TMA
+  CUtensorMap mo = {}, mi = {}, mq = {};
+  const void* in = MODE == kForward ? p.residual : MODE == kGradWeight && p.accumulate ? p.out : nullptr;
+  if (a.by_rows && !(encode(&mo, p.out, p.J, p.I, p.ldo, 32, 32) &&
+                     (!in || encode(&mi, in, p.J, p.I, MODE == kForward ? p.ldr : p.ldo, 32, 32)) &&
+                     (!a.q_by_rows || encode(&mq, p.q, p.J, p.I, p.ldq, 32, 32, true))))
+    return cudaErrorNotSupported;
+  return launch(pair_kernel<MODE>, g.ctas, 2 * g.shares, kPairThreads, kPairBytes, s, ma, mb, mo, mi, mq, a);
 }
 
 // A product's kernel: go.narrow<MODE, BN>() or go.pair<MODE>(). Up to 128 rows the weight's columns take the tile's rows.

@@ -63,6 +63,11 @@ __device__ __forceinline__ void tma_load(uint32_t to, const CUtensorMap* map, in
       : "memory");
 }
 
+__device__ __forceinline__ void tma_store(const CUtensorMap* map, uint32_t from, int x, int y) {
+  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];" ::"l"(map), "r"(from), "r"(x),
+               "r"(y)
+               : "memory");
+}
 __device__ __forceinline__ void tma_load3(uint32_t to, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
   asm volatile(
       "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(
@@ -170,7 +175,7 @@ __device__ __forceinline__ void put_part(float* p, const float (&v)[N]) {
 // The shares' sums added in the cluster's order, several CTAs' loads in flight.
 template <int N, class Load>
 __device__ __forceinline__ void add_parts(uint32_t shares, float (&v)[N], Load&& load) {
-  constexpr int kAhead = N == 32 ? 2 : 4;
+  constexpr int kAhead = N == 32 ? 1 : 4;
 #pragma unroll
   for (int t = 0; t < N; ++t) v[t] = 0.0f;
   for (uint32_t s = 0; s < shares; s += kAhead) {
@@ -217,13 +222,13 @@ inline Encode encoder() {
 // How many clusters of `shares` CTAs of a kernel run at once on the current device, asked for once (a GPU's parts hold
 // different numbers of SMs, so this is less than SMs / shares).
 template <class F>
-int64_t clusters_at_once(F* f, int shares, int bytes, std::atomic<int> (&known)[64][9]) {
+int64_t clusters_at_once(F* f, int shares, int threads, int bytes, std::atomic<int> (&known)[64][9]) {
   int dev = 0, n = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev >= 64) return 1;
   if ((n = known[dev][shares].load(std::memory_order_relaxed)) > 0) return n;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)shares);
-  cfg.blockDim = dim3(kThreads);
+  cfg.blockDim = dim3(threads);
   cfg.dynamicSmemBytes = bytes;
   cudaLaunchAttribute at[1];
   at[0].id = cudaLaunchAttributeClusterDimension;
