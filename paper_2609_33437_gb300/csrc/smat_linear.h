@@ -48,6 +48,10 @@ struct Product {
   int64_t ldr, ldo, ldq, lde;
   int act;
   int accumulate;  // grad_weight: add to what out holds
+  // bf16 grad_weight: db [I] from shares of its sums, [sum_shares][I]; db NULL: none
+  const float* sums;
+  void* db;
+  int sum_shares, add_db;
 };
 
 // fp32 (smat_linear_f32.cu): any size, stride and alignment. `workspace`: f32_workspace() bytes, which go by mode, I, J
@@ -73,9 +77,33 @@ cudaError_t launch_unpack8(const int8_t* q, int64_t ldq, const uint8_t* e, int64
 cudaError_t launch_row_sums(const void* dy, int64_t lddy, void* db, int64_t rows, int64_t cols, int dtype, bool add,
                             int sms, cudaStream_t s);
 
-// A bf16 matrix [rows, cols] copied to rows of stride ldto
-cudaError_t launch_copy_rows(const void* from, int64_t ld, void* to, int64_t ldto, int64_t rows, int64_t cols, int sms,
-                             cudaStream_t s);
+// What a bf16 product needs done before it: nothing for a job whose first pointer (sums: `to`) is NULL. Rows written
+// start on 32 bytes.
+struct Prepare {
+  struct Copy {
+    const void* from;
+    void* to;
+    int64_t rows, cols, ld, ldto;
+    int ctas;
+  } copy[2];
+  struct Unpack {  // act(h^)
+    const int8_t* q;
+    const uint8_t* e;
+    void* to;
+    int64_t rows, cols, ldq, lde, ldto;
+    int ctas;
+    bool vq;
+  } unpack;
+  struct Sums {  // [shares][cols]: of every column over the rows of a share
+    const void* dy;
+    float* to;
+    int64_t rows, cols, lddy;
+    int shares;
+    bool vec;
+  } sums;
+};
+int sum_shares(int64_t rows);
+cudaError_t launch_prepare(Prepare a, int act, int sms, cudaStream_t s);
 
 }  // namespace lin
 }  // namespace smat

@@ -149,7 +149,8 @@ struct Operands {
   Operand a, b;
   size_t values;  // bytes of grad_weight's x^
   size_t parts;   // bytes of the product's own
-  size_t bytes() const { return values + operand_bytes(a) + operand_bytes(b) + parts; }
+  size_t sums;    // bytes of the shares of db's sums
+  size_t bytes() const { return values + operand_bytes(a) + operand_bytes(b) + sums + parts; }
 };
 
 size_t parts_of(int mode, int32_t dtype, int64_t I, int64_t J, int64_t L) {
@@ -180,11 +181,13 @@ Operands operands(const smat_grad_weight_args* g) {
     o.values = copy_bytes(g->rows, g->k, elem_of(g->dtype));
   else
     o.b = operand(g->x, g->rows, g->k, g->ldx, g->dtype);
+  if (g->db && g->dtype == SMAT_BF16) o.sums = up(sizeof(float) * (size_t)sum_shares(g->rows) * (size_t)g->n);
   return o;
 }
 
-// Copies what has to be copied, then the product.
-smat_status run_product(Product& p, const Operands& o, char* d_workspace, int sms, cudaStream_t s, const char* what) {
+// What has to be done first (`first`: grad_weight's x^ and sums, where it is bf16), then the product.
+smat_status run_product(Product& p, const Operands& o, Prepare& first, char* d_workspace, int act, int sms, cudaStream_t s,
+                        const char* what) {
   const Operand* in[2] = {&o.a, &o.b};
   const void** to[2] = {&p.a, &p.b};
   int64_t* ld[2] = {&p.lda, &p.ldb};
@@ -195,10 +198,17 @@ smat_status run_product(Product& p, const Operands& o, char* d_workspace, int sm
     if (!in[i]->copied) continue;
     *to[i] = d_workspace;
     *ld[i] = ld_of(in[i]->cols);
-    const smat_status st = cuda_status(
-        launch_copy_rows(in[i]->p, in[i]->ld, d_workspace, *ld[i], in[i]->rows, in[i]->cols, sms, s), "copy launch");
-    if (st != SMAT_OK) return st;
+    first.copy[i] = {in[i]->p, d_workspace, in[i]->rows, in[i]->cols, in[i]->ld, *ld[i], 0};
     d_workspace += operand_bytes(*in[i]);
+  }
+  if (first.sums.to) {
+    p.sums = first.sums.to = (float*)d_workspace;
+    p.sum_shares = first.sums.shares;
+    d_workspace += o.sums;
+  }
+  if (p.dtype == SMAT_BF16) {
+    const smat_status st = cuda_status(launch_prepare(first, act, sms, s), "preparing launch");
+    if (st != SMAT_OK) return st;
   }
   return cuda_status(p.dtype == SMAT_BF16 ? launch_tc(p, sms, d_workspace, s)
                                             : launch_f32(p, sms, d_workspace, s),
@@ -265,7 +275,8 @@ static smat_status linear(const smat_linear_args* a, void* d_workspace, size_t w
   p.bias = a->bias, p.residual = a->residual, p.out = a->y, p.q = a->q, p.e = a->e;
   p.ldr = a->ldr, p.ldo = a->ldy, p.ldq = a->ldq, p.lde = a->lde;
   p.act = a->act;
-  return run_product(p, ops, (char*)d_workspace, sms, stream, "linear launch");
+  Prepare first = {};
+  return run_product(p, ops, first, (char*)d_workspace, SMAT_ACT_NONE, sms, stream, "linear launch");
 }
 
 static smat_status grad_input(const smat_grad_input_args* a, void* d_workspace, size_t workspace_bytes,
@@ -300,7 +311,8 @@ static smat_status grad_input(const smat_grad_input_args* a, void* d_workspace, 
   p.out = a->dx, p.q = const_cast<int8_t*>(a->q), p.e = const_cast<uint8_t*>(a->e);
   p.ldo = a->lddx, p.ldq = a->ldq, p.lde = a->lde;
   p.act = a->act;
-  return run_product(p, ops, (char*)d_workspace, sms, stream, "grad_input launch");
+  Prepare first = {};
+  return run_product(p, ops, first, (char*)d_workspace, SMAT_ACT_NONE, sms, stream, "grad_input launch");
 }
 
 static smat_status grad_weight(const smat_grad_weight_args* a, void* d_workspace, size_t workspace_bytes,
@@ -333,17 +345,8 @@ static smat_status grad_weight(const smat_grad_weight_args* a, void* d_workspace
   int sms = 1;
   st = device_sms(&sms);
   if (st != SMAT_OK) return st;
-  if (a->db) {
-    st = cuda_status(launch_row_sums(a->dy, a->lddy, a->db, m, n, a->dtype, a->accumulate & SMAT_ACCUMULATE_DB, sms,
-                                     stream), "row sums launch");
-    if (st != SMAT_OK) return st;
-  }
-  if (k == 0) return SMAT_OK;
-  if (ops.values) {
-    st = cuda_status(launch_unpack8(a->q, a->ldq, a->e, a->lde, nullptr, 0, d_workspace, ld_of(k), m, k, a->dtype,
-                                    a->act, sms, stream), "unpack launch");
-    if (st != SMAT_OK) return st;
-  }
+  const bool bf16 = a->dtype == SMAT_BF16;
+  Prepare first = {};
   Product p = {};
   p.mode = kGradWeight;
   p.dtype = a->dtype;
@@ -351,7 +354,24 @@ static smat_status grad_weight(const smat_grad_weight_args* a, void* d_workspace
   p.I = n, p.J = k, p.L = m;
   p.out = a->dw, p.ldo = a->lddw;
   p.accumulate = a->accumulate & SMAT_ACCUMULATE_DW;
-  return run_product(p, ops, (char*)d_workspace + ops.values, sms, stream, "grad_weight launch");
+  if (a->db && bf16 && ops.sums) {
+    first.sums = {a->dy, (float*)d_workspace, m, n, a->lddy, sum_shares(m), false};
+    p.db = a->db;
+    p.add_db = a->accumulate & SMAT_ACCUMULATE_DB;
+  } else if (a->db) {
+    st = cuda_status(launch_row_sums(a->dy, a->lddy, a->db, m, n, a->dtype, a->accumulate & SMAT_ACCUMULATE_DB, sms,
+                                     stream), "row sums launch");
+    if (st != SMAT_OK) return st;
+  }
+  if (k == 0) return SMAT_OK;
+  if (ops.values && bf16) {
+    first.unpack = {a->q, a->e, d_workspace, m, k, a->ldq, a->lde, ld_of(k), 0, false};
+  } else if (ops.values) {
+    st = cuda_status(launch_unpack8(a->q, a->ldq, a->e, a->lde, nullptr, 0, d_workspace, ld_of(k), m, k, a->dtype,
+                                    a->act, sms, stream), "unpack launch");
+    if (st != SMAT_OK) return st;
+  }
+  return run_product(p, ops, first, (char*)d_workspace + ops.values, a->act, sms, stream, "grad_weight launch");
 }
 
 smat_status smat_linear(const smat_linear_args* a, void* d_workspace, size_t workspace_bytes, smat_stream_t stream) {

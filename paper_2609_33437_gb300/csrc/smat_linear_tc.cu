@@ -638,6 +638,15 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       }
     }
   } else if (warp < kPairEpi) {
+    if (MODE == kGradWeight && a.p.db) {  // db, while the first sums are made
+      bf16* db = (bf16*)a.p.db;
+      for (int64_t n = (int64_t)blockIdx.x * (32 * kPairEpi) + threadIdx.x; n < a.p.I; n += (int64_t)gridDim.x * (32 * kPairEpi)) {
+        float t = 0.0f;
+#pragma unroll 4
+        for (int s = 0; s < a.p.sum_shares; ++s) t += a.p.sums[s * a.p.I + n];
+        db[n] = from_float<bf16>(a.p.add_db ? to_float(db[n]) + t : t);
+      }
+    }
     const int quarter = warp % 4;  // the 32 rows of tensor memory that this warp may read
     const uint32_t sums_empty_there = cluster_address_of(sums_empty, leader);
     // this warp's blocks of 32 columns

@@ -122,7 +122,20 @@ __global__ void __launch_bounds__(kThreads) pack8_kernel(const T* x, int64_t ldx
   }
 }
 
-// out = act(h^), or dy * act'(h^) where DY
+// One unit of out = act(h^), or dy * act'(h^) where DY.
+template <class T, int ACT, bool DY>
+__device__ __forceinline__ void unpack_unit(const int8_t* q, const uint8_t* e, const T* dy, T* out, int count, bool vq,
+                                            bool vdy, bool vout) {
+  uint32_t w[4];
+  load_q(q, count, vq, w);
+  float h[kUnit], v[kUnit];
+  unpack_words8<4>(w, *e, h);
+  if (DY) load_unit(dy, count, vdy, v);
+#pragma unroll
+  for (int i = 0; i < kUnit; ++i) v[i] = DY ? v[i] * act_slope<ACT>(h[i]) : act_value<ACT>(h[i]);
+  store_unit(out, count, vout, v);
+}
+
 template <class T, int ACT, bool DY>
 __global__ void __launch_bounds__(kThreads)
     unpack8_kernel(const int8_t* q, int64_t ldq, const uint8_t* e, int64_t lde, const T* dy, int64_t lddy, T* out,
@@ -131,14 +144,8 @@ __global__ void __launch_bounds__(kThreads)
     const int64_t c = (int64_t)u * kUnit;
     const int count = (int)(cols - c < 0 ? 0 : (cols - c < kUnit ? cols - c : kUnit));
     if (count == 0) continue;
-    uint32_t w[4];
-    load_q(q + r * ldq + c, count, vq, w);
-    float h[kUnit], v[kUnit];
-    unpack_words8<4>(w, e[r * lde + u / 2], h);
-    if (DY) load_unit(dy + r * lddy + c, count, vdy, v);
-#pragma unroll
-    for (int i = 0; i < kUnit; ++i) v[i] = DY ? v[i] * act_slope<ACT>(h[i]) : act_value<ACT>(h[i]);
-    store_unit(out + r * ldout + c, count, vout, v);
+    unpack_unit<T, ACT, DY>(q + r * ldq + c, e + r * lde + u / 2, DY ? dy + r * lddy + c : nullptr, out + r * ldout + c,
+                            count, vq, vdy, vout);
   }
 }
 
@@ -164,17 +171,23 @@ __device__ __forceinline__ void add8(const uint4* u, float (&s)[8]) {
   }
 }
 
+struct SumSpace {
+  float part[kSumRows][kSumCols + 1];
+  float total[kSumCols];
+};
+
+// total[c] = the sum of column 64 * block + c over the rows of a share: every 32 * shares-th block of 32 rows
 template <class T>
-__global__ void __launch_bounds__(kThreads)
-    row_sums_kernel(const T* dy, int64_t lddy, T* db, int64_t rows, int64_t cols, bool vec, bool add) {
-  __shared__ float part[kSumRows][kSumCols + 1];
-  __shared__ float total[kSumCols];
+__device__ __forceinline__ void column_sums(const T* dy, int64_t lddy, int64_t rows, int64_t cols, bool vec, int64_t block,
+                                            int64_t share, int64_t shares, SumSpace& space) {
+  float (*part)[kSumCols + 1] = space.part;
+  float* total = space.total;
   const int lane = threadIdx.x % kSumLanes, row = threadIdx.x / kSumLanes;
-  const int64_t c = (int64_t)blockIdx.x * kSumCols + lane * 8;
+  const int64_t c = (int64_t)block * kSumCols + lane * 8;
   const int count = (int)(cols - c < 0 ? 0 : (cols - c < 8 ? cols - c : 8));
   float s[8] = {};
-  const int64_t step = (int64_t)kSumRows * gridDim.y;
-  int64_t r = (int64_t)blockIdx.y * kSumRows + row;
+  const int64_t step = (int64_t)kSumRows * shares;
+  int64_t r = (int64_t)share * kSumRows + row;
   if (vec && count == 8) {
     // eight rows' loads in flight per thread: with one at a time the pass waits for memory (23 us instead of 6 at
     // 8224 x 1024 bf16)
@@ -209,6 +222,14 @@ __global__ void __launch_bounds__(kThreads)
     for (int i = 0; i < kSumRows; ++i) t += part[i][threadIdx.x];
     total[threadIdx.x] = t;
   }
+}
+
+template <class T>
+__global__ void __launch_bounds__(kThreads)
+    row_sums_kernel(const T* dy, int64_t lddy, T* db, int64_t rows, int64_t cols, bool vec, bool add) {
+  __shared__ SumSpace space;
+  column_sums(dy, lddy, rows, cols, vec, blockIdx.x, blockIdx.y, gridDim.y, space);
+  const float* total = space.total;
   cluster_sync();
   const int64_t n = (int64_t)blockIdx.x * kSumCols + threadIdx.x;
   if (blockIdx.y == 0 && threadIdx.x < kSumCols && n < cols) {
@@ -219,18 +240,56 @@ __global__ void __launch_bounds__(kThreads)
   cluster_sync();  // the shares stay until they have been read
 }
 
-// Rows of 2-byte values to rows that start on 16 bytes: a thread moves 8 neighbouring values, read one by one.
-__global__ void __launch_bounds__(kThreads)
-    copy_rows_kernel(const uint16_t* from, int64_t ld, uint16_t* to, int64_t ldto, int64_t rows, int64_t cols) {
-  for (int64_t r = (int64_t)blockIdx.y * blockDim.y + threadIdx.y; r < rows; r += (int64_t)gridDim.y * blockDim.y)
-    for (int64_t c = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) * 8; c < cols;
-         c += (int64_t)gridDim.x * blockDim.x * 8) {
-      uint32_t w[4] = {};
+// What a bf16 product on the tensor cores needs done first, in one launch: rows copied to rows that start on 16 bytes, x^
+// read back from 8 bits, and shares of dy's sums over its rows (which the product's kernel adds up). The CTAs are dealt
+// out to the jobs; each walks its job's rows with threads side by side along a row.
+template <int ACT>
+__global__ void __launch_bounds__(kThreads) prepare_kernel(const Prepare a) {
+  __shared__ SumSpace space;
+  int cta = blockIdx.x;
+  for (int k = 0; k < 2; ++k) {
+    const Prepare::Copy& c = a.copy[k];
+    if (cta < c.ctas) {
+      const int64_t units = (c.cols + 7) / 8;
+      const int wide = (int)(units < kThreads ? units : kThreads), high = kThreads / wide;
+      const int tx = threadIdx.x % wide, ty = threadIdx.x / wide;
+      const uint16_t* from = (const uint16_t*)c.from;
+      uint16_t* to = (uint16_t*)c.to;
+      if (ty < high)
+        for (int64_t r = (int64_t)cta * high + ty; r < c.rows; r += (int64_t)c.ctas * high)
+          for (int64_t u = tx; u < units; u += wide) {
+            const int64_t at = 8 * u;
+            uint32_t w[4] = {};
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (c + i < cols) w[i / 2] |= (uint32_t)from[r * ld + c + i] << (16 * (i % 2));
-      *reinterpret_cast<uint4*>(to + r * ldto + c) = make_uint4(w[0], w[1], w[2], w[3]);
+            for (int i = 0; i < 8; ++i)
+              if (at + i < c.cols) w[i / 2] |= (uint32_t)from[r * c.ld + at + i] << (16 * (i % 2));
+            *reinterpret_cast<uint4*>(to + r * c.ldto + at) = make_uint4(w[0], w[1], w[2], w[3]);
+          }
+      return;
     }
+    cta -= c.ctas;
+  }
+  const Prepare::Unpack& p = a.unpack;
+  if (cta < p.ctas) {
+    const int64_t units = (p.cols + kUnit - 1) / kUnit;
+    const int wide = (int)(units < kThreads ? units : kThreads), high = kThreads / wide;
+    const int tx = threadIdx.x % wide, ty = threadIdx.x / wide;
+    __nv_bfloat16* to = (__nv_bfloat16*)p.to;
+    if (ty < high)
+      for (int64_t r = (int64_t)cta * high + ty; r < p.rows; r += (int64_t)p.ctas * high)
+        for (int64_t u = tx; u < units; u += wide) {
+          const int64_t c = u * kUnit;
+          const int count = (int)(p.cols - c < kUnit ? p.cols - c : kUnit);
+          unpack_unit<__nv_bfloat16, ACT, false>(p.q + r * p.ldq + c, p.e + r * p.lde + u / 2, nullptr, to + r * p.ldto + c,
+                                                 count, p.vq, false, true);
+        }
+    return;
+  }
+  cta -= p.ctas;
+  const Prepare::Sums& m = a.sums;
+  const int64_t block = cta / m.shares, share = cta % m.shares, n = block * kSumCols + threadIdx.x;
+  column_sums((const __nv_bfloat16*)m.dy, m.lddy, m.rows, m.cols, m.vec, block, share, m.shares, space);
+  if (threadIdx.x < kSumCols && n < m.cols) m.to[share * m.cols + n] = space.total[threadIdx.x];
 }
 
 bool can(const void* p, int64_t ld, size_t elem, size_t bytes) {
@@ -291,10 +350,23 @@ cudaError_t launch_unpack8(const int8_t* q, int64_t ldq, const uint8_t* e, int64
             : unpack_as<float, false>(q, ldq, e, lde, dy, lddy, out, ldout, rows, cols, act, sms, s);
 }
 
-cudaError_t launch_copy_rows(const void* from, int64_t ld, void* to, int64_t ldto, int64_t rows, int64_t cols, int sms,
-                             cudaStream_t s) {
-  const Shape h = shape_for(rows, (cols + 7) / 8, sms);
-  copy_rows_kernel<<<h.grid, h.block, 0, s>>>((const uint16_t*)from, ld, (uint16_t*)to, ldto, rows, cols);
+int sum_shares(int64_t rows) { return (int)(rows < 256 ? 1 : rows / 128 < 16 ? rows / 128 : 16); }
+
+cudaError_t launch_prepare(Prepare a, int act, int sms, cudaStream_t s) {
+  // CTAs by the threads that a job keeps busy with 16 bytes to write each, eight CTAs per SM for all copying at most
+  auto ctas_of = [&](int64_t rows, int64_t units) {
+    if (rows == 0 || units == 0) return 0;
+    const int64_t wide = units < kThreads ? units : kThreads, high = kThreads / wide, n = (rows + high - 1) / high;
+    return (int)(n < 8 * sms ? n : 8 * sms);
+  };
+  for (Prepare::Copy& c : a.copy) c.ctas = c.from ? ctas_of(c.rows, (c.cols + 7) / 8) : 0;
+  a.unpack.ctas = a.unpack.q ? ctas_of(a.unpack.rows, (a.unpack.cols + kUnit - 1) / kUnit) : 0;
+  a.unpack.vq = can(a.unpack.q, a.unpack.ldq, 1, 16);
+  a.sums.vec = can(a.sums.dy, a.sums.lddy, 2, 16);
+  const int sums = a.sums.to ? (int)((a.sums.cols + kSumCols - 1) / kSumCols) * a.sums.shares : 0;
+  const int ctas = a.copy[0].ctas + a.copy[1].ctas + a.unpack.ctas + sums;
+  if (ctas == 0) return cudaSuccess;
+  SMAT_WITH_ACT(act, (prepare_kernel<ACT><<<ctas, kThreads, 0, s>>>(a)))
   return cudaGetLastError();
 }
 

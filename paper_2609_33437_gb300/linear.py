@@ -33,34 +33,53 @@ _GRAD_WEIGHT = struct.Struct("@6P8q4i")
 
 class Packed8:
     """A tensor in 8 bits: q int8 of the tensor's shape, e uint8 with ceil(columns / 32) in place of the columns;
-    it stands for q * 2^(e - 127), e by groups of 32 columns."""
-    __slots__ = ("q", "e")
+    it stands for q * 2^(e - 127), e by groups of 32 columns. Packed8(q, e) takes tensors that hold these; what the
+    operators make is one buffer, q's rows and then e's, of which q and e are views."""
+    __slots__ = ("_q", "_e", "_buffer", "_at", "shape", "device")
 
     def __init__(self, q: torch.Tensor, e: torch.Tensor):
         if q.dtype is not torch.int8 or e.dtype is not torch.uint8 or q.dim() < 1 or e.dim() != q.dim():
             raise ValueError("q must be int8 and e uint8, with the same leading dimensions")
         if e.shape[:-1] != q.shape[:-1] or e.shape[-1] != -(-q.shape[-1] // GROUP):
             raise ValueError(f"e must be shaped {(*q.shape[:-1], -(-q.shape[-1] // GROUP))}")
-        self.q, self.e = q, e
+        self._q, self._e, self._buffer = q, e, None
+        self.shape, self.device = q.shape, q.device
 
     @classmethod
-    def empty(cls, shape, device) -> "Packed8":
-        q = torch.empty(shape, dtype=torch.int8, device=device)
-        e = torch.empty((*shape[:-1], -(-shape[-1] // GROUP)), dtype=torch.uint8, device=device)
-        p = object.__new__(cls)  # made to fit: nothing to check
-        p.q, p.e = q, e
+    def _make(cls, shape, rows: int, cols: int, device) -> "Packed8":
+        """An empty one for the operators to fill (rows: the leading dimensions' product)."""
+        p = object.__new__(cls)
+        p._q = p._e = None
+        p._at = -(-rows * cols // 256) * 256  # of e in the buffer
+        p._buffer = torch.empty(p._at + rows * -(-cols // GROUP), dtype=torch.uint8, device=device)
+        p.shape, p.device = torch.Size(shape), device
         return p
 
     @property
-    def shape(self):
-        return self.q.shape
+    def q(self) -> torch.Tensor:
+        if self._q is None:
+            self._q = self._buffer[:self.shape.numel()].view(torch.int8).view(self.shape)
+        return self._q
 
     @property
-    def device(self):
-        return self.q.device
+    def e(self) -> torch.Tensor:
+        if self._e is None:
+            self._e = self._buffer[self._at:].view(*self.shape[:-1], -(-self.shape[-1] // GROUP))
+        return self._e
 
     def nbytes(self) -> int:
-        return self.q.numel() + self.e.numel()
+        rows = self.shape[:-1].numel()
+        return rows * (self.shape[-1] - (-self.shape[-1] // GROUP))
+
+    def _places(self, name: str, device, rows: int, cols: int):
+        """(address and row stride of q, and of e); what does not fit [rows, cols] on `device` is refused."""
+        if self._buffer is not None:
+            shape = self.shape
+            if shape[-1] == cols and shape[:-1].numel() == rows and self.device == device:
+                at = self._buffer.data_ptr()
+                return at, cols, at + self._at, -(-cols // GROUP)
+        return (*_like(name + ".q", self.q, torch.int8, device, rows, cols),
+                *_like(name + ".e", self.e, torch.uint8, device, rows, -(-cols // GROUP)))
 
 
 def _rows(name: str, t: torch.Tensor) -> Tuple[int, int, int]:
@@ -115,13 +134,6 @@ def _vector(name: str, t: torch.Tensor, dtype, device, n: int) -> int:
     if t.dtype is not dtype or t.device != device or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
         raise ValueError(f"{name}: must be a contiguous vector of {n} {dtype} on {device}")
     return t.data_ptr()
-
-
-def _packed(name: str, p: Packed8, device, rows: int, cols: int):
-    """(q, ldq, e, lde)"""
-    q, ldq = _like(name + ".q", p.q, torch.int8, device, rows, cols)
-    e, lde = _like(name + ".e", p.e, torch.uint8, device, rows, -(-cols // GROUP))
-    return q, ldq, e, lde
 
 
 # The current stream's handle without a Stream object around it (2.8 us of a small call otherwise).
@@ -197,9 +209,8 @@ def linear(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor] = None
         py, ldy = y.data_ptr(), n
     else:
         py, ldy = _like("out", y, dtype, device, rows, n)
-    saved = Packed8.empty(shape, device) if save else None
-    pq, pe, lde = (saved.q.data_ptr(), saved.e.data_ptr(), saved.e.shape[-1]) if save else (0, 0, 1)
-    ldq = n
+    saved = Packed8._make(shape, rows, n, device) if save else None
+    pq, ldq, pe, lde = saved._places("saved", device, rows, n) if save else (0, n, 0, 1)
     args = _LINEAR.pack(x.data_ptr(), pw, pb, pr, py, pq, pe, rows, k, n, ldx, ldw, ldr, ldy, ldq, lde, code, a)
     _run("smat_linear", args, device)
     return (y, saved) if save else y
@@ -221,7 +232,7 @@ def linear_grad_input(dy: torch.Tensor, w: torch.Tensor, act: str = "none", save
         raise ValueError("w: must be a matrix")
     k = w.shape[1]
     pw, ldw = _like("w", w, dtype, device, n, k)
-    pq, ldq, pe, lde = _packed("saved", saved, device, rows, k) if saved is not None else (0, k, 0, 1)
+    pq, ldq, pe, lde = saved._places("saved", device, rows, k) if saved is not None else (0, k, 0, 1)
     dx = out
     if dx is None:
         dx = torch.empty((*dy.shape[:-1], k), dtype=dtype, device=device)
@@ -257,7 +268,7 @@ def linear_grad_weight(dy: torch.Tensor, x: Union[torch.Tensor, Packed8], act: s
     px = pq = pe = 0
     ldx, ldq, lde = k, k, 1
     if packed:
-        pq, ldq, pe, lde = _packed("x", x, device, rows, k)
+        pq, ldq, pe, lde = x._places("x", device, rows, k)
     else:
         px, ldx = _like("x", x, dtype, device, rows, k)
     dw = out
@@ -284,9 +295,8 @@ def pack8(x: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> Packed
         return _on(stream, pack8, x)
     rows, cols, ldx = _rows("x", x)
     code = S.dtype_code(x.dtype)
-    p = Packed8.empty(x.shape, x.device)
-    _call("smat_pack8", x.device, x.data_ptr(), ldx, p.q.data_ptr(), cols, p.e.data_ptr(),
-          p.e.shape[-1], rows, cols, code)
+    p = Packed8._make(x.shape, rows, cols, x.device)
+    _call("smat_pack8", x.device, x.data_ptr(), ldx, *p._places("p", x.device, rows, cols), rows, cols, code)
     return p
 
 
@@ -297,16 +307,15 @@ def unpack8(p: Packed8, act: str = "none", dtype: torch.dtype = torch.bfloat16, 
         return _on(stream, unpack8, p, act, dtype, out)
     a = _act(act)
     code = S.dtype_code(dtype)
-    rows, cols, ldq = _rows("p.q", p.q)
-    pe, lde = _like("p.e", p.e, torch.uint8, p.device, rows, p.e.shape[-1])
+    device, cols = p.device, p.shape[-1]
+    rows = p.shape[:-1].numel()
     y = out
     if y is None:
-        y = torch.empty(p.q.shape, dtype=dtype, device=p.q.device)
+        y = torch.empty(p.shape, dtype=dtype, device=device)
         py, ldy = y.data_ptr(), cols
     else:
-        py, ldy = _like("out", y, dtype, p.device, rows, cols)
-    _call("smat_unpack8", p.device, p.q.data_ptr(), ldq, pe, lde, py, ldy,
-          rows, cols, code, a)
+        py, ldy = _like("out", y, dtype, device, rows, cols)
+    _call("smat_unpack8", device, *p._places("p", device, rows, cols), py, ldy, rows, cols, code, a)
     return y
 
 
@@ -318,15 +327,14 @@ def act_grad8(dy: torch.Tensor, saved: Packed8, act: str, out: Optional[torch.Te
     a = _act(act)
     rows, cols, lddy = _rows("dy", dy)
     code = S.dtype_code(dy.dtype)
-    pq, ldq, pe, lde = _packed("saved", saved, dy.device, rows, cols)
+    places = saved._places("saved", dy.device, rows, cols)
     dh = out
     if dh is None:
         dh = torch.empty(dy.shape, dtype=dy.dtype, device=dy.device)
         ph, ldh = dh.data_ptr(), cols
     else:
         ph, ldh = _like("out", dh, dy.dtype, dy.device, rows, cols)
-    _call("smat_act_grad8", dy.device, dy.data_ptr(), lddy, pq, ldq, pe,
-          lde, ph, ldh, rows, cols, code, a)
+    _call("smat_act_grad8", dy.device, dy.data_ptr(), lddy, *places, ph, ldh, rows, cols, code, a)
     return dh
 
 
