@@ -24,7 +24,15 @@ namespace lin {
 namespace {
 
 constexpr int kUnits = 256;  // threads that make a tile on the fp32 units
-constexpr int kBN = 128, kSimtK = 16, kPad = 4;
+constexpr int kBN = 128, kPad = 4;
+// Slices along the sum: what is on its way from memory per CTA. Tiles of 32 rows wait for it, so theirs are long (rows 1 to 32
+// of 4096 x 4096: 51 us with slices of 16).
+template <int BM>
+constexpr int kSimtK = BM == 32 ? 64 : 16;
+
+// In shared memory four neighbours of a slice [K][R + kPad] lie at a place that changes with every four rows, so that the
+// stores of a slice that arrives along the sum meet in few banks.
+__device__ __forceinline__ int place(int k, int i) { return i ^ ((k >> 2 & 7) << 2); }
 
 // A barrier of the first kUnits threads (both kernels' warps 0 to 7).
 __device__ __forceinline__ void units_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
@@ -42,10 +50,10 @@ __device__ __forceinline__ float4 load4(const float* p, int64_t count, bool vec)
   return make_float4(count > 0 ? p[0] : 0.0f, count > 1 ? p[1] : 0.0f, count > 2 ? p[2] : 0.0f, count > 3 ? p[3] : 0.0f);
 }
 
-// One operand's slice [R][kSimtK] into registers, then into shared memory as [kSimtK][R + kPad].
-template <int R, bool MN>
+// One operand's slice [R][K] into registers, then into shared memory as [K][R + kPad].
+template <int R, bool MN, int K>
 struct Slice {
-  static constexpr int kVecs = R * kSimtK / 4, kSteps = (kVecs + kUnits - 1) / kUnits;
+  static constexpr int kVecs = R * K / 4, kSteps = (kVecs + kUnits - 1) / kUnits;
   float4 v[kSteps];
 
   __device__ __forceinline__ void load(const float* p, int64_t ld, int64_t first, int64_t end, int64_t l, int64_t l_end,
@@ -59,7 +67,7 @@ struct Slice {
         const int64_t k = l + at / (R / 4), i = first + at % (R / 4) * 4;
         if (k < l_end) v[s] = load4(p + k * ld + i, end - i, vec);
       } else {
-        const int64_t i = first + at / (kSimtK / 4), k = l + at % (kSimtK / 4) * 4;
+        const int64_t i = first + at / (K / 4), k = l + at % (K / 4) * 4;
         if (i < end) v[s] = load4(p + i * ld + k, l_end - k, vec);
       }
     }
@@ -71,9 +79,10 @@ struct Slice {
       const int at = threadIdx.x + s * kUnits;
       if (kVecs % kUnits && at >= kVecs) continue;
       if (MN) {
-        *reinterpret_cast<float4*>(&to[at / (R / 4)][at % (R / 4) * 4]) = v[s];
+        const int k = at / (R / 4);
+        *reinterpret_cast<float4*>(&to[k][place(k, at % (R / 4) * 4)]) = v[s];
       } else {
-        const int i = at / (kSimtK / 4), k = at % (kSimtK / 4) * 4;
+        const int k = at % (K / 4) * 4, i = place(k, at / (K / 4));
         to[k][i] = v[s].x, to[k + 1][i] = v[s].y, to[k + 2][i] = v[s].z, to[k + 3][i] = v[s].w;
       }
     }
@@ -150,17 +159,17 @@ __device__ __forceinline__ void finish4(const Args& a, int64_t i, int64_t j, flo
 // ------------------------------------------------------------- fp32 units ---
 
 template <int BM>
-constexpr int kSlicesBytes = 2 * kSimtK * (BM + kPad + kBN + kPad) * 4;
+constexpr int kSlicesBytes = 2 * kSimtK<BM> * (BM + kPad + kBN + kPad) * 4;
 template <int BM>
 constexpr int kSimtBytes = kSlicesBytes<BM> > BM * kBN * 4 ? kSlicesBytes<BM> : BM * kBN * 4;
 
 // The sums of BM x 128 from (i0, j0) over l0 .. l1, left in `shared` as [BM][128]; threads 0 to 255.
 template <int BM, bool A_MN, bool B_MN>
 __device__ __forceinline__ void simt_sums(const Args& a, float* shared, int64_t i0, int64_t j0, int64_t l0, int64_t l1) {
-  constexpr int TM = BM / 16;  // consecutive rows per thread
+  constexpr int TM = BM / 16, K = kSimtK<BM>;  // consecutive rows per thread; a slice
   static_assert(TM == 8 || TM == 2, "");
-  float (*sa)[kSimtK][BM + kPad] = reinterpret_cast<float (*)[kSimtK][BM + kPad]>(shared);
-  float (*sb)[kSimtK][kBN + kPad] = reinterpret_cast<float (*)[kSimtK][kBN + kPad]>(shared + 2 * kSimtK * (BM + kPad));
+  float (*sa)[K][BM + kPad] = reinterpret_cast<float (*)[K][BM + kPad]>(shared);
+  float (*sb)[K][kBN + kPad] = reinterpret_cast<float (*)[K][kBN + kPad]>(shared + 2 * K * (BM + kPad));
   float (*sums)[kBN] = reinterpret_cast<float (*)[kBN]>(shared);  // afterwards
 
   const Product& p = a.p;
@@ -171,8 +180,8 @@ __device__ __forceinline__ void simt_sums(const Args& a, float* shared, int64_t 
 #pragma unroll
     for (int j = 0; j < 4; ++j) acc[i][j] = 0;
 
-  Slice<BM, A_MN> na;
-  Slice<kBN, B_MN> nb;
+  Slice<BM, A_MN, K> na;
+  Slice<kBN, B_MN, K> nb;
   const float *pa = (const float*)p.a, *pb = (const float*)p.b;
   if (l0 < l1) {
     na.load(pa, p.lda, i0, p.I, l0, l1, a.va);
@@ -182,22 +191,22 @@ __device__ __forceinline__ void simt_sums(const Args& a, float* shared, int64_t 
   }
   units_sync();
   int at = 0;
-  for (int64_t l = l0; l < l1; l += kSimtK, at ^= 1) {
-    const bool more = l + kSimtK < l1;
+  for (int64_t l = l0; l < l1; l += K, at ^= 1) {
+    const bool more = l + K < l1;
     if (more) {
-      na.load(pa, p.lda, i0, p.I, l + kSimtK, l1, a.va);
-      nb.load(pb, p.ldb, j0, p.J, l + kSimtK, l1, a.vb);
+      na.load(pa, p.lda, i0, p.I, l + K, l1, a.va);
+      nb.load(pb, p.ldb, j0, p.J, l + K, l1, a.vb);
     }
-#pragma unroll
-    for (int k = 0; k < kSimtK; ++k) {
-      const ulonglong2 b01 = *reinterpret_cast<const ulonglong2*>(&sb[at][k][tx * 4]);
-      const ulonglong2 b23 = *reinterpret_cast<const ulonglong2*>(&sb[at][k][64 + tx * 4]);
+#pragma unroll 16
+    for (int k = 0; k < K; ++k) {
+      const ulonglong2 b01 = *reinterpret_cast<const ulonglong2*>(&sb[at][k][place(k, tx * 4)]);
+      const ulonglong2 b23 = *reinterpret_cast<const ulonglong2*>(&sb[at][k][place(k, 64 + tx * 4)]);
       float x[TM];
       if constexpr (TM == 8) {
-        *reinterpret_cast<float4*>(x) = *reinterpret_cast<const float4*>(&sa[at][k][ty * TM]);
-        *reinterpret_cast<float4*>(x + 4) = *reinterpret_cast<const float4*>(&sa[at][k][ty * TM + 4]);
+        *reinterpret_cast<float4*>(x) = *reinterpret_cast<const float4*>(&sa[at][k][place(k, ty * TM)]);
+        *reinterpret_cast<float4*>(x + 4) = *reinterpret_cast<const float4*>(&sa[at][k][place(k, ty * TM + 4)]);
       } else {
-        *reinterpret_cast<float2*>(x) = *reinterpret_cast<const float2*>(&sa[at][k][ty * TM]);
+        *reinterpret_cast<float2*>(x) = *reinterpret_cast<const float2*>(&sa[at][k][place(k, ty * TM)]);
       }
 #pragma unroll
       for (int i = 0; i < TM; ++i) {
@@ -222,7 +231,7 @@ __device__ __forceinline__ void simt_sums(const Args& a, float* shared, int64_t 
 }
 
 template <int BM, bool A_MN, bool B_MN>
-__global__ void __launch_bounds__(kUnits, BM == 128 ? 2 : 3) simt_kernel(const Args a) {
+__global__ void __launch_bounds__(kUnits, 2) simt_kernel(const Args a) {
   extern __shared__ __align__(16) float shared[];
   const Product& p = a.p;
   const int64_t i0 = (int64_t)blockIdx.x * BM, j0 = (int64_t)blockIdx.y * kBN;
@@ -577,7 +586,8 @@ cudaError_t launch_simt_tile(Args a, int sms, cudaStream_t s) {
   int shares = 1;
   // two CTAs fit on an SM; a share is at least 64 long
   while (shares < 8 && ti * tj * shares * 2 <= 2 * sms && a.p.L >= (int64_t)shares * 2 * 64) shares *= 2;
-  a.share = (a.p.L + shares * kSimtK - 1) / (shares * kSimtK) * kSimtK;
+  constexpr int K = kSimtK<BM>;
+  a.share = (a.p.L + shares * K - 1) / (shares * K) * K;
   cudaLaunchAttribute at;
   const cudaLaunchConfig_t cfg = config(dim3((unsigned)ti, (unsigned)tj, (unsigned)shares), kUnits, kSimtBytes<BM>,
                                         dim3(1, 1, (unsigned)shares), &at, s);
@@ -587,7 +597,7 @@ cudaError_t launch_simt_tile(Args a, int sms, cudaStream_t s) {
 template <bool A_MN, bool B_MN>
 cudaError_t launch_simt(const Product& p, int sms, cudaStream_t s) {
   const Args a = args_of(p);
-  return p.I <= 32 ? launch_simt_tile<32, A_MN, B_MN>(a, sms, s) : launch_simt_tile<128, A_MN, B_MN>(a, sms, s);
+  return launch_simt_tile<32, A_MN, B_MN>(a, sms, s);
 }
 
 // What a product on the tensor cores needs: an operand's parts, flags, shares of sums.

@@ -10,9 +10,8 @@
 // and CTA for 256 columns, where a CTA by itself needs 48 KB and the copies bound it (8192 x 11008 x 4096: 484 us).
 // `width` and the shares of the sum are chosen by an estimate of the time, see plan_pair. The tile's rows are rows i of
 // the result. A thread holds 32 columns of a row, whole groups of the 8-bit form; 32 columns of a warp's 32 rows leave
-// through shared memory by TMA, and what is added to them comes in that way (stores of 32 bytes a row and lane bound the
-// kernel by their number: 2056 x 64 x 4096 took 10 us, and more the more warps stored). Results whose rows do not start
-// on 16 bytes take a turn through shared memory, to 32 neighbouring columns per warp.
+// through shared memory by TMA, and what is added to them comes in that way; rows that do not start on 16 bytes are
+// copied to and from there by the warp itself, a column per lane.
 //
 // Products of at most 128 rows (narrow_kernel): the tile's 128 rows are columns j and its 32, 64 or 128 columns are rows
 // i, so that a wide weight fills the 128 and the few rows cost a narrow tile. A warp holds 32 neighbouring columns of a
@@ -47,10 +46,8 @@ struct Ring {
 constexpr int kPairRows = 2 * kBM, kPairStages = 5, kPairStage = 2 * kBytesA;
 constexpr int kPairEpi = 12;  // warps that finish a pair's sums
 constexpr int kPairThreads = 32 * (kPairEpi + 2);
-// A finishing warp's own shared memory: 32 rows of 32 results (64 bytes, swizzled) and of 32 q (32 bytes, swizzled). Rows
-// that are not copied by TMA are turned there, 16 at a time, 33 floats apart.
+// A finishing warp's own shared memory: 32 rows of 32 results (64 bytes, swizzled) and of 32 q (32 bytes, swizzled).
 constexpr int kDeskRows = 32 * 64, kDeskQ = 32 * 32, kDesk = kDeskRows + kDeskQ;
-static_assert(16 * 33 * 4 <= kDesk, "");
 constexpr int kPairBytes = kPairStages * kPairStage + kPairEpi * kDesk + 1024;
 constexpr int kSums = 256;  // columns of tensor memory for one tile's sums
 
@@ -62,8 +59,7 @@ struct Args {
   int width;                        // columns of a pair's tile
   float* parts;                     // the shares' sums, or NULL
   int* errors;                      // device error bits
-  bool by_rows;                     // rows of out and residual start on 16 bytes, those of q on 8: copied by TMA
-  bool q_by_rows;                   // those of q on 16: by TMA too
+  bool by_rows;                     // rows of out, residual and q start on 16 bytes: TMA copies them
   bool wide_bias;                   // bias on 16 bytes
 };
 
@@ -76,18 +72,6 @@ __device__ __forceinline__ void unpack_words(const uint32_t* w, int words, float
     v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
   }
 }
-// 32 q of a row that starts on 8 bytes
-__device__ __forceinline__ void load_q32(const int8_t* p, uint32_t* w) {
-#pragma unroll
-  for (int h = 0; h < 4; ++h)
-    asm volatile("ld.global.v2.b32 {%0,%1}, [%2];" : "=r"(w[2 * h]), "=r"(w[2 * h + 1]) : "l"(p + 8 * h));
-}
-__device__ __forceinline__ void store_q32(int8_t* p, const uint32_t* w) {
-#pragma unroll
-  for (int h = 0; h < 4; ++h)
-    asm volatile("st.global.v2.b32 [%0], {%1,%2};" ::"l"(p + 8 * h), "r"(w[2 * h]), "r"(w[2 * h + 1]) : "memory");
-}
-
 // A warp's desk: where its 32 rows of 32 columns wait for TMA, and come from it. 16 bytes of a row lie at a place that
 // changes with the row, as the copies' swizzle has it, so that 8 rows' accesses meet in no bank.
 struct Desk {
@@ -109,8 +93,54 @@ __device__ __forceinline__ void desk_store(uint32_t at, const uint32_t* w) {
   asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
 }
 
-// Columns j .. j + 31 of rows i .. i + 31, a row per lane, out by TMA (which leaves out what lies outside the result).
-// sums(v): their sums.
+// The same by the warp's own accesses, for rows that TMA cannot copy: a column per lane, all 32 rows' loads in flight.
+template <class T>
+__device__ __forceinline__ uint32_t desk_place(const Desk& desk, int row, int column) {
+  if (sizeof(T) == 2) return desk.row_at(row, column >> 3) + (column & 7) * 2;
+  return desk.q_at(row, column >> 4) + (column & 15);
+}
+template <class T>  // uint16_t: rows of bf16; uint8_t: q
+__device__ __forceinline__ void desk_fetch(const Desk& desk, const void* from, int64_t ld, int64_t i, int64_t j, int64_t I,
+                                           int64_t J) {
+  const int lane = threadIdx.x % 32;
+  const int rows = j + lane < J ? (int)(I - i < 32 ? I - i : 32) : 0;
+  const T* p = (const T*)from + i * ld + j + lane;
+  T x[32];
+#pragma unroll
+  for (int t = 0; t < 32; ++t) x[t] = t < rows ? p[t * ld] : (T)0;
+#pragma unroll
+  for (int t = 0; t < 32; ++t) {
+    if (sizeof(T) == 2)
+      asm volatile("st.shared.u16 [%0], %1;" ::"r"(desk_place<T>(desk, t, lane)), "h"((uint16_t)x[t]) : "memory");
+    else
+      asm volatile("st.shared.u8 [%0], %1;" ::"r"(desk_place<T>(desk, t, lane)), "r"((uint32_t)x[t]) : "memory");
+  }
+}
+template <class T>
+__device__ __forceinline__ void desk_send(const Desk& desk, void* to, int64_t ld, int64_t i, int64_t j, int64_t I, int64_t J) {
+  const int lane = threadIdx.x % 32;
+  const int rows = j + lane < J ? (int)(I - i < 32 ? I - i : 32) : 0;
+  T* p = (T*)to + i * ld + j + lane;
+  T x[32];
+#pragma unroll
+  for (int t = 0; t < 32; ++t) {
+    if (sizeof(T) == 2) {
+      uint16_t u;
+      asm volatile("ld.shared.u16 %0, [%1];" : "=h"(u) : "r"(desk_place<T>(desk, t, lane)) : "memory");
+      x[t] = (T)u;
+    } else {
+      uint32_t u;
+      asm volatile("ld.shared.u8 %0, [%1];" : "=r"(u) : "r"(desk_place<T>(desk, t, lane)) : "memory");
+      x[t] = (T)u;
+    }
+  }
+#pragma unroll
+  for (int t = 0; t < 32; ++t)
+    if (t < rows) p[t * ld] = x[t];
+}
+
+// Columns j .. j + 31 of rows i .. i + 31, a row per lane, out by TMA (which leaves out what lies outside the result) or
+// by hand. sums(v): their sums.
 template <int MODE, class Sums>
 __device__ __forceinline__ void finish_block(const Args& a, const CUtensorMap* map_out, const CUtensorMap* map_in,
                                             const CUtensorMap* map_q, int64_t i, int64_t j, Desk& desk,
@@ -121,15 +151,24 @@ __device__ __forceinline__ void finish_block(const Args& a, const CUtensorMap* m
   const bool slope = MODE == kGradInput && p.act != SMAT_ACT_NONE;
   const bool add = MODE == kForward ? p.residual != nullptr : MODE == kGradWeight && p.accumulate;
   const bool save = MODE == kForward && p.q;
-  if (lane == 0) {
-    asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");  // the last unit has left the desk
-    if (add || (slope && a.q_by_rows)) {
-      bar_expect(desk.bar, add ? kDeskRows : kDeskQ);
-      if (add)
-        tma_load(desk.rows, map_in, (int)j, (int)i, desk.bar);
-      else
-        tma_load(desk.q, map_q, (int)j, (int)i, desk.bar);
+  const void* from = MODE == kForward ? p.residual : p.out;  // what is added
+  const int64_t ld_from = MODE == kForward ? p.ldr : p.ldo;
+  const bool copied = a.by_rows && (add || slope);  // by TMA
+  if (a.by_rows) {
+    if (lane == 0) {
+      asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");  // the last block has left the desk
+      if (copied) {
+        bar_expect(desk.bar, add ? kDeskRows : kDeskQ);
+        if (add)
+          tma_load(desk.rows, map_in, (int)j, (int)i, desk.bar);
+        else
+          tma_load(desk.q, map_q, (int)j, (int)i, desk.bar);
+      }
     }
+  } else {
+    __syncwarp();  // the last block has been read
+    if (add) desk_fetch<uint16_t>(desk, from, ld_from, i, j, p.I, p.J);
+    if (slope) desk_fetch<uint8_t>(desk, p.q, p.ldq, i, j, p.I, p.J);
   }
   uint32_t e = 1;
   if (slope && there) e = p.e[(i + lane) * p.lde + j / kGroup];
@@ -166,42 +205,22 @@ __device__ __forceinline__ void finish_block(const Args& a, const CUtensorMap* m
       const uint32_t ex = pack_exponent(__float_as_uint(big[0]));
       uint32_t w[8];
       pack_words<8>(v, ex, w);
-      if (a.q_by_rows) {
-        desk_store(desk.q_at(lane, 0), w);
-        desk_store(desk.q_at(lane, 1), w + 4);
-      } else if (there && j + 32 <= p.J) {
-        store_q32(p.q + (i + lane) * p.ldq + j, w);
-      } else if (there) {
-#pragma unroll
-        for (int t = 0; t < 32; ++t)
-          if (j + t < p.J) p.q[(i + lane) * p.ldq + j + t] = (int8_t)(w[t / 4] >> (8 * (t % 4)));
-      }
+      desk_store(desk.q_at(lane, 0), w);
+      desk_store(desk.q_at(lane, 1), w + 4);
       if (there && j < p.J) p.e[(i + lane) * p.lde + j / kGroup] = (uint8_t)ex;
     }
     SMAT_WITH_ACT(p.act, _Pragma("unroll") for (int t = 0; t < 32; ++t) v[t] = act_value<ACT>(v[t]))
   }
-  if (add || (slope && a.q_by_rows)) {
+  if (copied) {
     if (!bar_wait(desk.bar, desk.phase & 1, dead, a.errors)) return;
     ++desk.phase;
   }
   if (slope) {
     uint32_t w[8];
-    if (a.q_by_rows) {
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const uint4 u = desk_load(desk.q_at(lane, t));
-        w[4 * t] = u.x, w[4 * t + 1] = u.y, w[4 * t + 2] = u.z, w[4 * t + 3] = u.w;
-      }
-    } else if (there && j + 32 <= p.J) {
-      load_q32(p.q + (i + lane) * p.ldq + j, w);
-    } else {
-#pragma unroll
-      for (int t = 0; t < 8; ++t) w[t] = 0;
-      if (there) {
-#pragma unroll
-        for (int t = 0; t < 32; ++t)
-          if (j + t < p.J) w[t / 4] |= (uint32_t)(uint8_t)p.q[(i + lane) * p.ldq + j + t] << (8 * (t % 4));
-      }
+    for (int t = 0; t < 2; ++t) {
+      const uint4 u = desk_load(desk.q_at(lane, t));
+      w[4 * t] = u.x, w[4 * t + 1] = u.y, w[4 * t + 2] = u.z, w[4 * t + 3] = u.w;
     }
     float x[32];
     unpack_words8<8>(w, e, x);
@@ -226,12 +245,18 @@ __device__ __forceinline__ void finish_block(const Args& a, const CUtensorMap* m
     }
     desk_store(at, w);
   }
-  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-  __syncwarp();
-  if (lane == 0) {
-    tma_store(map_out, desk.rows, (int)j, (int)i);
-    if (save && a.q_by_rows) tma_store(map_q, desk.q, (int)j, (int)i);
-    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+  if (a.by_rows) {
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+    if (lane == 0) {
+      tma_store(map_out, desk.rows, (int)j, (int)i);
+      if (save) tma_store(map_q, desk.q, (int)j, (int)i);
+      asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+    }
+  } else {
+    __syncwarp();
+    desk_send<uint16_t>(desk, p.out, p.ldo, i, j, p.I, p.J);
+    if (save) desk_send<uint8_t>(desk, p.q, p.ldq, i, j, p.I, p.J);
   }
 }
 
@@ -304,30 +329,15 @@ __device__ __forceinline__ void finish_column(const Args& a, int64_t i, int64_t 
 template <int MODE, class Sums>
 __device__ __forceinline__ void finish_blocks(const Args& a, const CUtensorMap* map_out, const CUtensorMap* map_in,
                                               const CUtensorMap* map_q, int64_t row0, int64_t col0, int first, int end,
-                                              int step, Desk& desk, float* turn, volatile int* dead, Sums&& sums) {
-  const int lane = threadIdx.x % 32;
+                                              int step, Desk& desk, volatile int* dead, Sums&& sums) {
 #pragma unroll 1
   for (int c = first; c < end; c += step) {
     const int64_t col = col0 + 32 * c;
-    if (a.by_rows && row0 < a.p.I && col < a.p.J) {
+    if (row0 < a.p.I && col < a.p.J) {
       finish_block<MODE>(a, map_out, map_in, map_q, row0, col, desk, dead, [&](float(&v)[32]) { sums(c, v); });
-      continue;
-    }
-    float v[32];
-    sums(c, v);
-    if (row0 >= a.p.I || col >= a.p.J) continue;
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {  // 16 rows at a time
-      __syncwarp();
-      if (lane / 16 == h) {
-#pragma unroll
-        for (int t = 0; t < 32; ++t) turn[lane % 16 * 33 + t] = v[t];
-      }
-      __syncwarp();
-      float x[16];
-#pragma unroll
-      for (int t = 0; t < 16; ++t) x[t] = turn[t * 33 + lane];
-      finish_column<MODE, 16>(a, row0 + 16 * h, col + lane, x);
+    } else {
+      float v[32];
+      sums(c, v);
     }
   }
 }
@@ -676,7 +686,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       };
       if (first == end) release();  // none of a narrow tile's columns
       if (shares == 1) {
-        finish_blocks<MODE>(a, &map_out, &map_in, &map_q, r0, c0, first, end, 1, desk, (float*)own, dead, take);
+        finish_blocks<MODE>(a, &map_out, &map_in, &map_q, r0, c0, first, end, 1, desk, dead, take);
       } else {
         float* part = a.parts + ((size_t)first_tile * ctas + rank) * a.width * kBM + 32 * quarter + lane;
         for (int c = first; c < end; ++c) {
@@ -701,7 +711,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       const size_t apart = (size_t)2 * a.width * kBM;
       const int blocks = r0 < a.p.I ? (int)((min((int64_t)a.width, a.p.J - c0) + 31) / 32) : 0;
       finish_blocks<MODE>(a, &map_out, &map_in, &map_q, r0, c0, (int)share + (int)shares * (warp / 4), blocks,
-                          (int)shares * (kPairEpi / 4), desk, (float*)own, dead, [&](int c, float(&v)[32]) {
+                          (int)shares * (kPairEpi / 4), desk, dead, [&](int c, float(&v)[32]) {
                            add_parts(shares, v, [&](uint32_t s, int t) { return __ldcg(part + s * apart + (32 * c + t) * kBM); });
                          });
     }
@@ -814,8 +824,7 @@ cudaError_t fill_args(const Product& p, const Plan& g, void* workspace, Args* ar
     return (uintptr_t)q % bytes == 0 && (uint64_t)ld * elem % bytes == 0;
   };
   a.by_rows = rows_on(p.out, p.ldo, 2, 16) && (!p.residual || rows_on(p.residual, p.ldr, 2, 16)) &&
-              (!p.q || rows_on(p.q, p.ldq, 1, 8));
-  a.q_by_rows = p.q && rows_on(p.q, p.ldq, 1, 16);
+              (!p.q || rows_on(p.q, p.ldq, 1, 16));
   a.wide_bias = (uintptr_t)p.bias % 16 == 0;
   *args = a;
   return e;
@@ -868,7 +877,7 @@ cudaError_t launch_pair(const Product& p, void* workspace, cudaStream_t s) {
   const void* in = MODE == kForward ? p.residual : MODE == kGradWeight && p.accumulate ? p.out : nullptr;
   if (a.by_rows && !(encode(&mo, p.out, p.J, p.I, p.ldo, 32, 32) &&
                      (!in || encode(&mi, in, p.J, p.I, MODE == kForward ? p.ldr : p.ldo, 32, 32)) &&
-                     (!a.q_by_rows || encode(&mq, p.q, p.J, p.I, p.ldq, 32, 32, true))))
+                     (!p.q || encode(&mq, p.q, p.J, p.I, p.ldq, 32, 32, true))))
     return cudaErrorNotSupported;
   return launch(pair_kernel<MODE>, g.ctas, 2 * g.shares, kPairThreads, kPairBytes, s, ma, mb, mo, mi, mq, a);
 }
