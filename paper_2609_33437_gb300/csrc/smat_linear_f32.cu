@@ -9,8 +9,9 @@
 // An infinity times a part that is 0 would give NaN. So the first kernel says whether it met an infinity or NaN, and
 // where it did, the second one makes its tiles on the fp32 units instead.
 //
-// Small ones, and those of few rows, run on the fp32 units as they are: the cutting would cost more than it gains.
-// A CTA of 256 threads makes a tile of BM x 128 sums, BM / 16 x 8 of them in each thread's registers as packed pairs (one
+// Products of at most 16 rows read a weight once and wait for it: rows_kernel multiplies it as it comes, in registers.
+//
+// Other small ones run on the fp32 units too: the cutting would cost more than it gains. A CTA of 256 threads makes a tile of BM x 128 sums, BM / 16 x 8 of them in each thread's registers as packed pairs (one
 // instruction multiplies and adds two). Slices of 16 along l go through shared memory, the next one loaded to registers
 // while one is multiplied. Where the tiles are fewer than the SMs, l is cut among the CTAs of a cluster; each leaves its
 // sums in its own shared memory and then adds up and finishes its share of the rows, in the cluster's order: no atomics,
@@ -257,6 +258,217 @@ __global__ void __launch_bounds__(kUnits, 2) simt_kernel(const Args a) {
       }
     }
     finish4(a, i0 + row, j0 + lane * 4, v);
+  }
+  if (shares > 1) cluster_sync();  // nobody leaves while its sums are read
+}
+
+// ----------------------------------------------------------------- few rows ---
+
+// One sum (i, j) to what the call returns; the warp holds 32 neighbouring columns from a multiple of 32 on.
+__device__ __forceinline__ void finish1(const Args& a, int64_t i, int64_t j, float v) {
+  const Product& p = a.p;
+  const bool there = i < p.I && j < p.J;
+  if (p.mode == kForward) {
+    if (p.bias && there) v += ((const float*)p.bias)[j];
+    if (p.q) {
+      const uint32_t ex =
+          pack_exponent(__reduce_max_sync(0xFFFFFFFFu, there ? __float_as_uint(fabsf(v)) : 0u));
+      if (there) {
+        p.q[i * p.ldq + j] = (int8_t)pack_one(v, ex);
+        if (j % kGroup == 0) p.e[i * p.lde + j / kGroup] = (uint8_t)ex;
+      }
+    }
+    if (!there) return;
+    SMAT_WITH_ACT(p.act, v = act_value<ACT>(v))
+    if (p.residual) v += ((const float*)p.residual)[i * p.ldr + j];
+  } else {
+    if (!there) return;
+    if (p.act != SMAT_ACT_NONE) {
+      const float h = (float)p.q[i * p.ldq + j] * unpack_scale(p.e[i * p.lde + j / kGroup]);
+      SMAT_WITH_ACT(p.act, v *= act_slope<ACT>(h))
+    }
+  }
+  ((float*)p.out)[i * p.ldo + j] = v;
+}
+
+constexpr int kRowWarps = 8;
+// Rows up to which it is taken (4096 x 4096: 16 rows 28 us forward and 24 us back; 32 rows would be 65 and 81 us, cut for the
+// tensor cores they are 58 and 55).
+constexpr int kFewRows = 16;
+
+// A product of at most R rows with a weight that is read once, where the copies bound it (rows 1 of 4096 x 4096: 67 MB).
+// The sum is cut among the CTAs of a cluster; each leaves its share in shared memory, the cluster adds the shares in order.
+//
+// Forward: y(i, j) sums along W's row j. A CTA has 32 rows of W, a warp four of them; a lane multiplies 4 neighbours of
+// each with those of every row of x, which the warps share, and the lanes' sums are added at the end.
+// grad_input: dx(i, j) sums down W's column j. A CTA has 128 columns, a lane four neighbours; its warps take every eighth
+// row of W, whose factors dy(i, l) are the same for all lanes, and their sums are added at the end.
+template <int MODE, int R, bool VEC>
+__global__ void __launch_bounds__(32 * kRowWarps, 2) rows_kernel(const Args a) {
+  constexpr int kCols = MODE == kForward ? 32 : 128;  // of the result, per CTA
+  constexpr int kWays = 4, kAtOnce = R < 8 ? R : 8;  // how the warps' sums of grad_input meet, see below
+  constexpr int kChunk = 256, kFactorRow = R < 4 ? 4 : R + (R > 4 ? 4 : 0);
+  constexpr int kSpace = kWays * kAtOnce * kCols > kChunk * kFactorRow ? kWays * kAtOnce * kCols : kChunk * kFactorRow;
+  __shared__ __align__(16) float share[R][kCols];
+  __shared__ __align__(16) float space[MODE == kForward ? R * kChunk : kSpace];
+  const Product& p = a.p;
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const int64_t j0 = (int64_t)blockIdx.x * kCols;
+  const int64_t l0 = (int64_t)blockIdx.y * a.share, l1 = l0 + a.share < p.L ? l0 + a.share : p.L;
+  const float *x = (const float*)p.a, *w = (const float*)p.b;
+  uint32_t shares;
+  asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(shares));
+
+  float acc[R][4];
+#pragma unroll
+  for (int i = 0; i < R; ++i)
+#pragma unroll
+    for (int t = 0; t < 4; ++t) acc[i][t] = 0.0f;
+
+  if constexpr (MODE == kForward) {
+    const int64_t j = j0 + 4 * warp;
+    if constexpr (R == 1) {  // x from L1: 7.7 us for 4096 x 4096, through shared memory 12.4
+#pragma unroll 2
+      for (int64_t l = l0 + 4 * lane; l < l1; l += 128) {
+        float4 b[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+          b[t] = j + t < p.J ? load4(w + (j + t) * p.ldb + l, l1 - l, VEC) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        const float4 f = load4(x + l, l1 - l, VEC);
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+          acc[0][t] = fmaf(f.x, b[t].x, fmaf(f.y, b[t].y, fmaf(f.z, b[t].z, fmaf(f.w, b[t].w, acc[0][t]))));
+      }
+    }
+    float (*rows)[kChunk] = reinterpret_cast<float (*)[kChunk]>(space);  // of x
+    for (int64_t c0 = R == 1 ? l1 : l0; c0 < l1; c0 += kChunk) {
+      // W's values first: they are on their way while x is put down
+      float4 b[kChunk / 128][4];
+#pragma unroll
+      for (int h = 0; h < kChunk / 128; ++h)
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const int64_t l = c0 + 128 * h + 4 * lane;
+          b[h][t] = j + t < p.J ? load4(w + (j + t) * p.ldb + l, l1 - l, VEC) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        }
+      __syncthreads();
+#pragma unroll 4
+      for (int at = threadIdx.x; at < R * kChunk / 4; at += 32 * kRowWarps) {
+        const int i = at / (kChunk / 4), n = at % (kChunk / 4) * 4;
+        *reinterpret_cast<float4*>(&rows[i][n]) =
+            i < p.I ? load4(x + i * p.lda + c0 + n, l1 - c0 - n, VEC) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      }
+      __syncthreads();
+#pragma unroll
+      for (int h = 0; h < kChunk / 128; ++h)
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+          const float4 f = *reinterpret_cast<const float4*>(&rows[i][128 * h + 4 * lane]);
+#pragma unroll
+          for (int t = 0; t < 4; ++t)
+            acc[i][t] = fmaf(f.x, b[h][t].x, fmaf(f.y, b[h][t].y, fmaf(f.z, b[h][t].z, fmaf(f.w, b[h][t].w, acc[i][t]))));
+        }
+    }
+    // the lanes' sums: kSums at a time, each step halves what a lane still holds
+    constexpr int kSums = 4 * R < 32 ? 4 * R : 32;
+#pragma unroll
+    for (int i0 = 0; i0 < R; i0 += kSums / 4) {
+      float v[kSums];
+#pragma unroll
+      for (int t = 0; t < kSums; ++t) v[t] = acc[i0 + t / 4][t % 4];
+#pragma unroll
+      for (int d = 16; d >= kSums; d /= 2)
+#pragma unroll
+        for (int t = 0; t < kSums; ++t) v[t] += __shfl_xor_sync(0xFFFFFFFFu, v[t], d);
+#pragma unroll
+      for (int d = kSums / 2; d > 0; d /= 2) {
+        const bool high = lane & d;
+#pragma unroll
+        for (int t = 0; t < d; ++t) {
+          const float give = high ? v[t] : v[t + d], keep = high ? v[t + d] : v[t];
+          v[t] = keep + __shfl_xor_sync(0xFFFFFFFFu, give, d);
+        }
+      }
+      if (lane < kSums) share[i0 + lane / 4][4 * warp + lane % 4] = v[0];
+    }
+  } else {
+    const int64_t j = j0 + 4 * lane;
+    constexpr int kAhead = 8;  // rows of W in flight per warp
+    // factors of kChunk rows of W, [row of W][row of dy]
+    float (*factor)[kFactorRow] = reinterpret_cast<float (*)[kFactorRow]>(space);
+    for (int64_t c0 = l0; c0 < l1; c0 += kChunk) {
+      const int rows = (int)(l1 - c0 < kChunk ? l1 - c0 : kChunk);
+      __syncthreads();
+      for (int at = threadIdx.x; at < R * kChunk; at += 32 * kRowWarps) {
+        const int i = at / kChunk, n = at % kChunk;
+        factor[n][i] = i < p.I && n < rows ? x[i * p.lda + c0 + n] : 0.0f;
+      }
+      __syncthreads();
+      for (int n0 = warp; n0 < rows; n0 += kAhead * kRowWarps) {
+        float4 b[kAhead];
+#pragma unroll
+        for (int h = 0; h < kAhead; ++h) {
+          const int n = n0 + h * kRowWarps;
+          b[h] = n < rows ? load4(w + (c0 + n) * p.ldb + j, p.J - j, VEC) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        }
+#pragma unroll
+        for (int h = 0; h < kAhead; ++h) {
+          const int n = n0 + h * kRowWarps < kChunk ? n0 + h * kRowWarps : 0;  // past the last row: times 0
+          float f[R < 4 ? 4 : R];
+#pragma unroll
+          for (int i = 0; i < R; i += 4) *reinterpret_cast<float4*>(f + i) = *reinterpret_cast<const float4*>(&factor[n][i]);
+#pragma unroll
+          for (int i = 0; i < R; ++i) {
+            acc[i][0] = fmaf(f[i], b[h].x, acc[i][0]), acc[i][1] = fmaf(f[i], b[h].y, acc[i][1]);
+            acc[i][2] = fmaf(f[i], b[h].z, acc[i][2]), acc[i][3] = fmaf(f[i], b[h].w, acc[i][3]);
+          }
+        }
+      }
+    }
+    float (*more)[kAtOnce][kCols] = reinterpret_cast<float (*)[kAtOnce][kCols]>(space);
+    // the warps' sums, up to 8 rows at a time: a first half of the warps leaves its sums, the other adds its own; then
+    // they are added up in order
+#pragma unroll
+    for (int i0 = 0; i0 < R; i0 += kAtOnce) {
+      __syncthreads();
+      if (warp < kWays)
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i)
+          *reinterpret_cast<float4*>(&more[warp][i][4 * lane]) =
+              make_float4(acc[i0 + i][0], acc[i0 + i][1], acc[i0 + i][2], acc[i0 + i][3]);
+      __syncthreads();
+      if (warp >= kWays)
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+          float4* at = reinterpret_cast<float4*>(&more[warp - kWays][i][4 * lane]);
+          const float4 t = *at;
+          *at = make_float4(t.x + acc[i0 + i][0], t.y + acc[i0 + i][1], t.z + acc[i0 + i][2], t.w + acc[i0 + i][3]);
+        }
+      __syncthreads();
+      for (int at = threadIdx.x; at < kAtOnce * kCols; at += 32 * kRowWarps) {
+        float v = 0.0f;
+#pragma unroll
+        for (int h = 0; h < kWays; ++h) v += more[h][at / kCols][at % kCols];
+        share[i0 + at / kCols][at % kCols] = v;
+      }
+    }
+  }
+  if (shares > 1)
+    cluster_sync();
+  else
+    __syncthreads();
+  // blocks of 32 columns of a row go around among the cluster's CTAs and their warps
+  constexpr int kBlocks = kCols / 32;
+  for (int at = (int)blockIdx.y * kRowWarps + warp; at < (int)p.I * kBlocks; at += (int)shares * kRowWarps) {
+    const int i = at / kBlocks, c = at % kBlocks * 32 + lane;
+    float v = 0.0f;
+    if (shares == 1) {
+      v = share[i][c];
+    } else {
+#pragma unroll 8
+      for (uint32_t s = 0; s < shares; ++s) v += cluster_load(&share[i][c], s);
+    }
+    finish1(a, i, j0 + c, v);
   }
   if (shares > 1) cluster_sync();  // nobody leaves while its sums are read
 }
@@ -594,6 +806,32 @@ cudaError_t launch_simt_tile(Args a, int sms, cudaStream_t s) {
   return cudaLaunchKernelEx(&cfg, f, a);
 }
 
+template <int MODE, int R, bool VEC>
+cudaError_t launch_rows_as(Args a, int sms, cudaStream_t s) {
+  constexpr int kCols = MODE == kForward ? 32 : 128;
+  const int64_t tiles = (a.p.J + kCols - 1) / kCols;
+  // four CTAs' worth of warps per SM, a share at least 256 long
+  int shares = 1;
+  while (shares < 8 && tiles * shares * 2 <= 4 * sms && a.p.L >= (int64_t)shares * 2 * 256) shares *= 2;
+  a.share = (a.p.L + shares * 128 - 1) / (shares * 128) * 128;
+  cudaLaunchAttribute at;
+  const cudaLaunchConfig_t cfg = config(dim3((unsigned)tiles, (unsigned)shares), 32 * kRowWarps, 0,
+                                        dim3(1, (unsigned)shares, 1), &at, s);
+  return cudaLaunchKernelEx(&cfg, rows_kernel<MODE, R, VEC>, a);
+}
+template <int MODE, int R>
+cudaError_t launch_rows_of(const Args& a, int sms, cudaStream_t s) {
+  return (MODE == kForward ? a.va && a.vb : a.vb) ? launch_rows_as<MODE, R, true>(a, sms, s)
+                                                  : launch_rows_as<MODE, R, false>(a, sms, s);
+}
+template <int MODE>
+cudaError_t launch_rows(const Product& p, int sms, cudaStream_t s) {
+  const Args a = args_of(p);
+  if (p.I <= 1) return launch_rows_of<MODE, 1>(a, sms, s);
+  if (p.I <= 4) return launch_rows_of<MODE, 4>(a, sms, s);
+  return launch_rows_of<MODE, 16>(a, sms, s);
+}
+
 template <bool A_MN, bool B_MN>
 cudaError_t launch_simt(const Product& p, int sms, cudaStream_t s) {
   const Args a = args_of(p);
@@ -691,7 +929,7 @@ cudaError_t launch_tc32(const Product& p, int sms, char* workspace, cudaStream_t
 
 // Whether cutting the operands pays.
 bool on_tensor_cores(const Product& p) {
-  return p.L > 0 && p.I > 32 && (double)p.I * (double)p.J * (double)p.L >= 1 << 25;
+  return p.L > 0 && (p.I > kFewRows || p.mode == kGradWeight) && (double)p.I * (double)p.J * (double)p.L >= 1 << 25;
 }
 
 }  // namespace
@@ -710,11 +948,15 @@ cudaError_t f32_workspace(const Product& p, int sms, size_t* bytes) {
 cudaError_t launch_f32(const Product& p, int sms, void* workspace, cudaStream_t s) {
   const bool tc = on_tensor_cores(p);
   char* w = (char*)workspace;
-  switch (p.mode) {
-    case kForward: return tc ? launch_tc32<false, false>(p, sms, w, s) : launch_simt<false, false>(p, sms, s);
-    case kGradInput: return tc ? launch_tc32<false, true>(p, sms, w, s) : launch_simt<false, true>(p, sms, s);
-    default: return tc ? launch_tc32<true, true>(p, sms, w, s) : launch_simt<true, true>(p, sms, s);
+  if (p.mode == kForward) {
+    if (p.I <= kFewRows) return launch_rows<kForward>(p, sms, s);
+    return tc ? launch_tc32<false, false>(p, sms, w, s) : launch_simt<false, false>(p, sms, s);
   }
+  if (p.mode == kGradInput) {
+    if (p.I <= kFewRows) return launch_rows<kGradInput>(p, sms, s);
+    return tc ? launch_tc32<false, true>(p, sms, w, s) : launch_simt<false, true>(p, sms, s);
+  }
+  return tc ? launch_tc32<true, true>(p, sms, w, s) : launch_simt<true, true>(p, sms, s);
 }
 
 }  // namespace lin
