@@ -264,31 +264,58 @@ __global__ void __launch_bounds__(kUnits, 2) simt_kernel(const Args a) {
 
 // ----------------------------------------------------------------- few rows ---
 
-// One sum (i, j) to what the call returns; the warp holds 32 neighbouring columns from a multiple of 32 on.
-__device__ __forceinline__ void finish1(const Args& a, int64_t i, int64_t j, float v) {
+// Column j of rows i .. i + N - 1 to what the call returns; the warp holds 32 neighbouring columns from a multiple of 32 on.
+// What the rows read is asked for first, all of it.
+template <int N>
+__device__ __forceinline__ void finish_column(const Args& a, int64_t i, int64_t j, float (&v)[N]) {
   const Product& p = a.p;
-  const bool there = i < p.I && j < p.J;
-  if (p.mode == kForward) {
-    if (p.bias && there) v += ((const float*)p.bias)[j];
+  if (i >= p.I) return;
+  const bool there = j < p.J;
+  const int mine = there ? (int)(p.I - i < N ? p.I - i : N) : 0;
+  float* out = (float*)p.out + i * p.ldo + j;
+  const bool forward = p.mode == kForward, slope = p.mode == kGradInput && p.act != SMAT_ACT_NONE;
+  const float* from = forward ? (const float*)p.residual : p.accumulate ? (const float*)p.out : nullptr;
+  const int64_t ld = forward ? p.ldr : p.ldo;
+  float x[N];
+  if (from) {
+#pragma unroll
+    for (int t = 0; t < N; ++t) x[t] = t < mine ? from[(i + t) * ld + j] : 0.0f;
+  }
+  if (slope) {
+    int qs[N];
+    uint32_t es[N];
+#pragma unroll
+    for (int t = 0; t < N; ++t) {
+      qs[t] = t < mine ? p.q[(i + t) * p.ldq + j] : 0;
+      es[t] = t < mine ? p.e[(i + t) * p.lde + j / kGroup] : 0;
+    }
+#pragma unroll
+    for (int t = 0; t < N; ++t) x[t] = (float)qs[t] * unpack_scale(es[t]);
+    SMAT_WITH_ACT(p.act, _Pragma("unroll") for (int t = 0; t < N; ++t) v[t] *= act_slope<ACT>(x[t]))
+  }
+  if (forward) {
+    const float bias = p.bias && there ? ((const float*)p.bias)[j] : 0.0f;
+#pragma unroll
+    for (int t = 0; t < N; ++t) v[t] += bias;
     if (p.q) {
-      const uint32_t ex =
-          pack_exponent(__reduce_max_sync(0xFFFFFFFFu, there ? __float_as_uint(fabsf(v)) : 0u));
-      if (there) {
-        p.q[i * p.ldq + j] = (int8_t)pack_one(v, ex);
-        if (j % kGroup == 0) p.e[i * p.lde + j / kGroup] = (uint8_t)ex;
+#pragma unroll
+      for (int t = 0; t < N; ++t) {
+        const uint32_t ex = pack_exponent(__reduce_max_sync(0xFFFFFFFFu, there ? __float_as_uint(fabsf(v[t])) : 0u));
+        if (t < mine) {
+          p.q[(i + t) * p.ldq + j] = (int8_t)pack_one(v[t], ex);
+          if (j % kGroup == 0) p.e[(i + t) * p.lde + j / kGroup] = (uint8_t)ex;
+        }
       }
     }
-    if (!there) return;
-    SMAT_WITH_ACT(p.act, v = act_value<ACT>(v))
-    if (p.residual) v += ((const float*)p.residual)[i * p.ldr + j];
-  } else {
-    if (!there) return;
-    if (p.act != SMAT_ACT_NONE) {
-      const float h = (float)p.q[i * p.ldq + j] * unpack_scale(p.e[i * p.lde + j / kGroup]);
-      SMAT_WITH_ACT(p.act, v *= act_slope<ACT>(h))
-    }
+    SMAT_WITH_ACT(p.act, _Pragma("unroll") for (int t = 0; t < N; ++t) v[t] = act_value<ACT>(v[t]))
   }
-  ((float*)p.out)[i * p.ldo + j] = v;
+  if (from) {
+#pragma unroll
+    for (int t = 0; t < N; ++t) v[t] += x[t];
+  }
+#pragma unroll
+  for (int t = 0; t < N; ++t)
+    if (t < mine) out[t * p.ldo] = v[t];
 }
 
 constexpr int kRowWarps = 8;
@@ -461,24 +488,32 @@ __global__ void __launch_bounds__(32 * kRowWarps, 2) rows_kernel(const Args a) {
   constexpr int kBlocks = kCols / 32;
   for (int at = (int)blockIdx.y * kRowWarps + warp; at < (int)p.I * kBlocks; at += (int)shares * kRowWarps) {
     const int i = at / kBlocks, c = at % kBlocks * 32 + lane;
-    float v = 0.0f;
+    float v[1] = {0.0f};
     if (shares == 1) {
-      v = share[i][c];
+      v[0] = share[i][c];
     } else {
 #pragma unroll 8
-      for (uint32_t s = 0; s < shares; ++s) v += cluster_load(&share[i][c], s);
+      for (uint32_t s = 0; s < shares; ++s) v[0] += cluster_load(&share[i][c], s);
     }
-    finish1(a, i, j0 + c, v);
+    finish_column(a, i, j0 + c, v);
   }
   if (shares > 1) cluster_sync();  // nobody leaves while its sums are read
 }
 
 // ------------------------------------------------------------ tensor cores ---
 
+// A tile has 128 columns j of the result along tensor memory's rows and `width` of its rows i along the columns, 32 to 160,
+// so that its sums fit in the registers of the warps that add them up and 515 rows need no fifth tile of 128. A warp then
+// holds 32 neighbouring columns of a row, 128 bytes.
 constexpr int kParts = 3;
-constexpr int kPart = kBM * kBK * 2;                // a slice of one part of one operand
-constexpr int kStage = 2 * kParts * kPart, kStages = 2;
+constexpr int kPart = kBM * kBK * 2;  // a slice of one part of the operand along the tile's rows
+constexpr int kMostWidth = 160, kStages = 2;
+constexpr int kBlock = 16, kMostBlocks = kMostWidth / kBlock / 2;  // of a warp's sums
+// a part of the columns' operand; 64 columns at a time, the last 64 reach past 160
+constexpr int kMostPartB = kMostWidth * kBK * 2;
+constexpr int kStage = kParts * (kPart + kMostPartB);
 constexpr int kTcBytes = kStages * kStage + 1024;
+constexpr int kSums = 256;  // columns of tensor memory apart
 static_assert(kSimtBytes<128> <= kStages * kStage, "a tile on the fp32 units takes the ring's place");
 
 // One operand to cut: fp32 [rows, cols] to parts [3][rows][ldp] of bf16.
@@ -534,28 +569,10 @@ __global__ void __launch_bounds__(256) cut_kernel(const Cut a, const Cut b, int 
   if (threadIdx.x == 0) flags[blockIdx.x] = any;
 }
 
-// A warp's 32 x 32 sums from (i, j) on, a row per thread: through shared memory, so that 8 lanes finish 4 columns each of
-// a row. A row's eight quadruples lie in an order of its own, so that neither side's accesses meet in a bank.
-__device__ __forceinline__ void finish_block(const Args& a, int64_t i, int64_t j, const float (&v)[32], float* turn) {
-  if (i >= a.p.I || j >= a.p.J) return;
-  const int lane = threadIdx.x % 32;
-  __syncwarp();
-#pragma unroll
-  for (int t = 0; t < 32; t += 4)
-    *reinterpret_cast<float4*>(turn + lane * 32 + (t ^ (lane % 8 * 4))) = make_float4(v[t], v[t + 1], v[t + 2], v[t + 3]);
-  __syncwarp();
-#pragma unroll 2
-  for (int t = 0; t < 32; t += 4) {
-    const int row = t + lane / 8, col = lane % 8 * 4;
-    const float4 f = *reinterpret_cast<const float4*>(turn + row * 32 + (col ^ (row % 8 * 4)));
-    float x[4] = {f.x, f.y, f.z, f.w};
-    finish4(a, i + row, j + col, x);
-  }
-}
-
 struct TcArgs {
   Args f;
-  int64_t tiles, tiles_r, tiles_c;
+  int64_t tiles, tiles_r, tiles_c;  // of 128 columns j, of `width` rows i
+  int width;
   int slices, share;  // slices of 64, and those of a CTA of a cluster
   float* parts;       // shares of sums
   const uint32_t* flags;
@@ -563,15 +580,15 @@ struct TcArgs {
   int* errors;
 };
 
-// The six products of a slice, small ones first: (part of A, part of B)
+// The six products of a slice, small ones first: (part of the rows' operand, part of the columns')
 __device__ constexpr int kOrder[6][2] = {{2, 0}, {0, 2}, {1, 1}, {1, 0}, {0, 1}, {0, 0}};
 
+// A: the operand of j (the product's b), B: that of i (its a)
 template <bool A_MN, bool B_MN>
 __global__ void __launch_bounds__(kThreads, 1)
     f32_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                const __grid_constant__ TcArgs a) {
   extern __shared__ uint8_t raw[];
-  __shared__ __align__(16) float turns[kEpiWarps][32 * 32];
   __shared__ __align__(8) uint64_t bars[2 * kStages + 5];
   __shared__ uint32_t tmem_at;
   __shared__ int dead_flag;
@@ -605,7 +622,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   __syncwarp();
   if (warp == kMmaWarp) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_address(&tmem_at)),
-                 "r"(2 * kBN)
+                 "r"(2 * kSums)
                  : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
     fence_before();
@@ -617,39 +634,42 @@ __global__ void __launch_bounds__(kThreads, 1)
   const uint32_t tmem = tmem_at;
 
   if (odd) {
-    // an infinity or NaN in an operand: the cluster's first CTA makes the tile on the fp32 units
-    if (warp < kEpiWarps && rank == 0) {
+    // an infinity or NaN in an operand: all CTAs make tiles of 128 x 128 on the fp32 units
+    if (warp < kEpiWarps) {
       float* sums = reinterpret_cast<float*>(ring);
-      for (int64_t tile = first_tile; tile < a.tiles; tile += step) {
-        int64_t tr, tc;
-        tile_place<16>(a.tiles_r, a.tiles_c, tile, tr, tc);
-        simt_sums<128, A_MN, B_MN>(a.f, sums, tr * kBM, tc * kBN, 0, p.L);
+      const int64_t ti = (p.I + kBM - 1) / kBM, tj = (p.J + kBN - 1) / kBN;
+      for (int64_t tile = blockIdx.x; tile < ti * tj; tile += gridDim.x) {
+        const int64_t i0 = tile % ti * kBM, j0 = tile / ti * kBN;
+        simt_sums<128, B_MN, A_MN>(a.f, sums, i0, j0, 0, p.L);
         units_sync();
-        for (int row = warp; row < kBM && tr * kBM + row < p.I; row += 8) {
+        for (int row = warp; row < kBM && i0 + row < p.I; row += 8) {
           const float4 t = *reinterpret_cast<const float4*>(sums + row * kBN + lane * 4);
           float v[4] = {t.x, t.y, t.z, t.w};
-          finish4(a.f, tr * kBM + row, tc * kBN + lane * 4, v);
+          finish4(a.f, i0 + row, j0 + lane * 4, v);
         }
         units_sync();
       }
     }
   } else if (warp == kTmaWarp && lane == 0) {
+    // a part of the columns' operand: rows of the tile's width, or 64 columns of it at a time
+    const int blocks_b = B_MN ? (a.width + 63) / 64 : 1;
+    const int part_b = B_MN ? blocks_b * 8192 : a.width * kBK * 2;
     uint32_t n = 0;
     bool ok = true;
     for (int64_t tile = first_tile; ok && tile < a.tiles; tile += step) {
       int64_t tr, tc;
       tile_place<16>(a.tiles_r, a.tiles_c, tile, tr, tc);
-      const int r0 = (int)(tr * kBM), c0 = (int)(tc * kBN);
+      const int r0 = (int)(tr * kBM), c0 = (int)(tc * a.width);
       for (int k = 0; k < slices; ++k, ++n) {
         const uint32_t s = n % kStages;
         ok = bar_wait(empty + 8 * s, (n / kStages + 1) & 1, dead, a.errors);
         if (!ok) break;
         const int l = (slice0 + k) * kBK;
         const uint32_t bar = full + 8 * s, to = smem_address(ring) + s * kStage;
-        bar_expect(bar, kStage);
+        bar_expect(bar, kParts * (kPart + part_b));
 #pragma unroll
         for (int q = 0; q < kParts; ++q) {
-          const uint32_t to_a = to + q * kPart, to_b = to + (kParts + q) * kPart;
+          const uint32_t to_a = to + q * kPart, to_b = to + kParts * kPart + q * kMostPartB;
           if (A_MN) {
             tma_load3(to_a, &map_a, r0, l, q, bar);
             tma_load3(to_a + 8192, &map_a, r0 + 64, l, q, bar);
@@ -657,8 +677,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             tma_load3(to_a, &map_a, l, r0, q, bar);
           }
           if (B_MN) {
-            tma_load3(to_b, &map_b, c0, l, q, bar);
-            tma_load3(to_b + 8192, &map_b, c0 + 64, l, q, bar);
+            for (int b = 0; b < blocks_b; ++b) tma_load3(to_b + 8192 * b, &map_b, c0 + 64 * b, l, q, bar);
           } else {
             tma_load3(to_b, &map_b, l, c0, q, bar);
           }
@@ -672,12 +691,12 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       }
   } else if (warp == kMmaWarp && lane == 0) {
-    constexpr uint32_t kInst = kInstruction<A_MN, B_MN, kBN>;
+    const uint32_t inst = kInstruction<A_MN, B_MN, 0> | (uint32_t)(a.width >> 3) << 17;
     uint32_t n = 0;
     bool ok = true;
     for (int64_t tile = first_tile; ok && tile < a.tiles; tile += step)
       for (int k = 0; k < slices; ++k, ++n) {
-        const uint32_t s = n % kStages, half = n & 1, sums = tmem + half * kBN;
+        const uint32_t s = n % kStages, half = n & 1, sums = tmem + half * kSums;
         ok = bar_wait(sums_empty + 8 * half, (n / 2 + 1) & 1, dead, a.errors) &&
              bar_wait(full + 8 * s, n / kStages & 1, dead, a.errors);
         if (!ok) break;
@@ -686,10 +705,10 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
         for (int o = 0; o < 6; ++o) {
           const uint64_t da = descriptor<A_MN>(at + kOrder[o][0] * kPart);
-          const uint64_t db = descriptor<B_MN>(at + (kParts + kOrder[o][1]) * kPart);
+          const uint64_t db = descriptor<B_MN>(at + kParts * kPart + kOrder[o][1] * kMostPartB);
 #pragma unroll
           for (int t = 0; t < kBK / 16; ++t)
-            mma(sums, da + t * kStep16<A_MN>, db + t * kStep16<B_MN>, kInst, o > 0 || t > 0);
+            mma(sums, da + t * kStep16<A_MN>, db + t * kStep16<B_MN>, inst, o > 0 || t > 0);
         }
         mma_commit(empty + 8 * s);
         mma_commit(sums_full + 8 * half);
@@ -700,41 +719,45 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
     }
   } else if (warp < kEpiWarps) {
-    // this warp's sums: 32 rows, 64 columns of the tile
-    const int quarter = warp % 4, first = warp / 4 * 64;
-    float* turn = turns[warp];
+    // this warp's sums: 32 rows and half the columns of the tile, 16 columns at a time
+    const int quarter = warp % 4, blocks = a.width / kBlock / 2, first = warp / 4 * blocks;
     uint32_t n = 0;
     bool ok = true;
     for (int64_t tile = first_tile; ok && tile < a.tiles; tile += step) {
       int64_t tr, tc;
       tile_place<16>(a.tiles_r, a.tiles_c, tile, tr, tc);
-      float acc[2][32];
+      float acc[kMostBlocks][kBlock];
 #pragma unroll
-      for (int t = 0; t < 32; ++t) acc[0][t] = acc[1][t] = 0.0f;
+      for (int b = 0; b < kMostBlocks; ++b)
+#pragma unroll
+        for (int t = 0; t < kBlock; ++t) acc[b][t] = 0.0f;
       for (int k = 0; k < slices; ++k, ++n) {
         const uint32_t half = n & 1;
         ok = bar_wait(sums_full + 8 * half, n / 2 & 1, dead, a.errors);
         if (!ok) break;
         fence_after();
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          float v[32];
-          take32(tmem + half * kBN + first + 32 * b + ((uint32_t)(32 * quarter) << 16), v);
+        for (int b = 0; b < kMostBlocks; ++b)
+          if (b < blocks) {
+            float v[kBlock];
+            take16(tmem + half * kSums + kBlock * (first + b) + ((uint32_t)(32 * quarter) << 16), v);
 #pragma unroll
-          for (int t = 0; t < 32; ++t) acc[b][t] += v[t];
-        }
+            for (int t = 0; t < kBlock; ++t) acc[b][t] += v[t];
+          }
         fence_before();
         __syncwarp();
         if (lane == 0) bar_arrive(sums_empty + 8 * half);
       }
-      const int64_t r0 = tr * kBM + 32 * quarter;
+      const int64_t j = tr * kBM + 32 * quarter, i0 = tc * a.width;
       if (shares > 1) {
-        float* part = a.parts + ((size_t)first_tile * shares + rank) * kBN * kBM + 32 * quarter + lane;
+        float* part = a.parts + ((size_t)first_tile * shares + rank) * a.width * kBM + 32 * quarter + lane;
 #pragma unroll
-        for (int b = 0; b < 2; ++b) put_part(part + (first + 32 * b) * kBM, acc[b]);
-      } else if (ok) {
+        for (int b = 0; b < kMostBlocks; ++b)
+          if (b < blocks) put_part(part + kBlock * (first + b) * kBM, acc[b]);
+      } else if (ok && j < p.J) {
 #pragma unroll
-        for (int b = 0; b < 2; ++b) finish_block(a.f, r0, tc * kBN + first + 32 * b, acc[b], turn);
+        for (int b = 0; b < kMostBlocks; ++b)
+          if (b < blocks) finish_column(a.f, i0 + kBlock * (first + b), j + lane, acc[b]);
       }
     }
   }
@@ -746,19 +769,21 @@ __global__ void __launch_bounds__(kThreads, 1)
       int64_t tr, tc;
       tile_place<16>(a.tiles_r, a.tiles_c, first_tile, tr, tc);
       const int quarter = warp % 4;
-      const float* part = a.parts + (size_t)first_tile * shares * kBN * kBM + 32 * quarter + lane;
-      for (int c = (int)rank + (int)shares * (warp / 4); c < kBN / 32; c += 2 * (int)shares) {
-        float v[32];
-        add_parts(shares, v, [&](uint32_t s, int t) { return __ldcg(part + ((size_t)s * kBN + 32 * c + t) * kBM); });
-        finish_block(a.f, tr * kBM + 32 * quarter, tc * kBN + 32 * c, v, turns[warp]);
+      const int64_t j = tr * kBM + 32 * quarter, i0 = tc * a.width;
+      const float* part = a.parts + (size_t)first_tile * shares * a.width * kBM + 32 * quarter + lane;
+      for (int b = (int)rank + (int)shares * (warp / 4); b < a.width / kBlock && i0 + kBlock * b < p.I && j < p.J;
+           b += 2 * (int)shares) {
+        float v[kBlock];
+        add_parts(shares, v, [&](uint32_t s, int t) { return __ldcg(part + ((size_t)s * a.width + kBlock * b + t) * kBM); });
+        finish_column(a.f, i0 + kBlock * b, j + lane, v);
       }
     }
-    cluster_sync();
+    cluster_meet();
   }
   fence_before();
   __syncthreads();
   if (warp == kMmaWarp)
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2 * kBN));
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2 * kSums));
 }
 
 // ------------------------------------------------------------- host side ---
@@ -841,7 +866,7 @@ cudaError_t launch_simt(const Product& p, int sms, cudaStream_t s) {
 // What a product on the tensor cores needs: an operand's parts, flags, shares of sums.
 struct Plan {
   int64_t tiles_r, tiles_c, ctas;
-  int slices, share, shares, cuts_a, cuts_b;
+  int slices, share, shares, width, cuts_a, cuts_b;
   int64_t rows_a, cols_a, ldp_a, rows_b, cols_b, ldp_b;
   size_t bytes_a, bytes_b, bytes_flags, bytes_parts;
   size_t bytes() const { return bytes_a + bytes_b + bytes_flags + bytes_parts; }
@@ -863,25 +888,41 @@ cudaError_t plan_tc(const Product& p, int sms, Plan* plan) {
   const cudaError_t e = allow_shared(f, kTcBytes, allowed);
   if (e != cudaSuccess) return e;
   Plan g = {};
-  g.tiles_r = (p.I + kBM - 1) / kBM;
-  g.tiles_c = (p.J + kBN - 1) / kBN;
   g.slices = (int)((p.L + kBK - 1) / kBK);
-  const int64_t tiles = g.tiles_r * g.tiles_c;
-  int shares = 8;
-  while (shares > 1 && (tiles * shares > sms || g.slices < 3 * shares ||
-                        tiles > clusters_at_once(f, shares, kThreads, kTcBytes, clusters)))
-    --shares;
-  g.share = (g.slices + shares - 1) / shares;
-  g.shares = shares > 1 ? (g.slices + g.share - 1) / g.share : 1;
-  g.ctas = g.shares > 1 ? tiles * g.shares : (tiles < sms ? tiles : sms);
-  g.rows_a = A_MN ? p.L : p.I, g.cols_a = A_MN ? p.I : p.L;
-  g.rows_b = B_MN ? p.L : p.J, g.cols_b = B_MN ? p.J : p.L;
+  g.tiles_r = (p.J + kBM - 1) / kBM;
+  // Width and shares of the sum by the least estimate in cycles: a slice takes the longer of its multiplications (12 per
+  // column) and its copies (48 KB and 384 bytes per column at 45 bytes a cycle, as measured with two slices in flight);
+  // shares are written and read through L2. All clusters of a shared sum run at once.
+  double least = 0;
+  for (int width = kMostWidth; width >= 32; width -= 32) {
+    if (B_MN && width == kMostWidth) continue;  // its third 64 columns would not fit
+    const int64_t tiles_c = (p.I + width - 1) / width, tiles = g.tiles_r * tiles_c;
+    for (int shares = 1; shares <= 8; ++shares) {
+      if (shares > 1 && (tiles * shares > sms || g.slices < 3 * shares ||
+                         tiles > clusters_at_once(f, shares, kThreads, kTcBytes, clusters)))
+        break;
+      const int share = (g.slices + shares - 1) / shares;
+      const double rounds = shares > 1 ? 1.0 : (double)((tiles + sms - 1) / sms);
+      const double copies = (49152.0 + 384.0 * width) / 45.0, slice = 12.0 * width > copies ? 12.0 * width : copies;
+      const double time = rounds * (share * slice + 1000.0 + 20.0 * width) + (shares > 1 ? 3000.0 + 14.0 * width : 0.0);
+      if (g.width == 0 || time < least) {
+        least = time;
+        g.width = width;
+        g.tiles_c = tiles_c;
+        g.share = share;
+        g.shares = shares > 1 ? (g.slices + share - 1) / share : 1;
+        g.ctas = g.shares > 1 ? tiles * g.shares : (tiles < sms ? tiles : sms);
+        g.bytes_parts = g.shares > 1 ? (size_t)tiles * g.shares * width * kBM * sizeof(float) : 0;
+      }
+    }
+  }
+  g.rows_a = A_MN ? p.L : p.J, g.cols_a = A_MN ? p.J : p.L;
+  g.rows_b = B_MN ? p.L : p.I, g.cols_b = B_MN ? p.I : p.L;
   g.ldp_a = (g.cols_a + 31) / 32 * 32, g.ldp_b = (g.cols_b + 31) / 32 * 32;
   g.cuts_a = cuts_of(g.rows_a, g.ldp_a, sms), g.cuts_b = cuts_of(g.rows_b, g.ldp_b, sms);
   g.bytes_a = up((size_t)kParts * g.rows_a * g.ldp_a * 2);
   g.bytes_b = up((size_t)kParts * g.rows_b * g.ldp_b * 2);
   g.bytes_flags = up(sizeof(uint32_t) * (g.cuts_a + g.cuts_b));
-  g.bytes_parts = g.shares > 1 ? (size_t)tiles * g.shares * kBN * kBM * sizeof(float) : 0;
   *plan = g;
   return cudaSuccess;
 }
@@ -907,16 +948,16 @@ cudaError_t launch_tc32(const Product& p, int sms, char* workspace, cudaStream_t
   if (e != cudaSuccess) return e;
   a.f = args_of(p);
   char *pa = workspace, *pb = pa + g.bytes_a, *pf = pb + g.bytes_b;
-  const Cut ca = {(const float*)p.a, (uint16_t*)pa, g.rows_a, g.cols_a, p.lda, g.ldp_a, a.f.va};
-  const Cut cb = {(const float*)p.b, (uint16_t*)pb, g.rows_b, g.cols_b, p.ldb, g.ldp_b, a.f.vb};
+  const Cut ca = {(const float*)p.b, (uint16_t*)pa, g.rows_a, g.cols_a, p.ldb, g.ldp_a, a.f.vb};
+  const Cut cb = {(const float*)p.a, (uint16_t*)pb, g.rows_b, g.cols_b, p.lda, g.ldp_b, a.f.va};
   a.flags = (const uint32_t*)pf;
   a.n_flags = g.cuts_a + g.cuts_b;
   a.parts = (float*)(pf + g.bytes_flags);
   a.tiles_r = g.tiles_r, a.tiles_c = g.tiles_c, a.tiles = g.tiles_r * g.tiles_c;
-  a.slices = g.slices, a.share = g.share;
+  a.slices = g.slices, a.share = g.share, a.width = g.width;
   CUtensorMap ma, mb;
   if (!encode_parts(&ma, pa, g.cols_a, g.rows_a, g.ldp_a, A_MN ? kBK : kBM) ||
-      !encode_parts(&mb, pb, g.cols_b, g.rows_b, g.ldp_b, B_MN ? kBK : kBN))
+      !encode_parts(&mb, pb, g.cols_b, g.rows_b, g.ldp_b, B_MN ? kBK : g.width))
     return cudaErrorNotSupported;
   cut_kernel<<<g.cuts_a + g.cuts_b, 256, 0, s>>>(ca, cb, g.cuts_a, (uint32_t*)pf);
   e = cudaGetLastError();
@@ -939,7 +980,7 @@ cudaError_t f32_workspace(const Product& p, int sms, size_t* bytes) {
   if (!on_tensor_cores(p)) return cudaSuccess;
   Plan g;
   const cudaError_t e = p.mode == kForward     ? plan_tc<false, false>(p, sms, &g)
-                        : p.mode == kGradInput ? plan_tc<false, true>(p, sms, &g)
+                        : p.mode == kGradInput ? plan_tc<true, false>(p, sms, &g)
                                                : plan_tc<true, true>(p, sms, &g);
   if (e == cudaSuccess) *bytes = g.bytes();
   return e;
@@ -954,7 +995,7 @@ cudaError_t launch_f32(const Product& p, int sms, void* workspace, cudaStream_t 
   }
   if (p.mode == kGradInput) {
     if (p.I <= kFewRows) return launch_rows<kGradInput>(p, sms, s);
-    return tc ? launch_tc32<false, true>(p, sms, w, s) : launch_simt<false, true>(p, sms, s);
+    return tc ? launch_tc32<true, false>(p, sms, w, s) : launch_simt<false, true>(p, sms, s);
   }
   return tc ? launch_tc32<true, true>(p, sms, w, s) : launch_simt<true, true>(p, sms, s);
 }
