@@ -92,7 +92,7 @@ struct Prepare {
     void* to;
     int64_t rows, cols, ldq, lde, ldto;
     int ctas;
-    bool vq;
+    bool whole;  // q's rows start on 16 bytes
   } unpack;
   struct Sums {  // [shares][cols]: of every column over the rows of a share
     const void* dy;
