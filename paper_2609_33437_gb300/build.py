@@ -18,7 +18,7 @@ LIB = os.path.join(PKG, "libsmat.so")
 SOURCES = ["smat_fused_bf16.cu", "smat_fused_f32.cu", "smat_sim_bf16.cu", "smat_sim_f32.cu",
            "smat_inplace_bf16.cu", "smat_inplace_f32.cu", "smat_inplace_sim_bf16.cu", "smat_inplace_sim_f32.cu",
            "smat_laplace_bf16.cu", "smat_laplace_f32.cu", "smat_merge.cu", "smat_gradmap.cu", "smat_aux.cu", "smat_noalloc.cu",
-           "smat_pack8.cu", "smat_linear_f32.cu", "smat_linear_tc.cu", "smat_linear_host.cpp", "smat_host.cpp"]
+           "smat_pack8.cu", "smat_linear_f32.cu", "smat_linear_tc.cu", "smat_linear_outer.cu", "smat_linear_host.cpp", "smat_host.cpp"]
 # The forward and gradient-map units are compiled a second time with
 # SMAT_DRAW16 defined: the launchers of the 16-bit draw option (suffix _d16).
 DRAW16_SOURCES = ["smat_fused_bf16.cu", "smat_fused_f32.cu", "smat_sim_bf16.cu", "smat_sim_f32.cu",

@@ -173,8 +173,12 @@ Operands operands(const smat_grad_input_args* g) {
   return {operand(g->dy, g->rows, g->n, g->lddy, g->dtype), operand(g->w, g->n, g->k, g->ldw, g->dtype), 0,
           parts_of(kGradInput, g->dtype, g->rows, g->k, g->n)};
 }
+// Whether a weight gradient is written row by row of it, without a product's tiles (at least one row of dy).
+bool few_rows(const smat_grad_weight_args* g) {
+  return g->rows >= 1 && g->rows <= (g->dtype == SMAT_BF16 ? kOuterRowsBf16 : kOuterRows);
+}
 Operands operands(const smat_grad_weight_args* g) {
-  if (g->k == 0 || g->n == 0 || g->rows == 0) return {};
+  if (g->k == 0 || g->n == 0 || g->rows == 0 || few_rows(g)) return {};
   Operands o = {operand(g->dy, g->rows, g->n, g->lddy, g->dtype), {}, 0,
                 parts_of(kGradWeight, g->dtype, g->n, g->k, g->rows)};
   if (g->q)
@@ -345,6 +349,11 @@ static smat_status grad_weight(const smat_grad_weight_args* a, void* d_workspace
   int sms = 1;
   st = device_sms(&sms);
   if (st != SMAT_OK) return st;
+  if (k > 0 && few_rows(a)) {
+    const Outer o = {a->dy, a->x, a->q, a->e, a->dw, a->db, m, k, n, a->lddy, a->ldx, a->ldq, a->lde, a->lddw, a->act,
+                     (a->accumulate & SMAT_ACCUMULATE_DW) != 0, (a->accumulate & SMAT_ACCUMULATE_DB) != 0};
+    return cuda_status(launch_outer(o, a->dtype, sms, stream), "grad_weight launch");
+  }
   const bool bf16 = a->dtype == SMAT_BF16;
   Prepare first = {};
   Product p = {};
