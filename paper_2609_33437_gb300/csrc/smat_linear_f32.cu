@@ -973,9 +973,10 @@ cudaError_t launch_tc32(const Product& p, int sms, char* workspace, cudaStream_t
 }
 
 // Whether cutting the operands pays: not for few rows (rows_kernel), nor for products that start and end as fast as they
-// run (100 x 200 x 300: 11 us as it is; 256 x 512 x 512, 67 M products, 13 us cut).
+// run. Call after call with other operands, cut and as they are: 64 x 1024 x 1024 (gradient of a weight) 9.6 and 8.2 us,
+// 256 x 512 x 512 12.7 and 9.9, 384 x 512 x 512 13.2 and 15.3, 17 x 2048 x 2048 (gradient of a weight) 15.7 and 23.6.
 bool on_tensor_cores(const Product& p) {
-  return p.L > 0 && (p.I > kFewRows || p.mode == kGradWeight) && (double)p.I * (double)p.J * (double)p.L >= 1 << 25;
+  return p.L > 0 && (p.I > kFewRows || p.mode == kGradWeight) && (double)p.I * (double)p.J * (double)p.L > 1 << 26;
 }
 
 }  // namespace

@@ -574,3 +574,16 @@ def test_refusals_leave_outputs_alone():
     assert (out == 5.0).all()
     y = L.linear(x, w, b, out=out)  # and the next call works
     _check_linear(x, w, b, "none", None, y)
+
+
+@pytest.mark.parametrize("rows,k,n", [(64, 1024, 1024), (65, 1024, 1024), (129, 515, 1031)])
+def test_f32_products_around_the_size_from_which_operands_are_cut(rows, k, n):
+    x, w, dy = _rand(1, rows, k, dtype=F32), _rand(2, n, k, dtype=F32), _rand(3, rows, n, dtype=F32)
+    _check_linear(x, w, None, "none", None, L.linear(x, w))
+    _check_grad_input(dy, w, "none", None, L.linear_grad_input(dy, w))
+    _check_grad_weight(dy, _d(x), L.linear_grad_weight(dy, x)[0], None)
+    assert L.poll_errors() == 0
+
+
+def test_f32_infinities_and_nan_just_above_that_size():
+    test_f32_infinities_and_nan_as_in_the_definition(330, 536, 392)
