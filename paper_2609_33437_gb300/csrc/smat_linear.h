@@ -78,8 +78,9 @@ cudaError_t launch_row_sums(const void* dy, int64_t lddy, void* db, int64_t rows
                             int sms, cudaStream_t s);
 
 // A weight gradient over 1 to kOuterRows rows (smat_linear_outer.cu): x, or q and e read through act; db may be NULL. Up to
-// these many it is faster than the products' tiles (4096 x 4096: bf16 one row 7.2 us against 21, 8 rows 18 against 20, with rows
-// off 16 bytes 18 against 37; fp32 one row 12 us against 82, 16 rows 37 against 42).
+// these many it is faster than the products' tiles (4096 x 4096, call after call: bf16 one row 7.0 us against 18, 8 rows 17.6
+// against 18.1, with rows off 16 bytes 18 against 37; fp32 one row 12 us against 80, 16 rows 37 against 38; with nothing in L2
+// 14 against 26, 25.6 against 26.1, 24 against 92, 50 against 61).
 constexpr int64_t kOuterRows = 16, kOuterRowsBf16 = 8;
 struct Outer {
   const void* dy;

@@ -15,12 +15,15 @@
 // Measured: 8192 x 11008 x 4096 with residual 405 us from cold (1,825 TFLOP/s, 94% of cuBLAS's burst, tensor pipe 86% busy)
 // and 446 us call after call, when the power limit holds the clock down; the weight gradient of 4099 x 4096 x 4096 98 us
 // (1,410 TFLOP/s): 256 tiles for 76 pairs are four rounds for 3.4, and L2 hands out 15 TB/s. 2056 x 1024 x 4096 with bias,
-// activation and 8 bits 21 us: two rounds of 1.9, each ended by 10 MB of results at once, and 5 us to start and end.
+// activation and 8 bits 21 us with operands in L2: two rounds of 1.9, each ended by 10 MB of results at once, and some 5 us to
+// start and end.
 //
 // Products of at most 128 rows (narrow_kernel): the tile's 128 rows are columns j and its 32, 64 or 128 columns are rows
 // i, so that a wide weight fills the 128 and the few rows cost a narrow tile. A warp holds 32 neighbouring columns of a
-// row, one per lane. Bound by the weight's bytes: 24 x 4096 x 11008 takes 13 us, 6.9 TB/s; one row of 4096 x 4096 takes
-// 9.4 us, half of them to start, join the shares and end.
+// row, one per lane. With a weight that is not in L2 24 x 4096 x 11008 takes 20.4 us (4.4 TB/s) and one row of 4096 x 4096
+// 12.3 us (2.7 TB/s), with one that is 13.6 and 9.3: the weight's bytes, and some 7 us to launch, start, join the shares and
+// end. 4096 x 4096 in wide tiles takes longer up to 128 rows (weight not in L2: 33 rows 11.5 us and 16.9 wide, 128 rows 14.5
+// and 17.9).
 //
 // Where the tiles are fewer than the SMs, the sum is cut among the CTAs (or pairs) of a cluster: each leaves its share of
 // the sums, then every CTA adds up some of the columns in the cluster's order and finishes them. No atomics, the same
@@ -50,8 +53,9 @@ struct Ring {
 
 constexpr int kPairRows = 2 * kBM, kPairStages = 5, kPairStage = 2 * kBytesA;
 // Warps that finish a pair's sums, and slices on their way. Finishing waits for latencies: with 8 warps 2056 x 1024 x 4096
-// saved in 8 bits takes 2.6 us longer, with 4 9 us, with 16 (96 registers) 1.6 us. With 4 slices 8192 x 11008 x 4096 takes
-// 480 us instead of 446; a sixth gains 2% in weight gradients and leaves no room for 12 warps.
+// saved in 8 bits takes 2.4 us longer, with 4 (and a sixth slice) 9 us, with 16 (96 registers) 1.6 us. With 4 slices
+// 8192 x 11008 x 4096 takes 480 us instead of 446; with a sixth, and 8 warps to make room for it, the weight gradient of
+// 4099 x 4096 x 4096 115 instead of 117, the first MLP layer 29.5 instead of 26.9.
 constexpr int kPairEpi = 12;
 constexpr int kPairThreads = 32 * (kPairEpi + 2);
 // A finishing warp's own shared memory: 32 rows of 32 results (64 bytes, swizzled) and of 32 q (32 bytes, swizzled).

@@ -441,8 +441,8 @@ __global__ void __launch_bounds__(kThreads)
 
 // What a bf16 product on the tensor cores needs done first, in one launch: rows copied to rows that start on 16 bytes, x^
 // read back from 8 bits, and shares of dy's sums over its rows (which the product's kernel adds up). The CTAs are dealt
-// out to the jobs; each walks its job's rows with threads side by side along a row. Copies run at 5 TB/s read and written
-// (9216 x 4292: 33 us); 8224 x 4096 values through quick GELU and the sums of 8224 x 1024 take 26 us for 118 MB.
+// out to the jobs; each walks its job's rows with threads side by side along a row. Copies run at 4 TB/s read and written (9216
+// x 4292: 39 us); 8224 x 4096 values through quick GELU and the sums of 8224 x 1024 take 26 us for 118 MB.
 template <int ACT>
 __global__ void __launch_bounds__(kThreads) prepare_kernel(const Prepare a) {
   __shared__ union {
