@@ -358,22 +358,45 @@ def _row_sums(dy: torch.Tensor) -> torch.Tensor:
     return linear_grad_weight(dy, dy.new_empty(dy.shape[0], 0), bias=True)[1]
 
 
+class _FirstOnly(torch.autograd.Function):
+    """Gradients as they are; going back through them raises. `anchor` and `dy` tie them to all that they depend on, so
+    that a second derivative meets this, whichever of those it is taken by."""
+
+    @staticmethod
+    def forward(ctx, anchor, dy, *grads):
+        return tuple(g.view_as(g) if g is not None else None for g in grads)
+
+    @staticmethod
+    def backward(ctx, *_):
+        raise RuntimeError("Linear8 and Mlp8 have first derivatives only: their gradients cannot be differentiated")
+
+
+def _first_only(anchor, dy, grads):
+    """The backward passes run in the library's kernels and build no graph. Where one is asked for (create_graph), their
+    results refuse to be differentiated; otherwise terms of a second derivative would be left out silently."""
+    return _FirstOnly.apply(anchor, dy, *grads) if torch.is_grad_enabled() else grads
+
+
 class _Linear8(torch.autograd.Function):
+    """(y, anchor): `anchor` is empty and stands for the inputs in _FirstOnly."""
+
     @staticmethod
     def forward(ctx, x, w, b, residual, act):
         ctx.act = act
+        ctx.set_materialize_grads(False)
         need_h = act != "none" and any(ctx.needs_input_grad[:3])
         y = linear(x, w, b, act, residual, save=need_h)
         y, h = y if need_h else (y, None)
         p = pack8(x) if ctx.needs_input_grad[1] else None
-        ctx.save_for_backward(w, *((h.q, h.e) if h else (None, None)), *((p.q, p.e) if p else (None, None)))
-        return y
+        anchor = x.new_empty(0)
+        ctx.save_for_backward(w, *((h.q, h.e) if h else (None, None)), *((p.q, p.e) if p else (None, None)), anchor)
+        return y, anchor
 
     @staticmethod
-    def backward(ctx, dy):
-        w, hq, he, xq, xe = ctx.saved_tensors
+    def backward(ctx, grad, _):
+        w, hq, he, xq, xe, anchor = ctx.saved_tensors
         need_x, need_w, need_b, need_r, _ = ctx.needs_input_grad
-        dy = _rows_like(dy)
+        dy = _rows_like(grad.detach())
         dh = act_grad8(dy, Packed8(hq, he), ctx.act) if hq is not None else dy
         dx = dw = db = None
         if need_x:
@@ -382,25 +405,29 @@ class _Linear8(torch.autograd.Function):
             dw, db = linear_grad_weight(dh, Packed8(xq, xe), bias=need_b)
         elif need_b:
             db = _row_sums(dh)
-        return dx, dw, db, (dy if need_r else None), None
+        return *_first_only(anchor, grad, (dx, dw, db)), (grad if need_r else None), None
 
 
 class _Mlp8(torch.autograd.Function):
+    """As _Linear8."""
+
     @staticmethod
     def forward(ctx, x, w1, b1, w2, b2, residual, act):
         ctx.act = act
+        ctx.set_materialize_grads(False)
         a, h = linear(x, w1, b1, act, save=True)
         y = linear(a, w2, b2, "none", residual)
         p = pack8(x) if ctx.needs_input_grad[1] else None
-        ctx.save_for_backward(w1, w2, *((p.q, p.e) if p else (None, None)), h.q, h.e)
-        return y
+        anchor = x.new_empty(0)
+        ctx.save_for_backward(w1, w2, *((p.q, p.e) if p else (None, None)), h.q, h.e, anchor)
+        return y, anchor
 
     @staticmethod
-    def backward(ctx, dy):
-        w1, w2, xq, xe, hq, he = ctx.saved_tensors
+    def backward(ctx, grad, _):
+        w1, w2, xq, xe, hq, he, anchor = ctx.saved_tensors
         need_x, need_w1, need_b1, need_w2, need_b2, need_r, _ = ctx.needs_input_grad
         h = Packed8(hq, he)
-        dy = _rows_like(dy)
+        dy = _rows_like(grad.detach())
         dx = dw1 = db1 = dw2 = db2 = None
         if need_w2:
             dw2, db2 = linear_grad_weight(dy, h, ctx.act, bias=need_b2)
@@ -414,12 +441,13 @@ class _Mlp8(torch.autograd.Function):
                 db1 = _row_sums(dh)
             if need_x:
                 dx = linear_grad_input(dh, w1)
-        return dx, dw1, db1, dw2, db2, (dy if need_r else None), None
+        return *_first_only(anchor, grad, (dx, dw1, db1, dw2, db2)), (grad if need_r else None), None
 
 
 class Linear8(torch.nn.Linear):
     """torch.nn.Linear followed by an activation and a residual; its backward pass reads the input and, with an
-    activation, the pre-activation in 8 bits instead of keeping them whole."""
+    activation, the pre-activation in 8 bits instead of keeping them whole. First derivatives only: one taken of its
+    gradients raises RuntimeError."""
 
     def __init__(self, in_features: int, out_features: int, bias: bool = True, act: str = "none", device=None,
                  dtype=None):
@@ -430,12 +458,13 @@ class Linear8(torch.nn.Linear):
     def forward(self, x: torch.Tensor, residual: Optional[torch.Tensor] = None) -> torch.Tensor:
         if not torch.is_grad_enabled():
             return linear(x, self.weight, self.bias, self.act, residual)
-        return _Linear8.apply(x, self.weight, self.bias, residual, self.act)
+        return _Linear8.apply(x, self.weight, self.bias, residual, self.act)[0]
 
 
 class Mlp8(torch.nn.Module):
     """y = act(x W1^T + b1) W2^T + b2 + residual. Between forward and backward it holds x and the pre-activation in
-    8 bits, 33 / 32 bytes per element; the second layer's input is recomputed from the pre-activation."""
+    8 bits, 33 / 32 bytes per element; the second layer's input is recomputed from the pre-activation. First
+    derivatives only, as Linear8."""
 
     def __init__(self, features: int, hidden: int, bias: bool = True, act: str = "gelu", device=None, dtype=None):
         super().__init__()
@@ -448,4 +477,4 @@ class Mlp8(torch.nn.Module):
         if not torch.is_grad_enabled():
             a = linear(x, self.fc1.weight, self.fc1.bias, self.act)
             return linear(a, self.fc2.weight, self.fc2.bias, "none", residual)
-        return _Mlp8.apply(x, self.fc1.weight, self.fc1.bias, self.fc2.weight, self.fc2.bias, residual, self.act)
+        return _Mlp8.apply(x, self.fc1.weight, self.fc1.bias, self.fc2.weight, self.fc2.bias, residual, self.act)[0]
