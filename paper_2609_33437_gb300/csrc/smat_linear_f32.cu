@@ -1,10 +1,12 @@
 // The linear layers' products of fp32 matrices, to fp32 accuracy (smat_linear.h, Product; include/smat.h).
 //
-// Large ones run on the tensor cores. A first kernel cuts every fp32 value into three bf16 values, hi + mid + lo, 8 bits
-// of its significand each: exactly the value. The product then is six products of those parts (the three left out are
-// below 2^-24 of the whole, like one rounding), for a slice of 64 of the sum at a time and the small ones first, so that
-// what an addition in tensor memory cuts off is cut off sums that are small yet; eight warps add the slices' sums in
-// registers, rounding to nearest. Measured: 4096 x 4096 x 4096 585 us, 235 TFLOP/s of fp32 products where the fp32 units
+// Large ones run on the tensor cores. A first kernel cuts every fp32 value into three bf16 values, hi + mid + lo, each the
+// nearest to what is left: exactly the value (from 2^-110 on; below, lo's last bits fall under bf16's smallest number, 2^-133).
+// mid is at most 2^-8 and lo 2^-17 of the value's power of two (twice that next to the largest fp32 number), so the three of nine products that are left out, mid lo, lo
+// mid and lo lo, are below 2^-24 (1 + 2^-9) of the whole, like one rounding, and of either sign. The product then is the other
+// six, for a slice of 64 of the sum at a time and the small ones first, so that what an addition in tensor memory cuts off is
+// cut off sums that are small yet (the last four additions of a slice cut off up to 2^-23 of it each); eight warps add the
+// slices' sums in registers, rounding to nearest. Measured: 4096 x 4096 x 4096 585 us, 235 TFLOP/s of fp32 products where the fp32 units
 // reach 75 at most; 515 x 896 x 4864 36 us, 10 of them to cut 19 MB, the rest bound by the copies into shared memory (110 KB
 // for 1,920 cycles of multiplications). Its error against 64 bits there is 1.9e-7, a plain fp32 product's 6.2e-7.
 //
@@ -528,13 +530,22 @@ struct Cut {
   bool vec;  // rows on 16 bytes
 };
 
-// hi and mid are cut off (so that no value rounds up to infinity), lo is what is left: 8 bits at most, exact.
-__device__ __forceinline__ void cut(float x, uint32_t& hi, uint32_t& mid, uint32_t& lo, uint32_t& odd) {
-  hi = __float_as_uint(x) & 0xFFFF0000u;
-  const float r = x - __uint_as_float(hi);
-  mid = __float_as_uint(r) & 0xFFFF0000u;
-  lo = __float_as_uint(r - __uint_as_float(mid));
-  odd |= (__float_as_uint(x) & 0x7F800000u) == 0x7F800000u;
+// Two values' nearest bf16, y's in the upper half; what would round to infinity stays bf16's largest number.
+__device__ __forceinline__ uint32_t nearest2(float x, float y) {
+  uint32_t w;
+  asm("cvt.rn.satfinite.bf16x2.f32 %0, %1, %2;" : "=r"(w) : "f"(y), "f"(x));
+  return w;
+}
+// The parts of two values, in pairs; x and y end as what is left, 0 from 2^-110 on. Cut off instead of rounded, the parts
+// would have the value's sign, and what is left out of a product would be up to 2^-21 of it and always of one sign.
+__device__ __forceinline__ void cut2(float x, float y, uint32_t (&w)[3], uint32_t& odd) {
+  odd |= (__float_as_uint(x) & 0x7F800000u) == 0x7F800000u || (__float_as_uint(y) & 0x7F800000u) == 0x7F800000u;
+#pragma unroll
+  for (int t = 0; t < 3; ++t) {
+    w[t] = nearest2(x, y);
+    x -= __uint_as_float(w[t] << 16);
+    y -= __uint_as_float(w[t] & 0xFFFF0000u);
+  }
 }
 
 // Both operands of a product; flags[CTA]: whether it met an infinity or NaN. A thread cuts 8 neighbours of a row: 32
@@ -558,12 +569,9 @@ __global__ void __launch_bounds__(256) cut_kernel(const Cut a, const Cut b, int 
         uint32_t w[3][4];
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
-          uint32_t h0, m0, l0, h1, m1, l1;
-          cut(v[2 * t], h0, m0, l0, odd);
-          cut(v[2 * t + 1], h1, m1, l1, odd);
-          w[0][t] = __byte_perm(h0, h1, 0x7632);
-          w[1][t] = __byte_perm(m0, m1, 0x7632);
-          w[2][t] = __byte_perm(l0, l1, 0x7632);
+          uint32_t parts[3];
+          cut2(v[2 * t], v[2 * t + 1], parts, odd);
+          w[0][t] = parts[0], w[1][t] = parts[1], w[2][t] = parts[2];
         }
 #pragma unroll
         for (int t = 0; t < 3; ++t)

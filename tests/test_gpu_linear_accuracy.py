@@ -1,0 +1,90 @@
+"""How near the fp32 linear operators come to their definitions in 64 bits, with bounds that follow the arithmetic and not
+the size of the sum, on the GPU.
+
+fp32 products of large matrices are six of the nine products of three bf16 parts (smat_linear_f32.cu). With parts rounded to
+nearest |mid| <= 2^-8 and |lo| <= 2^-17 of a value's power of two, so what is left out, mid lo + lo mid + lo lo, is at most
+2^-24 (1 + 2^-9) of a product. An addition in tensor memory may cut off one unit in the last place, 2^-23 of the partial
+sum; the parts' products come small ones first, so that only the last ones, of hi and hi, are added to sums of full size:
+those before are below 2^-6 of it."""
+
+import pytest
+import torch
+
+from paper_2609_33437_gb300 import linear as L
+
+pytestmark = pytest.mark.gpu
+
+F32 = torch.float32
+U = 2.0 ** -24  # half a unit in the last place, relative
+DROPPED = U * (1 + 2.0 ** -9)
+
+
+@pytest.fixture(autouse=True)
+def _cuda():
+    if not torch.cuda.is_available():
+        pytest.skip("needs a CUDA GPU")
+
+
+def _d(t):
+    return t.double().cpu()
+
+
+def _products(a, b):
+    """forward, input's and weight's gradient, each as [i, l] times [j, l]: (name, result, A, B) of one pair."""
+    return (("linear", L.linear(a, b), a, b),
+            ("grad_input", L.linear_grad_input(a, b.T.contiguous()), a, b),
+            ("grad_weight", L.linear_grad_weight(a.T.contiguous(), b.T.contiguous())[0], a, b))
+
+
+def _single(values_a, values_b, length, at):
+    """[i, length] and [j, length] whose only column that is not 0 is `at`: every result is one product."""
+    a = torch.zeros(len(values_a), length, device="cuda")
+    b = torch.zeros(len(values_b), length, device="cuda")
+    a[:, at], b[:, at] = values_a.cuda(), values_b.cuda()
+    return a, b
+
+
+@pytest.mark.parametrize("length,at", [(600, 7), (1030, 1029), (5000, 2500)])
+def test_f32_single_products(length, at):
+    """One product per result, on the tensor cores (more than 2^26 products): what is left out, and one addition's cut."""
+    g = torch.Generator().manual_seed(length)
+    i, j = 400, 520
+    va = (1 + torch.rand(i, generator=g)) * torch.ldexp(torch.ones(i), torch.randint(-30, 30, (i,), generator=g))
+    vb = (1 + torch.rand(j, generator=g)) * torch.where(torch.rand(j, generator=g) < 0.5, -1.0, 1.0)
+    va[:50] = 1.0078124  # just under a bf16 number: cut off instead of rounded, its parts are 1.0, 0.0078, 3e-5
+    vb[:60] = 1.0078124
+    a, b = _single(va, vb, length, at)
+    ref = va.double()[:, None] * vb.double()[None, :]
+    for name, got, _, _ in _products(a, b):
+        off = ((_d(got) - ref) / ref).abs().max()
+        assert off <= DROPPED + 2 * U * (1 + 2.0 ** -4), (name, float(off) / U)
+    assert L.poll_errors() == 0
+
+
+@pytest.mark.parametrize("value", [1.0078124, 1.5, 1.9960937])
+def test_f32_sums_of_one_sign(value):
+    """Sums whose terms are all alike, so that no error averages out. A slice of 64 adds four times 16 products of hi and hi
+    (each addition cuts off up to 2^-23 of the sum so far: 1/4, 2/4, 3/4 and all of it) after 20 additions below 2^-6; the
+    slices are added with one rounding each, of partial sums 1/S, 2/S, ..., and up to 8 shares."""
+    i, j, length = 300, 300, 1024
+    a = torch.full((i, length), value, device="cuda")
+    b = torch.full((j, length), value, device="cuda")
+    ref = float(length) * float(a[0, 0].double()) ** 2
+    slices = length // 64
+    bound = DROPPED + 2 * U * (2.5 + 20 * 2.0 ** -6) + U * ((slices + 1) / 2 + 8)
+    for name, got, _, _ in _products(a, b):
+        off = float(((_d(got) - ref) / ref).abs().max())
+        assert off <= bound, (name, off / U, bound / U)
+    assert L.poll_errors() == 0
+
+
+def test_f32_products_next_to_the_largest_number():
+    """Parts that are rounded up do not make infinities of products under the largest number."""
+    most = torch.finfo(F32).max
+    for va, vb in ((2.0 ** 64 * (1 - 2.0 ** -10), 2.0 ** 64), (2.0 ** 64 * (1 - 2.0 ** -10), 2.0 ** 64 * (1 - 2.0 ** -10)),
+                   (most, 1.0), (most, -0.75), (-2.0 ** 127 * 1.9970703, 1.0), (1.0000001, most * 0.9999)):
+        a, b = _single(torch.full((400,), va), torch.full((520,), vb), 600, 3)
+        ref = float(a[0, 3].double() * b[0, 3].double())
+        for name, got, _, _ in _products(a, b):
+            assert bool(((_d(got) - ref).abs() <= (DROPPED + 2 * U * (1 + 2.0 ** -4)) * abs(ref)).all()), (name, va, vb)
+    assert L.poll_errors() == 0
