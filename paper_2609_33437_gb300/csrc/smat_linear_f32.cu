@@ -10,8 +10,9 @@
 // reach 75 at most; 515 x 896 x 4864 36 us, 10 of them to cut 19 MB, the rest bound by the copies into shared memory (110 KB
 // for 1,920 cycles of multiplications). Its error against 64 bits there is 1.9e-7, a plain fp32 product's 6.2e-7.
 //
-// An infinity times a part that is 0 would give NaN. So the first kernel says whether it met an infinity or NaN, and
-// where it did, the second one makes its tiles on the fp32 units instead.
+// An infinity times a part that is 0 would give NaN, and the parts of an operand whose largest value is below 2^-86 miss bits
+// that matter. So the first kernel says what it met, and in those cases the second one makes its tiles on the fp32 units
+// instead. (Beside larger values those below 2^-110 are off by up to 2^-134.)
 //
 // Products of at most 16 rows read a weight once and wait for it: rows_kernel multiplies it as it comes, in registers.
 //
@@ -538,8 +539,9 @@ __device__ __forceinline__ uint32_t nearest2(float x, float y) {
 }
 // The parts of two values, in pairs; x and y end as what is left, 0 from 2^-110 on. Cut off instead of rounded, the parts
 // would have the value's sign, and what is left out of a product would be up to 2^-21 of it and always of one sign.
-__device__ __forceinline__ void cut2(float x, float y, uint32_t (&w)[3], uint32_t& odd) {
-  odd |= (__float_as_uint(x) & 0x7F800000u) == 0x7F800000u || (__float_as_uint(y) & 0x7F800000u) == 0x7F800000u;
+// `top`: the largest magnitude's bits so far.
+__device__ __forceinline__ void cut2(float x, float y, uint32_t (&w)[3], uint32_t& top) {
+  top = max(top, max(__float_as_uint(x) & 0x7FFFFFFFu, __float_as_uint(y) & 0x7FFFFFFFu));
 #pragma unroll
   for (int t = 0; t < 3; ++t) {
     w[t] = nearest2(x, y);
@@ -548,14 +550,22 @@ __device__ __forceinline__ void cut2(float x, float y, uint32_t (&w)[3], uint32_
   }
 }
 
-// Both operands of a product; flags[CTA]: whether it met an infinity or NaN. A thread cuts 8 neighbours of a row: 32
-// bytes in, 3 x 16 out.
+// What an operand's largest magnitude (as bits) says of its parts. From infinity on they do not stand for the values. Nor do
+// they below 2^-86, if there is anything: 2^-24 of the largest value is then less than the 2^-110 from which they are exact.
+enum Flag : uint32_t { kOdd = 1, kSmall = 2, kLarge = 4 };  // an operand is odd, or small in one CTA and large in none
+constexpr uint32_t kSmallest = (127u - 86u) << 23;
+__device__ __forceinline__ uint32_t flag_of(uint32_t top) {
+  return top >= 0x7F800000u ? kOdd : top >= kSmallest ? kLarge : top > 0u ? kSmall : 0u;
+}
+
+// Both operands of a product; flags[CTA]: flag_of what it met. A thread cuts 8 neighbours of a row: 32 bytes in, 3 x 16 out.
 __global__ void __launch_bounds__(256) cut_kernel(const Cut a, const Cut b, int ctas_a, uint32_t* flags) {
+  __shared__ uint32_t tops[8];
   const bool first = (int)blockIdx.x < ctas_a;
   const Cut& c = first ? a : b;
   const int64_t ctas = first ? ctas_a : gridDim.x - ctas_a, cta = first ? blockIdx.x : blockIdx.x - ctas_a;
   const int64_t units = c.ldp / 8, plane = c.rows * c.ldp;
-  uint32_t odd = 0;
+  uint32_t top = 0;
   // a CTA's rows one after another, its threads side by side along a row (a short row's threads share out rows)
   const int wide = (int)(units < 256 ? units : 256), high = 256 / wide;
   const int tx = threadIdx.x % wide, ty = threadIdx.x / wide;
@@ -570,15 +580,20 @@ __global__ void __launch_bounds__(256) cut_kernel(const Cut a, const Cut b, int 
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
           uint32_t parts[3];
-          cut2(v[2 * t], v[2 * t + 1], parts, odd);
+          cut2(v[2 * t], v[2 * t + 1], parts, top);
           w[0][t] = parts[0], w[1][t] = parts[1], w[2][t] = parts[2];
         }
 #pragma unroll
         for (int t = 0; t < 3; ++t)
           *reinterpret_cast<uint4*>(c.to + t * plane + r * c.ldp + at) = make_uint4(w[t][0], w[t][1], w[t][2], w[t][3]);
       }
-  const int any = __syncthreads_or((int)odd);
-  if (threadIdx.x == 0) flags[blockIdx.x] = any;
+  top = __reduce_max_sync(0xFFFFFFFFu, top);
+  if (threadIdx.x % 32 == 0) tops[threadIdx.x / 32] = top;
+  __syncthreads();
+  if (threadIdx.x < 8) {
+    top = __reduce_max_sync(0xFFu, tops[threadIdx.x]);
+    if (threadIdx.x == 0) flags[blockIdx.x] = flag_of(top);
+  }
 }
 
 struct TcArgs {
@@ -588,7 +603,7 @@ struct TcArgs {
   int slices, share;  // slices of 64, and those of a CTA of a cluster
   float* parts;       // shares of sums
   const uint32_t* flags;
-  int n_flags;
+  int flags_a, n_flags;  // those of the first operand that was cut come first
   int* errors;
 };
 
@@ -602,7 +617,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                const __grid_constant__ TcArgs a) {
   extern __shared__ uint8_t raw[];
   __shared__ __align__(8) uint64_t bars[2 * kStages + 5];
-  __shared__ uint32_t tmem_at;
+  __shared__ uint32_t tmem_at, met_here[kThreads / 32];
   __shared__ int dead_flag;
   uint8_t* ring = raw + ((1024 - (smem_address(raw) & 1023)) & 1023);
   volatile int* dead = &dead_flag;
@@ -639,14 +654,20 @@ __global__ void __launch_bounds__(kThreads, 1)
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
     fence_before();
   }
-  uint32_t odd = 0;
-  for (int i = threadIdx.x; i < a.n_flags; i += kThreads) odd |= a.flags[i];
-  odd = __syncthreads_or((int)odd);
+  uint32_t met = 0;  // the second operand's flags from bit 8 on
+  for (int i = threadIdx.x; i < a.n_flags; i += kThreads) met |= a.flags[i] << (i < a.flags_a ? 0 : 8);
+  met = __reduce_or_sync(0xFFFFFFFFu, met);
+  if (lane == 0) met_here[warp] = met;
+  __syncthreads();
   fence_after();
   const uint32_t tmem = tmem_at;
+#pragma unroll
+  for (int w = 0; w < kThreads / 32; ++w) met |= met_here[w];
+  auto uncut = [](uint32_t f) { return (f & kOdd) || (f & (kSmall | kLarge)) == kSmall; };
+  const bool odd = uncut(met) || uncut(met >> 8);
 
   if (odd) {
-    // an infinity or NaN in an operand: all CTAs make tiles of 128 x 128 on the fp32 units
+    // an operand whose parts do not stand for it: all CTAs make tiles of 128 x 128 on the fp32 units
     if (warp < kEpiWarps) {
       float* sums = reinterpret_cast<float*>(ring);
       const int64_t ti = (p.I + kBM - 1) / kBM, tj = (p.J + kBN - 1) / kBN;
@@ -963,7 +984,7 @@ cudaError_t launch_tc32(const Product& p, int sms, char* workspace, cudaStream_t
   const Cut ca = {(const float*)p.b, (uint16_t*)pa, g.rows_a, g.cols_a, p.ldb, g.ldp_a, a.f.vb};
   const Cut cb = {(const float*)p.a, (uint16_t*)pb, g.rows_b, g.cols_b, p.lda, g.ldp_b, a.f.va};
   a.flags = (const uint32_t*)pf;
-  a.n_flags = g.cuts_a + g.cuts_b;
+  a.flags_a = g.cuts_a, a.n_flags = g.cuts_a + g.cuts_b;
   a.parts = (float*)(pf + g.bytes_flags);
   a.tiles_r = g.tiles_r, a.tiles_c = g.tiles_c, a.tiles = g.tiles_r * g.tiles_c;
   a.slices = g.slices, a.share = g.share, a.width = g.width;

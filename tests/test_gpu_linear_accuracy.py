@@ -88,3 +88,51 @@ def test_f32_products_next_to_the_largest_number():
         for name, got, _, _ in _products(a, b):
             assert bool(((_d(got) - ref).abs() <= (DROPPED + 2 * U * (1 + 2.0 ** -4)) * abs(ref)).all()), (name, va, vb)
     assert L.poll_errors() == 0
+
+
+@pytest.mark.parametrize("rows,k,n", [(300, 520, 520), (1100, 300, 260)])
+@pytest.mark.parametrize("power", [-88, -100, -118])
+def test_f32_operands_that_are_small_all_over(rows, k, n, power):
+    """An operand below the size at which three bf16 parts hold its bits, times one that makes up for it: fp32's bound for a
+    sum, 8 sqrt(terms) + 4 roundings of the magnitudes' sum. (Values below 2^-126 have fewer bits themselves: inputs are
+    normal numbers, of one sign and at least 2^power, and results are.)"""
+    g = torch.Generator(device="cuda").manual_seed(power + 200)
+    small = torch.ldexp(1 + torch.rand(rows, k, generator=g, device="cuda"), torch.tensor(float(power), device="cuda"))
+    large = torch.ldexp(torch.randn(n, k, generator=g, device="cuda"), torch.tensor(40.0, device="cuda"))
+    for a, b in ((small, large), (large, small)):
+        ref, mag = _d(a) @ _d(b).T, _d(a).abs() @ _d(b).abs().T
+        for name, got, _, _ in _products(a, b):
+            worst = float(((_d(got) - ref).abs() / mag).max()) / U
+            assert worst <= 8 * k ** 0.5 + 4, (name, worst)
+    assert L.poll_errors() == 0
+
+
+def test_f32_operands_of_nothing_and_of_mixed_sizes():
+    """Zeros all over are 0, not small; one value of 2^-86 keeps the parts in use, and what is below them then is off by
+    2^-134 of its factor at most (and the sum's roundings)."""
+    zero, one = torch.zeros(300, 520, device="cuda"), torch.ones(520, 520, device="cuda")
+    for name, got, _, _ in _products(zero, one):
+        assert not got.any(), name
+    g = torch.Generator(device="cuda").manual_seed(1)
+    a = torch.ldexp(torch.randn(300, 520, generator=g, device="cuda"), torch.tensor(-116.0, device="cuda"))
+    a[7, 9] = 2.0 ** -86
+    b = torch.ldexp(torch.randn(520, 520, generator=g, device="cuda"), torch.tensor(40.0, device="cuda"))
+    ref, mag = _d(a) @ _d(b).T, _d(a).abs() @ _d(b).abs().T
+    tol = (8 * 520 ** 0.5 + 4) * U * mag + 2.0 ** -134 * _d(b).abs().sum(1)
+    for name, got, _, _ in _products(a, b):
+        assert bool(((_d(got) - ref).abs() <= tol).all()), name
+    assert L.poll_errors() == 0
+
+
+@pytest.mark.parametrize("power", [-90, -112, -120])
+def test_f32_single_products_of_small_values(power):
+    """As test_f32_single_products, one operand small all over: the result's bits are there all the same."""
+    g = torch.Generator().manual_seed(3)
+    va = torch.ldexp(1 + torch.rand(400, generator=g), torch.tensor(float(power)))
+    vb = torch.ldexp(1 + torch.rand(520, generator=g), torch.tensor(40.0))
+    for x, y in ((va, vb), (vb, va)):
+        a, b = _single(x, y, 600, 599)
+        ref = x.double()[:, None] * y.double()[None, :]
+        for name, got, _, _ in _products(a, b):
+            off = ((_d(got) - ref) / ref).abs().max()
+            assert off <= DROPPED + 2 * U * (1 + 2.0 ** -4), (name, float(off) / U)
