@@ -14,8 +14,11 @@ namespace lin {
 
 constexpr int kGroup = SMAT_PACK8_GROUP;
 
-// The hardware's 2^x and 1 / x, 2 ulp and 1 ulp, results below 2^-126 flushed to 0: one instruction each, where
-// expf and a division are 6 to 10. An epilogue makes a value per sum, and its instructions bound it.
+// Activations of bf16 calls go by the hardware's 2^x and 1 / x, 2 ulp and 1 ulp, results below 2^-126 flushed to 0: one
+// instruction each, where expf and a division are 6 to 10. A product's epilogue makes a value per sum, and its instructions
+// bound it; a result's rounding to bf16 hides their error. Those of fp32 calls, whose results would show it, are right to a
+// few units in the last place. Memory bounds those mostly: 8191 x 4096 read back through none 27.3 us, silu 28.5, GELU 33.3 (with
+// the forms for bf16 28.1 and 29.9), with rows off every boundary 8191 x 1100 14.7, 18.2 and 20.9 (16.4 and 19.4).
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -29,16 +32,44 @@ __device__ __forceinline__ float rcp_fast(float x) {
 
 constexpr float kLog2e = 1.4426950408889634f;
 
-// sigmoid(c h), 1e-6 relative where it is above 2^-120, with its limits at infinities. The activations with a
-// sigmoid form use it, the tanh form of GELU too (1 + tanh u = 2 sigmoid(2u)), so that small values far out on the
-// negative side keep their digits.
-__device__ __forceinline__ float sigmoid(float x, float c = 1.0f) {
-  return rcp_fast(1.0f + exp2_fast(-c * kLog2e * x));
+// sigmoid(c x) with its limits at infinities. The exponent is one fp32 number: relative error (1.5 |c x| + 4) 2^-23, 5e-7 near
+// 0 and 5e-6 at -20, down to 2^-126 (c x = -87), below which it is 0. The activations with a sigmoid form use it, the tanh form
+// of GELU too (1 + tanh u = 2 sigmoid(2u)), so that small values far out on the negative side keep their digits.
+__device__ __forceinline__ float sigmoid_fast(float x, float c) { return rcp_fast(1.0f + exp2_fast(-c * kLog2e * x)); }
+
+// sigmoid(x) and sigmoid(x) sigmoid(-x), by e = exp(-|x|), which never overflows: 8 2^-24 relative and 5 more, of an x that is
+// exact, down to where e is below 2^-126
+struct Sigmoid {
+  float s, slope;
+};
+__device__ __forceinline__ Sigmoid sigmoid_full(float x) {
+  const float e = expf(-fabsf(x)), r = rcp_fast(1.0f + e);
+  return {x < 0.0f ? e * r : r, e * r * r};
+}
+
+// Phi(h) = exp(-h^2 / 2) t Q(t), t = 1 / (1 + 0.35 |h|), taken from the side where it is small; Q and its error, 5 2^-24
+// relative with its roundings, by fit_normal_cdf.py. With the reciprocal (2) and the exponential (4, and 1.5 h^2 for the
+// roundings of its argument, which expf would have nearly all too) (13 + 1.5 h^2) 2^-24, down to 2^-126; `g` = exp(-h^2 / 2).
+// CUDA's normcdff takes 71 us to read 8191 x 4096 back through GELU, with expf here it was 41.
+__device__ __forceinline__ float normal_cdf(float h, float& g) {
+  const float t = rcp_fast(fmaf(0.35f, fabsf(h), 1.0f));
+  g = exp2_fast(h * h * (-0.5f * kLog2e));
+  float s = fmaf(t, -0.0291206744f, 0.143846497f);
+  s = fmaf(s, t, -0.255450249f);
+  s = fmaf(s, t, 0.158865809f);
+  s = fmaf(s, t, -0.0228923205f);
+  s = fmaf(s, t, 0.105413429f);
+  s = fmaf(s, t, 0.119857527f);
+  s = fmaf(s, t, 0.13985835f);
+  s = fmaf(s, t, 0.139621615f);
+  s = s * t * g;
+  return h > 0.0f ? 1.0f - s : s;
 }
 
 // Phi(h) by Abramowitz and Stegun 7.1.26 (erfc(z) = t (a1 + t (a2 + ...)) exp(-z^2), t = 1 / (1 + p z), z = |h| /
-// sqrt2; off by 1.5e-7 at most, so Phi by 0.75e-7), taken from the side where it is small; `g` = exp(-h^2 / 2).
-__device__ __forceinline__ float normal_cdf(float h, float& g) {
+// sqrt2; off by 1.5e-7 at most, so Phi by 0.75e-7), taken from the side where it is small; `g` = exp(-h^2 / 2). In the tail
+// that is 0.16% of Phi at -5, 1% at -8 and 3.7% at -13: fewer digits than a bf16 result has from -6.2 on.
+__device__ __forceinline__ float normal_cdf_fast(float h, float& g) {
   const float t = rcp_fast(fmaf(0.3275911f * 0.70710678f, fabsf(h), 1.0f));
   g = exp2_fast(h * h * (-0.5f * kLog2e));
   float s = fmaf(t, 0.5f * 1.061405429f, 0.5f * -1.453152027f);
@@ -52,38 +83,52 @@ __device__ __forceinline__ float normal_cdf(float h, float& g) {
 constexpr float kTanhGain = 1.5957691216057308f;  // 2 sqrt(2 / pi)
 constexpr float kTanhCube = 0.044715f;
 
-template <int ACT>
+// T: the call's type
+template <int ACT, class T>
 __device__ __forceinline__ float act_value(float h) {
+  constexpr bool kFull = sizeof(T) == 4;
   if (ACT == SMAT_ACT_RELU) return h > 0.0f || h != h ? h : 0.0f;
   if (ACT == SMAT_ACT_GELU) {
     float g;
-    return h * normal_cdf(h, g);
+    return h * (kFull ? normal_cdf(h, g) : normal_cdf_fast(h, g));
   }
-  if (ACT == SMAT_ACT_GELU_TANH) return h * sigmoid(h * fmaf(kTanhCube, h * h, 1.0f), kTanhGain);
-  if (ACT == SMAT_ACT_QUICK_GELU) return h * sigmoid(h, 1.702f);
-  if (ACT == SMAT_ACT_SILU) return h * sigmoid(h);
+  if (ACT == SMAT_ACT_GELU_TANH) {
+    const float x = h * fmaf(kTanhCube, h * h, 1.0f);
+    return h * (kFull ? sigmoid_full(kTanhGain * x).s : sigmoid_fast(x, kTanhGain));
+  }
+  if (ACT == SMAT_ACT_QUICK_GELU) return h * (kFull ? sigmoid_full(1.702f * h).s : sigmoid_fast(h, 1.702f));
+  if (ACT == SMAT_ACT_SILU) return h * (kFull ? sigmoid_full(h).s : sigmoid_fast(h, 1.0f));
   return h;
 }
 
-// act'. Beyond +-100 every slope here is 0 or 1 in fp32; h is held there, so that an infinity or a huge h gives
+// act'. Beyond +-200 every slope here is 0 or 1 in fp32; h is held there, so that an infinity or a huge h gives
 // the limit and not inf * 0. NaN stays NaN.
-template <int ACT>
+template <int ACT, class T>
 __device__ __forceinline__ float act_slope(float h) {
+  constexpr bool kFull = sizeof(T) == 4;
   if (ACT == SMAT_ACT_RELU) return h > 0.0f ? 1.0f : (h != h ? h : 0.0f);
   if (ACT == SMAT_ACT_NONE) return 1.0f;
-  asm("min.NaN.f32 %0, %0, 0f42C80000;\nmax.NaN.f32 %0, %0, 0fC2C80000;" : "+f"(h));
+  asm("min.NaN.f32 %0, %0, 0f43480000;\nmax.NaN.f32 %0, %0, 0fC3480000;" : "+f"(h));
   if (ACT == SMAT_ACT_GELU) {
     float g;
-    const float c = normal_cdf(h, g);
+    const float c = kFull ? normal_cdf(h, g) : normal_cdf_fast(h, g);
     return fmaf(h * 0.39894228040143268f, g, c);
   }
   if (ACT == SMAT_ACT_GELU_TANH) {
-    const float u = h * h;
-    const float s = sigmoid(h * fmaf(kTanhCube, u, 1.0f), kTanhGain);
-    return fmaf(h * fmaf(3.0f * kTanhCube * kTanhGain, u, kTanhGain), fmaf(-s, s, s), s);
+    const float u = h * h, x = h * fmaf(kTanhCube, u, 1.0f), by = h * fmaf(3.0f * kTanhCube * kTanhGain, u, kTanhGain);
+    if (kFull) {
+      const Sigmoid t = sigmoid_full(kTanhGain * x);
+      return fmaf(by, t.slope, t.s);
+    }
+    const float s = sigmoid_fast(x, kTanhGain);
+    return fmaf(by, fmaf(-s, s, s), s);
   }
   const float c = ACT == SMAT_ACT_QUICK_GELU ? 1.702f : 1.0f;
-  const float s = sigmoid(h, c);
+  if (kFull) {
+    const Sigmoid t = sigmoid_full(c * h);
+    return fmaf(c * h, t.slope, t.s);
+  }
+  const float s = sigmoid_fast(h, c);
   return fmaf(c * h, fmaf(-s, s, s), s);
 }
 

@@ -51,7 +51,7 @@ __global__ void __launch_bounds__(kThreads) outer_kernel(const Outer a, int per)
       }
   }
   SMAT_WITH_ACT(a.act, _Pragma("unroll") for (int m = 0; m < L; ++m) _Pragma("unroll") for (int c = 0; c < C; ++c)
-                    x[m][c] = m <= last ? stored<T>(act_value<ACT>(x[m][c])) : 0.0f)
+                    x[m][c] = m <= last ? stored<T>(act_value<ACT, T>(x[m][c])) : 0.0f)
   __syncthreads();
   if (a.db && blockIdx.x == 0 && threadIdx.x < per && n0 + threadIdx.x < a.n) {
     T* db = (T*)a.db + n0 + threadIdx.x;

@@ -221,7 +221,7 @@ __device__ __forceinline__ void finish_block(const Args& a, const CUtensorMap* m
       desk_store(desk.q_at(lane, 1), w + 4);
       if (there && j < p.J) p.e[(i + lane) * p.lde + j / kGroup] = (uint8_t)ex;
     }
-    SMAT_WITH_ACT(p.act, _Pragma("unroll") for (int t = 0; t < 32; ++t) v[t] = act_value<ACT>(v[t]))
+    SMAT_WITH_ACT(p.act, _Pragma("unroll") for (int t = 0; t < 32; ++t) v[t] = act_value<ACT, bf16>(v[t]))
   }
   if (copied) {
     if (!bar_wait(desk.bar, desk.phase & 1, dead, a.errors)) return;
@@ -236,7 +236,7 @@ __device__ __forceinline__ void finish_block(const Args& a, const CUtensorMap* m
     }
     float x[32];
     unpack_words8<8>(w, e, x);
-    SMAT_WITH_ACT(p.act, _Pragma("unroll") for (int t = 0; t < 32; ++t) v[t] *= act_slope<ACT>(x[t]))
+    SMAT_WITH_ACT(p.act, _Pragma("unroll") for (int t = 0; t < 32; ++t) v[t] *= act_slope<ACT, bf16>(x[t]))
   }
 #pragma unroll
   for (int c = 0; c < 4; ++c) {
@@ -304,7 +304,7 @@ __device__ __forceinline__ void finish_column(const Args& a, int64_t i, int64_t 
         }
       }
     }
-    SMAT_WITH_ACT(p.act, _Pragma("unroll") for (int t = 0; t < N; ++t) v[t] = act_value<ACT>(v[t]))
+    SMAT_WITH_ACT(p.act, _Pragma("unroll") for (int t = 0; t < N; ++t) v[t] = act_value<ACT, bf16>(v[t]))
     if (p.residual) {
 #pragma unroll
       for (int t = 0; t < N; ++t) v[t] += x[t];
@@ -323,7 +323,7 @@ __device__ __forceinline__ void finish_column(const Args& a, int64_t i, int64_t 
       }
 #pragma unroll
       for (int t = 0; t < N; ++t) x[t] = (float)qs[t] * unpack_scale(es[t]);
-      SMAT_WITH_ACT(p.act, _Pragma("unroll") for (int t = 0; t < N; ++t) v[t] *= act_slope<ACT>(x[t]))
+      SMAT_WITH_ACT(p.act, _Pragma("unroll") for (int t = 0; t < N; ++t) v[t] *= act_slope<ACT, bf16>(x[t]))
     } else {
 #pragma unroll
       for (int t = 0; t < N; ++t) x[t] = t < mine ? to_float(out[t * p.ldo]) : 0.0f;

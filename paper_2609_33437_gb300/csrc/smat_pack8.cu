@@ -289,12 +289,12 @@ __global__ void __launch_bounds__(kThreads, 4)
 }
 
 // act(h^) of one unit, or dy * act'(h^) where DY (v: dy in, the result out)
-template <int ACT, bool DY>
+template <class T, int ACT, bool DY>
 __device__ __forceinline__ void value_unit(const uint32_t (&w)[4], uint32_t e, float (&v)[kUnit]) {
   float h[kUnit];
   unpack_words8<4>(w, e, h);
 #pragma unroll
-  for (int i = 0; i < kUnit; ++i) v[i] = DY ? v[i] * act_slope<ACT>(h[i]) : act_value<ACT>(h[i]);
+  for (int i = 0; i < kUnit; ++i) v[i] = DY ? v[i] * act_slope<ACT, T>(h[i]) : act_value<ACT, T>(h[i]);
 }
 
 template <class T, int ACT, bool DY>
@@ -310,7 +310,7 @@ __global__ void __launch_bounds__(kThreads)
     const uint32_t ex = e[r * lde + u / 2];
     float v[kUnit];
     if (DY) load_unit(dy + r * lddy + c, count, ady, v);
-    value_unit<ACT, DY>(w, ex, v);
+    value_unit<T, ACT, DY>(w, ex, v);
     store_unit(out + r * ldout + c, count, aout, v);
   }
 }
@@ -330,7 +330,7 @@ __device__ __forceinline__ void unpack_pieces(const int8_t* q, int64_t ldq, cons
     const uint32_t ex = there ? e[row * lde + col / kGroup] : 1u;
     float v[kUnit];
     if (DY) piece_in(s, dy + r * lddy + c, lddy, buf, v);
-    value_unit<ACT, DY>(w, ex, v);
+    value_unit<T, ACT, DY>(w, ex, v);
     if (aligned) {
       if (there) store_unit(out + row * ldout + col, (int)(cols - col < kUnit ? cols - col : kUnit), kWhole, v);
     } else {
@@ -495,7 +495,7 @@ __global__ void __launch_bounds__(kThreads) prepare_kernel(const Prepare a) {
           uint32_t w[4];
           load_q(p.q + r * p.ldq + c, count, kWhole, w);
           float v[kUnit];
-          value_unit<ACT, false>(w, p.e[r * p.lde + u / 2], v);
+          value_unit<__nv_bfloat16, ACT, false>(w, p.e[r * p.lde + u / 2], v);
           store_unit(to + r * p.ldto + c, count, kWhole, v);
         }
     return;

@@ -1,5 +1,5 @@
-"""How near the fp32 linear operators come to their definitions in 64 bits, with bounds that follow the arithmetic and not
-the size of the sum, on the GPU.
+"""How near the linear operators come to their definitions in 64 bits, with bounds that follow the arithmetic and not the
+size of the sum, on the GPU: fp32 products, and the activations of both types.
 
 fp32 products of large matrices are six of the nine products of three bf16 parts (smat_linear_f32.cu). With parts rounded to
 nearest |mid| <= 2^-8 and |lo| <= 2^-17 of a value's power of two, so what is left out, mid lo + lo mid + lo lo, is at most
@@ -7,14 +7,17 @@ nearest |mid| <= 2^-8 and |lo| <= 2^-17 of a value's power of two, so what is le
 sum; the parts' products come small ones first, so that only the last ones, of hi and hi, are added to sums of full size:
 those before are below 2^-6 of it."""
 
+import math
+
 import pytest
 import torch
 
+import _linear_ref as R
 from paper_2609_33437_gb300 import linear as L
 
 pytestmark = pytest.mark.gpu
 
-F32 = torch.float32
+BF, F32 = torch.bfloat16, torch.float32
 U = 2.0 ** -24  # half a unit in the last place, relative
 DROPPED = U * (1 + 2.0 ** -9)
 
@@ -136,3 +139,81 @@ def test_f32_single_products_of_small_values(power):
         for name, got, _, _ in _products(a, b):
             off = ((_d(got) - ref) / ref).abs().max()
             assert off <= DROPPED + 2 * U * (1 + 2.0 ** -4), (name, float(off) / U)
+
+
+# Activations and slopes, relative to themselves: nothing hides behind an absolute tolerance where they are small.
+# Errors in units of 2^-24, by the steps taken. fp32: expf 2 ulp (4), 1 + e (1), reciprocal 1 ulp (2), e r (1), h s (1): 9; the
+# argument's own relative error, times its size: 0 for silu, 1.702 h 1.5, the tanh form's 6. GELU: polynomial with its roundings
+# (5), reciprocal (2), ex2 (4) of h^2 log2(e) / 2 (a square, a constant, a product: 1.5 h^2), two products (2), 1 - s (1),
+# h Phi (1): 15 + 1.5 h^2.
+# bf16: ex2 2 ulp (4), 1 + e (1), reciprocal 2, product 1: 8; the exponent's relative error, times its size: its constant (1)
+# and its product (1), the tanh form's four more; then the rounding to bf16.
+EXPF, ARGUMENT_FULL, ARGUMENT_FAST = 9, {"silu": 0, "quick_gelu": 1.5, "gelu_tanh": 6}, {"silu": 2, "quick_gelu": 3, "gelu_tanh": 7}
+GAIN = 2.0 * math.sqrt(2.0 / math.pi)
+
+
+def _argument(act, h):
+    return {"silu": h, "quick_gelu": 1.702 * h, "gelu_tanh": GAIN * (h + 0.044715 * h ** 3)}[act]
+
+
+def _published_cdf(h):
+    """Abramowitz and Stegun's 7.1.26 for Phi(-|h|), what bf16 calls' GELU goes by, in 64 bits."""
+    t = 1 / (1 + 0.3275911 * h.abs() / math.sqrt(2.0))
+    p = t * (0.254829592 + t * (-0.284496736 + t * (1.421413741 + t * (-1.453152027 + t * 1.061405429))))
+    return 0.5 * p * torch.exp(-0.5 * h * h)
+
+
+def _saved_range(low, high, dtype):
+    """Values in 8 bits from low to high, and what they stand for (in groups of 32 neighbours, steps small near 0)."""
+    x = torch.cat([torch.linspace(low, high, 4096), torch.linspace(low / 64, high / 64, 4096)]).view(-1, 64)
+    p = L.pack8(x.to(dtype).cuda())
+    return p, R.unpack(p.q, p.e)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF])
+@pytest.mark.parametrize("act", ["gelu", "gelu_tanh", "quick_gelu", "silu"])
+def test_activations_keep_their_digits(act, dtype):
+    low = {"gelu": -12.5, "gelu_tanh": -7.0, "quick_gelu": -48.0, "silu": -80.0}[act]  # down to about 2^-116
+    p, h = _saved_range(low, 30.0, dtype)
+    got, ref = _d(L.unpack8(p, act, dtype)), R.act(act, h)
+    if act == "gelu":
+        if dtype == F32:
+            tol = (15 + 1.5 * h * h) * U * ref.abs()
+        else:  # its published form's error; then 1 - s, polynomial (20) and exponent (its argument twice rounded)
+            tail = (_published_cdf(h) - 0.5 * torch.special.erfc(h.abs() / math.sqrt(2.0))).abs() * h.abs()
+            tol = tail + (24 + 3 * 0.5 * h * h) * U * ref.abs()
+    else:
+        x = _argument(act, h).abs()
+        tol = (EXPF + x * (ARGUMENT_FULL if dtype == F32 else ARGUMENT_FAST)[act]) * U * ref.abs()
+    if dtype == BF:
+        tol = tol * 1.01 + R.rounding(BF) * ref.abs()
+    bad = (got - ref).abs() > tol
+    assert not bool(bad.any()), (h[bad][0].item(), got[bad][0].item(), ref[bad][0].item(), int(bad.sum()))
+    # a product's epilogue applies the same function: times the unit matrix, in few rows and in many
+    x, y = L.unpack8(p, dtype=dtype).view(16, 512), L.unpack8(p, act, dtype).view(16, 512)
+    eye = torch.eye(512, device="cuda", dtype=dtype)
+    for rows in (1, 2, 16, 40, 640):
+        reps = -(-rows // 16)
+        assert torch.equal(L.linear(x.repeat(reps, 1)[:rows], eye, act=act), y.repeat(reps, 1)[:rows]), rows
+
+
+@pytest.mark.parametrize("act", ["gelu", "gelu_tanh", "quick_gelu", "silu"])
+def test_f32_slopes_keep_their_digits(act):
+    """s + c h s (1 - s) (Phi + h phi): relative to the two terms' magnitudes, since they may cancel. The second term has the
+    first's exponential, one more factor s (1 + 2 + 2) and its own products (3)."""
+    low = {"gelu": -12.5, "gelu_tanh": -7.0, "quick_gelu": -48.0, "silu": -80.0}[act]
+    p, h = _saved_range(low, 30.0, F32)
+    got = _d(L.act_grad8(torch.ones(p.shape, device="cuda"), p, act))
+    if act == "gelu":
+        first, second = 0.5 * torch.special.erfc(-h / math.sqrt(2.0)), h * torch.exp(-0.5 * h * h) / math.sqrt(2 * math.pi)
+        tol = (15 + 1.5 * h * h) * U * first + (4 + 4 + 1.5 * h * h) * U * second.abs()
+    else:
+        x = _argument(act, h)
+        s = torch.sigmoid(x)
+        by = {"silu": h, "quick_gelu": 1.702 * h, "gelu_tanh": GAIN * h * (1 + 3 * 0.044715 * h * h)}[act]
+        first, second = s, by * s * torch.sigmoid(-x)
+        tol = (EXPF + x.abs() * ARGUMENT_FULL[act]) * U * (first + second.abs()) + 12 * U * second.abs()
+    ref = first + second
+    tol = tol + U * ref.abs()
+    bad = (got - ref).abs() > tol
+    assert not bool(bad.any()), (h[bad][0].item(), got[bad][0].item(), ref[bad][0].item(), int(bad.sum()))
