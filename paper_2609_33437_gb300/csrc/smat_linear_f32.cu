@@ -720,8 +720,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (!ok)  // copies in flight land before the CTA ends
       for (uint32_t s = 0; s < kStages && s < n; ++s) {
         const uint32_t last = n - 1 - s;
-        for (int i = 0; i < (1 << 20) && !bar_try(full + 8 * (last % kStages), last / kStages & 1); ++i) {
-        }
+        bar_drain(full + 8 * (last % kStages), last / kStages & 1);
       }
   } else if (warp == kMmaWarp && lane == 0) {
     const uint32_t inst = kInstruction<A_MN, B_MN, 0> | (uint32_t)(a.width >> 3) << 17;
@@ -748,8 +747,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
     if (!ok) {  // products in flight end before the CTA does
       mma_commit(drained);
-      for (int i = 0; i < (1 << 20) && !bar_try(drained, 0); ++i) {
-      }
+      bar_drain(drained, 0);
     }
   } else if (warp < kEpiWarps) {
     // this warp's sums: 32 rows and half the columns of the tile, 16 columns at a time
@@ -766,7 +764,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int t = 0; t < kBlock; ++t) acc[b][t] = 0.0f;
       for (int k = 0; k < slices; ++k, ++n) {
         const uint32_t half = n & 1;
-        ok = bar_wait(sums_full + 8 * half, n / 2 & 1, dead, a.errors);
+        ok = bar_wait_warp(sums_full + 8 * half, n / 2 & 1, dead, a.errors);
         if (!ok) break;
         fence_after();
 #pragma unroll
@@ -805,7 +803,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (shares > 1) {
     __syncthreads();
     cluster_sync();
-    if (!odd && warp < kEpiWarps && !*dead) {
+    if (!odd && warp < kEpiWarps && !__any_sync(0xFFFFFFFFu, *dead)) {
       int64_t tr, tc;
       tile_place<16>(a.tiles_r, a.tiles_c, first_tile, tr, tc);
       const int quarter = warp % 4;

@@ -152,9 +152,9 @@ __device__ __forceinline__ void desk_send(const Desk& desk, void* to, int64_t ld
 }
 
 // Columns j .. j + 31 of rows i .. i + 31, a row per lane, out by TMA (which leaves out what lies outside the result) or
-// by hand. sums(v): their sums.
+// by hand. sums(v): their sums. False if a wait for what comes in has given up.
 template <int MODE, class Sums>
-__device__ __forceinline__ void finish_block(const Args& a, const CUtensorMap* map_out, const CUtensorMap* map_in,
+__device__ __forceinline__ bool finish_block(const Args& a, const CUtensorMap* map_out, const CUtensorMap* map_in,
                                             const CUtensorMap* map_q, int64_t i, int64_t j, Desk& desk,
                                             volatile int* dead, Sums&& sums) {
   const Product& p = a.p;
@@ -224,7 +224,10 @@ __device__ __forceinline__ void finish_block(const Args& a, const CUtensorMap* m
     SMAT_WITH_ACT(p.act, _Pragma("unroll") for (int t = 0; t < 32; ++t) v[t] = act_value<ACT, bf16>(v[t]))
   }
   if (copied) {
-    if (!bar_wait(desk.bar, desk.phase & 1, dead, a.errors)) return;
+    if (!bar_wait_warp(desk.bar, desk.phase & 1, dead, a.errors)) {
+      bar_drain(desk.bar, desk.phase & 1);
+      return false;
+    }
     ++desk.phase;
   }
   if (slope) {
@@ -270,6 +273,7 @@ __device__ __forceinline__ void finish_block(const Args& a, const CUtensorMap* m
     desk_send<uint16_t>(desk, p.out, p.ldo, i, j, p.I, p.J);
     if (save) desk_send<uint8_t>(desk, p.q, p.ldq, i, j, p.I, p.J);
   }
+  return true;
 }
 
 // Column j of rows i .. i + N - 1, one thread; the warp holds 32 neighbouring columns from a multiple of 32 on. What
@@ -337,21 +341,23 @@ __device__ __forceinline__ void finish_column(const Args& a, int64_t i, int64_t 
 }
 
 // Blocks `first`, `first + step`, ... below `end` of 32 columns of a tile that begins at row row0 (this warp's 32) and
-// column col0 of the result: `sums(c, v)` gives block c's sums.
+// column col0 of the result: `sums(c, v)` gives block c's sums. False: as finish_block, the blocks after it left out.
 template <int MODE, class Sums>
-__device__ __forceinline__ void finish_blocks(const Args& a, const CUtensorMap* map_out, const CUtensorMap* map_in,
+__device__ __forceinline__ bool finish_blocks(const Args& a, const CUtensorMap* map_out, const CUtensorMap* map_in,
                                               const CUtensorMap* map_q, int64_t row0, int64_t col0, int first, int end,
                                               int step, Desk& desk, volatile int* dead, Sums&& sums) {
 #pragma unroll 1
   for (int c = first; c < end; c += step) {
     const int64_t col = col0 + 32 * c;
     if (row0 < a.p.I && col < a.p.J) {
-      finish_block<MODE>(a, map_out, map_in, map_q, row0, col, desk, dead, [&](float(&v)[32]) { sums(c, v); });
+      if (!finish_block<MODE>(a, map_out, map_in, map_q, row0, col, desk, dead, [&](float(&v)[32]) { sums(c, v); }))
+        return false;
     } else {
       float v[32];
       sums(c, v);
     }
   }
+  return true;
 }
 
 template <int MODE, int BN>
@@ -437,8 +443,7 @@ __global__ void __launch_bounds__(kThreads, Ring<BN>::kCtas)
     if (!ok)  // copies in flight land before the CTA ends
       for (uint32_t s = 0; s < kStages && s < n; ++s) {
         const uint32_t last = n - 1 - s;
-        for (int i = 0; i < (1 << 20) && !bar_try(full + 8 * (last % kStages), last / kStages & 1); ++i) {
-        }
+        bar_drain(full + 8 * (last % kStages), last / kStages & 1);
       }
   } else if (warp == kMmaWarp && lane == 0) {
     constexpr uint32_t kInst = kInstruction<A_MN, B_MN, BN>;
@@ -465,8 +470,7 @@ __global__ void __launch_bounds__(kThreads, Ring<BN>::kCtas)
     }
     if (!ok) {  // products in flight end before the CTA does
       mma_commit(drained);
-      for (int i = 0; i < (1 << 20) && !bar_try(drained, 0); ++i) {
-      }
+      bar_drain(drained, 0);
     }
   } else if (warp < kEpiWarps) {
     const int quarter = warp % 4;  // the 32 rows of tensor memory that this warp may read
@@ -479,7 +483,7 @@ __global__ void __launch_bounds__(kThreads, Ring<BN>::kCtas)
       tile_place<16>(a.tiles_r, a.tiles_c, tile, tr, tc);
       const int64_t r0 = tr * kBM + 32 * quarter, c0 = tc * BN;
       const uint32_t half = made & 1, sums = tmem + half * BN + ((uint32_t)(32 * quarter) << 16);
-      if (!bar_wait(sums_full + 8 * half, made / 2 & 1, dead, a.errors)) break;
+      if (!bar_wait_warp(sums_full + 8 * half, made / 2 & 1, dead, a.errors)) break;
       fence_after();
       auto release = [&] {  // this warp has what it needs of these sums
         fence_before();
@@ -509,7 +513,7 @@ __global__ void __launch_bounds__(kThreads, Ring<BN>::kCtas)
     // one tile per cluster: its CTAs add up and finish blocks of its columns in turn
     __syncthreads();
     cluster_sync();
-    if (warp < kEpiWarps && !*dead) {
+    if (warp < kEpiWarps && !__any_sync(0xFFFFFFFFu, *dead)) {
       int64_t tr, tc;
       tile_place<16>(a.tiles_r, a.tiles_c, first_tile, tr, tc);
       const int quarter = warp % 4;
@@ -624,12 +628,14 @@ __global__ void __launch_bounds__(kPairThreads, 1)
         }
       }
     }
-    if (!ok && member == 0)  // both CTAs' copies in flight land before either ends (they meet below)
+    // both CTAs' copies in flight land before either ends (they meet below)
+    if (!ok && member == 0)
       for (uint32_t s = 0; s < kStages && s < n; ++s) {
         const uint32_t last = n - 1 - s;
-        for (int i = 0; i < (1 << 20) && !bar_try(full + 8 * (last % kStages), last / kStages & 1); ++i) {
-        }
+        bar_drain(full + 8 * (last % kStages), last / kStages & 1);
       }
+    else if (!ok)  // they signal the other CTA's barriers, which may have given up on them
+      drain_pause();
   } else if (warp == kPairEpi + 1 && lane == 0 && member == 0) {
     const uint32_t inst = kInstruction<A_MN, B_MN, 0, kPairRows> | (uint32_t)(a.width >> 3) << 17;
     const uint16_t both = (uint16_t)(3u << rank);
@@ -656,8 +662,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     }
     if (!ok) {  // products in flight end before the CTAs do
       mma_commit_pair(drained, (uint16_t)(1u << rank));
-      for (int i = 0; i < (1 << 20) && !bar_try(drained, 0); ++i) {
-      }
+      bar_drain(drained, 0);
     }
   } else if (warp < kPairEpi) {
     if (MODE == kGradWeight && a.p.db) {  // db, while the first sums are made
@@ -680,7 +685,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       tile_place<8>(a.tiles_r, a.tiles_c, tile, tr, tc);
       const int64_t r0 = tr * kPairRows + (int)member * kBM + 32 * quarter, c0 = tc * a.width;
       const uint32_t half = made & 1, sums = tmem + half * kSums + ((uint32_t)(32 * quarter) << 16);
-      if (!bar_wait(sums_full + 8 * half, made / 2 & 1, dead, a.errors)) break;
+      if (!bar_wait_warp(sums_full + 8 * half, made / 2 & 1, dead, a.errors)) break;
       fence_after();
       auto release = [&] {  // this warp has what it needs of these sums
         fence_before();
@@ -698,7 +703,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       };
       if (first == end) release();  // none of a narrow tile's columns
       if (shares == 1) {
-        finish_blocks<MODE>(a, &map_out, &map_in, &map_q, r0, c0, first, end, 1, desk, dead, take);
+        if (!finish_blocks<MODE>(a, &map_out, &map_in, &map_q, r0, c0, first, end, 1, desk, dead, take)) break;
       } else {
         float* part = a.parts + ((size_t)first_tile * ctas + rank) * a.width * kBM + 32 * quarter + lane;
         for (int c = first; c < end; ++c) {
@@ -714,7 +719,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     // one tile per cluster: its CTAs add up and finish blocks of their rows' columns in turn
     __syncthreads();
     cluster_sync();
-    if (warp < kPairEpi && !*dead) {
+    if (warp < kPairEpi && !__any_sync(0xFFFFFFFFu, *dead)) {
       int64_t tr, tc;
       tile_place<8>(a.tiles_r, a.tiles_c, first_tile, tr, tc);
       const int quarter = warp % 4;

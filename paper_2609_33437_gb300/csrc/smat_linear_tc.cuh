@@ -56,6 +56,31 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile
   return bar_try(bar, parity) || bar_wait_long(bar, parity, dead, errors);
 }
 
+// A whole warp's wait: its lanes may time out one by one, but they all go on, or all give up.
+__device__ __forceinline__ bool bar_wait_warp(uint32_t bar, uint32_t parity, volatile int* dead, int* errors) {
+  return __all_sync(0xFFFFFFFFu, bar_wait(bar, parity, dead, errors));
+}
+
+// After a wait has given up: what this CTA has under way itself (copies into its shared memory, multiplications) ends before
+// the CTA does. Until the phase is over, or kDrainNs; and for what signals another CTA's barrier, kPauseNs.
+constexpr unsigned long long kDrainNs = 100000000ull, kPauseNs = 1000000ull;
+static __device__ __noinline__ void bar_drain(uint32_t bar, uint32_t parity) {
+  unsigned long long begin, now;
+  asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(begin));
+  do {
+    if (bar_try(bar, parity)) return;
+    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(now));
+  } while (now - begin < kDrainNs);
+}
+static __device__ __noinline__ void drain_pause() {
+  unsigned long long begin, now;
+  asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(begin));
+  do {
+    __nanosleep(1000);
+    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(now));
+  } while (now - begin < kPauseNs);
+}
+
 __device__ __forceinline__ void tma_load(uint32_t to, const CUtensorMap* map, int x, int y, uint32_t bar) {
   asm volatile(
       "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(to),
