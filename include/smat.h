@@ -528,8 +528,10 @@ smat_status smat_act_grad8(const void* dy, int64_t lddy, const int8_t* q, int64_
                            int64_t lde, void* out, int64_t ldout, int64_t rows, int64_t cols, int32_t dtype,
                            int32_t act, smat_stream_t stream);
 
-/* Every wait inside a bf16 product is bounded (two seconds). One that runs out sets bit 0 here and leaves that
- * call's results unfinished. Reads and clears the bits of the current device; waits for the stream. */
+/* Every wait inside a bf16 product, and inside an fp32 one on the tensor cores, is bounded: two seconds, and two
+ * microseconds more for every 64 terms of the sum where it lasts for the whole sum. One that runs out sets bit 0 here and
+ * leaves that call's results unfinished, although the call returned SMAT_OK: poll after a synchronisation, before results
+ * are kept. Reads and clears the bits of the current device; waits for the stream. */
 smat_status smat_linear_poll_errors(smat_stream_t stream, int32_t* errors_out);
 
 /* SMAT_ABI_VERSION of the loaded library. */

@@ -483,7 +483,7 @@ __global__ void __launch_bounds__(kThreads, Ring<BN>::kCtas)
       tile_place<16>(a.tiles_r, a.tiles_c, tile, tr, tc);
       const int64_t r0 = tr * kBM + 32 * quarter, c0 = tc * BN;
       const uint32_t half = made & 1, sums = tmem + half * BN + ((uint32_t)(32 * quarter) << 16);
-      if (!bar_wait_warp(sums_full + 8 * half, made / 2 & 1, dead, a.errors)) break;
+      if (!bar_wait_warp(sums_full + 8 * half, made / 2 & 1, dead, a.errors, kWaitNs + slices * kSliceNs)) break;
       fence_after();
       auto release = [&] {  // this warp has what it needs of these sums
         fence_before();
@@ -685,7 +685,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       tile_place<8>(a.tiles_r, a.tiles_c, tile, tr, tc);
       const int64_t r0 = tr * kPairRows + (int)member * kBM + 32 * quarter, c0 = tc * a.width;
       const uint32_t half = made & 1, sums = tmem + half * kSums + ((uint32_t)(32 * quarter) << 16);
-      if (!bar_wait_warp(sums_full + 8 * half, made / 2 & 1, dead, a.errors)) break;
+      if (!bar_wait_warp(sums_full + 8 * half, made / 2 & 1, dead, a.errors, kWaitNs + slices * kSliceNs)) break;
       fence_after();
       auto release = [&] {  // this warp has what it needs of these sums
         fence_before();

@@ -12,7 +12,9 @@ constexpr int kBM = 128, kBK = 64;  // a tile's rows; a slice of the sum
 constexpr int kEpiWarps = 8;
 constexpr int kThreads = 32 * (kEpiWarps + 2);
 constexpr int kTmaWarp = kEpiWarps, kMmaWarp = kEpiWarps + 1;
-constexpr unsigned long long kWaitNs = 2000000000ull;
+// A wait's limit; one that lasts for a whole share of a sum has kSliceNs more for each slice of it. (A slice takes 290 ns where
+// one cluster works by itself and up to 450 with every SM copying; the largest share has 2^23 of them, 2.4 s.)
+constexpr unsigned long long kWaitNs = 2000000000ull, kSliceNs = 2000ull;
 
 __device__ __forceinline__ uint32_t smem_address(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
@@ -35,9 +37,10 @@ __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
   return ok != 0;
 }
 
-// Waits until the barrier's phase `parity` is over; false after kWaitNs, or once another wait of this CTA has given
+// Waits until the barrier's phase `parity` is over; false after `limit`, or once another wait of this CTA has given
 // up: the caller then leaves its loop, the CTA gives back its tensor memory and ends, and *errors tells the host.
-static __device__ __noinline__ bool bar_wait_long(uint32_t bar, uint32_t parity, volatile int* dead, int* errors) {
+static __device__ __noinline__ bool bar_wait_long(uint32_t bar, uint32_t parity, volatile int* dead, int* errors,
+                                                  unsigned long long limit) {
   unsigned long long begin, now;
   asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(begin));
   for (;;) {
@@ -45,20 +48,22 @@ static __device__ __noinline__ bool bar_wait_long(uint32_t bar, uint32_t parity,
       if (bar_try(bar, parity)) return true;
     asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(now));
     if (*dead) return false;
-    if (now - begin > kWaitNs) {
+    if (now - begin > limit) {
       *dead = 1;
       atomicOr(errors, 1);
       return false;
     }
   }
 }
-__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int* dead, int* errors) {
-  return bar_try(bar, parity) || bar_wait_long(bar, parity, dead, errors);
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int* dead, int* errors,
+                                         unsigned long long limit = kWaitNs) {
+  return bar_try(bar, parity) || bar_wait_long(bar, parity, dead, errors, limit);
 }
 
 // A whole warp's wait: its lanes may time out one by one, but they all go on, or all give up.
-__device__ __forceinline__ bool bar_wait_warp(uint32_t bar, uint32_t parity, volatile int* dead, int* errors) {
-  return __all_sync(0xFFFFFFFFu, bar_wait(bar, parity, dead, errors));
+__device__ __forceinline__ bool bar_wait_warp(uint32_t bar, uint32_t parity, volatile int* dead, int* errors,
+                                              unsigned long long limit = kWaitNs) {
+  return __all_sync(0xFFFFFFFFu, bar_wait(bar, parity, dead, errors, limit));
 }
 
 // After a wait has given up: what this CTA has under way itself (copies into its shared memory, multiplications) ends before
