@@ -12,7 +12,9 @@ surrounds them, and activations saved in 8 bits for the backward pass (include/s
 
 Tensors are CUDA tensors of one dtype per call (float32 or bfloat16); activations may have any number of leading
 dimensions and a row stride (the last dimension is contiguous). Argument marshalling only: every operator runs in
-the library's kernels, on the current stream or the one given.
+the library's kernels, on the current stream or the one given. The operators build no autograd graph and refuse tensors
+whose gradient or tangent that would lose: call them under torch.no_grad(), in a torch.autograd.Function, or on detached
+tensors; the layers are differentiable.
 """
 
 import ctypes
@@ -20,6 +22,7 @@ import struct
 from typing import Optional, Tuple, Union
 
 import torch
+import torch.autograd.forward_ad as forward_ad
 
 from . import smat as S
 
@@ -113,6 +116,20 @@ def _rows(name: str, t: torch.Tensor) -> Tuple[int, int, int]:
     return rows, cols, ld
 
 
+def _no_graph(*tensors: Optional[torch.Tensor]) -> None:
+    """The operators' results belong to no graph: refuses what autograd would lose without a word."""
+    if torch.is_grad_enabled():
+        for t in tensors:
+            if t is not None and t.requires_grad:
+                raise ValueError("the operator builds no graph, and an argument requires a gradient: use Linear8 or Mlp8, "
+                                 "torch.no_grad() or detach()")
+    if forward_ad._current_level >= 0:
+        for t in tensors:
+            if t is not None and forward_ad.unpack_dual(t).tangent is not None:
+                raise ValueError("an argument has a tangent, which the operator would lose: there is no forward-mode "
+                                 "derivative")
+
+
 def _act(act: str) -> int:
     a = ACTS.get(act)
     if a is None:
@@ -192,6 +209,7 @@ def linear(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor] = None
     x [..., k], w [n, k], bias [n], residual and out [..., n]; out may be the residual."""
     if stream is not None:
         return _on(stream, linear, x, w, bias, act, residual, save, out)
+    _no_graph(x, w, bias, residual)
     a = _act(act)
     rows, k, ldx = _rows("x", x)
     code = S.dtype_code(x.dtype)
@@ -222,6 +240,7 @@ def linear_grad_input(dy: torch.Tensor, w: torch.Tensor, act: str = "none", save
     from the pre-activation `saved` ([..., k]; none with act "none"). dy [..., n], w [n, k]."""
     if stream is not None:
         return _on(stream, linear_grad_input, dy, w, act, saved, out)
+    _no_graph(dy, w)
     a = _act(act)
     if (a != 0) != (saved is not None):
         raise ValueError("saved: needed with an activation, and only then")
@@ -253,8 +272,9 @@ def linear_grad_weight(dy: torch.Tensor, x: Union[torch.Tensor, Packed8], act: s
     the input from. With accumulate, dW is added to `out`, and db to `bias_out` where that is given."""
     if stream is not None:
         return _on(stream, linear_grad_weight, dy, x, act, bias, out, bias_out, accumulate)
-    a = _act(act)
     packed = isinstance(x, Packed8)
+    _no_graph(dy, None if packed else x)
+    a = _act(act)
     if a and not packed:
         raise ValueError("act: is applied to x in 8 bits only")
     if accumulate and out is None:
@@ -293,6 +313,7 @@ def pack8(x: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> Packed
     """x in 8 bits."""
     if stream is not None:
         return _on(stream, pack8, x)
+    _no_graph(x)
     rows, cols, ldx = _rows("x", x)
     code = S.dtype_code(x.dtype)
     p = Packed8._make(x.shape, rows, cols, x.device)
@@ -324,6 +345,7 @@ def act_grad8(dy: torch.Tensor, saved: Packed8, act: str, out: Optional[torch.Te
     """dy * act'(h^): a gradient back through an activation, from the pre-activation's 8 bits."""
     if stream is not None:
         return _on(stream, act_grad8, dy, saved, act, out)
+    _no_graph(dy)
     a = _act(act)
     rows, cols, lddy = _rows("dy", dy)
     code = S.dtype_code(dy.dtype)
@@ -396,15 +418,16 @@ class _Linear8(torch.autograd.Function):
     def backward(ctx, grad, _):
         w, hq, he, xq, xe, anchor = ctx.saved_tensors
         need_x, need_w, need_b, need_r, _ = ctx.needs_input_grad
-        dy = _rows_like(grad.detach())
-        dh = act_grad8(dy, Packed8(hq, he), ctx.act) if hq is not None else dy
         dx = dw = db = None
-        if need_x:
-            dx = linear_grad_input(dh, w)
-        if need_w:
-            dw, db = linear_grad_weight(dh, Packed8(xq, xe), bias=need_b)
-        elif need_b:
-            db = _row_sums(dh)
+        with torch.no_grad():
+            dy = _rows_like(grad)
+            dh = act_grad8(dy, Packed8(hq, he), ctx.act) if hq is not None else dy
+            if need_x:
+                dx = linear_grad_input(dh, w)
+            if need_w:
+                dw, db = linear_grad_weight(dh, Packed8(xq, xe), bias=need_b)
+            elif need_b:
+                db = _row_sums(dh)
         return *_first_only(anchor, grad, (dx, dw, db)), (grad if need_r else None), None
 
 
@@ -427,20 +450,21 @@ class _Mlp8(torch.autograd.Function):
         w1, w2, xq, xe, hq, he, anchor = ctx.saved_tensors
         need_x, need_w1, need_b1, need_w2, need_b2, need_r, _ = ctx.needs_input_grad
         h = Packed8(hq, he)
-        dy = _rows_like(grad.detach())
         dx = dw1 = db1 = dw2 = db2 = None
-        if need_w2:
-            dw2, db2 = linear_grad_weight(dy, h, ctx.act, bias=need_b2)
-        elif need_b2:
-            db2 = _row_sums(dy)
-        if need_x or need_w1 or need_b1:
-            dh = linear_grad_input(dy, w2, ctx.act, h if ctx.act != "none" else None)
-            if need_w1:
-                dw1, db1 = linear_grad_weight(dh, Packed8(xq, xe), bias=need_b1)
-            elif need_b1:
-                db1 = _row_sums(dh)
-            if need_x:
-                dx = linear_grad_input(dh, w1)
+        with torch.no_grad():
+            dy = _rows_like(grad)
+            if need_w2:
+                dw2, db2 = linear_grad_weight(dy, h, ctx.act, bias=need_b2)
+            elif need_b2:
+                db2 = _row_sums(dy)
+            if need_x or need_w1 or need_b1:
+                dh = linear_grad_input(dy, w2, ctx.act, h if ctx.act != "none" else None)
+                if need_w1:
+                    dw1, db1 = linear_grad_weight(dh, Packed8(xq, xe), bias=need_b1)
+                elif need_b1:
+                    db1 = _row_sums(dh)
+                if need_x:
+                    dx = linear_grad_input(dh, w1)
         return *_first_only(anchor, grad, (dx, dw1, db1, dw2, db2)), (grad if need_r else None), None
 
 

@@ -9,12 +9,14 @@ from paper_2609_33437_gb300 import linear as L
 
 
 def _linear(x, w, bias=None, act="none", residual=None, save=False, out=None, stream=None):
+    L._no_graph(x, w, bias, residual)
     h = x @ w.T + (bias if bias is not None else 0)
     y = R.act(act, h) + (residual if residual is not None else 0)
-    return (y, _pack8(h)) if save else y
+    return (y, _pack8(h.detach())) if save else y
 
 
 def _pack8(x, stream=None):
+    L._no_graph(x)
     q, e = R.pack(x.reshape(-1, x.shape[-1]))
     return L.Packed8(q.view(x.shape), e.view(*x.shape[:-1], -1))
 
@@ -24,16 +26,19 @@ def _value(p, dtype):
 
 
 def _grad_input(dy, w, act="none", saved=None, out=None, stream=None):
+    L._no_graph(dy, w)
     return dy @ w * (R.slope(act, _value(saved, dy.dtype)) if saved is not None else 1)
 
 
 def _grad_weight(dy, x, act="none", bias=False, out=None, bias_out=None, accumulate=False, stream=None):
+    L._no_graph(dy, x if isinstance(x, torch.Tensor) else None)
     v = R.act(act, _value(x, dy.dtype)) if isinstance(x, L.Packed8) else x
     dy = dy.reshape(-1, dy.shape[-1])
     return dy.T @ v.reshape(dy.shape[0], -1), dy.sum(0) if bias else None
 
 
 def _act_grad8(dy, saved, act, out=None, stream=None):
+    L._no_graph(dy)
     return dy * R.slope(act, _value(saved, dy.dtype))
 
 
