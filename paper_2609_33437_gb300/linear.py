@@ -97,6 +97,8 @@ def _rows(name: str, t: torch.Tensor) -> Tuple[int, int, int]:
         if d == 0:
             raise ValueError(f"{name}: needs at least one dimension")
         cols, inner = t.shape[-1], t.stride(-1)
+        if 0 in t.shape[:-1]:  # no row, whatever the strides say
+            return 0, cols, cols
         rows, ld = 1, cols
         for n, s in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
             if n == 1:
