@@ -446,7 +446,7 @@ smat_status smat_merge_ties_thresholds(const smat_merge_tensor* tensors, int32_t
  * lose 0.02 of it). q is [rows, columns] with row stride ldq, e is
  * [rows, ceil(columns / 32)] with row stride lde.
  *
- * rows, k and n may be 0 (sums over nothing are 0). Outputs must not overlap inputs or one another, except that
+ * rows, k and n may be 0 (sums over nothing are 0); pointers to nothing may be NULL. Outputs must not overlap inputs or one another, except that
  * y may be the residual itself (same pointer and stride). */
 typedef enum {
   SMAT_ACT_NONE = 0,

@@ -289,10 +289,11 @@ static smat_status grad_input(const smat_grad_input_args* a, void* d_workspace, 
   smat_status st = check_sizes(a->rows, a->k, a->n, a->dtype, a->act);
   if (st != SMAT_OK) return st;
   const bool act = a->act != SMAT_ACT_NONE;
-  if (act != (a->q != nullptr) || act != (a->e != nullptr))
+  const int64_t m = a->rows, k = a->k, n = a->n;
+  const bool read = act && m > 0 && k > 0;  // of nothing q and e may be NULL, as memory of no bytes often is
+  if ((read && (!a->q || !a->e)) || (!act && (a->q || a->e)))
     return lfail(SMAT_ERR_INVALID_ARG, "q and e: give both with an activation, neither without");
   const size_t es = elem_of(a->dtype);
-  const int64_t m = a->rows, k = a->k, n = a->n;
   const Mat mats[] = {
       {"dx", a->dx, m, k, a->lddx, es, true},
       {"dy", a->dy, k ? m : 0, n, a->lddy, es, false},
@@ -328,7 +329,7 @@ static smat_status grad_weight(const smat_grad_weight_args* a, void* d_workspace
   const int64_t m = a->rows, k = a->k, n = a->n;
   const bool some = m > 0 && k > 0 && n > 0;
   if (some && !a->x == !a->q) return lfail(SMAT_ERR_INVALID_ARG, "give x, or q and e, not both");
-  if (!a->q && a->act != SMAT_ACT_NONE)
+  if (!a->q && a->act != SMAT_ACT_NONE && (some || a->x))  // of nothing q may be NULL
     return lfail(SMAT_ERR_INVALID_ARG, "an activation is applied to x in 8 bits only");
   if ((a->accumulate & ~(SMAT_ACCUMULATE_DW | SMAT_ACCUMULATE_DB)) || a->reserved)
     return lfail(SMAT_ERR_UNSUPPORTED, "unknown accumulate flags 0x%x", a->accumulate);
