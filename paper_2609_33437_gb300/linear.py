@@ -90,6 +90,8 @@ def _rows(name: str, t: torch.Tensor) -> Tuple[int, int, int]:
     if not t.is_cuda:
         raise ValueError(f"{name}: must be a CUDA tensor")
     d = t.dim()
+    if 0 in t.shape[:-1]:  # no row, whatever the strides say
+        return 0, t.shape[-1], t.shape[-1]
     if d == 2:
         rows, cols = t.shape
         ld, inner = t.stride()
@@ -97,8 +99,6 @@ def _rows(name: str, t: torch.Tensor) -> Tuple[int, int, int]:
         if d == 0:
             raise ValueError(f"{name}: needs at least one dimension")
         cols, inner = t.shape[-1], t.stride(-1)
-        if 0 in t.shape[:-1]:  # no row, whatever the strides say
-            return 0, cols, cols
         rows, ld = 1, cols
         for n, s in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
             if n == 1:
@@ -371,9 +371,16 @@ def poll_errors(stream: Optional[torch.cuda.Stream] = None) -> int:
 
 
 # ------------------------------------------------------------------- layers ---
-def _rows_like(g: torch.Tensor) -> torch.Tensor:
-    """An incoming gradient as the operators take it: broadcast or strided ones are written out."""
-    return g if g.is_contiguous() else g.contiguous()
+def _rows_like(t: Optional[torch.Tensor]) -> Optional[torch.Tensor]:
+    """A layer's input as the operators take it: one that is transposed, broadcast or strided otherwise than as rows of one
+    stride is written out, as torch.nn.Linear does."""
+    if t is None or t.is_contiguous():
+        return t
+    try:
+        _rows("", t)
+        return t
+    except ValueError:
+        return t.contiguous()
 
 
 def _row_sums(dy: torch.Tensor) -> torch.Tensor:
@@ -408,6 +415,7 @@ class _Linear8(torch.autograd.Function):
     def forward(ctx, x, w, b, residual, act):
         ctx.act = act
         ctx.set_materialize_grads(False)
+        x, w, b, residual = map(_rows_like, (x, w, b, residual))
         need_h = act != "none" and any(ctx.needs_input_grad[:3])
         y = linear(x, w, b, act, residual, save=need_h)
         y, h = y if need_h else (y, None)
@@ -422,7 +430,7 @@ class _Linear8(torch.autograd.Function):
         need_x, need_w, need_b, need_r, _ = ctx.needs_input_grad
         dx = dw = db = None
         with torch.no_grad():
-            dy = _rows_like(grad)
+            dy = grad.contiguous()
             dh = act_grad8(dy, Packed8(hq, he), ctx.act) if hq is not None else dy
             if need_x:
                 dx = linear_grad_input(dh, w)
@@ -440,6 +448,7 @@ class _Mlp8(torch.autograd.Function):
     def forward(ctx, x, w1, b1, w2, b2, residual, act):
         ctx.act = act
         ctx.set_materialize_grads(False)
+        x, w1, b1, w2, b2, residual = map(_rows_like, (x, w1, b1, w2, b2, residual))
         a, h = linear(x, w1, b1, act, save=True)
         y = linear(a, w2, b2, "none", residual)
         p = pack8(x) if ctx.needs_input_grad[1] else None
@@ -454,7 +463,7 @@ class _Mlp8(torch.autograd.Function):
         h = Packed8(hq, he)
         dx = dw1 = db1 = dw2 = db2 = None
         with torch.no_grad():
-            dy = _rows_like(grad)
+            dy = grad.contiguous()
             if need_w2:
                 dw2, db2 = linear_grad_weight(dy, h, ctx.act, bias=need_b2)
             elif need_b2:
@@ -483,7 +492,8 @@ class Linear8(torch.nn.Linear):
 
     def forward(self, x: torch.Tensor, residual: Optional[torch.Tensor] = None) -> torch.Tensor:
         if not torch.is_grad_enabled():
-            return linear(x, self.weight, self.bias, self.act, residual)
+            x, w, b, residual = map(_rows_like, (x, self.weight, self.bias, residual))
+            return linear(x, w, b, self.act, residual)
         return _Linear8.apply(x, self.weight, self.bias, residual, self.act)[0]
 
 
@@ -501,6 +511,7 @@ class Mlp8(torch.nn.Module):
 
     def forward(self, x: torch.Tensor, residual: Optional[torch.Tensor] = None) -> torch.Tensor:
         if not torch.is_grad_enabled():
-            a = linear(x, self.fc1.weight, self.fc1.bias, self.act)
-            return linear(a, self.fc2.weight, self.fc2.bias, "none", residual)
+            x, w1, b1, w2, b2, residual = map(_rows_like, (x, self.fc1.weight, self.fc1.bias, self.fc2.weight, self.fc2.bias,
+                                                           residual))
+            return linear(linear(x, w1, b1, self.act), w2, b2, "none", residual)
         return _Mlp8.apply(x, self.fc1.weight, self.fc1.bias, self.fc2.weight, self.fc2.bias, residual, self.act)[0]

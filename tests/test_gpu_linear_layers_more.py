@@ -49,3 +49,56 @@ def test_operators_refuse_what_requires_a_gradient():
     with torch.no_grad():
         y = L.linear(x, m.weight, m.bias)
     assert torch.equal(y, L.linear(x, m.weight.detach(), m.bias.detach()))
+
+
+def _same_as_contiguous(m, x, residual=None):
+    """Outputs and gradients of inputs of any stride are those of their contiguous copies."""
+    res = []
+    for f in (lambda t: t, lambda t: t.contiguous()):
+        for p in m.parameters():
+            p.grad = None
+        leaf = x.detach().requires_grad_(True)  # keeps the strides
+        y = m(f(leaf), residual=None if residual is None else f(residual))
+        y.float().square().sum().backward()
+        with torch.no_grad():
+            z = m(f(x.detach()), residual=None if residual is None else f(residual))
+        res.append([y, z, leaf.grad, *(p.grad for p in m.parameters())])
+    assert res[0][0].shape == (*x.shape[:-1], 96)
+    for a, b in zip(*res):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_inputs_of_any_stride(dtype):
+    for m in _layers(dtype):
+        base = _input(12, 10, 96, dtype=dtype, grad=False)
+        _same_as_contiguous(m, base.transpose(0, 1))                             # sequence first
+        _same_as_contiguous(m, _input(96, 50, dtype=dtype, grad=False).T)        # a transposed view
+        _same_as_contiguous(m, _input(20, 192, dtype=dtype, grad=False)[:, ::2])  # every second column
+        _same_as_contiguous(m, _input(96, dtype=dtype, grad=False).expand(7, 96))  # one row, broadcast
+        _same_as_contiguous(m, base[:, :4], residual=_input(96, 4, 12, dtype=dtype, grad=False).permute(2, 1, 0))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_weights_of_any_stride(dtype):
+    """As a parametrisation or a tied, transposed weight leaves them."""
+    for m in _layers(dtype):
+        other = type(m)(96, 96 if isinstance(m, L.Linear8) else 160, act=m.act, device="cuda", dtype=dtype)
+        for p, q in zip(m.parameters(), other.parameters()):
+            q.data = p.data.T.contiguous().T if p.dim() == 2 else torch.stack([p.data, p.data], 1)[:, 0]
+            assert not q.is_contiguous()
+        x = _input(40, 96, dtype=dtype)
+        for k in (m, other):
+            k(x).float().square().sum().backward()
+        for p, q in zip(m.parameters(), other.parameters()):
+            assert torch.equal(p.grad, q.grad)
+
+
+@pytest.mark.parametrize("shape", [(0, 96), (3, 0, 96), (0, 3, 96)])
+def test_batches_of_nothing(shape):
+    for m in _layers(BF):
+        x = _input(*shape, dtype=BF)
+        y = m(x, residual=x)
+        assert y.shape == shape
+        y.sum().backward()
+        assert x.grad.shape == shape and all(not p.grad.any() for p in m.parameters())

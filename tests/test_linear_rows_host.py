@@ -17,6 +17,8 @@ class Fake:
 def test_no_rows(shape):
     for t in (torch.zeros(shape), torch.zeros(*shape[:-1], 16)[..., 4:12], torch.zeros(*shape[:-2], shape[-2] + 2, 8)[..., :shape[-2], :]):
         assert L._rows("t", Fake(t)) == (0, 8, 8)
+    # as the gradient of a sum arrives: one number for all, of which there are none
+    assert L._rows("t", Fake(torch.zeros(()).expand(shape))) == (0, 8, 8)
 
 
 @pytest.mark.parametrize("shape,rows", [((5, 0), 5), ((2, 3, 0), 6), ((0, 0), 0)])
