@@ -383,6 +383,22 @@ def _rows_like(t: Optional[torch.Tensor]) -> Optional[torch.Tensor]:
         return t.contiguous()
 
 
+def _autocast(*tensors: Optional[torch.Tensor]):
+    """Under torch.autocast, the tensors in its type, as torch.nn.Linear takes them (64-bit ones stay as they are)."""
+    if not torch.is_autocast_enabled("cuda"):
+        return tensors
+    dtype = torch.get_autocast_dtype("cuda")
+    return tuple(t if t is None or t.dtype is torch.float64 else t.to(dtype) for t in tensors)
+
+
+def _with_residual(layer, x: torch.Tensor, residual: Optional[torch.Tensor]) -> torch.Tensor:
+    """layer(residual); under autocast one of a wider type is added afterwards, and is the result's type, as it would be
+    beside torch.nn.Linear."""
+    if residual is None or residual.dtype is x.dtype or not torch.is_autocast_enabled("cuda"):
+        return layer(residual)
+    return layer(None) + residual
+
+
 def _row_sums(dy: torch.Tensor) -> torch.Tensor:
     """db alone, of a layer whose weight is frozen: the weight gradient's own sums, with no columns of x."""
     dy = dy.reshape(-1, dy.shape[-1])
@@ -482,7 +498,8 @@ class _Mlp8(torch.autograd.Function):
 class Linear8(torch.nn.Linear):
     """torch.nn.Linear followed by an activation and a residual; its backward pass reads the input and, with an
     activation, the pre-activation in 8 bits instead of keeping them whole. First derivatives only: one taken of its
-    gradients raises RuntimeError."""
+    gradients raises RuntimeError. Inputs and weights may have any strides; torch.autocast to bf16 casts them as it does for
+    torch.nn.Linear."""
 
     def __init__(self, in_features: int, out_features: int, bias: bool = True, act: str = "none", device=None,
                  dtype=None):
@@ -491,16 +508,20 @@ class Linear8(torch.nn.Linear):
         self.act = act
 
     def forward(self, x: torch.Tensor, residual: Optional[torch.Tensor] = None) -> torch.Tensor:
+        x, w, b = _autocast(x, self.weight, self.bias)
+        return _with_residual(lambda r: self._forward(x, w, b, r), x, residual)
+
+    def _forward(self, x, w, b, residual):
         if not torch.is_grad_enabled():
-            x, w, b, residual = map(_rows_like, (x, self.weight, self.bias, residual))
+            x, w, b, residual = map(_rows_like, (x, w, b, residual))
             return linear(x, w, b, self.act, residual)
-        return _Linear8.apply(x, self.weight, self.bias, residual, self.act)[0]
+        return _Linear8.apply(x, w, b, residual, self.act)[0]
 
 
 class Mlp8(torch.nn.Module):
     """y = act(x W1^T + b1) W2^T + b2 + residual. Between forward and backward it holds x and the pre-activation in
     8 bits, 33 / 32 bytes per element; the second layer's input is recomputed from the pre-activation. First
-    derivatives only, as Linear8."""
+    derivatives only, inputs and autocast as Linear8."""
 
     def __init__(self, features: int, hidden: int, bias: bool = True, act: str = "gelu", device=None, dtype=None):
         super().__init__()
@@ -510,8 +531,11 @@ class Mlp8(torch.nn.Module):
         self.fc2 = torch.nn.Linear(hidden, features, bias, device=device, dtype=dtype)
 
     def forward(self, x: torch.Tensor, residual: Optional[torch.Tensor] = None) -> torch.Tensor:
+        x, *w = _autocast(x, self.fc1.weight, self.fc1.bias, self.fc2.weight, self.fc2.bias)
+        return _with_residual(lambda r: self._forward(x, *w, r), x, residual)
+
+    def _forward(self, x, w1, b1, w2, b2, residual):
         if not torch.is_grad_enabled():
-            x, w1, b1, w2, b2, residual = map(_rows_like, (x, self.fc1.weight, self.fc1.bias, self.fc2.weight, self.fc2.bias,
-                                                           residual))
+            x, w1, b1, w2, b2, residual = map(_rows_like, (x, w1, b1, w2, b2, residual))
             return linear(linear(x, w1, b1, self.act), w2, b2, "none", residual)
-        return _Mlp8.apply(x, self.fc1.weight, self.fc1.bias, self.fc2.weight, self.fc2.bias, residual, self.act)[0]
+        return _Mlp8.apply(x, w1, b1, w2, b2, residual, self.act)[0]

@@ -102,3 +102,34 @@ def test_batches_of_nothing(shape):
         assert y.shape == shape
         y.sum().backward()
         assert x.grad.shape == shape and all(not p.grad.any() for p in m.parameters())
+
+
+@pytest.mark.parametrize("grad", [True, False])
+def test_autocast(grad):
+    """fp32 weights under autocast to bf16 are the bf16 layer's, for inputs of either type; gradients come in the tensors' own
+    types; a residual of 32 bits keeps them and the result's type, as beside torch.nn.Linear."""
+    for m, low in zip(_layers(F32), _layers(BF)):
+        low.load_state_dict({k: v.to(BF) for k, v in m.state_dict().items()})
+        plain = torch.nn.Linear(96, 96, device="cuda")
+        for dtype in (F32, BF):
+            x, y = _input(40, 96, dtype=dtype), _input(40, 96, dtype=BF)
+            wide = torch.randn(40, 96, device="cuda")
+            with torch.set_grad_enabled(grad):
+                want = low(y, residual=y)
+                with torch.autocast("cuda", torch.bfloat16):
+                    got, bare = m(x, residual=x.to(BF)), m(x)
+                    sums = m(x, residual=wide)
+                    assert sums.dtype is (plain(x) + wide).dtype is F32
+                assert got.dtype is bare.dtype is BF and torch.equal(got, want)
+                assert torch.equal(sums, bare + wide)
+            if grad:
+                for net, z, t in ((m, got, x), (low, want, y)):
+                    for p in net.parameters():
+                        p.grad = None
+                    z.float().square().sum().backward()
+                for p, q in zip((x, *m.parameters()), (y, *low.parameters())):
+                    assert p.grad.dtype is p.dtype and torch.equal(p.grad.to(BF), q.grad)
+        with torch.autocast("cuda", torch.float16), pytest.raises(TypeError):
+            m(x)  # a type that the operators do not have
+        with torch.autocast("cuda", enabled=False):
+            assert m(x.detach().float()).dtype is F32
