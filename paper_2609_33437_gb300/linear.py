@@ -90,15 +90,17 @@ def _rows(name: str, t: torch.Tensor) -> Tuple[int, int, int]:
     if not t.is_cuda:
         raise ValueError(f"{name}: must be a CUDA tensor")
     d = t.dim()
-    if 0 in t.shape[:-1]:  # no row, whatever the strides say
-        return 0, t.shape[-1], t.shape[-1]
     if d == 2:
         rows, cols = t.shape
         ld, inner = t.stride()
+        if rows == 0:  # whatever the strides say
+            return 0, cols, cols
     else:
         if d == 0:
             raise ValueError(f"{name}: needs at least one dimension")
         cols, inner = t.shape[-1], t.stride(-1)
+        if 0 in t.shape[:-1]:
+            return 0, cols, cols
         rows, ld = 1, cols
         for n, s in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
             if n == 1:
@@ -118,15 +120,15 @@ def _rows(name: str, t: torch.Tensor) -> Tuple[int, int, int]:
     return rows, cols, ld
 
 
-def _no_graph(*tensors: Optional[torch.Tensor]) -> None:
-    """The operators' results belong to no graph: refuses what autograd would lose without a word."""
-    if torch.is_grad_enabled():
-        for t in tensors:
-            if t is not None and t.requires_grad:
-                raise ValueError("the operator builds no graph, and an argument requires a gradient: use Linear8 or Mlp8, "
-                                 "torch.no_grad() or detach()")
+def _no_graph(a: torch.Tensor, b: Optional[torch.Tensor] = None, c: Optional[torch.Tensor] = None,
+              d: Optional[torch.Tensor] = None) -> None:
+    """The operators' results belong to no graph: refuses what autograd would lose without a word. (0.3 us of a call.)"""
+    if torch.is_grad_enabled() and (a.requires_grad or (b is not None and b.requires_grad)
+                                    or (c is not None and c.requires_grad) or (d is not None and d.requires_grad)):
+        raise ValueError("the operator builds no graph, and an argument requires a gradient: use Linear8 or Mlp8, "
+                         "torch.no_grad() or detach()")
     if forward_ad._current_level >= 0:
-        for t in tensors:
+        for t in (a, b, c, d):
             if t is not None and forward_ad.unpack_dual(t).tangent is not None:
                 raise ValueError("an argument has a tangent, which the operator would lose: there is no forward-mode "
                                  "derivative")
