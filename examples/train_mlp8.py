@@ -62,7 +62,12 @@ def train(steps=200, width=256, hidden=1024, blocks=4, batch=2056, classes=10, d
         opt.zero_grad()
         losses.append(loss.detach())
     sched.close()
-    return torch.stack(losses).tolist()
+    losses = torch.stack(losses).tolist()
+    # the losses have been waited for: a look at what no call returns. Before a checkpoint is written is the place for it in
+    # a longer run.
+    if L.poll_errors():
+        raise RuntimeError("a wait inside a product ran out: some step's gradients are unfinished")
+    return losses
 
 
 if __name__ == "__main__":

@@ -366,7 +366,8 @@ def act_grad8(dy: torch.Tensor, saved: Packed8, act: str, out: Optional[torch.Te
 
 def poll_errors(stream: Optional[torch.cuda.Stream] = None) -> int:
     """Read and clear the products' device error flags (0 = none; 1 = a bounded wait ran out and a result is
-    unfinished); synchronises the stream."""
+    unfinished, of either dtype); synchronises the stream. No call returns this, and no layer asks for it: poll where the
+    program waits for the GPU anyway, before results are kept (a loss that is read, a checkpoint)."""
     v = ctypes.c_int32()
     S.check("smat_linear_poll_errors", S.load_library().smat_linear_poll_errors(S._stream_handle(stream), ctypes.byref(v)))
     return v.value
@@ -501,7 +502,7 @@ class Linear8(torch.nn.Linear):
     """torch.nn.Linear followed by an activation and a residual; its backward pass reads the input and, with an
     activation, the pre-activation in 8 bits instead of keeping them whole. First derivatives only: one taken of its
     gradients raises RuntimeError. Inputs and weights may have any strides; torch.autocast to bf16 casts them as it does for
-    torch.nn.Linear."""
+    torch.nn.Linear. What poll_errors says of its products is for the caller to ask."""
 
     def __init__(self, in_features: int, out_features: int, bias: bool = True, act: str = "none", device=None,
                  dtype=None):
@@ -523,7 +524,7 @@ class Linear8(torch.nn.Linear):
 class Mlp8(torch.nn.Module):
     """y = act(x W1^T + b1) W2^T + b2 + residual. Between forward and backward it holds x and the pre-activation in
     8 bits, 33 / 32 bytes per element; the second layer's input is recomputed from the pre-activation. First
-    derivatives only, inputs and autocast as Linear8."""
+    derivatives only, inputs, autocast and poll_errors as Linear8."""
 
     def __init__(self, features: int, hidden: int, bias: bool = True, act: str = "gelu", device=None, dtype=None):
         super().__init__()

@@ -1,6 +1,9 @@
 """The layers (Linear8, Mlp8) on the GPU beside their first derivatives: graphs of gradients, and the inputs that
 torch.nn.Linear takes."""
 
+import importlib.util
+import os
+
 import pytest
 import torch
 
@@ -133,3 +136,16 @@ def test_autocast(grad):
             m(x)  # a type that the operators do not have
         with torch.autocast("cuda", enabled=False):
             assert m(x.detach().float()).dtype is F32
+
+
+def test_the_example_does_not_keep_unfinished_results(monkeypatch):
+    """A training loop ends with an error, not with losses, where the products' flag is up."""
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "train_mlp8.py")
+    spec = importlib.util.spec_from_file_location("train_mlp8", path)
+    ex = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(ex)
+    kw = dict(steps=2, width=64, hidden=96, blocks=1, batch=64)
+    assert len(ex.train(**kw)) == 2
+    monkeypatch.setattr(ex.L, "poll_errors", lambda stream=None: 1)
+    with pytest.raises(RuntimeError, match="unfinished"):
+        ex.train(**kw)
