@@ -280,6 +280,7 @@ __device__ __forceinline__ bool finish_block(const Args& a, const CUtensorMap* m
 // the rows read is asked for first, all of it.
 template <int MODE, int N>
 __device__ __forceinline__ void finish_column(const Args& a, int64_t i, int64_t j, float (&v)[N]) {
+  static_assert(MODE != kGradWeight, "weight gradients are wide products");
   const Product& p = a.p;
   if (i >= p.I) return;
   const int rows = (int)(p.I - i < N ? p.I - i : N);
@@ -313,27 +314,20 @@ __device__ __forceinline__ void finish_column(const Args& a, int64_t i, int64_t 
 #pragma unroll
       for (int t = 0; t < N; ++t) v[t] += x[t];
     }
-  } else if (MODE == kGradInput ? p.act != SMAT_ACT_NONE : p.accumulate != 0) {
+  } else if (p.act != SMAT_ACT_NONE) {
     float x[N];
-    if (MODE == kGradInput) {
-      const int8_t* q = p.q + i * p.ldq + j;
-      const uint8_t* e = p.e + i * p.lde + j / kGroup;
-      int qs[N];
-      uint32_t es[N];
+    const int8_t* q = p.q + i * p.ldq + j;
+    const uint8_t* e = p.e + i * p.lde + j / kGroup;
+    int qs[N];
+    uint32_t es[N];
 #pragma unroll
-      for (int t = 0; t < N; ++t) {
-        qs[t] = t < mine ? q[t * p.ldq] : 0;
-        es[t] = t < mine ? e[t * p.lde] : 0;
-      }
-#pragma unroll
-      for (int t = 0; t < N; ++t) x[t] = (float)qs[t] * unpack_scale(es[t]);
-      SMAT_WITH_ACT(p.act, _Pragma("unroll") for (int t = 0; t < N; ++t) v[t] *= act_slope<ACT, bf16>(x[t]))
-    } else {
-#pragma unroll
-      for (int t = 0; t < N; ++t) x[t] = t < mine ? to_float(out[t * p.ldo]) : 0.0f;
-#pragma unroll
-      for (int t = 0; t < N; ++t) v[t] += x[t];
+    for (int t = 0; t < N; ++t) {
+      qs[t] = t < mine ? q[t * p.ldq] : 0;
+      es[t] = t < mine ? e[t * p.lde] : 0;
     }
+#pragma unroll
+    for (int t = 0; t < N; ++t) x[t] = (float)qs[t] * unpack_scale(es[t]);
+    SMAT_WITH_ACT(p.act, _Pragma("unroll") for (int t = 0; t < N; ++t) v[t] *= act_slope<ACT, bf16>(x[t]))
   }
 #pragma unroll
   for (int t = 0; t < N; ++t)
