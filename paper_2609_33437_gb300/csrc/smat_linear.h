@@ -80,7 +80,9 @@ cudaError_t launch_row_sums(const void* dy, int64_t lddy, void* db, int64_t rows
 // A weight gradient over 1 to kOuterRows rows (smat_linear_outer.cu): x, or q and e read through act; db may be NULL. Up to
 // these many it is faster than the products' tiles (4096 x 4096, call after call: bf16 one row 7.0 us against 18, 8 rows 17.6
 // against 18.1, with rows off 16 bytes 18 against 37; fp32 one row 12 us against 80, 16 rows 37 against 38; with nothing in L2
-// 14 against 26, 25.6 against 26.1, 24 against 92, 50 against 61).
+// 14 against 26, 25.6 against 26.1, 24 against 92, 50 against 61). With other operands every call, bf16 8 and fp32 16 rows: 128 x
+// 64 3.3 us against 5.2 and 3.1 against 5.7, 512 x 512 3.2 and 5.4, 3.5 and 5.7, 896 x 4864 9.1 and 11.2, 16.2 and 16.8, 4096 x
+// 1024 9.2 and 10.3, 16.2 and 24.9; 11008 x 4096 39.2 and 38.1, 91.5 and 86.5, where it no longer is, by 3 and 6%.
 constexpr int64_t kOuterRows = 16, kOuterRowsBf16 = 8;
 struct Outer {
   const void* dy;

@@ -2,13 +2,13 @@
 //
 // Large ones run on the tensor cores. A first kernel cuts every fp32 value into three bf16 values, hi + mid + lo, each the
 // nearest to what is left: exactly the value (from 2^-110 on; below, lo's last bits fall under bf16's smallest number, 2^-133).
-// mid is at most 2^-8 and lo 2^-17 of the value's power of two (twice that next to the largest fp32 number), so the three of nine products that are left out, mid lo, lo
-// mid and lo lo, are below 2^-24 (1 + 2^-9) of the whole, like one rounding, and of either sign. The product then is the other
-// six, for a slice of 64 of the sum at a time and the small ones first, so that what an addition in tensor memory cuts off is
-// cut off sums that are small yet (the last four additions of a slice cut off up to 2^-23 of it each); eight warps add the
-// slices' sums in registers, rounding to nearest. Measured: 4096 x 4096 x 4096 585 us, 235 TFLOP/s of fp32 products where the fp32 units
-// reach 75 at most; 515 x 896 x 4864 36 us, 10 of them to cut 19 MB, the rest bound by the copies into shared memory (110 KB
-// for 1,920 cycles of multiplications). Its error against 64 bits there is 1.9e-7, a plain fp32 product's 6.2e-7.
+// mid is at most 2^-8 and lo 2^-17 of the value's power of two (twice that next to the largest fp32 number), so the three of
+// nine products that are left out, mid lo, lo mid and lo lo, are below 2^-24 (1 + 2^-9) of the whole, like one rounding, and of
+// either sign. The product then is the other six, for a slice of 64 of the sum at a time and the small ones first, so that what
+// an addition in tensor memory cuts off is cut off sums that are small yet (the last four additions of a slice cut off up to 2^-23 of it each); eight warps add the
+// slices' sums in registers, rounding to nearest. Measured: 4096 x 4096 x 4096 576 us, 239 TFLOP/s of fp32 products where the
+// fp32 units reach 75 at most; 515 x 896 x 4864 37 us, 10 of them to cut 19 MB, the rest bound by the copies into shared memory
+// (110 KB for 1,920 cycles of multiplications). Its error against 64 bits there is 1.5e-7, a plain fp32 product's 6.2e-7.
 //
 // An infinity times a part that is 0 would give NaN, and the parts of an operand whose largest value is below 2^-86 miss bits
 // that matter. So the first kernel says what it met, and in those cases the second one makes its tiles on the fp32 units
@@ -326,7 +326,11 @@ __device__ __forceinline__ void finish_column(const Args& a, int64_t i, int64_t 
 
 constexpr int kRowWarps = 8;
 // Rows up to which it is taken. 4096 x 4096 with a weight that is not in L2, forward and back: one row 14.0 and 15.3 us (4.8
-// and 4.4 TB/s; on the fp32 units' tiles 52 and 49), 16 rows 38 and 31 us (cut for the tensor cores 54 and 52).
+// and 4.4 TB/s; on the fp32 units' tiles 52 and 49), 16 rows 38 and 31 us (cut for the tensor cores 54 and 52). With other
+// operands every call 8 rows of a 4864 x 896 weight take 11.2 and 25.7 us (24.6 and 36.4 otherwise), of 11008 x 4096 100 and 67
+// (149 and 130), of 1024 x 1024 5.3 and 9.8 (10.2 and 10.1); 16 rows 12.8 and 30.7 (20.2 and 25.6), 125 and 74 (149 and 130),
+// 5.7 and 10.8 (10.4 and 10.0). So back through smaller weights it is the slower one towards 16 rows, by 8 to 20%, and through
+// 256 x 256 from 8 rows on (8.9 and 6.4): forward it is the faster one at all of these.
 constexpr int kFewRows = 16;
 
 // A product of at most R rows with a weight that is read once, where the copies bound it (rows 1 of 4096 x 4096: 67 MB).
@@ -509,9 +513,9 @@ __global__ void __launch_bounds__(32 * kRowWarps, 2) rows_kernel(const Args a) {
 
 // ------------------------------------------------------------ tensor cores ---
 
-// A tile has 128 columns j of the result along tensor memory's rows and `width` of its rows i along the columns, 32 to 160,
-// so that its sums fit in the registers of the warps that add them up and 515 rows need no fifth tile of 128. A warp then
-// holds 32 neighbouring columns of a row, 128 bytes.
+// A tile has 128 columns j of the result along tensor memory's rows and `width` of its rows i along the columns, 32 to 160:
+// the sums of 160 take 80 registers of each of the 256 threads that add them up. A warp then holds 32 neighbouring columns of
+// a row, 128 bytes.
 constexpr int kParts = 3;
 constexpr int kPart = kBM * kBK * 2;  // a slice of one part of the operand along the tile's rows
 constexpr int kMostWidth = 160, kStages = 2;

@@ -28,6 +28,10 @@
 // Where the tiles are fewer than the SMs, the sum is cut among the CTAs (or pairs) of a cluster: each leaves its share of
 // the sums, then every CTA adds up some of the columns in the cluster's order and finishes them. No atomics, the same
 // result every time.
+//
+// Tensor memory's additions cut off instead of rounding: 1,024 terms come out 0.8e-6 of the sum too small in the mean, 4,096
+// 1.8e-6. A rounding to bf16 hides that, the 8-bit form nearly (3 to 8 of 100,000 bytes are one step off, of exact fp32 sums 1
+// to 2); adding slices in registers, as fp32 products do, would take warps the pair's products need.
 
 #include "smat_linear.h"
 #include "smat_linear_tc.cuh"
@@ -783,10 +787,13 @@ cudaError_t plan_narrow(const Product& p, int sms, Plan* plan) {
 }
 
 // Width and shares of a pair's tile: the least estimate of the time in cycles. A slice takes the longer of its
-// multiplications (2 per column) and its copies (16 KB and 64 bytes per column at 64 bytes a cycle, as measured with
-// every SM copying); a tile's columns take about 16 each to finish, beside the next tile's products, and at the end by
-// themselves; shares are written and read through L2. All clusters of a shared sum run at once. Of the 28 choices it took
-// the fastest, or one within 1%, in each of six forward shapes from 257 x 1024 x 4096 to 4096 x 592 x 1024.
+// multiplications (2 per column) and its copies (16 KB and 64 bytes per column at 64 bytes a cycle); a tile's columns take
+// about 16 each to finish, beside the next tile's products, and at the end by themselves; shares are written and read through
+// L2. All clusters of a shared sum run at once. The estimate orders choices, it is no time: a slice of 256 columns was 0.41 us
+// in 2056 x 4096 with k from 1024 to 4096, where 512 cycles are 0.25. Of the 28 choices it took the fastest, or one within 1%,
+// in each of six forward shapes from 257 x 1024 x 4096 to 4096 x 592 x 1024, and among 15 others (five input gradients, three
+// of them with slopes, from 515 x 4864 x 896 to 8192 x 11008 x 4096; seven weight gradients from 300 x 512 x 512 to 8224 x 4096 x
+// 1024; three forward ones with bias, activation and 8 bits) one that no other beat by more than the 2 us that were resolved.
 template <int MODE>
 cudaError_t plan_pair(const Product& p, Plan* plan) {
   static std::atomic<uint64_t> allowed;

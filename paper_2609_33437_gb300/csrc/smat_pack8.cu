@@ -6,7 +6,8 @@
 // magnitude by one shuffle. Matrices whose rows do not start there are taken by warps that read and write 32 neighbours at
 // a time and hand each lane its 16 columns through shared memory (8192 x 8191 bf16 saved in 78 us and read back in 82;
 // element by element 167 and 360). Rows on 32 bytes run at 6.1 to 6.6 TB/s from 8191 x 11008 on, unaligned ones at 2.5;
-// reading back through the erf form of GELU (68 us for 8191 x 11008, others 45) is bound by its instructions.
+// reading back through the erf form of GELU (bf16 68 us for 8191 x 11008, others 45) is bound by its instructions. A gradient
+// times slopes: bf16 76 us (6.0 TB/s; GELU 87), fp32 118 (6.9, part of it from L2); 8192 x 8191 141 and 130 us.
 
 #include "smat_linear.cuh"
 #include "smat_linear.h"
