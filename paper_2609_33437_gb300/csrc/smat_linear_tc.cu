@@ -76,6 +76,7 @@ struct Args {
   float* parts;                     // the shares' sums, or NULL
   int* errors;                      // device error bits
   bool by_rows;                     // rows of out, residual and q start on 16 bytes: TMA copies them
+  bool whole_ends;                  // and those that are written end on 16 bytes
   bool wide_bias;                   // bias on 16 bytes
 };
 
@@ -155,8 +156,9 @@ __device__ __forceinline__ void desk_send(const Desk& desk, void* to, int64_t ld
     if (t < rows) p[t * ld] = x[t];
 }
 
-// Columns j .. j + 31 of rows i .. i + 31, a row per lane, out by TMA (which leaves out what lies outside the result) or
-// by hand. sums(v): their sums. False if a wait for what comes in has given up.
+// Columns j .. j + 31 of rows i .. i + 31, a row per lane, out by TMA or by hand. A copy out leaves out rows outside the
+// result, but writes whole 16 bytes at a row's end: one that ends elsewhere has its last columns sent by hand, so that what
+// lies beside the result stays as it is. sums(v): their sums. False if a wait for what comes in has given up.
 template <int MODE, class Sums>
 __device__ __forceinline__ bool finish_block(const Args& a, const CUtensorMap* map_out, const CUtensorMap* map_in,
                                             const CUtensorMap* map_q, int64_t i, int64_t j, Desk& desk,
@@ -169,8 +171,9 @@ __device__ __forceinline__ bool finish_block(const Args& a, const CUtensorMap* m
   const bool save = MODE == kForward && p.q;
   const void* from = MODE == kForward ? p.residual : p.out;  // what is added
   const int64_t ld_from = MODE == kForward ? p.ldr : p.ldo;
-  const bool copied = a.by_rows && (add || slope);  // by TMA
-  if (a.by_rows) {
+  const bool tma = a.by_rows && (a.whole_ends || j + 32 <= p.J);
+  const bool copied = tma && (add || slope);
+  if (tma) {
     if (lane == 0) {
       asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");  // the last block has left the desk
       if (copied) {
@@ -182,6 +185,7 @@ __device__ __forceinline__ bool finish_block(const Args& a, const CUtensorMap* m
       }
     }
   } else {
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
     __syncwarp();  // the last block has been read
     if (add) desk_fetch<uint16_t>(desk, from, ld_from, i, j, p.I, p.J);
     if (slope) desk_fetch<uint8_t>(desk, p.q, p.ldq, i, j, p.I, p.J);
@@ -264,7 +268,7 @@ __device__ __forceinline__ bool finish_block(const Args& a, const CUtensorMap* m
     }
     desk_store(at, w);
   }
-  if (a.by_rows) {
+  if (tma) {
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     __syncwarp();
     if (lane == 0) {
@@ -276,6 +280,8 @@ __device__ __forceinline__ bool finish_block(const Args& a, const CUtensorMap* m
     __syncwarp();
     desk_send<uint16_t>(desk, p.out, p.ldo, i, j, p.I, p.J);
     if (save) desk_send<uint8_t>(desk, p.q, p.ldq, i, j, p.I, p.J);
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // the next block may come and go by TMA
+    __syncwarp();
   }
   return true;
 }
@@ -844,6 +850,7 @@ cudaError_t fill_args(const Product& p, const Plan& g, void* workspace, Args* ar
   };
   a.by_rows = rows_on(p.out, p.ldo, 2, 16) && (!p.residual || rows_on(p.residual, p.ldr, 2, 16)) &&
               (!p.q || rows_on(p.q, p.ldq, 1, 16));
+  a.whole_ends = p.J % 8 == 0 && (p.mode != kForward || !p.q || p.J % 16 == 0);
   a.wide_bias = (uintptr_t)p.bias % 16 == 0;
   *args = a;
   return e;
