@@ -386,20 +386,15 @@ def _rows_like(t: Optional[torch.Tensor]) -> Optional[torch.Tensor]:
         return t.contiguous()
 
 
-def _autocast(*tensors: Optional[torch.Tensor]):
-    """Under torch.autocast, the tensors in its type, as torch.nn.Linear takes them (64-bit ones stay as they are)."""
-    if not torch.is_autocast_enabled("cuda"):
-        return tensors
+def _autocast(layer, x: torch.Tensor, *rest: Optional[torch.Tensor]) -> torch.Tensor:
+    """layer(x, parameters, residual) under torch.autocast: in its type, as torch.nn.Linear would be (64-bit tensors stay as they
+    are). A residual of another type is added afterwards, and the result has the wider one, as beside torch.nn.Linear."""
     dtype = torch.get_autocast_dtype("cuda")
-    return tuple(t if t is None or t.dtype is torch.float64 else t.to(dtype) for t in tensors)
-
-
-def _with_residual(layer, x: torch.Tensor, residual: Optional[torch.Tensor]) -> torch.Tensor:
-    """layer(residual); under autocast one of a wider type is added afterwards, and is the result's type, as it would be
-    beside torch.nn.Linear."""
-    if residual is None or residual.dtype is x.dtype or not torch.is_autocast_enabled("cuda"):
-        return layer(residual)
-    return layer(None) + residual
+    x, *params = (t if t is None or t.dtype is torch.float64 else t.to(dtype) for t in (x, *rest[:-1]))
+    residual = rest[-1]
+    if residual is None or residual.dtype is x.dtype:
+        return layer(x, *params, residual)
+    return layer(x, *params, None) + residual
 
 
 def _row_sums(dy: torch.Tensor) -> torch.Tensor:
@@ -421,10 +416,17 @@ class _FirstOnly(torch.autograd.Function):
         raise RuntimeError("Linear8 and Mlp8 have first derivatives only: their gradients cannot be differentiated")
 
 
-def _first_only(anchor, dy, grads):
-    """The backward passes run in the library's kernels and build no graph. Where one is asked for (create_graph), their
-    results refuse to be differentiated; otherwise terms of a second derivative would be left out silently."""
-    return _FirstOnly.apply(anchor, dy, *grads) if torch.is_grad_enabled() else grads
+def _first_only(ctx, dy, gradients):
+    """gradients(ctx, dy). They are made by the library's kernels and belong to no graph. Where one is asked for
+    (create_graph), they refuse to be differentiated; otherwise terms of a second derivative would be left out silently. The
+    residual's gradient, which is dy, has the graph that dy has."""
+    if not torch.is_grad_enabled():
+        return gradients(ctx, dy)
+    with torch.no_grad():
+        grads = gradients(ctx, dy)
+    anchor = ctx.saved_tensors[-1]
+    refusing = _FirstOnly.apply(anchor, dy, *(None if g is dy else g for g in grads))
+    return tuple(dy if g is dy else h for g, h in zip(grads, refusing))
 
 
 class _Linear8(torch.autograd.Function):
@@ -444,20 +446,23 @@ class _Linear8(torch.autograd.Function):
         return y, anchor
 
     @staticmethod
-    def backward(ctx, grad, _):
-        w, hq, he, xq, xe, anchor = ctx.saved_tensors
+    def backward(ctx, dy, _):
+        return _first_only(ctx, dy, _Linear8._gradients)
+
+    @staticmethod
+    def _gradients(ctx, grad):
+        w, hq, he, xq, xe, _ = ctx.saved_tensors
         need_x, need_w, need_b, need_r, _ = ctx.needs_input_grad
+        dy = grad.contiguous()
+        dh = act_grad8(dy, Packed8(hq, he), ctx.act) if hq is not None else dy
         dx = dw = db = None
-        with torch.no_grad():
-            dy = grad.contiguous()
-            dh = act_grad8(dy, Packed8(hq, he), ctx.act) if hq is not None else dy
-            if need_x:
-                dx = linear_grad_input(dh, w)
-            if need_w:
-                dw, db = linear_grad_weight(dh, Packed8(xq, xe), bias=need_b)
-            elif need_b:
-                db = _row_sums(dh)
-        return *_first_only(anchor, grad, (dx, dw, db)), (grad if need_r else None), None
+        if need_x:
+            dx = linear_grad_input(dh, w)
+        if need_w:
+            dw, db = linear_grad_weight(dh, Packed8(xq, xe), bias=need_b)
+        elif need_b:
+            db = _row_sums(dh)
+        return dx, dw, db, (grad if need_r else None), None
 
 
 class _Mlp8(torch.autograd.Function):
@@ -476,26 +481,29 @@ class _Mlp8(torch.autograd.Function):
         return y, anchor
 
     @staticmethod
-    def backward(ctx, grad, _):
-        w1, w2, xq, xe, hq, he, anchor = ctx.saved_tensors
+    def backward(ctx, dy, _):
+        return _first_only(ctx, dy, _Mlp8._gradients)
+
+    @staticmethod
+    def _gradients(ctx, grad):
+        w1, w2, xq, xe, hq, he, _ = ctx.saved_tensors
         need_x, need_w1, need_b1, need_w2, need_b2, need_r, _ = ctx.needs_input_grad
         h = Packed8(hq, he)
+        dy = grad.contiguous()
         dx = dw1 = db1 = dw2 = db2 = None
-        with torch.no_grad():
-            dy = grad.contiguous()
-            if need_w2:
-                dw2, db2 = linear_grad_weight(dy, h, ctx.act, bias=need_b2)
-            elif need_b2:
-                db2 = _row_sums(dy)
-            if need_x or need_w1 or need_b1:
-                dh = linear_grad_input(dy, w2, ctx.act, h if ctx.act != "none" else None)
-                if need_w1:
-                    dw1, db1 = linear_grad_weight(dh, Packed8(xq, xe), bias=need_b1)
-                elif need_b1:
-                    db1 = _row_sums(dh)
-                if need_x:
-                    dx = linear_grad_input(dh, w1)
-        return *_first_only(anchor, grad, (dx, dw1, db1, dw2, db2)), (grad if need_r else None), None
+        if need_w2:
+            dw2, db2 = linear_grad_weight(dy, h, ctx.act, bias=need_b2)
+        elif need_b2:
+            db2 = _row_sums(dy)
+        if need_x or need_w1 or need_b1:
+            dh = linear_grad_input(dy, w2, ctx.act, h if ctx.act != "none" else None)
+            if need_w1:
+                dw1, db1 = linear_grad_weight(dh, Packed8(xq, xe), bias=need_b1)
+            elif need_b1:
+                db1 = _row_sums(dh)
+            if need_x:
+                dx = linear_grad_input(dh, w1)
+        return dx, dw1, db1, dw2, db2, (grad if need_r else None), None
 
 
 class Linear8(torch.nn.Linear):
@@ -511,8 +519,9 @@ class Linear8(torch.nn.Linear):
         self.act = act
 
     def forward(self, x: torch.Tensor, residual: Optional[torch.Tensor] = None) -> torch.Tensor:
-        x, w, b = _autocast(x, self.weight, self.bias)
-        return _with_residual(lambda r: self._forward(x, w, b, r), x, residual)
+        if torch.is_autocast_enabled("cuda"):
+            return _autocast(self._forward, x, self.weight, self.bias, residual)
+        return self._forward(x, self.weight, self.bias, residual)
 
     def _forward(self, x, w, b, residual):
         if not torch.is_grad_enabled():
@@ -534,8 +543,10 @@ class Mlp8(torch.nn.Module):
         self.fc2 = torch.nn.Linear(hidden, features, bias, device=device, dtype=dtype)
 
     def forward(self, x: torch.Tensor, residual: Optional[torch.Tensor] = None) -> torch.Tensor:
-        x, *w = _autocast(x, self.fc1.weight, self.fc1.bias, self.fc2.weight, self.fc2.bias)
-        return _with_residual(lambda r: self._forward(x, *w, r), x, residual)
+        fc1, fc2 = self.fc1, self.fc2
+        if torch.is_autocast_enabled("cuda"):
+            return _autocast(self._forward, x, fc1.weight, fc1.bias, fc2.weight, fc2.bias, residual)
+        return self._forward(x, fc1.weight, fc1.bias, fc2.weight, fc2.bias, residual)
 
     def _forward(self, x, w1, b1, w2, b2, residual):
         if not torch.is_grad_enabled():
