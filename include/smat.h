@@ -538,6 +538,115 @@ smat_status smat_act_grad8(const void* dy, int64_t lddy, const int8_t* q, int64_
  * are kept. Reads and clears the bits of the current device; waits for the stream. */
 smat_status smat_linear_poll_errors(smat_stream_t stream, int32_t* errors_out);
 
+/* ------------------------------------------------------------------ norms ---
+ * The normalisation before a layer, with the residual stream's sum before it in the same pass, and its gradient.
+ *
+ *   h = x + residual (rounded to the type), or x without one
+ *   s = 1 / sqrt(v + eps),   y = (h - mu) s w + b
+ *       layer: mu = mean of h's row, v = mean of (h - mu)^2;   rms: mu = 0, v = mean of h^2
+ *   back, with a = dy w and xh = (h - mu) s:
+ *       dx = s (a - mean(a) - xh mean(a xh)) + dh,  without mean(a) for rms;  dh: the gradient that reaches h otherwise
+ *       dw = sum over rows of dy xh,   db = sum over rows of dy
+ *
+ * Matrices [rows, cols] are row-major with a row stride and of one dtype; w, b, dw and db [cols] are of weight_dtype: the
+ * same, or fp32 beside bf16. Means, squares and the sums over rows are held in fp32; what is written is rounded once (y and
+ * the statistics are made from h as it is rounded). `stats` [2][rows] holds mu and s of every row ([1][rows], s, for rms): the
+ * forward pass writes it on request and the backward pass reads it. Results do not depend on timing: no atomics. rows may be 0
+ * (dw and db of no rows are 0), cols is at least 1. w NULL stands for ones, b NULL for zeros. Outputs must not overlap inputs
+ * or one another, except that h may be the residual itself and dx may be dh itself (same pointer and stride). */
+typedef enum { SMAT_NORM_LAYER = 0, SMAT_NORM_RMS = 1 } smat_norm_kind;
+
+typedef struct {
+  const void* x;
+  const void* residual; /* or NULL; then h is NULL too */
+  const void* w;        /* or NULL */
+  const void* b;        /* or NULL */
+  void* h;              /* x + residual */
+  void* y;
+  float* stats; /* or NULL */
+  int64_t rows, cols;
+  int64_t ldx, ldr, ldh, ldy;
+  int32_t dtype, weight_dtype; /* smat_dtype */
+  int32_t kind;                /* smat_norm_kind */
+  float eps;                   /* >= 0 */
+} smat_norm_args;
+
+typedef struct {
+  const void* dy;
+  const void* h;      /* what was normalised: x, or x + residual */
+  const float* stats; /* as the forward pass wrote it */
+  const void* w;      /* or NULL */
+  const void* dh;     /* or NULL */
+  void* dx;           /* dx, dw, db: NULL where not wanted */
+  void* dw;
+  void* db;
+  int64_t rows, cols;
+  int64_t lddy, ldh, lddh, lddx;
+  int32_t dtype, weight_dtype;
+  int32_t kind;
+  int32_t accumulate; /* 1: dw and db are added to what they hold */
+} smat_norm_grad_args;
+
+/* Workspace and streams as for the linear layers; smat_norm needs no workspace. */
+smat_status smat_norm(const smat_norm_args* args, smat_stream_t stream);
+size_t smat_norm_grad_workspace_bytes(const smat_norm_grad_args* args);
+smat_status smat_norm_grad(const smat_norm_grad_args* args, void* d_workspace, size_t workspace_bytes,
+                           smat_stream_t stream);
+
+/* ------------------------------------------------------------------ AdamW ---
+ * The optimizer's update on ordinary steps: one AdamW step over a list of tensors in one launch (for every 1,300 tensors),
+ * with moments in 32 bits or in 8. For every element, each operation rounded to fp32 in this order, as
+ * smat_grad_map_adamw_multi does it:
+ *   g = scale grad;  m1 = beta1 m1 + fl(1 - beta1) g;  m2 = beta2 m2 + fl(1 - beta2) (g g);  r = sqrt(m2)
+ *   theta = fl(1 - lr wd) theta - fl(lr / (1 - beta1^t)) (m1 / (r / fl(sqrt(1 - beta2^t)) + eps))
+ * and theta is rounded to its type. The constants fl(...) are computed in double and rounded once.
+ *
+ * The list: tensor k's elements lie at the places starts[k] .. starts[k] + numels[k] - 1, starts[0] = 0 and starts[k + 1] =
+ * starts[k] + numels[k] rounded up to a multiple of SMAT_ADAMW_GROUP; the moments are kept by place, `places` (the next start
+ * after the last tensor) of each. Those between two tensors are 0 and stay 0.
+ *
+ * 32 bits: m1 and m2 are fp32 [places]. 8 bits: m1 and r = sqrt(m2) are bytes [places], and SMAT_ADAMW_GROUP neighbours share a
+ * power of two 2^(e - 127) each, the unit, e bytes [places / SMAT_ADAMW_GROUP]. A byte's low 7 bits c (m1; bit 7 is its sign)
+ * stand for c units below 8, else for (8 + c % 8) 2^(c / 8 - 1) units; a byte c of r stands for c units below 16, else for
+ * (16 + c % 16) 2^(c / 16 - 1) units. bf16 holds each such value exactly. e is the biased exponent of the group's largest
+ * magnitude less 16 (m1) or 17 (r), 1 at least. A value becomes the neighbour below it or above it with the probability that
+ * its place between the two gives, decided by 16 bits of a number made of its place in the list, the seed and t, so that a
+ * change below a step is not lost from one step to the next; the same call gives the same bits every time. A group that would
+ * hold an infinity or NaN has e = 255 and reads back as NaN throughout, so that an overflow stays visible, for its neighbours'
+ * moments too. The parameter is updated with the moments before they are rounded to 8 bits. places is below 2^32 then. */
+#define SMAT_ADAMW_GROUP 256
+
+typedef struct {
+  void* const* params;       /* HOST arrays of n_tensors: DEVICE pointers to numels[k] contiguous elements */
+  const void* const* grads;  /* ... a NULL: that tensor and its moments stay as they are */
+  const int64_t* numels;
+  void* m1;                  /* DEVICE, on 16 bytes: fp32, or bytes */
+  void* m2;                  /* ... m2, or r's bytes */
+  uint8_t* e1;               /* 8 bits; NULL for 32 */
+  uint8_t* e2;
+  const float* scale_at;     /* DEVICE, one number each that a captured call reads anew, or NULL: scale, lr, step */
+  const float* lr_at;
+  const int64_t* step_at;
+  double scale;              /* finite */
+  double lr, beta1, beta2, eps, weight_decay; /* as smat_adamw */
+  int64_t step;              /* t, 1 .. 2^31 - 1 */
+  uint64_t seed;             /* of the 8 bits' roundings */
+  int32_t n_tensors;
+  int32_t dtype, grad_dtype; /* smat_dtype of all params, of all grads */
+  int32_t bits;              /* 8 or 32 */
+} smat_adamw_args;
+
+/* The number of places of a list (0 on invalid arguments). */
+int64_t smat_adamw_places(const int64_t* numels, int32_t n_tensors);
+
+/* One step. Asynchronous on `stream`; the host arrays are read before return. No workspace. Parameters and moments must not
+ * overlap one another or anything that is read. */
+smat_status smat_adamw_step(const smat_adamw_args* args, smat_stream_t stream);
+
+/* What moments in 8 bits stand for: bf16 m1 and r, [places] each, on 16 bytes (as q1 and q2 are). */
+smat_status smat_adamw_values(const uint8_t* q1, const uint8_t* e1, const uint8_t* q2, const uint8_t* e2, void* m1, void* r,
+                              int64_t places, smat_stream_t stream);
+
 /* SMAT_ABI_VERSION of the loaded library. */
 int32_t smat_abi_version(void);
 

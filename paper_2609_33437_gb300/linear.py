@@ -413,7 +413,7 @@ class _FirstOnly(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, *_):
-        raise RuntimeError("Linear8 and Mlp8 have first derivatives only: their gradients cannot be differentiated")
+        raise RuntimeError("the layer has first derivatives only: its gradients cannot be differentiated")
 
 
 def _first_only(ctx, dy, gradients):

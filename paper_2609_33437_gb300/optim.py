@@ -1,0 +1,215 @@
+"""The optimizer's update on ordinary steps: one AdamW step over many tensors in one launch, moments in 32 bits or in 8
+(include/smat.h, "AdamW").
+
+    moments = Moments(params, bits=8)
+    adamw(params, grads, moments, step=t, lr=1e-4)            params and moments in place
+
+`AdamW` is a torch.optim.Optimizer around it. Parameters are contiguous CUDA tensors of one dtype per call (float32 or
+bfloat16), gradients of one dtype. Argument marshalling only: the step runs in the library's kernel, on the current stream or
+the one given. On simulated-loss steps `PeriodicSmat.optimizer_step` takes an AdamW of 32 bits into the gradient map's pass.
+"""
+
+import ctypes
+import struct
+from typing import Dict, List, Optional, Sequence, Union
+
+import torch
+
+from . import linear as L
+from . import smat as S
+
+GROUP = 256
+
+_ADAMW = struct.Struct("@10P6dqQ4i")
+_numel, _contiguous, _get_device, _data_ptr = (torch.Tensor.numel, torch.Tensor.is_contiguous, torch.Tensor.get_device,
+                                               torch.Tensor.data_ptr)
+
+
+class Moments:
+    """The moments of a list of tensors, zeros at first. Tensor k's lie at starts[k] .. starts[k] + sizes[k] - 1 of each buffer;
+    starts are multiples of 256.
+
+    bits 32: m1 and m2, float32. bits 8: m1 and r = sqrt(m2) as bytes q1 and q2, and a power of two for every 256 of them, e1
+    and e2; two bytes an element where 32 bits take eight."""
+
+    def __init__(self, params: Sequence[torch.Tensor], bits: int = 32):
+        params = list(params)
+        if bits not in (8, 32):
+            raise ValueError("bits: 8 or 32")
+        if not params:
+            raise ValueError("params: at least one tensor")
+        self.bits, self.device = bits, params[0].device
+        if any(p.device != self.device for p in params):
+            raise ValueError("params: on one device")
+        self.sizes: List[int] = [p.numel() for p in params]
+        self.starts: List[int] = []
+        at = 0
+        for n in self.sizes:
+            self.starts.append(at)
+            at += -(-n // GROUP) * GROUP
+        self.places = at
+        if bits == 8 and at >= 1 << 32:
+            raise ValueError(f"8 bits: {at} places, 2^32 and more are not numbered")
+        kw = dict(device=self.device)
+        if bits == 8:
+            self._buffers = {"q1": torch.zeros(at, dtype=torch.uint8, **kw),
+                             "e1": torch.ones(at // GROUP, dtype=torch.uint8, **kw),
+                             "q2": torch.zeros(at, dtype=torch.uint8, **kw),
+                             "e2": torch.ones(at // GROUP, dtype=torch.uint8, **kw)}
+        else:
+            self._buffers = {"m1": torch.zeros(at, dtype=torch.float32, **kw), "m2": torch.zeros(at, dtype=torch.float32, **kw)}
+        # what a call hands over of the list
+        self._numels = struct.pack(f"{len(self.sizes)}q", *self.sizes)
+        self._pointers = struct.Struct(f"{len(self.sizes)}P")
+        b = self._buffers
+        self._places = ((b["q1"].data_ptr(), b["q2"].data_ptr(), b["e1"].data_ptr(), b["e2"].data_ptr()) if bits == 8 else
+                        (b["m1"].data_ptr(), b["m2"].data_ptr(), 0, 0))
+
+    def buffers(self) -> Dict[str, torch.Tensor]:
+        """The buffers by name: m1 and m2, or q1, e1, q2 and e2. They may be read and written (a checkpoint)."""
+        return dict(self._buffers)
+
+    def values(self, stream: Optional[torch.cuda.Stream] = None):
+        """(m1, m2) for 32 bits, the buffers themselves; (m1, r) in bfloat16, which holds what 8 bits stand for exactly."""
+        b = self._buffers
+        if self.bits == 32:
+            return b["m1"], b["m2"]
+        if stream is not None:
+            return L._on(stream, self.values)
+        m1, r = (torch.empty(self.places, dtype=torch.bfloat16, device=self.device) for _ in range(2))
+        L._call("smat_adamw_values", self.device, b["q1"].data_ptr(), b["e1"].data_ptr(), b["q2"].data_ptr(), b["e2"].data_ptr(),
+                m1.data_ptr(), r.data_ptr(), self.places)
+        return m1, r
+
+    def views(self, name: str) -> List[torch.Tensor]:
+        """A buffer of 32 bits by tensors, each flat."""
+        b = self._buffers[name]
+        return [b[a:a + n] for a, n in zip(self.starts, self.sizes)]
+
+    def nbytes(self) -> int:
+        return sum(t.numel() * t.element_size() for t in self._buffers.values())
+
+
+def _addresses(name: str, ts: Sequence[Optional[torch.Tensor]], sizes: Sequence[int], index: int, optional: bool):
+    """(their addresses, their dtype): contiguous tensors of one dtype and these sizes on the device. A None: 0."""
+    first = next((t for t in ts if t is not None), None)
+    if first is None:
+        return [0] * len(ts), None
+    dt, out = first.dtype, []
+    for t, n in zip(ts, sizes):
+        if t is None and optional:
+            out.append(0)
+            continue
+        if t.dtype is not dt or _numel(t) != n or _get_device(t) != index or not _contiguous(t):
+            raise ValueError(f"{name}[{len(out)}]: must be contiguous {dt} of {n} elements on cuda:{index}")
+        out.append(_data_ptr(t))
+    return out, dt
+
+
+def _one(name: str, v, dtype, device):
+    """(number, address) of a number, or of a tensor that holds one."""
+    if not isinstance(v, torch.Tensor):
+        return v, 0
+    if v.dtype is not dtype or v.device != device or v.numel() != 1:
+        raise ValueError(f"{name}: must be a number, or one {dtype} on {device}")
+    return 0, v.data_ptr()
+
+
+def adamw(params: Sequence[torch.Tensor], grads: Sequence[Optional[torch.Tensor]], moments: Moments,
+          step: Union[int, torch.Tensor], lr: Union[float, torch.Tensor] = 1e-3, beta1: float = 0.9, beta2: float = 0.999,
+          eps: float = 1e-8, weight_decay: float = 0.01, scale: Union[float, torch.Tensor] = 1.0, seed: int = 0,
+          stream: Optional[torch.cuda.Stream] = None) -> None:
+    """One AdamW step of params and moments, in place. A tensor whose gradient is None is left as it is.
+
+    step: t, from 1 on. scale: what gradients are multiplied with first (one over a loss scale, a clipping factor). seed: of the
+    roundings to 8 bits. step (int64), lr and scale (float32) may be tensors of one element on the device: a captured call then
+    goes on with what they hold at each replay."""
+    if stream is not None:
+        return L._on(stream, adamw, params, grads, moments, step, lr, beta1, beta2, eps, weight_decay, scale, seed)
+    n = len(moments.sizes)
+    if len(params) != n or len(grads) != n:
+        raise ValueError(f"{len(params)} params and {len(grads)} grads for moments of {n}")
+    device = moments.device
+    index = device.index
+    if index is None:
+        raise ValueError("params: must be CUDA tensors")
+    pp, pdt = _addresses("params", params, moments.sizes, index, False)
+    gp, gdt = _addresses("grads", grads, moments.sizes, index, True)
+    code = S.dtype_code(pdt)
+    t, step_at = _one("step", step, torch.int64, device)
+    rate, lr_at = _one("lr", lr, torch.float32, device)
+    by, scale_at = _one("scale", scale, torch.float32, device)
+    pack = moments._pointers.pack
+    # the arrays live until the call returns
+    arrays = ctypes.create_string_buffer(pack(*pp) + pack(*gp) + moments._numels)
+    at = ctypes.addressof(arrays)
+    args = _ADAMW.pack(at, at + 8 * n, at + 16 * n, *moments._places, scale_at, lr_at, step_at, by, rate, beta1, beta2, eps,
+                       weight_decay, t, seed & 0xFFFFFFFFFFFFFFFF, n, code, code if gdt is None else S.dtype_code(gdt),
+                       moments.bits)
+    L._call("smat_adamw_step", device, args)
+
+
+class AdamW(torch.optim.Optimizer):
+    """AdamW whose step is one launch for every group of parameters of one dtype (gradients then share one dtype, and every
+    parameter without one is left as it is). bits 8 keeps two bytes of moments per element; with 32 the moments are fp32
+    whatever the parameters' type. The group's hyperparameters are those of torch.optim.AdamW. Its step count is one for all; in
+    a captured graph use `adamw` with a step on the device."""
+
+    def __init__(self, params, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.01, bits: int = 32,
+                 seed: int = 0):
+        if bits not in (8, 32):
+            raise ValueError("bits: 8 or 32")
+        self.bits, self.seed, self.steps = bits, int(seed), 0
+        self._lists = None
+        super().__init__(params, dict(lr=lr, betas=tuple(betas), eps=eps, weight_decay=weight_decay))
+
+    def add_param_group(self, group):
+        if self._lists is not None:
+            raise RuntimeError("the moments are laid out: parameters cannot be added after the first step")
+        super().add_param_group(group)
+
+    def lists(self):
+        """[(group, parameters of one dtype, their Moments)], laid out at the first step."""
+        if self._lists is None:
+            lists = []
+            for group in self.param_groups:
+                for dt in dict.fromkeys(p.dtype for p in group["params"]):
+                    ps = [p for p in group["params"] if p.dtype is dt]
+                    lists.append((group, ps, Moments(ps, self.bits)))
+            self._lists = lists
+        return self._lists
+
+    @torch.no_grad()
+    def step(self, closure=None, scale: Union[float, torch.Tensor] = 1.0):
+        """One step; scale: see adamw."""
+        loss = None
+        if closure is not None:
+            with torch.enable_grad():
+                loss = closure()
+        t = self.steps + 1
+        for k, (group, ps, moments) in enumerate(self.lists()):
+            beta1, beta2 = group["betas"]
+            adamw(ps, [p.grad if p.grad is None or p.grad.is_contiguous() else p.grad.contiguous() for p in ps], moments, t,
+                  group["lr"], beta1, beta2, group["eps"], group["weight_decay"], scale, self.seed + k)
+            torch.autograd.graph.increment_version(ps)  # what a graph saved of them is no longer what it saved
+        self.steps = t
+        return loss
+
+    def state_dict(self):
+        """The step count, the moments' buffers list by list, and the groups' hyperparameters."""
+        return {"steps": self.steps, "bits": self.bits, "seed": self.seed,
+                "moments": [dict(sizes=list(m.sizes), **m.buffers()) for _, _, m in self.lists()],
+                "param_groups": [{k: v for k, v in g.items() if k != "params"} for g in self.param_groups]}
+
+    def load_state_dict(self, state_dict):
+        lists = self.lists()
+        if state_dict["bits"] != self.bits or [m["sizes"] for m in state_dict["moments"]] != [m.sizes for _, _, m in lists]:
+            raise ValueError("the state is of other parameters, or of moments in other bits")
+        if len(state_dict["param_groups"]) != len(self.param_groups):
+            raise ValueError("the state is of other parameter groups")
+        self.steps, self.seed = int(state_dict["steps"]), int(state_dict["seed"])
+        for (_, _, m), saved in zip(lists, state_dict["moments"]):
+            for name, t in m.buffers().items():
+                t.copy_(saved[name])
+        for group, saved in zip(self.param_groups, state_dict["param_groups"]):
+            group.update(saved)

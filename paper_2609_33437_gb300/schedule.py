@@ -26,8 +26,9 @@ Usage (a training loop with any optimizer):
         sched.after_backward(step)
         opt.step(); opt.zero_grad()
 
-or, with torch.optim.AdamW on fp32 parameters, the gradient map folded into
-the optimizer's read of the gradient on simulated-loss steps:
+or, with torch.optim.AdamW on fp32 parameters or optim.AdamW (bits=32), the
+gradient map folded into the optimizer's read of the gradient on
+simulated-loss steps:
 
         sched.before_forward(step)
         loss_fn(model, batch).backward()
@@ -38,6 +39,7 @@ from typing import List, Optional, Sequence
 
 import torch
 
+from . import optim
 from .smat import SmatSession
 
 
@@ -128,15 +130,34 @@ class PeriodicSmat:
         steps = {float(opt.state[p]["step"]) if "step" in opt.state[p] else 0.0 for p in self.params}
         return len(steps) == 1
 
+    def _own_fusable(self, opt) -> bool:
+        """One list of 32-bit moments of exactly this schedule's parameters, each with a contiguous gradient of one dtype."""
+        if type(opt) is not optim.AdamW or opt.bits != 32 or len(opt.lists()) != 1 or torch.is_tensor(opt.param_groups[0]["lr"]):
+            return False
+        grads = [p.grad for p in self.params]
+        return ([id(p) for p in opt.lists()[0][1]] == [id(p) for p in self.params]
+                and all(g is not None and g.is_contiguous() and g.dtype == grads[0].dtype for g in grads))
+
     def optimizer_step(self, step: int, opt):
         """After the backward pass: on an ordinary step, opt.step(). On a
         simulated-loss step with an AdamW the fused path accepts (see
         _fusable), the storage is switched back and the gradient map and the
         AdamW update run as one pass (smat_grad_map_adamw_multi) on the
         optimizer's own moments; the mapped gradient is not written (p.grad
-        keeps g~). Otherwise after_backward, then opt.step()."""
+        keeps g~). So they do with an optim.AdamW of 32-bit moments over exactly
+        these parameters. Otherwise after_backward, then opt.step()."""
         if not self.is_smat_step(step):
             opt.step()
+            return
+        if self._own_fusable(opt):
+            group, _, moments = opt.lists()[0]
+            self._swap()
+            beta1, beta2 = group["betas"]
+            self.session.grad_map_adamw_multi(step, [p.grad for p in self.params], moments.views("m1"), moments.views("m2"),
+                                              lr=group["lr"], beta1=beta1, beta2=beta2, eps=group["eps"],
+                                              weight_decay=group["weight_decay"], adam_step=opt.steps + 1)
+            opt.steps += 1
+            self._refill_after()
             return
         if not self._fusable(opt):
             self.after_backward(step)

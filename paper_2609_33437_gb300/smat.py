@@ -33,7 +33,9 @@ EXPORTED = ("smat_workspace_bytes", "smat_init", "smat_simulate_multi", "smat_gr
             "smat_merge_workspace_bytes", "smat_merge", "smat_merge_ties_thresholds",
             "smat_grad_map_adamw_multi", "smat_linear_workspace_bytes", "smat_grad_input_workspace_bytes",
             "smat_grad_weight_workspace_bytes", "smat_linear", "smat_grad_input", "smat_grad_weight",
-            "smat_pack8", "smat_unpack8", "smat_act_grad8", "smat_linear_poll_errors")
+            "smat_pack8", "smat_unpack8", "smat_act_grad8", "smat_linear_poll_errors",
+            "smat_norm", "smat_norm_grad_workspace_bytes", "smat_norm_grad",
+            "smat_adamw_places", "smat_adamw_step", "smat_adamw_values")
 
 
 class AdamW(ctypes.Structure):
@@ -112,7 +114,7 @@ def load_library(build_if_missing: bool = True) -> ctypes.CDLL:
     L.smat_debug_fused.argtypes = [P, U32, P, I32, U32, P]
     L.smat_delta_sigma_noalloc.argtypes = [P, P, I64, I32, ctypes.c_float, P, P]
     L.smat_delta_sigma_noalloc.restype = I32
-    for name in ("smat_linear", "smat_grad_input", "smat_grad_weight"):
+    for name in ("smat_linear", "smat_grad_input", "smat_grad_weight", "smat_norm_grad"):
         getattr(L, name + "_workspace_bytes").argtypes = [P]
         getattr(L, name + "_workspace_bytes").restype = ctypes.c_size_t
         getattr(L, name).argtypes = [P, P, ctypes.c_size_t, P]
@@ -121,7 +123,12 @@ def load_library(build_if_missing: bool = True) -> ctypes.CDLL:
     L.smat_unpack8.argtypes = [P, I64, P, I64, P, I64, I64, I64, I32, I32, P]
     L.smat_act_grad8.argtypes = [P, I64, P, I64, P, I64, P, I64, I64, I64, I32, I32, P]
     L.smat_linear_poll_errors.argtypes = [P, ctypes.POINTER(I32)]
-    for name in ("smat_pack8", "smat_unpack8", "smat_act_grad8", "smat_linear_poll_errors"):
+    L.smat_norm.argtypes = [P, P]
+    L.smat_adamw_places.argtypes = [P, I32]
+    L.smat_adamw_places.restype = I64
+    L.smat_adamw_step.argtypes = [P, P]
+    L.smat_adamw_values.argtypes = [P, P, P, P, P, P, I64, P]
+    for name in ("smat_norm", "smat_adamw_step", "smat_adamw_values", "smat_pack8", "smat_unpack8", "smat_act_grad8", "smat_linear_poll_errors"):
         getattr(L, name).restype = I32
     L.smat_timing_enable.argtypes = [P, I32]
     L.smat_timing_read.argtypes = [P, P, P]

@@ -1,0 +1,120 @@
+"""CPU-only checks of the AdamW step over many tensors: what the C ABI and the binding refuse before anything reaches a GPU
+(pointers here are numbers; none is read), and the 8-bit form's definition in `_adamw_ref`."""
+
+import ctypes
+import struct
+
+import numpy as np
+import pytest
+import torch
+
+import _adamw_ref as A
+from paper_2609_33437_gb300 import optim as O
+from paper_2609_33437_gb300 import smat as S
+
+INVALID, UNSUPPORTED, ALIGNMENT = 1, 2, 3
+BASE = 0x10000000
+
+
+@pytest.fixture(scope="module")
+def lib():
+    return S.load_library()
+
+
+def _call(lib, params=(BASE, BASE + 0x1000), grads=(2 * BASE, 2 * BASE + 0x1000), numels=(300, 5), **kw):
+    n = len(numels)
+    arrays = [ctypes.create_string_buffer(struct.pack(f"{n}{c}", *v)) for c, v in (("P", params), ("P", grads), ("q", numels))]
+    v = dict(params_at=ctypes.addressof(arrays[0]), grads_at=ctypes.addressof(arrays[1]), numels_at=ctypes.addressof(arrays[2]), m1=3 * BASE,
+             m2=4 * BASE, e1=0, e2=0, scale_at=0, lr_at=0, step_at=0, scale=1.0, lr=1e-3, beta1=0.9, beta2=0.99, eps=1e-8, wd=0.0,
+             step=1, seed=0, n=n, dtype=1, gdtype=1, bits=32)
+    v.update(kw)
+    return lib.smat_adamw_step(O._ADAMW.pack(*v.values()), None)
+
+
+@pytest.mark.parametrize("bad,code", [
+    (dict(dtype=2), UNSUPPORTED), (dict(gdtype=-1), UNSUPPORTED), (dict(bits=16), UNSUPPORTED), (dict(lr=-1.0), INVALID),
+    (dict(lr=float("inf")), INVALID), (dict(lr=float("nan")), INVALID), (dict(beta1=1.0), INVALID), (dict(beta2=-0.1), INVALID),
+    (dict(eps=0.0), INVALID), (dict(eps=float("nan")), INVALID), (dict(wd=-1.0), INVALID), (dict(scale=float("nan")), INVALID),
+    (dict(step=0), INVALID), (dict(step=1 << 31), INVALID), (dict(n=-1), INVALID), (dict(params_at=0), INVALID), (dict(numels_at=0), INVALID),
+    (dict(numels=(-1, 5)), INVALID), (dict(numels=(1 << 41, 5)), INVALID), (dict(m1=0), INVALID), (dict(m2=4 * BASE + 8), ALIGNMENT),
+    (dict(e1=5 * BASE), INVALID), (dict(bits=8), INVALID), (dict(bits=8, e1=5 * BASE), INVALID),
+    (dict(bits=8, e1=5 * BASE, e2=5 * BASE), INVALID), (dict(m2=3 * BASE), INVALID), (dict(m1=BASE), INVALID),
+    (dict(scale_at=4 * BASE), INVALID), (dict(lr_at=4 * BASE), INVALID), (dict(step_at=3 * BASE), INVALID),
+    (dict(step_at=6 * BASE + 4), ALIGNMENT),
+])
+def test_refuses(lib, bad, code):
+    kw = dict(bad)
+    lists = {k: kw.pop(k) for k in ("numels",) if k in kw}
+    assert _call(lib, **lists, **kw) == code
+    assert lib.smat_last_error()
+
+
+def test_refuses_pointers(lib):
+    assert _call(lib, params=(BASE, 0)) == INVALID
+    assert _call(lib, params=(BASE, BASE + 0x1001)) == ALIGNMENT
+    assert _call(lib, params=(BASE, BASE)) == INVALID            # the same tensor twice
+    assert _call(lib, params=(BASE, BASE + 598)) == INVALID      # 300 bf16 end at 600
+    assert _call(lib, grads=(BASE, 2 * BASE)) == INVALID         # a gradient in its parameter
+    assert _call(lib, grads=(0, 0)) == 0                         # nothing to do
+    assert _call(lib, numels=(0, 0), params=(0, 0), grads=(0, 0)) == 0
+    assert lib.smat_adamw_step(None, None) == INVALID
+    assert _call(lib, numels=(1 << 32, 5), bits=8, e1=5 * BASE, e2=6 * BASE) == INVALID
+
+
+def test_places_and_values(lib):
+    numels = struct.pack("3q", 1, 256, 257)
+    assert lib.smat_adamw_places(numels, 3) == 256 + 256 + 512
+    assert lib.smat_adamw_places(None, 0) == 0 and lib.smat_adamw_places(numels, -1) == 0
+    b = [BASE * k for k in range(1, 7)]
+    assert lib.smat_adamw_values(*b, 100, None) == INVALID and lib.smat_adamw_values(*b, -256, None) == INVALID
+    assert lib.smat_adamw_values(*b, 0, None) == 0
+    assert lib.smat_adamw_values(b[0], b[1], b[2], b[3], b[0], b[5], 256, None) == INVALID
+    assert lib.smat_adamw_values(b[0] + 4, *b[1:], 256, None) == ALIGNMENT
+
+
+def test_binding_refuses():
+    p = torch.zeros(4)
+    with pytest.raises(ValueError, match="bits"):
+        O.Moments([p], bits=16)
+    with pytest.raises(ValueError, match="at least one"):
+        O.Moments([])
+    m = O.Moments([p])
+    assert m.places == 256 and m.starts == [0] and [v.shape for v in m.views("m1")] == [(4,)]
+    with pytest.raises(ValueError, match="moments of 1"):
+        O.adamw([p, p], [p], m, 1)
+    with pytest.raises(ValueError, match="CUDA"):
+        O.adamw([p], [p], m, 1)
+    with pytest.raises(ValueError, match=r"grads\[1\]"):
+        O._addresses("grads", [p, p[:2]], [4, 4], -1, True)
+    with pytest.raises(ValueError, match=r"params\[0\]"):
+        O._addresses("params", [torch.zeros(4, 2).t()], [8], -1, False)
+    with pytest.raises(ValueError, match="step"):
+        O._one("step", torch.zeros(2, dtype=torch.int64), torch.int64, p.device)
+    with pytest.raises(ValueError, match="bits"):
+        O.AdamW([p], bits=4)
+
+
+def test_the_8_bit_form():
+    """Every code reads back and packs to itself; a value in between is rounded up as often as its place says."""
+    q = np.arange(256, dtype=np.uint8)
+    for places, less, count in ((3, 16, 120), (4, 17, 240)):
+        v = np.zeros(A.GROUP)
+        v[:count] = A.table(places)[:count]  # up to the largest code a group's largest magnitude can have
+        e = np.array([90], np.uint8)
+        values = (v * 2.0 ** (90 - 127)).astype(np.float32)
+        for part in (0, 65535):
+            got, ge = A.codes(values, np.full(A.GROUP, part), places, less)
+            assert ge[0] == e[0] and bool((got[:count] == q[:count]).all())
+        assert bool((A.values(got, ge, places) == values).all())
+    v = np.full(A.GROUP, 1.0, np.float32)
+    v[1:] = 0.6 + 1 / 64 * 0.3  # steps are 1/16 of 1/2 there
+    rng = np.random.default_rng(0)
+    ups, n = 0, 400
+    for _ in range(n):
+        got, e = A.codes(v, rng.integers(0, 65536, A.GROUP), 3, 16)
+        back = A.values(got, e, 3)[1:]
+        ups += int((back > v[1:]).sum())
+        assert bool((abs(back - v[1:]) < 1 / 16).all())
+    low = np.floor(float(v[1]) * 16) / 16
+    p = (float(v[1]) - low) * 16
+    assert abs(ups / (n * 255) - p) < 5 * (p * (1 - p) / (n * 255)) ** 0.5

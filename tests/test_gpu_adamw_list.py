@@ -1,0 +1,355 @@
+"""The AdamW step over many tensors on the GPU (include/smat.h, "AdamW"): bit for bit against the definition in fp32
+(`_adamw_ref`), against 64 bits with every rounding counted, over ragged lists, both types and widths of moments, addresses off
+every boundary, gradients that are missing, special values, what the device holds, graphs, long lists and long tensors; the
+optimizer class, its state, and the periodic schedule around it."""
+
+import numpy as np
+import pytest
+import torch
+
+import _adamw_ref as A
+from paper_2609_33437_gb300 import optim as O
+from paper_2609_33437_gb300 import smat as S
+
+pytestmark = pytest.mark.gpu
+
+BF, F32 = torch.bfloat16, torch.float32
+SIZES = [1, 255, 256, 257, 0, 1000, 7, 4099, 512, 2048, 70001, 3]
+HYPER = dict(lr=1e-2, beta1=0.9, beta2=0.99, eps=1e-6, weight_decay=0.1)
+
+
+@pytest.fixture(autouse=True)
+def _cuda():
+    if not torch.cuda.is_available():
+        pytest.skip("needs a CUDA GPU")
+
+
+def _tensors(seed, sizes, dtype, scale, off=0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    out = []
+    for n in sizes:
+        t = torch.empty(n + off, device="cuda", dtype=dtype)[off:]
+        t.copy_(torch.randn(n, generator=g, device="cuda") * torch.exp(2 * torch.randn(n, generator=g, device="cuda")) * scale)
+        out.append(t)
+    return out
+
+
+def _flat(ts, sizes):
+    """fp32 numpy by place, 0 between tensors."""
+    at, total = A.starts(sizes)
+    out = np.zeros(total, np.float32)
+    for a, n, t in zip(at, sizes, ts):
+        if t is not None:
+            out[a:a + n] = t.float().cpu().numpy()
+    return out
+
+
+def _there(sizes, given):
+    at, total = A.starts(sizes)
+    out = np.zeros(total, bool)
+    for a, n, t in zip(at, sizes, given):
+        out[a:a + n] = t is not None
+    return out
+
+
+def _same(a, b):
+    a, b = np.asarray(a), np.asarray(b)
+    return a.shape == b.shape and bool(((a == b) | (np.isnan(a) & np.isnan(b))).all())
+
+
+class Model:
+    """The list and its moments on the CPU, stepped by the definition."""
+
+    def __init__(self, sizes, bits):
+        self.sizes, self.bits = sizes, bits
+        _, total = A.starts(sizes)
+        if bits == 8:
+            z = np.zeros(total, np.uint8)
+            self.state = [z, np.ones(total // A.GROUP, np.uint8), z.copy(), np.ones(total // A.GROUP, np.uint8)]
+        else:
+            self.state = [np.zeros(total, np.float32), np.zeros(total, np.float32)]
+
+    def step(self, params, grads, t, seed=0, scale=1.0, **hyper):
+        """The parameters as they will be, by place, in fp32 before their rounding; the state is stepped."""
+        there = _there(self.sizes, grads)
+        groups = there.reshape(-1, A.GROUP).any(1)
+        p, g = _flat(params, self.sizes), _flat(grads, self.sizes)
+        if self.bits == 8:
+            m1, r = (v.astype(np.float32) for v in A.unpack(*self.state))
+            m2 = r * r
+        else:
+            m1, m2 = self.state
+        q, m1, m2, r = A.step(p, g, m1, m2, A.constants(t, **hyper), scale)
+        zero = np.float32(0)
+        if self.bits == 8:
+            new = A.pack(np.where(there, m1, zero), np.where(there, r, zero), t, seed)
+            wide = np.repeat(groups, A.GROUP)
+            self.state = [np.where(wide if n.size == wide.size else groups, n, o) for n, o in zip(new, self.state)]
+        else:
+            self.state = [np.where(there, n, o) for n, o in zip((m1, m2), self.state)]
+        return q, there
+
+    def check(self, params, moments, want, there, dtype):
+        got = _flat(params, self.sizes)
+        want = torch.from_numpy(want).to(dtype).float().numpy()
+        bad = ~((got == want) | (np.isnan(got) & np.isnan(want))) & there
+        assert not bad.any(), f"{bad.sum()} parameters, first at {np.nonzero(bad)[0][0]}: {got[bad][0]} for {want[bad][0]}"
+        for (name, b), ref in zip(moments.buffers().items(), self.state):
+            b = b.cpu().numpy()
+            assert _same(b, ref), f"{name}: {(b != ref).sum()} off, first at {np.nonzero(b != ref)[0][:1]}"
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+@pytest.mark.parametrize("dt,gt", [(F32, F32), (BF, BF), (BF, F32), (F32, BF)])
+@pytest.mark.parametrize("off", [0, 1, 8])
+def test_steps_bit_for_bit(bits, dt, gt, off):
+    params = _tensors(0, SIZES, dt, 0.1, off)
+    moments, model = O.Moments(params, bits=bits), Model(SIZES, bits)
+    for t in (1, 2, 3):
+        grads = _tensors(10 + t, SIZES, gt, 1e-3, off if t > 1 else 0)
+        want, there = model.step(params, grads, t, seed=5 << 33 | 17, scale=0.5, **HYPER)
+        O.adamw(params, grads, moments, t, seed=5 << 33 | 17, scale=0.5, **HYPER)
+        model.check(params, moments, want, there, dt)
+    if bits == 8:
+        m1, r = moments.values()
+        for got, ref in zip((m1, r), A.unpack(*model.state)):
+            assert _same(got.double().cpu().numpy(), ref)
+        assert sum(t.numel() * t.element_size() for t in moments.buffers().values()) == moments.nbytes() <= 2.01 * moments.places
+    else:
+        assert moments.values()[0] is moments.buffers()["m1"]
+
+
+def test_against_64_bits():
+    """Every operation rounds by 2^-24 of its result at most, and the constants by as much."""
+    sizes = [70001, 300]
+    params, grads = _tensors(0, sizes, F32, 0.1), _tensors(1, sizes, F32, 1e-3)
+    moments = O.Moments(params)
+    m1, m2 = moments.values()
+    m1.copy_(torch.randn(m1.numel(), device="cuda") * 1e-3)
+    m2.copy_(torch.rand(m1.numel(), device="cuda") * 1e-6)
+    p, g, a, b = (v.astype(np.float64) for v in (_flat(params, sizes), _flat(grads, sizes), m1.cpu().numpy(), m2.cpu().numpy()))
+    O.adamw(params, grads, moments, 7, scale=0.25, **HYPER)
+    u, h = 2.0 ** -24, HYPER
+    g = g * 0.25
+    x, y = h["beta1"] * a, (1 - h["beta1"]) * g
+    m = x + y
+    e_m = 4 * u * (abs(x) + abs(y))
+    v = h["beta2"] * b + (1 - h["beta2"]) * g * g
+    d = np.sqrt(v) / np.sqrt(1 - h["beta2"] ** 7) + h["eps"]
+    k = h["lr"] / (1 - h["beta1"] ** 7)
+    want = p * (1 - h["lr"] * h["weight_decay"]) - k * m / d
+    tol = 4 * u * abs(p) + k * (e_m / d + 10 * u * abs(m) / d)  # v: 5 roundings, half of them left by the root; r, / bc2, + eps
+    there = _there(sizes, params)
+    for got, ref, e in ((_flat(params, sizes), want, tol), (m1.cpu().numpy(), m, e_m), (m2.cpu().numpy(), v, 6 * u * v)):
+        assert bool((abs(got - ref) <= 1.01 * e + 1e-40)[there].all())
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_missing_gradients_and_what_lies_beside(bits):
+    """Tensors without a gradient, their moments, and the elements beside a tensor stay as they are."""
+    sizes = [300, 5, 0, 1024, 77, 256]
+    whole = [torch.full((n + 16,), 7.0, device="cuda", dtype=BF) for n in sizes]
+    params = [w[8:8 + n] for w, n in zip(whole, sizes)]
+    moments, model = O.Moments(params, bits=bits), Model(sizes, bits)
+    for t, skip in ((1, ()), (2, (0, 3)), (3, (5,)), (4, (1, 4)), (5, range(6))):
+        grads = [None if k in skip else g for k, g in enumerate(_tensors(t, sizes, F32, 1e-2))]
+        want, there = model.step(params, grads, t, **HYPER)
+        O.adamw(params, grads, moments, t, **HYPER)
+        model.check(params, moments, want, there, BF)
+    for w, n in zip(whole, sizes):
+        assert bool((w[:8] == 7).all()) and bool((w[8 + n:] == 7).all())
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_special_values(bits):
+    """Zeros, subnormal and huge gradients; an infinity or NaN is seen in its element, and in 8 bits in its group."""
+    sizes = [600, 256]
+    params = _tensors(0, sizes, F32, 1.0)
+    moments, model = O.Moments(params, bits=bits), Model(sizes, bits)
+    for t, plant in ((1, {}), (2, {3: 1e-42, 4: -1e-30, 5: 1e18, 300: -1e-44}), (3, {10: float("inf")}), (4, {400: float("nan")}),
+                     (5, {})):
+        grads = [torch.zeros(n, device="cuda") for n in sizes]
+        for i, v in plant.items():
+            grads[0][i] = v
+        want, there = model.step(params, grads, t, **HYPER)
+        O.adamw(params, grads, moments, t, **HYPER)
+        model.check(params, moments, want, there, F32)
+    m1 = moments.values()[0][:600].float()
+    if bits == 8:
+        assert bool(m1[:512].isnan().all()) and not bool(m1[512:].isnan().any())
+    else:
+        assert int((~torch.isfinite(m1)).sum()) == 2
+    assert bool(torch.isfinite(moments.values()[0][768:].float()).all())
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_many_tensors(bits):
+    """More tensors than one launch takes."""
+    sizes = [1 + k % 5 * 80 for k in range(2701)]
+    params, grads = _tensors(0, sizes, BF, 0.1), _tensors(1, sizes, BF, 1e-3)
+    moments, model = O.Moments(params, bits=bits), Model(sizes, bits)
+    want, there = model.step(params, grads, 1, seed=3, **HYPER)
+    O.adamw(params, grads, moments, 1, seed=3, **HYPER)
+    model.check(params, moments, want, there, BF)
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_what_the_device_holds(bits):
+    """step, lr and scale on the device: as the same numbers from the host, and read anew by a replay."""
+    sizes = [1000, 33]
+    start, grads = _tensors(0, sizes, F32, 0.1), _tensors(1, sizes, F32, 1e-3)
+    hyper = {k: v for k, v in HYPER.items() if k != "lr"}
+    lr, scale = torch.full((), 0.0078125, device="cuda"), torch.full((1,), 0.5, device="cuda")
+    one, two = ([t.clone() for t in start] for _ in range(2))
+    m_one, m_two = O.Moments(one, bits=bits), O.Moments(two, bits=bits)
+    step = torch.ones((), dtype=torch.int64, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):  # captured, not run
+        O.adamw(two, grads, m_two, step, lr=lr, scale=scale, seed=9, **hyper)
+        step.add_(1)
+    for t in (1, 2, 3):
+        O.adamw(one, grads, m_one, t, lr=0.0078125 * t, scale=0.5, seed=9, **hyper)
+        lr.fill_(0.0078125 * t)
+        graph.replay()
+    assert int(step) == 4
+    # the constants are made in double on either side and rounded once: off by a unit in the last place at most where the two
+    # functions differ, and a byte by a step
+    for a, b in zip(one, two):
+        assert float((a - b).abs().max()) <= 3 * 2.0 ** -22 * 0.03 + 2.0 ** -23 * float(a.abs().max())
+    if bits == 32:
+        for a, b in zip(m_one.values(), m_two.values()):
+            assert torch.equal(a, b)
+    three, m_three = [t.clone() for t in start], O.Moments(start, bits=bits)
+    O.adamw(three, grads, m_three, 1, lr=lr, scale=0.5, seed=9, **hyper)
+    four, m_four = [t.clone() for t in start], O.Moments(start, bits=bits)
+    O.adamw(four, grads, m_four, 1, lr=float(lr), scale=0.5, seed=9, **hyper)
+    assert all(torch.equal(a, b) for a, b in zip(three, four))
+
+
+def test_streams_and_repeats():
+    sizes = [4096, 100]
+    start, grads = _tensors(0, sizes, BF, 0.1), _tensors(1, sizes, BF, 1e-3)
+    outs = []
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for stream in (None, side):
+        p = [t.clone() for t in start]
+        m = O.Moments(p, bits=8)
+        torch.cuda.synchronize()
+        for t in (1, 2):
+            O.adamw(p, grads, m, t, stream=stream, **HYPER)
+        v = m.values(stream=stream)
+        torch.cuda.synchronize()
+        outs.append((*p, *v))
+    assert all(torch.equal(a, b) for a, b in zip(*outs))
+
+
+def test_long_tensor_in_8_bits():
+    """Places past 2^31 and offsets past 32 bits: the ends of a long tensor and the tensor after it."""
+    n = (1 << 31) + 777
+    big, small = torch.zeros(n, device="cuda", dtype=BF), torch.zeros(100, device="cuda", dtype=BF)
+    grad, gsmall = torch.zeros(n, device="cuda", dtype=BF), _tensors(2, [100], BF, 1e-3)[0]
+    tail = _tensors(1, [5000], BF, 1e-3)[0]
+    grad[-5000:] = tail
+    moments = O.Moments([big, small], bits=8)
+    O.adamw([big, small], [grad, gsmall], moments, 1, seed=4, **HYPER)
+    first = (n - 5000) // A.GROUP * A.GROUP
+    g = np.zeros(moments.places - first, np.float32)
+    g[n - 5000 - first:n - first] = tail.float().cpu().numpy()
+    g[moments.starts[1] - first:moments.starts[1] - first + 100] = gsmall.float().cpu().numpy()
+    z = np.zeros_like(g)
+    p, m1, _, r = A.step(z, g, z, z, A.constants(1, **HYPER))
+    for (name, b), ref in zip(moments.buffers().items(), A.pack(m1, r, 1, 4, first)):
+        assert _same(b[-ref.size:].cpu().numpy(), ref), name
+    got = torch.cat([big[first:], torch.zeros(moments.starts[1] - n, device="cuda", dtype=BF), small]).cpu()
+    assert torch.equal(got, torch.from_numpy(p[:got.numel()]).to(BF))
+    assert not bool(big[:1 << 20].any()) and int(moments.buffers()["q1"][:first].max()) == 0
+
+
+def test_optimizer_matches_torch():
+    """optim.AdamW against torch.optim.AdamW in fp32: the same formula, a few roundings apart after ten steps."""
+    torch.manual_seed(0)
+    a = [torch.nn.Parameter(torch.randn(33, 7, device="cuda")), torch.nn.Parameter(torch.randn(40, device="cuda"))]
+    b = [torch.nn.Parameter(t.detach().clone()) for t in a]
+    groups = lambda ps: [dict(params=ps[:1], weight_decay=0.1), dict(params=ps[1:], lr=3e-3)]  # noqa: E731
+    mine, ref = O.AdamW(groups(a), lr=1e-2), torch.optim.AdamW(groups(b), lr=1e-2)
+    for t in range(10):
+        for p, q in zip(a, b):
+            q.grad = torch.randn_like(q)
+            p.grad = q.grad.clone()
+        mine.step()
+        ref.step()
+    for p, q in zip(a, b):
+        # ten steps of at most lr each, with about 12 roundings a step of their size, and two a step of the parameter
+        assert float((p - q).abs().max()) <= 10 * (12 * 1e-2 + 2 * 4.0) * 2.0 ** -24
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_optimizer_state_goes_on(bits):
+    """A saved and loaded state goes on with the same bits; mixed types make a list each."""
+    def make():
+        torch.manual_seed(1)
+        return [torch.nn.Parameter(torch.randn(300, device="cuda")), torch.nn.Parameter(torch.randn(4, 5, device="cuda").to(BF))]
+
+    def grads(ps, t):
+        g = torch.Generator(device="cuda").manual_seed(t)
+        for p in ps:
+            p.grad = torch.randn(p.shape, generator=g, device="cuda").to(p.dtype)
+
+    one = make()
+    opt = O.AdamW(one, lr=1e-2, bits=bits, seed=3)
+    for t in range(4):
+        grads(one, t)
+        opt.step()
+        if t == 1:
+            saved = {k: v for k, v in opt.state_dict().items()}
+            saved["moments"] = [{k: v.cpu().clone() if torch.is_tensor(v) else v for k, v in m.items()} for m in saved["moments"]]
+            two = [torch.nn.Parameter(p.detach().clone()) for p in one]
+    assert len(opt.lists()) == 2
+    again = O.AdamW(two, lr=1.0, bits=bits)
+    again.load_state_dict(saved)
+    for t in (2, 3):
+        grads(two, t)
+        again.step()
+    assert all(torch.equal(p, q) for p, q in zip(one, two)) and again.steps == 4
+    with pytest.raises(ValueError, match="other"):
+        O.AdamW(two, bits=40 - bits).load_state_dict(saved)
+
+
+def test_a_graph_that_saved_a_parameter_notices():
+    w = torch.nn.Parameter(torch.randn(8, 8, device="cuda"))
+    x = torch.randn(4, 8, device="cuda", requires_grad=True)
+    loss = (x @ w).sum()
+    w.grad = torch.ones_like(w)
+    O.AdamW([w]).step()
+    with pytest.raises(RuntimeError, match="modified by an inplace"):
+        loss.backward()
+
+
+@pytest.mark.parametrize("dt", [F32, BF])
+def test_schedule_takes_the_step_into_the_gradient_map(dt):
+    """PeriodicSmat.optimizer_step with an AdamW of 32 bits: the same bits as the mapped gradient and a step of its own (the
+    hyperparameters are powers of two, which the two calls' constants agree on)."""
+    from paper_2609_33437_gb300.schedule import PeriodicSmat
+
+    def run(fused):
+        torch.manual_seed(2)
+        params = [torch.nn.Parameter((torch.randn(n, device="cuda") * 0.1).to(dt)) for n in (700, 64)]
+        theta0 = [(p.detach() + 0.01).to(dt) for p in params]
+        sched = PeriodicSmat(params, [0.5, 1.0], [1e-3] * 2, theta0=theta0, period=2, seed=1, alpha_min=0.5, alpha_max=1.0,
+                             alpha_mode=S.SMAT_ALPHA_GLOBAL, noise=S.SMAT_NOISE_UNIFORM)
+        opt = O.AdamW(params, lr=2.0 ** -9, betas=(0.5, 0.75), eps=2.0 ** -20, weight_decay=2.0 ** -4)
+        for step in range(4):
+            sched.before_forward(step)
+            sum((p.float() ** 2).sum() for p in params).backward()
+            if fused:
+                sched.optimizer_step(step, opt)
+            else:
+                sched.after_backward(step)
+                opt.step()
+            opt.zero_grad()
+        assert opt.steps == 4
+        sched.close()
+        return [p.detach().clone() for p in params] + [v.clone() for v in opt.lists()[0][2].values()]
+
+    assert all(torch.equal(a, b) for a, b in zip(run(True), run(False)))
