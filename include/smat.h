@@ -593,6 +593,56 @@ size_t smat_norm_grad_workspace_bytes(const smat_norm_grad_args* args);
 smat_status smat_norm_grad(const smat_norm_grad_args* args, void* d_workspace, size_t workspace_bytes,
                            smat_stream_t stream);
 
+/* ------------------------------------------------------ loss over a vocabulary ---
+ * The loss behind a language model's last layer, softmax cross entropy of the logits l = x W^T, without keeping them, and its
+ * gradient, which makes them again, a piece of the vocabulary at a time.
+ *
+ *   lse_i = log sum_v exp l_iv,   loss_i = lse_i - l_i,t_i, and 0 where t_i = ignore
+ *   d_iv = g_i (exp(l_iv - lse_i) - [v = t_i]), and 0 where t_i = ignore:   dx = d W,  dW = d^T x
+ *
+ * x [rows, k] and W [n, k] of one dtype, row-major with row strides; targets int64 [rows]; loss, lse and g fp32 [rows]; dx and
+ * dW as x and W. g is the gradient that reaches the losses. Logits, their sums and those of dx and dW are held in fp32; a bf16
+ * call multiplies on the tensor cores (as smat_linear says) and rounds d to bf16 before its products with W and x. A target
+ * outside 0 .. n - 1 that is not `ignore` gives a loss of NaN and gradients of NaN. Rows with t_i = ignore have an lse like
+ * every row; back, they are left out: what they hold (infinities, NaN) reaches nothing, and their dx is 0. The workspace of the
+ * gradient is some 200 MB for pieces of d, and x's rows and dx in fp32; it does not grow with the vocabulary. Results do not
+ * depend on timing. rows and k may be 0, n is at least 1. Outputs must not overlap inputs or one another. What
+ * smat_linear_poll_errors says holds for these products too. */
+typedef struct {
+  const void* x;
+  const void* w;
+  const int64_t* targets;
+  float* loss;
+  float* lse;
+  int64_t rows, k, n;
+  int64_t ldx, ldw;
+  int64_t ignore;
+  int32_t dtype;
+  int32_t reserved; /* 0 */
+} smat_token_loss_args;
+
+typedef struct {
+  const float* g;
+  const void* x;
+  const void* w;
+  const int64_t* targets;
+  const float* lse; /* as smat_token_loss wrote it */
+  void* dx;         /* dx, dw: NULL where not wanted */
+  void* dw;
+  int64_t rows, k, n;
+  int64_t ldx, ldw, lddx, lddw;
+  int64_t ignore;
+  int32_t dtype;
+  int32_t accumulate; /* 1: dw is added to what it holds */
+} smat_token_loss_grad_args;
+
+/* Workspace and streams as for the linear layers. */
+size_t smat_token_loss_workspace_bytes(const smat_token_loss_args* args);
+smat_status smat_token_loss(const smat_token_loss_args* args, void* d_workspace, size_t workspace_bytes, smat_stream_t stream);
+size_t smat_token_loss_grad_workspace_bytes(const smat_token_loss_grad_args* args);
+smat_status smat_token_loss_grad(const smat_token_loss_grad_args* args, void* d_workspace, size_t workspace_bytes,
+                                 smat_stream_t stream);
+
 /* ------------------------------------------------------------------ AdamW ---
  * The optimizer's update on ordinary steps: one AdamW step over a list of tensors in one launch (for every 1,300 tensors),
  * with moments in 32 bits or in 8. For every element, each operation rounded to fp32 in this order, as

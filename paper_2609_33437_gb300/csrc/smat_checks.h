@@ -104,6 +104,25 @@ inline smat_status check_workspace(const void* d_workspace, size_t bytes, size_t
   return SMAT_OK;
 }
 
+// The tensor-core products read bf16 operands whose rows start on 16 bytes. One that does not is copied to the
+// workspace first: rows of ld_of(cols) elements.
+inline int64_t ld_of(int64_t cols) { return (cols + 31) / 32 * 32; }
+inline size_t copy_bytes(int64_t rows, int64_t cols, size_t elem) { return up((size_t)rows * (size_t)ld_of(cols) * elem); }
+
+struct Operand {
+  const void* p;
+  int64_t rows, cols, ld;
+  bool copied;
+};
+inline Operand operand(const void* p, int64_t rows, int64_t cols, int64_t ld, int32_t dtype) {
+  Operand o = {p, rows, cols, ld, false};
+  if (dtype != SMAT_BF16 || rows == 0 || cols == 0) return o;
+  if (rows == 1) o.ld = ld_of(cols);  // any stride will do
+  o.copied = (uintptr_t)p % 16 || o.ld % 8;
+  return o;
+}
+inline size_t operand_bytes(const Operand& o) { return o.copied ? copy_bytes(o.rows, o.cols, 2) : 0; }
+
 // An exception (the host's memory running out) is a status like any other failure.
 template <class F>
 smat_status guarded(F&& f) {

@@ -29,25 +29,6 @@ smat_status check_sizes(int64_t rows, int64_t k, int64_t n, int32_t dtype, int32
 
 int64_t groups_of(int64_t cols) { return (cols + SMAT_PACK8_GROUP - 1) / SMAT_PACK8_GROUP; }
 
-// The tensor-core products read bf16 operands whose rows start on 16 bytes. One that does not is copied to the
-// workspace first: rows of ld_of(cols) elements.
-int64_t ld_of(int64_t cols) { return (cols + 31) / 32 * 32; }
-size_t copy_bytes(int64_t rows, int64_t cols, size_t elem) { return up((size_t)rows * (size_t)ld_of(cols) * elem); }
-
-struct Operand {
-  const void* p;
-  int64_t rows, cols, ld;
-  bool copied;
-};
-Operand operand(const void* p, int64_t rows, int64_t cols, int64_t ld, int32_t dtype) {
-  Operand o = {p, rows, cols, ld, false};
-  if (dtype != SMAT_BF16 || rows == 0 || cols == 0) return o;
-  if (rows == 1) o.ld = ld_of(cols);  // any stride will do
-  o.copied = (uintptr_t)p % 16 || o.ld % 8;
-  return o;
-}
-size_t operand_bytes(const Operand& o) { return o.copied ? copy_bytes(o.rows, o.cols, 2) : 0; }
-
 // The operands of the three products, rows and columns as they lie in memory; of grad_weight's x^ in 8 bits, the
 // values it is read back to.
 struct Operands {

@@ -63,8 +63,12 @@ constexpr int kPairRows = 2 * kBM, kPairStages = 5, kPairStage = 2 * kBytesA;
 constexpr int kPairEpi = 12;
 constexpr int kPairThreads = 32 * (kPairEpi + 2);
 // A finishing warp's own shared memory: 32 rows of 32 results (64 bytes, swizzled) and of 32 q (32 bytes, swizzled).
-constexpr int kDeskRows = 32 * 64, kDeskQ = 32 * 32, kDesk = kDeskRows + kDeskQ;
-constexpr int kPairBytes = kPairStages * kPairStage + kPairEpi * kDesk + 1024;
+// Results in fp32 take 128 bytes a row and leave no q.
+constexpr int kDeskRows = 32 * 64, kDeskQ = 32 * 32;
+template <int MODE>
+constexpr int kDesk = MODE == kGradInputSum ? 32 * 128 : kDeskRows + kDeskQ;
+template <int MODE>
+constexpr int kPairBytes = kPairStages * kPairStage + kPairEpi * kDesk<MODE> + 1024;
 constexpr int kSums = 256;  // columns of tensor memory for one tile's sums
 
 struct Args {
@@ -81,6 +85,12 @@ struct Args {
 };
 
 using bf16 = __nv_bfloat16;
+
+template <int MODE>
+constexpr bool kWeightGrad = MODE == kGradWeight || MODE == kGradWeightRows;
+// Whether the tile's columns run along the other operand's rows, the sum down them.
+template <int MODE>
+constexpr bool kSumDown = MODE == kGradInput || MODE == kGradInputSum || kWeightGrad<MODE>;
 
 __device__ __forceinline__ void unpack_words(const uint32_t* w, int words, float* v) {
 #pragma unroll
@@ -158,16 +168,17 @@ __device__ __forceinline__ void desk_send(const Desk& desk, void* to, int64_t ld
 
 // Columns j .. j + 31 of rows i .. i + 31, a row per lane, out by TMA or by hand. A copy out leaves out rows outside the
 // result, but writes whole 16 bytes at a row's end: one that ends elsewhere has its last columns sent by hand, so that what
-// lies beside the result stays as it is. sums(v): their sums. False if a wait for what comes in has given up.
+// lies beside the result stays as it is. sums(v): their sums. False if a wait for what comes in has given up. rows: how many
+// count (kLogitGrad).
 template <int MODE, class Sums>
 __device__ __forceinline__ bool finish_block(const Args& a, const CUtensorMap* map_out, const CUtensorMap* map_in,
-                                            const CUtensorMap* map_q, int64_t i, int64_t j, Desk& desk,
+                                            const CUtensorMap* map_q, int64_t i, int64_t j, int64_t rows, Desk& desk,
                                             volatile int* dead, Sums&& sums) {
   const Product& p = a.p;
   const int lane = threadIdx.x % 32;
   const bool there = i + lane < p.I;
   const bool slope = MODE == kGradInput && p.act != SMAT_ACT_NONE;
-  const bool add = MODE == kForward ? p.residual != nullptr : MODE == kGradWeight && p.accumulate;
+  const bool add = MODE == kForward ? p.residual != nullptr : kWeightGrad<MODE> && p.accumulate;
   const bool save = MODE == kForward && p.q;
   const void* from = MODE == kForward ? p.residual : p.out;  // what is added
   const int64_t ld_from = MODE == kForward ? p.ldr : p.ldo;
@@ -192,9 +203,28 @@ __device__ __forceinline__ bool finish_block(const Args& a, const CUtensorMap* m
   }
   uint32_t e = 1;
   if (slope && there) e = p.e[(i + lane) * p.lde + j / kGroup];
+  LossRow row = {0.0f, 0.0f, -1, 0.0f};
+  bool counts = false;
+  if (MODE == kLogitGrad) {
+    counts = there && i + lane < rows;
+    if (counts) row = p.loss_rows[i + lane];
+  }
   __syncwarp();
   float v[32];
   sums(v);
+  if (MODE == kLogitGrad) {
+#pragma unroll
+    for (int t = 0; t < 32; ++t) v[t] = exp2_fast(fmaf(v[t], kLog2e, -row.lse2)) * row.g;
+    const int64_t at = row.target - p.first_col - j;  // of the target among the columns
+    if (row.target >= 0 && at >= 0 && at < 32) {
+#pragma unroll
+      for (int t = 0; t < 32; ++t) v[t] -= t == at ? row.g : 0.0f;
+    }
+    if (!counts) {  // rows behind the last one: they meet other rows in the weight's gradient
+#pragma unroll
+      for (int t = 0; t < 32; ++t) v[t] = 0.0f;
+    }
+  }
   if (MODE == kForward) {
     if (p.bias) {
       const bf16* b = (const bf16*)p.bias + j;
@@ -286,6 +316,83 @@ __device__ __forceinline__ bool finish_block(const Args& a, const CUtensorMap* m
   return true;
 }
 
+// The same in fp32, out by TMA, stored or added to what is there: one addition for each element and launch, so the order of the
+// launches is that of the additions.
+template <class Sums>
+__device__ __forceinline__ void finish_sum_block(const Args& a, const CUtensorMap* map_out, int64_t i, int64_t j, Desk& desk,
+                                                 Sums&& sums) {
+  const int lane = threadIdx.x % 32;
+  float v[32];
+  sums(v);
+  if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");  // the last block has left the desk
+  __syncwarp();
+#pragma unroll
+  for (int c = 0; c < 8; ++c) {
+    const uint32_t w[4] = {__float_as_uint(v[4 * c]), __float_as_uint(v[4 * c + 1]), __float_as_uint(v[4 * c + 2]),
+                           __float_as_uint(v[4 * c + 3])};
+    desk_store(desk.rows + lane * 128 + ((c ^ (lane & 7)) << 4), w);
+  }
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  __syncwarp();
+  if (lane == 0) {
+    if (a.p.accumulate)
+      tma_add(map_out, desk.rows, (int)j, (int)i);
+    else
+      tma_store(map_out, desk.rows, (int)j, (int)i);
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+  }
+}
+
+// The larger value; NaN if one is.
+__device__ __forceinline__ float top_of(float a, float b) {
+  float y;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+  return y;
+}
+
+// A row's logits as they come, a thread: their largest m and the sum of exp(logit - m), and the target's logit.
+struct LogitRow {
+  float m = -INFINITY, s = 0.0f;
+  int64_t row, target;  // among the product's columns; one outside them: none
+  bool there;
+
+  __device__ __forceinline__ LogitRow(const Product& p, int64_t i) : row(i), target(-1), there(i < p.I) {
+    if (there) target = p.targets[i] - p.first_col;
+  }
+  // columns j .. j + 31
+  __device__ __forceinline__ void add(const Product& p, int64_t j, float (&v)[32]) {
+    if (j + 32 > p.J) {
+#pragma unroll
+      for (int t = 0; t < 32; ++t) v[t] = j + t < p.J ? v[t] : -INFINITY;
+    }
+    float top[8];
+#pragma unroll
+    for (int t = 0; t < 8; ++t) top[t] = top_of(top_of(v[t], v[t + 8]), top_of(v[t + 16], v[t + 24]));
+#pragma unroll
+    for (int t = 4; t > 0; t /= 2)
+#pragma unroll
+      for (int u = 0; u < t; ++u) top[u] = top_of(top[u], top[u + t]);
+    const int64_t at = target - j;
+    if (there && at >= 0 && at < 32 && target < p.J) {
+      float x = v[0];
+#pragma unroll
+      for (int t = 1; t < 32; ++t) x = t == at ? v[t] : x;
+      p.picked[row] = x;
+    }
+    const float next = top_of(m, top[0]);
+    if (next == -INFINITY) return;  // logits of -infinity: exp(-infinity + infinity) would be NaN
+    const float next2 = next * kLog2e;
+    float part[4] = {s * exp2_fast((m - next) * kLog2e), 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int t = 0; t < 32; ++t) part[t % 4] += exp2_fast(fmaf(v[t], kLog2e, -next2));
+    s = (part[0] + part[1]) + (part[2] + part[3]);
+    m = next;
+  }
+  __device__ __forceinline__ void put(const Product& p, int64_t slot) const {
+    if (there) p.partials[slot * p.I + row] = make_float2(m, s);
+  }
+};
+
 // Column j of rows i .. i + N - 1, one thread; the warp holds 32 neighbouring columns from a multiple of 32 on. What
 // the rows read is asked for first, all of it.
 template <int MODE, int N>
@@ -349,12 +456,14 @@ __device__ __forceinline__ void finish_column(const Args& a, int64_t i, int64_t 
 template <int MODE, class Sums>
 __device__ __forceinline__ bool finish_blocks(const Args& a, const CUtensorMap* map_out, const CUtensorMap* map_in,
                                               const CUtensorMap* map_q, int64_t row0, int64_t col0, int first, int end,
-                                              int step, Desk& desk, volatile int* dead, Sums&& sums) {
+                                              int step, int64_t rows, Desk& desk, volatile int* dead, Sums&& sums) {
 #pragma unroll 1
   for (int c = first; c < end; c += step) {
     const int64_t col = col0 + 32 * c;
     if (row0 < a.p.I && col < a.p.J) {
-      if (!finish_block<MODE>(a, map_out, map_in, map_q, row0, col, desk, dead, [&](float(&v)[32]) { sums(c, v); }))
+      if constexpr (MODE == kGradInputSum)
+        finish_sum_block(a, map_out, row0, col, desk, [&](float(&v)[32]) { sums(c, v); });
+      else if (!finish_block<MODE>(a, map_out, map_in, map_q, row0, col, rows, desk, dead, [&](float(&v)[32]) { sums(c, v); }))
         return false;
     } else {
       float v[32];
@@ -362,6 +471,20 @@ __device__ __forceinline__ bool finish_blocks(const Args& a, const CUtensorMap* 
     }
   }
   return true;
+}
+
+// The same for logits, whose blocks leave as one part of a row's columns, number `slot`.
+template <class Sums>
+__device__ __forceinline__ void finish_logits(const Args& a, int64_t row0, int64_t col0, int first, int end, int step,
+                                              int64_t slot, Sums&& sums) {
+  LogitRow row(a.p, row0 + threadIdx.x % 32);
+#pragma unroll 1
+  for (int c = first; c < end; c += step) {
+    float v[32];
+    sums(c, v);
+    if (col0 + 32 * c < a.p.J) row.add(a.p, col0 + 32 * c, v);
+  }
+  row.put(a.p, slot);
 }
 
 template <int MODE, int BN>
@@ -551,7 +674,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                 const __grid_constant__ CUtensorMap map_out, const __grid_constant__ CUtensorMap map_in,
                 const __grid_constant__ CUtensorMap map_q, const __grid_constant__ Args a) {
-  constexpr bool A_MN = MODE == kGradWeight, B_MN = MODE != kForward;
+  constexpr bool A_MN = kWeightGrad<MODE>, B_MN = kSumDown<MODE>;
   constexpr int kStages = kPairStages, kStage = kPairStage;
 
   extern __shared__ uint8_t raw[];
@@ -563,15 +686,24 @@ __global__ void __launch_bounds__(kPairThreads, 1)
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const uint32_t full = smem_address(bars), empty = full + 8 * kStages, sums_full = empty + 8 * kStages,
                  sums_empty = sums_full + 16, drained = sums_empty + 16;
-  uint8_t* own = ring + kStages * kStage + warp * kDesk;  // a finishing warp's desk
+  uint8_t* own = ring + kStages * kStage + warp * kDesk<MODE>;  // a finishing warp's desk
   Desk desk = {smem_address(own), smem_address(own) + kDeskRows, drained + 8 + 8 * (uint32_t)warp, 0};
 
   uint32_t ctas, rank;
   asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(ctas));
   asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
   const uint32_t shares = ctas / 2, share = rank / 2, member = rank & 1, leader = rank & ~1u;
+  // rows that only the device counts: tiles and slices behind the last one are left out
+  int64_t tiles_r = a.tiles_r, tiles = a.tiles, rows = a.p.I;
+  int slices_there = a.slices;
+  if (MODE == kGradWeightRows) slices_there = min(slices_there, (*a.p.count + kBK - 1) / kBK);
+  if (MODE == kLogitGrad || MODE == kGradInputSum) {
+    rows = min(rows, (int64_t)*a.p.count);
+    tiles_r = (rows + kPairRows - 1) / kPairRows;
+    tiles = tiles_r * a.tiles_c;
+  }
   const int slice0 = (int)share * a.share;
-  const int slices = max(0, min(a.share, a.slices - slice0));
+  const int slices = max(0, min(a.share, slices_there - slice0));
   const int64_t first_tile = blockIdx.x / ctas, step = gridDim.x / ctas;
   const int half_width = a.width / 2;
 
@@ -608,9 +740,9 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     const uint32_t full_there = cluster_address_of(full, leader);
     uint32_t n = 0;  // slices fetched so far
     bool ok = true;
-    for (int64_t tile = first_tile; ok && tile < a.tiles; tile += step) {
+    for (int64_t tile = first_tile; ok && tile < tiles; tile += step) {
       int64_t tr, tc;
-      tile_place<8>(a.tiles_r, a.tiles_c, tile, tr, tc);
+      tile_place<8>(tiles_r, a.tiles_c, tile, tr, tc);
       const int r0 = (int)(tr * kPairRows) + (int)member * kBM, c0 = (int)(tc * a.width) + (int)member * half_width;
       for (int k = 0; k < slices; ++k, ++n) {
         const uint32_t s = n % kStages;
@@ -645,7 +777,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     const uint16_t both = (uint16_t)(3u << rank);
     uint32_t n = 0, made = 0;
     bool ok = true;
-    for (int64_t tile = first_tile; ok && tile < a.tiles; tile += step, ++made) {
+    for (int64_t tile = first_tile; ok && tile < tiles; tile += step, ++made) {
       const uint32_t half = made & 1, sums = tmem + half * kSums;
       ok = bar_wait(sums_empty + 8 * half, (made / 2 + 1) & 1, dead, a.errors);
       if (!ok) break;
@@ -684,9 +816,9 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     constexpr int kBeside = kPairEpi / 4;  // warps that share 32 rows
     const int blocks = a.width / 32, first = warp / 4 * blocks / kBeside, end = (warp / 4 + 1) * blocks / kBeside;
     uint32_t made = 0;
-    for (int64_t tile = first_tile; tile < a.tiles; tile += step, ++made) {
+    for (int64_t tile = first_tile; tile < tiles; tile += step, ++made) {
       int64_t tr, tc;
-      tile_place<8>(a.tiles_r, a.tiles_c, tile, tr, tc);
+      tile_place<8>(tiles_r, a.tiles_c, tile, tr, tc);
       const int64_t r0 = tr * kPairRows + (int)member * kBM + 32 * quarter, c0 = tc * a.width;
       const uint32_t half = made & 1, sums = tmem + half * kSums + ((uint32_t)(32 * quarter) << 16);
       if (!bar_wait_warp(sums_full + 8 * half, made / 2 & 1, dead, a.errors, kWaitNs + slices * kSliceNs)) break;
@@ -707,7 +839,11 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       };
       if (first == end) release();  // none of a narrow tile's columns
       if (shares == 1) {
-        if (!finish_blocks<MODE>(a, &map_out, &map_in, &map_q, r0, c0, first, end, 1, desk, dead, take)) break;
+        if constexpr (MODE == kLogits) {
+          finish_logits(a, r0, c0, first, end, 1, tc * kBeside + warp / 4, take);
+        } else if (!finish_blocks<MODE>(a, &map_out, &map_in, &map_q, r0, c0, first, end, 1, rows, desk, dead, take)) {
+          break;
+        }
       } else {
         float* part = a.parts + ((size_t)first_tile * ctas + rank) * a.width * kBM + 32 * quarter + lane;
         for (int c = first; c < end; ++c) {
@@ -723,18 +859,22 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     // one tile per cluster: its CTAs add up and finish blocks of their rows' columns in turn
     __syncthreads();
     cluster_sync();
-    if (warp < kPairEpi && !__any_sync(0xFFFFFFFFu, *dead)) {
+    if (warp < kPairEpi && first_tile < tiles && !__any_sync(0xFFFFFFFFu, *dead)) {
       int64_t tr, tc;
-      tile_place<8>(a.tiles_r, a.tiles_c, first_tile, tr, tc);
+      tile_place<8>(tiles_r, a.tiles_c, first_tile, tr, tc);
       const int quarter = warp % 4;
       const int64_t r0 = tr * kPairRows + (int)member * kBM + 32 * quarter, c0 = tc * a.width;
       const float* part = a.parts + ((size_t)first_tile * ctas + member) * a.width * kBM + 32 * quarter + lane;
       const size_t apart = (size_t)2 * a.width * kBM;
       const int blocks = r0 < a.p.I ? (int)((min((int64_t)a.width, a.p.J - c0) + 31) / 32) : 0;
-      finish_blocks<MODE>(a, &map_out, &map_in, &map_q, r0, c0, (int)share + (int)shares * (warp / 4), blocks,
-                          (int)shares * (kPairEpi / 4), desk, dead, [&](int c, float(&v)[32]) {
-                           add_parts(shares, v, [&](uint32_t s, int t) { return __ldcg(part + s * apart + (32 * c + t) * kBM); });
-                         });
+      const int first = (int)share + (int)shares * (warp / 4), step = (int)shares * (kPairEpi / 4);
+      auto joined = [&](int c, float(&v)[32]) {
+        add_parts(shares, v, [&](uint32_t s, int t) { return __ldcg(part + s * apart + (32 * c + t) * kBM); });
+      };
+      if constexpr (MODE == kLogits)
+        finish_logits(a, r0, c0, first, blocks, step, (tc * shares + share) * (kPairEpi / 4) + warp / 4, joined);
+      else
+        finish_blocks<MODE>(a, &map_out, &map_in, &map_q, r0, c0, first, blocks, step, rows, desk, dead, joined);
     }
   }
   if (warp < kPairEpi && lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");  // the desk has been read
@@ -746,17 +886,19 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2 * kSums));
 }
 
-// A row-major matrix [outer, inner] of bf16 or bytes in boxes of `wide` x `high`, swizzled over a box's row; what lies
+// A row-major matrix [outer, inner] of bf16, bytes or fp32 in boxes of `wide` x `high`, swizzled over a box's row; what lies
 // outside reads as 0.
 bool encode(CUtensorMap* map, const void* p, int64_t inner, int64_t outer, int64_t ld, int high, int wide = 64,
-            bool bytes = false) {
+            int elem = 2) {
   const cuuint64_t dims[2] = {(cuuint64_t)inner, (cuuint64_t)outer};
-  const cuuint64_t strides[1] = {(cuuint64_t)ld * (bytes ? 1 : 2)};
+  const cuuint64_t strides[1] = {(cuuint64_t)ld * elem};
   const cuuint32_t boxes[2] = {(cuuint32_t)wide, (cuuint32_t)high}, ones[2] = {1, 1};
-  const int row = wide * (bytes ? 1 : 2);
+  const int row = wide * elem;
   const Encode f = encoder();
-  return f && f(map, bytes ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(p),
-                dims, strides, boxes, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+  return f && f(map, elem == 1   ? CU_TENSOR_MAP_DATA_TYPE_UINT8
+                     : elem == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
+                                 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32,
+                2, const_cast<void*>(p), dims, strides, boxes, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
                 row == 128  ? CU_TENSOR_MAP_SWIZZLE_128B
                 : row == 64 ? CU_TENSOR_MAP_SWIZZLE_64B
                             : CU_TENSOR_MAP_SWIZZLE_32B,
@@ -805,7 +947,7 @@ cudaError_t plan_pair(const Product& p, Plan* plan) {
   static std::atomic<uint64_t> allowed;
   static std::atomic<int> clusters[64][9];
   auto* f = pair_kernel<MODE>;
-  const cudaError_t e = allow_shared(f, kPairBytes, allowed);
+  const cudaError_t e = allow_shared(f, kPairBytes<MODE>, allowed);
   if (e != cudaSuccess) return e;
   Plan best = {};
   double least = 0;
@@ -814,7 +956,7 @@ cudaError_t plan_pair(const Product& p, Plan* plan) {
   for (int width = 256; width >= 64; width -= 32) {
     const int64_t tiles_c = (p.J + width - 1) / width, tiles = tiles_r * tiles_c;
     for (int shares = 1; shares <= 4; ++shares) {
-      const int64_t at_once = clusters_at_once(f, 2 * shares, kPairThreads, kPairBytes, clusters);
+      const int64_t at_once = clusters_at_once(f, 2 * shares, kPairThreads, kPairBytes<MODE>, clusters);
       if (shares > 1 && (tiles > at_once || slices < 3 * shares)) break;
       const int share = (slices + shares - 1) / shares;
       const double rounds = (double)((tiles + at_once - 1) / at_once);
@@ -848,7 +990,7 @@ cudaError_t fill_args(const Product& p, const Plan& g, void* workspace, Args* ar
   auto rows_on = [](const void* q, int64_t ld, int elem, int bytes) {
     return (uintptr_t)q % bytes == 0 && (uint64_t)ld * elem % bytes == 0;
   };
-  a.by_rows = rows_on(p.out, p.ldo, 2, 16) && (!p.residual || rows_on(p.residual, p.ldr, 2, 16)) &&
+  a.by_rows = rows_on(p.out, p.ldo, p.mode == kGradInputSum ? 4 : 2, 16) && (!p.residual || rows_on(p.residual, p.ldr, 2, 16)) &&
               (!p.q || rows_on(p.q, p.ldq, 1, 16));
   a.whole_ends = p.J % 8 == 0 && (p.mode != kForward || !p.q || p.J % 16 == 0);
   a.wide_bias = (uintptr_t)p.bias % 16 == 0;
@@ -888,7 +1030,7 @@ cudaError_t launch_narrow(const Product& p, int sms, void* workspace, cudaStream
 
 template <int MODE>
 cudaError_t launch_pair(const Product& p, void* workspace, cudaStream_t s) {
-  constexpr bool A_MN = MODE == kGradWeight, B_MN = MODE != kForward;
+  constexpr bool A_MN = kWeightGrad<MODE>, B_MN = kSumDown<MODE>;
   Plan g;
   Args a;
   cudaError_t e = plan_pair<MODE>(p, &g);
@@ -900,18 +1042,20 @@ cudaError_t launch_pair(const Product& p, void* workspace, cudaStream_t s) {
     return cudaErrorNotSupported;
   // the results' rows, what is added to them, and q: those that are copied by TMA
   CUtensorMap mo = {}, mi = {}, mq = {};
-  const void* in = MODE == kForward ? p.residual : MODE == kGradWeight && p.accumulate ? p.out : nullptr;
-  if (a.by_rows && !(encode(&mo, p.out, p.J, p.I, p.ldo, 32, 32) &&
+  const void* in = MODE == kForward ? p.residual : kWeightGrad<MODE> && p.accumulate ? p.out : nullptr;
+  if (MODE == kGradInputSum) {
+    if (!a.by_rows || !encode(&mo, p.out, p.J, p.I, p.ldo, 32, 32, 4)) return cudaErrorNotSupported;
+  } else if (MODE != kLogits && a.by_rows && !(encode(&mo, p.out, p.J, p.I, p.ldo, 32, 32) &&
                      (!in || encode(&mi, in, p.J, p.I, MODE == kForward ? p.ldr : p.ldo, 32, 32)) &&
-                     (!p.q || encode(&mq, p.q, p.J, p.I, p.ldq, 32, 32, true))))
+                     (!p.q || encode(&mq, p.q, p.J, p.I, p.ldq, 32, 32, 1))))
     return cudaErrorNotSupported;
-  return launch(pair_kernel<MODE>, g.ctas, 2 * g.shares, kPairThreads, kPairBytes, s, ma, mb, mo, mi, mq, a);
+  return launch(pair_kernel<MODE>, g.ctas, 2 * g.shares, kPairThreads, kPairBytes<MODE>, s, ma, mb, mo, mi, mq, a);
 }
 
 // A product's kernel: go.narrow<MODE, BN>() or go.pair<MODE>(). Up to 128 rows the weight's columns take the tile's rows.
 template <int MODE, class Go>
 cudaError_t choose_mode(const Product& p, Go&& go) {
-  if constexpr (MODE != kGradWeight) {
+  if constexpr (MODE == kForward || MODE == kGradInput) {
     if (p.I <= 32) return go.template narrow<MODE, 32>();
     if (p.I <= 64) return go.template narrow<MODE, 64>();
     if (p.I <= 128) return go.template narrow<MODE, 128>();
@@ -923,6 +1067,10 @@ cudaError_t choose(const Product& p, Go&& go) {
   switch (p.mode) {
     case kForward: return choose_mode<kForward>(p, go);
     case kGradInput: return choose_mode<kGradInput>(p, go);
+    case kLogits: return choose_mode<kLogits>(p, go);
+    case kLogitGrad: return choose_mode<kLogitGrad>(p, go);
+    case kGradInputSum: return choose_mode<kGradInputSum>(p, go);
+    case kGradWeightRows: return choose_mode<kGradWeightRows>(p, go);
     default: return choose_mode<kGradWeight>(p, go);
   }
 }
@@ -966,6 +1114,13 @@ struct Size {
 cudaError_t tc_workspace(const Product& p, int sms, size_t* bytes) { return choose(p, Size{p, sms, bytes}); }
 cudaError_t launch_tc(const Product& p, int sms, void* workspace, cudaStream_t s) {
   return choose(p, Launch{p, sms, workspace, s});
+}
+
+cudaError_t logit_slots(const Product& p, int64_t* slots) {
+  Plan g = {};
+  const cudaError_t e = plan_pair<kLogits>(p, &g);
+  *slots = g.tiles_c * g.shares * (kPairEpi / 4);
+  return e;
 }
 
 cudaError_t error_word(int** at) {

@@ -98,6 +98,11 @@ __device__ __forceinline__ void tma_store(const CUtensorMap* map, uint32_t from,
                "r"(y)
                : "memory");
 }
+__device__ __forceinline__ void tma_add(const CUtensorMap* map, uint32_t from, int x, int y) {
+  asm volatile("cp.reduce.async.bulk.tensor.2d.global.shared::cta.add.tile.bulk_group [%0, {%2, %3}], [%1];" ::"l"(map),
+               "r"(from), "r"(x), "r"(y)
+               : "memory");
+}
 __device__ __forceinline__ void tma_load3(uint32_t to, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
   asm volatile(
       "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(

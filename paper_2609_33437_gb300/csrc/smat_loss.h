@@ -1,0 +1,53 @@
+// What the host side of the loss over a vocabulary (smat_loss_host.cpp) and its kernels (smat_loss.cu; the products are the
+// linear layers') share.
+#pragma once
+
+#include <cstdint>
+
+#include <cuda_runtime.h>
+
+#include "smat_linear.h"
+
+namespace smat {
+namespace loss {
+
+using lin::LossRow;
+
+// The rows that count (their target is not `ignore`) by number: place[row] or -1; info[place]; *count.
+struct Index {
+  const int64_t* targets;
+  const float* g;
+  const float* lse;
+  int64_t rows, n, ignore;
+  int* place;
+  LossRow* info;
+  int* count;
+};
+cudaError_t launch_index(const Index& a, cudaStream_t s);
+// x's rows that count, at their places; rows of zeros behind them up to the next multiple of 64 (bf16) or to the end (fp32).
+cudaError_t launch_gather(const void* x, int64_t ldx, const int* place, const int* count, void* to, int64_t ldto, int64_t rows,
+                          int64_t k, int dtype, int sms, cudaStream_t s);
+// dx from sums at the rows' places; 0 for a row that has none.
+cudaError_t launch_scatter(const float* from, int64_t ldfrom, const int* place, void* dx, int64_t lddx, int64_t rows, int64_t k,
+                           int dtype, int sms, cudaStream_t s);
+// A row's parts [slots][rows] (largest logit, sum of exponentials) joined.
+struct Join {
+  const float2* partials;
+  const float* picked;
+  const int64_t* targets;
+  float* loss;
+  float* lse;
+  int64_t rows, slots, n, ignore;
+};
+cudaError_t launch_join(const Join& a, cudaStream_t s);
+// fp32 logits of a piece of the vocabulary, [rows, cols]: their part of each row, and their gradient in their place (rows behind
+// the last one that counts: 0).
+cudaError_t launch_row_part(const float* z, int64_t ldz, int64_t rows, int64_t cols, int64_t first_col, const int64_t* targets,
+                            float2* part, float* picked, int sms, cudaStream_t s);
+cudaError_t launch_row_grad(float* z, int64_t ldz, int64_t rows, int64_t cols, int64_t first_col, const LossRow* info,
+                            const int* count, int sms, cudaStream_t s);
+// to += from, [rows, cols] both, row stride ld
+cudaError_t launch_add(float* to, const float* from, int64_t ld, int64_t rows, int64_t cols, int sms, cudaStream_t s);
+
+}  // namespace loss
+}  // namespace smat

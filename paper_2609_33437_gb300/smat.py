@@ -35,6 +35,7 @@ EXPORTED = ("smat_workspace_bytes", "smat_init", "smat_simulate_multi", "smat_gr
             "smat_grad_weight_workspace_bytes", "smat_linear", "smat_grad_input", "smat_grad_weight",
             "smat_pack8", "smat_unpack8", "smat_act_grad8", "smat_linear_poll_errors",
             "smat_norm", "smat_norm_grad_workspace_bytes", "smat_norm_grad",
+            "smat_token_loss_workspace_bytes", "smat_token_loss", "smat_token_loss_grad_workspace_bytes", "smat_token_loss_grad",
             "smat_adamw_places", "smat_adamw_step", "smat_adamw_values")
 
 
@@ -114,7 +115,8 @@ def load_library(build_if_missing: bool = True) -> ctypes.CDLL:
     L.smat_debug_fused.argtypes = [P, U32, P, I32, U32, P]
     L.smat_delta_sigma_noalloc.argtypes = [P, P, I64, I32, ctypes.c_float, P, P]
     L.smat_delta_sigma_noalloc.restype = I32
-    for name in ("smat_linear", "smat_grad_input", "smat_grad_weight", "smat_norm_grad"):
+    for name in ("smat_linear", "smat_grad_input", "smat_grad_weight", "smat_norm_grad", "smat_token_loss",
+                 "smat_token_loss_grad"):
         getattr(L, name + "_workspace_bytes").argtypes = [P]
         getattr(L, name + "_workspace_bytes").restype = ctypes.c_size_t
         getattr(L, name).argtypes = [P, P, ctypes.c_size_t, P]
