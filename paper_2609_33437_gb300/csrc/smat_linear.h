@@ -23,18 +23,10 @@ cudaError_t allow_shared(F* f, int bytes, std::atomic<uint64_t>& done) {
   return e;
 }
 
-// What happens to a product's sums on their way out. The last four are the bf16 products of the loss over a vocabulary
-// (smat_loss.h): logits that leave as their rows' largest values and sums of exponentials, logits that leave as their gradient,
-// an input's gradient in fp32, stored or added to what is there, and a weight's gradient over rows that the device counts.
-enum Mode : int {
-  kForward = 0,
-  kGradInput = 1,
-  kGradWeight = 2,
-  kLogits = 3,
-  kLogitGrad = 4,
-  kGradInputSum = 5,
-  kGradWeightRows = 6
-};
+// What happens to a product's sums on their way out. The last three are bf16 products of the loss over a vocabulary
+// (smat_loss.h): logits that leave as their gradient, an input's gradient in fp32, stored or added to what is there, and a
+// weight's gradient over rows that the device counts.
+enum Mode : int { kForward = 0, kGradInput = 1, kGradWeight = 2, kLogitGrad = 3, kGradInputSum = 4, kGradWeightRows = 5 };
 
 // A row of a logits' gradient: g (exp2(log2(e) logit - lse2) - [column = target]).
 struct LossRow {
@@ -73,10 +65,7 @@ struct Product {
   // the loss's products
   const int* count;         // kLogitGrad and on; on the device: how many rows there are, at most I (kGradWeightRows: L)
   const LossRow* loss_rows; // kLogitGrad: [I]
-  const int64_t* targets;   // kLogits: [I]
-  float2* partials;         // kLogits: [slots][I], a row's largest logit and sum of exponentials over a part of the columns
-  float* picked;            // kLogits: [I], the target's logit, where the target is one of the columns
-  int64_t first_col;        // kLogits, kLogitGrad: of the vocabulary
+  int64_t first_col;        // kLogitGrad: the first column's place in the vocabulary
 };
 
 // fp32 (smat_linear_f32.cu): any size, stride and alignment. `workspace`: f32_workspace() bytes, which go by mode, I, J
@@ -88,8 +77,6 @@ cudaError_t launch_f32(const Product& p, int sms, void* workspace, cudaStream_t 
 // `workspace`: tc_workspace() bytes, which go by mode, I, J and L alone.
 cudaError_t tc_workspace(const Product& p, int sms, size_t* bytes);
 cudaError_t launch_tc(const Product& p, int sms, void* workspace, cudaStream_t s);
-// kLogits: the parts that a row's columns come in.
-cudaError_t logit_slots(const Product& p, int64_t* slots);
 // The tensor-core products' error bits of the current device; read and cleared (waits for the stream).
 cudaError_t error_word(int** at);
 cudaError_t read_errors(int* out, cudaStream_t s);

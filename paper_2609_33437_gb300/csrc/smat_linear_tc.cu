@@ -343,56 +343,6 @@ __device__ __forceinline__ void finish_sum_block(const Args& a, const CUtensorMa
   }
 }
 
-// The larger value; NaN if one is.
-__device__ __forceinline__ float top_of(float a, float b) {
-  float y;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
-  return y;
-}
-
-// A row's logits as they come, a thread: their largest m and the sum of exp(logit - m), and the target's logit.
-struct LogitRow {
-  float m = -INFINITY, s = 0.0f;
-  int64_t row, target;  // among the product's columns; one outside them: none
-  bool there;
-
-  __device__ __forceinline__ LogitRow(const Product& p, int64_t i) : row(i), target(-1), there(i < p.I) {
-    if (there) target = p.targets[i] - p.first_col;
-  }
-  // columns j .. j + 31
-  __device__ __forceinline__ void add(const Product& p, int64_t j, float (&v)[32]) {
-    if (j + 32 > p.J) {
-#pragma unroll
-      for (int t = 0; t < 32; ++t) v[t] = j + t < p.J ? v[t] : -INFINITY;
-    }
-    float top[8];
-#pragma unroll
-    for (int t = 0; t < 8; ++t) top[t] = top_of(top_of(v[t], v[t + 8]), top_of(v[t + 16], v[t + 24]));
-#pragma unroll
-    for (int t = 4; t > 0; t /= 2)
-#pragma unroll
-      for (int u = 0; u < t; ++u) top[u] = top_of(top[u], top[u + t]);
-    const int64_t at = target - j;
-    if (there && at >= 0 && at < 32 && target < p.J) {
-      float x = v[0];
-#pragma unroll
-      for (int t = 1; t < 32; ++t) x = t == at ? v[t] : x;
-      p.picked[row] = x;
-    }
-    const float next = top_of(m, top[0]);
-    if (next == -INFINITY) return;  // logits of -infinity: exp(-infinity + infinity) would be NaN
-    const float next2 = next * kLog2e;
-    float part[4] = {s * exp2_fast((m - next) * kLog2e), 0.0f, 0.0f, 0.0f};
-#pragma unroll
-    for (int t = 0; t < 32; ++t) part[t % 4] += exp2_fast(fmaf(v[t], kLog2e, -next2));
-    s = (part[0] + part[1]) + (part[2] + part[3]);
-    m = next;
-  }
-  __device__ __forceinline__ void put(const Product& p, int64_t slot) const {
-    if (there) p.partials[slot * p.I + row] = make_float2(m, s);
-  }
-};
-
 // Column j of rows i .. i + N - 1, one thread; the warp holds 32 neighbouring columns from a multiple of 32 on. What
 // the rows read is asked for first, all of it.
 template <int MODE, int N>
@@ -471,20 +421,6 @@ __device__ __forceinline__ bool finish_blocks(const Args& a, const CUtensorMap* 
     }
   }
   return true;
-}
-
-// The same for logits, whose blocks leave as one part of a row's columns, number `slot`.
-template <class Sums>
-__device__ __forceinline__ void finish_logits(const Args& a, int64_t row0, int64_t col0, int first, int end, int step,
-                                              int64_t slot, Sums&& sums) {
-  LogitRow row(a.p, row0 + threadIdx.x % 32);
-#pragma unroll 1
-  for (int c = first; c < end; c += step) {
-    float v[32];
-    sums(c, v);
-    if (col0 + 32 * c < a.p.J) row.add(a.p, col0 + 32 * c, v);
-  }
-  row.put(a.p, slot);
 }
 
 template <int MODE, int BN>
@@ -839,11 +775,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       };
       if (first == end) release();  // none of a narrow tile's columns
       if (shares == 1) {
-        if constexpr (MODE == kLogits) {
-          finish_logits(a, r0, c0, first, end, 1, tc * kBeside + warp / 4, take);
-        } else if (!finish_blocks<MODE>(a, &map_out, &map_in, &map_q, r0, c0, first, end, 1, rows, desk, dead, take)) {
-          break;
-        }
+        if (!finish_blocks<MODE>(a, &map_out, &map_in, &map_q, r0, c0, first, end, 1, rows, desk, dead, take)) break;
       } else {
         float* part = a.parts + ((size_t)first_tile * ctas + rank) * a.width * kBM + 32 * quarter + lane;
         for (int c = first; c < end; ++c) {
@@ -867,14 +799,10 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       const float* part = a.parts + ((size_t)first_tile * ctas + member) * a.width * kBM + 32 * quarter + lane;
       const size_t apart = (size_t)2 * a.width * kBM;
       const int blocks = r0 < a.p.I ? (int)((min((int64_t)a.width, a.p.J - c0) + 31) / 32) : 0;
-      const int first = (int)share + (int)shares * (warp / 4), step = (int)shares * (kPairEpi / 4);
-      auto joined = [&](int c, float(&v)[32]) {
-        add_parts(shares, v, [&](uint32_t s, int t) { return __ldcg(part + s * apart + (32 * c + t) * kBM); });
-      };
-      if constexpr (MODE == kLogits)
-        finish_logits(a, r0, c0, first, blocks, step, (tc * shares + share) * (kPairEpi / 4) + warp / 4, joined);
-      else
-        finish_blocks<MODE>(a, &map_out, &map_in, &map_q, r0, c0, first, blocks, step, rows, desk, dead, joined);
+      finish_blocks<MODE>(a, &map_out, &map_in, &map_q, r0, c0, (int)share + (int)shares * (warp / 4), blocks,
+                          (int)shares * (kPairEpi / 4), rows, desk, dead, [&](int c, float(&v)[32]) {
+                           add_parts(shares, v, [&](uint32_t s, int t) { return __ldcg(part + s * apart + (32 * c + t) * kBM); });
+                         });
     }
   }
   if (warp < kPairEpi && lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");  // the desk has been read
@@ -884,25 +812,6 @@ __global__ void __launch_bounds__(kPairThreads, 1)
   cluster_meet();  // the partner's multiplications read this CTA's shared memory, and its arrivals write it
   if (warp == kPairEpi + 1)
     asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2 * kSums));
-}
-
-// A row-major matrix [outer, inner] of bf16, bytes or fp32 in boxes of `wide` x `high`, swizzled over a box's row; what lies
-// outside reads as 0.
-bool encode(CUtensorMap* map, const void* p, int64_t inner, int64_t outer, int64_t ld, int high, int wide = 64,
-            int elem = 2) {
-  const cuuint64_t dims[2] = {(cuuint64_t)inner, (cuuint64_t)outer};
-  const cuuint64_t strides[1] = {(cuuint64_t)ld * elem};
-  const cuuint32_t boxes[2] = {(cuuint32_t)wide, (cuuint32_t)high}, ones[2] = {1, 1};
-  const int row = wide * elem;
-  const Encode f = encoder();
-  return f && f(map, elem == 1   ? CU_TENSOR_MAP_DATA_TYPE_UINT8
-                     : elem == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
-                                 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32,
-                2, const_cast<void*>(p), dims, strides, boxes, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                row == 128  ? CU_TENSOR_MAP_SWIZZLE_128B
-                : row == 64 ? CU_TENSOR_MAP_SWIZZLE_64B
-                            : CU_TENSOR_MAP_SWIZZLE_32B,
-                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 // One product's launch: tiles, shares of the sum, workspace.
@@ -998,21 +907,6 @@ cudaError_t fill_args(const Product& p, const Plan& g, void* workspace, Args* ar
   return e;
 }
 
-template <class F, class... A>
-cudaError_t launch(F* f, int64_t ctas, int cluster, int threads, int bytes, cudaStream_t s, const A&... args) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)ctas);
-  cfg.blockDim = dim3(threads);
-  cfg.dynamicSmemBytes = bytes;
-  cfg.stream = s;
-  cudaLaunchAttribute at[1];
-  at[0].id = cudaLaunchAttributeClusterDimension;
-  at[0].val.clusterDim = {(unsigned)cluster, 1, 1};
-  cfg.attrs = at;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, f, args...);
-}
-
 template <int MODE, int BN>
 cudaError_t launch_narrow(const Product& p, int sms, void* workspace, cudaStream_t s) {
   Plan g;
@@ -1045,7 +939,7 @@ cudaError_t launch_pair(const Product& p, void* workspace, cudaStream_t s) {
   const void* in = MODE == kForward ? p.residual : kWeightGrad<MODE> && p.accumulate ? p.out : nullptr;
   if (MODE == kGradInputSum) {
     if (!a.by_rows || !encode(&mo, p.out, p.J, p.I, p.ldo, 32, 32, 4)) return cudaErrorNotSupported;
-  } else if (MODE != kLogits && a.by_rows && !(encode(&mo, p.out, p.J, p.I, p.ldo, 32, 32) &&
+  } else if (a.by_rows && !(encode(&mo, p.out, p.J, p.I, p.ldo, 32, 32) &&
                      (!in || encode(&mi, in, p.J, p.I, MODE == kForward ? p.ldr : p.ldo, 32, 32)) &&
                      (!p.q || encode(&mq, p.q, p.J, p.I, p.ldq, 32, 32, 1))))
     return cudaErrorNotSupported;
@@ -1067,7 +961,6 @@ cudaError_t choose(const Product& p, Go&& go) {
   switch (p.mode) {
     case kForward: return choose_mode<kForward>(p, go);
     case kGradInput: return choose_mode<kGradInput>(p, go);
-    case kLogits: return choose_mode<kLogits>(p, go);
     case kLogitGrad: return choose_mode<kLogitGrad>(p, go);
     case kGradInputSum: return choose_mode<kGradInputSum>(p, go);
     case kGradWeightRows: return choose_mode<kGradWeightRows>(p, go);
@@ -1114,13 +1007,6 @@ struct Size {
 cudaError_t tc_workspace(const Product& p, int sms, size_t* bytes) { return choose(p, Size{p, sms, bytes}); }
 cudaError_t launch_tc(const Product& p, int sms, void* workspace, cudaStream_t s) {
   return choose(p, Launch{p, sms, workspace, s});
-}
-
-cudaError_t logit_slots(const Product& p, int64_t* slots) {
-  Plan g = {};
-  const cudaError_t e = plan_pair<kLogits>(p, &g);
-  *slots = g.tiles_c * g.shares * (kPairEpi / 4);
-  return e;
 }
 
 cudaError_t error_word(int** at) {

@@ -1,6 +1,8 @@
 // What the tensor-core products share: barriers, TMA copies, tcgen05 instructions and their descriptors.
 #pragma once
 
+#include <atomic>
+
 #include <cuda.h>
 
 #include "smat_linear.cuh"
@@ -264,6 +266,40 @@ inline Encode encoder() {
     return reinterpret_cast<Encode>(p);
   }();
   return f;
+}
+
+// A row-major matrix [outer, inner] of bf16, bytes or fp32 in boxes of `wide` x `high`, swizzled over a box's row; what lies
+// outside reads as 0.
+inline bool encode(CUtensorMap* map, const void* p, int64_t inner, int64_t outer, int64_t ld, int high, int wide = 64,
+            int elem = 2) {
+  const cuuint64_t dims[2] = {(cuuint64_t)inner, (cuuint64_t)outer};
+  const cuuint64_t strides[1] = {(cuuint64_t)ld * elem};
+  const cuuint32_t boxes[2] = {(cuuint32_t)wide, (cuuint32_t)high}, ones[2] = {1, 1};
+  const int row = wide * elem;
+  const Encode f = encoder();
+  return f && f(map, elem == 1   ? CU_TENSOR_MAP_DATA_TYPE_UINT8
+                     : elem == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
+                                 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32,
+                2, const_cast<void*>(p), dims, strides, boxes, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                row == 128  ? CU_TENSOR_MAP_SWIZZLE_128B
+                : row == 64 ? CU_TENSOR_MAP_SWIZZLE_64B
+                            : CU_TENSOR_MAP_SWIZZLE_32B,
+                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <class F, class... A>
+cudaError_t launch(F* f, int64_t ctas, int cluster, int threads, int bytes, cudaStream_t s, const A&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)ctas);
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = bytes;
+  cfg.stream = s;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim = {(unsigned)cluster, 1, 1};
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, f, args...);
 }
 
 // How many clusters of `shares` CTAs of a kernel run at once on the current device, asked for once (a GPU's parts hold

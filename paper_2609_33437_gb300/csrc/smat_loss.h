@@ -13,6 +13,20 @@ namespace loss {
 
 using lin::LossRow;
 
+// bf16 logits x W^T of a piece of the vocabulary (smat_loss_tc.cu): x and w on 16-byte boundaries, row strides multiples of 8.
+struct Logits {
+  const void* x;
+  const void* w;
+  const int64_t* targets;
+  float2* partials;  // [slots][rows]: largest logit and sum of exponentials of what is left, of a part of the words
+  float* picked;     // [rows]: the target's logit, where the target is one of the words
+  int64_t rows, k, cols, ldx, ldw;
+  int64_t first_col;  // the first word's place in the vocabulary
+};
+// The parts that a row's words come in: by rows, k and cols alone.
+cudaError_t logit_slots(const Logits& p, int sms, int64_t* slots);
+cudaError_t launch_logits(const Logits& p, int sms, cudaStream_t s);
+
 // The rows that count (their target is not `ignore`) by number: place[row] or -1; info[place]; *count.
 struct Index {
   const int64_t* targets;

@@ -99,8 +99,10 @@ struct ForwardPlan {
   size_t partials, picked, xcopy, wcopy, z, parts, bytes;
 };
 
-Product logits(const smat_token_loss_args* a, int64_t cols) {
-  return product(a->dtype == SMAT_BF16 ? kLogits : kForward, a->dtype, a->rows, cols, a->k);
+loss::Logits logits(const smat_token_loss_args* a, int64_t cols) {
+  loss::Logits p = {};
+  p.rows = a->rows, p.k = a->k, p.cols = cols;
+  return p;
 }
 
 smat_status plan(const smat_token_loss_args* a, int sms, ForwardPlan* out) {
@@ -118,8 +120,8 @@ smat_status plan(const smat_token_loss_args* a, int sms, ForwardPlan* out) {
   int64_t last_slots = 1;
   f.slots = 1;
   if (bf) {
-    cudaError_t e = logit_slots(logits(a, f.piece), &f.slots);
-    if (e == cudaSuccess) e = logit_slots(logits(a, last), &last_slots);
+    cudaError_t e = loss::logit_slots(logits(a, f.piece), sms, &f.slots);
+    if (e == cudaSuccess) e = loss::logit_slots(logits(a, last), sms, &last_slots);
     if (e != cudaSuccess) return cuda_status(e, "plan of the logits' product");
   }
   Space s;
@@ -128,7 +130,9 @@ smat_status plan(const smat_token_loss_args* a, int sms, ForwardPlan* out) {
   f.xcopy = s.take(operand_bytes(f.x));
   f.wcopy = s.take(f.w.copied ? copy_bytes(f.piece, k, 2) : 0);
   f.z = s.take(bf ? 0 : copy_bytes(m, f.piece, 4));
-  f.parts = s.take(std::max(product_bytes(logits(a, f.piece), sms), product_bytes(logits(a, last), sms)));
+  if (!bf)
+    f.parts = s.take(std::max(product_bytes(product(kForward, a->dtype, m, f.piece, k), sms),
+                              product_bytes(product(kForward, a->dtype, m, last, k), sms)));
   f.bytes = s.at;
   *out = f;
   return SMAT_OK;
@@ -169,19 +173,22 @@ smat_status forward(const smat_token_loss_args* a, void* d_workspace, size_t wor
     Rows w;
     e = rows_of(a->w, a->ldw, f.w, c, cols, k, es, ws + f.wcopy, sms, s, &w);
     if (e != cudaSuccess) break;
-    Product p = logits(a, cols);
-    p.a = x.p, p.lda = x.ld, p.b = w.p, p.ldb = w.ld;
-    p.targets = a->targets, p.picked = picked, p.partials = partials + slots * m, p.first_col = c;
-    int64_t made = 1;
     if (bf) {
-      e = logit_slots(p, &made);
+      loss::Logits p = logits(a, cols);
+      p.x = x.p, p.ldx = x.ld, p.w = w.p, p.ldw = w.ld;
+      p.targets = a->targets, p.partials = partials + slots * m, p.picked = picked, p.first_col = c;
+      int64_t made = 0;
+      e = loss::logit_slots(p, sms, &made);
+      if (e == cudaSuccess) e = loss::launch_logits(p, sms, s);
+      slots += made;
     } else {
-      p.out = ws + f.z, p.ldo = ld_of(f.piece);
+      Product p = product(kForward, a->dtype, m, cols, k);
+      p.a = x.p, p.lda = x.ld, p.b = w.p, p.ldb = w.ld, p.out = ws + f.z, p.ldo = ld_of(f.piece);
+      e = launch_product(p, sms, ws + f.parts, s);
+      if (e == cudaSuccess)
+        e = loss::launch_row_part((const float*)p.out, p.ldo, m, cols, c, a->targets, partials + slots * m, picked, sms, s);
+      ++slots;
     }
-    if (e == cudaSuccess) e = launch_product(p, sms, ws + f.parts, s);
-    if (e == cudaSuccess && !bf)
-      e = loss::launch_row_part((const float*)p.out, p.ldo, m, cols, c, a->targets, p.partials, picked, sms, s);
-    slots += made;
   }
   if (e == cudaSuccess) e = loss::launch_join({partials, picked, a->targets, a->loss, a->lse, m, slots, n, a->ignore}, s);
   return cuda_status(e, "token_loss launch");
