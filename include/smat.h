@@ -663,14 +663,15 @@ smat_status smat_token_loss_grad(const smat_token_loss_grad_args* args, void* d_
  * its place between the two gives, decided by 16 bits of a number made of its place in the list, the seed and t, so that a
  * change below a step is not lost from one step to the next; the same call gives the same bits every time. A group that would
  * hold an infinity or NaN has e = 255 and reads back as NaN throughout, so that an overflow stays visible, for its neighbours'
- * moments too. The parameter is updated with the moments before they are rounded to 8 bits. places is below 2^32 then. */
+ * moments too. The parameter is updated with the moments before they are rounded to 8 bits; what is subtracted from it is made with
+ * the hardware's reciprocal then, and is off by 3 units in its last place. places is below 2^32. */
 #define SMAT_ADAMW_GROUP 256
 
 typedef struct {
   void* const* params;       /* HOST arrays of n_tensors: DEVICE pointers to numels[k] contiguous elements */
   const void* const* grads;  /* ... a NULL: that tensor and its moments stay as they are */
   const int64_t* numels;
-  void* m1;                  /* DEVICE, on 16 bytes: fp32, or bytes */
+  void* m1;                  /* DEVICE, on 32 bytes: fp32, or bytes */
   void* m2;                  /* ... m2, or r's bytes */
   uint8_t* e1;               /* 8 bits; NULL for 32 */
   uint8_t* e2;
@@ -678,7 +679,7 @@ typedef struct {
   const float* lr_at;
   const int64_t* step_at;
   double scale;              /* finite */
-  double lr, beta1, beta2, eps, weight_decay; /* as smat_adamw */
+  double lr, beta1, beta2, eps, weight_decay; /* as smat_adamw, eps at least 2^-126 */
   int64_t step;              /* t, 1 .. 2^31 - 1 */
   uint64_t seed;             /* of the 8 bits' roundings */
   int32_t n_tensors;

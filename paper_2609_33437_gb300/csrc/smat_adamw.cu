@@ -1,8 +1,9 @@
 // One AdamW step over a list of tensors, moments in 32 bits or in 8 (include/smat.h, "AdamW").
 //
 // A warp takes a group of 256 neighbours at a time, 8 a lane, so that the largest magnitudes of a group in 8 bits are one
-// reduction over the warp. Every CTA walks through a stretch of the list's groups; the tensors' addresses come with the launch
-// (no table on the device, nothing to copy), and a warp looks for its tensor once and then goes on from it.
+// reduction over the warp. All CTAs walk through the list side by side, 8 groups each at a time (a stretch of its own for each: 1,500
+// us for 16.8e6 x 22 elements in fp32, 5.9 TB/s; like this 1,360 us, 6.5 TB/s); the tensors' addresses come with the launch (no
+// table on the device, nothing to copy), and a warp looks for its tensor once and then goes on from it.
 
 #include "smat_adamw.h"
 
@@ -31,8 +32,10 @@ struct Launch {
 template <class T>
 __device__ __forceinline__ void load8(const T* p, float (&v)[8]) {
   if constexpr (sizeof(T) == 4) {
-    const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
-    v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+    asm volatile("ld.global.L1::no_allocate.v8.f32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7])
+                 : "l"(p)
+                 : "memory");
   } else {
     const uint4 u = *reinterpret_cast<const uint4*>(p);
     const uint32_t w[4] = {u.x, u.y, u.z, u.w};
@@ -43,8 +46,9 @@ __device__ __forceinline__ void load8(const T* p, float (&v)[8]) {
 template <class T>
 __device__ __forceinline__ void store8(T* p, const float (&v)[8]) {
   if constexpr (sizeof(T) == 4) {
-    reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
-    reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+    asm volatile("st.global.v8.f32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]),
+                 "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7])
+                 : "memory");
   } else {
     uint32_t w[4];
 #pragma unroll
@@ -57,41 +61,73 @@ __device__ __forceinline__ void store8(T* p, const float (&v)[8]) {
 }
 
 // A code of PLACES binary places is a small float: its upper bits an exponent, 0 for multiples of the unit. At the places of an
-// fp32 number's exponent and fraction it is its value times 2^-(126 + PLACES) (a subnormal number where the exponent is 0), so
-// two exact products make the value: by 2^127, and by 2^(PLACES - 1) and the unit. e = 255 stands for NaN: 0 by infinity.
+// fp32 number's exponent and fraction it is its value times 2^-(126 + PLACES) (a subnormal number where the exponent is 0), so an
+// exact product makes the value: by 2^(126 + PLACES) times the unit, 2^(e + PLACES - 1). For large units that is no fp32 number
+// and takes two factors (`far`); e = 255 stands for NaN: 0 by infinity.
+__device__ __forceinline__ float float_of(uint32_t bits) { return __uint_as_float(bits); }
 template <int PLACES>
-__device__ __forceinline__ float unit_of(uint32_t e) {
-  return __uint_as_float(min(e + PLACES - 1, 255u) << 23);
+struct Unit {
+  float by, more;
+  __device__ __forceinline__ Unit(uint32_t e, bool far)
+      : by(far ? 0x1p127f : float_of((e + PLACES + 126u) << 23)), more(float_of(min(e + PLACES - 1, 255u) << 23)) {}
+  __device__ __forceinline__ float operator()(float code, bool far) const {
+    const float v = __fmul_rn(code, by);
+    return far ? __fmul_rn(v, more) : v;
+  }
+};
+__device__ __forceinline__ bool far_units(uint32_t e1, uint32_t e2) { return max(e1, e2) > 120u; }
+// Byte i of four as such a float: m1's has a sign before 7 bits, r's 8 bits.
+__device__ __forceinline__ float signed_code(uint32_t w, int i) {
+  return __int_as_float((int)__byte_perm(w, 0, i << 12 | 0x0444) >> 4 & (int)0x87F00000u);
 }
+__device__ __forceinline__ float plain_code(uint32_t w, int i) { return __uint_as_float(__byte_perm(w, 0, i << 12 | 0x0444) >> 5); }
+
+// A code is the upper bits of an fp32 number: of v >= 0 itself from the first full-precision code on (B = 2^(e + PLACES - 127)), of
+// v + B less an exponent's step below; the larger of the two numbers (as bits) is the right one on either side of B. v + B is
+// rounded down, and what is below the code's last place is a fraction of 23 - PLACES bits to which the 16 bits of `part`, and a
+// half of their last one, are added: a carry is the neighbour above. The result's upper byte is the code. part: the 16 bits in
+// the middle of a word.
 template <int PLACES>
-__device__ __forceinline__ float value_of(uint32_t code, float unit) {
-  return __fmul_rn(__fmul_rn(__uint_as_float(code << (23 - PLACES)), 0x1p127f), unit);
+struct Coder {
+  float first;
+  uint32_t off;
+  __device__ __forceinline__ explicit Coder(uint32_t e)
+      : first(float_of((e + PLACES) << 23)), off(128u - ((e + PLACES - 1) << 23 << (PLACES + 1))) {}
+  __device__ __forceinline__ uint32_t operator()(float v, uint32_t part) const {
+    const uint32_t low = __float_as_uint(__fadd_rd(v, first)) - (1u << 23);
+    return max(low, __float_as_uint(v)) * (2u << PLACES) + (part + off);
+  }
+};
+// The upper bytes of four words
+__device__ __forceinline__ uint32_t upper_bytes(const uint32_t* w) {
+  return __byte_perm(__byte_perm(w[0], w[1], 0x0073), __byte_perm(w[2], w[3], 0x0073), 0x5410);
 }
-// The code of v >= 0, `inverse` being 1 / unit: the neighbour below, or the one above if the place between the two plus the
-// 16 bits of `part` reaches 1.
-template <int PLACES>
-__device__ __forceinline__ uint32_t code_of(float v, float inverse, uint32_t part) {
-  const float f = __fmul_rn(v, inverse);
-  const int at = max((int)(__float_as_uint(f) >> 23) - 127 - PLACES, 0);
-  const float by = __uint_as_float((uint32_t)(127 - at) << 23);
-  const float u = __uint_as_float(0x3F800000u | part << 7) - (1.0f - 0x1p-17f);  // (part + 1/2) 2^-16, exactly
-  // its whole part: the low bits of a sum with 2^23, rounded down
-  const uint32_t whole = __float_as_uint(__fadd_rd(__fadd_rn(__fmul_rn(f, by), u), 8388608.0f)) & 0xFFu;
-  return ((uint32_t)at << PLACES) + whole;
+// The largest magnitude; NaN if one is.
+__device__ __forceinline__ float larger_of(float a, float b, float c) {
+  float y;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(fabsf(b)), "f"(fabsf(c)));
+  return y;
 }
 // e of a group whose largest magnitude has the bits `top`
 __device__ __forceinline__ uint32_t exponent_of(uint32_t top, int less) {
   return top >= 0x7F800000u ? 255u : (uint32_t)max((int)(top >> 23) - less, 1);
 }
 
-// m1, m2 and the parameter, each operation rounded (as smat_grad_map_adamw_multi does it).
+// m1 and m2, each operation rounded (as smat_grad_map_adamw_multi does it).
 __device__ __forceinline__ void moments(const Constants& c, float g, float& m1, float& m2) {
   m1 = __fadd_rn(__fmul_rn(c.b1, m1), __fmul_rn(c.omb1, g));
   m2 = __fadd_rn(__fmul_rn(c.b2, m2), __fmul_rn(c.omb2, __fmul_rn(g, g)));
 }
+// The parameter. With moments in 32 bits rounded like them; with 8, whose steps of 1/16 hide it, by the hardware's reciprocal: off by
+// 3 units in the last place of what is subtracted (1 of the reciprocal, half a unit each of 1 / bc2, the sum and the product).
+template <int BITS>
 __device__ __forceinline__ float updated(const Constants& c, float p, float m1, float r) {
-  const float d = __fadd_rn(__fdiv_rn(r, c.bc2), c.eps);
-  return __fsub_rn(__fmul_rn(p, c.decay), __fmul_rn(c.step, __fdiv_rn(m1, d)));
+  if (BITS == 32) {
+    const float d = __fadd_rn(__fdiv_rn(r, c.bc2), c.eps);
+    return __fsub_rn(__fmul_rn(p, c.decay), __fmul_rn(c.step, __fdiv_rn(m1, d)));
+  }
+  const float d = fmaf(r, c.inv_bc2, c.eps);
+  return fmaf(-c.step, m1 * lin::rcp_fast(d), __fmul_rn(p, c.decay));
 }
 
 template <int BITS, class P, class G, int N>
@@ -106,7 +142,8 @@ __global__ void __launch_bounds__(32 * kWarps) step_kernel(const __grid_constant
       if (a.c.step_at) {
         const double t = (double)*a.c.step_at;
         c.step = (float)(lr / -expm1(t * a.c.log_b1));
-        c.bc2 = (float)sqrt(-expm1(t * a.c.log_b2));
+        const double root = sqrt(-expm1(t * a.c.log_b2));
+        c.bc2 = (float)root, c.inv_bc2 = (float)(1.0 / root);
         key = mix(mix(a.c.seed_key ^ (uint32_t)*a.c.step_at));
       } else {
         c.step = (float)(lr / a.c.bc1);
@@ -119,10 +156,9 @@ __global__ void __launch_bounds__(32 * kWarps) step_kernel(const __grid_constant
   }
   const float scale = a.c.scale_at ? *a.c.scale_at : a.c.scale;
   const int lane = threadIdx.x % 32;
-  const uint32_t begin = (uint32_t)((uint64_t)a.c.groups * blockIdx.x / gridDim.x);
-  const uint32_t end = (uint32_t)((uint64_t)a.c.groups * (blockIdx.x + 1) / gridDim.x);
-  uint32_t group = begin + threadIdx.x / 32;
-  if (group >= end) return;
+  const uint32_t first_place = (uint32_t)a.c.place;
+  int64_t group = (int64_t)blockIdx.x * kWarps + threadIdx.x / 32;
+  if (group >= a.c.groups) return;
   int at = 0;
   for (int high = a.c.n; high - at > 1;) {  // entries[at].first <= group < entries[high].first
     const int mid = (at + high) / 2;
@@ -131,12 +167,12 @@ __global__ void __launch_bounds__(32 * kWarps) step_kernel(const __grid_constant
     else
       high = mid;
   }
-  for (; group < end; group += kWarps) {
+  for (; group < a.c.groups; group += (int64_t)gridDim.x * kWarps) {
     while (at + 1 < a.c.n && a.entries[at + 1].first <= group) ++at;
     const Entry& e = a.entries[at];
     const uint32_t after = at + 1 < a.c.n ? a.entries[at + 1].first : a.c.groups;
     const int count = kGroup - (group + 1 == after ? e.lacks : 0);  // of this group's elements
-    const int64_t in = (int64_t)(group - e.first) * kGroup + lane * kEach, place = (int64_t)group * kGroup + lane * kEach;
+    const int64_t in = (group - e.first) * kGroup + lane * kEach, place = group * kGroup + lane * kEach;
     P* pp = (P*)e.p + in;
     const G* gp = (const G*)e.g + in;
     const int mine = min(max(count - lane * kEach, 0), kEach);
@@ -164,43 +200,69 @@ __global__ void __launch_bounds__(32 * kWarps) step_kernel(const __grid_constant
       }
     }
     if constexpr (BITS == 8) {
-      const float u1 = unit_of<3>(x1), u2 = unit_of<4>(x2);
-      uint32_t top1 = 0, top2 = 0;
+      const uint32_t w1[2] = {q1.x, q1.y}, w2[2] = {q2.x, q2.y};
       float r[8];
+      auto read = [&](auto is_far) {
+        constexpr bool kFar = decltype(is_far)::value;
+        const Unit<3> u1(x1, kFar);
+        const Unit<4> u2(x2, kFar);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          m1[i] = u1(signed_code(w1[i / 4], i % 4), kFar);
+          r[i] = u2(plain_code(w2[i / 4], i % 4), kFar);
+        }
+      };
+      if (far_units(x1, x2))
+        read(std::true_type());
+      else
+        read(std::false_type());
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const uint32_t b1 = (i < 4 ? q1.x : q1.y) >> 8 * (i % 4), b2 = (i < 4 ? q2.x : q2.y) >> 8 * (i % 4);
-        m1[i] = __uint_as_float(__float_as_uint(value_of<3>(b1 & 127u, u1)) | (b1 & 128u) << 24);
-        r[i] = value_of<4>(b2 & 255u, u2);
         m2[i] = __fmul_rn(r[i], r[i]);
         moments(c, __fmul_rn(g[i], scale), m1[i], m2[i]);
-        if (i >= mine) m1[i] = m2[i] = 0.0f;
-        r[i] = __fsqrt_rn(m2[i]);
-        top1 = max(top1, __float_as_uint(m1[i]) & 0x7FFFFFFFu);
-        top2 = max(top2, __float_as_uint(r[i]) & 0x7FFFFFFFu);
-        p[i] = updated(c, p[i], m1[i], r[i]);
       }
-      top1 = __reduce_max_sync(0xFFFFFFFFu, top1);
-      top2 = __reduce_max_sync(0xFFFFFFFFu, top2);
-      x1 = exponent_of(top1, 16), x2 = exponent_of(top2, 17);
-      uint32_t w1[2] = {0, 0}, w2[2] = {0, 0};
-      const float v1 = __uint_as_float((254u - min(x1, 253u)) << 23), v2 = __uint_as_float((254u - min(x2, 253u)) << 23);
+      if (mine < kEach) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (i >= mine) m1[i] = m2[i] = 0.0f;
+      }
+      float top1 = 0.0f, top2 = 0.0f;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const uint32_t d = mix((uint32_t)(a.c.place + place + i) ^ key);
-        const uint32_t c1 = code_of<3>(fabsf(m1[i]), v1, d & 0xFFFFu) | (m1[i] < 0.0f ? 128u : 0u);
-        const uint32_t c2 = code_of<4>(r[i], v2, d >> 16);
-        w1[i / 4] |= (x1 == 255u ? 0u : c1) << 8 * (i % 4);
-        w2[i / 4] |= (x2 == 255u ? 0u : c2) << 8 * (i % 4);
+        r[i] = __fsqrt_rn(m2[i]);
+        p[i] = updated<BITS>(c, p[i], m1[i], r[i]);
+        if (i % 2) top1 = larger_of(top1, m1[i - 1], m1[i]), top2 = larger_of(top2, r[i - 1], r[i]);
       }
-      *reinterpret_cast<uint2*>((uint8_t*)a.c.m1 + place) = make_uint2(w1[0], w1[1]);
-      *reinterpret_cast<uint2*>((uint8_t*)a.c.m2 + place) = make_uint2(w2[0], w2[1]);
+      x1 = exponent_of(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(top1)), 16);
+      x2 = exponent_of(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(top2)), 17);
+      const Coder<3> code1(x1);
+      const Coder<4> code2(x2);
+      // a lane's places differ in the last three bits, which the first step of their mixing leaves where they are
+      uint32_t mixed = (first_place + (uint32_t)place) ^ key;
+      mixed ^= mixed >> 16;
+      uint32_t c1[8], c2[8], sign[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        uint32_t d = (mixed ^ i) * kMix1;
+        d = (d ^ d >> 13) * kMix2;  // the last step, d ^ d >> 16, leaves the upper half as it is
+        const uint32_t upper = __byte_perm(d, 0, 0x4324), lower = __byte_perm(d, 0, 0x4104) ^ upper;
+        c1[i] = code1(fabsf(m1[i]), lower);
+        c2[i] = code2(r[i], upper);
+        sign[i] = __float_as_uint(m1[i]);
+      }
+      uint2 s1 = make_uint2(upper_bytes(c1) | (upper_bytes(sign) & 0x80808080u),
+                            upper_bytes(c1 + 4) | (upper_bytes(sign + 4) & 0x80808080u));
+      uint2 s2 = make_uint2(upper_bytes(c2), upper_bytes(c2 + 4));
+      if (x1 == 255u) s1 = make_uint2(0, 0);
+      if (x2 == 255u) s2 = make_uint2(0, 0);
+      *reinterpret_cast<uint2*>((uint8_t*)a.c.m1 + place) = s1;
+      *reinterpret_cast<uint2*>((uint8_t*)a.c.m2 + place) = s2;
       if (lane == 0) a.c.e1[group] = (uint8_t)x1, a.c.e2[group] = (uint8_t)x2;
     } else {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         moments(c, __fmul_rn(g[i], scale), m1[i], m2[i]);
-        p[i] = updated(c, p[i], m1[i], __fsqrt_rn(m2[i]));
+        p[i] = updated<BITS>(c, p[i], m1[i], __fsqrt_rn(m2[i]));
       }
       if (mine == kEach) {
         store8((float*)a.c.m1 + place, m1);
@@ -226,13 +288,15 @@ __global__ void __launch_bounds__(256) values_kernel(const uint8_t* q1, const ui
                                                      bf16* m1, bf16* r, int64_t places) {
   for (int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8; at < places; at += (int64_t)gridDim.x * 256 * 8) {
     const uint2 a = *reinterpret_cast<const uint2*>(q1 + at), b = *reinterpret_cast<const uint2*>(q2 + at);
-    const float u1 = unit_of<3>(e1[at / kGroup]), u2 = unit_of<4>(e2[at / kGroup]);
+    const uint32_t x1 = e1[at / kGroup], x2 = e2[at / kGroup];
+    const bool far = far_units(x1, x2);
+    const Unit<3> u1(x1, far);
+    const Unit<4> u2(x2, far);
     float v[8], w[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const uint32_t b1 = (i < 4 ? a.x : a.y) >> 8 * (i % 4), b2 = (i < 4 ? b.x : b.y) >> 8 * (i % 4);
-      v[i] = __uint_as_float(__float_as_uint(value_of<3>(b1 & 127u, u1)) | (b1 & 128u) << 24);
-      w[i] = value_of<4>(b2 & 255u, u2);
+      v[i] = u1(signed_code(i < 4 ? a.x : a.y, i % 4), far);
+      w[i] = u2(plain_code(i < 4 ? b.x : b.y, i % 4), far);
     }
     store8(m1 + at, v);
     store8(r + at, w);

@@ -23,7 +23,7 @@ struct Entry {
 
 struct Constants {  // computed in double, rounded once
   float b1, omb1, b2, omb2, eps;
-  float decay, step, bc2;  // 1 - lr wd, lr / (1 - b1^t), sqrt(1 - b2^t)
+  float decay, step, bc2, inv_bc2;  // 1 - lr wd, lr / (1 - b1^t), sqrt(1 - b2^t) and one over it
 };
 
 struct Call {
@@ -47,11 +47,12 @@ struct Call {
 // As many tensors as fit beside a Call in a launch's parameters (32,764 bytes).
 constexpr int kMaxEntries = 1300;
 
+constexpr uint32_t kMix1 = 0x85EBCA6Bu, kMix2 = 0xC2B2AE35u;
 __host__ __device__ inline uint32_t mix(uint32_t h) {  // the 32-bit finaliser of MurmurHash3 (A. Appleby)
   h ^= h >> 16;
-  h *= 0x85EBCA6Bu;
+  h *= kMix1;
   h ^= h >> 13;
-  h *= 0xC2B2AE35u;
+  h *= kMix2;
   return h ^ h >> 16;
 }
 

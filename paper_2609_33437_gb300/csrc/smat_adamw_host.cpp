@@ -83,7 +83,7 @@ smat_status step(const smat_adamw_args* a, cudaStream_t stream) {
   if (!within(a->lr, 0.0, huge)) return lfail(SMAT_ERR_INVALID_ARG, "lr must be finite and 0 or more");
   if (!within(a->beta1, 0.0, 1.0) || !within(a->beta2, 0.0, 1.0))
     return lfail(SMAT_ERR_INVALID_ARG, "betas must be in [0, 1)");
-  if (!within(a->eps, 1e-45, huge)) return lfail(SMAT_ERR_INVALID_ARG, "eps must be finite and above 0");
+  if (!within(a->eps, 1.1754944e-38, huge)) return lfail(SMAT_ERR_INVALID_ARG, "eps must be finite and at least 2^-126");
   if (!within(a->weight_decay, 0.0, huge))
     return lfail(SMAT_ERR_INVALID_ARG, "weight_decay must be finite and 0 or more");
   if (!a->step_at && (a->step < 1 || a->step >= (int64_t(1) << 31)))
@@ -110,8 +110,8 @@ smat_status step(const smat_adamw_args* a, cudaStream_t stream) {
     add("grads", k, a->grads[k], (size_t)a->numels[k] * eg, false, eg);
   }
   if (!any) return SMAT_OK;
-  add("m1", -1, a->m1, (size_t)places * em, true, 16);
-  add("m2", -1, a->m2, (size_t)places * em, true, 16);
+  add("m1", -1, a->m1, (size_t)places * em, true, 32);
+  add("m2", -1, a->m2, (size_t)places * em, true, 32);
   if (a->bits == 8) {
     add("e1", -1, a->e1, (size_t)(places / adamw::kGroup), true, 1);
     add("e2", -1, a->e2, (size_t)(places / adamw::kGroup), true, 1);
@@ -132,7 +132,8 @@ smat_status step(const smat_adamw_args* a, cudaStream_t stream) {
   const double bc1 = a->step_at ? 1.0 : -std::expm1(t * c.log_b1), bc2 = a->step_at ? 1.0 : -std::expm1(t * c.log_b2);
   c.bc1 = bc1;
   c.c = {(float)a->beta1, (float)(1.0 - a->beta1), (float)a->beta2, (float)(1.0 - a->beta2), (float)a->eps,
-         (float)(1.0 - a->lr * a->weight_decay), (float)(a->lr / bc1), (float)std::sqrt(bc2)};
+         (float)(1.0 - a->lr * a->weight_decay), (float)(a->lr / bc1), (float)std::sqrt(bc2),
+         (float)(1.0 / std::sqrt(bc2))};
   c.scale = (float)a->scale, c.scale_at = a->scale_at, c.lr_at = a->lr_at, c.step_at = a->step_at;
   c.seed_key = adamw::mix(adamw::mix((uint32_t)a->seed) ^ (uint32_t)(a->seed >> 32));
   c.key = adamw::mix(adamw::mix(c.seed_key ^ (uint32_t)a->step));

@@ -15,62 +15,75 @@ using lin::from_float;
 using lin::to_float;
 using bf16 = __nv_bfloat16;
 
-constexpr int kScan = 1024, kScanEach = 8;
+constexpr int kScan = 1024, kScanEach = 8, kScanWarps = kScan / 32;
 
-// One CTA: kScan threads take kScanEach neighbouring targets each at a time.
+// One CTA: kScanEach x kScan targets at a time, a warp's 32 neighbours counted by a vote.
 __global__ void __launch_bounds__(kScan) index_kernel(const Index a) {
-  __shared__ int sums[32];
+  constexpr int kVotes = kScanEach * kScanWarps;  // in the rows' order
+  __shared__ int counts[kVotes], sums[kVotes / 32];
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   int before = 0;  // that count, of the targets so far
   for (int64_t base = 0; base < a.rows; base += kScan * kScanEach) {
-    const int64_t first = base + (int64_t)threadIdx.x * kScanEach;
     int64_t t[kScanEach];
-    int mine = 0;
+    uint32_t votes[kScanEach];
 #pragma unroll
     for (int i = 0; i < kScanEach; ++i) {
-      t[i] = first + i < a.rows ? a.targets[first + i] : a.ignore;
-      mine += t[i] != a.ignore;
+      const int64_t row = base + i * kScan + threadIdx.x;
+      t[i] = row < a.rows ? a.targets[row] : a.ignore;
     }
-    int up = mine;  // inclusive, over the warp
 #pragma unroll
-    for (int d = 1; d < 32; d *= 2) {
-      const int v = __shfl_up_sync(0xFFFFFFFFu, up, d);
-      if (lane >= d) up += v;
+    for (int i = 0; i < kScanEach; ++i) {
+      votes[i] = __ballot_sync(0xFFFFFFFFu, t[i] != a.ignore);
+      if (lane == 0) counts[i * kScanWarps + warp] = __popc(votes[i]);
     }
-    if (lane == 31) sums[warp] = up;
     __syncthreads();
-    int at = before + up - mine, all = 0;
-    for (int w = 0; w < kScan / 32; ++w) {
-      if (w < warp) at += sums[w];
+    int up = 0;  // inclusive, over 32 votes
+    if (threadIdx.x < kVotes) {
+      up = counts[threadIdx.x];
+#pragma unroll
+      for (int d = 1; d < 32; d *= 2) {
+        const int v = __shfl_up_sync(0xFFFFFFFFu, up, d);
+        if (lane >= d) up += v;
+      }
+      if (lane == 31) sums[warp] = up;
+    }
+    __syncthreads();
+    int all = 0, here = before;
+#pragma unroll
+    for (int w = 0; w < kVotes / 32; ++w) {
+      if (w < warp) here += sums[w];
       all += sums[w];
+    }
+    if (threadIdx.x < kVotes) counts[threadIdx.x] = here + up - counts[threadIdx.x];  // before this vote
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kScanEach; ++i) {
+      const int64_t row = base + i * kScan + threadIdx.x;
+      const bool counted = votes[i] >> lane & 1;
+      if (row < a.rows) a.place[row] = counted ? counts[i * kScanWarps + warp] + __popc(votes[i] & ((1u << lane) - 1)) : -1;
     }
     before += all;
     __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kScanEach; ++i) {
-      const int64_t row = first + i;
-      if (row >= a.rows) break;
-      const bool counts = t[i] != a.ignore;
-      a.place[row] = counts ? at : -1;
-      if (!counts) continue;
-      const bool good = t[i] >= 0 && t[i] < a.n;
-      const float lse = a.lse[row];
-      a.info[at++] = {lse * lin::kLog2e, good ? a.g[row] : __int_as_float(0x7FC00000), good ? (int)t[i] : -1, lse};
-    }
   }
   if (threadIdx.x == 0) *a.count = before;
 }
 
 // A CTA per row at a time.
 template <class T, bool VEC>
-__global__ void __launch_bounds__(256) gather_kernel(const T* x, int64_t ldx, const int* place, const int* count, T* to,
-                                                     int64_t ldto, int64_t rows, int64_t k) {
-  const int there = *count;
+__global__ void __launch_bounds__(256) gather_kernel(const Index a, const T* x, int64_t ldx, T* to, int64_t ldto, int64_t k) {
+  const int there = *a.count;
+  const int64_t rows = a.rows;
   // rows that a product meets behind the last one: up to a whole slice in bf16, all of them in fp32
   const int64_t slice = sizeof(T) == 2 ? (there + 63) / 64 * 64 : rows, end = slice < rows ? slice : rows;
   for (int64_t row = blockIdx.x; row < rows; row += gridDim.x) {
-    const int at = place[row];
+    const int at = a.place[row];
     if (at >= 0) {
+      if (threadIdx.x == 0) {
+        const int64_t t = a.targets[row];
+        const bool good = t >= 0 && t < a.n;
+        const float lse = a.lse[row];
+        a.info[at] = {lse * lin::kLog2e, good ? a.g[row] : __int_as_float(0x7FC00000), good ? (int)t : -1, lse};
+      }
       const T* from = x + row * ldx;
       T* p = to + at * ldto;
       if (VEC) {
@@ -87,50 +100,72 @@ __global__ void __launch_bounds__(256) gather_kernel(const T* x, int64_t ldx, co
   }
 }
 
-template <class T>
+template <class T, bool VEC>
 __global__ void __launch_bounds__(256) scatter_kernel(const float* from, int64_t ldfrom, const int* place, T* dx, int64_t lddx,
                                                       int64_t rows, int64_t k) {
   for (int64_t row = blockIdx.x; row < rows; row += gridDim.x) {
     const int at = place[row];
-    for (int64_t j = threadIdx.x; j < k; j += 256) dx[row * lddx + j] = from_float<T>(at >= 0 ? from[at * ldfrom + j] : 0.0f);
-  }
-}
-
-// Largest value and sum of exponentials of what is left, joined with another's; NaN stays NaN.
-__device__ __forceinline__ void join(float& m, float& s, float m2, float s2) {
-  if (m2 == -INFINITY) return;
-  const float top = m2 > m || m2 != m2 ? m2 : m;
-  s = s * expf(m - top) + s2 * expf(m2 - top);
-  m = top;
-}
-
-// A lane per row, the warps share the parts.
-__global__ void __launch_bounds__(1024) join_kernel(const Join a) {
-  __shared__ float2 space[32][33];
-  const int lane = threadIdx.x, warp = threadIdx.y;
-  const int64_t row = (int64_t)blockIdx.x * 32 + lane;
-  float m = -INFINITY, s = 0.0f;
-  if (row < a.rows) {
-#pragma unroll 4
-    for (int64_t p = warp; p < a.slots; p += blockDim.y) {
-      const float2 v = a.partials[p * a.rows + row];
-      join(m, s, v.x, v.y);
+    const float* p = from + at * ldfrom;
+    T* to = dx + row * lddx;
+    if (VEC) {
+      for (int64_t j = threadIdx.x; j < k / 4; j += 256) {
+        const float4 v = at >= 0 ? __ldcs(reinterpret_cast<const float4*>(p) + j) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if constexpr (sizeof(T) == 2) {
+          const __nv_bfloat162 lo = __floats2bfloat162_rn(v.x, v.y), hi = __floats2bfloat162_rn(v.z, v.w);
+          reinterpret_cast<uint2*>(to)[j] = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+        } else {
+          reinterpret_cast<float4*>(to)[j] = v;
+        }
+      }
+      for (int64_t j = k / 4 * 4 + threadIdx.x; j < k; j += 256) to[j] = from_float<T>(at >= 0 ? p[j] : 0.0f);
+    } else {
+      for (int64_t j = threadIdx.x; j < k; j += 256) to[j] = from_float<T>(at >= 0 ? p[j] : 0.0f);
     }
   }
-  space[warp][lane] = make_float2(m, s);
-  __syncthreads();
-  if (warp > 0 || row >= a.rows) return;
-  for (int w = 1; w < (int)blockDim.y; ++w) join(m, s, space[w][lane].x, space[w][lane].y);
-  const float lse = m == -INFINITY ? m : m + logf(s);
-  const int64_t t = a.targets[row];
-  a.lse[row] = lse;
-  a.loss[row] = t == a.ignore ? 0.0f : t >= 0 && t < a.n ? lse - a.picked[row] : __int_as_float(0x7FC00000);
 }
 
 __device__ __forceinline__ float larger_of(float a, float b) {
   float y;
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
   return y;
+}
+
+// kJoinRows neighbouring rows a CTA; the other lanes and the warps share the parts: first the largest, then the sum of what they
+// stand for, so that no thread waits for its last step.
+constexpr int kJoinRows = 8;
+__global__ void __launch_bounds__(1024) join_kernel(const Join a) {
+  __shared__ float space[2][32][kJoinRows];
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, r = threadIdx.x % kJoinRows, warps = blockDim.x / 32;
+  const int64_t row = (int64_t)blockIdx.x * kJoinRows + r, first = threadIdx.x / kJoinRows, step = blockDim.x / kJoinRows;
+  float m = -INFINITY;
+  if (row < a.rows) {
+#pragma unroll 4
+    for (int64_t p = first; p < a.slots; p += step) m = larger_of(m, a.partials[p * a.rows + row].x);
+  }
+#pragma unroll
+  for (int d = kJoinRows; d < 32; d *= 2) m = larger_of(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
+  if (lane < kJoinRows) space[0][warp][r] = m;
+  __syncthreads();
+  for (int w = 0; w < warps; ++w) m = larger_of(m, space[0][w][r]);
+  float s = 0.0f;
+  if (row < a.rows && m != -INFINITY) {
+#pragma unroll 4
+    for (int64_t p = first; p < a.slots; p += step) {
+      const float2 v = a.partials[p * a.rows + row];
+      if (v.x != -INFINITY) s += v.y * expf(v.x - m);
+    }
+  }
+#pragma unroll
+  for (int d = kJoinRows; d < 32; d *= 2) s += __shfl_xor_sync(0xFFFFFFFFu, s, d);
+  if (lane < kJoinRows) space[1][warp][r] = s;
+  __syncthreads();
+  if (threadIdx.x >= kJoinRows || row >= a.rows) return;
+  s = 0.0f;
+  for (int w = 0; w < warps; ++w) s += space[1][w][r];
+  const float lse = m == -INFINITY ? m : m + logf(s);
+  const int64_t t = a.targets[row];
+  a.lse[row] = lse;
+  a.loss[row] = t == a.ignore ? 0.0f : t >= 0 && t < a.n ? lse - a.picked[row] : __int_as_float(0x7FC00000);
 }
 
 // A CTA per row at a time: the row's largest value, then the exponentials' sum.
@@ -141,7 +176,11 @@ __global__ void __launch_bounds__(256) row_part_kernel(const float* z, int64_t l
   for (int64_t row = blockIdx.x; row < rows; row += gridDim.x) {
     const float* p = z + row * ldz;
     float m = -INFINITY;
-    for (int64_t j = threadIdx.x; j < cols; j += 256) m = larger_of(m, p[j]);
+    for (int64_t j = threadIdx.x; j < cols / 4; j += 256) {
+      const float4 v = reinterpret_cast<const float4*>(p)[j];
+      m = larger_of(larger_of(m, larger_of(v.x, v.y)), larger_of(v.z, v.w));
+    }
+    for (int64_t j = cols / 4 * 4 + threadIdx.x; j < cols; j += 256) m = larger_of(m, p[j]);
 #pragma unroll
     for (int d = 16; d > 0; d /= 2) m = larger_of(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
     if (lane == 0) space[0][warp] = m;
@@ -149,8 +188,13 @@ __global__ void __launch_bounds__(256) row_part_kernel(const float* z, int64_t l
 #pragma unroll
     for (int w = 0; w < 8; ++w) m = larger_of(m, space[0][w]);
     float s = 0.0f;
-    if (m != -INFINITY)
-      for (int64_t j = threadIdx.x; j < cols; j += 256) s += expf(p[j] - m);
+    if (m != -INFINITY) {
+      for (int64_t j = threadIdx.x; j < cols / 4; j += 256) {
+        const float4 v = reinterpret_cast<const float4*>(p)[j];
+        s += (expf(v.x - m) + expf(v.y - m)) + (expf(v.z - m) + expf(v.w - m));
+      }
+      for (int64_t j = cols / 4 * 4 + threadIdx.x; j < cols; j += 256) s += expf(p[j] - m);
+    }
 #pragma unroll
     for (int d = 16; d > 0; d /= 2) s += __shfl_xor_sync(0xFFFFFFFFu, s, d);
     if (lane == 0) space[1][warp] = s;
@@ -191,15 +235,14 @@ cudaError_t launch_index(const Index& a, cudaStream_t s) {
   return cudaGetLastError();
 }
 
-cudaError_t launch_gather(const void* x, int64_t ldx, const int* place, const int* count, void* to, int64_t ldto, int64_t rows,
-                          int64_t k, int dtype, int sms, cudaStream_t s) {
-  if (rows == 0 || k == 0) return cudaSuccess;
+cudaError_t launch_gather(const Index& a, const void* x, int64_t ldx, void* to, int64_t ldto, int64_t k, int dtype, int sms,
+                          cudaStream_t s) {
   const int elem = dtype == SMAT_BF16 ? 2 : 4;
-  const bool vec = (uintptr_t)x % 16 == 0 && (rows == 1 || ldx * elem % 16 == 0);
-  const unsigned ctas = row_ctas(rows, sms);
+  const bool vec = (uintptr_t)x % 16 == 0 && (a.rows == 1 || ldx * elem % 16 == 0);
+  const unsigned ctas = row_ctas(a.rows, sms);
   auto go = [&](auto t, auto v) {
     using T = decltype(t);
-    gather_kernel<T, decltype(v)::value><<<ctas, 256, 0, s>>>((const T*)x, ldx, place, count, (T*)to, ldto, rows, k);
+    gather_kernel<T, decltype(v)::value><<<ctas, 256, 0, s>>>(a, (const T*)x, ldx, (T*)to, ldto, k);
     return cudaGetLastError();
   };
   if (dtype == SMAT_BF16) return vec ? go(bf16(), std::true_type()) : go(bf16(), std::false_type());
@@ -208,17 +251,23 @@ cudaError_t launch_gather(const void* x, int64_t ldx, const int* place, const in
 
 cudaError_t launch_scatter(const float* from, int64_t ldfrom, const int* place, void* dx, int64_t lddx, int64_t rows, int64_t k,
                            int dtype, int sms, cudaStream_t s) {
-  if (rows == 0 || k == 0) return cudaSuccess;
-  if (dtype == SMAT_BF16)
-    scatter_kernel<bf16><<<row_ctas(rows, sms), 256, 0, s>>>(from, ldfrom, place, (bf16*)dx, lddx, rows, k);
-  else
-    scatter_kernel<float><<<row_ctas(rows, sms), 256, 0, s>>>(from, ldfrom, place, (float*)dx, lddx, rows, k);
-  return cudaGetLastError();
+  const int bytes = dtype == SMAT_BF16 ? 8 : 16;  // of four elements
+  const bool vec = (uintptr_t)dx % bytes == 0 && (rows == 1 || lddx % 4 == 0);
+  auto go = [&](auto t, auto v) {
+    using T = decltype(t);
+    scatter_kernel<T, decltype(v)::value><<<row_ctas(rows, sms), 256, 0, s>>>(from, ldfrom, place, (T*)dx, lddx, rows, k);
+    return cudaGetLastError();
+  };
+  if (dtype == SMAT_BF16) return vec ? go(bf16(), std::true_type()) : go(bf16(), std::false_type());
+  return vec ? go(float(), std::true_type()) : go(float(), std::false_type());
 }
 
-cudaError_t launch_join(const Join& a, cudaStream_t s) {
-  const unsigned warps = (unsigned)(a.slots < 32 ? a.slots : 32);
-  join_kernel<<<(unsigned)((a.rows + 31) / 32), dim3(32, warps), 0, s>>>(a);
+cudaError_t launch_join(const Join& a, int sms, cudaStream_t s) {
+  // warps for all parts at once, but no more than run at once, or 8
+  const int64_t ctas = (a.rows + kJoinRows - 1) / kJoinRows, all = (a.slots * kJoinRows + 31) / 32;
+  int64_t warps = 32;
+  while (warps > 8 && ctas * warps > (int64_t)sms * 64) warps /= 2;
+  join_kernel<<<(unsigned)ctas, (unsigned)(32 * (all < warps ? all : warps)), 0, s>>>(a);
   return cudaGetLastError();
 }
 

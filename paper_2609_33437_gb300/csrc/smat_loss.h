@@ -27,7 +27,7 @@ struct Logits {
 cudaError_t logit_slots(const Logits& p, int sms, int64_t* slots);
 cudaError_t launch_logits(const Logits& p, int sms, cudaStream_t s);
 
-// The rows that count (their target is not `ignore`) by number: place[row] or -1; info[place]; *count.
+// The rows that count (their target is not `ignore`) by number: place[row] or -1, and *count.
 struct Index {
   const int64_t* targets;
   const float* g;
@@ -38,9 +38,10 @@ struct Index {
   int* count;
 };
 cudaError_t launch_index(const Index& a, cudaStream_t s);
-// x's rows that count, at their places; rows of zeros behind them up to the next multiple of 64 (bf16) or to the end (fp32).
-cudaError_t launch_gather(const void* x, int64_t ldx, const int* place, const int* count, void* to, int64_t ldto, int64_t rows,
-                          int64_t k, int dtype, int sms, cudaStream_t s);
+// x's rows that count and their info, at their places; rows of zeros behind them up to the next multiple of 64 (bf16) or to the end
+// (fp32).
+cudaError_t launch_gather(const Index& a, const void* x, int64_t ldx, void* to, int64_t ldto, int64_t k, int dtype, int sms,
+                          cudaStream_t s);
 // dx from sums at the rows' places; 0 for a row that has none.
 cudaError_t launch_scatter(const float* from, int64_t ldfrom, const int* place, void* dx, int64_t lddx, int64_t rows, int64_t k,
                            int dtype, int sms, cudaStream_t s);
@@ -53,7 +54,7 @@ struct Join {
   float* lse;
   int64_t rows, slots, n, ignore;
 };
-cudaError_t launch_join(const Join& a, cudaStream_t s);
+cudaError_t launch_join(const Join& a, int sms, cudaStream_t s);
 // fp32 logits of a piece of the vocabulary, [rows, cols]: their part of each row, and their gradient in their place (rows behind
 // the last one that counts: 0).
 cudaError_t launch_row_part(const float* z, int64_t ldz, int64_t rows, int64_t cols, int64_t first_col, const int64_t* targets,

@@ -190,7 +190,7 @@ smat_status forward(const smat_token_loss_args* a, void* d_workspace, size_t wor
       ++slots;
     }
   }
-  if (e == cudaSuccess) e = loss::launch_join({partials, picked, a->targets, a->loss, a->lse, m, slots, n, a->ignore}, s);
+  if (e == cudaSuccess) e = loss::launch_join({partials, picked, a->targets, a->loss, a->lse, m, slots, n, a->ignore}, sms, s);
   return cuda_status(e, "token_loss launch");
 }
 
@@ -278,8 +278,9 @@ smat_status backward(const smat_token_loss_grad_args* a, void* d_workspace, size
   LossRow* info = (LossRow*)(ws + f.info);
   const int64_t ldk = ld_of(k), ldd = ld_of(f.piece);
   float *sums = (float*)(ws + f.sums), *more = (float*)(ws + f.more);
-  cudaError_t e = loss::launch_index({a->targets, a->g, a->lse, m, n, a->ignore, place, info, count}, s);
-  if (e == cudaSuccess) e = loss::launch_gather(a->x, a->ldx, place, count, ws + f.x, ldk, m, k, a->dtype, sms, s);
+  const loss::Index index = {a->targets, a->g, a->lse, m, n, a->ignore, place, info, count};
+  cudaError_t e = loss::launch_index(index, s);
+  if (e == cudaSuccess) e = loss::launch_gather(index, a->x, a->ldx, ws + f.x, ldk, k, a->dtype, sms, s);
   for (int64_t c = 0; e == cudaSuccess && c < n; c += f.piece) {
     const int64_t cols = std::min(f.piece, n - c);
     Rows w;

@@ -62,8 +62,8 @@ def codes(v, part, places, less):
     f = np.ldexp(v, (127 - e)[:, None].astype(np.int32)).astype(np.float32)
     one = 1 << places
     at = np.where(f >= one, np.frexp(f)[1] - 1 - places, 0)
-    u = ((part.astype(np.float64) + 0.5) / 65536).astype(np.float32)
-    whole = np.floor((np.ldexp(f, -at.astype(np.int32)) + u).astype(np.float32)).astype(np.int64)
+    u = (part.astype(np.float64) + 0.5) / 65536  # 64 bits hold the sum exactly, but for values far below the unit, which it leaves
+    whole = np.floor(np.ldexp(f, -at.astype(np.int32)).astype(np.float64) + u).astype(np.int64)
     q = np.where(bad[:, None], 0, at * one + whole).astype(np.uint8)
     return q.reshape(-1), np.where(bad, 255, e).astype(np.uint8)
 
@@ -82,7 +82,7 @@ def values(q, e, places):
 def pack(m1, r, t, seed, first=0):
     n = numbers(np.arange(first, first + m1.size), t, seed)
     q1, e1 = codes(np.abs(m1), n & np.uint32(0xFFFF), 3, 16)
-    q1 = np.where(np.repeat(e1 == 255, GROUP), 0, q1 | np.where(m1 < 0, 128, 0)).astype(np.uint8)
+    q1 = np.where(np.repeat(e1 == 255, GROUP), 0, q1 | np.where(np.signbit(m1), 128, 0)).astype(np.uint8)
     q2, e2 = codes(r, n >> np.uint32(16), 4, 17)
     return q1, e1, q2, e2
 

@@ -36,7 +36,7 @@ def _call(lib, params=(BASE, BASE + 0x1000), grads=(2 * BASE, 2 * BASE + 0x1000)
     (dict(lr=float("inf")), INVALID), (dict(lr=float("nan")), INVALID), (dict(beta1=1.0), INVALID), (dict(beta2=-0.1), INVALID),
     (dict(eps=0.0), INVALID), (dict(eps=float("nan")), INVALID), (dict(wd=-1.0), INVALID), (dict(scale=float("nan")), INVALID),
     (dict(step=0), INVALID), (dict(step=1 << 31), INVALID), (dict(n=-1), INVALID), (dict(params_at=0), INVALID), (dict(numels_at=0), INVALID),
-    (dict(numels=(-1, 5)), INVALID), (dict(numels=(1 << 41, 5)), INVALID), (dict(m1=0), INVALID), (dict(m2=4 * BASE + 8), ALIGNMENT),
+    (dict(numels=(-1, 5)), INVALID), (dict(numels=(1 << 41, 5)), INVALID), (dict(m1=0), INVALID), (dict(m2=4 * BASE + 16), ALIGNMENT),
     (dict(e1=5 * BASE), INVALID), (dict(bits=8), INVALID), (dict(bits=8, e1=5 * BASE), INVALID),
     (dict(bits=8, e1=5 * BASE, e2=5 * BASE), INVALID), (dict(m2=3 * BASE), INVALID), (dict(m1=BASE), INVALID),
     (dict(scale_at=4 * BASE), INVALID), (dict(lr_at=4 * BASE), INVALID), (dict(step_at=3 * BASE), INVALID),

@@ -79,7 +79,10 @@ class Model:
             m2 = r * r
         else:
             m1, m2 = self.state
-        q, m1, m2, r = A.step(p, g, m1, m2, A.constants(t, **hyper), scale)
+        c = A.constants(t, **hyper)
+        q, m1, m2, r = A.step(p, g, m1, m2, c, scale)
+        with np.errstate(all="ignore"):
+            self.taken = np.abs(c["step"] * (m1 / (r / c["bc2"] + c["eps"])))
         zero = np.float32(0)
         if self.bits == 8:
             new = A.pack(np.where(there, m1, zero), np.where(there, r, zero), t, seed)
@@ -91,8 +94,15 @@ class Model:
 
     def check(self, params, moments, want, there, dtype):
         got = _flat(params, self.sizes)
+        exact = want.astype(np.float64)
         want = torch.from_numpy(want).to(dtype).float().numpy()
         bad = ~((got == want) | (np.isnan(got) & np.isnan(want))) & there
+        if self.bits == 8:
+            # what is subtracted is off by 3 units in its last place (a reciprocal's 1, three roundings), the definition's by its
+            # own four roundings, 2 units; either difference is rounded in fp32, and the kernel's to the type
+            with np.errstate(all="ignore"):
+                off = 5 * 2.0 ** -23 * self.taken + 2.0 ** -23 * np.abs(exact)
+                bad &= ~(np.abs(got - exact) <= off + (2.0 ** -8 if dtype == BF else 0.0) * (np.abs(exact) + off))
         assert not bad.any(), f"{bad.sum()} parameters, first at {np.nonzero(bad)[0][0]}: {got[bad][0]} for {want[bad][0]}"
         for (name, b), ref in zip(moments.buffers().items(), self.state):
             b = b.cpu().numpy()
@@ -262,7 +272,8 @@ def test_long_tensor_in_8_bits():
     for (name, b), ref in zip(moments.buffers().items(), A.pack(m1, r, 1, 4, first)):
         assert _same(b[-ref.size:].cpu().numpy(), ref), name
     got = torch.cat([big[first:], torch.zeros(moments.starts[1] - n, device="cuda", dtype=BF), small]).cpu()
-    assert torch.equal(got, torch.from_numpy(p[:got.numel()]).to(BF))
+    want = torch.from_numpy(p[:got.numel()]).double()
+    assert bool(((got.double() - want).abs() <= (2.0 ** -8 + 7 * 2.0 ** -23) * want.abs()).all())  # see Model.check
     assert not bool(big[:1 << 20].any()) and int(moments.buffers()["q1"][:first].max()) == 0
 
 
