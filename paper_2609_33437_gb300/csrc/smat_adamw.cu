@@ -19,7 +19,7 @@ using bf16 = __nv_bfloat16;
 using lin::from_float;
 using lin::to_float;
 
-constexpr int kWarps = 8, kEach = kGroup / 32;
+constexpr int kWarps = 8, kCtas = 4, kEach = kGroup / 32;
 static_assert(kEach == 8, "a lane's elements");
 
 template <int N>
@@ -60,6 +60,26 @@ __device__ __forceinline__ void store8(T* p, const float (&v)[8]) {
   }
 }
 
+// Two fp32 numbers, which one instruction multiplies. (Not for sums that have to be rounded by themselves: the compiler makes one
+// instruction of a product and a sum of pairs, whatever rounding they name.)
+struct Two {
+  uint64_t u;
+  __device__ __forceinline__ Two() {}
+  __device__ __forceinline__ Two(float a, float b) { asm("mov.b64 %0, {%1, %2};" : "=l"(u) : "f"(a), "f"(b)); }
+  __device__ __forceinline__ explicit Two(float a) : Two(a, a) {}
+  __device__ __forceinline__ void apart(float& a, float& b) const { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(u)); }
+};
+__device__ __forceinline__ Two operator*(Two a, Two b) {
+  Two y;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(y.u) : "l"(a.u), "l"(b.u));
+  return y;
+}
+__device__ __forceinline__ Two fma2(Two a, Two b, Two c) {
+  Two y;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(y.u) : "l"(a.u), "l"(b.u), "l"(c.u));
+  return y;
+}
+
 // A code of PLACES binary places is a small float: its upper bits an exponent, 0 for multiples of the unit. At the places of an
 // fp32 number's exponent and fraction it is its value times 2^-(126 + PLACES) (a subnormal number where the exponent is 0), so an
 // exact product makes the value: by 2^(126 + PLACES) times the unit, 2^(e + PLACES - 1). For large units that is no fp32 number
@@ -70,9 +90,10 @@ struct Unit {
   float by, more;
   __device__ __forceinline__ Unit(uint32_t e, bool far)
       : by(far ? 0x1p127f : float_of((e + PLACES + 126u) << 23)), more(float_of(min(e + PLACES - 1, 255u) << 23)) {}
-  __device__ __forceinline__ float operator()(float code, bool far) const {
-    const float v = __fmul_rn(code, by);
-    return far ? __fmul_rn(v, more) : v;
+  __device__ __forceinline__ void operator()(float a, float b, bool far, float& x, float& y) const {
+    Two v = Two(a, b) * Two(by);
+    if (far) v = v * Two(more);
+    v.apart(x, y);
   }
 };
 __device__ __forceinline__ bool far_units(uint32_t e1, uint32_t e2) { return max(e1, e2) > 120u; }
@@ -118,20 +139,14 @@ __device__ __forceinline__ void moments(const Constants& c, float g, float& m1, 
   m1 = __fadd_rn(__fmul_rn(c.b1, m1), __fmul_rn(c.omb1, g));
   m2 = __fadd_rn(__fmul_rn(c.b2, m2), __fmul_rn(c.omb2, __fmul_rn(g, g)));
 }
-// The parameter. With moments in 32 bits rounded like them; with 8, whose steps of 1/16 hide it, by the hardware's reciprocal: off by
-// 3 units in the last place of what is subtracted (1 of the reciprocal, half a unit each of 1 / bc2, the sum and the product).
-template <int BITS>
+// The parameter, with moments in 32 bits, rounded like them.
 __device__ __forceinline__ float updated(const Constants& c, float p, float m1, float r) {
-  if (BITS == 32) {
-    const float d = __fadd_rn(__fdiv_rn(r, c.bc2), c.eps);
-    return __fsub_rn(__fmul_rn(p, c.decay), __fmul_rn(c.step, __fdiv_rn(m1, d)));
-  }
-  const float d = fmaf(r, c.inv_bc2, c.eps);
-  return fmaf(-c.step, m1 * lin::rcp_fast(d), __fmul_rn(p, c.decay));
+  const float d = __fadd_rn(__fdiv_rn(r, c.bc2), c.eps);
+  return __fsub_rn(__fmul_rn(p, c.decay), __fmul_rn(c.step, __fdiv_rn(m1, d)));
 }
 
 template <int BITS, class P, class G, int N>
-__global__ void __launch_bounds__(32 * kWarps) step_kernel(const __grid_constant__ Launch<N> a) {
+__global__ void __launch_bounds__(32 * kWarps, kCtas) step_kernel(const __grid_constant__ Launch<N> a) {
   __shared__ Constants shared_c;
   __shared__ uint32_t shared_key;
   Constants c = a.c.c;
@@ -207,20 +222,25 @@ __global__ void __launch_bounds__(32 * kWarps) step_kernel(const __grid_constant
         const Unit<3> u1(x1, kFar);
         const Unit<4> u2(x2, kFar);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          m1[i] = u1(signed_code(w1[i / 4], i % 4), kFar);
-          r[i] = u2(plain_code(w2[i / 4], i % 4), kFar);
+        for (int i = 0; i < 8; i += 2) {
+          u1(signed_code(w1[i / 4], i % 4), signed_code(w1[i / 4], i % 4 + 1), kFar, m1[i], m1[i + 1]);
+          u2(plain_code(w2[i / 4], i % 4), plain_code(w2[i / 4], i % 4 + 1), kFar, r[i], r[i + 1]);
         }
       };
       if (far_units(x1, x2))
         read(std::true_type());
       else
         read(std::false_type());
+      // two at a time: with moments in 8 bits the instructions bound the step
+      const Two by(scale);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        m2[i] = __fmul_rn(r[i], r[i]);
-        moments(c, __fmul_rn(g[i], scale), m1[i], m2[i]);
+      for (int i = 0; i < 8; i += 2) {
+        const Two old(r[i], r[i + 1]);
+        (old * old).apart(m2[i], m2[i + 1]);
+        (Two(g[i], g[i + 1]) * by).apart(g[i], g[i + 1]);
       }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) moments(c, g[i], m1[i], m2[i]);
       if (mine < kEach) {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
@@ -228,10 +248,16 @@ __global__ void __launch_bounds__(32 * kWarps) step_kernel(const __grid_constant
       }
       float top1 = 0.0f, top2 = 0.0f;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        r[i] = __fsqrt_rn(m2[i]);
-        p[i] = updated<BITS>(c, p[i], m1[i], r[i]);
-        if (i % 2) top1 = larger_of(top1, m1[i - 1], m1[i]), top2 = larger_of(top2, r[i - 1], r[i]);
+      for (int i = 0; i < 4; ++i) {
+        const int e = 2 * i, f = e + 1;
+        r[e] = __fsqrt_rn(m2[e]), r[f] = __fsqrt_rn(m2[f]);
+        top1 = larger_of(top1, m1[e], m1[f]), top2 = larger_of(top2, r[e], r[f]);
+        // the parameter, whose change the moments' steps of 1/16 make coarse anyway, by the hardware's reciprocal: what is
+        // subtracted is off by 3 units in its last place (1 of the reciprocal, half a unit each of 1 / bc2, the sum, the product)
+        float d0, d1;
+        fma2(Two(r[e], r[f]), Two(c.inv_bc2), Two(c.eps)).apart(d0, d1);
+        const Two x = Two(m1[e], m1[f]) * Two(lin::rcp_fast(d0), lin::rcp_fast(d1));
+        fma2(Two(-c.step), x, Two(p[e], p[f]) * Two(c.decay)).apart(p[e], p[f]);
       }
       x1 = exponent_of(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(top1)), 16);
       x2 = exponent_of(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(top2)), 17);
@@ -262,7 +288,7 @@ __global__ void __launch_bounds__(32 * kWarps) step_kernel(const __grid_constant
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         moments(c, __fmul_rn(g[i], scale), m1[i], m2[i]);
-        p[i] = updated<BITS>(c, p[i], m1[i], __fsqrt_rn(m2[i]));
+        p[i] = updated(c, p[i], m1[i], __fsqrt_rn(m2[i]));
       }
       if (mine == kEach) {
         store8((float*)a.c.m1 + place, m1);
@@ -294,9 +320,10 @@ __global__ void __launch_bounds__(256) values_kernel(const uint8_t* q1, const ui
     const Unit<4> u2(x2, far);
     float v[8], w[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      v[i] = u1(signed_code(i < 4 ? a.x : a.y, i % 4), far);
-      w[i] = u2(plain_code(i < 4 ? b.x : b.y, i % 4), far);
+    for (int i = 0; i < 8; i += 2) {
+      const uint32_t x = i < 4 ? a.x : a.y, y = i < 4 ? b.x : b.y;
+      u1(signed_code(x, i % 4), signed_code(x, i % 4 + 1), far, v[i], v[i + 1]);
+      u2(plain_code(y, i % 4), plain_code(y, i % 4 + 1), far, w[i], w[i + 1]);
     }
     store8(m1 + at, v);
     store8(r + at, w);
@@ -308,7 +335,7 @@ cudaError_t launch_of(const Call& c, const Entry* entries, int sms, cudaStream_t
   Launch<N> a;
   a.c = c;
   for (int i = 0; i < c.n; ++i) a.entries[i] = entries[i];
-  const int64_t sets = ((int64_t)c.groups + kWarps - 1) / kWarps, room = (int64_t)sms * 4;
+  const int64_t sets = ((int64_t)c.groups + kWarps - 1) / kWarps, room = (int64_t)sms * kCtas;
   step_kernel<BITS, P, G, N><<<(unsigned)(sets < room ? sets : room), 32 * kWarps, 0, s>>>(a);
   return cudaGetLastError();
 }
