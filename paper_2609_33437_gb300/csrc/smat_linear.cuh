@@ -213,6 +213,35 @@ __device__ __forceinline__ void unpack_words8(const uint32_t* w, uint32_t e, flo
     v[i] = fmaf(__uint_as_float(__byte_perm(w[i / 4] ^ 0x80808080u, 0x4B000000u, 0x7540 | (i % 4))), by, less);
 }
 
+// fp32 numbers cut into bf16 parts for the tensor cores, see smat_linear_f32.cu.
+constexpr int kParts = 3;
+// Two values' nearest bf16, y's in the upper half; what would round to infinity stays bf16's largest number.
+__device__ __forceinline__ uint32_t nearest2(float x, float y) {
+  uint32_t w;
+  asm("cvt.rn.satfinite.bf16x2.f32 %0, %1, %2;" : "=r"(w) : "f"(y), "f"(x));
+  return w;
+}
+// The parts of two values, in pairs; x and y end as what is left, 0 from 2^-110 on. Cut off instead of rounded, the parts
+// would have the value's sign, and what is left out of a product would be up to 2^-21 of it and always of one sign.
+// `top`: the largest magnitude's bits so far.
+__device__ __forceinline__ void cut2(float x, float y, uint32_t (&w)[3], uint32_t& top) {
+  top = max(top, max(__float_as_uint(x) & 0x7FFFFFFFu, __float_as_uint(y) & 0x7FFFFFFFu));
+#pragma unroll
+  for (int t = 0; t < 3; ++t) {
+    w[t] = nearest2(x, y);
+    x -= __uint_as_float(w[t] << 16);
+    y -= __uint_as_float(w[t] & 0xFFFF0000u);
+  }
+}
+
+// What an operand's largest magnitude (as bits) says of its parts. From infinity on they do not stand for the values. Nor do
+// they below 2^-86, if there is anything: 2^-24 of the largest value is then less than the 2^-110 from which they are exact.
+enum Flag : uint32_t { kOdd = 1, kSmall = 2, kLarge = 4 };  // an operand is odd, or small in one CTA and large in none
+constexpr uint32_t kSmallest = (127u - 86u) << 23;
+__device__ __forceinline__ uint32_t flag_of(uint32_t top) {
+  return top >= 0x7F800000u ? kOdd : top >= kSmallest ? kLarge : top > 0u ? kSmall : 0u;
+}
+
 // Thread-block cluster: a barrier of all its threads (with release and acquire of shared memory), and a float of
 // the shared memory of its CTA `rank`, at the place that `p` has here.
 __device__ __forceinline__ void cluster_sync() {

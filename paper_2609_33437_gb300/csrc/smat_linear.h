@@ -63,7 +63,7 @@ struct Product {
   void* db;
   int sum_shares, add_db;
   // the loss's products
-  const int* count;         // kLogitGrad and on; on the device: how many rows there are, at most I (kGradWeightRows: L)
+  const int* count;         // kLogitGrad and on, launch_f32_parts; on the device: how many rows there are, at most I (or L)
   const LossRow* loss_rows; // kLogitGrad: [I]
   int64_t first_col;        // kLogitGrad: the first column's place in the vocabulary
 };
@@ -72,6 +72,28 @@ struct Product {
 // and L alone.
 cudaError_t f32_workspace(const Product& p, int sms, size_t* bytes);
 cudaError_t launch_f32(const Product& p, int sms, void* workspace, cudaStream_t s);
+
+// The same in steps, for operands that several products share and rows that the device counts (p.count: the rows i, for a weight's
+// gradient the terms of the sum). An operand [rows, cols] is cut into parts of bf16, [3][rows][parts_ld(cols)], and flags that say
+// whether they stand for it. Only for products that f32_on_tensor_cores() names.
+struct Parts {
+  void* p;  // parts_bytes(rows, cols)
+  uint32_t* flags;
+  int n_flags;  // parts_flags(rows, cols), where launch_cut makes them
+};
+struct Uncut {
+  const float* from;  // or NULL: nothing to cut
+  int64_t rows, cols, ld;
+  const int* count;  // or NULL: on the device, the rows there are; those behind them up to a multiple of 64 hold zeros
+  Parts to;
+};
+bool f32_on_tensor_cores(const Product& p);
+int64_t parts_ld(int64_t cols);
+size_t parts_bytes(int64_t rows, int64_t cols);
+int parts_flags(int64_t rows, int64_t cols, int sms);
+cudaError_t launch_cut(const Uncut& a, const Uncut& b, int sms, cudaStream_t s);
+cudaError_t f32_parts_workspace(const Product& p, int sms, size_t* bytes);
+cudaError_t launch_f32_parts(const Product& p, const Parts& of_b, const Parts& of_a, int sms, void* workspace, cudaStream_t s);
 
 // bf16 on the tensor cores (smat_linear_tc.cu): a and b on 16-byte boundaries, lda and ldb multiples of 8.
 // `workspace`: tc_workspace() bytes, which go by mode, I, J and L alone.

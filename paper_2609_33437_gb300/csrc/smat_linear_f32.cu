@@ -516,7 +516,6 @@ __global__ void __launch_bounds__(32 * kRowWarps, 2) rows_kernel(const Args a) {
 // A tile has 128 columns j of the result along tensor memory's rows and `width` of its rows i along the columns, 32 to 160:
 // the sums of 160 take 80 registers of each of the 256 threads that add them up. A warp then holds 32 neighbouring columns of
 // a row, 128 bytes.
-constexpr int kParts = 3;
 constexpr int kPart = kBM * kBK * 2;  // a slice of one part of the operand along the tile's rows
 constexpr int kMostWidth = 160, kStages = 2;
 constexpr int kBlock = 16, kMostBlocks = kMostWidth / kBlock / 2;  // of a warp's sums
@@ -532,35 +531,9 @@ struct Cut {
   const float* from;
   uint16_t* to;
   int64_t rows, cols, ld, ldp;
-  bool vec;  // rows on 16 bytes
+  bool vec;          // rows on 16 bytes
+  const int* count;  // or NULL: on the device, the rows there are; those up to the next multiple of 64 are cut too
 };
-
-// Two values' nearest bf16, y's in the upper half; what would round to infinity stays bf16's largest number.
-__device__ __forceinline__ uint32_t nearest2(float x, float y) {
-  uint32_t w;
-  asm("cvt.rn.satfinite.bf16x2.f32 %0, %1, %2;" : "=r"(w) : "f"(y), "f"(x));
-  return w;
-}
-// The parts of two values, in pairs; x and y end as what is left, 0 from 2^-110 on. Cut off instead of rounded, the parts
-// would have the value's sign, and what is left out of a product would be up to 2^-21 of it and always of one sign.
-// `top`: the largest magnitude's bits so far.
-__device__ __forceinline__ void cut2(float x, float y, uint32_t (&w)[3], uint32_t& top) {
-  top = max(top, max(__float_as_uint(x) & 0x7FFFFFFFu, __float_as_uint(y) & 0x7FFFFFFFu));
-#pragma unroll
-  for (int t = 0; t < 3; ++t) {
-    w[t] = nearest2(x, y);
-    x -= __uint_as_float(w[t] << 16);
-    y -= __uint_as_float(w[t] & 0xFFFF0000u);
-  }
-}
-
-// What an operand's largest magnitude (as bits) says of its parts. From infinity on they do not stand for the values. Nor do
-// they below 2^-86, if there is anything: 2^-24 of the largest value is then less than the 2^-110 from which they are exact.
-enum Flag : uint32_t { kOdd = 1, kSmall = 2, kLarge = 4 };  // an operand is odd, or small in one CTA and large in none
-constexpr uint32_t kSmallest = (127u - 86u) << 23;
-__device__ __forceinline__ uint32_t flag_of(uint32_t top) {
-  return top >= 0x7F800000u ? kOdd : top >= kSmallest ? kLarge : top > 0u ? kSmall : 0u;
-}
 
 // Both operands of a product; flags[CTA]: flag_of what it met. A thread cuts 8 neighbours of a row: 32 bytes in, 3 x 16 out.
 __global__ void __launch_bounds__(256) cut_kernel(const Cut a, const Cut b, int ctas_a, uint32_t* flags) {
@@ -569,12 +542,13 @@ __global__ void __launch_bounds__(256) cut_kernel(const Cut a, const Cut b, int 
   const Cut& c = first ? a : b;
   const int64_t ctas = first ? ctas_a : gridDim.x - ctas_a, cta = first ? blockIdx.x : blockIdx.x - ctas_a;
   const int64_t units = c.ldp / 8, plane = c.rows * c.ldp;
+  const int64_t rows = c.count ? min(c.rows, (*c.count + (int64_t)63) / 64 * 64) : c.rows;
   uint32_t top = 0;
   // a CTA's rows one after another, its threads side by side along a row (a short row's threads share out rows)
   const int wide = (int)(units < 256 ? units : 256), high = 256 / wide;
   const int tx = threadIdx.x % wide, ty = threadIdx.x / wide;
   if (ty < high)
-    for (int64_t r = cta * high + ty; r < c.rows; r += ctas * high)
+    for (int64_t r = cta * high + ty; r < rows; r += ctas * high)
       for (int64_t u = tx; u < units; u += wide) {
         const int64_t at = 8 * u;
         const float* p = c.from + r * c.ld + at;
@@ -606,16 +580,17 @@ struct TcArgs {
   int width;
   int slices, share;  // slices of 64, and those of a CTA of a cluster
   float* parts;       // shares of sums
-  const uint32_t* flags;
-  int flags_a, n_flags;  // those of the first operand that was cut come first
+  const uint32_t *flags_a, *flags_b;
+  int n_flags_a, n_flags;  // of the first operand, of both
   int* errors;
 };
 
 // The six products of a slice, small ones first: (part of the rows' operand, part of the columns')
 __device__ constexpr int kOrder[6][2] = {{2, 0}, {0, 2}, {1, 1}, {1, 0}, {0, 1}, {0, 0}};
 
-// A: the operand of j (the product's b), B: that of i (its a)
-template <bool A_MN, bool B_MN>
+// A: the operand of j (the product's b), B: that of i (its a). COUNTED: the rows i, or of a weight's gradient the terms of the sum,
+// are those that the device counts (p.count).
+template <bool A_MN, bool B_MN, bool COUNTED>
 __global__ void __launch_bounds__(kThreads, 1)
     f32_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                const __grid_constant__ TcArgs a) {
@@ -633,8 +608,18 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint32_t shares, rank;
   asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(shares));
   asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+  int64_t tiles_c = a.tiles_c, tiles = a.tiles, I = p.I, L = p.L;
+  int slices_there = a.slices;
+  if (COUNTED && A_MN && B_MN) {
+    L = min(L, (int64_t)*p.count);
+    slices_there = (int)((L + kBK - 1) / kBK);
+  } else if (COUNTED) {
+    I = min(I, (int64_t)*p.count);
+    tiles_c = (I + a.width - 1) / a.width;
+    tiles = a.tiles_r * tiles_c;
+  }
   const int slice0 = (int)rank * a.share;
-  const int slices = max(0, min(a.share, a.slices - slice0));
+  const int slices = max(0, min(a.share, slices_there - slice0));
   const int64_t first_tile = blockIdx.x / shares, step = gridDim.x / shares;
 
   if (warp == kTmaWarp && lane == 0) {
@@ -659,7 +644,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     fence_before();
   }
   uint32_t met = 0;  // the second operand's flags from bit 8 on
-  for (int i = threadIdx.x; i < a.n_flags; i += kThreads) met |= a.flags[i] << (i < a.flags_a ? 0 : 8);
+  for (int i = threadIdx.x; i < a.n_flags; i += kThreads) met |= i < a.n_flags_a ? a.flags_a[i] : a.flags_b[i - a.n_flags_a] << 8;
   met = __reduce_or_sync(0xFFFFFFFFu, met);
   if (lane == 0) met_here[warp] = met;
   __syncthreads();
@@ -674,12 +659,12 @@ __global__ void __launch_bounds__(kThreads, 1)
     // an operand whose parts do not stand for it: all CTAs make tiles of 128 x 128 on the fp32 units
     if (warp < kEpiWarps) {
       float* sums = reinterpret_cast<float*>(ring);
-      const int64_t ti = (p.I + kBM - 1) / kBM, tj = (p.J + kBN - 1) / kBN;
+      const int64_t ti = (I + kBM - 1) / kBM, tj = (p.J + kBN - 1) / kBN;
       for (int64_t tile = blockIdx.x; tile < ti * tj; tile += gridDim.x) {
         const int64_t i0 = tile % ti * kBM, j0 = tile / ti * kBN;
-        simt_sums<128, B_MN, A_MN>(a.f, sums, i0, j0, 0, p.L);
+        simt_sums<128, B_MN, A_MN>(a.f, sums, i0, j0, 0, L);
         units_sync();
-        for (int row = warp; row < kBM && i0 + row < p.I; row += 8) {
+        for (int row = warp; row < kBM && i0 + row < I; row += 8) {
           const float4 t = *reinterpret_cast<const float4*>(sums + row * kBN + lane * 4);
           float v[4] = {t.x, t.y, t.z, t.w};
           finish4(a.f, i0 + row, j0 + lane * 4, v);
@@ -693,9 +678,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int part_b = B_MN ? blocks_b * 8192 : a.width * kBK * 2;
     uint32_t n = 0;
     bool ok = true;
-    for (int64_t tile = first_tile; ok && tile < a.tiles; tile += step) {
+    for (int64_t tile = first_tile; ok && tile < tiles; tile += step) {
       int64_t tr, tc;
-      tile_place<16>(a.tiles_r, a.tiles_c, tile, tr, tc);
+      tile_place<16>(a.tiles_r, tiles_c, tile, tr, tc);
       const int r0 = (int)(tr * kBM), c0 = (int)(tc * a.width);
       for (int k = 0; k < slices; ++k, ++n) {
         const uint32_t s = n % kStages;
@@ -730,7 +715,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t inst = kInstruction<A_MN, B_MN, 0> | (uint32_t)(a.width >> 3) << 17;
     uint32_t n = 0;
     bool ok = true;
-    for (int64_t tile = first_tile; ok && tile < a.tiles; tile += step)
+    for (int64_t tile = first_tile; ok && tile < tiles; tile += step)
       for (int k = 0; k < slices; ++k, ++n) {
         const uint32_t s = n % kStages, half = n & 1, sums = tmem + half * kSums;
         ok = bar_wait(sums_empty + 8 * half, (n / 2 + 1) & 1, dead, a.errors) &&
@@ -758,9 +743,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int quarter = warp % 4, blocks = a.width / kBlock / 2, first = warp / 4 * blocks;
     uint32_t n = 0;
     bool ok = true;
-    for (int64_t tile = first_tile; ok && tile < a.tiles; tile += step) {
+    for (int64_t tile = first_tile; ok && tile < tiles; tile += step) {
       int64_t tr, tc;
-      tile_place<16>(a.tiles_r, a.tiles_c, tile, tr, tc);
+      tile_place<16>(a.tiles_r, tiles_c, tile, tr, tc);
       float acc[kMostBlocks][kBlock];
 #pragma unroll
       for (int b = 0; b < kMostBlocks; ++b)
@@ -807,9 +792,9 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (shares > 1) {
     __syncthreads();
     cluster_sync();
-    if (!odd && warp < kEpiWarps && !__any_sync(0xFFFFFFFFu, *dead)) {
+    if (!odd && warp < kEpiWarps && first_tile < tiles && !__any_sync(0xFFFFFFFFu, *dead)) {
       int64_t tr, tc;
-      tile_place<16>(a.tiles_r, a.tiles_c, first_tile, tr, tc);
+      tile_place<16>(a.tiles_r, tiles_c, first_tile, tr, tc);
       const int quarter = warp % 4;
       const int64_t j = tr * kBM + 32 * quarter, i0 = tc * a.width;
       const float* part = a.parts + (size_t)first_tile * shares * a.width * kBM + 32 * quarter + lane;
@@ -922,11 +907,11 @@ int cuts_of(int64_t rows, int64_t ldp, int sms) {
   return (int)(ctas < 8 * sms ? (ctas < 1 ? 1 : ctas) : 8 * sms);
 }
 
-template <bool A_MN, bool B_MN>
+template <bool A_MN, bool B_MN, bool COUNTED = false>
 cudaError_t plan_tc(const Product& p, int sms, Plan* plan) {
   static std::atomic<uint64_t> allowed;
   static std::atomic<int> clusters[64][9];
-  auto* f = f32_kernel<A_MN, B_MN>;
+  auto* f = f32_kernel<A_MN, B_MN, COUNTED>;
   const cudaError_t e = allow_shared(f, kTcBytes, allowed);
   if (e != cudaSuccess) return e;
   Plan g = {};
@@ -980,34 +965,42 @@ bool encode_parts(CUtensorMap* map, const void* p, int64_t cols, int64_t rows, i
                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <bool A_MN, bool B_MN>
-cudaError_t launch_tc32(const Product& p, int sms, char* workspace, cudaStream_t s) {
-  Plan g;
-  cudaError_t e = plan_tc<A_MN, B_MN>(p, sms, &g);
-  if (e != cudaSuccess) return e;
+// The product of operands that are cut: a's parts and flags are those of p.b, b's of p.a.
+template <bool A_MN, bool B_MN, bool COUNTED>
+cudaError_t launch_parts(const Product& p, const Plan& g, const Parts& pa, const Parts& pb, float* sums, cudaStream_t s) {
   TcArgs a = {};
-  e = error_word(&a.errors);
+  const cudaError_t e = error_word(&a.errors);
   if (e != cudaSuccess) return e;
   a.f = args_of(p);
-  char *pa = workspace, *pb = pa + g.bytes_a, *pf = pb + g.bytes_b;
-  const Cut ca = {(const float*)p.b, (uint16_t*)pa, g.rows_a, g.cols_a, p.ldb, g.ldp_a, a.f.vb};
-  const Cut cb = {(const float*)p.a, (uint16_t*)pb, g.rows_b, g.cols_b, p.lda, g.ldp_b, a.f.va};
-  a.flags = (const uint32_t*)pf;
-  a.flags_a = g.cuts_a, a.n_flags = g.cuts_a + g.cuts_b;
-  a.parts = (float*)(pf + g.bytes_flags);
+  a.flags_a = pa.flags, a.flags_b = pb.flags;
+  a.n_flags_a = pa.n_flags, a.n_flags = pa.n_flags + pb.n_flags;
+  a.parts = sums;
   a.tiles_r = g.tiles_r, a.tiles_c = g.tiles_c, a.tiles = g.tiles_r * g.tiles_c;
   a.slices = g.slices, a.share = g.share, a.width = g.width;
   CUtensorMap ma, mb;
-  if (!encode_parts(&ma, pa, g.cols_a, g.rows_a, g.ldp_a, A_MN ? kBK : kBM) ||
-      !encode_parts(&mb, pb, g.cols_b, g.rows_b, g.ldp_b, B_MN ? kBK : g.width))
+  if (!encode_parts(&ma, pa.p, g.cols_a, g.rows_a, g.ldp_a, A_MN ? kBK : kBM) ||
+      !encode_parts(&mb, pb.p, g.cols_b, g.rows_b, g.ldp_b, B_MN ? kBK : g.width))
     return cudaErrorNotSupported;
-  cut_kernel<<<g.cuts_a + g.cuts_b, 256, 0, s>>>(ca, cb, g.cuts_a, (uint32_t*)pf);
-  e = cudaGetLastError();
-  if (e != cudaSuccess) return e;
   cudaLaunchAttribute at;
   const cudaLaunchConfig_t cfg =
       config(dim3((unsigned)g.ctas), kThreads, kTcBytes, dim3((unsigned)g.shares, 1, 1), &at, s);
-  return cudaLaunchKernelEx(&cfg, f32_kernel<A_MN, B_MN>, ma, mb, a);
+  return cudaLaunchKernelEx(&cfg, f32_kernel<A_MN, B_MN, COUNTED>, ma, mb, a);
+}
+
+template <bool A_MN, bool B_MN>
+cudaError_t launch_tc32(const Product& p, int sms, char* workspace, cudaStream_t s) {
+  Plan g;
+  const cudaError_t e = plan_tc<A_MN, B_MN>(p, sms, &g);
+  if (e != cudaSuccess) return e;
+  char *pa = workspace, *pb = pa + g.bytes_a, *pf = pb + g.bytes_b;
+  uint32_t* flags = (uint32_t*)pf;
+  const Cut ca = {(const float*)p.b, (uint16_t*)pa, g.rows_a, g.cols_a, p.ldb, g.ldp_a, can(p.b, p.ldb), nullptr};
+  const Cut cb = {(const float*)p.a, (uint16_t*)pb, g.rows_b, g.cols_b, p.lda, g.ldp_b, can(p.a, p.lda), nullptr};
+  cut_kernel<<<g.cuts_a + g.cuts_b, 256, 0, s>>>(ca, cb, g.cuts_a, flags);
+  const cudaError_t f = cudaGetLastError();
+  if (f != cudaSuccess) return f;
+  return launch_parts<A_MN, B_MN, false>(p, g, {pa, flags, g.cuts_a}, {pb, flags + g.cuts_a, g.cuts_b},
+                                         (float*)(pf + g.bytes_flags), s);
 }
 
 // Whether cutting the operands pays: not for few rows (rows_kernel), nor for products that start and end as fast as they
@@ -1042,6 +1035,51 @@ cudaError_t launch_f32(const Product& p, int sms, void* workspace, cudaStream_t 
     return tc ? launch_tc32<true, false>(p, sms, w, s) : launch_simt<false, true>(p, sms, s);
   }
   return tc ? launch_tc32<true, true>(p, sms, w, s) : launch_simt<true, true>(p, sms, s);
+}
+
+bool f32_on_tensor_cores(const Product& p) { return on_tensor_cores(p) && (p.mode == kGradWeight || p.I > kFewRows); }
+
+int64_t parts_ld(int64_t cols) { return (cols + 31) / 32 * 32; }
+size_t parts_bytes(int64_t rows, int64_t cols) { return up((size_t)kParts * (size_t)rows * (size_t)parts_ld(cols) * 2); }
+int parts_flags(int64_t rows, int64_t cols, int sms) { return cuts_of(rows, parts_ld(cols), sms); }
+
+cudaError_t launch_cut(const Uncut& a, const Uncut& b, int sms, cudaStream_t s) {
+  auto job = [](const Uncut& u) {
+    return Cut{u.from, (uint16_t*)u.to.p, u.rows, u.cols, u.ld, parts_ld(u.cols), can(u.from, u.ld), u.count};
+  };
+  // flags of both lie side by side only by chance: a launch for each
+  for (const Uncut* u : {&a, &b}) {
+    if (!u->from) continue;
+    cut_kernel<<<u->to.n_flags, 256, 0, s>>>(job(*u), job(*u), u->to.n_flags, u->to.flags);
+    const cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+  }
+  return cudaSuccess;
+}
+
+cudaError_t f32_parts_workspace(const Product& p, int sms, size_t* bytes) {
+  Plan g = {};
+  const cudaError_t e = p.mode == kForward     ? plan_tc<false, false, true>(p, sms, &g)
+                        : p.mode == kGradInput ? plan_tc<true, false, true>(p, sms, &g)
+                                               : plan_tc<true, true, true>(p, sms, &g);
+  *bytes = e == cudaSuccess ? g.bytes_parts : 0;
+  return e;
+}
+
+cudaError_t launch_f32_parts(const Product& p, const Parts& of_b, const Parts& of_a, int sms, void* workspace, cudaStream_t s) {
+  Plan g;
+  float* sums = (float*)workspace;
+  cudaError_t e;
+  if (p.mode == kForward) {
+    e = plan_tc<false, false, true>(p, sms, &g);
+    return e == cudaSuccess ? launch_parts<false, false, true>(p, g, of_b, of_a, sums, s) : e;
+  }
+  if (p.mode == kGradInput) {
+    e = plan_tc<true, false, true>(p, sms, &g);
+    return e == cudaSuccess ? launch_parts<true, false, true>(p, g, of_b, of_a, sums, s) : e;
+  }
+  e = plan_tc<true, true, true>(p, sms, &g);
+  return e == cudaSuccess ? launch_parts<true, true, true>(p, g, of_b, of_a, sums, s) : e;
 }
 
 }  // namespace lin

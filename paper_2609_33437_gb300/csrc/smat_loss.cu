@@ -70,11 +70,12 @@ __global__ void __launch_bounds__(kScan) index_kernel(const Index a) {
 
 // A CTA per row at a time.
 template <class T, bool VEC>
-__global__ void __launch_bounds__(256) gather_kernel(const Index a, const T* x, int64_t ldx, T* to, int64_t ldto, int64_t k) {
+__global__ void __launch_bounds__(256) gather_kernel(const Index a, const T* x, int64_t ldx, T* to, int64_t ldto, int64_t k,
+                                                     bool to_end) {
   const int there = *a.count;
   const int64_t rows = a.rows;
-  // rows that a product meets behind the last one: up to a whole slice in bf16, all of them in fp32
-  const int64_t slice = sizeof(T) == 2 ? (there + 63) / 64 * 64 : rows, end = slice < rows ? slice : rows;
+  // rows that a product meets behind the last one: up to a whole slice of its sum, or all of them
+  const int64_t slice = to_end ? rows : (there + (int64_t)63) / 64 * 64, end = slice < rows ? slice : rows;
   for (int64_t row = blockIdx.x; row < rows; row += gridDim.x) {
     const int at = a.place[row];
     if (at >= 0) {
@@ -221,6 +222,52 @@ __global__ void __launch_bounds__(256) row_grad_kernel(float* z, int64_t ldz, in
   }
 }
 
+// As cut_kernel of the linear layers: a thread has 8 neighbours of a row.
+__global__ void __launch_bounds__(256) row_grad_cut_kernel(float* z, int64_t ldz, int64_t rows, int64_t cols, int64_t first_col,
+                                                           const LossRow* info, const int* count, uint16_t* parts, int64_t ldp,
+                                                           uint32_t* flags) {
+  __shared__ uint32_t tops[8];
+  const int there = *count;
+  const int64_t slice = (there + (int64_t)63) / 64 * 64, end = slice < rows ? slice : rows, units = ldp / 8, plane = rows * ldp;
+  const int wide = (int)(units < 256 ? units : 256), high = 256 / wide, tx = threadIdx.x % wide, ty = threadIdx.x / wide;
+  uint32_t top = 0;
+  if (ty < high)
+    for (int64_t row = (int64_t)blockIdx.x * high + ty; row < end; row += (int64_t)gridDim.x * high) {
+      const LossRow r = row < there ? info[row] : LossRow{0.0f, 0.0f, -1, 0.0f};
+      const int64_t t = r.target >= 0 ? r.target - first_col : -1;
+      for (int64_t u = tx; u < units; u += wide) {
+        const int64_t at = 8 * u;
+        float* p = z + row * ldz + at;
+        float v[8];
+        // z's rows have room for whole groups of 32
+        *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(p);
+        *reinterpret_cast<float4*>(v + 4) = *reinterpret_cast<const float4*>(p + 4);
+        uint32_t w[3][4];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          v[i] = row < there && at + i < cols ? (expf(v[i] - r.lse) - (at + i == t ? 1.0f : 0.0f)) * r.g : 0.0f;
+        *reinterpret_cast<float4*>(p) = *reinterpret_cast<const float4*>(v);
+        *reinterpret_cast<float4*>(p + 4) = *reinterpret_cast<const float4*>(v + 4);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          uint32_t of[3];
+          lin::cut2(v[2 * i], v[2 * i + 1], of, top);
+          w[0][i] = of[0], w[1][i] = of[1], w[2][i] = of[2];
+        }
+#pragma unroll
+        for (int q = 0; q < 3; ++q)
+          *reinterpret_cast<uint4*>(parts + q * plane + row * ldp + at) = make_uint4(w[q][0], w[q][1], w[q][2], w[q][3]);
+      }
+    }
+  top = __reduce_max_sync(0xFFFFFFFFu, top);
+  if (threadIdx.x % 32 == 0) tops[threadIdx.x / 32] = top;
+  __syncthreads();
+  if (threadIdx.x < 8) {
+    top = __reduce_max_sync(0xFFu, tops[threadIdx.x]);
+    if (threadIdx.x == 0) flags[blockIdx.x] = lin::flag_of(top);
+  }
+}
+
 __global__ void __launch_bounds__(256) add_kernel(float* to, const float* from, int64_t ld, int64_t rows, int64_t cols) {
   for (int64_t row = blockIdx.x; row < rows; row += gridDim.x)
     for (int64_t j = threadIdx.x; j < cols; j += 256) to[row * ld + j] += from[row * ld + j];
@@ -235,14 +282,14 @@ cudaError_t launch_index(const Index& a, cudaStream_t s) {
   return cudaGetLastError();
 }
 
-cudaError_t launch_gather(const Index& a, const void* x, int64_t ldx, void* to, int64_t ldto, int64_t k, int dtype, int sms,
-                          cudaStream_t s) {
+cudaError_t launch_gather(const Index& a, const void* x, int64_t ldx, void* to, int64_t ldto, int64_t k, int dtype, bool to_end,
+                          int sms, cudaStream_t s) {
   const int elem = dtype == SMAT_BF16 ? 2 : 4;
   const bool vec = (uintptr_t)x % 16 == 0 && (a.rows == 1 || ldx * elem % 16 == 0);
   const unsigned ctas = row_ctas(a.rows, sms);
   auto go = [&](auto t, auto v) {
     using T = decltype(t);
-    gather_kernel<T, decltype(v)::value><<<ctas, 256, 0, s>>>(a, (const T*)x, ldx, (T*)to, ldto, k);
+    gather_kernel<T, decltype(v)::value><<<ctas, 256, 0, s>>>(a, (const T*)x, ldx, (T*)to, ldto, k, to_end);
     return cudaGetLastError();
   };
   if (dtype == SMAT_BF16) return vec ? go(bf16(), std::true_type()) : go(bf16(), std::false_type());
@@ -282,6 +329,13 @@ cudaError_t launch_row_grad(float* z, int64_t ldz, int64_t rows, int64_t cols, i
   const int64_t wide = (cols + 1023) / 1024, high = 8 * (int64_t)sms / wide + 1;
   row_grad_kernel<<<dim3((unsigned)wide, (unsigned)(rows < high ? rows : high)), 256, 0, s>>>(z, ldz, rows, cols, first_col,
                                                                                              info, count);
+  return cudaGetLastError();
+}
+
+cudaError_t launch_row_grad_cut(float* z, int64_t ldz, int64_t rows, int64_t cols, int64_t first_col, const LossRow* info,
+                                const int* count, const lin::Parts& parts, cudaStream_t s) {
+  row_grad_cut_kernel<<<parts.n_flags, 256, 0, s>>>(z, ldz, rows, cols, first_col, info, count, (uint16_t*)parts.p,
+                                                    lin::parts_ld(cols), parts.flags);
   return cudaGetLastError();
 }
 

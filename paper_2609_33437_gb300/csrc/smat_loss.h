@@ -38,10 +38,10 @@ struct Index {
   int* count;
 };
 cudaError_t launch_index(const Index& a, cudaStream_t s);
-// x's rows that count and their info, at their places; rows of zeros behind them up to the next multiple of 64 (bf16) or to the end
-// (fp32).
-cudaError_t launch_gather(const Index& a, const void* x, int64_t ldx, void* to, int64_t ldto, int64_t k, int dtype, int sms,
-                          cudaStream_t s);
+// x's rows that count and their info, at their places; rows of zeros behind them up to the next multiple of 64, or to the
+// end.
+cudaError_t launch_gather(const Index& a, const void* x, int64_t ldx, void* to, int64_t ldto, int64_t k, int dtype, bool to_end,
+                          int sms, cudaStream_t s);
 // dx from sums at the rows' places; 0 for a row that has none.
 cudaError_t launch_scatter(const float* from, int64_t ldfrom, const int* place, void* dx, int64_t lddx, int64_t rows, int64_t k,
                            int dtype, int sms, cudaStream_t s);
@@ -61,6 +61,10 @@ cudaError_t launch_row_part(const float* z, int64_t ldz, int64_t rows, int64_t c
                             float2* part, float* picked, int sms, cudaStream_t s);
 cudaError_t launch_row_grad(float* z, int64_t ldz, int64_t rows, int64_t cols, int64_t first_col, const LossRow* info,
                             const int* count, int sms, cudaStream_t s);
+// The same for rows that count, and those behind them up to a multiple of 64, with the gradient's parts for the tensor cores beside
+// it (flags: one of each CTA, parts.n_flags of them).
+cudaError_t launch_row_grad_cut(float* z, int64_t ldz, int64_t rows, int64_t cols, int64_t first_col, const LossRow* info,
+                                const int* count, const lin::Parts& parts, cudaStream_t s);
 // to += from, [rows, cols] both, row stride ld
 cudaError_t launch_add(float* to, const float* from, int64_t ld, int64_t rows, int64_t cols, int sms, cudaStream_t s);
 

@@ -199,7 +199,8 @@ smat_status forward(const smat_token_loss_args* a, void* d_workspace, size_t wor
 struct GradPlan {
   Operand w;
   int64_t piece;
-  size_t count, place, info, x, d, sums, more, wcopy, parts, bytes;
+  bool cut;  // fp32: the products share operands that are cut for the tensor cores
+  size_t count, place, info, x, d, sums, more, wcopy, cut_x, cut_w, cut_d, parts, bytes;
 };
 
 // The three products of a piece.
@@ -230,11 +231,30 @@ smat_status plan(const smat_token_loss_grad_args* a, int sms, GradPlan* out) {
   g.more = s.take(a->dx && !bf && pieces > 1 ? copy_bytes(m, k, 4) : 0);
   g.wcopy = s.take(g.w.copied ? copy_bytes(g.piece, k, 2) : 0);
   size_t parts = 0;
+  g.cut = !bf;
   for (int64_t cols : {g.piece, last}) {
     Product p[3];
     products(a, cols, p);
-    for (int i = 0; i < 3; ++i)
-      if (i == 0 || (i == 1 ? a->dx : a->dw)) parts = std::max(parts, product_bytes(p[i], sms));
+    for (const Product& q : p) g.cut = g.cut && f32_on_tensor_cores(q);
+  }
+  for (int64_t cols : {g.piece, last}) {
+    Product p[3];
+    products(a, cols, p);
+    for (int i = 0; i < 3; ++i) {
+      if (i > 0 && !(i == 1 ? a->dx : a->dw)) continue;
+      size_t bytes = 0;
+      if (!g.cut)
+        bytes = product_bytes(p[i], sms);
+      else if (f32_parts_workspace(p[i], sms, &bytes) != cudaSuccess)
+        bytes = 0;
+      parts = std::max(parts, bytes);
+    }
+  }
+  if (g.cut) {
+    auto cut = [&](int64_t rows, int64_t cols) {
+      return s.take(parts_bytes(rows, cols) + up(sizeof(uint32_t) * (size_t)parts_flags(rows, cols, sms)));
+    };
+    g.cut_x = cut(m, k), g.cut_w = cut(g.piece, k), g.cut_d = cut(m, g.piece);
   }
   g.parts = s.take(parts);
   g.bytes = s.at;
@@ -280,7 +300,10 @@ smat_status backward(const smat_token_loss_grad_args* a, void* d_workspace, size
   float *sums = (float*)(ws + f.sums), *more = (float*)(ws + f.more);
   const loss::Index index = {a->targets, a->g, a->lse, m, n, a->ignore, place, info, count};
   cudaError_t e = loss::launch_index(index, s);
-  if (e == cudaSuccess) e = loss::launch_gather(index, a->x, a->ldx, ws + f.x, ldk, k, a->dtype, sms, s);
+  if (e == cudaSuccess) e = loss::launch_gather(index, a->x, a->ldx, ws + f.x, ldk, k, a->dtype, !bf && !f.cut, sms, s);
+  auto parts_at = [&](size_t at, int64_t rows, int64_t cols) {
+    return Parts{ws + at, (uint32_t*)(ws + at + parts_bytes(rows, cols)), parts_flags(rows, cols, sms)};
+  };
   for (int64_t c = 0; e == cudaSuccess && c < n; c += f.piece) {
     const int64_t cols = std::min(f.piece, n - c);
     Rows w;
@@ -294,6 +317,17 @@ smat_status backward(const smat_token_loss_grad_args* a, void* d_workspace, size
     p[1].out = bf || c == 0 ? sums : more, p[1].accumulate = bf && c > 0;
     p[2].a = ws + f.d, p[2].lda = ldd, p[2].b = ws + f.x, p[2].ldb = ldk, p[2].ldo = a->lddw, p[2].accumulate = a->accumulate;
     p[2].out = a->dw ? (char*)a->dw + (size_t)c * (size_t)a->lddw * es : nullptr;
+    if (f.cut) {
+      const Parts px = parts_at(f.cut_x, m, k), pw = parts_at(f.cut_w, cols, k), pd = parts_at(f.cut_d, m, cols);
+      const Uncut rows = {c == 0 ? (const float*)(ws + f.x) : nullptr, m, k, ldk, count, px};
+      e = launch_cut(rows, {(const float*)w.p, cols, k, w.ld, nullptr, pw}, sms, s);
+      if (e == cudaSuccess) e = launch_f32_parts(p[0], pw, px, sms, ws + f.parts, s);
+      if (e == cudaSuccess) e = loss::launch_row_grad_cut((float*)(ws + f.d), ldd, m, cols, c, info, count, pd, s);
+      if (e == cudaSuccess && a->dx) e = launch_f32_parts(p[1], pw, pd, sms, ws + f.parts, s);
+      if (e == cudaSuccess && a->dx && c > 0) e = loss::launch_add(sums, more, ldk, m, k, sms, s);
+      if (e == cudaSuccess && a->dw) e = launch_f32_parts(p[2], px, pd, sms, ws + f.parts, s);
+      continue;
+    }
     e = launch_product(p[0], sms, ws + f.parts, s);
     if (e == cudaSuccess && !bf) e = loss::launch_row_grad((float*)(ws + f.d), ldd, m, cols, c, info, count, sms, s);
     if (e == cudaSuccess && a->dx) e = launch_product(p[1], sms, ws + f.parts, s);
