@@ -1,11 +1,11 @@
 // Layer norm and rms norm, forward and backward (include/smat.h, "norms").
 //
-// A row is held in registers by a group of warps, E values a thread, so that it is read once: its mean, then the squares of
-// what is left (both sums in fp32, over lanes and then warps in a fixed order), then the result. The groups walk over the
-// rows with the weights in registers and the next row's loads under way. Backward the columns a thread holds are the same for
-// every row, so it adds up dw and db for them as it goes; every CTA leaves its sums in the workspace, and a second launch
-// adds those in the CTAs' order: no atomics, the same bits every time. Rows of more than kMaxCols columns are read three
-// times by a CTA each (the later times mostly from L2).
+// A row is held in registers by some lanes of a warp, a warp or several, E values a thread, so that it is read once: its mean,
+// then the squares of what is left (both sums in fp32, over lanes and then warps in a fixed order), then the result. The threads
+// walk over the rows with the next row's loads under way. Backward the columns a thread holds are the same for every row, so it
+// adds up dw and db for them as it goes; every CTA leaves its sums in the workspace, and a second launch adds those in the CTAs'
+// order: no atomics, the same bits every time. Rows of more than kMaxCols columns are read three times by a CTA each (the later
+// times mostly from L2).
 
 #include "smat_norm.h"
 
@@ -23,7 +23,8 @@ using bf16 = __nv_bfloat16;
 
 constexpr int kMaxWarps = 32, kMaxCols = 16384;
 
-// VEC neighbours as they lie in memory
+// VEC neighbours as they lie in memory. (Pairs of bf16 are taken apart and made as whole words: element by element a row of 4,096
+// took 39 instructions a value, and they bound it.)
 template <class T, int VEC>
 struct Raw {
   static constexpr int kBytes = VEC * (int)sizeof(T);
@@ -32,32 +33,88 @@ struct Raw {
   Word u;
   __device__ __forceinline__ void load(const T* p) { u = *reinterpret_cast<const Word*>(p); }
   __device__ __forceinline__ void zero() { u = Word{}; }
-  __device__ __forceinline__ float at(int i) const { return to_float(reinterpret_cast<const T*>(&u)[i]); }
-  __device__ __forceinline__ void set(int i, float v) { reinterpret_cast<T*>(&u)[i] = from_float<T>(v); }
+  __device__ __forceinline__ float at(int i) const {
+    if constexpr (sizeof(T) == 4) return reinterpret_cast<const float*>(&u)[i];
+    if constexpr (VEC == 1) return __uint_as_float((uint32_t)u << 16);
+    if constexpr (sizeof(T) == 2 && VEC > 1) {
+      const uint32_t w = reinterpret_cast<const uint32_t*>(&u)[i / 2];
+      return __uint_as_float(i % 2 ? w & 0xFFFF0000u : w << 16);
+    }
+  }
+  __device__ __forceinline__ void set(const float (&v)[VEC]) {
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) reinterpret_cast<float*>(&u)[i] = v[i];
+    } else if constexpr (VEC == 1) {
+      u = __bfloat16_as_ushort(__float2bfloat16_rn(v[0]));
+    } else {
+#pragma unroll
+      for (int i = 0; i < VEC; i += 2) {
+        const __nv_bfloat162 w = __floats2bfloat162_rn(v[i], v[i + 1]);
+        reinterpret_cast<uint32_t*>(&u)[i / 2] = *reinterpret_cast<const uint32_t*>(&w);
+      }
+    }
+  }
   __device__ __forceinline__ void store(T* p) const { *reinterpret_cast<Word*>(p) = u; }
 };
 
-// A vector of weights: its own alignment is any.
+// A vector of weights, from a multiple of VEC on; whole vectors lie on 16 bytes.
 template <class W, int VEC>
 __device__ __forceinline__ void load_weights(const W* p, int64_t at, bool there, float other, float (&v)[VEC]) {
+  constexpr int kWide = 16 / (int)sizeof(W);
 #pragma unroll
-  for (int i = 0; i < VEC; ++i) v[i] = there && p ? to_float(p[at + i]) : other;
+  for (int i = 0; i < VEC; ++i) v[i] = other;
+  if (!p || !there) return;
+  if constexpr (VEC % kWide == 0) {
+#pragma unroll
+    for (int i = 0; i < VEC; i += kWide) {
+      Raw<W, kWide> u;
+      u.load(p + at + i);
+#pragma unroll
+      for (int j = 0; j < kWide; ++j) v[i + j] = u.at(j);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) v[i] = to_float(p[at + i]);
+  }
 }
 
-__device__ __forceinline__ float warp_sum(float v) {
+// Weights as they lie in registers: bf16 in pairs
+template <class W, int E>
+struct Weights {
+  float v[E];
+  __device__ __forceinline__ void set(int i, float x) { v[i] = x; }
+  __device__ __forceinline__ float at(int i) const { return v[i]; }
+};
+template <int E>
+struct Weights<bf16, E> {
+  uint32_t v[E / 2];
+  __device__ __forceinline__ void set(int i, float x) {
+    const uint32_t u = __float_as_uint(x) >> 16;  // a bf16 number's
+    v[i / 2] = i % 2 ? v[i / 2] | u << 16 : u;
+  }
+  __device__ __forceinline__ float at(int i) const { return __uint_as_float(i % 2 ? v[i / 2] & 0xFFFF0000u : v[i / 2] << 16); }
+};
+
+// over `width` neighbouring lanes, a power of two
+__device__ __forceinline__ float lane_sum(float v, int width) {
 #pragma unroll
-  for (int d = 16; d > 0; d /= 2) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
+  for (int d = 16; d > 0; d /= 2) {
+    const float other = __shfl_xor_sync(0xFFFFFFFFu, v, d);
+    v += d < width ? other : 0.0f;
+  }
   return v;
 }
 
-// N sums over a row's warps. `space`: [rows of the CTA][warps][N], another one than the last call's: a thread that writes to
-// the last call's place has passed this call's barrier, and so has everybody who read it.
+// N sums over a row's threads: less than a warp, or whole ones. `space`: [rows of the CTA][warps][N], another one than the last
+// call's: a thread that writes to the last call's place has passed this call's barrier, and so has everybody who read it.
 template <int N>
 __device__ __forceinline__ void row_sums(float (&v)[N], float* space) {
+  const int width = blockDim.x < 32 ? blockDim.x : 32;
 #pragma unroll
-  for (int n = 0; n < N; ++n) v[n] = warp_sum(v[n]);
+  for (int n = 0; n < N; ++n) v[n] = lane_sum(v[n], width);
   const int warps = blockDim.x / 32;
-  if (warps == 1) return;
+  if (warps <= 1) return;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   float* mine = space + (size_t)threadIdx.y * warps * N;
   if (lane == 0)
@@ -65,12 +122,12 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float* space) {
     for (int n = 0; n < N; ++n) mine[warp * N + n] = v[n];
   __syncthreads();
 #pragma unroll
-  for (int n = 0; n < N; ++n) v[n] = warp_sum(lane < warps ? mine[lane * N + n] : 0.0f);
+  for (int n = 0; n < N; ++n) v[n] = lane_sum(lane < warps ? mine[lane * N + n] : 0.0f, 32);
 }
 
 // CTA: blockDim.y rows at a time, blockDim.x threads each.
-template <class T, class W, int VEC, int E>
-__global__ void __launch_bounds__(32 * kMaxWarps) forward_kernel(const Forward a) {
+template <class T, class W, int VEC, int E, int THREADS>
+__global__ void __launch_bounds__(THREADS, E == 32 ? 2 : 1024 / THREADS) forward_kernel(const Forward a) {
   constexpr int C = E / VEC;
   __shared__ float space[2][kMaxWarps];
   const int64_t step = (int64_t)gridDim.x * blockDim.y;
@@ -106,8 +163,10 @@ __global__ void __launch_bounds__(32 * kMaxWarps) forward_kernel(const Forward a
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       if (a.r) {
+        float sum[VEC];
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) x[c].set(i, x[c].at(i) + r[c].at(i));
+        for (int i = 0; i < VEC; ++i) sum[i] = x[c].at(i) + r[c].at(i);
+        x[c].set(sum);
         if (there && in[c]) x[c].store((T*)a.h + row * a.ldh + at(c));
       }
 #pragma unroll
@@ -123,7 +182,11 @@ __global__ void __launch_bounds__(32 * kMaxWarps) forward_kernel(const Forward a
       turn ^= 1;
       mean = sum[0] * per;
 #pragma unroll
-      for (int i = 0; i < E; ++i) v[i] = in[i / VEC] ? v[i] - mean : 0.0f;
+      for (int c = 0; c < C; ++c) {
+        const float less = in[c] ? mean : 0.0f;  // columns that are not there hold 0
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) v[c * VEC + i] -= less;
+      }
     }
     float sq[1] = {0.0f};
 #pragma unroll
@@ -142,9 +205,11 @@ __global__ void __launch_bounds__(32 * kMaxWarps) forward_kernel(const Forward a
       float w[VEC], b[VEC];
       load_weights<W, VEC>((const W*)a.w, at(c), true, 1.0f, w);
       load_weights<W, VEC>((const W*)a.b, at(c), true, 0.0f, b);
-      Raw<T, VEC> y;
+      float out[VEC];
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) y.set(i, fmaf(v[c * VEC + i] * inv, w[i], b[i]));
+      for (int i = 0; i < VEC; ++i) out[i] = fmaf(v[c * VEC + i] * inv, w[i], b[i]);
+      Raw<T, VEC> y;
+      y.set(out);
       y.store((T*)a.y + row * a.ldy + at(c));
     }
   }
@@ -189,55 +254,73 @@ __global__ void __launch_bounds__(1024) forward_long_kernel(const Forward a) {
   }
 }
 
-// A CTA takes every gridDim.x'th set of blockDim.y rows. THREADS: the most it has.
-template <class T, class W, int VEC, int E, int THREADS>
-__global__ void __launch_bounds__(THREADS) backward_kernel(const Backward a) {
+// A CTA takes every gridDim.x'th set of blockDim.y rows. THREADS: the most it has, CTAS: how many are to share an SM; AHEAD: the
+// next rows' loads are under way while a row is worked on.
+template <class T, class W, int VEC, int E, int THREADS, int CTAS, bool AHEAD>
+__global__ void __launch_bounds__(THREADS, CTAS) backward_kernel(const Backward a) {
   constexpr int C = E / VEC;
   __shared__ float space[2][2 * kMaxWarps];
   extern __shared__ float sums[];  // [2][cols], where several rows' threads of the CTA meet at the end
   const int64_t step = (int64_t)gridDim.x * blockDim.y;
   const float per = 1.0f / (float)a.cols;
+  const bool add = a.dh && a.dx;
   float dw[E], db[E];
-#pragma unroll
-  for (int i = 0; i < E; ++i) dw[i] = db[i] = 0.0f;
+  Weights<W, E> w;
   bool in[C];
-#pragma unroll
-  for (int c = 0; c < C; ++c) in[c] = (int64_t)(c * blockDim.x + threadIdx.x) * VEC < a.cols;
   auto at = [&](int c) { return (int64_t)(c * blockDim.x + threadIdx.x) * VEC; };
-  int turn = 0;
-  for (int64_t first = (int64_t)blockIdx.x * blockDim.y; first < a.rows; first += step, turn ^= 1) {
-    const int64_t row = first + threadIdx.y;
-    const bool there = row < a.rows;
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    in[c] = at(c) < a.cols;
+    float v[VEC];
+    load_weights<W, VEC>((const W*)a.w, at(c), in[c], 1.0f, v);
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) {
+      w.set(c * VEC + i, v[i]);
+      dw[c * VEC + i] = db[c * VEC + i] = 0.0f;
+    }
+  }
+  struct Row {
     Raw<T, VEC> h[C], dy[C], dh[C];
+    float mean, inv;
+  };
+  auto fetch = [&](int64_t row) {
+    Row r;
+    const bool there = row < a.rows;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
+      r.h[c].zero(), r.dy[c].zero(), r.dh[c].zero();
       if (there && in[c]) {
-        h[c].load((const T*)a.h + row * a.ldh + at(c));
-        dy[c].load((const T*)a.dy + row * a.lddy + at(c));
-        if (a.dh && a.dx) dh[c].load((const T*)a.dh + row * a.lddh + at(c));
-      } else {
-        h[c].zero();
-        dy[c].zero();
+        r.h[c].load((const T*)a.h + row * a.ldh + at(c));
+        r.dy[c].load((const T*)a.dy + row * a.lddy + at(c));
+        if (add) r.dh[c].load((const T*)a.dh + row * a.lddh + at(c));
       }
     }
-    const float mean = there && !a.rms ? a.stats[row] : 0.0f;
-    const float inv = there ? a.stats[(a.rms ? 0 : a.rows) + row] : 0.0f;
+    r.mean = there && !a.rms ? a.stats[row] : 0.0f;
+    r.inv = there ? a.stats[(a.rms ? 0 : a.rows) + row] : 0.0f;
+    return r;
+  };
+  int turn = 0;
+  int64_t row = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
+  Row next;
+  if (AHEAD) next = fetch(row);
+  for (int64_t first = (int64_t)blockIdx.x * blockDim.y; first < a.rows; first += step, row += step, turn ^= 1) {
+    const bool there = row < a.rows;
+    const Row r = AHEAD ? next : fetch(row);
+    if (AHEAD) next = fetch(row + step);
+    // of a row that is not there, or a column, dy is 0, and with it all that is added up
+    auto xh = [&](int c, int i) { return (r.h[c].at(i) - r.mean) * r.inv; };
+    auto g = [&](int c, int i) { return r.dy[c].at(i) * w.at(c * VEC + i); };
     float s[2] = {0.0f, 0.0f};
-    float xh[E], g[E];
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      float w[VEC];
-      load_weights<W, VEC>((const W*)a.w, at(c), in[c], 1.0f, w);
 #pragma unroll
       for (int i = 0; i < VEC; ++i) {
         const int e = c * VEC + i;
-        const float d = dy[c].at(i);
-        xh[e] = there && in[c] ? (h[c].at(i) - mean) * inv : 0.0f;
-        g[e] = d * w[i];
-        dw[e] = fmaf(d, xh[e], dw[e]);
+        const float d = r.dy[c].at(i), x = xh(c, i);
+        dw[e] = fmaf(d, x, dw[e]);
         db[e] += d;
-        s[0] = fmaf(g[e], xh[e], s[0]);
-        s[1] += g[e];
+        s[0] = fmaf(g(c, i), x, s[0]);
+        s[1] += g(c, i);
       }
     }
     if (!a.dx) continue;
@@ -247,52 +330,64 @@ __global__ void __launch_bounds__(THREADS) backward_kernel(const Backward a) {
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       if (!in[c]) continue;
-      Raw<T, VEC> dx;
+      float out[VEC];
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) {
-        const int e = c * VEC + i;
-        float v = (g[e] - off - xh[e] * by) * inv;
-        if (a.dh) v += dh[c].at(i);
-        dx.set(i, v);
+      for (int i = 0; i < VEC; ++i) out[i] = fmaf(-by, xh(c, i), g(c, i) - off) * r.inv;
+      if (add) {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) out[i] += r.dh[c].at(i);
       }
+      Raw<T, VEC> dx;
+      dx.set(out);
       dx.store((T*)a.dx + row * a.lddx + at(c));
     }
   }
   if (!a.dw && !a.db) return;
-  // the CTA's sums: its rows' threads in turn
-  if (blockDim.y > 1) {
-    for (int t = 0; t < (int)blockDim.y; ++t) {
-      if ((int)threadIdx.y == t) {
+  // the CTA's sums: rows' lanes of a warp first, then what is left in turn
+  const bool narrow = blockDim.x < 32;
+  const int thread = threadIdx.y * blockDim.x + threadIdx.x;
+  if (narrow) {
 #pragma unroll
-        for (int c = 0; c < C; ++c)
-          if (in[c])
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-              const int e = c * VEC + i;
-              float* p = sums + at(c) + i;
-              if (t > 0) dw[e] += p[0], db[e] += p[a.cols];
-              p[0] = dw[e];
-              p[a.cols] = db[e];
-            }
+    for (int e = 0; e < E; ++e)
+      for (int d = blockDim.x; d < 32; d *= 2) {
+        dw[e] += __shfl_xor_sync(0xFFFFFFFFu, dw[e], d);
+        db[e] += __shfl_xor_sync(0xFFFFFFFFu, db[e], d);
       }
-      __syncthreads();
-    }
   }
-  if (threadIdx.y == blockDim.y - 1) {
-    float* to = a.parts + (size_t)blockIdx.x * ((a.dw != nullptr) + (a.db != nullptr)) * a.cols;
+  const int turns = narrow ? (int)(blockDim.x * blockDim.y / 32) : (int)blockDim.y, mine = narrow ? thread / 32 : (int)threadIdx.y;
+  const bool takes_part = !narrow || thread % 32 < (int)blockDim.x;
+  for (int t = 0; t < turns - 1; ++t) {
+    if (mine == t && takes_part) {
 #pragma unroll
-    for (int c = 0; c < C; ++c)
-      if (in[c])
+      for (int c = 0; c < C; ++c)
+        if (in[c])
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-          float* p = to + at(c) + i;
-          if (a.dw) {
-            *p = dw[c * VEC + i];
-            p += a.cols;
+          for (int i = 0; i < VEC; ++i) {
+            const int e = c * VEC + i;
+            float* p = sums + at(c) + i;
+            if (t > 0) dw[e] += p[0], db[e] += p[a.cols];
+            p[0] = dw[e];
+            p[a.cols] = db[e];
           }
-          if (a.db) *p = db[c * VEC + i];
-        }
+    }
+    __syncthreads();
   }
+  if (mine != turns - 1 || !takes_part) return;
+  float* to = a.parts + (size_t)blockIdx.x * ((a.dw != nullptr) + (a.db != nullptr)) * a.cols;
+#pragma unroll
+  for (int c = 0; c < C; ++c)
+    if (in[c])
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        const int e = c * VEC + i;
+        const float* q = sums + at(c) + i;
+        float* p = to + at(c) + i;
+        if (a.dw) {
+          *p = turns > 1 ? dw[e] + q[0] : dw[e];
+          p += a.cols;
+        }
+        if (a.db) *p = turns > 1 ? db[e] + q[a.cols] : db[e];
+      }
 }
 
 // Any number of columns: dx by a CTA per row at a time ...
@@ -362,15 +457,21 @@ __global__ void __launch_bounds__(1024) join_kernel(const Backward a) {
   out[at] = from_float<W>(a.accumulate ? to_float(out[at]) + v : v);
 }
 
+// CTAs per SM of backward_kernel for short rows
+template <class T>
+constexpr int kShortCtas = sizeof(T) == 2 ? 3 : 2;
+
 bool on(const void* p, int64_t ld, int64_t rows, int elem, int bytes) {
   return !p || ((uintptr_t)p % bytes == 0 && (rows <= 1 || (uint64_t)ld * elem % bytes == 0));
 }
 
-// Threads of a row, rows of a CTA.
+// Threads of a row (some of a warp's lanes or whole warps), rows of a CTA.
 dim3 block_of(int64_t cols, int per_thread, int threads) {
-  const int warps = (int)((cols + 32 * per_thread - 1) / (32 * per_thread));
-  const int rows = threads / (32 * warps);
-  return dim3(32 * warps, rows > 1 ? rows : 1);
+  const int64_t needed = (cols + per_thread - 1) / per_thread;
+  int wide = 4;
+  while (wide < 32 && wide < needed) wide *= 2;
+  if (needed > 32) wide = (int)((needed + 31) / 32 * 32);
+  return dim3(wide, threads / wide > 1 ? threads / wide : 1);
 }
 
 // Runs f with a type and a vector: f(T, W, integral_constant VEC)
@@ -396,7 +497,8 @@ cudaError_t launch_forward(const Forward& a, int dtype, int weight_dtype, int sm
     return a.cols * elem % bytes == 0 && on(a.x, a.ldx, a.rows, elem, bytes) && on(a.r, a.ldr, a.rows, elem, bytes) &&
            on(a.h, a.ldh, a.rows, elem, bytes) && on(a.y, a.ldy, a.rows, elem, bytes);
   };
-  const int bytes = all_on(16) ? 16 : all_on(4) ? 4 : 2;
+  const bool weights_on = ((uintptr_t)a.w | (uintptr_t)a.b) % 16 == 0;
+  const int bytes = weights_on && all_on(16) ? 16 : all_on(4) ? 4 : 2;
   return with_types(dtype, weight_dtype, bytes, [&](auto t, auto w, auto vec) {
     using T = decltype(t);
     using W = decltype(w);
@@ -406,35 +508,43 @@ cudaError_t launch_forward(const Forward& a, int dtype, int weight_dtype, int sm
       forward_long_kernel<T, W><<<(unsigned)ctas, 1024, 0, s>>>(a);
       return cudaGetLastError();
     }
-    auto go = [&](auto e) {
-      constexpr int E = decltype(e)::value;
+    auto go = [&](auto e, auto threads) {
+      constexpr int E = decltype(e)::value, THREADS = decltype(threads)::value;
       const dim3 block = block_of(a.cols, E, 256);
       const int64_t sets = (a.rows + block.y - 1) / block.y;
-      const int64_t room = (int64_t)sms * (2048 / (block.x * block.y) / 2 > 0 ? 2048 / (block.x * block.y) / 2 : 1);
-      forward_kernel<T, W, VEC, E><<<(unsigned)(sets < room ? sets : room), block, 0, s>>>(a);
+      const int64_t room = (int64_t)sms * (E == 32 ? 3 : 1024 / THREADS);
+      forward_kernel<T, W, VEC, E, THREADS><<<(unsigned)(sets < room ? sets : room), block, 0, s>>>(a);
       return cudaGetLastError();
     };
-    if (a.cols <= 2048) return go(std::integral_constant<int, 8>());
-    return go(std::integral_constant<int, 16>());
+    using std::integral_constant;
+    if constexpr (VEC * sizeof(T) == 16) {
+      // a warp per row, which then meets nobody
+      if (a.cols > 512 && a.cols <= 1024 && a.rows >= 4 * sms) return go(integral_constant<int, 32>(), integral_constant<int, 256>());
+    }
+    if (a.cols <= 256 || (a.cols <= 2048 && a.cols > 512) || a.rows < 4 * sms && a.cols <= 2048)
+      return go(integral_constant<int, 8>(), integral_constant<int, 256>());
+    if (a.cols <= 4096) return go(integral_constant<int, 16>(), integral_constant<int, 256>());
+    if (a.cols <= 8192) return go(integral_constant<int, 16>(), integral_constant<int, 512>());
+    return go(integral_constant<int, 16>(), integral_constant<int, 1024>());
   });
 }
 
-int backward_shares(int64_t rows, int64_t cols, int sms) {
+int backward_shares(int64_t rows, int64_t cols, int dtype, int sms) {
   if (cols > kMaxCols) return (int)(rows < 16 ? rows : 16);
   const dim3 block = block_of(cols, cols <= 2048 ? 8 : 16, 256);
-  const int64_t sets = (rows + block.y - 1) / block.y, room = 2 * (int64_t)sms;
+  const int64_t sets = (rows + block.y - 1) / block.y, room = (cols <= 2048 ? (dtype == SMAT_BF16 ? kShortCtas<bf16> : kShortCtas<float>) : cols <= 4096 ? 2 : 1) * (int64_t)sms;
   return (int)(sets < room ? sets : room);
 }
 
 cudaError_t launch_backward(const Backward& given, int dtype, int weight_dtype, int sms, cudaStream_t s) {
   Backward a = given;
-  a.shares = backward_shares(a.rows, a.cols, sms);
+  a.shares = backward_shares(a.rows, a.cols, dtype, sms);
   const int elem = dtype == SMAT_BF16 ? 2 : 4, wanted = (a.dw != nullptr) + (a.db != nullptr);
   auto all_on = [&](int bytes) {
     return a.cols * elem % bytes == 0 && on(a.dy, a.lddy, a.rows, elem, bytes) && on(a.h, a.ldh, a.rows, elem, bytes) &&
            on(a.dh, a.lddh, a.rows, elem, bytes) && on(a.dx, a.lddx, a.rows, elem, bytes);
   };
-  const int bytes = all_on(16) ? 16 : all_on(4) ? 4 : 2;
+  const int bytes = (uintptr_t)a.w % 16 == 0 && all_on(16) ? 16 : all_on(4) ? 4 : 2;
   return with_types(dtype, weight_dtype, bytes, [&](auto t, auto w, auto vec) {
     using T = decltype(t);
     using W = decltype(w);
@@ -452,19 +562,26 @@ cudaError_t launch_backward(const Backward& given, int dtype, int weight_dtype, 
         e = cudaGetLastError();
       }
     } else if (a.rows > 0) {
-      auto go = [&](auto e, auto threads) {
-        constexpr int E = decltype(e)::value, THREADS = decltype(threads)::value;
+      auto go = [&](auto e, auto threads, auto ctas, auto ahead) {
+        constexpr int E = decltype(e)::value, THREADS = decltype(threads)::value, CTAS = decltype(ctas)::value;
         const dim3 block = block_of(a.cols, E, 256);
         const size_t bytes = block.y > 1 && wanted ? 2 * (size_t)a.cols * sizeof(float) : 0;
-        backward_kernel<T, W, VEC, E, THREADS><<<a.shares, block, bytes, s>>>(a);
+        backward_kernel<T, W, VEC, E, THREADS, CTAS, decltype(ahead)::value><<<a.shares, block, bytes, s>>>(a);
         return cudaGetLastError();
       };
+      using std::integral_constant;
+      // registers for the next rows' loads: rows in whole vectors, of fp32 with 8 values a thread
+      constexpr bool kVec = VEC * sizeof(T) == 16;
       if (a.cols <= 2048)
-        e = go(std::integral_constant<int, 8>(), std::integral_constant<int, 256>());
+        e = go(integral_constant<int, 8>(), integral_constant<int, 256>(), integral_constant<int, kShortCtas<T>>(), std::true_type());
+      else if (a.cols <= 4096)
+        e = go(integral_constant<int, 16>(), integral_constant<int, 256>(), integral_constant<int, 2>(),
+               std::integral_constant<bool, kVec && sizeof(T) == 2>());
       else if (a.cols <= 8192)
-        e = go(std::integral_constant<int, 16>(), std::integral_constant<int, 512>());
+        e = go(integral_constant<int, 16>(), integral_constant<int, 512>(), integral_constant<int, 1>(),
+               std::integral_constant<bool, kVec && sizeof(T) == 2>());
       else
-        e = go(std::integral_constant<int, 16>(), std::integral_constant<int, 1024>());
+        e = go(integral_constant<int, 16>(), integral_constant<int, 1024>(), integral_constant<int, 1>(), std::false_type());
     }
     if (e != cudaSuccess || !wanted) return e;
     join_kernel<W><<<(unsigned)((wanted * a.cols + 31) / 32), dim3(32, 32), 0, s>>>(a);

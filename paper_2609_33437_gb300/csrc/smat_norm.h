@@ -40,7 +40,7 @@ struct Backward {
 
 cudaError_t launch_forward(const Forward& a, int dtype, int weight_dtype, int sms, cudaStream_t s);
 // The shares of the rows that a weight's gradient is summed in: a call's workspace is shares * wanted * cols floats.
-int backward_shares(int64_t rows, int64_t cols, int sms);
+int backward_shares(int64_t rows, int64_t cols, int dtype, int sms);
 cudaError_t launch_backward(const Backward& a, int dtype, int weight_dtype, int sms, cudaStream_t s);
 
 }  // namespace norm

@@ -58,7 +58,7 @@ size_t grad_bytes(const smat_norm_grad_args* a, int* shares) {
   int sms = 0;
   *shares = 0;
   if (a->rows == 0 || (!a->dw && !a->db) || device_sms(&sms) != SMAT_OK) return 0;
-  *shares = norm::backward_shares(a->rows, a->cols, sms);
+  *shares = norm::backward_shares(a->rows, a->cols, a->dtype, sms);
   return up((size_t)*shares * ((a->dw != nullptr) + (a->db != nullptr)) * (size_t)a->cols * sizeof(float));
 }
 
