@@ -125,29 +125,93 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float* space) {
   for (int n = 0; n < N; ++n) v[n] = lane_sum(lane < warps ? mine[lane * N + n] : 0.0f, 32);
 }
 
+// The columns that a thread holds, C vectors of VEC. SHIFT: rows do not all start on 16 bytes, but those of all matrices lie alike.
+// Vectors are those of memory then, of which a row's first starts before it by as much as the row's address is past 16 bytes, and
+// the same for all the rows of a thread, which are a multiple of 16 / sizeof(T) apart. Of a vector that reaches out of the row
+// what is outside counts as 0, and only what is inside is written.
+template <class T, int VEC, int C, bool SHIFT>
+struct Columns {
+  // (in 32 bits a shifted row is faster, 4099 x 1023 19 us and not 33; a whole one in 64 bits, 8192 x 4096 in fp32 84 and not 110)
+  using Place = std::conditional_t<SHIFT, int, int64_t>;
+  Place cols, before;
+  bool in[C], inside[C];  // the vector meets the row; lies in it
+  // first: the thread's first row's place in memory, of any of the matrices
+  __device__ __forceinline__ Columns(int64_t n, const void* base, int64_t first)
+      : cols((Place)n), before(SHIFT ? (Place)(((uintptr_t)base + (uint64_t)first * sizeof(T)) % 16 / sizeof(T)) : 0) {
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      in[c] = at(c) < cols && (!SHIFT || at(c) + VEC > 0);
+      inside[c] = !SHIFT || (at(c) >= 0 && at(c) + VEC <= cols);
+    }
+  }
+  __device__ __forceinline__ Place at(int c) const {
+    const Place first = (Place)(c * blockDim.x + threadIdx.x) * VEC;
+    return SHIFT ? first - before : first;
+  }
+  __device__ __forceinline__ bool has(int c, int i) const { return !SHIFT || (at(c) + i >= 0 && at(c) + i < cols); }
+  __device__ __forceinline__ bool whole(int c) const { return inside[c]; }
+  __device__ __forceinline__ void load(Raw<T, VEC>& v, const T* row, int c) const {
+    v.load(row + at(c));
+    if (SHIFT && !whole(c)) {
+      float x[VEC];
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) x[i] = has(c, i) ? v.at(i) : 0.0f;
+      v.set(x);
+    }
+  }
+  __device__ __forceinline__ void store(const Raw<T, VEC>& v, T* row, int c) const {
+    if (whole(c)) {
+      v.store(row + at(c));
+    } else {
+#pragma unroll
+      for (int i = 0; i < VEC; ++i)
+        if (has(c, i)) row[at(c) + i] = from_float<T>(v.at(i));
+    }
+  }
+  template <class W>
+  __device__ __forceinline__ void weights(const W* p, int c, float other, float (&v)[VEC]) const {
+    if (!SHIFT) {
+      load_weights<W, VEC>(p, at(c), in[c], other, v);
+    } else {
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) v[i] = p && has(c, i) ? to_float(p[at(c) + i]) : other;
+    }
+  }
+};
+
 // CTA: blockDim.y rows at a time, blockDim.x threads each.
-template <class T, class W, int VEC, int E, int THREADS>
-__global__ void __launch_bounds__(THREADS, E == 32 ? 2 : 1024 / THREADS) forward_kernel(const Forward a) {
+template <class T, class W, int VEC, int E, int THREADS, bool SHIFT>
+__global__ void __launch_bounds__(THREADS, E == 32 || SHIFT ? 512 / THREADS + (THREADS > 512) : 1024 / THREADS)
+    forward_kernel(const Forward a) {
   constexpr int C = E / VEC;
   __shared__ float space[2][kMaxWarps];
   const int64_t step = (int64_t)gridDim.x * blockDim.y;
   const float per = 1.0f / (float)a.cols;
   Raw<T, VEC> x[C], r[C];
-  bool in[C];
+  const Columns<T, VEC, C, SHIFT> own(a.cols, a.x, ((int64_t)blockIdx.x * blockDim.y + threadIdx.y) * a.ldx);
+  const bool(&in)[C] = own.in;
+  Weights<W, E> ws, bs;  // SHIFT: a thread's weights lie off every boundary; it keeps them
+  if (SHIFT) {
 #pragma unroll
-  for (int c = 0; c < C; ++c) in[c] = (int64_t)(c * blockDim.x + threadIdx.x) * VEC < a.cols;
-  auto at = [&](int c) { return (int64_t)(c * blockDim.x + threadIdx.x) * VEC; };
+    for (int c = 0; c < C; ++c) {
+      float w[VEC], b[VEC];
+      own.weights((const W*)a.w, c, 1.0f, w);
+      own.weights((const W*)a.b, c, 0.0f, b);
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) ws.set(c * VEC + i, w[i]), bs.set(c * VEC + i, b[i]);
+    }
+  }
   auto fetch = [&](int64_t row) {
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       const bool there = in[c] && row < a.rows;
       if (there)
-        x[c].load((const T*)a.x + row * a.ldx + at(c));
+        own.load(x[c], (const T*)a.x + row * a.ldx, c);
       else
         x[c].zero();
       if (a.r) {
         if (there)
-          r[c].load((const T*)a.r + row * a.ldr + at(c));
+          own.load(r[c], (const T*)a.r + row * a.ldr, c);
         else
           r[c].zero();
       }
@@ -167,7 +231,7 @@ __global__ void __launch_bounds__(THREADS, E == 32 ? 2 : 1024 / THREADS) forward
 #pragma unroll
         for (int i = 0; i < VEC; ++i) sum[i] = x[c].at(i) + r[c].at(i);
         x[c].set(sum);
-        if (there && in[c]) x[c].store((T*)a.h + row * a.ldh + at(c));
+        if (there && in[c]) own.store(x[c], (T*)a.h + row * a.ldh, c);
       }
 #pragma unroll
       for (int i = 0; i < VEC; ++i) v[c * VEC + i] = x[c].at(i);
@@ -186,6 +250,10 @@ __global__ void __launch_bounds__(THREADS, E == 32 ? 2 : 1024 / THREADS) forward
         const float less = in[c] ? mean : 0.0f;  // columns that are not there hold 0
 #pragma unroll
         for (int i = 0; i < VEC; ++i) v[c * VEC + i] -= less;
+        if (SHIFT && !own.whole(c)) {
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) v[c * VEC + i] = own.has(c, i) ? v[c * VEC + i] : 0.0f;
+        }
       }
     }
     float sq[1] = {0.0f};
@@ -203,14 +271,19 @@ __global__ void __launch_bounds__(THREADS, E == 32 ? 2 : 1024 / THREADS) forward
     for (int c = 0; c < C; ++c) {
       if (!in[c]) continue;
       float w[VEC], b[VEC];
-      load_weights<W, VEC>((const W*)a.w, at(c), true, 1.0f, w);
-      load_weights<W, VEC>((const W*)a.b, at(c), true, 0.0f, b);
+      if (SHIFT) {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) w[i] = ws.at(c * VEC + i), b[i] = bs.at(c * VEC + i);
+      } else {
+        own.weights((const W*)a.w, c, 1.0f, w);
+        own.weights((const W*)a.b, c, 0.0f, b);
+      }
       float out[VEC];
 #pragma unroll
       for (int i = 0; i < VEC; ++i) out[i] = fmaf(v[c * VEC + i] * inv, w[i], b[i]);
       Raw<T, VEC> y;
       y.set(out);
-      y.store((T*)a.y + row * a.ldy + at(c));
+      own.store(y, (T*)a.y + row * a.ldy, c);
     }
   }
 }
@@ -256,7 +329,7 @@ __global__ void __launch_bounds__(1024) forward_long_kernel(const Forward a) {
 
 // A CTA takes every gridDim.x'th set of blockDim.y rows. THREADS: the most it has, CTAS: how many are to share an SM; AHEAD: the
 // next rows' loads are under way while a row is worked on.
-template <class T, class W, int VEC, int E, int THREADS, int CTAS, bool AHEAD>
+template <class T, class W, int VEC, int E, int THREADS, int CTAS, bool AHEAD, bool SHIFT>
 __global__ void __launch_bounds__(THREADS, CTAS) backward_kernel(const Backward a) {
   constexpr int C = E / VEC;
   __shared__ float space[2][2 * kMaxWarps];
@@ -266,13 +339,12 @@ __global__ void __launch_bounds__(THREADS, CTAS) backward_kernel(const Backward 
   const bool add = a.dh && a.dx;
   float dw[E], db[E];
   Weights<W, E> w;
-  bool in[C];
-  auto at = [&](int c) { return (int64_t)(c * blockDim.x + threadIdx.x) * VEC; };
+  const Columns<T, VEC, C, SHIFT> own(a.cols, a.dy, ((int64_t)blockIdx.x * blockDim.y + threadIdx.y) * a.lddy);
+  const bool(&in)[C] = own.in;
 #pragma unroll
   for (int c = 0; c < C; ++c) {
-    in[c] = at(c) < a.cols;
     float v[VEC];
-    load_weights<W, VEC>((const W*)a.w, at(c), in[c], 1.0f, v);
+    own.weights((const W*)a.w, c, 1.0f, v);
 #pragma unroll
     for (int i = 0; i < VEC; ++i) {
       w.set(c * VEC + i, v[i]);
@@ -290,9 +362,9 @@ __global__ void __launch_bounds__(THREADS, CTAS) backward_kernel(const Backward 
     for (int c = 0; c < C; ++c) {
       r.h[c].zero(), r.dy[c].zero(), r.dh[c].zero();
       if (there && in[c]) {
-        r.h[c].load((const T*)a.h + row * a.ldh + at(c));
-        r.dy[c].load((const T*)a.dy + row * a.lddy + at(c));
-        if (add) r.dh[c].load((const T*)a.dh + row * a.lddh + at(c));
+        own.load(r.h[c], (const T*)a.h + row * a.ldh, c);
+        own.load(r.dy[c], (const T*)a.dy + row * a.lddy, c);
+        if (add) own.load(r.dh[c], (const T*)a.dh + row * a.lddh, c);
       }
     }
     r.mean = there && !a.rms ? a.stats[row] : 0.0f;
@@ -339,12 +411,12 @@ __global__ void __launch_bounds__(THREADS, CTAS) backward_kernel(const Backward 
       }
       Raw<T, VEC> dx;
       dx.set(out);
-      dx.store((T*)a.dx + row * a.lddx + at(c));
+      own.store(dx, (T*)a.dx + row * a.lddx, c);
     }
   }
   if (!a.dw && !a.db) return;
-  // the CTA's sums: rows' lanes of a warp first, then what is left in turn
-  const bool narrow = blockDim.x < 32;
+  // the CTA's sums: rows' lanes of a warp first (where they hold the same columns), then what is left in turn
+  const bool narrow = !SHIFT && blockDim.x < 32;
   const int thread = threadIdx.y * blockDim.x + threadIdx.x;
   if (narrow) {
 #pragma unroll
@@ -364,7 +436,8 @@ __global__ void __launch_bounds__(THREADS, CTAS) backward_kernel(const Backward 
 #pragma unroll
           for (int i = 0; i < VEC; ++i) {
             const int e = c * VEC + i;
-            float* p = sums + at(c) + i;
+            float* p = sums + own.at(c) + i;
+            if (!own.has(c, i)) continue;
             if (t > 0) dw[e] += p[0], db[e] += p[a.cols];
             p[0] = dw[e];
             p[a.cols] = db[e];
@@ -380,8 +453,9 @@ __global__ void __launch_bounds__(THREADS, CTAS) backward_kernel(const Backward 
 #pragma unroll
       for (int i = 0; i < VEC; ++i) {
         const int e = c * VEC + i;
-        const float* q = sums + at(c) + i;
-        float* p = to + at(c) + i;
+        const float* q = sums + own.at(c) + i;
+        float* p = to + own.at(c) + i;
+        if (!own.has(c, i)) continue;
         if (a.dw) {
           *p = turns > 1 ? dw[e] + q[0] : dw[e];
           p += a.cols;
@@ -445,6 +519,7 @@ __global__ void __launch_bounds__(1024) join_kernel(const Backward a) {
   const int64_t width = wanted * a.cols, j = (int64_t)blockIdx.x * 32 + threadIdx.x;
   float v = 0.0f;
   if (j < width)
+#pragma unroll 4
     for (int s = threadIdx.y; s < a.shares; s += 32) v += a.parts[(size_t)s * width + j];
   space[threadIdx.y][threadIdx.x] = v;
   __syncthreads();
@@ -457,14 +532,6 @@ __global__ void __launch_bounds__(1024) join_kernel(const Backward a) {
   out[at] = from_float<W>(a.accumulate ? to_float(out[at]) + v : v);
 }
 
-// CTAs per SM of backward_kernel for short rows
-template <class T>
-constexpr int kShortCtas = sizeof(T) == 2 ? 3 : 2;
-
-bool on(const void* p, int64_t ld, int64_t rows, int elem, int bytes) {
-  return !p || ((uintptr_t)p % bytes == 0 && (rows <= 1 || (uint64_t)ld * elem % bytes == 0));
-}
-
 // Threads of a row (some of a warp's lanes or whole warps), rows of a CTA.
 dim3 block_of(int64_t cols, int per_thread, int threads) {
   const int64_t needed = (cols + per_thread - 1) / per_thread;
@@ -474,83 +541,129 @@ dim3 block_of(int64_t cols, int per_thread, int threads) {
   return dim3(wide, threads / wide > 1 ? threads / wide : 1);
 }
 
-// Runs f with a type and a vector: f(T, W, integral_constant VEC)
+// How rows are read: whole vectors from 16 bytes on, vectors of memory that a row starts inside of, or element by element. The
+// second pays in bf16 (4099 x 1023 and 4095, layer norm with residual 19 and 82 us, element by element 25 and 112; back with dh 32
+// and 93, 36 and 145), in fp32 back through long rows alone (4095: 125 and 166; 1023: 45 and 21; forward 4095: 127 and 109).
+enum Way { kWhole, kShifted, kSingly };
+
+// Runs f with types, a vector and whether rows are shifted: f(T, W, integral_constant VEC, bool_constant SHIFT)
 template <class T, class W, class F>
-cudaError_t with_vec(int bytes, F&& f) {
+cudaError_t with_vec(Way way, F&& f) {
   constexpr int kWide = 16 / (int)sizeof(T);
-  if (bytes == 16) return f(T(), W(), std::integral_constant<int, kWide>());
-  if (bytes == 4 && sizeof(T) == 2) return f(T(), W(), std::integral_constant<int, 2>());
-  return f(T(), W(), std::integral_constant<int, 1>());
+  if (way == kWhole) return f(T(), W(), std::integral_constant<int, kWide>(), std::false_type());
+  if (way == kShifted) return f(T(), W(), std::integral_constant<int, kWide>(), std::true_type());
+  return f(T(), W(), std::integral_constant<int, 1>(), std::false_type());
 }
 template <class F>
-cudaError_t with_types(int dtype, int weight_dtype, int bytes, F&& f) {
-  if (dtype == SMAT_F32) return with_vec<float, float>(bytes, f);
-  if (weight_dtype == SMAT_F32) return with_vec<bf16, float>(bytes, f);
-  return with_vec<bf16, bf16>(bytes, f);
+cudaError_t with_types(int dtype, int weight_dtype, Way way, F&& f) {
+  if (dtype == SMAT_F32) return with_vec<float, float>(way, f);
+  if (weight_dtype == SMAT_F32) return with_vec<bf16, float>(way, f);
+  return with_vec<bf16, bf16>(way, f);
 }
+
+// Matrices of a call, those that are there
+struct Lie {
+  int elem;
+  int64_t rows, cols;
+  bool whole = true, alike = true;
+  uintptr_t start = 0, stride = 0;
+  bool any = false;
+  Lie(int dtype, int64_t m, int64_t n) : elem(dtype == SMAT_BF16 ? 2 : 4), rows(m), cols(n) { whole = n * elem % 16 == 0; }
+  Lie& add(const void* p, int64_t ld) {
+    if (!p) return *this;
+    const uintptr_t at = (uintptr_t)p % 16, by = rows > 1 ? (uint64_t)ld * elem % 16 : 0;
+    whole = whole && at == 0 && by == 0;
+    alike = alike && (!any || (at == start && by == stride));
+    start = at, stride = by, any = true;
+    return *this;
+  }
+  // `pays`: whether shifted rows are faster than single elements
+  Way way(const void* w, const void* b, bool pays) const {
+    if (whole && ((uintptr_t)w | (uintptr_t)b) % 16 == 0) return kWhole;
+    return alike && pays ? kShifted : kSingly;
+  }
+};
+
+// A grid whose rows of a thread lie alike: their distance is a multiple of 16 / elem rows.
+int64_t whole_steps(int64_t ctas) { return (ctas + 7) / 8 * 8; }
 
 }  // namespace
 
 cudaError_t launch_forward(const Forward& a, int dtype, int weight_dtype, int sms, cudaStream_t s) {
-  const int elem = dtype == SMAT_BF16 ? 2 : 4;
-  auto all_on = [&](int bytes) {
-    return a.cols * elem % bytes == 0 && on(a.x, a.ldx, a.rows, elem, bytes) && on(a.r, a.ldr, a.rows, elem, bytes) &&
-           on(a.h, a.ldh, a.rows, elem, bytes) && on(a.y, a.ldy, a.rows, elem, bytes);
-  };
-  const bool weights_on = ((uintptr_t)a.w | (uintptr_t)a.b) % 16 == 0;
-  const int bytes = weights_on && all_on(16) ? 16 : all_on(4) ? 4 : 2;
-  return with_types(dtype, weight_dtype, bytes, [&](auto t, auto w, auto vec) {
+  const Way way = Lie(dtype, a.rows, a.cols).add(a.x, a.ldx).add(a.r, a.ldr).add(a.h, a.ldh).add(a.y, a.ldy).way(a.w, a.b, dtype == SMAT_BF16);
+  return with_types(dtype, weight_dtype, way, [&](auto t, auto w, auto vec, auto shift) {
     using T = decltype(t);
     using W = decltype(w);
     constexpr int VEC = decltype(vec)::value;
-    if (a.cols > kMaxCols) {
+    constexpr bool SHIFT = decltype(shift)::value;
+    const int64_t cols = a.cols + (SHIFT ? VEC - 1 : 0);  // with those before a row's first
+    if (cols > kMaxCols) {
       const int64_t ctas = a.rows < 2 * sms ? a.rows : 2 * sms;
       forward_long_kernel<T, W><<<(unsigned)ctas, 1024, 0, s>>>(a);
       return cudaGetLastError();
     }
     auto go = [&](auto e, auto threads) {
       constexpr int E = decltype(e)::value, THREADS = decltype(threads)::value;
-      const dim3 block = block_of(a.cols, E, 256);
+      const dim3 block = block_of(cols, E, 256);
       const int64_t sets = (a.rows + block.y - 1) / block.y;
-      const int64_t room = (int64_t)sms * (E == 32 ? 3 : 1024 / THREADS);
-      forward_kernel<T, W, VEC, E, THREADS><<<(unsigned)(sets < room ? sets : room), block, 0, s>>>(a);
+      const int64_t room = (int64_t)sms * (E == 32 ? 3 : 1024 / THREADS), ctas = sets < room ? sets : room;
+      forward_kernel<T, W, VEC, E, THREADS, SHIFT><<<(unsigned)(SHIFT ? whole_steps(ctas) : ctas), block, 0, s>>>(a);
       return cudaGetLastError();
     };
     using std::integral_constant;
-    if constexpr (VEC * sizeof(T) == 16) {
+    if constexpr (VEC * sizeof(T) == 16 && !SHIFT) {
       // a warp per row, which then meets nobody
-      if (a.cols > 512 && a.cols <= 1024 && a.rows >= 4 * sms) return go(integral_constant<int, 32>(), integral_constant<int, 256>());
+      if (cols > 512 && cols <= 1024 && a.rows >= 4 * sms) return go(integral_constant<int, 32>(), integral_constant<int, 256>());
     }
-    if (a.cols <= 256 || (a.cols <= 2048 && a.cols > 512) || a.rows < 4 * sms && a.cols <= 2048)
+    if (cols <= 256 || (cols <= 2048 && (cols > 512 || a.rows < 4 * sms)))
       return go(integral_constant<int, 8>(), integral_constant<int, 256>());
-    if (a.cols <= 4096) return go(integral_constant<int, 16>(), integral_constant<int, 256>());
-    if (a.cols <= 8192) return go(integral_constant<int, 16>(), integral_constant<int, 512>());
+    if (cols <= 4096) return go(integral_constant<int, 16>(), integral_constant<int, 256>());
+    if (cols <= 8192) return go(integral_constant<int, 16>(), integral_constant<int, 512>());
     return go(integral_constant<int, 16>(), integral_constant<int, 1024>());
   });
 }
 
+// Values a thread, most threads and CTAs per SM of backward_kernel for so many columns.
+struct Shape {
+  int each, threads, ctas;
+};
+// What was measured (layer norm with dh, us, memory would take): bf16 8223 x 1024 with 8 values 22, with 32 (a warp per row) 24, 10;
+// 8192 x 4096 with 16 values 69, with 32 77, with 8 (512 threads) 71, 40; 2048 x 11008 with 16 values (1,024 threads, whose 64
+// registers do not hold them) 102, with 32 64, 27. fp32 8223 x 1024 with 8 values 21, 20; 8192 x 4096 with 16 88, 79.
+Shape shape_of(int64_t cols, bool f32) {
+  if (cols <= 2048) return {8, 256, f32 ? 2 : 3};
+  if (cols <= 4096) return {16, 256, 2};
+  if (cols <= 8192) return {16, 512, 1};
+  if (f32) return {16, 1024, 1};
+  return cols <= 12288 ? Shape{32, 384, 1} : Shape{32, 512, 1};
+}
+
 int backward_shares(int64_t rows, int64_t cols, int dtype, int sms) {
   if (cols > kMaxCols) return (int)(rows < 16 ? rows : 16);
-  const dim3 block = block_of(cols, cols <= 2048 ? 8 : 16, 256);
-  const int64_t sets = (rows + block.y - 1) / block.y, room = (cols <= 2048 ? (dtype == SMAT_BF16 ? kShortCtas<bf16> : kShortCtas<float>) : cols <= 4096 ? 2 : 1) * (int64_t)sms;
-  return (int)(sets < room ? sets : room);
+  const Shape shape = shape_of(cols, dtype == SMAT_F32);
+  const dim3 block = block_of(cols, shape.each, 256);
+  const int64_t sets = (rows + block.y - 1) / block.y, room = shape.ctas * (int64_t)sms;
+  return (int)whole_steps(sets < room ? sets : room);
 }
 
 cudaError_t launch_backward(const Backward& given, int dtype, int weight_dtype, int sms, cudaStream_t s) {
   Backward a = given;
   a.shares = backward_shares(a.rows, a.cols, dtype, sms);
-  const int elem = dtype == SMAT_BF16 ? 2 : 4, wanted = (a.dw != nullptr) + (a.db != nullptr);
-  auto all_on = [&](int bytes) {
-    return a.cols * elem % bytes == 0 && on(a.dy, a.lddy, a.rows, elem, bytes) && on(a.h, a.ldh, a.rows, elem, bytes) &&
-           on(a.dh, a.lddh, a.rows, elem, bytes) && on(a.dx, a.lddx, a.rows, elem, bytes);
-  };
-  const int bytes = (uintptr_t)a.w % 16 == 0 && all_on(16) ? 16 : all_on(4) ? 4 : 2;
-  return with_types(dtype, weight_dtype, bytes, [&](auto t, auto w, auto vec) {
+  const int wanted = (a.dw != nullptr) + (a.db != nullptr);
+  const Way way = Lie(dtype, a.rows, a.cols)
+                      .add(a.dy, a.lddy)
+                      .add(a.h, a.ldh)
+                      .add(a.dx ? a.dh : nullptr, a.lddh)
+                      .add(a.dx, a.lddx)
+                      .way(a.w, nullptr, dtype == SMAT_BF16 || a.cols > 2048);
+  return with_types(dtype, weight_dtype, way, [&](auto t, auto w, auto vec, auto shift) {
     using T = decltype(t);
     using W = decltype(w);
     constexpr int VEC = decltype(vec)::value;
+    constexpr bool SHIFT = decltype(shift)::value;
     cudaError_t e = cudaSuccess;
-    if (a.rows > 0 && a.cols > kMaxCols) {
+    const int64_t cols = a.cols + (SHIFT ? VEC - 1 : 0);  // with those before a row's first
+    if (a.rows > 0 && cols > kMaxCols) {
       if (a.dx) {
         const int64_t ctas = a.rows < 2 * sms ? a.rows : 2 * sms;
         backward_long_kernel<T, W><<<(unsigned)ctas, 1024, 0, s>>>(a);
@@ -562,26 +675,29 @@ cudaError_t launch_backward(const Backward& given, int dtype, int weight_dtype, 
         e = cudaGetLastError();
       }
     } else if (a.rows > 0) {
-      auto go = [&](auto e, auto threads, auto ctas, auto ahead) {
+      const Shape shape = shape_of(cols, sizeof(T) == 4);
+      const dim3 block = block_of(cols, shape.each, 256);
+      const size_t bytes = block.y > 1 && wanted ? 2 * (size_t)a.cols * sizeof(float) : 0;
+      // registers for the next rows' loads: rows in whole vectors, 8 values a thread or 16 in bf16
+      constexpr bool kVec = VEC * sizeof(T) == 16;
+      auto go = [&](auto e, auto threads, auto ctas) {
         constexpr int E = decltype(e)::value, THREADS = decltype(threads)::value, CTAS = decltype(ctas)::value;
-        const dim3 block = block_of(a.cols, E, 256);
-        const size_t bytes = block.y > 1 && wanted ? 2 * (size_t)a.cols * sizeof(float) : 0;
-        backward_kernel<T, W, VEC, E, THREADS, CTAS, decltype(ahead)::value><<<a.shares, block, bytes, s>>>(a);
+        backward_kernel<T, W, VEC, E, THREADS, CTAS, kVec && (E == 8 || (E == 16 && sizeof(T) == 2)), SHIFT><<<a.shares, block, bytes, s>>>(a);
         return cudaGetLastError();
       };
       using std::integral_constant;
-      // registers for the next rows' loads: rows in whole vectors, of fp32 with 8 values a thread
-      constexpr bool kVec = VEC * sizeof(T) == 16;
-      if (a.cols <= 2048)
-        e = go(integral_constant<int, 8>(), integral_constant<int, 256>(), integral_constant<int, kShortCtas<T>>(), std::true_type());
-      else if (a.cols <= 4096)
-        e = go(integral_constant<int, 16>(), integral_constant<int, 256>(), integral_constant<int, 2>(),
-               std::integral_constant<bool, kVec && sizeof(T) == 2>());
-      else if (a.cols <= 8192)
-        e = go(integral_constant<int, 16>(), integral_constant<int, 512>(), integral_constant<int, 1>(),
-               std::integral_constant<bool, kVec && sizeof(T) == 2>());
+      if (shape.each == 8)
+        e = go(integral_constant<int, 8>(), integral_constant<int, 256>(), integral_constant<int, sizeof(T) == 4 ? 2 : 3>());
+      else if (shape.threads == 256)
+        e = go(integral_constant<int, 16>(), integral_constant<int, 256>(), integral_constant<int, 2>());
+      else if (shape.threads == 512 && shape.each == 16)
+        e = go(integral_constant<int, 16>(), integral_constant<int, 512>(), integral_constant<int, 1>());
+      else if constexpr (sizeof(T) == 4)
+        e = go(integral_constant<int, 16>(), integral_constant<int, 1024>(), integral_constant<int, 1>());
+      else if (shape.threads == 384)
+        e = go(integral_constant<int, 32>(), integral_constant<int, 384>(), integral_constant<int, 1>());
       else
-        e = go(integral_constant<int, 16>(), integral_constant<int, 1024>(), integral_constant<int, 1>(), std::false_type());
+        e = go(integral_constant<int, 32>(), integral_constant<int, 512>(), integral_constant<int, 1>());
     }
     if (e != cudaSuccess || !wanted) return e;
     join_kernel<W><<<(unsigned)((wanted * a.cols + 31) / 32), dim3(32, 32), 0, s>>>(a);
