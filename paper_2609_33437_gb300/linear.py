@@ -160,6 +160,8 @@ def _vector(name: str, t: torch.Tensor, dtype, device, n: int) -> int:
 # The current stream's handle without a Stream object around it (2.8 us of a small call otherwise).
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
     (lambda index: torch.cuda.current_stream(index).cuda_stream)
+# (the device's number likewise)
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 _functions = {}  # name -> (size query or None, function), as they are first called
 
 
@@ -174,7 +176,7 @@ def _function(name: str):
 def _run(name: str, args: bytes, device):
     """Workspace, then the call, on the tensors' device and the current stream."""
     index = device.index
-    if index != torch.cuda.current_device():
+    if index != _current_device():
         with torch.cuda.device(device):
             return _run(name, args, device)
     size, f = _function(name)
@@ -190,7 +192,7 @@ def _run(name: str, args: bytes, device):
 
 def _call(name: str, device, *args):
     index = device.index
-    if index != torch.cuda.current_device():
+    if index != _current_device():
         with torch.cuda.device(device):
             return _call(name, device, *args)
     st = _function(name)[1](*args, _raw_stream(index))

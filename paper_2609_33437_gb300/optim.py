@@ -10,6 +10,7 @@ the one given. On simulated-loss steps `PeriodicSmat.optimizer_step` takes an Ad
 """
 
 import ctypes
+import operator
 import struct
 from typing import Dict, List, Optional, Sequence, Union
 
@@ -23,6 +24,7 @@ GROUP = 256
 _ADAMW = struct.Struct("@10P6dqQ4i")
 _numel, _contiguous, _get_device, _data_ptr = (torch.Tensor.numel, torch.Tensor.is_contiguous, torch.Tensor.get_device,
                                                torch.Tensor.data_ptr)
+_dtype = operator.attrgetter("dtype")
 
 
 class Moments:
@@ -92,6 +94,13 @@ class Moments:
 
 def _addresses(name: str, ts: Sequence[Optional[torch.Tensor]], sizes: Sequence[int], index: int, optional: bool):
     """(their addresses, their dtype): contiguous tensors of one dtype and these sizes on the device. A None: 0."""
+    try:  # whole lists by functions in C: 24 tensors 4 us, one by one 6.5
+        dts = set(map(_dtype, ts))
+        if (len(dts) == 1 and list(map(_numel, ts)) == sizes and all(map(_contiguous, ts))
+                and set(map(_get_device, ts)) == {index}):
+            return list(map(_data_ptr, ts)), dts.pop()
+    except (TypeError, AttributeError):  # something else than a tensor among them
+        pass
     first = next((t for t in ts if t is not None), None)
     if first is None:
         return [0] * len(ts), None
