@@ -33,7 +33,7 @@ struct LossRow {
   float lse2;  // log2(e) lse
   float g;
   int target;  // or -1
-  float lse;
+  float own;   // fp32: lse; bf16: the target's own gradient, see gather_kernel in smat_loss.cu
 };
 
 // One product: out(i, j) from sum over l of A(i, l) B(j, l), i < I, j < J, l < L. An operand with the sum running

@@ -218,7 +218,7 @@ __device__ __forceinline__ bool finish_block(const Args& a, const CUtensorMap* m
     const int64_t at = row.target - p.first_col - j;  // of the target among the columns
     if (row.target >= 0 && at >= 0 && at < 32) {
 #pragma unroll
-      for (int t = 0; t < 32; ++t) v[t] -= t == at ? row.g : 0.0f;
+      for (int t = 0; t < 32; ++t) v[t] = t == at ? row.own : v[t];
     }
     if (!counts) {  // rows behind the last one: they meet other rows in the weight's gradient
 #pragma unroll

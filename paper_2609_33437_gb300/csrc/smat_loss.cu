@@ -68,10 +68,16 @@ __global__ void __launch_bounds__(kScan) index_kernel(const Index a) {
   if (threadIdx.x == 0) *a.count = before;
 }
 
-// A CTA per row at a time.
+// A CTA per row at a time. VEC: rows of x, and of W in bf16, on 16 bytes.
+//
+// bf16: the target's logit is made here once more, in fp32, and its gradient g (exp(logit - lse) - 1) from it. Where a model is sure
+// of a word the two nearly cancel, and what tensor memory cuts off a sum (2e-5 of a logit of 12) would be a tenth of a percent of
+// the largest gradient there is.
 template <class T, bool VEC>
 __global__ void __launch_bounds__(256) gather_kernel(const Index a, const T* x, int64_t ldx, T* to, int64_t ldto, int64_t k,
                                                      bool to_end) {
+  constexpr int kEach = 16 / (int)sizeof(T);
+  __shared__ float space[8];
   const int there = *a.count;
   const int64_t rows = a.rows;
   // rows that a product meets behind the last one: up to a whole slice of its sum, or all of them
@@ -79,21 +85,43 @@ __global__ void __launch_bounds__(256) gather_kernel(const Index a, const T* x, 
   for (int64_t row = blockIdx.x; row < rows; row += gridDim.x) {
     const int at = a.place[row];
     if (at >= 0) {
-      if (threadIdx.x == 0) {
-        const int64_t t = a.targets[row];
-        const bool good = t >= 0 && t < a.n;
-        const float lse = a.lse[row];
-        a.info[at] = {lse * lin::kLog2e, good ? a.g[row] : __int_as_float(0x7FC00000), good ? (int)t : -1, lse};
-      }
+      const int64_t t = a.targets[row];
+      const bool good = t >= 0 && t < a.n;
       const T* from = x + row * ldx;
+      const T* w = (const T*)a.w + (good ? t : 0) * a.ldw;
       T* p = to + at * ldto;
-      if (VEC) {
-        constexpr int kEach = 16 / (int)sizeof(T);
-        for (int64_t j = threadIdx.x; j < k / kEach; j += 256)
-          reinterpret_cast<uint4*>(p)[j] = reinterpret_cast<const uint4*>(from)[j];
-        for (int64_t j = k / kEach * kEach + threadIdx.x; j < k; j += 256) p[j] = from[j];
-      } else {
-        for (int64_t j = threadIdx.x; j < k; j += 256) p[j] = from[j];
+      float dot = 0.0f;
+      const int64_t whole = VEC ? k / kEach : 0;
+      for (int64_t j = threadIdx.x; j < whole; j += 256) {
+        const uint4 u = reinterpret_cast<const uint4*>(from)[j];
+        reinterpret_cast<uint4*>(p)[j] = u;
+        if (sizeof(T) == 2) {
+          const uint4 v = reinterpret_cast<const uint4*>(w)[j];
+          const uint32_t c[4] = {u.x, u.y, u.z, u.w}, d[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            dot = fmaf(__uint_as_float(c[i] << 16), __uint_as_float(d[i] << 16), dot);
+            dot = fmaf(__uint_as_float(c[i] & 0xFFFF0000u), __uint_as_float(d[i] & 0xFFFF0000u), dot);
+          }
+        }
+      }
+      for (int64_t j = whole * kEach + threadIdx.x; j < k; j += 256) {
+        p[j] = from[j];
+        if (sizeof(T) == 2) dot = fmaf(to_float(from[j]), to_float(w[j]), dot);
+      }
+      if (sizeof(T) == 2) {
+#pragma unroll
+        for (int d = 16; d > 0; d /= 2) dot += __shfl_xor_sync(0xFFFFFFFFu, dot, d);
+        if (threadIdx.x % 32 == 0) space[threadIdx.x / 32] = dot;
+        __syncthreads();
+        dot = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) dot += space[i];
+        __syncthreads();
+      }
+      if (threadIdx.x == 0) {
+        const float lse = a.lse[row], g = good ? a.g[row] : __int_as_float(0x7FC00000);
+        a.info[at] = {lse * lin::kLog2e, g, good ? (int)t : -1, sizeof(T) == 2 ? g * expm1f(dot - lse) : lse};
       }
     }
     if (row >= there && row < end)
@@ -218,7 +246,7 @@ __global__ void __launch_bounds__(256) row_grad_kernel(float* z, int64_t ldz, in
     const int64_t t = r.target >= 0 ? r.target - first_col : -1;
     float* p = z + row * ldz;
     for (int64_t j = (int64_t)blockIdx.x * 256 + threadIdx.x; j < cols; j += (int64_t)gridDim.x * 256)
-      p[j] = row < there ? (expf(p[j] - r.lse) - (j == t ? 1.0f : 0.0f)) * r.g : 0.0f;
+      p[j] = row < there ? (expf(p[j] - r.own) - (j == t ? 1.0f : 0.0f)) * r.g : 0.0f;
   }
 }
 
@@ -245,7 +273,7 @@ __global__ void __launch_bounds__(256) row_grad_cut_kernel(float* z, int64_t ldz
         uint32_t w[3][4];
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-          v[i] = row < there && at + i < cols ? (expf(v[i] - r.lse) - (at + i == t ? 1.0f : 0.0f)) * r.g : 0.0f;
+          v[i] = row < there && at + i < cols ? (expf(v[i] - r.own) - (at + i == t ? 1.0f : 0.0f)) * r.g : 0.0f;
         *reinterpret_cast<float4*>(p) = *reinterpret_cast<const float4*>(v);
         *reinterpret_cast<float4*>(p + 4) = *reinterpret_cast<const float4*>(v + 4);
 #pragma unroll
@@ -285,7 +313,8 @@ cudaError_t launch_index(const Index& a, cudaStream_t s) {
 cudaError_t launch_gather(const Index& a, const void* x, int64_t ldx, void* to, int64_t ldto, int64_t k, int dtype, bool to_end,
                           int sms, cudaStream_t s) {
   const int elem = dtype == SMAT_BF16 ? 2 : 4;
-  const bool vec = (uintptr_t)x % 16 == 0 && (a.rows == 1 || ldx * elem % 16 == 0);
+  const bool vec = (uintptr_t)x % 16 == 0 && (a.rows == 1 || ldx * elem % 16 == 0) &&
+                   (dtype != SMAT_BF16 || ((uintptr_t)a.w % 16 == 0 && (a.n == 1 || a.ldw * elem % 16 == 0)));
   const unsigned ctas = row_ctas(a.rows, sms);
   auto go = [&](auto t, auto v) {
     using T = decltype(t);

@@ -32,6 +32,8 @@ struct Index {
   const int64_t* targets;
   const float* g;
   const float* lse;
+  const void* w;  // as the call has it
+  int64_t ldw;
   int64_t rows, n, ignore;
   int* place;
   LossRow* info;

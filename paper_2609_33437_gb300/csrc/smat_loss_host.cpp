@@ -298,7 +298,7 @@ smat_status backward(const smat_token_loss_grad_args* a, void* d_workspace, size
   LossRow* info = (LossRow*)(ws + f.info);
   const int64_t ldk = ld_of(k), ldd = ld_of(f.piece);
   float *sums = (float*)(ws + f.sums), *more = (float*)(ws + f.more);
-  const loss::Index index = {a->targets, a->g, a->lse, m, n, a->ignore, place, info, count};
+  const loss::Index index = {a->targets, a->g, a->lse, a->w, a->ldw, m, n, a->ignore, place, info, count};
   cudaError_t e = loss::launch_index(index, s);
   if (e == cudaSuccess) e = loss::launch_gather(index, a->x, a->ldx, ws + f.x, ldk, k, a->dtype, !bf && !f.cut, sms, s);
   auto parts_at = [&](size_t at, int64_t rows, int64_t cols) {

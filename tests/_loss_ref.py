@@ -38,6 +38,9 @@ def gradient(g, x, w, targets, lse, ignore):
     counts = targets != ignore
     p = torch.exp(l - lse.double()[:, None])
     hot = torch.zeros_like(p).scatter_(1, torch.where(counts, targets, 0)[:, None], 1.0)
+    if x.dtype == torch.bfloat16:  # the target's own logit is made in fp32
+        mag = (x.double().abs() * w.double()[torch.where(counts, targets, 0)].abs()).sum(1, keepdim=True)
+        err = torch.where(hot > 0, R.sum_error(mag, torch.float32, x.shape[-1]), err)
     gd = torch.where(counts, g.double(), 0.0)[:, None]
     d = torch.where(counts[:, None], gd * (p - hot), 0.0)
     # p: the logit's error, the roundings of its argument, the exponential's units; then the difference and the product; bf16

@@ -194,6 +194,17 @@ def test_nothing(dt):
 
 
 @pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("m,k,n", [(20, 1024, 600), (200, 2048, 4000), (33, 515, 500)])
+def test_rows_that_are_sure(m, k, n, dt):
+    """Where the target has nearly all of the probability its gradient is what is left of two numbers that nearly cancel."""
+    x, w, t, g = _inputs(1, m, k, n, dt, 0.1)
+    lean = 16.0 / (w[t.clamp(min=0)].float() ** 2).sum(1, keepdim=True)
+    x = (0.2 * x.float() + lean * w[t.clamp(min=0)].float()).to(dt)
+    p = torch.exp(-_check(x, w, t, g)[0])[t != IGNORE]
+    assert float(p.min()) > 0.97 and float(p.max()) < 0.99999
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
 def test_options(dt):
     x, w, t, g = _inputs(3, 140, 160, 3000, dt, 0.2)
     _, lse = T.token_loss(x, w, t)
