@@ -602,7 +602,8 @@ smat_status smat_norm_grad(const smat_norm_grad_args* args, void* d_workspace, s
  *
  * x [rows, k] and W [n, k] of one dtype, row-major with row strides; targets int64 [rows]; loss, lse and g fp32 [rows]; dx and
  * dW as x and W. g is the gradient that reaches the losses. Logits, their sums and those of dx and dW are held in fp32; a bf16
- * call multiplies on the tensor cores (as smat_linear says) and rounds d to bf16 before its products with W and x. A target
+ * call multiplies on the tensor cores (as smat_linear says; the sums of lse and loss are made in parts, as near as plain fp32) and
+ * rounds d to bf16 before its products with W and x (of at most 128 rows to two bf16 numbers, 16 bits). A target
  * outside 0 .. n - 1 that is not `ignore` gives a loss of NaN and gradients of NaN. Rows with t_i = ignore have an lse like
  * every row; back, they are left out: what they hold (infinities, NaN) reaches nothing, and their dx is 0. The workspace of the
  * gradient is some 200 MB for pieces of d, and x's rows and dx in fp32; it does not grow with the vocabulary. Results do not

@@ -66,6 +66,7 @@ struct Product {
   const int* count;         // kLogitGrad and on, launch_f32_parts; on the device: how many rows there are, at most I (or L)
   const LossRow* loss_rows; // kLogitGrad: [I]
   int64_t first_col;        // kLogitGrad: the first column's place in the vocabulary
+  int halves;               // kLogitGrad: rows from count / 2 on are what the same rows before them lose by their rounding
 };
 
 // fp32 (smat_linear_f32.cu): any size, stride and alignment. `workspace`: f32_workspace() bytes, which go by mode, I, J

@@ -220,6 +220,10 @@ __device__ __forceinline__ bool finish_block(const Args& a, const CUtensorMap* m
 #pragma unroll
       for (int t = 0; t < 32; ++t) v[t] = t == at ? row.own : v[t];
     }
+    if (p.halves && i + lane >= rows / 2) {
+#pragma unroll
+      for (int t = 0; t < 32; ++t) v[t] -= to_float(from_float<bf16>(v[t]));
+    }
     if (!counts) {  // rows behind the last one: they meet other rows in the weight's gradient
 #pragma unroll
       for (int t = 0; t < 32; ++t) v[t] = 0.0f;

@@ -65,7 +65,7 @@ __global__ void __launch_bounds__(kScan) index_kernel(const Index a) {
     before += all;
     __syncthreads();
   }
-  if (threadIdx.x == 0) *a.count = before;
+  if (threadIdx.x == 0) *a.count = a.twice ? 2 * before : before;
 }
 
 // A CTA per row at a time. VEC: rows of x, and of W in bf16, on 16 bytes.
@@ -79,9 +79,11 @@ __global__ void __launch_bounds__(256) gather_kernel(const Index a, const T* x, 
   constexpr int kEach = 16 / (int)sizeof(T);
   __shared__ float space[8];
   const int there = *a.count;
-  const int64_t rows = a.rows;
+  const int64_t rows = a.rows, room = a.twice ? 2 * rows : rows;
   // rows that a product meets behind the last one: up to a whole slice of its sum, or all of them
-  const int64_t slice = to_end ? rows : (there + (int64_t)63) / 64 * 64, end = slice < rows ? slice : rows;
+  const int64_t slice = to_end ? room : (there + (int64_t)63) / 64 * 64, end = slice < room ? slice : room;
+  for (int64_t behind = there + blockIdx.x; behind < end; behind += gridDim.x)
+    for (int64_t j = threadIdx.x; j < k; j += 256) to[behind * ldto + j] = from_float<T>(0.0f);
   for (int64_t row = blockIdx.x; row < rows; row += gridDim.x) {
     const int at = a.place[row];
     if (at >= 0) {
@@ -90,11 +92,13 @@ __global__ void __launch_bounds__(256) gather_kernel(const Index a, const T* x, 
       const T* from = x + row * ldx;
       const T* w = (const T*)a.w + (good ? t : 0) * a.ldw;
       T* p = to + at * ldto;
+      T* second = a.twice ? to + (at + there / 2) * ldto : p;
       float dot = 0.0f;
       const int64_t whole = VEC ? k / kEach : 0;
       for (int64_t j = threadIdx.x; j < whole; j += 256) {
         const uint4 u = reinterpret_cast<const uint4*>(from)[j];
         reinterpret_cast<uint4*>(p)[j] = u;
+        if (a.twice) reinterpret_cast<uint4*>(second)[j] = u;
         if (sizeof(T) == 2) {
           const uint4 v = reinterpret_cast<const uint4*>(w)[j];
           const uint32_t c[4] = {u.x, u.y, u.z, u.w}, d[4] = {v.x, v.y, v.z, v.w};
@@ -107,6 +111,7 @@ __global__ void __launch_bounds__(256) gather_kernel(const Index a, const T* x, 
       }
       for (int64_t j = whole * kEach + threadIdx.x; j < k; j += 256) {
         p[j] = from[j];
+        if (a.twice) second[j] = from[j];
         if (sizeof(T) == 2) dot = fmaf(to_float(from[j]), to_float(w[j]), dot);
       }
       if (sizeof(T) == 2) {
@@ -121,35 +126,41 @@ __global__ void __launch_bounds__(256) gather_kernel(const Index a, const T* x, 
       }
       if (threadIdx.x == 0) {
         const float lse = a.lse[row], g = good ? a.g[row] : __int_as_float(0x7FC00000);
-        a.info[at] = {lse * lin::kLog2e, g, good ? (int)t : -1, sizeof(T) == 2 ? g * expm1f(dot - lse) : lse};
+        const LossRow r = {lse * lin::kLog2e, g, good ? (int)t : -1, sizeof(T) == 2 ? g * expm1f(dot - lse) : lse};
+        a.info[at] = r;
+        if (a.twice) a.info[at + there / 2] = r;
       }
     }
-    if (row >= there && row < end)
-      for (int64_t j = threadIdx.x; j < k; j += 256) to[row * ldto + j] = from_float<T>(0.0f);
   }
 }
 
 template <class T, bool VEC>
-__global__ void __launch_bounds__(256) scatter_kernel(const float* from, int64_t ldfrom, const int* place, T* dx, int64_t lddx,
-                                                      int64_t rows, int64_t k) {
-  for (int64_t row = blockIdx.x; row < rows; row += gridDim.x) {
-    const int at = place[row];
+__global__ void __launch_bounds__(256) scatter_kernel(const float* from, int64_t ldfrom, const Index a, T* dx, int64_t lddx,
+                                                      int64_t k) {
+  const int64_t half = a.twice ? *a.count / 2 * ldfrom : 0;
+  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    const int at = a.place[row];
     const float* p = from + at * ldfrom;
     T* to = dx + row * lddx;
-    if (VEC) {
-      for (int64_t j = threadIdx.x; j < k / 4; j += 256) {
-        const float4 v = at >= 0 ? __ldcs(reinterpret_cast<const float4*>(p) + j) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        if constexpr (sizeof(T) == 2) {
-          const __nv_bfloat162 lo = __floats2bfloat162_rn(v.x, v.y), hi = __floats2bfloat162_rn(v.z, v.w);
-          reinterpret_cast<uint2*>(to)[j] = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
-        } else {
-          reinterpret_cast<float4*>(to)[j] = v;
+    const int64_t whole = VEC ? k / 4 : 0;
+    for (int64_t j = threadIdx.x; j < whole; j += 256) {
+      float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      if (at >= 0) {
+        v = __ldcs(reinterpret_cast<const float4*>(p) + j);
+        if (half) {
+          const float4 w = __ldcs(reinterpret_cast<const float4*>(p + half) + j);
+          v.x += w.x, v.y += w.y, v.z += w.z, v.w += w.w;
         }
       }
-      for (int64_t j = k / 4 * 4 + threadIdx.x; j < k; j += 256) to[j] = from_float<T>(at >= 0 ? p[j] : 0.0f);
-    } else {
-      for (int64_t j = threadIdx.x; j < k; j += 256) to[j] = from_float<T>(at >= 0 ? p[j] : 0.0f);
+      if constexpr (sizeof(T) == 2) {
+        const __nv_bfloat162 lo = __floats2bfloat162_rn(v.x, v.y), hi = __floats2bfloat162_rn(v.z, v.w);
+        reinterpret_cast<uint2*>(to)[j] = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+      } else {
+        reinterpret_cast<float4*>(to)[j] = v;
+      }
     }
+    for (int64_t j = 4 * whole + threadIdx.x; j < k; j += 256)
+      to[j] = from_float<T>(at >= 0 ? half ? p[j] + p[half + j] : p[j] : 0.0f);
   }
 }
 
@@ -325,13 +336,13 @@ cudaError_t launch_gather(const Index& a, const void* x, int64_t ldx, void* to, 
   return vec ? go(float(), std::true_type()) : go(float(), std::false_type());
 }
 
-cudaError_t launch_scatter(const float* from, int64_t ldfrom, const int* place, void* dx, int64_t lddx, int64_t rows, int64_t k,
-                           int dtype, int sms, cudaStream_t s) {
+cudaError_t launch_scatter(const float* from, int64_t ldfrom, const Index& a, void* dx, int64_t lddx, int64_t k, int dtype,
+                           int sms, cudaStream_t s) {
   const int bytes = dtype == SMAT_BF16 ? 8 : 16;  // of four elements
-  const bool vec = (uintptr_t)dx % bytes == 0 && (rows == 1 || lddx % 4 == 0);
+  const bool vec = (uintptr_t)dx % bytes == 0 && (a.rows == 1 || lddx % 4 == 0);
   auto go = [&](auto t, auto v) {
     using T = decltype(t);
-    scatter_kernel<T, decltype(v)::value><<<row_ctas(rows, sms), 256, 0, s>>>(from, ldfrom, place, (T*)dx, lddx, rows, k);
+    scatter_kernel<T, decltype(v)::value><<<row_ctas(a.rows, sms), 256, 0, s>>>(from, ldfrom, a, (T*)dx, lddx, k);
     return cudaGetLastError();
   };
   if (dtype == SMAT_BF16) return vec ? go(bf16(), std::true_type()) : go(bf16(), std::false_type());

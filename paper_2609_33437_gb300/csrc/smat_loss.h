@@ -27,7 +27,8 @@ struct Logits {
 cudaError_t logit_slots(const Logits& p, int sms, int64_t* slots);
 cudaError_t launch_logits(const Logits& p, int sms, cudaStream_t s);
 
-// The rows that count (their target is not `ignore`) by number: place[row] or -1, and *count.
+// The rows that count (their target is not `ignore`) by number: place[row] or -1, and *count. twice: every one a second time, at
+// place + *count / 2.
 struct Index {
   const int64_t* targets;
   const float* g;
@@ -38,14 +39,15 @@ struct Index {
   int* place;
   LossRow* info;
   int* count;
+  bool twice;
 };
 cudaError_t launch_index(const Index& a, cudaStream_t s);
 // x's rows that count and their info, at their places; rows of zeros behind them up to the next multiple of 64, or to the
 // end.
 cudaError_t launch_gather(const Index& a, const void* x, int64_t ldx, void* to, int64_t ldto, int64_t k, int dtype, bool to_end,
                           int sms, cudaStream_t s);
-// dx from sums at the rows' places; 0 for a row that has none.
-cudaError_t launch_scatter(const float* from, int64_t ldfrom, const int* place, void* dx, int64_t lddx, int64_t rows, int64_t k,
+// dx from sums at the rows' places (both of them); 0 for a row that has none.
+cudaError_t launch_scatter(const float* from, int64_t ldfrom, const Index& a, void* dx, int64_t lddx, int64_t k,
                            int dtype, int sms, cudaStream_t s);
 // A row's parts [slots][rows] (largest logit, sum of exponentials) joined.
 struct Join {

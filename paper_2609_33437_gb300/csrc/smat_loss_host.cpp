@@ -203,19 +203,28 @@ struct GradPlan {
   size_t count, place, info, x, d, sums, more, wcopy, cut_x, cut_w, cut_d, parts, bytes;
 };
 
+// bf16 with so few rows that all of them twice fit one tile of the products: d is kept as two bf16 numbers, its nearest and what that
+// lacks, as rows of their own. Few rows' roundings of d do not cancel (one row: dx and dW off by up to 2^-8 beside their own
+// rounding), and the second rows are free.
+constexpr int64_t kTwiceRows = 128;
+int64_t rows_of_d(const smat_token_loss_grad_args* a) {
+  return a->dtype == SMAT_BF16 && a->rows <= kTwiceRows ? 2 * a->rows : a->rows;
+}
+
 // The three products of a piece.
 void products(const smat_token_loss_grad_args* a, int64_t cols, Product* p) {
   const bool bf = a->dtype == SMAT_BF16;
-  p[0] = product(bf ? kLogitGrad : kForward, a->dtype, a->rows, cols, a->k);
-  p[1] = product(bf ? kGradInputSum : kGradInput, a->dtype, a->rows, a->k, cols);
-  p[2] = product(bf ? kGradWeightRows : kGradWeight, a->dtype, cols, a->k, a->rows);
+  const int64_t rows = rows_of_d(a);
+  p[0] = product(bf ? kLogitGrad : kForward, a->dtype, rows, cols, a->k);
+  p[1] = product(bf ? kGradInputSum : kGradInput, a->dtype, rows, a->k, cols);
+  p[2] = product(bf ? kGradWeightRows : kGradWeight, a->dtype, cols, a->k, rows);
 }
 
 smat_status plan(const smat_token_loss_grad_args* a, int sms, GradPlan* out) {
   GradPlan g = {};
   const bool bf = a->dtype == SMAT_BF16;
   const size_t es = elem_of(a->dtype);
-  const int64_t m = a->rows, k = a->k, n = a->n;
+  const int64_t m = rows_of_d(a), k = a->k, n = a->n;
   g.w = operand(a->w, n, k, a->ldw, a->dtype);
   int64_t most = kPieceBytes / ((int64_t)es * m);
   if (g.w.copied) most = std::min(most, kCopyBytes / (2 * ld_of(k)));
@@ -298,7 +307,7 @@ smat_status backward(const smat_token_loss_grad_args* a, void* d_workspace, size
   LossRow* info = (LossRow*)(ws + f.info);
   const int64_t ldk = ld_of(k), ldd = ld_of(f.piece);
   float *sums = (float*)(ws + f.sums), *more = (float*)(ws + f.more);
-  const loss::Index index = {a->targets, a->g, a->lse, a->w, a->ldw, m, n, a->ignore, place, info, count};
+  const loss::Index index = {a->targets, a->g, a->lse, a->w, a->ldw, m, n, a->ignore, place, info, count, rows_of_d(a) > m};
   cudaError_t e = loss::launch_index(index, s);
   if (e == cudaSuccess) e = loss::launch_gather(index, a->x, a->ldx, ws + f.x, ldk, k, a->dtype, !bf && !f.cut, sms, s);
   auto parts_at = [&](size_t at, int64_t rows, int64_t cols) {
@@ -311,7 +320,7 @@ smat_status backward(const smat_token_loss_grad_args* a, void* d_workspace, size
     if (e != cudaSuccess) break;
     Product p[3];
     products(a, cols, p);
-    for (Product& q : p) q.count = count, q.loss_rows = info, q.first_col = c;
+    for (Product& q : p) q.count = count, q.loss_rows = info, q.first_col = c, q.halves = index.twice;
     p[0].a = ws + f.x, p[0].lda = ldk, p[0].b = w.p, p[0].ldb = w.ld, p[0].out = ws + f.d, p[0].ldo = ldd;
     p[1].a = ws + f.d, p[1].lda = ldd, p[1].b = w.p, p[1].ldb = w.ld, p[1].ldo = ldk;
     p[1].out = bf || c == 0 ? sums : more, p[1].accumulate = bf && c > 0;
@@ -334,7 +343,7 @@ smat_status backward(const smat_token_loss_grad_args* a, void* d_workspace, size
     if (e == cudaSuccess && a->dx && !bf && c > 0) e = loss::launch_add(sums, more, ldk, m, k, sms, s);
     if (e == cudaSuccess && a->dw) e = launch_product(p[2], sms, ws + f.parts, s);
   }
-  if (e == cudaSuccess && a->dx) e = loss::launch_scatter(sums, ldk, place, a->dx, a->lddx, m, k, a->dtype, sms, s);
+  if (e == cudaSuccess && a->dx) e = loss::launch_scatter(sums, ldk, index, a->dx, a->lddx, k, a->dtype, sms, s);
   return cuda_status(e, "token_loss_grad launch");
 }
 
