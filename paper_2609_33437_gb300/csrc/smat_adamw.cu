@@ -2,10 +2,10 @@
 //
 // A warp takes a group of 256 neighbours at a time, 8 a lane, so that the largest magnitudes of a group in 8 bits are one
 // reduction over the warp. All CTAs walk through the list side by side, 8 groups each at a time (a stretch of its own for each:
-// 1,500 us for 367e6 elements in fp32, 5.9 TB/s; like this 1,360 us, 6.5 TB/s, which is memory's rate); the tensors' addresses
+// 1,500 us for 315e6 elements in fp32, 5.9 TB/s; like this 1,360 us, 6.5 TB/s, which is memory's rate); the tensors' addresses
 // come with the launch (no table on the device, nothing to copy), and a warp looks for its tensor once and then goes on from it.
 //
-// With moments in 8 bits memory is not what bounds it: 142e6 elements of bf16 370 us (3.8 TB/s; the issue slots are 75% busy, 76
+// With moments in 8 bits memory is not what bounds it: 147e6 elements of bf16 370 us (4.0 TB/s; the issue slots are 75% busy, 76
 // instructions an element). Codes by exponents and shifts of every value took 480 us, with divisions too 580; five CTAs per SM
 // instead of four (48 registers) 375.
 

@@ -519,8 +519,13 @@ __global__ void __launch_bounds__(1024) join_kernel(const Backward a) {
   const int64_t width = wanted * a.cols, j = (int64_t)blockIdx.x * 32 + threadIdx.x;
   float v = 0.0f;
   if (j < width)
-#pragma unroll 4
-    for (int s = threadIdx.y; s < a.shares; s += 32) v += a.parts[(size_t)s * width + j];
+    for (int s = threadIdx.y; s < a.shares; s += 32 * 8) {
+      float x[8];  // asked for together; those behind the last one are the last one's and are not added
+#pragma unroll
+      for (int t = 0; t < 8; ++t) x[t] = a.parts[(size_t)min(s + 32 * t, a.shares - 1) * width + j];
+#pragma unroll
+      for (int t = 0; t < 8; ++t) v += s + 32 * t < a.shares ? x[t] : 0.0f;
+    }
   space[threadIdx.y][threadIdx.x] = v;
   __syncthreads();
   if (threadIdx.y != 0 || j >= width) return;
