@@ -66,6 +66,8 @@ struct Product {
   const int* count;         // kLogitGrad and on, launch_f32_parts; on the device: how many rows there are, at most I (or L)
   const LossRow* loss_rows; // kLogitGrad: [I]
   int64_t first_col;        // kLogitGrad: the first column's place in the vocabulary
+  int splits;               // kGradInputSum: parts of the sum that other clusters make, each `slab` rows after the last (0: one)
+  int64_t slab;             // a multiple of 256
   int halves;               // kLogitGrad: rows from count / 2 on are what the same rows before them lose by their rounding
 };
 
@@ -100,6 +102,8 @@ cudaError_t launch_f32_parts(const Product& p, const Parts& of_b, const Parts& o
 // `workspace`: tc_workspace() bytes, which go by mode, I, J and L alone.
 cudaError_t tc_workspace(const Product& p, int sms, size_t* bytes);
 cudaError_t launch_tc(const Product& p, int sms, void* workspace, cudaStream_t s);
+// kGradInputSum: into how many parts its sum is best cut, for few rows.
+cudaError_t grad_input_splits(const Product& p, int* splits);
 // The tensor-core products' error bits of the current device; read and cleared (waits for the stream).
 cudaError_t error_word(int** at);
 cudaError_t read_errors(int* out, cudaStream_t s);

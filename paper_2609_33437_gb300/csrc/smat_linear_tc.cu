@@ -34,6 +34,9 @@
 // to 2); adding slices in registers, as fp32 products do, would take warps the pair's products need.
 
 #include "smat_linear.h"
+
+#include <algorithm>
+
 #include "smat_linear_tc.cuh"
 
 namespace smat {
@@ -410,13 +413,14 @@ __device__ __forceinline__ void finish_column(const Args& a, int64_t i, int64_t 
 template <int MODE, class Sums>
 __device__ __forceinline__ bool finish_blocks(const Args& a, const CUtensorMap* map_out, const CUtensorMap* map_in,
                                               const CUtensorMap* map_q, int64_t row0, int64_t col0, int first, int end,
-                                              int step, int64_t rows, Desk& desk, volatile int* dead, Sums&& sums) {
+                                              int step, int64_t rows, int64_t slab, Desk& desk, volatile int* dead,
+                                              Sums&& sums) {
 #pragma unroll 1
   for (int c = first; c < end; c += step) {
     const int64_t col = col0 + 32 * c;
     if (row0 < a.p.I && col < a.p.J) {
       if constexpr (MODE == kGradInputSum)
-        finish_sum_block(a, map_out, row0, col, desk, [&](float(&v)[32]) { sums(c, v); });
+        finish_sum_block(a, map_out, slab + row0, col, desk, [&](float(&v)[32]) { sums(c, v); });
       else if (!finish_block<MODE>(a, map_out, map_in, map_q, row0, col, rows, desk, dead, [&](float(&v)[32]) { sums(c, v); }))
         return false;
     } else {
@@ -642,8 +646,18 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     tiles_r = (rows + kPairRows - 1) / kPairRows;
     tiles = tiles_r * a.tiles_c;
   }
-  const int slice0 = (int)share * a.share;
-  const int slices = max(0, min(a.share, slices_there - slice0));
+  // kGradInputSum: a tile comes once for every part of its sum
+  int64_t units = tiles;
+  int slice0 = (int)share * a.share;
+  int slices = max(0, min(a.share, slices_there - slice0));
+  if (MODE == kGradInputSum) units *= max(1, a.p.splits);
+  auto part_of = [&](int64_t unit, int& first_slice, int& count) {  // the unit's tile, and its slices
+    if (MODE != kGradInputSum) return unit;
+    const int64_t split = unit / tiles;
+    first_slice = (int)(share + split) * a.share;
+    count = max(0, min(a.share, slices_there - first_slice));
+    return unit - split * tiles;
+  };
   const int64_t first_tile = blockIdx.x / ctas, step = gridDim.x / ctas;
   const int half_width = a.width / 2;
 
@@ -680,7 +694,8 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     const uint32_t full_there = cluster_address_of(full, leader);
     uint32_t n = 0;  // slices fetched so far
     bool ok = true;
-    for (int64_t tile = first_tile; ok && tile < tiles; tile += step) {
+    for (int64_t unit = first_tile; ok && unit < units; unit += step) {
+      const int64_t tile = part_of(unit, slice0, slices);
       int64_t tr, tc;
       tile_place<8>(tiles_r, a.tiles_c, tile, tr, tc);
       const int r0 = (int)(tr * kPairRows) + (int)member * kBM, c0 = (int)(tc * a.width) + (int)member * half_width;
@@ -717,7 +732,8 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     const uint16_t both = (uint16_t)(3u << rank);
     uint32_t n = 0, made = 0;
     bool ok = true;
-    for (int64_t tile = first_tile; ok && tile < tiles; tile += step, ++made) {
+    for (int64_t unit = first_tile; ok && unit < units; unit += step, ++made) {
+      part_of(unit, slice0, slices);
       const uint32_t half = made & 1, sums = tmem + half * kSums;
       ok = bar_wait(sums_empty + 8 * half, (made / 2 + 1) & 1, dead, a.errors);
       if (!ok) break;
@@ -756,10 +772,12 @@ __global__ void __launch_bounds__(kPairThreads, 1)
     constexpr int kBeside = kPairEpi / 4;  // warps that share 32 rows
     const int blocks = a.width / 32, first = warp / 4 * blocks / kBeside, end = (warp / 4 + 1) * blocks / kBeside;
     uint32_t made = 0;
-    for (int64_t tile = first_tile; tile < tiles; tile += step, ++made) {
+    for (int64_t unit = first_tile; unit < units; unit += step, ++made) {
+      const int64_t tile = part_of(unit, slice0, slices);
       int64_t tr, tc;
       tile_place<8>(tiles_r, a.tiles_c, tile, tr, tc);
       const int64_t r0 = tr * kPairRows + (int)member * kBM + 32 * quarter, c0 = tc * a.width;
+      const int64_t slab = MODE == kGradInputSum ? unit / tiles * a.p.slab : 0;  // where this part's rows begin
       const uint32_t half = made & 1, sums = tmem + half * kSums + ((uint32_t)(32 * quarter) << 16);
       if (!bar_wait_warp(sums_full + 8 * half, made / 2 & 1, dead, a.errors, kWaitNs + slices * kSliceNs)) break;
       fence_after();
@@ -779,7 +797,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       };
       if (first == end) release();  // none of a narrow tile's columns
       if (shares == 1) {
-        if (!finish_blocks<MODE>(a, &map_out, &map_in, &map_q, r0, c0, first, end, 1, rows, desk, dead, take)) break;
+        if (!finish_blocks<MODE>(a, &map_out, &map_in, &map_q, r0, c0, first, end, 1, rows, slab, desk, dead, take)) break;
       } else {
         float* part = a.parts + ((size_t)first_tile * ctas + rank) * a.width * kBM + 32 * quarter + lane;
         for (int c = first; c < end; ++c) {
@@ -804,7 +822,7 @@ __global__ void __launch_bounds__(kPairThreads, 1)
       const size_t apart = (size_t)2 * a.width * kBM;
       const int blocks = r0 < a.p.I ? (int)((min((int64_t)a.width, a.p.J - c0) + 31) / 32) : 0;
       finish_blocks<MODE>(a, &map_out, &map_in, &map_q, r0, c0, (int)share + (int)shares * (warp / 4), blocks,
-                          (int)shares * (kPairEpi / 4), rows, desk, dead, [&](int c, float(&v)[32]) {
+                          (int)shares * (kPairEpi / 4), rows, 0, desk, dead, [&](int c, float(&v)[32]) {
                            add_parts(shares, v, [&](uint32_t s, int t) { return __ldcg(part + s * apart + (32 * c + t) * kBM); });
                          });
     }
@@ -866,6 +884,12 @@ cudaError_t plan_pair(const Product& p, Plan* plan) {
   double least = 0;
   const int slices = (int)((p.L + kBK - 1) / kBK);
   const int64_t tiles_r = (p.I + kPairRows - 1) / kPairRows;
+  if (MODE == kGradInputSum && p.splits > 1) {  // a pair for each part of each tile
+    const int64_t at_once = clusters_at_once(f, 2, kPairThreads, kPairBytes<MODE>, clusters);
+    const int64_t tiles_c = (p.J + 255) / 256, units = tiles_r * tiles_c * p.splits;
+    *plan = {tiles_r, tiles_c, 2 * std::min(units, at_once), slices, (slices + p.splits - 1) / p.splits, 1, 256, 0};
+    return cudaSuccess;
+  }
   for (int width = 256; width >= 64; width -= 32) {
     const int64_t tiles_c = (p.J + width - 1) / width, tiles = tiles_r * tiles_c;
     for (int shares = 1; shares <= 4; ++shares) {
@@ -942,7 +966,8 @@ cudaError_t launch_pair(const Product& p, void* workspace, cudaStream_t s) {
   CUtensorMap mo = {}, mi = {}, mq = {};
   const void* in = MODE == kForward ? p.residual : kWeightGrad<MODE> && p.accumulate ? p.out : nullptr;
   if (MODE == kGradInputSum) {
-    if (!a.by_rows || !encode(&mo, p.out, p.J, p.I, p.ldo, 32, 32, 4)) return cudaErrorNotSupported;
+    const int64_t rows = p.splits > 1 ? p.splits * p.slab : p.I;
+    if (!a.by_rows || !encode(&mo, p.out, p.J, rows, p.ldo, 32, 32, 4)) return cudaErrorNotSupported;
   } else if (a.by_rows && !(encode(&mo, p.out, p.J, p.I, p.ldo, 32, 32) &&
                      (!in || encode(&mi, in, p.J, p.I, MODE == kForward ? p.ldr : p.ldo, 32, 32)) &&
                      (!p.q || encode(&mq, p.q, p.J, p.I, p.ldq, 32, 32, 1))))
@@ -1011,6 +1036,23 @@ struct Size {
 cudaError_t tc_workspace(const Product& p, int sms, size_t* bytes) { return choose(p, Size{p, sms, bytes}); }
 cudaError_t launch_tc(const Product& p, int sms, void* workspace, cudaStream_t s) {
   return choose(p, Launch{p, sms, workspace, s});
+}
+
+// Few rows have few tiles and a sum as long as the vocabulary. A cluster's shares, four at most, left most of the GPU idle: 100 x 256
+// back from 100000 words took 120 us with 32 CTAs, and 26 in 32 parts with 64; 24 x 4096 from 32000 63 and 51, 300 x 1024 from 8000
+// 20 and 14, 8 x 512 from 5000 15 and 9.5. The parts are added in one order by whoever reads them. At least four slices each, one
+// round of pairs, and no more than 32 parts to be read again; 1 where the tiles fill the GPU by themselves.
+cudaError_t grad_input_splits(const Product& p, int* splits) {
+  static std::atomic<uint64_t> allowed;
+  static std::atomic<int> clusters[64][9];
+  auto* f = pair_kernel<kGradInputSum>;
+  *splits = 1;
+  const cudaError_t e = allow_shared(f, kPairBytes<kGradInputSum>, allowed);
+  if (e != cudaSuccess || p.I == 0 || p.J == 0) return e;
+  const int64_t at_once = clusters_at_once(f, 2, kPairThreads, kPairBytes<kGradInputSum>, clusters);
+  const int64_t tiles = (p.I + kPairRows - 1) / kPairRows * ((p.J + 255) / 256), slices = (p.L + kBK - 1) / kBK;
+  *splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(at_once / tiles, slices / 4), 32));
+  return cudaSuccess;
 }
 
 cudaError_t error_word(int** at) {

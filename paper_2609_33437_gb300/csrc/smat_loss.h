@@ -46,9 +46,15 @@ cudaError_t launch_index(const Index& a, cudaStream_t s);
 // end.
 cudaError_t launch_gather(const Index& a, const void* x, int64_t ldx, void* to, int64_t ldto, int64_t k, int dtype, bool to_end,
                           int sms, cudaStream_t s);
-// dx from sums at the rows' places (both of them); 0 for a row that has none.
-cudaError_t launch_scatter(const float* from, int64_t ldfrom, const Index& a, void* dx, int64_t lddx, int64_t k,
-                           int dtype, int sms, cudaStream_t s);
+// dx's sums, in `splits` parts that lie `apart` floats after one another.
+struct Sums {
+  const float* at;
+  int64_t ld;
+  int splits;
+  int64_t apart;
+};
+// dx from the sums at the rows' places (both of them); 0 for a row that has none.
+cudaError_t launch_scatter(const Sums& from, const Index& a, void* dx, int64_t lddx, int64_t k, int dtype, int sms, cudaStream_t s);
 // A row's parts [slots][rows] (largest logit, sum of exponentials) joined.
 struct Join {
   const float2* partials;

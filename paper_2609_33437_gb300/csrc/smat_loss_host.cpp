@@ -199,6 +199,8 @@ smat_status forward(const smat_token_loss_args* a, void* d_workspace, size_t wor
 struct GradPlan {
   Operand w;
   int64_t piece;
+  int splits;    // of dx's sum, bf16; each has `slab` rows of `sums`
+  int64_t slab;
   bool cut;  // fp32: the products share operands that are cut for the tensor cores
   size_t count, place, info, x, d, sums, more, wcopy, cut_x, cut_w, cut_d, parts, bytes;
 };
@@ -212,11 +214,12 @@ int64_t rows_of_d(const smat_token_loss_grad_args* a) {
 }
 
 // The three products of a piece.
-void products(const smat_token_loss_grad_args* a, int64_t cols, Product* p) {
+void products(const smat_token_loss_grad_args* a, const GradPlan& g, int64_t cols, Product* p) {
   const bool bf = a->dtype == SMAT_BF16;
   const int64_t rows = rows_of_d(a);
   p[0] = product(bf ? kLogitGrad : kForward, a->dtype, rows, cols, a->k);
   p[1] = product(bf ? kGradInputSum : kGradInput, a->dtype, rows, a->k, cols);
+  p[1].splits = g.splits, p[1].slab = g.slab;
   p[2] = product(bf ? kGradWeightRows : kGradWeight, a->dtype, cols, a->k, rows);
 }
 
@@ -230,25 +233,31 @@ smat_status plan(const smat_token_loss_grad_args* a, int sms, GradPlan* out) {
   if (g.w.copied) most = std::min(most, kCopyBytes / (2 * ld_of(k)));
   g.piece = piece_of(n, most);
   const int64_t pieces = (n + g.piece - 1) / g.piece, last = n - (pieces - 1) * g.piece;
+  g.splits = 1, g.slab = m;
+  if (bf && a->dx) {
+    const cudaError_t e = grad_input_splits(product(kGradInputSum, a->dtype, m, k, g.piece), &g.splits);
+    if (e != cudaSuccess) return cuda_status(e, "plan of dx's product");
+    if (g.splits > 1) g.slab = (m + 255) / 256 * 256;
+  }
   Space s;
   g.count = s.take(sizeof(int));
   g.place = s.take(sizeof(int) * (size_t)m);
   g.info = s.take(sizeof(LossRow) * (size_t)m);
   g.x = s.take(copy_bytes(m, k, es));
   g.d = s.take(copy_bytes(m, g.piece, es));
-  g.sums = s.take(a->dx ? copy_bytes(m, k, 4) : 0);
+  g.sums = s.take(a->dx ? copy_bytes(g.splits * g.slab, k, 4) : 0);
   g.more = s.take(a->dx && !bf && pieces > 1 ? copy_bytes(m, k, 4) : 0);
   g.wcopy = s.take(g.w.copied ? copy_bytes(g.piece, k, 2) : 0);
   size_t parts = 0;
   g.cut = !bf;
   for (int64_t cols : {g.piece, last}) {
     Product p[3];
-    products(a, cols, p);
+    products(a, g, cols, p);
     for (const Product& q : p) g.cut = g.cut && f32_on_tensor_cores(q);
   }
   for (int64_t cols : {g.piece, last}) {
     Product p[3];
-    products(a, cols, p);
+    products(a, g, cols, p);
     for (int i = 0; i < 3; ++i) {
       if (i > 0 && !(i == 1 ? a->dx : a->dw)) continue;
       size_t bytes = 0;
@@ -319,7 +328,7 @@ smat_status backward(const smat_token_loss_grad_args* a, void* d_workspace, size
     e = rows_of(a->w, a->ldw, f.w, c, cols, k, es, ws + f.wcopy, sms, s, &w);
     if (e != cudaSuccess) break;
     Product p[3];
-    products(a, cols, p);
+    products(a, f, cols, p);
     for (Product& q : p) q.count = count, q.loss_rows = info, q.first_col = c, q.halves = index.twice;
     p[0].a = ws + f.x, p[0].lda = ldk, p[0].b = w.p, p[0].ldb = w.ld, p[0].out = ws + f.d, p[0].ldo = ldd;
     p[1].a = ws + f.d, p[1].lda = ldd, p[1].b = w.p, p[1].ldb = w.ld, p[1].ldo = ldk;
@@ -343,7 +352,8 @@ smat_status backward(const smat_token_loss_grad_args* a, void* d_workspace, size
     if (e == cudaSuccess && a->dx && !bf && c > 0) e = loss::launch_add(sums, more, ldk, m, k, sms, s);
     if (e == cudaSuccess && a->dw) e = launch_product(p[2], sms, ws + f.parts, s);
   }
-  if (e == cudaSuccess && a->dx) e = loss::launch_scatter(sums, ldk, index, a->dx, a->lddx, k, a->dtype, sms, s);
+  if (e == cudaSuccess && a->dx)
+    e = loss::launch_scatter({sums, ldk, f.splits, f.slab * ldk}, index, a->dx, a->lddx, k, a->dtype, sms, s);
   return cuda_status(e, "token_loss_grad launch");
 }
 
