@@ -63,13 +63,24 @@ class Moments:
         # what a call hands over of the list
         self._numels = struct.pack(f"{len(self.sizes)}q", *self.sizes)
         self._pointers = struct.Struct(f"{len(self.sizes)}P")
-        b = self._buffers
-        self._places = ((b["q1"].data_ptr(), b["q2"].data_ptr(), b["e1"].data_ptr(), b["e2"].data_ptr()) if bits == 8 else
-                        (b["m1"].data_ptr(), b["m2"].data_ptr(), 0, 0))
 
     def buffers(self) -> Dict[str, torch.Tensor]:
-        """The buffers by name: m1 and m2, or q1, e1, q2 and e2. They may be read and written (a checkpoint)."""
+        """The buffers by name: m1 and m2, or q1, e1, q2 and e2. They may be read and written (a checkpoint), and moved away and
+        back: a step takes them where they lie then, and refuses them elsewhere or in another form."""
         return dict(self._buffers)
+
+    def _addresses(self):
+        """(m1, m2, 0, 0) or (q1, q2, e1, e2), where they lie now: whoever was handed a buffer may have given it other storage."""
+        out = []
+        index = self.device.index if self.device.index is not None else -1
+        for name in ("q1", "q2", "e1", "e2") if self.bits == 8 else ("m1", "m2"):
+            t = self._buffers[name]
+            count = self.places // GROUP if name[0] == "e" else self.places
+            dtype = torch.uint8 if self.bits == 8 else torch.float32
+            if t.dtype is not dtype or _numel(t) != count or _get_device(t) != index or not _contiguous(t):
+                raise ValueError(f"moments: {name} must be contiguous {dtype} of {count} elements on {self.device}, as it was made")
+            out.append(_data_ptr(t))
+        return out if self.bits == 8 else (*out, 0, 0)
 
     def values(self, stream: Optional[torch.cuda.Stream] = None):
         """(m1, m2) for 32 bits, the buffers themselves; (m1, r) in bfloat16, which holds what 8 bits stand for exactly."""
@@ -78,9 +89,9 @@ class Moments:
             return b["m1"], b["m2"]
         if stream is not None:
             return L._on(stream, self.values)
+        q1, q2, e1, e2 = self._addresses()
         m1, r = (torch.empty(self.places, dtype=torch.bfloat16, device=self.device) for _ in range(2))
-        L._call("smat_adamw_values", self.device, b["q1"].data_ptr(), b["e1"].data_ptr(), b["q2"].data_ptr(), b["e2"].data_ptr(),
-                m1.data_ptr(), r.data_ptr(), self.places)
+        L._call("smat_adamw_values", self.device, q1, e1, q2, e2, m1.data_ptr(), r.data_ptr(), self.places)
         return m1, r
 
     def views(self, name: str) -> List[torch.Tensor]:
@@ -152,7 +163,7 @@ def adamw(params: Sequence[torch.Tensor], grads: Sequence[Optional[torch.Tensor]
     # the arrays live until the call returns
     arrays = ctypes.create_string_buffer(pack(*pp) + pack(*gp) + moments._numels)
     at = ctypes.addressof(arrays)
-    args = _ADAMW.pack(at, at + 8 * n, at + 16 * n, *moments._places, scale_at, lr_at, step_at, by, rate, beta1, beta2, eps,
+    args = _ADAMW.pack(at, at + 8 * n, at + 16 * n, *moments._addresses(), scale_at, lr_at, step_at, by, rate, beta1, beta2, eps,
                        weight_decay, t, seed & 0xFFFFFFFFFFFFFFFF, n, code, code if gdt is None else S.dtype_code(gdt),
                        moments.bits)
     L._call("smat_adamw_step", device, args)

@@ -118,3 +118,26 @@ def test_the_8_bit_form():
     low = np.floor(float(v[1]) * 16) / 16
     p = (float(v[1]) - low) * 16
     assert abs(ups / (n * 255) - p) < 5 * (p * (1 - p) / (n * 255)) ** 0.5
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_moments_where_they_lie(bits):
+    """A buffer that was given other storage: a step takes that one, and refuses one of another size or stride."""
+    m = O.Moments([torch.zeros(300), torch.zeros(5)], bits=bits)
+    names = ("q1", "q2", "e1", "e2") if bits == 8 else ("m1", "m2")
+    keep = []
+    for k, name in enumerate(names):
+        t = m.buffers()[name]
+        keep.append(t.data)
+        t.data = t.data.clone()
+        assert t.data_ptr() != keep[-1].data_ptr() and m._addresses()[k] == t.data_ptr()
+    assert bits == 8 or m._addresses()[2:] == (0, 0)
+    t = m.buffers()[names[0]]
+    for bad in (t.data[:-1].clone(), t.data.repeat_interleave(2)[::2]):
+        was, t.data = t.data, bad
+        with pytest.raises(ValueError, match=f"moments: {names[0]}"):
+            m._addresses()
+        t.data = was
+    t.data = t.data[:0]
+    with pytest.raises(ValueError, match="moments"):
+        m.values() if bits == 8 else m._addresses()

@@ -364,3 +364,26 @@ def test_schedule_takes_the_step_into_the_gradient_map(dt):
         return [p.detach().clone() for p in params] + [v.clone() for v in opt.lists()[0][2].values()]
 
     assert all(torch.equal(a, b) for a, b in zip(run(True), run(False)))
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_moments_moved_away_and_back(bits):
+    """Buffers taken to the host and back, and given other storage: the step goes on with the bits of one that stayed."""
+    sizes = [700, 33]
+    start = _tensors(0, sizes, F32, 0.1)
+    lists, kept = [], []
+    for moved in (False, True):
+        params = [t.clone() for t in start]
+        moments = O.Moments(params, bits=bits)
+        for t in (1, 2, 3):
+            O.adamw(params, _tensors(t, sizes, F32, 1e-3), moments, t, **HYPER)
+            if moved:
+                for b in moments.buffers().values():
+                    kept.append(b.data)  # nobody else gets its place: a step that went there would be seen
+                    b.data = b.data.cpu()
+                with pytest.raises(ValueError, match="moments"):
+                    O.adamw(params, params, moments, t + 1, **HYPER)
+                for b in moments.buffers().values():
+                    b.data = b.data.cuda()
+        lists.append([*params, *moments.buffers().values()])
+    assert all(torch.equal(a, b) for a, b in zip(*lists))
