@@ -33,6 +33,21 @@ struct Raw {
   Word u;
   __device__ __forceinline__ void load(const T* p) { u = *reinterpret_cast<const Word*>(p); }
   __device__ __forceinline__ void zero() { u = Word{}; }
+  // Those that `has` names, one by one; 0 for the others, which are not read.
+  template <class Has>
+  __device__ __forceinline__ void load_some(const T* p, Has&& has) {
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) reinterpret_cast<uint32_t*>(&u)[i] = has(i) ? reinterpret_cast<const uint32_t*>(p)[i] : 0u;
+    } else {
+      const uint16_t* q = reinterpret_cast<const uint16_t*>(p);
+      uint32_t x[VEC];
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) x[i] = has(i) ? q[i] : 0u;
+#pragma unroll
+      for (int i = 0; i + 1 < VEC; i += 2) reinterpret_cast<uint32_t*>(&u)[i / 2] = x[i] | x[i + 1] << 16;
+    }
+  }
   __device__ __forceinline__ float at(int i) const {
     if constexpr (sizeof(T) == 4) return reinterpret_cast<const float*>(&u)[i];
     if constexpr (VEC == 1) return __uint_as_float((uint32_t)u << 16);
@@ -128,7 +143,7 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float* space) {
 // The columns that a thread holds, C vectors of VEC. SHIFT: rows do not all start on 16 bytes, but those of all matrices lie alike.
 // Vectors are those of memory then, of which a row's first starts before it by as much as the row's address is past 16 bytes, and
 // the same for all the rows of a thread, which are a multiple of 16 / sizeof(T) apart. Of a vector that reaches out of the row
-// what is outside counts as 0, and only what is inside is written.
+// only what is inside is read and written, element by element; what is outside counts as 0.
 template <class T, int VEC, int C, bool SHIFT>
 struct Columns {
   // (in 32 bits a shifted row is faster, 4099 x 1023 19 us and not 33; a whole one in 64 bits, 8192 x 4096 in fp32 84 and not 110)
@@ -151,12 +166,10 @@ struct Columns {
   __device__ __forceinline__ bool has(int c, int i) const { return !SHIFT || (at(c) + i >= 0 && at(c) + i < cols); }
   __device__ __forceinline__ bool whole(int c) const { return inside[c]; }
   __device__ __forceinline__ void load(Raw<T, VEC>& v, const T* row, int c) const {
-    v.load(row + at(c));
-    if (SHIFT && !whole(c)) {
-      float x[VEC];
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) x[i] = has(c, i) ? v.at(i) : 0.0f;
-      v.set(x);
+    if (!SHIFT || whole(c)) {
+      v.load(row + at(c));
+    } else {
+      v.load_some(row + at(c), [&](int i) { return has(c, i); });
     }
   }
   __device__ __forceinline__ void store(const Raw<T, VEC>& v, T* row, int c) const {
