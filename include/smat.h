@@ -605,9 +605,15 @@ smat_status smat_norm_grad(const smat_norm_grad_args* args, void* d_workspace, s
  * call multiplies on the tensor cores (as smat_linear says; the sums of lse and loss are made in parts, as near as plain fp32) and
  * rounds d to bf16 before its products with W and x (of at most 128 rows to two bf16 numbers, 16 bits). A target
  * outside 0 .. n - 1 that is not `ignore` gives a loss of NaN and gradients of NaN. Rows with t_i = ignore have an lse like
- * every row; back, they are left out: what they hold (infinities, NaN) reaches nothing, and their dx is 0. The workspace of the
- * gradient is some 200 MB for pieces of d, and x's rows and dx in fp32; it does not grow with the vocabulary. Results do not
- * depend on timing. rows and k may be 0, n is at least 1. Outputs must not overlap inputs or one another. What
+ * every row; back, they are left out: what they hold (infinities, NaN) reaches nothing, and their dx is 0.
+ *
+ * The vocabulary is taken in pieces of 2,048 words at least. The workspace of the gradient holds, whatever the vocabulary: a
+ * piece of d (192 MiB, or what 2,048 words take); the rows of x, and dx in fp32 (bf16 with few rows: in up to 32 parts of a
+ * multiple of 256 rows); a piece of W where its rows do not start on 16 bytes (64 MiB); and for fp32 on the tensor cores the
+ * three parts of x, of d (1.5 times d) and of a piece of W (1 GiB). That of the loss: 8 bytes for each row and 64 to 256 words
+ * (fp32: each row and piece), and in fp32 a piece of logits and the parts of x and W, of the same sizes.
+ *
+ * Results do not depend on timing. rows and k may be 0, n is at least 1. Outputs must not overlap inputs or one another. What
  * smat_linear_poll_errors says holds for these products too. */
 typedef struct {
   const void* x;

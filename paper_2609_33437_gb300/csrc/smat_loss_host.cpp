@@ -26,6 +26,9 @@ constexpr int64_t kMaxCols = int64_t(65535) * 64;
 constexpr int64_t kPieceBytes = int64_t(192) << 20, kPieceCols = 2048;
 // A piece of W that is copied because its rows do not start on 16 bytes.
 constexpr int64_t kCopyBytes = int64_t(64) << 20;
+// A piece of W cut for the tensor cores (fp32), which with few rows takes more space than d: 64 x 4096 of 151936 words 3.7 GB
+// beside 38 MB if taken whole. Smaller pieces cost more at their ends (384 MiB: 515 x 4096 x 32000 forward 955 us for 824).
+constexpr int64_t kCutBytes = int64_t(1) << 30;
 
 bool sizes_fit(int64_t rows, int64_t k, int64_t n) {
   return rows >= 0 && rows <= kMaxSize && k >= 0 && k <= kMaxCols && n >= 1 && n <= kMaxCols;
@@ -46,6 +49,16 @@ int64_t piece_of(int64_t n, int64_t most) {
   if (n <= most) return n;
   const int64_t pieces = (n + most - 1) / most;
   return std::min(n, ((n + pieces - 1) / pieces + 255) / 256 * 256);
+}
+
+// The most columns of a piece whose d, or fp32 logits, have `rows` rows.
+int64_t most_of(int64_t rows, int64_t k, int64_t n, int32_t dtype, const Operand& w) {
+  int64_t most = kPieceBytes / ((int64_t)elem_of(dtype) * rows);
+  if (w.copied) most = std::min(most, kCopyBytes / (2 * ld_of(k)));
+  Product p = {};
+  p.mode = kForward, p.dtype = dtype, p.I = rows, p.J = n, p.L = k;
+  if (dtype == SMAT_F32 && f32_on_tensor_cores(p)) most = std::min(most, kCutBytes / (6 * parts_ld(k)));
+  return most;
 }
 
 // Places in the workspace, in turn.
@@ -113,7 +126,7 @@ smat_status plan(const smat_token_loss_args* a, int sms, ForwardPlan* out) {
   f.w = operand(a->w, n, k, a->ldw, a->dtype);
   f.piece = n;
   if (!bf)
-    f.piece = piece_of(n, kPieceBytes / (4 * m));
+    f.piece = piece_of(n, most_of(m, k, n, a->dtype, f.w));
   else if (f.w.copied)
     f.piece = piece_of(n, kCopyBytes / (2 * ld_of(k)));
   const int64_t pieces = (n + f.piece - 1) / f.piece, last = n - (pieces - 1) * f.piece;
@@ -229,9 +242,7 @@ smat_status plan(const smat_token_loss_grad_args* a, int sms, GradPlan* out) {
   const size_t es = elem_of(a->dtype);
   const int64_t m = rows_of_d(a), k = a->k, n = a->n;
   g.w = operand(a->w, n, k, a->ldw, a->dtype);
-  int64_t most = kPieceBytes / ((int64_t)es * m);
-  if (g.w.copied) most = std::min(most, kCopyBytes / (2 * ld_of(k)));
-  g.piece = piece_of(n, most);
+  g.piece = piece_of(n, most_of(m, k, n, a->dtype, g.w));
   const int64_t pieces = (n + g.piece - 1) / g.piece, last = n - (pieces - 1) * g.piece;
   g.splits = 1, g.slab = m;
   if (bf && a->dx) {

@@ -341,3 +341,43 @@ def test_layers_and_autocast():
         value = T.cross_entropy(x32, w32, t[:5] % 300)
     value.backward()
     assert value.dtype is F32 and w32.grad.dtype is F32 and x32.grad.shape == x32.shape
+
+
+def _workspaces(m, k, n, dt):
+    """Bytes that the loss and its gradient ask for (addresses only have to be aligned)."""
+    code, at = 1 if dt is BF else 0, [4096 * i for i in range(1, 8)]
+    lib = L.S.load_library()
+    fwd = T._TOKEN_LOSS.pack(*at[:5], m, k, n, k, k, IGNORE, code, 0)
+    grad = T._TOKEN_LOSS_GRAD.pack(*at, m, k, n, k, k, k, k, IGNORE, code, 0)
+    return lib.smat_token_loss_workspace_bytes(fwd), lib.smat_token_loss_grad_workspace_bytes(grad)
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("m", [1, 16, 17, 64, 300, 2049, 8192])
+@pytest.mark.parametrize("k", [64, 896, 4096])
+def test_workspace_is_bounded_in_the_vocabulary(m, k, dt):
+    """The gradient's by what the header names, and no larger for four times the words; the loss's grows by its parts alone."""
+    n, mib = 151936, 1 << 20
+    fwd, grad = _workspaces(m, k, n, dt)
+    rows = 2 * m if dt is BF and m <= 128 else m
+    d = max(192 * mib, rows * 2048 * (2 if dt is BF else 4))
+    x = rows * (k + 32) * 4
+    if dt is BF:
+        most, part = d + 3 * x + 33 * 256 * (k + 32) * 4, 8 * m * (n // 64 + 400)
+    else:
+        most, part = 2.5 * d + 1024 * mib + 5 * x, d + 1024 * mib + 2 * x
+    slack = 48 * mib  # shares of sums of one tile an SM, flags, numbers of rows, rounding up
+    assert 0 < grad <= most + slack and 0 < fwd <= part + slack
+    fwd4, grad4 = _workspaces(m, k, 4 * n, dt)
+    assert grad4 <= most + slack and fwd4 <= 4 * part + slack
+    assert dt is BF or fwd4 <= part + slack
+
+
+@pytest.mark.parametrize("m,k,n", [(20, 4096, 50000), (300, 2048, 90000), (64, 4100, 45000)])
+def test_fp32_pieces_of_a_cut_vocabulary(m, k, n):
+    """fp32 on the tensor cores, W in more than one piece for the size of its parts; results added up over them."""
+    dx, dw = _check(*_inputs(m + n, m, k, n, F32, 0.3))[2:]
+    x, w, t, g = _inputs(m + n, m, k, n, F32, 0.3)
+    _, lse = T.token_loss(x, w, t)
+    again = T.token_loss_grad(g, x, w, t, lse, need_w=False)[0], T.token_loss_grad(g, x, w, t, lse, need_x=False)[1]
+    assert torch.equal(again[0], dx) and torch.equal(again[1], dw)
