@@ -211,7 +211,8 @@ class AdamW(torch.optim.Optimizer):
             beta1, beta2 = group["betas"]
             adamw(ps, [p.grad if p.grad is None or p.grad.is_contiguous() else p.grad.contiguous() for p in ps], moments, t,
                   group["lr"], beta1, beta2, group["eps"], group["weight_decay"], scale, self.seed + k)
-            torch.autograd.graph.increment_version(ps)  # what a graph saved of them is no longer what it saved
+            # what a graph saved of those that moved is no longer what it saved
+            torch.autograd.graph.increment_version([p for p in ps if p.grad is not None])
         self.steps = t
         return loss
 

@@ -387,3 +387,16 @@ def test_moments_moved_away_and_back(bits):
                     b.data = b.data.cuda()
         lists.append([*params, *moments.buffers().values()])
     assert all(torch.equal(a, b) for a, b in zip(*lists))
+
+
+def test_a_parameter_without_a_gradient_is_untouched():
+    """The step leaves it as it is: a graph that saved it goes on."""
+    w, v = torch.nn.Parameter(torch.randn(8, 8, device="cuda")), torch.nn.Parameter(torch.randn(8, 8, device="cuda"))
+    x = torch.randn(4, 8, device="cuda", requires_grad=True)
+    loss = (x @ w).sum()
+    v.grad = torch.ones_like(v)
+    versions = w._version, v._version
+    O.AdamW([w, v]).step()
+    assert w._version == versions[0] and v._version > versions[1]
+    loss.backward()
+    assert torch.equal(x.grad, torch.ones(4, 8, device="cuda") @ w.detach().T)
