@@ -701,6 +701,9 @@ int64_t smat_adamw_places(const int64_t* numels, int32_t n_tensors);
  * overlap one another or anything that is read. */
 smat_status smat_adamw_step(const smat_adamw_args* args, smat_stream_t stream);
 
+/* What that call would answer to these arguments, without the step: for a caller whose step is several calls. */
+smat_status smat_adamw_check(const smat_adamw_args* args);
+
 /* What moments in 8 bits stand for: bf16 m1 and r, [places] each, on 16 bytes (as q1 and q2 are). */
 smat_status smat_adamw_values(const uint8_t* q1, const uint8_t* e1, const uint8_t* q2, const uint8_t* e2, void* m1, void* r,
                               int64_t places, smat_stream_t stream);

@@ -72,7 +72,9 @@ smat_status check_ranges(std::vector<Range>& ranges) {
   return SMAT_OK;
 }
 
-smat_status step(const smat_adamw_args* a, cudaStream_t stream) {
+// What a step refuses; *any: whether it has anything to do.
+smat_status check(const smat_adamw_args* a, bool* any) {
+  *any = false;
   if (!a) return lfail(SMAT_ERR_INVALID_ARG, "args is NULL");
   if (a->dtype != SMAT_F32 && a->dtype != SMAT_BF16) return lfail(SMAT_ERR_UNSUPPORTED, "dtype %d not supported", a->dtype);
   if (a->grad_dtype != SMAT_F32 && a->grad_dtype != SMAT_BF16)
@@ -102,14 +104,13 @@ smat_status step(const smat_adamw_args* a, cudaStream_t stream) {
   auto add = [&](const char* name, int32_t i, const void* p, size_t bytes, bool written, size_t elem) {
     ranges.push_back({(uintptr_t)p, (uintptr_t)p + bytes, written, name, i, elem});
   };
-  bool any = false;
   for (int32_t k = 0; k < n; ++k) {
     if (a->numels[k] == 0 || !a->grads[k]) continue;
-    any = true;
+    *any = true;
     add("params", k, a->params[k], (size_t)a->numels[k] * ep, true, ep);
     add("grads", k, a->grads[k], (size_t)a->numels[k] * eg, false, eg);
   }
-  if (!any) return SMAT_OK;
+  if (!*any) return SMAT_OK;
   add("m1", -1, a->m1, (size_t)places * em, true, 32);
   add("m2", -1, a->m2, (size_t)places * em, true, 32);
   if (a->bits == 8) {
@@ -119,11 +120,18 @@ smat_status step(const smat_adamw_args* a, cudaStream_t stream) {
   if (a->scale_at) add("scale_at", -1, a->scale_at, 4, false, 4);
   if (a->lr_at) add("lr_at", -1, a->lr_at, 4, false, 4);
   if (a->step_at) add("step_at", -1, a->step_at, 8, false, 8);
-  smat_status st = check_ranges(ranges);
-  if (st != SMAT_OK) return st;
+  return check_ranges(ranges);
+}
+
+smat_status step(const smat_adamw_args* a, cudaStream_t stream) {
+  bool any;
+  smat_status st = check(a, &any);
+  if (st != SMAT_OK || !any) return st;
   int sms = 1;
   st = device_sms(&sms);
   if (st != SMAT_OK) return st;
+  const int32_t n = a->n_tensors;
+  const size_t em = a->bits == 8 ? 1 : 4;
 
   adamw::Call c = {};
   const double t = (double)a->step;
@@ -198,6 +206,13 @@ extern "C" {
 int64_t smat_adamw_places(const int64_t* numels, int32_t n_tensors) {
   const int64_t places = places_of(numels, n_tensors);
   return places < 0 ? 0 : places;
+}
+
+smat_status smat_adamw_check(const smat_adamw_args* args) {
+  return guarded([&] {
+    bool any;
+    return check(args, &any);
+  });
 }
 
 smat_status smat_adamw_step(const smat_adamw_args* args, smat_stream_t stream) {

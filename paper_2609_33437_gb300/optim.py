@@ -146,6 +146,12 @@ def adamw(params: Sequence[torch.Tensor], grads: Sequence[Optional[torch.Tensor]
     goes on with what they hold at each replay."""
     if stream is not None:
         return L._on(stream, adamw, params, grads, moments, step, lr, beta1, beta2, eps, weight_decay, scale, seed)
+    args, _ = _arguments(params, grads, moments, step, lr, beta1, beta2, eps, weight_decay, scale, seed)
+    L._call("smat_adamw_step", moments.device, args)
+
+
+def _arguments(params, grads, moments, step, lr, beta1, beta2, eps, weight_decay, scale, seed):
+    """(what smat_adamw_step takes, the arrays that have to live until it returns)"""
     n = len(moments.sizes)
     if len(params) != n or len(grads) != n:
         raise ValueError(f"{len(params)} params and {len(grads)} grads for moments of {n}")
@@ -160,13 +166,22 @@ def adamw(params: Sequence[torch.Tensor], grads: Sequence[Optional[torch.Tensor]
     rate, lr_at = _one("lr", lr, torch.float32, device)
     by, scale_at = _one("scale", scale, torch.float32, device)
     pack = moments._pointers.pack
-    # the arrays live until the call returns
     arrays = ctypes.create_string_buffer(pack(*pp) + pack(*gp) + moments._numels)
     at = ctypes.addressof(arrays)
     args = _ADAMW.pack(at, at + 8 * n, at + 16 * n, *moments._addresses(), scale_at, lr_at, step_at, by, rate, beta1, beta2, eps,
                        weight_decay, t, seed & 0xFFFFFFFFFFFFFFFF, n, code, code if gdt is None else S.dtype_code(gdt),
                        moments.bits)
-    L._call("smat_adamw_step", device, args)
+    return args, arrays
+
+
+def _check(args: bytes, device) -> None:
+    """Raises what the step would."""
+    if device.index != L._current_device():
+        with torch.cuda.device(device):
+            return _check(args, device)
+    st = L._function("smat_adamw_check")[1](args)
+    if st:
+        S.check("smat_adamw_check", st)
 
 
 class AdamW(torch.optim.Optimizer):
@@ -201,18 +216,26 @@ class AdamW(torch.optim.Optimizer):
 
     @torch.no_grad()
     def step(self, closure=None, scale: Union[float, torch.Tensor] = 1.0):
-        """One step; scale: see adamw."""
+        """One step; scale: see adamw. What is refused leaves every parameter, moment and count as it was."""
         loss = None
         if closure is not None:
             with torch.enable_grad():
                 loss = closure()
         t = self.steps + 1
+        calls = []
         for k, (group, ps, moments) in enumerate(self.lists()):
             beta1, beta2 = group["betas"]
-            adamw(ps, [p.grad if p.grad is None or p.grad.is_contiguous() else p.grad.contiguous() for p in ps], moments, t,
-                  group["lr"], beta1, beta2, group["eps"], group["weight_decay"], scale, self.seed + k)
+            grads = [p.grad if p.grad is None or p.grad.is_contiguous() else p.grad.contiguous() for p in ps]
+            args = _arguments(ps, grads, moments, t, group["lr"], beta1, beta2, group["eps"], group["weight_decay"], scale,
+                              self.seed + k)
+            calls.append((moments.device, args, ps, grads))
+        if len(calls) > 1:  # all of them before the first moves anything
+            for device, args, _, _ in calls:
+                _check(args[0], device)
+        for device, args, ps, grads in calls:
+            L._call("smat_adamw_step", device, args[0])
             # what a graph saved of those that moved is no longer what it saved
-            torch.autograd.graph.increment_version([p for p in ps if p.grad is not None])
+            torch.autograd.graph.increment_version([p for p, g in zip(ps, grads) if g is not None])
         self.steps = t
         return loss
 

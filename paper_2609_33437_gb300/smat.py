@@ -36,7 +36,7 @@ EXPORTED = ("smat_workspace_bytes", "smat_init", "smat_simulate_multi", "smat_gr
             "smat_pack8", "smat_unpack8", "smat_act_grad8", "smat_linear_poll_errors",
             "smat_norm", "smat_norm_grad_workspace_bytes", "smat_norm_grad",
             "smat_token_loss_workspace_bytes", "smat_token_loss", "smat_token_loss_grad_workspace_bytes", "smat_token_loss_grad",
-            "smat_adamw_places", "smat_adamw_step", "smat_adamw_values")
+            "smat_adamw_places", "smat_adamw_step", "smat_adamw_check", "smat_adamw_values")
 
 
 class AdamW(ctypes.Structure):
@@ -129,8 +129,10 @@ def load_library(build_if_missing: bool = True) -> ctypes.CDLL:
     L.smat_adamw_places.argtypes = [P, I32]
     L.smat_adamw_places.restype = I64
     L.smat_adamw_step.argtypes = [P, P]
+    L.smat_adamw_check.argtypes = [P]
     L.smat_adamw_values.argtypes = [P, P, P, P, P, P, I64, P]
-    for name in ("smat_norm", "smat_adamw_step", "smat_adamw_values", "smat_pack8", "smat_unpack8", "smat_act_grad8", "smat_linear_poll_errors"):
+    for name in ("smat_norm", "smat_adamw_step", "smat_adamw_check", "smat_adamw_values", "smat_pack8", "smat_unpack8", "smat_act_grad8",
+                 "smat_linear_poll_errors"):
         getattr(L, name).restype = I32
     L.smat_timing_enable.argtypes = [P, I32]
     L.smat_timing_read.argtypes = [P, P, P]

@@ -141,3 +141,22 @@ def test_moments_where_they_lie(bits):
     t.data = t.data[:0]
     with pytest.raises(ValueError, match="moments"):
         m.values() if bits == 8 else m._addresses()
+
+
+class _CheckOnly:
+    """A library whose step is the check alone."""
+
+    def __init__(self, lib):
+        self.smat_adamw_step, self.smat_last_error = lambda args, _: lib.smat_adamw_check(args), lib.smat_last_error
+
+
+@pytest.mark.parametrize("bad,code", [
+    (dict(dtype=2), UNSUPPORTED), (dict(bits=16), UNSUPPORTED), (dict(lr=-1.0), INVALID), (dict(beta1=1.0), INVALID),
+    (dict(eps=0.0), INVALID), (dict(step=0), INVALID), (dict(numels_at=0), INVALID), (dict(m2=4 * BASE + 16), ALIGNMENT),
+    (dict(bits=8, e1=5 * BASE, e2=5 * BASE), INVALID), (dict(lr_at=4 * BASE), INVALID),
+])
+def test_the_check_alone_refuses_the_same(lib, bad, code):
+    assert _call(_CheckOnly(lib), **bad) == _call(lib, **bad) == code
+    assert _call(_CheckOnly(lib), params=(BASE, BASE)) == INVALID
+    assert _call(_CheckOnly(lib), grads=(0, 0)) == 0
+    assert lib.smat_adamw_check(None) == INVALID

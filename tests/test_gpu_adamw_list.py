@@ -400,3 +400,42 @@ def test_a_parameter_without_a_gradient_is_untouched():
     assert w._version == versions[0] and v._version > versions[1]
     loss.backward()
     assert torch.equal(x.grad, torch.ones(4, 8, device="cuda") @ w.detach().T)
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+@pytest.mark.parametrize("why", ["eps of 0", "a gradient in its parameter's place", "a parameter that is not contiguous"])
+def test_a_refused_step_moves_nothing(why, bits):
+    """What is refused of a later list leaves the first as it was; the step is then as if it had been the first try."""
+    def make():
+        torch.manual_seed(3)
+        ps = [torch.nn.Parameter(torch.randn(300, device="cuda")), torch.nn.Parameter(torch.randn(16, 5, device="cuda").to(BF)),
+              torch.nn.Parameter(torch.randn(70, device="cuda").to(BF))]
+        return ps, O.AdamW([dict(params=ps[:1]), dict(params=ps[1:])], lr=1e-2, bits=bits, seed=5)
+
+    def grads(ps, t):
+        g = torch.Generator(device="cuda").manual_seed(t)
+        for p in ps:
+            p.grad = torch.randn(p.shape, generator=g, device="cuda").to(p.dtype)
+
+    ends = []
+    for interrupted in (False, True):
+        ps, opt = make()
+        for t in (1, 2):
+            grads(ps, t)
+            if interrupted:
+                before = [p.detach().clone() for p in ps] + [b.clone() for _, _, m in opt.lists() for b in m.buffers().values()]
+                was = ps[1].data, opt.param_groups[1]["eps"], ps[2].grad
+                if why == "eps of 0":
+                    opt.param_groups[1]["eps"] = 0.0
+                elif why == "a gradient in its parameter's place":
+                    ps[2].grad = ps[2].data
+                else:
+                    ps[1].data = torch.randn(5, 16, device="cuda").to(BF).t()
+                with pytest.raises((ValueError, S.SmatError)):
+                    opt.step()
+                ps[1].data, opt.param_groups[1]["eps"], ps[2].grad = was
+                after = [p.detach().clone() for p in ps] + [b.clone() for _, _, m in opt.lists() for b in m.buffers().values()]
+                assert opt.steps == t - 1 and all(torch.equal(a, b) for a, b in zip(before, after))
+            opt.step()
+        ends.append([p.detach().clone() for p in ps] + [b for _, _, m in opt.lists() for b in m.buffers().values()])
+    assert all(torch.equal(a, b) for a, b in zip(*ends))
