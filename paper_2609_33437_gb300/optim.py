@@ -187,15 +187,16 @@ def _check(args: bytes, device) -> None:
 class AdamW(torch.optim.Optimizer):
     """AdamW whose step is one launch for every group of parameters of one dtype (gradients then share one dtype, and every
     parameter without one is left as it is). bits 8 keeps two bytes of moments per element; with 32 the moments are fp32
-    whatever the parameters' type. The group's hyperparameters are those of torch.optim.AdamW. Its step count is one for all; in
-    a captured graph use `adamw` with a step on the device."""
+    whatever the parameters' type. The group's hyperparameters are those of torch.optim.AdamW, and so are the step counts, one for
+    each parameter, which its gradients count (parameters of one count are one launch); `steps` counts the calls. In a captured
+    graph use `adamw` with a step on the device."""
 
     def __init__(self, params, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.01, bits: int = 32,
                  seed: int = 0):
         if bits not in (8, 32):
             raise ValueError("bits: 8 or 32")
         self.bits, self.seed, self.steps = bits, int(seed), 0
-        self._lists = None
+        self._lists, self.counts = None, []
         super().__init__(params, dict(lr=lr, betas=tuple(betas), eps=eps, weight_decay=weight_decay))
 
     def add_param_group(self, group):
@@ -204,14 +205,14 @@ class AdamW(torch.optim.Optimizer):
         super().add_param_group(group)
 
     def lists(self):
-        """[(group, parameters of one dtype, their Moments)], laid out at the first step."""
+        """[(group, parameters of one dtype, their Moments)], laid out at the first step; `counts` holds their step counts."""
         if self._lists is None:
             lists = []
             for group in self.param_groups:
                 for dt in dict.fromkeys(p.dtype for p in group["params"]):
                     ps = [p for p in group["params"] if p.dtype is dt]
                     lists.append((group, ps, Moments(ps, self.bits)))
-            self._lists = lists
+            self._lists, self.counts = lists, [[0] * len(ps) for _, ps, _ in lists]
         return self._lists
 
     @torch.no_grad()
@@ -221,28 +222,35 @@ class AdamW(torch.optim.Optimizer):
         if closure is not None:
             with torch.enable_grad():
                 loss = closure()
-        t = self.steps + 1
         calls = []
         for k, (group, ps, moments) in enumerate(self.lists()):
             beta1, beta2 = group["betas"]
             grads = [p.grad if p.grad is None or p.grad.is_contiguous() else p.grad.contiguous() for p in ps]
-            args = _arguments(ps, grads, moments, t, group["lr"], beta1, beta2, group["eps"], group["weight_decay"], scale,
-                              self.seed + k)
-            calls.append((moments.device, args, ps, grads))
+            counts = self.counts[k]
+            there = {c for c, g in zip(counts, grads) if g is not None}
+            for t in there:
+                gs = grads if len(there) == 1 else [g if c == t else None for c, g in zip(counts, grads)]
+                args = _arguments(ps, gs, moments, t + 1, group["lr"], beta1, beta2, group["eps"], group["weight_decay"], scale,
+                                  self.seed + k)
+                calls.append((moments.device, args, ps, gs, counts))
         if len(calls) > 1:  # all of them before the first moves anything
-            for device, args, _, _ in calls:
+            for device, args, *_ in calls:
                 _check(args[0], device)
-        for device, args, ps, grads in calls:
+        for device, args, ps, gs, counts in calls:
             L._call("smat_adamw_step", device, args[0])
+            moved = [i for i, g in enumerate(gs) if g is not None]
             # what a graph saved of those that moved is no longer what it saved
-            torch.autograd.graph.increment_version([p for p, g in zip(ps, grads) if g is not None])
-        self.steps = t
+            torch.autograd.graph.increment_version([ps[i] for i in moved])
+            for i in moved:
+                counts[i] += 1
+        self.steps += 1
         return loss
 
     def state_dict(self):
-        """The step count, the moments' buffers list by list, and the groups' hyperparameters."""
-        return {"steps": self.steps, "bits": self.bits, "seed": self.seed,
-                "moments": [dict(sizes=list(m.sizes), **m.buffers()) for _, _, m in self.lists()],
+        """The step counts, the moments' buffers list by list, and the groups' hyperparameters."""
+        lists = self.lists()
+        return {"steps": self.steps, "counts": [list(c) for c in self.counts], "bits": self.bits, "seed": self.seed,
+                "moments": [dict(sizes=list(m.sizes), **m.buffers()) for _, _, m in lists],
                 "param_groups": [{k: v for k, v in g.items() if k != "params"} for g in self.param_groups]}
 
     def load_state_dict(self, state_dict):
@@ -252,6 +260,8 @@ class AdamW(torch.optim.Optimizer):
         if len(state_dict["param_groups"]) != len(self.param_groups):
             raise ValueError("the state is of other parameter groups")
         self.steps, self.seed = int(state_dict["steps"]), int(state_dict["seed"])
+        # (a state of before there were counts: one for all)
+        self.counts = [list(c) for c in state_dict.get("counts", [[self.steps] * len(ps) for _, ps, _ in lists])]
         for (_, _, m), saved in zip(lists, state_dict["moments"]):
             for name, t in m.buffers().items():
                 t.copy_(saved[name])

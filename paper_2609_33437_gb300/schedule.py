@@ -131,11 +131,12 @@ class PeriodicSmat:
         return len(steps) == 1
 
     def _own_fusable(self, opt) -> bool:
-        """One list of 32-bit moments of exactly this schedule's parameters, each with a contiguous gradient of one dtype."""
+        """One list of 32-bit moments of exactly this schedule's parameters, each with a contiguous gradient of one dtype, and all
+        with one step count."""
         if type(opt) is not optim.AdamW or opt.bits != 32 or len(opt.lists()) != 1 or torch.is_tensor(opt.param_groups[0]["lr"]):
             return False
         grads = [p.grad for p in self.params]
-        return ([id(p) for p in opt.lists()[0][1]] == [id(p) for p in self.params]
+        return ([id(p) for p in opt.lists()[0][1]] == [id(p) for p in self.params] and len(set(opt.counts[0])) == 1
                 and all(g is not None and g.is_contiguous() and g.dtype == grads[0].dtype for g in grads))
 
     def optimizer_step(self, step: int, opt):
@@ -151,11 +152,13 @@ class PeriodicSmat:
             return
         if self._own_fusable(opt):
             group, _, moments = opt.lists()[0]
+            t = opt.counts[0][0] + 1
             self._swap()
             beta1, beta2 = group["betas"]
             self.session.grad_map_adamw_multi(step, [p.grad for p in self.params], moments.views("m1"), moments.views("m2"),
                                               lr=group["lr"], beta1=beta1, beta2=beta2, eps=group["eps"],
-                                              weight_decay=group["weight_decay"], adam_step=opt.steps + 1)
+                                              weight_decay=group["weight_decay"], adam_step=t)
+            opt.counts[0] = [t] * len(self.params)
             opt.steps += 1
             self._refill_after()
             return

@@ -439,3 +439,82 @@ def test_a_refused_step_moves_nothing(why, bits):
             opt.step()
         ends.append([p.detach().clone() for p in ps] + [b for _, _, m in opt.lists() for b in m.buffers().values()])
     assert all(torch.equal(a, b) for a, b in zip(*ends))
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_a_first_gradient_that_comes_late(bits):
+    """Each parameter's step count is of its own gradients: a late one moves as it would by itself, and as with torch's."""
+    def make():
+        torch.manual_seed(4)
+        return [torch.nn.Parameter(torch.randn(300, device="cuda")) for _ in range(3)]
+
+    def grad(t, i):
+        g = torch.Generator(device="cuda").manual_seed(10 * t + i)
+        return torch.randn(300, generator=g, device="cuda")
+
+    there = lambda t, i: i == 0 or (i == 1 and t > 6) or (i == 2 and t % 3 == 0)  # noqa: E731
+    together, ref = make(), make()
+    opt, theirs = O.AdamW(together, lr=1e-2, bits=bits), torch.optim.AdamW(ref, lr=1e-2)
+    for t in range(1, 13):
+        for i in range(3):
+            together[i].grad = grad(t, i) if there(t, i) else None
+            ref[i].grad = grad(t, i) if there(t, i) else None
+        opt.step()
+        theirs.step()
+    assert opt.steps == 12 and opt.counts == [[12, 6, 4]]
+    state = opt.state_dict()
+    assert state["counts"] == [[12, 6, 4]]
+    if bits == 32:
+        for p, q in zip(together, ref):  # see test_optimizer_matches_torch
+            assert float((p - q).abs().max()) <= 12 * (12 * 1e-2 + 2 * 4.0) * 2.0 ** -24
+        for i in range(3):
+            alone = make()[i]
+            one = O.AdamW([alone], lr=1e-2)
+            for t in range(1, 13):
+                if there(t, i):
+                    alone.grad = grad(t, i)
+                    one.step()
+            assert torch.equal(alone, together[i])
+    else:
+        # a first step is one of lr, whenever it comes
+        alone = make()
+        late = O.AdamW(alone, lr=1e-2, bits=8, weight_decay=0.0)
+        for t in range(1, 4):
+            alone[0].grad = grad(t, 0)
+            late.step()
+        alone[1].grad, before = grad(9, 1), alone[1].detach().clone()
+        late.step()
+        assert float(((alone[1] - before).abs() - 1e-2).abs().max()) < 1e-5
+    again = O.AdamW(together, bits=bits)
+    again.load_state_dict(state)
+    assert again.counts == [[12, 6, 4]]
+    old = {k: v for k, v in state.items() if k != "counts"}
+    again.load_state_dict(old)
+    assert again.counts == [[12, 12, 12]]
+
+
+def test_schedule_with_step_counts_apart():
+    """A parameter whose gradients began later: the fused step has one count for all and is not taken."""
+    from paper_2609_33437_gb300.schedule import PeriodicSmat
+
+    def run(fused):
+        torch.manual_seed(5)
+        params = [torch.nn.Parameter(torch.randn(n, device="cuda") * 0.1) for n in (700, 64)]
+        theta0 = [p.detach() + 0.01 for p in params]
+        sched = PeriodicSmat(params, [0.5, 1.0], [1e-3] * 2, theta0=theta0, period=2, seed=1, alpha_min=0.5, alpha_max=1.0,
+                             alpha_mode=S.SMAT_ALPHA_GLOBAL, noise=S.SMAT_NOISE_UNIFORM)
+        opt = O.AdamW(params, lr=1e-2)
+        for step in range(4):
+            sched.before_forward(step)
+            sum((p.float() ** 2).sum() for p in (params[:1] if step == 0 else params)).backward()
+            if fused:
+                sched.optimizer_step(step, opt)
+            else:
+                sched.after_backward(step)
+                opt.step()
+            opt.zero_grad()
+        assert opt.steps == 4 and opt.counts == [[4, 3]]
+        sched.close()
+        return [p.detach().clone() for p in params] + [v.clone() for v in opt.lists()[0][2].values()]
+
+    assert all(torch.equal(a, b) for a, b in zip(run(True), run(False)))
