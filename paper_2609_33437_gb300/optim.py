@@ -62,7 +62,7 @@ class Moments:
             self._buffers = {"m1": torch.zeros(at, dtype=torch.float32, **kw), "m2": torch.zeros(at, dtype=torch.float32, **kw)}
         # what a call hands over of the list
         self._numels = struct.pack(f"{len(self.sizes)}q", *self.sizes)
-        self._pointers = struct.Struct(f"{len(self.sizes)}P")
+        self._pointers = f"{len(self.sizes)}P"
 
     def buffers(self) -> Dict[str, torch.Tensor]:
         """The buffers by name: m1 and m2, or q1, e1, q2 and e2. They may be read and written (a checkpoint), and moved away and
@@ -165,8 +165,7 @@ def _arguments(params, grads, moments, step, lr, beta1, beta2, eps, weight_decay
     t, step_at = _one("step", step, torch.int64, device)
     rate, lr_at = _one("lr", lr, torch.float32, device)
     by, scale_at = _one("scale", scale, torch.float32, device)
-    pack = moments._pointers.pack
-    arrays = ctypes.create_string_buffer(pack(*pp) + pack(*gp) + moments._numels)
+    arrays = ctypes.create_string_buffer(struct.pack(moments._pointers, *pp) + struct.pack(moments._pointers, *gp) + moments._numels)
     at = ctypes.addressof(arrays)
     args = _ADAMW.pack(at, at + 8 * n, at + 16 * n, *moments._addresses(), scale_at, lr_at, step_at, by, rate, beta1, beta2, eps,
                        weight_decay, t, seed & 0xFFFFFFFFFFFFFFFF, n, code, code if gdt is None else S.dtype_code(gdt),
@@ -198,6 +197,11 @@ class AdamW(torch.optim.Optimizer):
         self.bits, self.seed, self.steps = bits, int(seed), 0
         self._lists, self.counts = None, []
         super().__init__(params, dict(lr=lr, betas=tuple(betas), eps=eps, weight_decay=weight_decay))
+
+    def __getstate__(self):
+        """For copies and pickles, which torch.optim.Optimizer makes of its own fields alone."""
+        return {**super().__getstate__(), "bits": self.bits, "seed": self.seed, "steps": self.steps, "counts": self.counts,
+                "_lists": self._lists}
 
     def add_param_group(self, group):
         if self._lists is not None:

@@ -1,7 +1,9 @@
 """CPU-only checks of the AdamW step over many tensors: what the C ABI and the binding refuse before anything reaches a GPU
 (pointers here are numbers; none is read), and the 8-bit form's definition in `_adamw_ref`."""
 
+import copy
 import ctypes
+import pickle
 import struct
 
 import numpy as np
@@ -160,3 +162,30 @@ def test_the_check_alone_refuses_the_same(lib, bad, code):
     assert _call(_CheckOnly(lib), params=(BASE, BASE)) == INVALID
     assert _call(_CheckOnly(lib), grads=(0, 0)) == 0
     assert lib.smat_adamw_check(None) == INVALID
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+@pytest.mark.parametrize("laid_out", [False, True])
+@pytest.mark.parametrize("how", [copy.deepcopy, lambda v: pickle.loads(pickle.dumps(v))], ids=["deepcopy", "pickle"])
+def test_copies(how, laid_out, bits):
+    """A copied or pickled optimizer has its own parameters, moments and counts, which belong together as the original's do."""
+    ps = [torch.nn.Parameter(torch.ones(300)), torch.nn.Parameter(torch.ones(5, dtype=torch.bfloat16))]
+    opt = O.AdamW([dict(params=ps[:1]), dict(params=ps[1:], lr=0.5)], lr=0.25, bits=bits, seed=7)
+    if laid_out:
+        first = opt.lists()[0][2].buffers()
+        for k, b in enumerate(first.values()):
+            b.fill_(k + 2)
+        opt.steps, opt.counts[0][0] = 4, 3
+    new = how(opt)
+    assert (new.bits, new.seed, new.steps, new.counts) == (bits, 7, 4 if laid_out else 0, [[3], [0]] if laid_out else [])
+    assert [g["lr"] for g in new.param_groups] == [0.25, 0.5] and (new._lists is None) is not laid_out
+    lists = new.lists()
+    for (group, qs, moments), (_, _, old), mine in zip(lists, opt.lists(), new.param_groups):
+        assert group is mine and qs[0] is mine["params"][0] and qs[0] is not ps[0] and moments.sizes == old.sizes
+        for name, b in moments.buffers().items():
+            assert torch.equal(b, old.buffers()[name]) and b.data_ptr() != old.buffers()[name].data_ptr()
+        assert moments._addresses() != old._addresses()
+    new.counts[0][0] += 1
+    assert opt.counts[0][0] == (3 if laid_out else 0)
+    one = how(O.Moments(ps[:1], bits=bits))
+    assert one.sizes == [300] and one.places == 512

@@ -3,6 +3,8 @@
 every boundary, gradients that are missing, special values, what the device holds, graphs, long lists and long tensors; the
 optimizer class, its state, and the periodic schedule around it."""
 
+import copy
+
 import numpy as np
 import pytest
 import torch
@@ -518,3 +520,22 @@ def test_schedule_with_step_counts_apart():
         return [p.detach().clone() for p in params] + [v.clone() for v in opt.lists()[0][2].values()]
 
     assert all(torch.equal(a, b) for a, b in zip(run(True), run(False)))
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_a_copy_goes_on(bits):
+    """A deep copy of a model and its optimizer goes on with the same bits, each with its own state."""
+    ps = [torch.nn.Parameter(p) for p in _tensors(0, [300, 40], F32, 0.1)]
+    opt = O.AdamW(ps, lr=1e-2, bits=bits, seed=2)
+    for t in (1, 2):
+        for p, g in zip(ps, _tensors(t, [300, 40], F32, 1e-3)):
+            p.grad = g
+        opt.step()
+    qs, new = copy.deepcopy((ps, opt))
+    for params, o in ((ps, opt), (qs, new)):
+        for p, g in zip(params, _tensors(3, [300, 40], F32, 1e-3)):
+            p.grad = g
+        o.step()
+    assert new.counts == opt.counts == [[3, 3]] and all(torch.equal(p, q) and p is not q for p, q in zip(ps, qs))
+    for a, b in zip(opt.lists()[0][2].buffers().values(), new.lists()[0][2].buffers().values()):
+        assert torch.equal(a, b)
