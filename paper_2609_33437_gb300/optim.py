@@ -204,19 +204,32 @@ class AdamW(torch.optim.Optimizer):
                 "_lists": self._lists}
 
     def add_param_group(self, group):
-        if self._lists is not None:
-            raise RuntimeError("the moments are laid out: parameters cannot be added after the first step")
         super().add_param_group(group)
+        if self._lists is not None:  # further lists: those that are there keep their place
+            try:
+                self._lay_out(self.param_groups[-1])
+            except Exception:
+                self.param_groups.pop()
+                raise
+
+    def _lay_out(self, group):
+        lists = []
+        for dt in dict.fromkeys(p.dtype for p in group["params"]):
+            ps = [p for p in group["params"] if p.dtype is dt]
+            lists.append((group, ps, Moments(ps, self.bits)))
+        self._lists += lists
+        self.counts += [[0] * len(ps) for _, ps, _ in lists]
 
     def lists(self):
         """[(group, parameters of one dtype, their Moments)], laid out at the first step; `counts` holds their step counts."""
         if self._lists is None:
-            lists = []
-            for group in self.param_groups:
-                for dt in dict.fromkeys(p.dtype for p in group["params"]):
-                    ps = [p for p in group["params"] if p.dtype is dt]
-                    lists.append((group, ps, Moments(ps, self.bits)))
-            self._lists, self.counts = lists, [[0] * len(ps) for _, ps, _ in lists]
+            self._lists = []
+            try:
+                for group in self.param_groups:
+                    self._lay_out(group)
+            except Exception:
+                self._lists, self.counts = None, []
+                raise
         return self._lists
 
     @torch.no_grad()

@@ -189,3 +189,30 @@ def test_copies(how, laid_out, bits):
     assert opt.counts[0][0] == (3 if laid_out else 0)
     one = how(O.Moments(ps[:1], bits=bits))
     assert one.sizes == [300] and one.places == 512
+
+
+def test_groups_may_be_added():
+    """Before the moments are laid out, after (a saved state or `lists` lays them out), and after steps; what is there stays."""
+    ps = [torch.nn.Parameter(torch.ones(n)) for n in (300, 5, 7)]
+    opt = O.AdamW(ps[:1], lr=0.25, seed=7)
+    assert len(opt.state_dict()["moments"]) == 1
+    first = opt.lists()[0][2]
+    first.buffers()["m1"].fill_(2.0)
+    opt.counts[0][0] = 3
+    opt.add_param_group(dict(params=[ps[1], torch.nn.Parameter(torch.ones(4, dtype=torch.bfloat16))], lr=0.5))
+    assert [len(q) for _, q, _ in opt.lists()] == [1, 1, 1] and opt.counts == [[3], [0], [0]]
+    assert opt.lists()[0][2] is first and opt.lists()[1][0] is opt.param_groups[1] and opt.lists()[1][0]["lr"] == 0.5
+    with pytest.raises(ValueError):  # a parameter that is there
+        opt.add_param_group(dict(params=[ps[0]]))
+    with pytest.raises(ValueError, match="one device"):
+        opt.add_param_group(dict(params=[ps[2], torch.nn.Parameter(torch.ones(4, device="meta"))]))
+    assert len(opt.param_groups) == 2 and len(opt.lists()) == 3
+    opt.add_param_group(dict(params=[ps[2]]))
+    assert len(opt.param_groups) == 3 and opt.counts == [[3], [0], [0], [0]]
+    again = O.AdamW(ps[:1])
+    again.add_param_group(dict(params=ps[1:]))
+    assert [len(q) for _, q, _ in again.lists()] == [1, 2]
+    wrong = O.AdamW([ps[0], torch.nn.Parameter(torch.ones(4, device="meta"))])
+    for _ in range(2):
+        with pytest.raises(ValueError, match="one device"):
+            wrong.lists()

@@ -539,3 +539,26 @@ def test_a_copy_goes_on(bits):
     assert new.counts == opt.counts == [[3, 3]] and all(torch.equal(p, q) and p is not q for p, q in zip(ps, qs))
     for a, b in zip(opt.lists()[0][2].buffers().values(), new.lists()[0][2].buffers().values()):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_a_group_added_between_steps(bits):
+    """A layer that is trained from a later step on: it and what was there move as with torch's optimizer."""
+    torch.manual_seed(6)
+    ps = [torch.nn.Parameter(torch.randn(300, device="cuda")) for _ in range(2)]
+    qs = [torch.nn.Parameter(p.detach().clone()) for p in ps]
+    opt, ref = O.AdamW(ps[:1], lr=1e-2, bits=bits), torch.optim.AdamW(qs[:1], lr=1e-2)
+    for t in range(1, 7):
+        if t == 3:
+            opt.add_param_group(dict(params=ps[1:], lr=5e-3))
+            ref.add_param_group(dict(params=qs[1:], lr=5e-3))
+        for p, q, g in zip(ps, qs, _tensors(t, [300, 300], F32, 1.0)):
+            p.grad, q.grad = g.clone(), g.clone()
+        opt.step()
+        ref.step()
+    assert opt.counts == [[6], [4]]
+    # 32 bits: see test_optimizer_matches_torch; 8 bits: m1 and r are held to a step of 1/16 and 1/32 of their size, or of a group's
+    # largest / 2^16, so that an update, at most lr (1 - beta1) / sqrt(1 - beta2) = 3.2 lr, is off by 10% at most after each step
+    for p, q in zip(ps, qs):
+        tol = 6 * (12 * 1e-2 + 2 * 4.0) * 2.0 ** -24 if bits == 32 else 6 * 0.1 * 3.2e-2
+        assert float((p - q).abs().max()) <= tol
