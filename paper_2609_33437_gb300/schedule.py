@@ -160,7 +160,7 @@ class PeriodicSmat:
                                               weight_decay=group["weight_decay"], adam_step=t)
             opt.counts[0] = [t] * len(self.params)
             opt.steps += 1
-            self._refill_after()
+            self._stepped()
             return
         if not self._fusable(opt):
             self.after_backward(step)
@@ -183,6 +183,11 @@ class PeriodicSmat:
                                           weight_decay=g["weight_decay"], adam_step=t)
         for p in self.params:
             opt.state[p]["step"] += 1
+        self._stepped()
+
+    def _stepped(self):
+        """After a fused step: what a graph saved of the parameters is no longer what it saved, as after the optimizer's own."""
+        torch.autograd.graph.increment_version(self.params)
         self._refill_after()
 
     def _refill_after(self):

@@ -562,3 +562,26 @@ def test_a_group_added_between_steps(bits):
     for p, q in zip(ps, qs):
         tol = 6 * (12 * 1e-2 + 2 * 4.0) * 2.0 ** -24 if bits == 32 else 6 * 0.1 * 3.2e-2
         assert float((p - q).abs().max()) <= tol
+
+
+@pytest.mark.parametrize("make", [O.AdamW, torch.optim.AdamW])
+def test_a_graph_notices_the_fused_step(make):
+    """The step inside the gradient map raises the parameters' version, as an optimizer's own step does."""
+    from paper_2609_33437_gb300.schedule import PeriodicSmat
+
+    w = torch.nn.Parameter(torch.randn(8, 8, device="cuda"))
+    sched = PeriodicSmat([w], [0.5], [1e-3], theta0=[w.detach() + 0.01], period=1, seed=1, alpha_min=0.5, alpha_max=1.0,
+                         alpha_mode=S.SMAT_ALPHA_GLOBAL, noise=S.SMAT_NOISE_UNIFORM)
+    opt = make([w], lr=1e-2)
+    sched.before_forward(0)
+    x = torch.randn(4, 8, device="cuda", requires_grad=True)
+    loss = (x @ w).sum()
+    w.grad = torch.ones_like(w)
+    fused, session = [], sched.session
+    call = session.grad_map_adamw_multi
+    session.grad_map_adamw_multi = lambda *a, **k: (fused.append(1), call(*a, **k))
+    sched.optimizer_step(0, opt)
+    assert fused == [1]
+    with pytest.raises(RuntimeError, match="modified by an inplace"):
+        loss.backward()
+    sched.close()
