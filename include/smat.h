@@ -225,6 +225,21 @@ smat_status smat_grad_map_adamw_multi(smat_ctx* ctx, uint32_t step, const void* 
                                       float* const* m1, float* const* m2, int32_t gdtype,
                                       const smat_adamw* opt, smat_stream_t stream);
 
+/* The same with the hyperparameters in double: the constants fl(...) are those
+ * of smat_adamw_step, bit for bit, so that the two calls may share moments.
+ * (0.999 in fp32 makes 1 - beta2 off by 1.3e-5 of it.) */
+typedef struct {
+  double lr;            /* finite in fp32, >= 0 */
+  double beta1, beta2;  /* in [0, 1) */
+  double eps;           /* finite in fp32, >= 2^-126 */
+  double weight_decay;  /* finite in fp32, >= 0 */
+  int64_t step;         /* 1 .. 2^31 - 1 */
+} smat_adamw_double;
+
+smat_status smat_grad_map_adamw_double_multi(smat_ctx* ctx, uint32_t step, const void* const* g_sim,
+                                             float* const* m1, float* const* m2, int32_t gdtype,
+                                             const smat_adamw_double* opt, smat_stream_t stream);
+
 /* Parameter storage switch (Sec. 4.3): flips the active storage and returns
  * it in *active_out (0 = theta, the original storage; 1 = sim, theta~).
  * Host only: no device work, no copy. */
@@ -653,7 +668,8 @@ smat_status smat_token_loss_grad(const smat_token_loss_grad_args* args, void* d_
 /* ------------------------------------------------------------------ AdamW ---
  * The optimizer's update on ordinary steps: one AdamW step over a list of tensors in one launch (for every 1,300 tensors),
  * with moments in 32 bits or in 8. For every element, each operation rounded to fp32 in this order, as
- * smat_grad_map_adamw_multi does it:
+ * smat_grad_map_adamw_double_multi does it with the same constants (smat_grad_map_adamw_multi makes them of rounded
+ * hyperparameters):
  *   g = scale grad;  m1 = beta1 m1 + fl(1 - beta1) g;  m2 = beta2 m2 + fl(1 - beta2) (g g);  r = sqrt(m2)
  *   theta = fl(1 - lr wd) theta - fl(lr / (1 - beta1^t)) (m1 / (r / fl(sqrt(1 - beta2^t)) + eps))
  * and theta is rounded to its type. The constants fl(...) are computed in double and rounded once.

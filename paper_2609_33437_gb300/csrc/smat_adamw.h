@@ -1,6 +1,7 @@
 // What the host side of the AdamW step over many tensors (smat_adamw_host.cpp) and its kernels (smat_adamw.cu) share.
 #pragma once
 
+#include <cmath>
 #include <cstdint>
 
 #include <cuda_runtime.h>
@@ -25,6 +26,23 @@ struct Constants {  // computed in double, rounded once
   float b1, omb1, b2, omb2, eps;
   float decay, step, bc2, inv_bc2;  // 1 - lr wd, lr / (1 - b1^t), sqrt(1 - b2^t) and one over it
 };
+// 1 - beta^t (the logarithm of 0 is -infinity: its power is 0)
+inline double correction(double beta, double t) { return -std::expm1(t * std::log(beta)); }
+inline Constants constants_of(double lr, double beta1, double beta2, double eps, double weight_decay, double bc1, double bc2) {
+  return {(float)beta1, (float)(1.0 - beta1), (float)beta2, (float)(1.0 - beta2), (float)eps, (float)(1.0 - lr * weight_decay),
+          (float)(lr / bc1), (float)std::sqrt(bc2), (float)(1.0 / std::sqrt(bc2))};
+}
+inline bool within(double v, double low, double high) { return v >= low && v < high; }  // false for NaN
+// What is wrong with the hyperparameters, or NULL.
+inline const char* refuse(double lr, double beta1, double beta2, double eps, double weight_decay) {
+  const double huge = 3e38;  // finite in fp32
+  if (!within(lr, 0.0, huge)) return "lr must be finite and 0 or more";
+  if (!within(beta1, 0.0, 1.0) || !within(beta2, 0.0, 1.0)) return "betas must be in [0, 1)";
+  if (!within(eps, 1.1754944e-38, huge)) return "eps must be finite and at least 2^-126";
+  if (!within(weight_decay, 0.0, huge)) return "weight_decay must be finite and 0 or more";
+  return nullptr;
+}
+inline bool step_fits(int64_t t) { return t >= 1 && t < int64_t(1) << 31; }
 
 struct Call {
   Constants c;

@@ -31,8 +31,6 @@ int64_t places_of(const int64_t* numels, int32_t n) {
   return groups > (int64_t(1) << 40) ? -1 : groups * adamw::kGroup;
 }
 
-bool within(double v, double low, double high) { return v >= low && v < high; }  // false for NaN
-
 struct Range {
   uintptr_t begin, end;
   bool written;
@@ -81,14 +79,10 @@ smat_status check(const smat_adamw_args* a, bool* any) {
     return lfail(SMAT_ERR_UNSUPPORTED, "gradients' dtype %d not supported", a->grad_dtype);
   if (a->bits != 8 && a->bits != 32) return lfail(SMAT_ERR_UNSUPPORTED, "moments in %d bits not supported", a->bits);
   const double huge = 3e38;  // finite in fp32
-  if (!a->scale_at && !within(a->scale, -huge, huge)) return lfail(SMAT_ERR_INVALID_ARG, "scale must be finite");
-  if (!within(a->lr, 0.0, huge)) return lfail(SMAT_ERR_INVALID_ARG, "lr must be finite and 0 or more");
-  if (!within(a->beta1, 0.0, 1.0) || !within(a->beta2, 0.0, 1.0))
-    return lfail(SMAT_ERR_INVALID_ARG, "betas must be in [0, 1)");
-  if (!within(a->eps, 1.1754944e-38, huge)) return lfail(SMAT_ERR_INVALID_ARG, "eps must be finite and at least 2^-126");
-  if (!within(a->weight_decay, 0.0, huge))
-    return lfail(SMAT_ERR_INVALID_ARG, "weight_decay must be finite and 0 or more");
-  if (!a->step_at && (a->step < 1 || a->step >= (int64_t(1) << 31)))
+  if (!a->scale_at && !adamw::within(a->scale, -huge, huge)) return lfail(SMAT_ERR_INVALID_ARG, "scale must be finite");
+  if (const char* why = adamw::refuse(a->lr, a->beta1, a->beta2, a->eps, a->weight_decay))
+    return lfail(SMAT_ERR_INVALID_ARG, "%s", why);
+  if (!a->step_at && !adamw::step_fits(a->step))
     return lfail(SMAT_ERR_INVALID_ARG, "step %lld out of range", (long long)a->step);
   const int32_t n = a->n_tensors;
   const int64_t places = places_of(a->numels, n);
@@ -136,12 +130,10 @@ smat_status step(const smat_adamw_args* a, cudaStream_t stream) {
   adamw::Call c = {};
   const double t = (double)a->step;
   c.lr = a->lr, c.weight_decay = a->weight_decay;
-  c.log_b1 = std::log(a->beta1), c.log_b2 = std::log(a->beta2);  // -inf for 0: its power is 0
-  const double bc1 = a->step_at ? 1.0 : -std::expm1(t * c.log_b1), bc2 = a->step_at ? 1.0 : -std::expm1(t * c.log_b2);
-  c.bc1 = bc1;
-  c.c = {(float)a->beta1, (float)(1.0 - a->beta1), (float)a->beta2, (float)(1.0 - a->beta2), (float)a->eps,
-         (float)(1.0 - a->lr * a->weight_decay), (float)(a->lr / bc1), (float)std::sqrt(bc2),
-         (float)(1.0 / std::sqrt(bc2))};
+  c.log_b1 = std::log(a->beta1), c.log_b2 = std::log(a->beta2);  // as `correction` has them
+  const double bc2 = a->step_at ? 1.0 : adamw::correction(a->beta2, t);
+  c.bc1 = a->step_at ? 1.0 : adamw::correction(a->beta1, t);
+  c.c = adamw::constants_of(a->lr, a->beta1, a->beta2, a->eps, a->weight_decay, c.bc1, bc2);
   c.scale = (float)a->scale, c.scale_at = a->scale_at, c.lr_at = a->lr_at, c.step_at = a->step_at;
   c.seed_key = adamw::mix(adamw::mix((uint32_t)a->seed) ^ (uint32_t)(a->seed >> 32));
   c.key = adamw::mix(adamw::mix(c.seed_key ^ (uint32_t)a->step));

@@ -13,6 +13,7 @@
 #include <cuda_runtime.h>
 
 #include "smat.h"
+#include "smat_adamw.h"
 #include "smat_internal.h"
 
 using namespace smat;
@@ -726,21 +727,8 @@ smat_status smat_grad_map_multi(smat_ctx* c, uint32_t step, const void* const* g
   return SMAT_OK;
 }
 
-smat_status smat_grad_map_adamw_multi(smat_ctx* c, uint32_t step, const void* const* g_sim, float* const* m1,
-                                      float* const* m2, int32_t gdtype, const smat_adamw* opt,
-                                      smat_stream_t stream) {
-  if (!c) return fail(SMAT_ERR_INVALID_ARG, "ctx is NULL");
-  if (!opt) return fail(SMAT_ERR_INVALID_ARG, "opt is NULL");
-  if (gdtype != SMAT_F32 && gdtype != SMAT_BF16)
-    return fail(SMAT_ERR_UNSUPPORTED, "gradient dtype %d not supported", gdtype);
-  if (!(std::isfinite(opt->lr) && opt->lr >= 0.0f))
-    return fail(SMAT_ERR_INVALID_ARG, "lr must be finite and >= 0");
-  if (!(opt->beta1 >= 0.0f && opt->beta1 < 1.0f) || !(opt->beta2 >= 0.0f && opt->beta2 < 1.0f))
-    return fail(SMAT_ERR_INVALID_ARG, "beta1 and beta2 must lie in [0, 1)");
-  if (!(std::isfinite(opt->eps) && opt->eps > 0.0f)) return fail(SMAT_ERR_INVALID_ARG, "eps must be finite and > 0");
-  if (!(std::isfinite(opt->weight_decay) && opt->weight_decay >= 0.0f))
-    return fail(SMAT_ERR_INVALID_ARG, "weight_decay must be finite and >= 0");
-  if (opt->step < 1) return fail(SMAT_ERR_INVALID_ARG, "optimizer step %d: must be >= 1", opt->step);
+static smat_status grad_map_adamw(smat_ctx* c, uint32_t step, const void* const* g_sim, float* const* m1, float* const* m2,
+                                  int32_t gdtype, const AdamScalars& adam, smat_stream_t stream) {
   // same rule as the gradient map: the mask of the forward that produced the
   // gradient's theta~ (App. D)
   if (c->sim_step != (int64_t)step) {
@@ -795,15 +783,7 @@ smat_status smat_grad_map_adamw_multi(smat_ctx* c, uint32_t step, const void* co
     if (st != SMAT_OK) return st;
   }
   KArgs a = base_args(c, step);
-  const double b1 = opt->beta1, b2 = opt->beta2, tt = (double)opt->step;
-  a.adam.decay = (float)(1.0 - (double)opt->lr * (double)opt->weight_decay);
-  a.adam.b1 = opt->beta1;
-  a.adam.omb1 = (float)(1.0 - b1);
-  a.adam.b2 = opt->beta2;
-  a.adam.omb2 = (float)(1.0 - b2);
-  a.adam.bc2 = (float)std::sqrt(1.0 - std::pow(b2, tt));
-  a.adam.step = (float)((double)opt->lr / (1.0 - std::pow(b1, tt)));
-  a.adam.eps = opt->eps;
+  a.adam = adam;
   a.chunk_begin = 0;
   a.chunk_end = (int64_t)c->h_chunks.size();
   if (a.chunk_end <= 0) return SMAT_OK;
@@ -835,6 +815,53 @@ smat_status smat_grad_map_adamw_multi(smat_ctx* c, uint32_t step, const void* co
     if (e != cudaSuccess) return cuda_fail(e, "fused AdamW launch");
   }
   return SMAT_OK;
+}
+
+smat_status smat_grad_map_adamw_multi(smat_ctx* c, uint32_t step, const void* const* g_sim, float* const* m1,
+                                      float* const* m2, int32_t gdtype, const smat_adamw* opt,
+                                      smat_stream_t stream) {
+  if (!c) return fail(SMAT_ERR_INVALID_ARG, "ctx is NULL");
+  if (!opt) return fail(SMAT_ERR_INVALID_ARG, "opt is NULL");
+  if (gdtype != SMAT_F32 && gdtype != SMAT_BF16)
+    return fail(SMAT_ERR_UNSUPPORTED, "gradient dtype %d not supported", gdtype);
+  if (!(std::isfinite(opt->lr) && opt->lr >= 0.0f))
+    return fail(SMAT_ERR_INVALID_ARG, "lr must be finite and >= 0");
+  if (!(opt->beta1 >= 0.0f && opt->beta1 < 1.0f) || !(opt->beta2 >= 0.0f && opt->beta2 < 1.0f))
+    return fail(SMAT_ERR_INVALID_ARG, "beta1 and beta2 must lie in [0, 1)");
+  if (!(std::isfinite(opt->eps) && opt->eps > 0.0f)) return fail(SMAT_ERR_INVALID_ARG, "eps must be finite and > 0");
+  if (!(std::isfinite(opt->weight_decay) && opt->weight_decay >= 0.0f))
+    return fail(SMAT_ERR_INVALID_ARG, "weight_decay must be finite and >= 0");
+  if (opt->step < 1) return fail(SMAT_ERR_INVALID_ARG, "optimizer step %d: must be >= 1", opt->step);
+  AdamScalars adam;
+  const double b1 = opt->beta1, b2 = opt->beta2, tt = (double)opt->step;
+  adam.decay = (float)(1.0 - (double)opt->lr * (double)opt->weight_decay);
+  adam.b1 = opt->beta1;
+  adam.omb1 = (float)(1.0 - b1);
+  adam.b2 = opt->beta2;
+  adam.omb2 = (float)(1.0 - b2);
+  adam.bc2 = (float)std::sqrt(1.0 - std::pow(b2, tt));
+  adam.step = (float)((double)opt->lr / (1.0 - std::pow(b1, tt)));
+  adam.eps = opt->eps;
+  return grad_map_adamw(c, step, g_sim, m1, m2, gdtype, adam, stream);
+}
+
+smat_status smat_grad_map_adamw_double_multi(smat_ctx* c, uint32_t step, const void* const* g_sim, float* const* m1,
+                                             float* const* m2, int32_t gdtype, const smat_adamw_double* opt,
+                                             smat_stream_t stream) {
+  if (!c) return fail(SMAT_ERR_INVALID_ARG, "ctx is NULL");
+  if (!opt) return fail(SMAT_ERR_INVALID_ARG, "opt is NULL");
+  if (gdtype != SMAT_F32 && gdtype != SMAT_BF16)
+    return fail(SMAT_ERR_UNSUPPORTED, "gradient dtype %d not supported", gdtype);
+  if (const char* why = adamw::refuse(opt->lr, opt->beta1, opt->beta2, opt->eps, opt->weight_decay))
+    return fail(SMAT_ERR_INVALID_ARG, "%s", why);
+  if (!adamw::step_fits(opt->step))
+    return fail(SMAT_ERR_INVALID_ARG, "optimizer step %lld out of range", (long long)opt->step);
+  const double t = (double)opt->step;
+  const adamw::Constants k =
+      adamw::constants_of(opt->lr, opt->beta1, opt->beta2, opt->eps, opt->weight_decay, adamw::correction(opt->beta1, t),
+                          adamw::correction(opt->beta2, t));
+  const AdamScalars adam = {k.decay, k.b1, k.omb1, k.b2, k.omb2, k.bc2, k.step, k.eps};
+  return grad_map_adamw(c, step, g_sim, m1, m2, gdtype, adam, stream);
 }
 
 smat_status smat_swap(smat_ctx* c, int32_t* active_out) {

@@ -157,7 +157,7 @@ class PeriodicSmat:
             beta1, beta2 = group["betas"]
             self.session.grad_map_adamw_multi(step, [p.grad for p in self.params], moments.views("m1"), moments.views("m2"),
                                               lr=group["lr"], beta1=beta1, beta2=beta2, eps=group["eps"],
-                                              weight_decay=group["weight_decay"], adam_step=t)
+                                              weight_decay=group["weight_decay"], adam_step=t, double=True)
             opt.counts[0] = [t] * len(self.params)
             opt.steps += 1
             self._stepped()

@@ -6,7 +6,7 @@ no CPU fallback: if the library cannot be loaded the calls raise.
 
 Names follow the C ABI: smat_init -> SmatSession(...), smat_simulate_multi ->
 SmatSession.simulate_multi, smat_grad_map_multi -> SmatSession.grad_map_multi,
-smat_grad_map_adamw_multi -> SmatSession.grad_map_adamw_multi,
+smat_grad_map_adamw_multi, smat_grad_map_adamw_double_multi -> SmatSession.grad_map_adamw_multi,
 smat_swap -> SmatSession.swap, smat_mask_bits -> SmatSession.mask_bits,
 smat_tensor_scalars -> SmatSession.tensor_scalars.
 """
@@ -31,7 +31,7 @@ EXPORTED = ("smat_workspace_bytes", "smat_init", "smat_simulate_multi", "smat_gr
             "smat_delta_sigma_noalloc", "smat_timing_enable", "smat_timing_read", "smat_status_string",
             "smat_last_error", "smat_abi_version", "smat_refill_theta0", "smat_mark_theta0_resident",
             "smat_merge_workspace_bytes", "smat_merge", "smat_merge_ties_thresholds",
-            "smat_grad_map_adamw_multi", "smat_linear_workspace_bytes", "smat_grad_input_workspace_bytes",
+            "smat_grad_map_adamw_multi", "smat_grad_map_adamw_double_multi", "smat_linear_workspace_bytes", "smat_grad_input_workspace_bytes",
             "smat_grad_weight_workspace_bytes", "smat_linear", "smat_grad_input", "smat_grad_weight",
             "smat_pack8", "smat_unpack8", "smat_act_grad8", "smat_linear_poll_errors",
             "smat_norm", "smat_norm_grad_workspace_bytes", "smat_norm_grad",
@@ -44,6 +44,12 @@ class AdamW(ctypes.Structure):
     optimizer's own step count t >= 1."""
     _fields_ = [("lr", ctypes.c_float), ("beta1", ctypes.c_float), ("beta2", ctypes.c_float),
                 ("eps", ctypes.c_float), ("weight_decay", ctypes.c_float), ("step", ctypes.c_int32)]
+
+
+class AdamWDouble(ctypes.Structure):
+    """smat_adamw_double: the same in double."""
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
+                ("eps", ctypes.c_double), ("weight_decay", ctypes.c_double), ("step", ctypes.c_int64)]
 
 
 class SmatError(RuntimeError):
@@ -98,6 +104,7 @@ def load_library(build_if_missing: bool = True) -> ctypes.CDLL:
     L.smat_simulate_multi.argtypes = [P, U32, P]
     L.smat_grad_map_multi.argtypes = [P, U32, P, P, I32, I32, P]
     L.smat_grad_map_adamw_multi.argtypes = [P, U32, P, P, P, I32, ctypes.POINTER(AdamW), P]
+    L.smat_grad_map_adamw_double_multi.argtypes = [P, U32, P, P, P, I32, ctypes.POINTER(AdamWDouble), P]
     L.smat_swap.argtypes = [P, ctypes.POINTER(I32)]
     L.smat_active.argtypes = [P, ctypes.POINTER(I32)]
     L.smat_mask_bits.argtypes = [P, U32, I32, P, P]
@@ -141,7 +148,7 @@ def load_library(build_if_missing: bool = True) -> ctypes.CDLL:
     L.smat_last_error.argtypes = []
     L.smat_last_error.restype = ctypes.c_char_p
     L.smat_abi_version.restype = I32
-    for name in ("smat_init", "smat_simulate_multi", "smat_grad_map_multi", "smat_grad_map_adamw_multi",
+    for name in ("smat_init", "smat_simulate_multi", "smat_grad_map_multi", "smat_grad_map_adamw_multi", "smat_grad_map_adamw_double_multi",
                  "smat_swap", "smat_active",
                  "smat_mask_bits", "smat_tensor_scalars", "smat_destroy", "smat_debug_philox", "smat_debug_noise_unit",
                  "smat_poll_errors", "smat_debug_fused", "smat_timing_enable", "smat_timing_read",
@@ -294,9 +301,11 @@ class SmatSession:
     def grad_map_adamw_multi(self, step: int, g_sims: Sequence[torch.Tensor], m1s: Sequence[torch.Tensor],
                              m2s: Sequence[torch.Tensor], lr: float, beta1: float = 0.9, beta2: float = 0.999,
                              eps: float = 1e-8, weight_decay: float = 0.0, adam_step: int = 1,
-                             stream: Optional[torch.cuda.Stream] = None):
+                             stream: Optional[torch.cuda.Stream] = None, double: bool = False):
         """The gradient map fused with one AdamW step: theta (the descriptors'
-        own storage) and the fp32 moments m1s, m2s are updated in place."""
+        own storage) and the fp32 moments m1s, m2s are updated in place. The
+        hyperparameters are rounded to fp32 first, or with `double` taken as
+        they are, for the constants of optim.adamw bit for bit."""
         if len(g_sims) != self.n or len(m1s) != self.n or len(m2s) != self.n:
             raise ValueError("one gradient and two moment buffers per tensor expected")
         gd = None
@@ -308,10 +317,11 @@ class SmatSession:
             gd = dtype_code(dt)
         gp, p1, p2 = _pointers(g_sims, self._array), _pointers(m1s, self._array), _pointers(m2s, self._array)
         self._gkeep = (list(g_sims), list(m1s), list(m2s))
-        opt = AdamW(float(lr), float(beta1), float(beta2), float(eps), float(weight_decay), int(adam_step))
-        check("smat_grad_map_adamw_multi",
-              self._L.smat_grad_map_adamw_multi(self._ctx, int(step), gp, p1, p2, SMAT_F32 if gd is None else gd,
-                                                ctypes.byref(opt), _stream_handle(stream)))
+        name = "smat_grad_map_adamw_double_multi" if double else "smat_grad_map_adamw_multi"
+        opt = (AdamWDouble if double else AdamW)(float(lr), float(beta1), float(beta2), float(eps), float(weight_decay),
+                                                 int(adam_step))
+        check(name, getattr(self._L, name)(self._ctx, int(step), gp, p1, p2, SMAT_F32 if gd is None else gd,
+                                           ctypes.byref(opt), _stream_handle(stream)))
 
     def _refuse_adamw(self, g_sims, m1s, m2s):
         """Raise what is wrong with the first tensor that cannot be taken."""

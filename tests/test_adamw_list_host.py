@@ -216,3 +216,8 @@ def test_groups_may_be_added():
     for _ in range(2):
         with pytest.raises(ValueError, match="one device"):
             wrong.lists()
+
+
+def test_the_fused_step_in_double_refuses(lib):
+    opt = S.AdamWDouble(1e-3, 0.9, 0.999, 1e-8, 0.0, 1)
+    assert lib.smat_grad_map_adamw_double_multi(None, 0, None, None, None, 0, ctypes.byref(opt), None) == INVALID

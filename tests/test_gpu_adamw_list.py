@@ -585,3 +585,48 @@ def test_a_graph_notices_the_fused_step(make):
     with pytest.raises(RuntimeError, match="modified by an inplace"):
         loss.backward()
     sched.close()
+
+
+@pytest.mark.parametrize("dt", [F32, BF])
+@pytest.mark.parametrize("hyper", [dict(lr=1e-3), dict(lr=3e-4, betas=(0.9, 0.95), eps=1e-6, weight_decay=0.1)])
+def test_fused_step_has_the_list_steps_constants(hyper, dt):
+    """With hyperparameters that fp32 does not hold: the gradient map with the step inside, and the map and a step of its own, the
+    same bits, over steps of either kind."""
+    from paper_2609_33437_gb300.schedule import PeriodicSmat
+
+    def run(fused):
+        torch.manual_seed(2)
+        params = [torch.nn.Parameter((torch.randn(n, device="cuda") * 0.1).to(dt)) for n in (7000, 64)]
+        theta0 = [(p.detach() + 0.01).to(dt) for p in params]
+        sched = PeriodicSmat(params, [0.5, 1.0], [1e-3] * 2, theta0=theta0, period=2, seed=1, alpha_min=0.5, alpha_max=1.0,
+                             alpha_mode=S.SMAT_ALPHA_GLOBAL, noise=S.SMAT_NOISE_UNIFORM)
+        opt = O.AdamW(params, **hyper)
+        for step in range(6):
+            sched.before_forward(step)
+            sum((p.float() ** 2).sum() for p in params).backward()
+            if fused:
+                sched.optimizer_step(step, opt)
+            else:
+                sched.after_backward(step)
+                opt.step()
+            opt.zero_grad()
+        sched.close()
+        return [p.detach().clone() for p in params] + [v.clone() for v in opt.lists()[0][2].values()]
+
+    assert all(torch.equal(a, b) for a, b in zip(run(True), run(False)))
+
+
+def test_fused_step_in_double_refuses():
+    theta = [torch.ones(300, device="cuda")]
+    sim, theta0, g, m1, m2 = ([torch.full((300,), v, device="cuda")] for v in (0.0, 0.5, 1.0, 0.0, 0.0))
+    session = S.SmatSession(theta, theta0, sim, [0.5], [1e-3])
+    session.simulate_multi(0)
+    good = dict(lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, adam_step=1)
+    for bad in (dict(lr=-1.0), dict(lr=float("nan")), dict(lr=1e39), dict(beta1=1.0), dict(beta2=-0.1), dict(eps=0.0), dict(eps=1e-39),
+                dict(weight_decay=-1.0), dict(adam_step=0), dict(adam_step=1 << 31)):
+        with pytest.raises(S.SmatError):
+            session.grad_map_adamw_multi(0, g, m1, m2, **{**good, **bad}, double=True)
+    assert bool((theta[0] == 1).all()) and not bool(m1[0].any())
+    session.grad_map_adamw_multi(0, g, m1, m2, **good, double=True)
+    assert bool((theta[0] != 1).any()) and bool(m1[0].any())
+    session.close()
