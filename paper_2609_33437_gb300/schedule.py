@@ -153,11 +153,7 @@ class PeriodicSmat:
         if self._own_fusable(opt):
             group, _, moments = opt.lists()[0]
             t = opt.counts[0][0] + 1
-            self._swap()
-            beta1, beta2 = group["betas"]
-            self.session.grad_map_adamw_multi(step, [p.grad for p in self.params], moments.views("m1"), moments.views("m2"),
-                                              lr=group["lr"], beta1=beta1, beta2=beta2, eps=group["eps"],
-                                              weight_decay=group["weight_decay"], adam_step=t, double=True)
+            self._fused_step(step, [p.grad for p in self.params], moments.views("m1"), moments.views("m2"), group, t, double=True)
             opt.counts[0] = [t] * len(self.params)
             opt.steps += 1
             self._stepped()
@@ -174,16 +170,22 @@ class PeriodicSmat:
                 st["exp_avg"] = torch.zeros_like(p, memory_format=torch.preserve_format)
                 st["exp_avg_sq"] = torch.zeros_like(p, memory_format=torch.preserve_format)
         t = int(float(opt.state[self.params[0]]["step"])) + 1
-        grads = [p.grad for p in self.params]
-        self._swap()
-        beta1, beta2 = g["betas"]
-        self.session.grad_map_adamw_multi(step, grads, [opt.state[p]["exp_avg"] for p in self.params],
-                                          [opt.state[p]["exp_avg_sq"] for p in self.params], lr=g["lr"],
-                                          beta1=beta1, beta2=beta2, eps=g["eps"],
-                                          weight_decay=g["weight_decay"], adam_step=t)
+        self._fused_step(step, [p.grad for p in self.params], [opt.state[p]["exp_avg"] for p in self.params],
+                         [opt.state[p]["exp_avg_sq"] for p in self.params], g, t)
         for p in self.params:
             opt.state[p]["step"] += 1
         self._stepped()
+
+    def _fused_step(self, step: int, grads, m1s, m2s, group, t: int, double: bool = False):
+        """The storage switched back and the fused call; one that is refused leaves the storage as it was."""
+        beta1, beta2 = group["betas"]
+        self._swap()
+        try:
+            self.session.grad_map_adamw_multi(step, grads, m1s, m2s, lr=group["lr"], beta1=beta1, beta2=beta2, eps=group["eps"],
+                                              weight_decay=group["weight_decay"], adam_step=t, double=double)
+        except Exception:
+            self._swap()
+            raise
 
     def _stepped(self):
         """After a fused step: what a graph saved of the parameters is no longer what it saved, as after the optimizer's own."""

@@ -630,3 +630,32 @@ def test_fused_step_in_double_refuses():
     session.grad_map_adamw_multi(0, g, m1, m2, **good, double=True)
     assert bool((theta[0] != 1).any()) and bool(m1[0].any())
     session.close()
+
+
+@pytest.mark.parametrize("make", [O.AdamW, torch.optim.AdamW])
+def test_a_refused_fused_step_may_be_tried_again(make):
+    """The parameters' storage and the optimizer are as before the refusal, and the step is then as at the first try."""
+    from paper_2609_33437_gb300.schedule import PeriodicSmat
+
+    def run(refused):
+        torch.manual_seed(2)
+        params = [torch.nn.Parameter(torch.randn(n, device="cuda") * 0.1) for n in (700, 64)]
+        sched = PeriodicSmat(params, [0.5, 1.0], [1e-3] * 2, theta0=[p.detach() + 0.01 for p in params], period=2, seed=1,
+                             alpha_min=0.5, alpha_max=1.0, alpha_mode=S.SMAT_ALPHA_GLOBAL, noise=S.SMAT_NOISE_UNIFORM)
+        opt = make(params, lr=1e-2)
+        for step in range(4):
+            sched.before_forward(step)
+            sum((p.float() ** 2).sum() for p in params).backward()
+            if refused and step % 2:
+                there = [p.data_ptr() for p in params]
+                opt.param_groups[0]["eps"] = 0.0
+                with pytest.raises(S.SmatError):
+                    sched.optimizer_step(step, opt)
+                opt.param_groups[0]["eps"] = 1e-8
+                assert [p.data_ptr() for p in params] == there
+            sched.optimizer_step(step, opt)
+            opt.zero_grad()
+        sched.close()
+        return [p.detach().clone() for p in params]
+
+    assert all(torch.equal(a, b) for a, b in zip(run(True), run(False)))
