@@ -125,8 +125,8 @@ def _no_graph(a: torch.Tensor, b: Optional[torch.Tensor] = None, c: Optional[tor
     """The operators' results belong to no graph: refuses what autograd would lose without a word. (0.3 us of a call.)"""
     if torch.is_grad_enabled() and (a.requires_grad or (b is not None and b.requires_grad)
                                     or (c is not None and c.requires_grad) or (d is not None and d.requires_grad)):
-        raise ValueError("the operator builds no graph, and an argument requires a gradient: use Linear8 or Mlp8, "
-                         "torch.no_grad() or detach()")
+        raise ValueError("the operator builds no graph, and an argument requires a gradient: use a layer or the differentiable "
+                         "form (Linear8, Mlp8, norm.Norm, loss.cross_entropy), torch.no_grad() or detach()")
     if forward_ad._current_level >= 0:
         for t in (a, b, c, d):
             if t is not None and forward_ad.unpack_dual(t).tangent is not None:

@@ -87,3 +87,10 @@ def test_binding_checks_the_weights():
         N._weights(8, torch.bfloat16, meta, torch.zeros(8), torch.zeros(8, dtype=torch.bfloat16))
     with pytest.raises(ValueError, match="w: must be"):
         N._weights(8, torch.float32, meta, torch.zeros(9), None)
+
+
+def test_a_gradient_that_would_be_lost_names_the_layers():
+    x = torch.zeros(2, 4, requires_grad=True)
+    for call in (lambda: N.norm(x), lambda: N.norm_grad(x, x, x)):
+        with pytest.raises(ValueError, match="norm.Norm, loss.cross_entropy"):
+            call()
