@@ -564,19 +564,22 @@ dim3 block_of(int64_t cols, int per_thread, int threads) {
 // and 93, 36 and 145), in fp32 back through long rows alone (4095: 125 and 166; 1023: 45 and 21; forward 4095: 127 and 109).
 enum Way { kWhole, kShifted, kSingly };
 
-// Runs f with types, a vector and whether rows are shifted: f(T, W, integral_constant VEC, bool_constant SHIFT)
-template <class T, class W, class F>
+// Runs f with types, a vector and whether rows are shifted: f(T, W, integral_constant VEC, bool_constant SHIFT). F32_SHIFTS: fp32
+// rows may be.
+template <class T, class W, bool SHIFTS, class F>
 cudaError_t with_vec(Way way, F&& f) {
   constexpr int kWide = 16 / (int)sizeof(T);
   if (way == kWhole) return f(T(), W(), std::integral_constant<int, kWide>(), std::false_type());
-  if (way == kShifted) return f(T(), W(), std::integral_constant<int, kWide>(), std::true_type());
+  if constexpr (SHIFTS) {
+    if (way == kShifted) return f(T(), W(), std::integral_constant<int, kWide>(), std::true_type());
+  }
   return f(T(), W(), std::integral_constant<int, 1>(), std::false_type());
 }
-template <class F>
+template <bool F32_SHIFTS, class F>
 cudaError_t with_types(int dtype, int weight_dtype, Way way, F&& f) {
-  if (dtype == SMAT_F32) return with_vec<float, float>(way, f);
-  if (weight_dtype == SMAT_F32) return with_vec<bf16, float>(way, f);
-  return with_vec<bf16, bf16>(way, f);
+  if (dtype == SMAT_F32) return with_vec<float, float, F32_SHIFTS>(way, f);
+  if (weight_dtype == SMAT_F32) return with_vec<bf16, float, true>(way, f);
+  return with_vec<bf16, bf16, true>(way, f);
 }
 
 // Matrices of a call, those that are there
@@ -609,7 +612,7 @@ int64_t whole_steps(int64_t ctas) { return (ctas + 7) / 8 * 8; }
 
 cudaError_t launch_forward(const Forward& a, int dtype, int weight_dtype, int sms, cudaStream_t s) {
   const Way way = Lie(dtype, a.rows, a.cols).add(a.x, a.ldx).add(a.r, a.ldr).add(a.h, a.ldh).add(a.y, a.ldy).way(a.w, a.b, dtype == SMAT_BF16);
-  return with_types(dtype, weight_dtype, way, [&](auto t, auto w, auto vec, auto shift) {
+  return with_types<false>(dtype, weight_dtype, way, [&](auto t, auto w, auto vec, auto shift) {
     using T = decltype(t);
     using W = decltype(w);
     constexpr int VEC = decltype(vec)::value;
@@ -674,7 +677,7 @@ cudaError_t launch_backward(const Backward& given, int dtype, int weight_dtype, 
                       .add(a.dx ? a.dh : nullptr, a.lddh)
                       .add(a.dx, a.lddx)
                       .way(a.w, nullptr, dtype == SMAT_BF16 || a.cols > 2048);
-  return with_types(dtype, weight_dtype, way, [&](auto t, auto w, auto vec, auto shift) {
+  return with_types<true>(dtype, weight_dtype, way, [&](auto t, auto w, auto vec, auto shift) {
     using T = decltype(t);
     using W = decltype(w);
     constexpr int VEC = decltype(vec)::value;
@@ -704,9 +707,10 @@ cudaError_t launch_backward(const Backward& given, int dtype, int weight_dtype, 
         return cudaGetLastError();
       };
       using std::integral_constant;
-      if (shape.each == 8)
-        e = go(integral_constant<int, 8>(), integral_constant<int, 256>(), integral_constant<int, sizeof(T) == 4 ? 2 : 3>());
-      else if (shape.threads == 256)
+      if (shape.each == 8) {
+        if constexpr (!(SHIFT && sizeof(T) == 4))  // shifted rows of fp32 are longer
+          e = go(integral_constant<int, 8>(), integral_constant<int, 256>(), integral_constant<int, sizeof(T) == 4 ? 2 : 3>());
+      } else if (shape.threads == 256)
         e = go(integral_constant<int, 16>(), integral_constant<int, 256>(), integral_constant<int, 2>());
       else if (shape.threads == 512 && shape.each == 16)
         e = go(integral_constant<int, 16>(), integral_constant<int, 512>(), integral_constant<int, 1>());
