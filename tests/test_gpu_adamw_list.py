@@ -659,3 +659,53 @@ def test_a_refused_fused_step_may_be_tried_again(make):
         return [p.detach().clone() for p in params]
 
     assert all(torch.equal(a, b) for a, b in zip(run(True), run(False)))
+
+
+def test_schedule_around_moments_in_8_bits():
+    """The fused step holds 32 bits: on a simulated-loss step the gradient is mapped and an AdamW of 8 bits makes a step of its own."""
+    from paper_2609_33437_gb300.schedule import PeriodicSmat
+
+    def run(by_schedule):
+        torch.manual_seed(2)
+        params = [torch.nn.Parameter((torch.randn(n, device="cuda") * 0.1).to(BF)) for n in (700, 64)]
+        sched = PeriodicSmat(params, [0.5, 1.0], [1e-3] * 2, theta0=[(p.detach() + 0.01).to(BF) for p in params], period=2, seed=1,
+                             alpha_min=0.5, alpha_max=1.0, alpha_mode=S.SMAT_ALPHA_GLOBAL, noise=S.SMAT_NOISE_UNIFORM)
+        opt = O.AdamW(params, lr=1e-2, bits=8, seed=3)
+        for step in range(4):
+            sched.before_forward(step)
+            sum((p.float() ** 2).sum() for p in params).backward()
+            if by_schedule:
+                sched.optimizer_step(step, opt)
+            else:
+                sched.after_backward(step)
+                opt.step()
+            opt.zero_grad()
+        assert opt.steps == 4 and opt.counts == [[4, 4]]
+        sched.close()
+        return [p.detach().clone() for p in params] + list(opt.lists()[0][2].buffers().values())
+
+    assert all(torch.equal(a, b) for a, b in zip(run(True), run(False)))
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+@pytest.mark.parametrize("device", [False, True])
+def test_optimizer_step_scale_closure_and_strided_gradients(device, bits):
+    """A scale, gradients that are not contiguous and a closure: the bits of the call with these gradients."""
+    start, g = torch.randn(24, 40, device="cuda"), torch.randn(40, 24, device="cuda")
+    p = torch.nn.Parameter(start.clone())
+    opt = O.AdamW([p], lr=1e-2, bits=bits, seed=9)
+    scale = torch.full((1,), 0.25, device="cuda") if device else 0.25
+
+    def closure():
+        assert torch.is_grad_enabled()
+        p.grad = g.t()
+        return torch.tensor(3.0)
+
+    q, moments = start.clone(), O.Moments([start], bits=bits)
+    for t in (1, 2, 3):
+        assert float(opt.step(closure, scale=scale)) == 3.0
+        assert not p.grad.is_contiguous() and torch.equal(p.grad, g.t())
+        O.adamw([q], [g.t().contiguous()], moments, t, lr=1e-2, scale=0.25, seed=9)
+        assert torch.equal(p.detach(), q)
+    for a, b in zip(opt.lists()[0][2].buffers().values(), moments.buffers().values()):
+        assert torch.equal(a, b)
