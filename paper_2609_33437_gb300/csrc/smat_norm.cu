@@ -560,8 +560,10 @@ dim3 block_of(int64_t cols, int per_thread, int threads) {
 }
 
 // How rows are read: whole vectors from 16 bytes on, vectors of memory that a row starts inside of, or element by element. The
-// second pays in bf16 (4099 x 1023 and 4095, layer norm with residual 19 and 82 us, element by element 25 and 112; back with dh 32
-// and 93, 36 and 145), in fp32 back through long rows alone (4095: 125 and 166; 1023: 45 and 21; forward 4095: 127 and 109).
+// second pays forward in bf16 from some 800 columns on (4099 rows, layer norm with residual, us, shifted and one by one: 255 columns
+// 12.5 and 7.6, 511 16.9 and 16.8, 767 20 and 18, 1023 19 and 22 to 26, 2039 34 and 42, 4095 72 and 105; in fp32 not: 4095 127 and
+// 109), and back through long rows (with dh, bf16: 1023 31 and 18, 2039 37 and 32, 4095 100 and 137, 2048 x 11007 86 and 298; fp32:
+// 1023 45 and 21, 4095 82 and 152, 2048 x 11007 120 and 247).
 enum Way { kWhole, kShifted, kSingly };
 
 // Runs f with types, a vector and whether rows are shifted: f(T, W, integral_constant VEC, bool_constant SHIFT). F32_SHIFTS: fp32
@@ -611,7 +613,7 @@ int64_t whole_steps(int64_t ctas) { return (ctas + 7) / 8 * 8; }
 }  // namespace
 
 cudaError_t launch_forward(const Forward& a, int dtype, int weight_dtype, int sms, cudaStream_t s) {
-  const Way way = Lie(dtype, a.rows, a.cols).add(a.x, a.ldx).add(a.r, a.ldr).add(a.h, a.ldh).add(a.y, a.ldy).way(a.w, a.b, dtype == SMAT_BF16);
+  const Way way = Lie(dtype, a.rows, a.cols).add(a.x, a.ldx).add(a.r, a.ldr).add(a.h, a.ldh).add(a.y, a.ldy).way(a.w, a.b, dtype == SMAT_BF16 && a.cols > 800);
   return with_types<false>(dtype, weight_dtype, way, [&](auto t, auto w, auto vec, auto shift) {
     using T = decltype(t);
     using W = decltype(w);
@@ -676,7 +678,7 @@ cudaError_t launch_backward(const Backward& given, int dtype, int weight_dtype, 
                       .add(a.h, a.ldh)
                       .add(a.dx ? a.dh : nullptr, a.lddh)
                       .add(a.dx, a.lddx)
-                      .way(a.w, nullptr, dtype == SMAT_BF16 || a.cols > 2048);
+                      .way(a.w, nullptr, a.cols > 2048);
   return with_types<true>(dtype, weight_dtype, way, [&](auto t, auto w, auto vec, auto shift) {
     using T = decltype(t);
     using W = decltype(w);
@@ -708,7 +710,7 @@ cudaError_t launch_backward(const Backward& given, int dtype, int weight_dtype, 
       };
       using std::integral_constant;
       if (shape.each == 8) {
-        if constexpr (!(SHIFT && sizeof(T) == 4))  // shifted rows of fp32 are longer
+        if constexpr (!SHIFT)  // shifted rows are longer
           e = go(integral_constant<int, 8>(), integral_constant<int, 256>(), integral_constant<int, sizeof(T) == 4 ? 2 : 3>());
       } else if (shape.threads == 256)
         e = go(integral_constant<int, 16>(), integral_constant<int, 256>(), integral_constant<int, 2>());
