@@ -271,16 +271,25 @@ class AdamW(torch.optim.Optimizer):
                 "param_groups": [{k: v for k, v in g.items() if k != "params"} for g in self.param_groups]}
 
     def load_state_dict(self, state_dict):
+        """What does not fit is refused before anything is taken."""
         lists = self.lists()
-        if state_dict["bits"] != self.bits or [m["sizes"] for m in state_dict["moments"]] != [m.sizes for _, _, m in lists]:
+        saved = state_dict["moments"]
+        if state_dict["bits"] != self.bits or [m["sizes"] for m in saved] != [m.sizes for _, _, m in lists]:
             raise ValueError("the state is of other parameters, or of moments in other bits")
         if len(state_dict["param_groups"]) != len(self.param_groups):
             raise ValueError("the state is of other parameter groups")
-        self.steps, self.seed = int(state_dict["steps"]), int(state_dict["seed"])
+        steps, seed = int(state_dict["steps"]), int(state_dict["seed"])
         # (a state of before there were counts: one for all)
-        self.counts = [list(c) for c in state_dict.get("counts", [[self.steps] * len(ps) for _, ps, _ in lists])]
-        for (_, _, m), saved in zip(lists, state_dict["moments"]):
+        counts = [[int(c) for c in cs] for cs in state_dict.get("counts", [[steps] * len(ps) for _, ps, _ in lists])]
+        if [len(c) for c in counts] != [len(ps) for _, ps, _ in lists]:
+            raise ValueError("the state's step counts are of other parameters")
+        for (_, _, m), there in zip(lists, saved):
             for name, t in m.buffers().items():
-                t.copy_(saved[name])
-        for group, saved in zip(self.param_groups, state_dict["param_groups"]):
-            group.update(saved)
+                if name not in there or there[name].shape != t.shape or there[name].dtype is not t.dtype:
+                    raise ValueError(f"the state's {name} is missing or of another form")
+        self.steps, self.seed, self.counts = steps, seed, counts
+        for (_, _, m), there in zip(lists, saved):
+            for name, t in m.buffers().items():
+                t.copy_(there[name])
+        for group, there in zip(self.param_groups, state_dict["param_groups"]):
+            group.update(there)

@@ -221,3 +221,32 @@ def test_groups_may_be_added():
 def test_the_fused_step_in_double_refuses(lib):
     opt = S.AdamWDouble(1e-3, 0.9, 0.999, 1e-8, 0.0, 1)
     assert lib.smat_grad_map_adamw_double_multi(None, 0, None, None, None, 0, ctypes.byref(opt), None) == INVALID
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_a_state_that_does_not_fit_changes_nothing(bits):
+    ps = [torch.nn.Parameter(torch.ones(300)), torch.nn.Parameter(torch.ones(5))]
+    opt, other = (O.AdamW(ps, lr=lr, bits=bits, seed=seed) for lr, seed in ((0.25, 7), (0.5, 8)))
+    opt.lists()[0][2].buffers()["e1" if bits == 8 else "m1"].fill_(9)
+    opt.counts[0][:] = [3, 2]
+    other.lists()
+    name = "q1" if bits == 8 else "m2"
+
+    def state(**change):
+        s = opt.state_dict()
+        s.update(change)
+        return s
+
+    moments = opt.state_dict()["moments"][0]
+    wrong = [state(counts=[[3]]), state(counts=[]), state(counts=[[3, 2], [1]]), state(param_groups=[]), state(bits=40 - bits),
+             state(moments=[{k: v for k, v in moments.items() if k != name}]),
+             state(moments=[{**moments, name: moments[name][:-1]}]), state(moments=[{**moments, name: moments[name].double()}])]
+    before = {k: v.clone() for k, v in other.lists()[0][2].buffers().items()}
+    for s in wrong:
+        with pytest.raises(ValueError, match="state"):
+            other.load_state_dict(s)
+        assert (other.counts, other.seed, other.param_groups[0]["lr"]) == ([[0, 0]], 8, 0.5)
+        assert all(torch.equal(v, before[k]) for k, v in other.lists()[0][2].buffers().items())
+    other.load_state_dict(state())
+    assert (other.counts, other.seed, other.param_groups[0]["lr"]) == ([[3, 2]], 7, 0.25)
+    assert all(torch.equal(v, moments[k]) for k, v in other.lists()[0][2].buffers().items())
